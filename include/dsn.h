@@ -51,6 +51,10 @@ enum dsn_dtype { DSN_F32 = 0, DSN_BF16 = 1 };
 enum dsn_act { DSN_ACT_NONE = 0, DSN_ACT_RELU = 1, DSN_ACT_GELU = 2 };
 enum dsn_order { DSN_INPUT_ORDER = 0, DSN_GROUPED = 1 };
 enum dsn_tail { DSN_TAIL_UNTOUCHED = 0, DSN_TAIL_ZERO = 1 };
+/* Frequencies of rotary positions: one ladder over all pairs of a head, or one ladder for each axis. */
+enum dsn_rotary_ladder { DSN_ROTARY_SHARED = 0, DSN_ROTARY_PER_AXIS = 1 };
+/* Which elements of a head turn together: (i, i + pairs) or (2 i, 2 i + 1). */
+enum dsn_rotary_pairing { DSN_ROTARY_HALVES = 0, DSN_ROTARY_INTERLEAVED = 1 };
 enum dsn_layer_kind { DSN_LAYER_LINEAR = 0, DSN_LAYER_CONV = 1, DSN_LAYER_ATTENTION = 2, DSN_LAYER_DEPTHWISE = 3 };
 
 #define DSN_MAX_SLICES 64   /* largest T                                               */
@@ -169,6 +173,79 @@ typedef struct dsn_attention_desc {
   int32_t order;        /* dsn_order of qkv and out                                      */
 } dsn_attention_desc;
 
+/* Pre-norm of a transformer block on elastic widths, with the residual's addition before it and 8-bit codes behind it
+ * (not in the paper, whose blocks are evaluated in one precision).  A row of a sample of path t has k[t] columns:
+ *   h = x + residual                                     (fp32; h = x without a residual)
+ *   n = h / sqrt(mean_c h^2 + eps) * weight              (fp32)
+ *   s = max_c |n| / 127,   q = round(n / s) to the nearest, ties to even, in -127 .. 127   (an all-zero row: s = 0, q = 0)
+ * The code is computed as round(h weight * (127 / max|h weight|)) in fp32, each operation rounded once: the factor that
+ * all columns share drops out, so a code does not depend on the order of the sum of squares.
+ * A row that holds a NaN or an infinity comes out as s = NaN, q = 0, y = NaN; squares that overflow fp32 do not. */
+typedef struct dsn_norm_desc {
+  int32_t dtype;        /* DSN_BF16 or DSN_F32: x, residual, sum, y                      */
+  int32_t R;            /* rows per sample                                               */
+  int32_t C;            /* full width, 1..32767                                          */
+  int64_t ldx, ld_res, ld_sum, ldy; /* elements between rows of x, residual, sum, y: multiples of 16 bytes, >= C */
+  int64_t ldq;          /* bytes between rows of q: a multiple of 16, >= C               */
+  int32_t T;
+  const int32_t* k;     /* host [T], 1..C                                                */
+  const float* weight;  /* device [C], 16-byte aligned, or NULL (all ones)               */
+  float eps;            /* 1e-20 or more, finite                                         */
+  int32_t in_order;     /* dsn_order of x, residual and sum (the stream keeps its order) */
+  int32_t out_order;    /* dsn_order of q, q_scale and y: the gather to grouped order is part of the pass */
+} dsn_norm_desc;
+
+/* Sliced linear layer on 8-bit integers with a scale for every row of x and for every output channel:
+ *   y[i][r][o] = act((sum_{c < k_in[t]} x[i][r][c] W[o][c]) * x_scale[i][r] * w_scale[o] + bias[o] ...),  o < k_out[t],
+ * the products summed exactly in 32-bit integers; everything behind the sum as in dsn_linear_desc, in fp32. */
+typedef struct dsn_linear_i8_desc {
+  int32_t R;
+  int32_t C_in, C_out;
+  int64_t ldx, ldw;     /* bytes between rows of x, W: multiples of 16, >= C_in          */
+  int64_t ldy;          /* elements between rows of y and residual: a multiple of 16 bytes, >= C_out */
+  int32_t T;
+  const int32_t* k_in;  /* host [T], 1..C_in                                             */
+  const int32_t* k_out; /* host [T], 1..C_out                                            */
+  const int8_t* W;      /* device [C_out][ldw], 16-byte aligned                          */
+  const float* w_scale; /* device [C_out]                                                */
+  const float* bias;    /* device [C_out] or NULL                                        */
+  const float* bn_scale;/* device [T][C_out] or NULL, as in dsn_linear_desc              */
+  const float* bn_shift;
+  const void* residual; /* as in dsn_linear_desc: y's type, order and leading dimension  */
+  int32_t y_dtype;      /* DSN_BF16 or DSN_F32: y and residual                           */
+  int32_t act;          /* DSN_ACT_GELU: the fitted form for bf16 outputs, the erf form itself for fp32 outputs */
+  int32_t in_order;     /* dsn_order of x and x_scale                                    */
+  int32_t out_order;    /* dsn_order of y and residual                                   */
+  int32_t tail;
+} dsn_linear_i8_desc;
+
+/* Rotary positions with one to three axes (time, height, width of image and video tokens; one axis: text).
+ * A row holds H heads of `vectors` vectors of D elements each, of which the first `rotated` turn: vectors = 3, rotated = 2 is
+ * the [head][q|k|v][D_h] layout of the sliced attention core, vectors = 1 a plain row of heads.  The first
+ * 2 * (pairs[0] + pairs[1] + pairs[2]) elements of a vector turn, in P = pairs[0] + ... pairs; the first pairs[0] of them follow
+ * axis 0, the next pairs[1] axis 1, the rest axis 2:
+ *   angle(i) = position[axis(i)] * base^(-e),   e = i / P (DSN_ROTARY_SHARED) or j / pairs[axis], j counted inside the axis
+ *   (u, v) -> (u cos - v sin, u sin + v cos)
+ * Angles are reduced modulo a full turn in 64-bit fixed point, so they stay exact for every 32-bit position.  `inverse` turns
+ * back, which is also the gradient with respect to the input.  Heads >= heads[t] of a sample of path t are neither read nor written. */
+typedef struct dsn_rotary_desc {
+  int32_t dtype;        /* DSN_BF16 or DSN_F32                                           */
+  int32_t N;            /* rows (tokens) per sample                                      */
+  int32_t H, D;         /* full head count 1..4096, elements per vector 2..256           */
+  int32_t vectors, rotated; /* 1..8 vectors per head, of which the first 1..vectors turn */
+  int64_t ldx, ldy;     /* elements between rows, >= H * vectors * D                     */
+  int32_t T;
+  const int32_t* heads; /* host [T]: head count of each path, 1..H                       */
+  int32_t order;        /* dsn_order of x and y                                          */
+  int32_t n_axes;       /* 1..3                                                          */
+  int32_t pairs[3];     /* pairs that follow each axis, >= 1 for the axes used; 2 * their sum <= D */
+  int32_t ladder;       /* dsn_rotary_ladder                                             */
+  int32_t pairing;      /* dsn_rotary_pairing                                            */
+  double base;          /* > 1, finite                                                   */
+  int32_t shared_positions; /* 1: positions [n_axes][N], the same for every sample; 0: [n_axes][B * N], in the order of x's rows */
+  int32_t inverse;      /* 1: turn by the negative angle                                 */
+} dsn_rotary_desc;
+
 /* One dynamic block: optional gate, routing, then up to DSN_MAX_CHAIN layers that all inherit
  * the block's routing (Sec. 5, "inherit the control signal").  Layer j reads layer j-1's output;
  * layer 0 reads x in input order, the last layer writes y in input order; intermediate
@@ -246,6 +323,10 @@ typedef struct dsn_stats {
   uint64_t launches_copy;         /* gather / scatter, zero fill, channel scaling, Re-SBN folding          */
   uint64_t map_hits, map_misses;  /* tensor-map cache                                                      */
   uint64_t launches_gemm_chain_tmem; /* of launches_gemm_chain: last layer fed from tensor memory          */
+  uint64_t launches_norm;         /* residual + norm + 8-bit codes                                         */
+  uint64_t launches_gemm_i8;      /* 8-bit linear layers on the tensor cores, CTA pairs                    */
+  uint64_t launches_rows_i8;      /* 8-bit linear layers of a few rows                                     */
+  uint64_t launches_rotary;
 } dsn_stats;
 int dsn_get_stats(dsn_ctx* ctx, dsn_stats* out);
 
@@ -342,6 +423,26 @@ int dsn_sliced_depthwise(dsn_ctx* ctx, const dsn_depthwise_desc* d, const dsn_ro
  * second contraction, bf16 output. */
 int dsn_sliced_attention(dsn_ctx* ctx, const dsn_attention_desc* d, const dsn_routing* r, const void* qkv,
                          void* out, void* stream);
+
+/* ---- transformer blocks in 8 bits -------------------------------------------------------- */
+/* x, residual (or NULL), sum (or NULL: h in x's type is not wanted): rows in d->in_order.  q with q_scale (device float, one per
+ * row), both or neither; y (or NULL) in x's type: the values that the codes stand for, q * s, where q is given, else n itself.
+ * At least one of sum, q, y is given.  sum may be x or residual itself (same leading dimension); q and y overlap nothing else.
+ * Columns >= k[t] of every output keep what they held.  All row pointers 16-byte aligned. */
+int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r, const void* x, const void* residual,
+                      void* sum, int8_t* q, float* q_scale, void* y, void* stream);
+
+/* x: device int8, 16-byte aligned, rows as d->in_order says; x_scale: device float [B * R] in the same order of rows.
+ * workspace: device, 16-byte aligned, >= dsn_linear_i8_workspace_bytes (0 for most calls: it holds the rows of short samples
+ * that arrive in input order, gathered). */
+size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B);
+int dsn_sliced_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const dsn_routing* r, const int8_t* x,
+                         const float* x_scale, void* y, void* workspace, size_t ws_bytes, void* stream);
+
+/* positions: device int32, any values.  y may be x itself (same leading dimension): then only the turned elements are written;
+ * otherwise the heads of a sample's path are written whole, the vectors and elements that do not turn copied. */
+int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r, const int32_t* positions, const void* x,
+                    void* y, void* stream);
 
 /* ---- whole dynamic block (Eq. (dyn_net)) ------------------------------------------------ */
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L);

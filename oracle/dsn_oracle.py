@@ -362,3 +362,65 @@ def vit_mlp(x, Wfc1, Wfc2, idx, paths, mirror_bf16=True, samples=None):
 def executed_macs(idx, R, k_in, k_out, K=1):
     """Multiply-adds actually executed: sum_i R * k_in[t_i] * k_out[t_i] * K*K."""
     return int(sum(R * int(k_in[int(t)]) * int(k_out[int(t)]) * K * K for t in idx))
+
+
+# --------------------------------------------------------------------------- transformer blocks in 8 bits
+def rmsnorm_quant(x, idx, k, weight=None, eps=1e-6, residual=None):
+    """Residual + root-mean-square norm on the leading k[t] columns, and what the 8-bit codes round.
+
+    x, residual [B][R][C].  Returns h (the sum), n (the normalised row), scale [B][R] = max|n| / 127 and
+    steps = n / scale (0 where the row is all zero), before rounding to a code; NaN outside the slices.
+    """
+    h = np.full(np.shape(x), np.nan, dtype=F64)
+    n, steps = h.copy(), h.copy()
+    scale = np.zeros(np.shape(x)[:2], dtype=F64)
+    for i in range(x.shape[0]):
+        c = int(k[int(idx[i])])
+        row = np.asarray(x[i, :, :c], dtype=F64)
+        if residual is not None:
+            row = row + np.asarray(residual[i, :, :c], dtype=F64)
+        h[i, :, :c] = row
+        v = row / np.sqrt(np.mean(row * row, axis=-1, keepdims=True) + eps)
+        if weight is not None:
+            v = v * np.asarray(weight[:c], dtype=F64)
+        n[i, :, :c] = v
+        top = np.max(np.abs(v), axis=-1)
+        scale[i] = top / 127.0
+        steps[i, :, :c] = np.where(top[:, None] > 0, 127.0 * v / np.where(top > 0, top, 1.0)[:, None], 0.0)
+    return h, n, scale, steps
+
+
+def linear_i8(x, sx, W, sw, idx, k_in, k_out, bias=None, act=ACT_NONE, bn=None, residual=None, fill=np.nan):
+    """Sliced linear layer on integer rows and weights with a scale per row and per output channel."""
+    y = np.full((x.shape[0], x.shape[1], W.shape[0]), fill, dtype=F64)
+    for i in range(x.shape[0]):
+        t = int(idx[i])
+        ci, co = int(k_in[t]), int(k_out[t])
+        s = np.asarray(x[i, :, :ci], dtype=F64) @ np.asarray(W[:co, :ci], dtype=F64).T   # integers below 2^53: exact
+        z = s * np.asarray(sx[i], dtype=F64)[:, None] * np.asarray(sw[:co], dtype=F64)
+        if bias is not None:
+            z = z + np.asarray(bias[:co], dtype=F64)
+        if bn is not None:
+            z = z * np.asarray(bn[0][t][:co], dtype=F64) + np.asarray(bn[1][t][:co], dtype=F64)
+        if residual is not None:
+            z = z + np.asarray(residual[i, :, :co], dtype=F64)
+        y[i, :, :co] = activation(z, act)
+    return y
+
+
+def rotary_axes(x, positions, pairs, base=10000.0, per_axis=False, interleaved=False, inverse=False):
+    """Turns the leading 2 * sum(pairs) elements of the vectors x [..., D]; positions [axes][...] one per vector."""
+    y = np.array(x, dtype=F64)
+    P = sum(pairs)
+    i = 0
+    for a, n in enumerate(pairs):
+        for j in range(n):
+            angle = np.asarray(positions[a], dtype=F64) * base ** -((j / n) if per_axis else (i / P))
+            if inverse:
+                angle = -angle
+            u, v = (2 * i, 2 * i + 1) if interleaved else (i, i + P)
+            xu, xv = np.asarray(x[..., u], dtype=F64), np.asarray(x[..., v], dtype=F64)
+            y[..., u] = xu * np.cos(angle) - xv * np.sin(angle)
+            y[..., v] = xu * np.sin(angle) + xv * np.cos(angle)
+            i += 1
+    return y

@@ -5,5 +5,6 @@ There is no CPU or framework fallback: calling any compute entry point without t
 CUDA library raises ImportError.
 """
 from .binding import *  # noqa: F401,F403
-from .binding import (Context, DsnError, EXPORTS, LIB_PATH, Routing, GateDesc, LinearDesc, ConvDesc, LayerDesc, AttentionDesc, DepthwiseDesc, Stats,
+from .binding import (Context, DsnError, EXPORTS, LIB_PATH, Routing, GateDesc, LinearDesc, ConvDesc, LayerDesc, AttentionDesc, DepthwiseDesc, NormDesc,
+                      LinearI8Desc, RotaryDesc, Stats,
                       load_library)

@@ -20,6 +20,8 @@ F32, BF16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 INPUT_ORDER, GROUPED = 0, 1
 TAIL_UNTOUCHED, TAIL_ZERO = 0, 1
+ROTARY_SHARED, ROTARY_PER_AXIS = 0, 1
+ROTARY_HALVES, ROTARY_INTERLEAVED = 0, 1
 LAYER_LINEAR, LAYER_CONV, LAYER_ATTENTION, LAYER_DEPTHWISE = 0, 1, 2, 3
 MAX_SLICES, MAX_GROUPS, MAX_CHAIN = 64, 4096, 6
 
@@ -28,6 +30,7 @@ EXPORTS = [
     "dsn_executed_macs", "dsn_gate_workspace_bytes", "dsn_gate", "dsn_gate_static", "dsn_gate_attention", "dsn_scale_channels", "dsn_resbn_fold", "dsn_route", "dsn_permute_rows",
     "dsn_sliced_attention", "dsn_sliced_depthwise", "dsn_linear_workspace_bytes", "dsn_conv_workspace_bytes", "dsn_sliced_linear", "dsn_sliced_conv",
     "dsn_layer_workspace_bytes", "dsn_layer_forward",
+    "dsn_rmsnorm_quant", "dsn_linear_i8_workspace_bytes", "dsn_sliced_linear_i8", "dsn_rotary_axes",
 ]
 
 
@@ -78,11 +81,33 @@ class DepthwiseDesc(C.Structure):
                 ("out_order", C.c_int32)]
 
 
+class NormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("R", C.c_int32), ("C", C.c_int32), ("ldx", C.c_int64), ("ld_res", C.c_int64),
+                ("ld_sum", C.c_int64), ("ldy", C.c_int64), ("ldq", C.c_int64), ("T", C.c_int32), ("k", C.POINTER(C.c_int32)),
+                ("weight", C.c_void_p), ("eps", C.c_float), ("in_order", C.c_int32), ("out_order", C.c_int32)]
+
+
+class LinearI8Desc(C.Structure):
+    _fields_ = [("R", C.c_int32), ("C_in", C.c_int32), ("C_out", C.c_int32), ("ldx", C.c_int64), ("ldw", C.c_int64),
+                ("ldy", C.c_int64), ("T", C.c_int32), ("k_in", C.POINTER(C.c_int32)), ("k_out", C.POINTER(C.c_int32)),
+                ("W", C.c_void_p), ("w_scale", C.c_void_p), ("bias", C.c_void_p), ("bn_scale", C.c_void_p), ("bn_shift", C.c_void_p),
+                ("residual", C.c_void_p), ("y_dtype", C.c_int32), ("act", C.c_int32), ("in_order", C.c_int32),
+                ("out_order", C.c_int32), ("tail", C.c_int32)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("N", C.c_int32), ("H", C.c_int32), ("D", C.c_int32), ("vectors", C.c_int32),
+                ("rotated", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64), ("T", C.c_int32), ("heads", C.POINTER(C.c_int32)),
+                ("order", C.c_int32), ("n_axes", C.c_int32), ("pairs", C.c_int32 * 3), ("ladder", C.c_int32), ("pairing", C.c_int32),
+                ("base", C.c_double), ("shared_positions", C.c_int32), ("inverse", C.c_int32)]
+
+
 class Stats(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("calls", "launches", "launches_gemm_pair", "launches_gemm_halo", "launches_gemm_chain",
                                           "launches_gemm_one_cta", "launches_linear_f32", "launches_attention",
                                           "launches_depthwise", "launches_dwpw", "launches_gate", "launches_route",
-                                          "launches_copy", "map_hits", "map_misses", "launches_gemm_chain_tmem")]
+                                          "launches_copy", "map_hits", "map_misses", "launches_gemm_chain_tmem",
+                                          "launches_norm", "launches_gemm_i8", "launches_rows_i8", "launches_rotary")]
 
 
 class LayerDesc(C.Structure):
@@ -135,6 +160,11 @@ def load_library():
     lib.dsn_layer_workspace_bytes.argtypes = [C.POINTER(LayerDesc)]
     lib.dsn_layer_workspace_bytes.restype = sz
     lib.dsn_layer_forward.argtypes = [vp, C.POINTER(LayerDesc), vp, vp, vp, C.POINTER(Routing), vp, vp, sz, vp]
+    lib.dsn_rmsnorm_quant.argtypes = [vp, C.POINTER(NormDesc), C.POINTER(Routing), vp, vp, vp, vp, vp, vp, vp]
+    lib.dsn_linear_i8_workspace_bytes.argtypes = [C.POINTER(LinearI8Desc), i32]
+    lib.dsn_linear_i8_workspace_bytes.restype = sz
+    lib.dsn_sliced_linear_i8.argtypes = [vp, C.POINTER(LinearI8Desc), C.POINTER(Routing), vp, vp, vp, vp, sz, vp]
+    lib.dsn_rotary_axes.argtypes = [vp, C.POINTER(RotaryDesc), C.POINTER(Routing), vp, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("dsn_strerror", "dsn_executed_macs") and not name.endswith("workspace_bytes"):
@@ -185,6 +215,7 @@ class Context:
 
     def __init__(self, device: int = 0):
         self.lib = load_library()
+        self.device = device
         self.handle = C.c_void_p()
         _check(self.lib.dsn_create(C.byref(self.handle), device), "dsn_create")
 
@@ -370,3 +401,109 @@ def dsn_layer_forward(ctx: Context, L: LayerDesc, x, idx_in, y, workspace, r_out
     _check(ctx.lib.dsn_layer_forward(ctx.handle, C.byref(L), _ptr(x), _ptr(idx_in), _ptr(y),
                                      C.byref(r_out) if r_out is not None else None, _ptr(idx_out), _ptr(workspace),
                                      ws_bytes, _stream_handle(stream)), "dsn_layer_forward")
+
+
+# ---- transformer blocks in 8 bits.  These calls also check what a pointer cannot say: type, device and extent of every tensor.
+
+def _torch_dtype(code: int):
+    import torch
+    return {F32: torch.float32, BF16: torch.bfloat16}.get(code)
+
+
+def _buf(what: str, t, dtype, need: int, device: Optional[int] = None, rows: bool = False) -> Optional[int]:
+    """Pointer of a device tensor of this type with at least `need` elements: dense, or (rows) from its first one to its storage's end,
+    as rows with a leading dimension lie."""
+    if t is None:
+        return None
+    at = t.get_device()
+    if t.dtype is not dtype or at < 0 or (device is not None and at != device):
+        raise DsnError(ERR_INVALID_ARG, f"{what}: {t.dtype} on {t.device}, expected {dtype} on cuda" + ("" if device is None else f":{device}"))
+    if t.numel() < need and not (rows and t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() >= need):
+        raise DsnError(ERR_INVALID_ARG, f"{what}: {t.numel()} elements, at least {need} are read or written")
+    if not rows and not t.is_contiguous():
+        raise DsnError(ERR_INVALID_ARG, f"{what}: not contiguous")
+    return t.data_ptr()
+
+
+def _span(rows: int, ld: int, width: int) -> int:
+    return (rows - 1) * ld + width if rows > 0 else 0
+
+
+def make_norm_desc(dtype, R, Cn, k, weight=None, eps=1e-6, ldx=None, ld_res=None, ld_sum=None, ldq=None, ldy=None,
+                   in_order=INPUT_ORDER, out_order=INPUT_ORDER) -> NormDesc:
+    """Residual + root-mean-square norm + 8-bit codes; leading dimensions default to Cn."""
+    import torch
+    _buf("weight", weight, torch.float32, Cn)
+    ka = _i32_array(k)
+    d = NormDesc(dtype, R, Cn, *(Cn if v is None else v for v in (ldx, ld_res, ld_sum, ldy, ldq)), len(k), ka, _ptr(weight), eps,
+                 in_order, out_order)
+    d._keep = (ka, weight)
+    return d
+
+
+def dsn_rmsnorm_quant(ctx: Context, d: NormDesc, routing: Routing, x, q=None, scale=None, y=None, residual=None, sum_out=None, stream=None):
+    import torch
+    dt, rows, dev = _torch_dtype(d.dtype), routing.B * d.R, ctx.device
+    _check(ctx.lib.dsn_rmsnorm_quant(ctx.handle, C.byref(d), C.byref(routing), _buf("x", x, dt, _span(rows, d.ldx, d.C), dev, True),
+                                     _buf("residual", residual, dt, _span(rows, d.ld_res, d.C), dev, True),
+                                     _buf("sum_out", sum_out, dt, _span(rows, d.ld_sum, d.C), dev, True),
+                                     _buf("q", q, torch.int8, _span(rows, d.ldq, d.C), dev, True), _buf("scale", scale, torch.float32, rows, dev),
+                                     _buf("y", y, dt, _span(rows, d.ldy, d.C), dev, True), _stream_handle(stream)), "dsn_rmsnorm_quant")
+
+
+def make_linear_i8_desc(R, C_in, C_out, k_in, k_out, W, w_scale, bias=None, bn_scale=None, bn_shift=None, residual=None, y_dtype=BF16,
+                        act=ACT_NONE, in_order=INPUT_ORDER, out_order=INPUT_ORDER, tail=TAIL_UNTOUCHED, ldx=None, ldw=None,
+                        ldy=None) -> LinearI8Desc:
+    """Linear layer on int8 rows and weights; leading dimensions default to the extents."""
+    import torch
+    ldx, ldw, ldy = C_in if ldx is None else ldx, C_in if ldw is None else ldw, C_out if ldy is None else ldy
+    f = torch.float32
+    _buf("W", W, torch.int8, _span(C_out, ldw, C_in), rows=True)
+    for what, t, n in (("w_scale", w_scale, C_out), ("bias", bias, C_out), ("bn_scale", bn_scale, len(k_out) * C_out),
+                       ("bn_shift", bn_shift, len(k_out) * C_out)):
+        _buf(what, t, f, n)
+    ki, ko = _i32_array(k_in), _i32_array(k_out)
+    d = LinearI8Desc(R, C_in, C_out, ldx, ldw, ldy, len(k_in), ki, ko, _ptr(W), _ptr(w_scale), _ptr(bias), _ptr(bn_scale), _ptr(bn_shift),
+                     _ptr(residual), y_dtype, act, in_order, out_order, tail)
+    d._keep = (ki, ko, W, w_scale, bias, bn_scale, bn_shift, residual)
+    return d
+
+
+def dsn_linear_i8_workspace_bytes(d: LinearI8Desc, B: int) -> int:
+    return int(load_library().dsn_linear_i8_workspace_bytes(C.byref(d), B))
+
+
+def dsn_sliced_linear_i8(ctx: Context, d: LinearI8Desc, routing: Routing, x, x_scale, y, workspace=None, stream=None):
+    import torch
+    dt, rows, dev = _torch_dtype(d.y_dtype), routing.B * d.R, ctx.device
+    span = _span(rows, d.ldy, d.C_out)
+    _buf("residual", d._keep[-1], dt, span, dev, True)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is not None and workspace.get_device() != dev:
+        raise DsnError(ERR_INVALID_ARG, f"workspace on {workspace.device}, expected cuda:{dev}")
+    _check(ctx.lib.dsn_sliced_linear_i8(ctx.handle, C.byref(d), C.byref(routing), _buf("x", x, torch.int8, _span(rows, d.ldx, d.C_in), dev, True),
+                                        _buf("x_scale", x_scale, torch.float32, rows, dev), _buf("y", y, dt, span, dev, True), _ptr(workspace),
+                                        ws_bytes, _stream_handle(stream)), "dsn_sliced_linear_i8")
+
+
+def make_rotary_desc(dtype, N, H, D, heads, pairs, vectors=3, rotated=2, base=10000.0, ladder=ROTARY_SHARED, pairing=ROTARY_HALVES,
+                     shared_positions=True, inverse=False, order=INPUT_ORDER, ldx=None, ldy=None) -> RotaryDesc:
+    """Rotary positions; `pairs` lists the pairs of elements that follow each axis (one to three axes)."""
+    hs = _i32_array(heads)
+    if not 1 <= len(pairs) <= 3:
+        raise DsnError(ERR_INVALID_ARG, f"make_rotary_desc: {len(pairs)} axes")
+    row = H * vectors * D
+    d = RotaryDesc(dtype, N, H, D, vectors, rotated, row if ldx is None else ldx, row if ldy is None else ldy, len(heads), hs, order,
+                   len(pairs), (C.c_int32 * 3)(*pairs), ladder, pairing, base, int(shared_positions), int(inverse))
+    d._keep = (hs,)
+    return d
+
+
+def dsn_rotary_axes(ctx: Context, d: RotaryDesc, routing: Routing, positions, x, y, stream=None):
+    import torch
+    dt, rows, dev = _torch_dtype(d.dtype), routing.B * d.N, ctx.device
+    row = d.H * d.vectors * d.D
+    _check(ctx.lib.dsn_rotary_axes(ctx.handle, C.byref(d), C.byref(routing),
+                                   _buf("positions", positions, torch.int32, d.n_axes * (d.N if d.shared_positions else rows), dev),
+                                   _buf("x", x, dt, _span(rows, d.ldx, row), dev, True), _buf("y", y, dt, _span(rows, d.ldy, row), dev, True),
+                                   _stream_handle(stream)), "dsn_rotary_axes")

@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include "dsn_internal.cuh"
+#include "dsn_transformer.cuh"
 
 int dsn_pdl_enabled() {
   static int enabled = -1;
@@ -45,15 +46,17 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline cudaStream_t as_stream(void* s) { return static_cast<cudaStream_t>(s); }
 
-// bf16 tensor map of rank `rank` (3 or 4); dims/strides innermost first, strides[0] implied.
+// Tensor map of rank `rank` (2 to 4) over bf16 elements unless said otherwise; dims/strides innermost first, strides[0] implied.
 int encode_map(dsn_ctx* ctx, CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
-               const uint64_t* strides_bytes /* rank-1 */, const uint32_t* box) {
+               const uint64_t* strides_bytes /* rank-1 */, const uint32_t* box,
+               CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
   dsn_map_slot* slot = nullptr;
   dsn_map_key key;
   if (ctx->map_cache) {
     memset(&key, 0, sizeof(key));
     key.base = base;
     key.rank = (uint32_t)rank;
+    key.type = (uint32_t)type;
     for (int i = 0; i < rank; ++i) { key.dims[i] = dims[i]; key.box[i] = box[i]; }
     for (int i = 0; i + 1 < rank; ++i) key.strides[i] = strides_bytes[i];
     uint64_t h = 1469598103934665603ull;  // FNV-1a over the key
@@ -85,7 +88,7 @@ int encode_map(dsn_ctx* ctx, CUtensorMap* out, const void* base, int rank, const
     if (gs[i] % 16 != 0 || gs[i] == 0) return DSN_ERR_ALIGNMENT;
   }
   CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
-      out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gd, gs, bx, es,
+      out, type, (cuuint32_t)rank, const_cast<void*>(base), gd, gs, bx, es,
       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return DSN_ERR_CUDA;
@@ -310,15 +313,16 @@ int fill_gemm_maps(dsn_ctx* ctx, const LayerCall& c, const dsn_routing* r, const
   return DSN_OK;
 }
 
-// resident CTA pairs for this n-tile width (0: no pair can be resident, use one CTA per tile)
-int pair_clusters_for(dsn_ctx* ctx, int BN) {
-  if (ctx->gemm_mode != 0) return 0;
+// CTA pairs that can be resident at once for this n-tile width
+int resident_pairs(dsn_ctx* ctx, int BN) {
   const int bn_slot = BN == 256 ? 2 : (BN == 128 ? 1 : 0);
   if (ctx->pair_clusters[bn_slot] < 0) ctx->pair_clusters[bn_slot] = dsn_gemm_pair_max_clusters(227 * 1024);
   int clusters = ctx->pair_clusters[bn_slot];
   if (clusters > ctx->sm_count / 2) clusters = ctx->sm_count / 2;
   return clusters;
 }
+// the same where the context uses pairs at all (0: one CTA per tile)
+int pair_clusters_for(dsn_ctx* ctx, int BN) { return ctx->gemm_mode != 0 ? 0 : resident_pairs(ctx, BN); }
 
 int run_bf16(dsn_ctx* ctx, const LayerCall& c, const dsn_routing* r, const void* x, void* y, cudaStream_t s) {
   GemmParams p;
@@ -624,6 +628,213 @@ int check_gate(const dsn_gate_desc* g) {
     return DSN_ERR_INVALID_ARG;
   if ((size_t)4 * ((size_t)g->T * (g->C_mlp + 32) + 8 * (size_t)g->C_mlp + 8 * DSN_MAX_SLICES) > 200 * 1024)
     return DSN_ERR_UNSUPPORTED;  // score kernel stages W2 in shared memory
+  return DSN_OK;
+}
+
+// ------------------------------------------------------------------ transformer blocks in 8 bits
+bool valid_order(int o) { return o == DSN_INPUT_ORDER || o == DSN_GROUPED; }
+inline int elem_bytes(int dtype) { return dtype == DSN_BF16 ? 2 : 4; }
+constexpr int64_t kMaxRows = 0x7fffff00LL;  // row numbers, rounded up to whole tiles, stay in 32 bits
+
+// a row pointer and its leading dimension: 16-byte rows, at least `width` elements apart
+int check_rows(const void* base, int64_t ld, int64_t width, int elem) {
+  if (ld < width || ld > (1LL << 40)) return DSN_ERR_INVALID_ARG;
+  if (!aligned16(base) || (ld * elem) % 16) return DSN_ERR_ALIGNMENT;
+  return DSN_OK;
+}
+
+int check_norm(const dsn_norm_desc* d, const dsn_routing* r) {
+  if (!d || !d->k) return DSN_ERR_INVALID_ARG;
+  if (d->dtype != DSN_BF16 && d->dtype != DSN_F32) return DSN_ERR_INVALID_ARG;
+  if (d->R < 1 || d->C < 1 || d->C > 32767 || d->T < 1 || d->T > DSN_MAX_SLICES) return DSN_ERR_INVALID_ARG;
+  if (!(d->eps >= 1e-20f) || !(d->eps < INFINITY)) return DSN_ERR_INVALID_ARG;
+  if (!valid_order(d->in_order) || !valid_order(d->out_order)) return DSN_ERR_INVALID_ARG;
+  for (int t = 0; t < d->T; ++t)
+    if (d->k[t] < 1 || d->k[t] > d->C) return DSN_ERR_INVALID_ARG;
+  const int e = check_routing(r, d->T);
+  if (e) return e;
+  if ((int64_t)r->B * d->R > kMaxRows) return DSN_ERR_INVALID_ARG;
+  if (d->weight && !aligned16(d->weight)) return DSN_ERR_ALIGNMENT;
+  return DSN_OK;
+}
+
+LayerCall from_linear_i8(const dsn_linear_i8_desc* d) {
+  LayerCall c;
+  memset(&c, 0, sizeof(c));
+  c.dtype = d->y_dtype;
+  c.H = 1; c.W = d->R; c.K = 1;
+  c.C_in = d->C_in; c.C_out = d->C_out;
+  c.ldx = d->ldx; c.ldy = d->ldy;
+  c.w_row = d->ldw; c.w_tap = d->ldw;
+  c.T = d->T; c.k_in = d->k_in; c.k_out = d->k_out;
+  c.Wt = d->W; c.bias = d->bias; c.bn_scale = d->bn_scale; c.bn_shift = d->bn_shift; c.residual = d->residual;
+  c.R_in = d->R;
+  c.act = d->act; c.in_order = d->in_order; c.out_order = d->out_order; c.tail = d->tail;
+  return c;
+}
+
+int check_linear_i8(const dsn_linear_i8_desc* d) {
+  if (!d || !d->W || !d->w_scale) return DSN_ERR_INVALID_ARG;
+  if (d->R < 1 || d->C_in < 1 || d->C_in > 32767 || d->C_out < 1 || d->C_out > 32767) return DSN_ERR_INVALID_ARG;
+  if (d->y_dtype != DSN_BF16 && d->y_dtype != DSN_F32) return DSN_ERR_INVALID_ARG;
+  if (d->act < DSN_ACT_NONE || d->act > DSN_ACT_GELU || !valid_order(d->in_order) || !valid_order(d->out_order) ||
+      (d->tail != DSN_TAIL_UNTOUCHED && d->tail != DSN_TAIL_ZERO))
+    return DSN_ERR_INVALID_ARG;
+  if ((d->bn_scale == nullptr) != (d->bn_shift == nullptr)) return DSN_ERR_INVALID_ARG;
+  int e = check_slices(d->T, d->k_in, d->k_out, d->C_in, d->C_out);
+  if (e) return e;
+  e = check_rows(d->W, d->ldw, d->C_in, 1);
+  if (e) return e;
+  if (d->residual && !aligned16(d->residual)) return DSN_ERR_ALIGNMENT;
+  return DSN_OK;
+}
+
+// Rows that arrive in input order are tiled sample by sample (a sample's place is known only on the device), and the last
+// tile of each sample is filled up with zero rows.  Where that padding costs more products than a pass that gathers
+// the rows costs traffic, the rows are gathered first.
+bool linear_i8_gathers(const dsn_linear_i8_desc* d, int64_t B) {
+  if (d->in_order != DSN_INPUT_ORDER || B * d->R <= DSN_ROWS_I8_MAX || B < 2) return false;
+  return d->R <= 64;
+}
+
+// Tensor maps for the next DSN_GEMM_MAX_MAPS distinct slices not yet done (bytes; 128 of them a chunk).
+int fill_i8_maps(dsn_ctx* ctx, const LayerCall& c, const dsn_routing* r, const void* x, int64_t ldx, void* y, GemmParams& p,
+                 int* done, int& remaining) {
+  const GemmGeom& g = p.g;
+  int nmaps = 0;
+  int map_k[DSN_GEMM_MAX_MAPS], map_n[DSN_GEMM_MAX_MAPS];
+  memset(p.map_id, 0xFF, sizeof(p.map_id));
+  for (int t = 0; t < c.T; ++t) {
+    if (done[t]) continue;
+    int id = -1;
+    for (int m = 0; m < nmaps; ++m)
+      if (map_k[m] == c.k_in[t] && map_n[m] == c.k_out[t]) id = m;
+    if (id < 0) {
+      if (nmaps == DSN_GEMM_MAX_MAPS) continue;  // next launch
+      id = nmaps++;
+      map_k[id] = c.k_in[t];
+      map_n[id] = c.k_out[t];
+    }
+    p.map_id[t] = (uint8_t)id;
+    done[t] = 1;
+    --remaining;
+  }
+  const int es = elem_bytes(c.dtype), whole = 16 / es;
+  for (int m = 0; m < nmaps; ++m) {
+    const uint64_t kv = (uint64_t)map_k[m], ld = (uint64_t)ldx;
+    int e;
+    if (g.flat) {
+      const uint64_t rows = (uint64_t)r->B * g.R;
+      const uint64_t dims[4] = {kv, rows, 1, 1}, str[3] = {ld, ld * rows, ld * rows};
+      const uint32_t box[4] = {128, DSN_GEMM_BM, 1, 1};
+      e = encode_map(ctx, &p.mapA[m], x, 4, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8);
+    } else {
+      const uint64_t dims[4] = {kv, (uint64_t)g.W, 1, (uint64_t)r->B}, str[3] = {ld, ld * g.W, ld * g.W};
+      const uint32_t box[4] = {128, (uint32_t)g.bw, 1, (uint32_t)g.nb};
+      e = encode_map(ctx, &p.mapA[m], x, 4, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8);
+    }
+    if (e) return e;
+    const uint64_t wd[3] = {kv, 1, (uint64_t)map_n[m]}, ws[2] = {(uint64_t)c.w_row, (uint64_t)c.w_row};
+    const uint32_t wb[3] = {128, 1, (uint32_t)(g.BN / 2)};
+    e = encode_map(ctx, &p.mapB[m], c.Wt, 3, wd, ws, wb, CU_TENSOR_MAP_DATA_TYPE_UINT8);
+    if (e) return e;
+    // columns clipped at k_out rounded down to 16 bytes; the epilogue writes what lies beyond (widths below 8 never use the map)
+    const uint64_t yn = (uint64_t)(map_n[m] >= 8 ? map_n[m] / whole * whole : 8);
+    const uint64_t yd[2] = {yn, (uint64_t)r->B * g.R}, ys[1] = {(uint64_t)c.ldy * es};
+    const uint32_t yb[2] = {(uint32_t)(128 / es), 32};
+    e = encode_map(ctx, &p.mapY[m], y, 2, yd, ys, yb,
+                   es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+    if (e) return e;
+  }
+  return DSN_OK;
+}
+
+int run_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const LayerCall& c, const dsn_routing* r, const int8_t* x,
+                  const float* x_scale, void* y, void* workspace, size_t ws_bytes, cudaStream_t s) {
+  const int64_t rows = (int64_t)r->B * d->R;
+  const int f32 = d->y_dtype == DSN_F32;
+  if (rows <= DSN_ROWS_I8_MAX) {
+    RowsI8Params q;
+    memset(&q, 0, sizeof(q));
+    q.max_ki = q.max_ko = 1;
+    for (int t = 0; t < d->T; ++t) {
+      q.k_in[t] = (int16_t)d->k_in[t];
+      q.k_out[t] = (int16_t)d->k_out[t];
+      if (d->k_in[t] > q.max_ki) q.max_ki = d->k_in[t];
+      if (d->k_out[t] > q.max_ko) q.max_ko = d->k_out[t];
+    }
+    q.B = r->B; q.R = d->R; q.G = r->G; q.T = d->T; q.C_in = d->C_in;
+    q.in_input_order = d->in_order == DSN_INPUT_ORDER;
+    q.out_input_order = d->out_order == DSN_INPUT_ORDER;
+    q.offsets = r->offsets; q.perm = r->perm; q.group_slice = r->group_slice;
+    q.x = x; q.x_scale = x_scale; q.W = d->W; q.w_scale = d->w_scale; q.bias = d->bias;
+    q.bn_scale = d->bn_scale; q.bn_shift = d->bn_shift; q.bn_ld = d->C_out; q.act = d->act;
+    q.residual = d->residual; q.y = y; q.ldx = d->ldx; q.ldw = d->ldw; q.ldy = d->ldy;
+    count_launch(ctx, &dsn_stats::launches_rows_i8);
+    return dsn_launch_rows_i8(q, f32, s) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+  }
+  LayerCall cc = c;
+  int64_t ldx = d->ldx;
+  const void* src = x;
+  if (linear_i8_gathers(d, r->B)) {
+    SliceTable st;
+    fill_slice_table(st, c);
+    ldx = (int64_t)align_up((size_t)d->C_in, 16);
+    if (!workspace || ws_bytes < (size_t)(rows * ldx)) return DSN_ERR_WORKSPACE;
+    count_launch(ctx, &dsn_stats::launches_copy);
+    if (dsn_launch_permute_rows(st, 1, d->R, x, d->ldx, workspace, ldx, 1, r->B, r->G, r->offsets, r->perm, r->group_slice, s) !=
+        cudaSuccess)
+      return DSN_ERR_CUDA;
+    src = workspace;
+    cc.in_order = DSN_GROUPED;
+  }
+  GemmI8Params q;
+  fill_gemm_params(ctx, cc, r, y, false, q.g);
+  q.x_scale = x_scale;
+  q.w_scale = d->w_scale;
+  q.scale_input_order = d->in_order == DSN_INPUT_ORDER;
+  GemmGeom& g = q.g.g;
+  g.pair = 1;   // this layer has no one-CTA form: DSN_GEMM_MODE leaves it alone
+  const int clusters = resident_pairs(ctx, g.BN);
+  if (clusters <= 0) return DSN_ERR_UNSUPPORTED;
+  g.stages = g.BN == 256 ? 6 : 8;
+  while (g.stages > 2 && dsn_gemm_i8_smem_bytes(g.BN, g.stages, r->G) > 227 * 1024) --g.stages;
+  const size_t smem = dsn_gemm_i8_smem_bytes(g.BN, g.stages, r->G);
+  int done[DSN_MAX_SLICES];
+  memset(done, 0, sizeof(done));
+  int remaining = d->T;
+  while (remaining > 0) {
+    const int e = fill_i8_maps(ctx, cc, r, src, ldx, y, q.g, done, remaining);
+    if (e) return e;
+    count_launch(ctx, &dsn_stats::launches_gemm_i8);
+    if (dsn_launch_gemm_i8(q, f32, clusters, smem, s) != cudaSuccess) return DSN_ERR_CUDA;
+  }
+  return DSN_OK;
+}
+
+int check_rotary(const dsn_rotary_desc* d, const dsn_routing* r) {
+  if (!d || !d->heads) return DSN_ERR_INVALID_ARG;
+  if (d->dtype != DSN_BF16 && d->dtype != DSN_F32) return DSN_ERR_INVALID_ARG;
+  if (d->N < 1 || d->H < 1 || d->H > 4096 || d->D < 2 || d->D > 256) return DSN_ERR_INVALID_ARG;
+  if (d->vectors < 1 || d->vectors > 8 || d->rotated < 1 || d->rotated > d->vectors) return DSN_ERR_INVALID_ARG;
+  if (d->T < 1 || d->T > DSN_MAX_SLICES || !valid_order(d->order)) return DSN_ERR_INVALID_ARG;
+  if (d->n_axes < 1 || d->n_axes > 3) return DSN_ERR_INVALID_ARG;
+  int sum = 0;
+  for (int a = 0; a < d->n_axes; ++a) {
+    if (d->pairs[a] < 1 || d->pairs[a] > 128) return DSN_ERR_INVALID_ARG;
+    sum += d->pairs[a];
+  }
+  if (2 * sum > d->D) return DSN_ERR_INVALID_ARG;
+  if (d->ladder != DSN_ROTARY_SHARED && d->ladder != DSN_ROTARY_PER_AXIS) return DSN_ERR_INVALID_ARG;
+  if (d->pairing != DSN_ROTARY_HALVES && d->pairing != DSN_ROTARY_INTERLEAVED) return DSN_ERR_INVALID_ARG;
+  if (!(d->base > 1.0) || !(d->base < INFINITY)) return DSN_ERR_INVALID_ARG;
+  for (int t = 0; t < d->T; ++t)
+    if (d->heads[t] < 1 || d->heads[t] > d->H) return DSN_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)d->H * d->vectors * d->D;
+  if (d->ldx < row || d->ldy < row || d->ldx > (1LL << 40) || d->ldy > (1LL << 40)) return DSN_ERR_INVALID_ARG;
+  const int e = check_routing(r, d->T);
+  if (e) return e;
+  if ((int64_t)r->B * d->N > kMaxRows) return DSN_ERR_INVALID_ARG;
   return DSN_OK;
 }
 
@@ -1040,6 +1251,119 @@ int dsn_sliced_attention(dsn_ctx* ctx, const dsn_attention_desc* d, const dsn_ro
       cudaSuccess)
     return DSN_ERR_CUDA;
   return DSN_OK;
+}
+
+int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r, const void* x, const void* residual,
+                      void* sum, int8_t* q, float* q_scale, void* y, void* stream) {
+  if (!x || (!sum && !q && !y) || (q == nullptr) != (q_scale == nullptr)) return DSN_ERR_INVALID_ARG;
+  int e = check_ctx(ctx);
+  if (e) return e;
+  e = check_norm(d, r);
+  if (e) return e;
+  const int es = elem_bytes(d->dtype);
+  e = check_rows(x, d->ldx, d->C, es);
+  if (!e && residual) e = check_rows(residual, d->ld_res, d->C, es);
+  if (!e && sum) e = check_rows(sum, d->ld_sum, d->C, es);
+  if (!e && q) e = check_rows(q, d->ldq, d->C, 1);
+  if (!e && y) e = check_rows(y, d->ldy, d->C, es);
+  if (e) return e;
+  // in place only where a thread reads and writes the same elements; rows change their places on the way to q and y
+  if (sum && ((sum == x && d->ld_sum != d->ldx) || (sum == residual && d->ld_sum != d->ld_res))) return DSN_ERR_INVALID_ARG;
+  if (y && (y == x || y == residual || y == sum || y == q)) return DSN_ERR_INVALID_ARG;
+  if (q && (q == x || q == residual || q == sum)) return DSN_ERR_INVALID_ARG;
+  if (r->B == 0) return DSN_OK;
+  NormParams p;
+  memset(&p, 0, sizeof(p));
+  int max_k = 1;
+  for (int t = 0; t < d->T; ++t) {
+    p.k[t] = (int16_t)d->k[t];
+    if (d->k[t] > max_k) max_k = d->k[t];
+  }
+  p.R = d->R; p.B = r->B; p.G = r->G; p.T = d->T;
+  p.in_input_order = d->in_order == DSN_INPUT_ORDER;
+  p.out_input_order = d->out_order == DSN_INPUT_ORDER;
+  p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
+  p.x = x; p.residual = residual; p.sum = sum; p.q = q; p.scale = q_scale; p.y = y;
+  p.ldx = d->ldx; p.ld_res = d->ld_res; p.ld_sum = d->ld_sum; p.ldq = d->ldq; p.ldy = d->ldy;
+  p.weight = d->weight; p.eps = d->eps;
+  count_launch(ctx, &dsn_stats::launches_norm);
+  return dsn_launch_norm_quant(p, d->dtype == DSN_F32, max_k, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+}
+
+size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B) {
+  if (check_linear_i8(d) || B < 0 || !linear_i8_gathers(d, B)) return 0;
+  return (size_t)B * d->R * align_up((size_t)d->C_in, 16);
+}
+
+int dsn_sliced_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const dsn_routing* r, const int8_t* x,
+                         const float* x_scale, void* y, void* workspace, size_t ws_bytes, void* stream) {
+  if (!x || !x_scale || !y) return DSN_ERR_INVALID_ARG;
+  int e = check_ctx(ctx);
+  if (e) return e;
+  ++ctx->stats.calls;
+  log_call(ctx, "sliced layer (8-bit linear)", r ? r->B : -1, d ? d->T : -1);
+  e = check_linear_i8(d);
+  if (!e) e = check_routing(r, d->T);
+  if (!e) e = check_rows(x, d->ldx, d->C_in, 1);
+  if (!e) e = check_rows(y, d->ldy, d->C_out, elem_bytes(d->y_dtype));
+  if (e) return e;
+  if (d->residual == y || (int64_t)r->B * d->R > kMaxRows) return DSN_ERR_INVALID_ARG;
+  if (workspace && !aligned16(workspace)) return DSN_ERR_ALIGNMENT;
+  if (r->B == 0) return DSN_OK;
+  const LayerCall c = from_linear_i8(d);
+  e = run_linear_i8(ctx, d, c, r, x, x_scale, y, workspace, ws_bytes, as_stream(stream));
+  if (e) return e;
+  if (d->tail == DSN_TAIL_ZERO) {
+    SliceTable st;
+    fill_slice_table(st, c);
+    count_launch(ctx, &dsn_stats::launches_copy);
+    if (dsn_launch_zero_tail(st, elem_bytes(d->y_dtype), d->R, d->C_out, y, d->ldy, d->out_order == DSN_INPUT_ORDER, r->B, r->G,
+                             r->offsets, r->perm, r->group_slice, as_stream(stream)) != cudaSuccess)
+      return DSN_ERR_CUDA;
+  }
+  return DSN_OK;
+}
+
+int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r, const int32_t* positions, const void* x,
+                    void* y, void* stream) {
+  if (!positions || !x || !y) return DSN_ERR_INVALID_ARG;
+  int e = check_ctx(ctx);
+  if (e) return e;
+  e = check_rotary(d, r);
+  if (e) return e;
+  const int es = elem_bytes(d->dtype);
+  if (x == y && d->ldx != d->ldy) return DSN_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(x) % es || reinterpret_cast<uintptr_t>(y) % es) return DSN_ERR_ALIGNMENT;
+  if (r->B == 0) return DSN_OK;
+  RotaryParams p;
+  memset(&p, 0, sizeof(p));
+  const int n[3] = {d->pairs[0], d->n_axes > 1 ? d->pairs[1] : 0, d->n_axes > 2 ? d->pairs[2] : 0};
+  p.pairs = n[0] + n[1] + n[2];
+  int i = 0;
+  for (int a = 0; a < d->n_axes; ++a)
+    for (int j = 0; j < n[a]; ++j, ++i) {
+      // turns per unit of position in units of 2^-64 (at most 2^64 / 2 pi: fits), from 64-bit mantissas
+      const long double ex = d->ladder == DSN_ROTARY_SHARED ? (long double)i / p.pairs : (long double)j / n[a];
+      p.freq[i] = (uint64_t)(powl((long double)d->base, -ex) * 18446744073709551616.0L / 6.283185307179586476925286766559L + 0.5L);
+      p.axis[i] = (uint8_t)a;
+    }
+  int max_heads = 1;
+  for (int t = 0; t < d->T; ++t) {
+    p.heads[t] = (int16_t)d->heads[t];
+    if (d->heads[t] > max_heads) max_heads = d->heads[t];
+  }
+  p.N = d->N; p.D = d->D; p.vectors = d->vectors; p.rotated = d->rotated;
+  p.B = r->B; p.G = r->G; p.T = d->T; p.grouped = d->order == DSN_GROUPED;
+  p.shared = d->shared_positions != 0;
+  p.n_pos = p.shared ? d->N : r->B * d->N;
+  p.interleaved = d->pairing == DSN_ROTARY_INTERLEAVED;
+  p.inverse = d->inverse != 0;
+  p.in_place = x == y;
+  p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
+  p.positions = positions; p.x = x; p.y = y; p.ldx = d->ldx; p.ldy = d->ldy;
+  const int aligned = aligned16(x) && aligned16(y) && (d->ldx * es) % 16 == 0 && (d->ldy * es) % 16 == 0;
+  count_launch(ctx, &dsn_stats::launches_rotary);
+  return dsn_launch_rotary(p, d->dtype == DSN_F32, max_heads, aligned, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }
 
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L) {

@@ -1,0 +1,462 @@
+// Ragged grouped sliced linear layer on 8-bit integers, CTA pairs (tcgen05 cta_group::2, kind::i8, 32-bit integer sums):
+//   y = act((sum_c x[c] W[o][c]) * sx[row] * sw[o] + bias, per-path affine, + skip features).
+// Tiles, barriers and roles are those of the bf16 pair kernel: a cluster of two CTAs owns a 256-row x BN-column tile, each
+// CTA loads its 128 rows and half of the weight tile, the even CTA issues the products of both.  A 128-byte
+// row piece holds 128 columns here, an instruction takes 32 of them, and at twice the products per byte the main loop of a
+// tile is half as long, so the epilogue weighs twice as much: a warp fetches the channels' factors of its 64 columns before it waits
+// for the accumulator (sw and the affine folded into one factor and one addend, through shared memory), which leaves a
+// conversion, a multiplication and a packed multiply-add per element.
+// Barriers (every CTA has the same layout):
+//   full[s]    even CTA only: one arrival (expect_tx for the bytes of both CTAs), completed by the loads of both
+//   empty[s]   both CTAs: the multicast commit frees the stage
+//   tfull[a]   both CTAs: the accumulator is complete
+//   tempty[a]  even CTA only, 2 x 8 arrivals: the epilogue warps of both CTAs
+// Every wait is bounded; on a timeout the CTA flags DSN_ERR_TIMEOUT and leaves its loops.
+#include "dsn_gemm_pair_device.cuh"
+#include "dsn_transformer.cuh"
+
+namespace {
+
+using namespace dsn_gemm;
+
+constexpr int kBKB = 128;                          // bytes (= columns) of a chunk
+constexpr uint32_t kColBytes = kEpiWarps * 64 * 8; // per epilogue warp: factor and addend of 64 columns
+
+// D[tmem] (+)= A[smem] * B[smem]^T on both CTAs' tensor cores, signed 8-bit operands, 32-bit integer sums
+__device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor: D 32-bit integer, A and B signed 8-bit, both K-major, M x N tile.
+__device__ __forceinline__ uint32_t make_idesc_i8(int M, int N) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ float relu_nan(float v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(0.f));
+  return r;
+}
+
+// The fitted GELU for two values.  Its odd quintic turns round beyond |v| = 8, where the tanh has long been +-1, so v^2 is
+// held at 36 inside it (at |v| = 6 the argument is 10).
+__device__ __forceinline__ void gelu_pair_i8(float a, float b, float& ra, float& rb) {
+  const uint64_t zero2 = pack2(0.f, 0.f), v2 = pack2(a, b);
+  const uint64_t z2 = pack2(fminf(a * a, 36.f), fminf(b * b, 36.f));
+  uint64_t q = ffma2(z2, pack2(-0.00035873294f, -0.00035873294f), pack2(0.037050344f, 0.037050344f));
+  q = ffma2(z2, q, pack2(0.79745847f, 0.79745847f));
+  float u0, u1, t0, t1;
+  unpack2(ffma2(v2, q, zero2), u0, u1);
+  asm("tanh.approx.f32 %0, %1;" : "=f"(t0) : "f"(u0));
+  asm("tanh.approx.f32 %0, %1;" : "=f"(t1) : "f"(u1));
+  const uint64_t h2 = ffma2(v2, pack2(0.5f, 0.5f), zero2);
+  unpack2(ffma2(h2, pack2(t0, t1), h2), ra, rb);
+}
+
+struct EpiArgs {
+  const float* w_scale;   // at the tile's first column
+  const float* bias;
+  const float* bn_scale;
+  const float* bn_shift;
+};
+
+// Factor and addend of this lane's columns of the 32-column piece at `cb` into the warp's shared tile.
+__device__ __forceinline__ void stage_columns(const EpiArgs& a, int cb, int ncols, int lane, float* s_mul, float* s_add) {
+  float m = 0.f, d = 0.f;
+  const int c = cb + lane;
+  if (c < ncols) {
+    m = __ldg(a.w_scale + c);
+    if (a.bias) d = __ldg(a.bias + c);
+    if (a.bn_scale) {
+      const float sc = __ldg(a.bn_scale + c);
+      m *= sc;
+      d = fmaf(d, sc, __ldg(a.bn_shift + c));
+    }
+  }
+  s_mul[lane] = m;
+  s_add[lane] = d;
+}
+
+// 32 accumulator columns of this thread's row -> 32 values behind scales, affine, skip features and activation.
+template <bool F32, int ACT, bool RES>
+__device__ __forceinline__ void epilogue_i8_piece(uint32_t taddr, int cb, int ncols, float sx, const float* s_mul, const float* s_add,
+                                                  const void* res_row, float (&f)[32]) {
+  uint32_t v[32];
+  tmem_ld_32x32(taddr, v);
+  tmem_ld_wait();
+  const uint64_t sx2 = pack2(sx, sx), zero2 = pack2(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float4 m = reinterpret_cast<const float4*>(s_mul)[j], d = reinterpret_cast<const float4*>(s_add)[j];
+    uint64_t a = ffma2(pack2((float)(int)v[4 * j], (float)(int)v[4 * j + 1]), sx2, zero2);
+    uint64_t b = ffma2(pack2((float)(int)v[4 * j + 2], (float)(int)v[4 * j + 3]), sx2, zero2);
+    a = ffma2(a, pack2(m.x, m.y), pack2(d.x, d.y));
+    b = ffma2(b, pack2(m.z, m.w), pack2(d.z, d.w));
+    unpack2(a, f[4 * j], f[4 * j + 1]);
+    unpack2(b, f[4 * j + 2], f[4 * j + 3]);
+  }
+  if (RES && res_row) {
+    if (F32) {
+      const float* rp = static_cast<const float*>(res_row) + cb;
+      if (cb + 32 <= ncols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float4 r = __ldg(reinterpret_cast<const float4*>(rp) + j);
+          f[4 * j] += r.x; f[4 * j + 1] += r.y; f[4 * j + 2] += r.z; f[4 * j + 3] += r.w;
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+          if (cb + c < ncols) f[c] += __ldg(rp + c);
+      }
+    } else {
+      const __nv_bfloat16* rp = static_cast<const __nv_bfloat16*>(res_row) + cb;
+      if (cb + 32 <= ncols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint4 r = __ldg(reinterpret_cast<const uint4*>(rp) + j);
+          const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[8 * j + 2 * e] += __uint_as_float(w[e] << 16);
+            f[8 * j + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+          if (cb + c < ncols) f[c] += __bfloat162float(rp[c]);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 32; c += 2) {
+    if (ACT == DSN_ACT_RELU) {
+      f[c] = relu_nan(f[c]);
+      f[c + 1] = relu_nan(f[c + 1]);
+    } else if (ACT == DSN_ACT_GELU) {
+      if (F32) {
+        f[c] = 0.5f * f[c] * (1.f + erff(f[c] * 0.70710678118654752f));
+        f[c + 1] = 0.5f * f[c + 1] * (1.f + erff(f[c + 1] * 0.70710678118654752f));
+      } else {
+        gelu_pair_i8(f[c], f[c + 1], f[c], f[c + 1]);
+      }
+    }
+  }
+}
+
+// Epilogue of one tile for one warp; the warp takes the pieces of 128 bytes (64 bf16 or 32 fp32 columns) `first`, `first + 2`, ...:
+// 32 rows x 128 bytes, swizzled, staged in shared memory, out by one TMA store where the rows are consecutive, else by
+// row pieces.  Columns that a TMA store cannot clip (its granule is 16 bytes) are written by every lane for its own row.
+template <bool F32, int ACT, bool RES>
+__device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int n0, int first, const EpiArgs& cols, float sx, const void* res_row,
+                                                 uint8_t* stage_w, float* s_col, char* yrow, int lane, bool contig, const CUtensorMap* mapY, int base_row) {
+  constexpr int W = F32 ? 32 : 64;          // columns of a staged piece
+  constexpr int G = F32 ? 4 : 8;            // columns of 16 bytes
+  constexpr int ES = F32 ? 4 : 2;
+  for (int c0 = W * first; c0 < ncols; c0 += 2 * W) {
+    if (elect_one()) bulk_wait_read0();     // an earlier store of this warp has read the staging tile
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < W / 32; ++h) {
+      const int cb = c0 + 32 * h;
+      if (cb < ncols) {
+        stage_columns(cols, cb, ncols, lane, s_col + 64 * h, s_col + 64 * h + 32);
+        __syncwarp();
+        float f[32];
+        epilogue_i8_piece<F32, ACT, RES>(taddr + cb, cb, ncols, sx, s_col + 64 * h, s_col + 64 * h + 32, res_row, f);
+#pragma unroll
+        for (int j = 0; j < 32 / G; ++j) {
+          uint4 o;
+          if (F32) {
+            o = make_uint4(__float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j + 2]), __float_as_uint(f[4 * j + 3]));
+          } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              __nv_bfloat162 b = __floats2bfloat162_rn(f[(G * j + 2 * e) & 31], f[(G * j + 2 * e + 1) & 31]);
+              w[e] = *reinterpret_cast<uint32_t*>(&b);
+            }
+            o = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          const int jj = (32 / G) * h + j;   // 16-byte piece of the 128-byte row
+          *reinterpret_cast<uint4*>(stage_w + lane * 128 + ((jj ^ (lane & 7)) << 4)) = o;
+        }
+      }
+    }
+    const int last = ncols - c0 < W ? ncols - c0 : W;   // columns of this piece
+    if (contig) {
+      fence_async_smem();
+      __syncwarp();
+      if (elect_one()) {
+        tma_store_2d(mapY, n0 + c0, base_row, smem_u32(stage_w));
+        bulk_commit();
+      }
+      const int whole = last & ~(G - 1);
+      if (whole != last) {
+        const uint8_t* sp = stage_w + lane * 128 + (((whole / G) ^ (lane & 7)) << 4);
+        for (int e = 0; e < last - whole; ++e) {
+          if (F32) reinterpret_cast<float*>(yrow)[c0 + whole + e] = reinterpret_cast<const float*>(sp)[e];
+          else reinterpret_cast<uint16_t*>(yrow)[c0 + whole + e] = reinterpret_cast<const uint16_t*>(sp)[e];
+        }
+      }
+    } else {
+      __syncwarp();
+      const int j = lane & 7;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {          // eight lanes a row, 16 bytes each
+        const int row = 4 * i + (lane >> 3);
+        char* rp = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(yrow), row));
+        if (rp != nullptr && G * j < last) {
+          const uint8_t* sp = stage_w + row * 128 + ((j ^ (row & 7)) << 4);
+          char* dst = rp + (int64_t)(c0 + G * j) * ES;
+          if (G * j + G <= last) {
+            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(sp);
+          } else {
+            for (int e = 0; e < last - G * j; ++e) {
+              if (F32) reinterpret_cast<float*>(dst)[e] = reinterpret_cast<const float*>(sp)[e];
+              else reinterpret_cast<uint16_t*>(dst)[e] = reinterpret_cast<const uint16_t*>(sp)[e];
+            }
+          }
+        }
+      }
+      __syncwarp();
+    }
+  }
+}
+
+template <bool F32, bool RES>
+__global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_constant__ GemmI8Params P) {
+  extern __shared__ uint8_t smem_raw[];
+  const GemmParams& p = P.g;
+  const GemmGeom& g = p.g;
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (base - raw);
+
+  const uint32_t bar_full = base;
+  const uint32_t bar_empty = base + 8 * kMaxStages;
+  const uint32_t bar_tfull = base + 16 * kMaxStages;
+  const uint32_t bar_tempty = bar_tfull + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 16 * kMaxStages + 32);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 16 * kMaxStages + 36);
+
+  const int stages = g.stages;
+  const uint32_t bh_bytes = (uint32_t)(g.BN / 2) * kBKB;  // this CTA's half of the weight tile
+  const uint32_t stage_bytes = kABytes + bh_bytes;        // kABytes: 128 rows of 128 bytes
+  const uint32_t tiles_base = base + kCtrlBytes;
+  uint8_t* out_stage = smem + kCtrlBytes + (size_t)stages * stage_bytes;
+  float* col_stage = reinterpret_cast<float*>(out_stage + kStageOutBytes);
+  int32_t* s_prefix = reinterpret_cast<int32_t*>(out_stage + kStageOutBytes + kColBytes);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const uint32_t tmem_cols = 2u * (uint32_t)g.BN;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(bar_tfull + 8 * a, 1);
+      mbar_init(bar_tempty + 8 * a, 2 * kEpiWarps);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(tmem_slot), tmem_cols);
+    tmem_relinquish_pair();
+  }
+
+  auto ntiles_of = [&](int grp) {
+    const int sl = p.group_slice ? p.group_slice[grp] : grp;
+    if (sl < 0 || sl >= p.T || p.map_id[sl] == 0xFF) return 0;
+    const int cnt = p.offsets[grp + 1] - p.offsets[grp];
+    if (cnt <= 0) return 0;
+    const int mt = g.flat ? (cnt * g.R + BM - 1) / BM : ((cnt + g.nb - 1) / g.nb) * g.tiles_x * g.tiles_y;
+    return ((mt + 1) / 2) * ((p.k_out[sl] + g.BN - 1) / g.BN);
+  };
+  // barriers and TMEM are set up; everything below reads what earlier kernels wrote
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  // s_prefix[0..G]: tile prefix; [G+1 .. 2G+1]: group offsets; [2G+2 .. 3G+1]: slice of each group
+  for (int j = threadIdx.x; j <= p.G; j += blockDim.x) s_prefix[p.G + 1 + j] = p.offsets[j];
+  for (int j = threadIdx.x; j < p.G; j += blockDim.x) {
+    const int sl = p.group_slice ? p.group_slice[j] : j;
+    s_prefix[2 * p.G + 2 + j] = (sl >= 0 && sl < p.T) ? sl : 0;
+  }
+  dsn_build_tile_prefix(p.G, s_prefix, ntiles_of);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // the peer's barriers are initialised before anything can arrive on them
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int total = s_prefix[p.G];
+  PairCursor cursor;  // every role walks its own tile sequence
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer (both CTAs)
+    int stage = 0;
+    uint32_t phase = 0;
+    const uint32_t a_box_bytes = g.flat ? kABytes : (uint32_t)(g.bw * g.bh * g.nb) * kBKB;
+    const uint32_t tx_bytes = 2u * (a_box_bytes + bh_bytes);
+    bool ok = true;
+    for (int tile = pair; ok && tile < total; tile += npairs) {
+      const PairTile t = decode_pair_tile(p, s_prefix, tile, rank, cursor);
+      const CUtensorMap* mA = &p.mapA[t.map];
+      const CUtensorMap* mB = &p.mapB[t.map];
+      const int nkc = (t.ki + kBKB - 1) / kBKB;
+      const int n_inst = (t.ncols + 31) & ~31;
+      const int brow0 = t.n0 + rank * (n_inst >> 1);  // first weight row of this CTA's half
+      int bsel = t.b0;
+      if (g.a_input_order) bsel = t.b0 < t.p_end ? p.perm[t.b0] : p.B;  // past the group: out of range, zeros
+      const int cx = g.flat ? t.row0 : t.x0, cb = g.flat ? 0 : bsel;
+      for (int kc = 0; kc < nkc; ++kc) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status, 61));
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t full_lead = leader_addr(bar_full + 8 * stage);  // the even CTA's barrier
+          if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, tx_bytes);
+          const uint32_t sa = tiles_base + stage * stage_bytes;
+          tma_load_4d_pair(sa, mA, kc * kBKB, cx, 0, cb, full_lead);
+          tma_load_3d_pair(sa + kABytes, mB, kc * kBKB, 0, brow0, full_lead);
+        }
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (even CTA only)
+    if (rank == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      int it = 0;
+      bool ok = true;
+      const uint64_t da0 = make_smem_desc(tiles_base), db0 = make_smem_desc(tiles_base + kABytes);
+      const uint64_t dstep = (uint64_t)(stage_bytes >> 4);
+      uint64_t da = da0, db = db0;
+      for (int tile = pair; ok && tile < total; tile += npairs, ++it) {
+        const PairTile t = decode_pair_tile(p, s_prefix, tile, 0, cursor);
+        const int acc = it & 1;
+        const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, abort_flag, p.status, 62));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t idesc = make_idesc_i8(2 * BM, (t.ncols + 31) & ~31);
+        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * g.BN);
+        const int tail_ks = ((t.ki & (kBKB - 1)) + 31) >> 5;  // K steps of a partial last chunk (0: none)
+        uint32_t accumulate = 0;
+        for (int kc = (t.ki + kBKB - 1) / kBKB; kc > 0; --kc) {
+          ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag, p.status, 63));
+          if (!ok) break;
+          tc_fence_after();
+          const int nks = (kc == 1 && tail_ks != 0) ? tail_ks : kBKB / 32;
+          if (elect_one()) {
+            umma_i8_pair(d_tmem, da, db, idesc, accumulate);  // +32 bytes per K step
+            if (nks > 1) umma_i8_pair(d_tmem, da + 2u, db + 2u, idesc, 1u);
+            if (nks > 2) umma_i8_pair(d_tmem, da + 4u, db + 4u, idesc, 1u);
+            if (nks > 3) umma_i8_pair(d_tmem, da + 6u, db + 6u, idesc, 1u);
+            umma_commit_pair(bar_empty + 8 * stage);
+          }
+          accumulate = 1;
+          da += dstep;
+          db += dstep;
+          if (++stage == stages) { stage = 0; phase ^= 1u; da = da0; db = db0; }
+        }
+        if (ok && elect_one()) umma_commit_pair(bar_tfull + 8 * acc);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue (warps 2..9, both CTAs)
+    const int q = warp & 3;
+    const int first = (warp - 2) >> 2;
+    const int m = q * 32 + lane;
+    int it = 0;
+    bool ok = true;
+    const int es = F32 ? 4 : 2;
+    uint8_t* stage_w = out_stage + (warp - 2) * (32 * 128);
+    float* s_col = col_stage + (warp - 2) * 128;
+    for (int tile = pair; ok && tile < total; tile += npairs, ++it) {
+      const PairTile t = decode_pair_tile(p, s_prefix, tile, rank, cursor);
+      const int acc = it & 1;
+      const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
+      bool valid;
+      int pp, r;   // position and row inside the sample
+      if (g.flat) {
+        const int gr = t.row0 + m;
+        valid = gr < t.rows_end;
+        pp = gr / g.R;
+        r = gr - pp * g.R;
+      } else {
+        const int bi = m / g.bw;
+        r = t.x0 + (m - bi * g.bw);
+        pp = t.b0 + bi;
+        valid = bi < g.nb && r < g.R && pp < t.p_end;
+      }
+      int64_t out_row = 0;
+      float sx = 0.f;
+      if (valid) {
+        const int smp = (g.y_input_order || P.scale_input_order) ? p.perm[pp] : 0;
+        out_row = (int64_t)(g.y_input_order ? smp : pp) * g.R + r;
+        sx = __ldg(P.x_scale + (int64_t)(P.scale_input_order ? smp : pp) * g.R + r);
+      }
+      char* yrow = valid ? reinterpret_cast<char*>(p.y) + (out_row * p.ldy + t.n0) * es : nullptr;
+      const void* res_row = (RES && valid) ? reinterpret_cast<const char*>(p.residual) + (out_row * p.ldy + t.n0) * es : nullptr;
+      EpiArgs cols;
+      cols.w_scale = P.w_scale + t.n0;
+      cols.bias = p.bias ? p.bias + t.n0 : nullptr;
+      cols.bn_scale = p.bn_scale ? p.bn_scale + (int64_t)t.slice * p.bn_ld + t.n0 : nullptr;
+      cols.bn_shift = p.bn_scale ? p.bn_shift + (int64_t)t.slice * p.bn_ld + t.n0 : nullptr;
+      const int ncols = t.ncols;
+      const long long base_row = __shfl_sync(0xffffffffu, (long long)out_row, 0);
+      const bool contig = __all_sync(0xffffffffu, valid && out_row == base_row + lane) && t.ko >= 8;
+
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * acc, acc_phase, abort_flag, p.status, 64));
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * g.BN);
+      const CUtensorMap* mY = &p.mapY[t.map];
+      switch (p.act) {
+        case DSN_ACT_NONE: epilogue_i8_tile<F32, DSN_ACT_NONE, RES>(taddr, ncols, t.n0, first, cols, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+        case DSN_ACT_RELU: epilogue_i8_tile<F32, DSN_ACT_RELU, RES>(taddr, ncols, t.n0, first, cols, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+        default: epilogue_i8_tile<F32, DSN_ACT_GELU, RES>(taddr, ncols, t.n0, first, cols, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(leader_addr(bar_tempty + 8 * acc));  // the even CTA's issuing warp waits on it
+    }
+    if (elect_one()) bulk_wait0();  // the lane that issued this warp's TMA stores
+  }
+
+  // ------------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // neither CTA retires while its partner may still read its memory or signal its barriers
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, tmem_cols);
+  }
+}
+
+}  // namespace
+
+size_t dsn_gemm_i8_smem_bytes(int BN, int stages, int G) {
+  return 1024 + kCtrlBytes + (size_t)stages * (kABytes + (size_t)(BN / 2) * kBKB) + kStageOutBytes + kColBytes + sizeof(int32_t) * (3 * (size_t)G + 3);
+}
+
+cudaError_t dsn_launch_gemm_i8(const GemmI8Params& p, int f32, int clusters, size_t smem_bytes, cudaStream_t s) {
+  static size_t configured[4][DSN_MAX_DEVICES] = {};
+  const int form = (f32 ? 2 : 0) + (p.g.residual ? 1 : 0);
+  void (*kernel)(GemmI8Params) = form == 3 ? gemm_i8_pair_kernel<true, true>
+                                 : form == 2 ? gemm_i8_pair_kernel<true, false>
+                                 : form == 1 ? gemm_i8_pair_kernel<false, true> : gemm_i8_pair_kernel<false, false>;
+  const cudaError_t e = dsn_ensure_dynamic_smem(kernel, smem_bytes, configured[form]);
+  if (e != cudaSuccess) return e;
+  return dsn_launch(kernel, dim3(2 * clusters), dim3(kThreads), smem_bytes, s, 2, p);
+}

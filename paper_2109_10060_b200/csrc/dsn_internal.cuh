@@ -25,6 +25,7 @@ struct dsn_map_key {
   uint64_t strides[3];
   uint32_t box[4];
   uint32_t rank;
+  uint32_t type;  // CUtensorMapDataType
 };
 struct dsn_map_slot {
   dsn_map_key key;

@@ -1,0 +1,145 @@
+// Linear layer on 8-bit codes for a few rows in all (single tokens of a small batch): y = act(sx sw sum x W + ...).
+// Bound by the bytes of the weights, which are read once for all rows.  A CTA owns 16 output channels, its eight warps
+// split the reduction and meet in shared memory (integers: any order gives the same sum).  The products go through
+// the warp-level 8-bit matrix instruction (16 channels x 8 rows x 32 columns): at most 32 rows cannot fill the 128 rows of a
+// tensor-memory tile, and this form takes its operands straight from registers.  The order of the columns inside a sum
+// is free, so a lane's 16 consecutive bytes serve as its pieces of two instructions, the same way for weights and rows.
+// Rows of narrower paths are zero beyond their k_in, so all rows share one reduction over the widest path's columns.
+#include "dsn_transformer.cuh"
+
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kAhead = 4;   // steps of 64 columns whose weights are in flight
+
+struct RowInfo {
+  int64_t src, dst;   // rows of x and y; dst < 0: the row does not exist
+  float sx;
+  int ki, ko, slice;
+};
+
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 16 bytes of a row from byte `off`, zero at and beyond `end`
+__device__ __forceinline__ uint4 load16(const int8_t* row, int off, int end) {
+  if (off + 16 <= end) return __ldg(reinterpret_cast<const uint4*>(row + off));
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  if (off < end) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (off + i < end) w[i >> 2] |= (uint32_t)(uint8_t)row[off + i] << (8 * (i & 3));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <bool F32, int NT>   // NT tiles of eight rows
+__global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant__ RowsI8Params p) {
+  __shared__ RowInfo info[8 * NT];
+  __shared__ int part[kWarps][8 * NT][17];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, q = lane & 3;
+  const int o0 = blockIdx.x * 16;
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const int steps = (p.max_ki + 63) >> 6;
+  const int8_t* w0 = p.W + (int64_t)(o0 + g) * p.ldw;
+  const int8_t* w1 = w0 + 8 * p.ldw;
+  const int end0 = o0 + g < p.max_ko ? p.max_ki : 0, end1 = o0 + g + 8 < p.max_ko ? p.max_ki : 0;
+  uint4 a0[kAhead], a1[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {   // the weights do not wait for the rows' paths
+    const int st = warp + j * kWarps;
+    a0[j] = load16(w0, 64 * st + 16 * q, st < steps ? end0 : 0);
+    a1[j] = load16(w1, 64 * st + 16 * q, st < steps ? end1 : 0);
+  }
+  const int rows = p.B * p.R;
+  for (int i = warp; i < 8 * NT; i += kWarps) {
+    RowInfo ri{0, -1, 0.f, 0, 0, 0};
+    if (i < rows) {
+      const int pos = i / p.R, r = i - pos * p.R;
+      const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
+      if (at.slice >= 0) {
+        ri.src = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
+        ri.dst = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
+        ri.sx = p.x_scale[ri.src];
+        ri.ki = p.k_in[at.slice];
+        ri.ko = p.k_out[at.slice];
+        ri.slice = at.slice;
+      }
+    }
+    if (lane == 0) info[i] = ri;
+  }
+  __syncthreads();
+  const int8_t* xr[NT];
+  int xe[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    xr[n] = p.x + info[8 * n + g].src * p.ldx;
+    xe[n] = info[8 * n + g].ki;
+  }
+  int c[NT][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[n][i] = 0;
+  for (int base = warp; base < steps; base += kAhead * kWarps) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int st = base + j * kWarps;
+      if (st < steps) {
+        const int off = 64 * st + 16 * q;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint4 b = load16(xr[n], off, xe[n]);
+          mma_s8(c[n], a0[j].x, a1[j].x, a0[j].y, a1[j].y, b.x, b.y);
+          mma_s8(c[n], a0[j].z, a1[j].z, a0[j].w, a1[j].w, b.z, b.w);
+        }
+        const int nx = st + kAhead * kWarps;   // this slot's next step
+        a0[j] = load16(w0, 64 * nx + 16 * q, nx < steps ? end0 : 0);
+        a1[j] = load16(w1, 64 * nx + 16 * q, nx < steps ? end1 : 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {   // accumulator: channels g and g + 8, rows 2 q and 2 q + 1 of the tile
+    part[warp][8 * n + 2 * q][g] = c[n][0];
+    part[warp][8 * n + 2 * q + 1][g] = c[n][1];
+    part[warp][8 * n + 2 * q][g + 8] = c[n][2];
+    part[warp][8 * n + 2 * q + 1][g + 8] = c[n][3];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < 16 * 8 * NT; e += kThreads) {
+    const int row = e >> 4, ch = e & 15, o = o0 + ch;
+    const RowInfo ri = info[row];
+    if (ri.dst < 0 || o >= ri.ko) continue;
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) sum += part[i][row][ch];
+    float v = (float)sum * ri.sx * p.w_scale[o];
+    if (p.bias) v += p.bias[o];
+    if (p.bn_scale) v = fmaf(v, p.bn_scale[(int64_t)ri.slice * p.bn_ld + o], p.bn_shift[(int64_t)ri.slice * p.bn_ld + o]);
+    const int64_t at = ri.dst * p.ldy + o;
+    if (p.residual) v += F32 ? static_cast<const float*>(p.residual)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at]);
+    if (p.act == DSN_ACT_RELU) asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(v), "f"(0.f));   // a NaN stays visible
+    if (p.act == DSN_ACT_GELU) v = 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+    if (F32) static_cast<float*>(p.y)[at] = v; else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
+  }
+}
+
+template <bool F32>
+cudaError_t pick(const RowsI8Params& p, cudaStream_t s) {
+  const dim3 grid((p.max_ko + 15) / 16), block(kThreads);
+  const int rows = p.B * p.R;
+  if (rows <= 8) return dsn_launch(rows_i8_kernel<F32, 1>, grid, block, 0, s, 1, p);
+  if (rows <= 16) return dsn_launch(rows_i8_kernel<F32, 2>, grid, block, 0, s, 1, p);
+  return dsn_launch(rows_i8_kernel<F32, 4>, grid, block, 0, s, 1, p);
+}
+
+}  // namespace
+
+cudaError_t dsn_launch_rows_i8(const RowsI8Params& p, int f32, cudaStream_t s) {
+  return f32 ? pick<true>(p, s) : pick<false>(p, s);
+}

@@ -1,0 +1,106 @@
+// Parameters and launchers of the 8-bit transformer operators: residual + norm + codes (dsn_norm_quant.cu),
+// linear layers on codes (dsn_gemm_i8_pair.cu, dsn_rows_i8.cu), rotary positions (dsn_rotary.cu).
+#pragma once
+
+#include "dsn_internal.cuh"
+
+// Where a grouped position lies: its sample and the slice of its group.  Up to 32 groups take one load per lane, more
+// a binary search.  All lanes of the warp call this with the same arguments; slice < 0: no work at this position.
+struct PosInfo {
+  int sample;
+  int slice;
+};
+__device__ __forceinline__ PosInfo dsn_locate_warp(int p, int G, int T, const int32_t* __restrict__ offsets,
+                                                   const int32_t* __restrict__ perm, const int32_t* __restrict__ group_slice) {
+  const int lane = threadIdx.x & 31;
+  int g;
+  if (G <= 32) {
+    const int end = lane < G ? offsets[lane + 1] : 0x7fffffff;
+    g = __popc(__ballot_sync(0xffffffffu, end <= p));   // groups that end at or before p, empty ones among them
+  } else {
+    if (p >= offsets[G]) return PosInfo{0, -1};
+    int lo = 0, hi = G;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (offsets[mid] <= p) lo = mid; else hi = mid;
+    }
+    g = lo;
+  }
+  if (g >= G) return PosInfo{0, -1};
+  PosInfo i;
+  i.sample = perm[p];
+  i.slice = group_slice ? group_slice[g] : g;
+  if (i.sample < 0 || i.slice >= T) i.slice = -1;
+  return i;
+}
+
+struct NormParams {
+  int16_t k[DSN_MAX_SLICES];
+  int32_t R, B, G, T;
+  int32_t in_input_order, out_input_order;
+  const int32_t* offsets;
+  const int32_t* perm;
+  const int32_t* group_slice;
+  const void* x;
+  const void* residual;
+  void* sum;
+  int8_t* q;
+  float* scale;
+  void* y;
+  int64_t ldx, ld_res, ld_sum, ldq, ldy;
+  const float* weight;
+  float eps;
+};
+cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int max_k, cudaStream_t s);
+
+struct RotaryParams {
+  uint64_t freq[128];   // turns per unit of position, in units of 2^-64
+  uint8_t axis[128];
+  int16_t heads[DSN_MAX_SLICES];
+  int32_t N, D, vectors, rotated, pairs;
+  int32_t B, G, T, grouped;
+  int32_t n_pos;        // rows of one axis of `positions`
+  int32_t shared, interleaved, inverse, in_place;
+  const int32_t* offsets;
+  const int32_t* perm;
+  const int32_t* group_slice;
+  const int32_t* positions;
+  const void* x;
+  void* y;
+  int64_t ldx, ldy;
+};
+cudaError_t dsn_launch_rotary(const RotaryParams& p, int f32, int max_heads, int aligned, cudaStream_t s);
+
+// 8-bit linear layer on CTA pairs: `g` as in the bf16 pair kernel (maps on bytes, 128 a chunk; y, residual of either type)
+struct GemmI8Params {
+  GemmParams g;
+  const float* x_scale;   // one per row of x
+  const float* w_scale;   // one per output channel
+  int32_t scale_input_order;  // rows of x_scale by sample (else by grouped position)
+};
+size_t dsn_gemm_i8_smem_bytes(int BN, int stages, int G);
+cudaError_t dsn_launch_gemm_i8(const GemmI8Params& p, int f32, int clusters, size_t smem_bytes, cudaStream_t s);
+
+// 8-bit linear layer of at most DSN_ROWS_I8_MAX rows in all
+#define DSN_ROWS_I8_MAX 32
+struct RowsI8Params {
+  int16_t k_in[DSN_MAX_SLICES];
+  int16_t k_out[DSN_MAX_SLICES];
+  int32_t B, R, G, T, C_in, max_ki, max_ko;
+  int32_t in_input_order, out_input_order;
+  const int32_t* offsets;
+  const int32_t* perm;
+  const int32_t* group_slice;
+  const int8_t* x;
+  const float* x_scale;
+  const int8_t* W;
+  const float* w_scale;
+  const float* bias;
+  const float* bn_scale;
+  const float* bn_shift;
+  int32_t bn_ld, act;
+  const void* residual;
+  void* y;
+  int64_t ldx, ldw, ldy;
+};
+cudaError_t dsn_launch_rows_i8(const RowsI8Params& p, int f32, cudaStream_t s);
