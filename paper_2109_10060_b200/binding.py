@@ -188,9 +188,21 @@ def _check(code: int, what: str):
 
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return int(torch.cuda.current_stream().cuda_stream) or None
+        return _current_stream() or None
     return int(stream.cuda_stream) or None
+
+
+def _current_stream() -> int:
+    """Handle of the current device's current stream (torch.cuda.current_stream() builds two Python objects for it, 4 us a call)."""
+    global _current_stream
+    import torch
+    raw, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    torch.cuda.init()
+    if raw and dev:
+        _current_stream = lambda: raw(dev())
+    else:
+        _current_stream = lambda: int(torch.cuda.current_stream().cuda_stream)
+    return _current_stream()
 
 
 def dsn_strerror(code: int) -> str:
@@ -405,9 +417,20 @@ def dsn_layer_forward(ctx: Context, L: LayerDesc, x, idx_in, y, workspace, r_out
 
 # ---- transformer blocks in 8 bits.  These calls also check what a pointer cannot say: type, device and extent of every tensor.
 
-def _torch_dtype(code: int):
-    import torch
-    return {F32: torch.float32, BF16: torch.bfloat16}.get(code)
+class _Types:
+    """torch's types by the library's codes, looked up once."""
+    of_code = None
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.i8, cls.i32, cls.f32 = torch.int8, torch.int32, torch.float32
+        cls.of_code = {F32: torch.float32, BF16: torch.bfloat16}
+        return cls
+
+
+def _types():
+    return _Types if _Types.of_code else _Types.load()
 
 
 def _buf(what: str, t, dtype, need: int, device: Optional[int] = None, rows: bool = False) -> Optional[int]:
@@ -432,8 +455,7 @@ def _span(rows: int, ld: int, width: int) -> int:
 def make_norm_desc(dtype, R, Cn, k, weight=None, eps=1e-6, ldx=None, ld_res=None, ld_sum=None, ldq=None, ldy=None,
                    in_order=INPUT_ORDER, out_order=INPUT_ORDER) -> NormDesc:
     """Residual + root-mean-square norm + 8-bit codes; leading dimensions default to Cn."""
-    import torch
-    _buf("weight", weight, torch.float32, Cn)
+    _buf("weight", weight, _types().f32, Cn)
     ka = _i32_array(k)
     d = NormDesc(dtype, R, Cn, *(Cn if v is None else v for v in (ldx, ld_res, ld_sum, ldy, ldq)), len(k), ka, _ptr(weight), eps,
                  in_order, out_order)
@@ -442,12 +464,12 @@ def make_norm_desc(dtype, R, Cn, k, weight=None, eps=1e-6, ldx=None, ld_res=None
 
 
 def dsn_rmsnorm_quant(ctx: Context, d: NormDesc, routing: Routing, x, q=None, scale=None, y=None, residual=None, sum_out=None, stream=None):
-    import torch
-    dt, rows, dev = _torch_dtype(d.dtype), routing.B * d.R, ctx.device
-    _check(ctx.lib.dsn_rmsnorm_quant(ctx.handle, C.byref(d), C.byref(routing), _buf("x", x, dt, _span(rows, d.ldx, d.C), dev, True),
+    ty, rows, dev = _types(), routing.B * d.R, ctx.device
+    dt = ty.of_code.get(d.dtype)
+    _check(ctx.lib.dsn_rmsnorm_quant(ctx.handle, d, routing, _buf("x", x, dt, _span(rows, d.ldx, d.C), dev, True),
                                      _buf("residual", residual, dt, _span(rows, d.ld_res, d.C), dev, True),
                                      _buf("sum_out", sum_out, dt, _span(rows, d.ld_sum, d.C), dev, True),
-                                     _buf("q", q, torch.int8, _span(rows, d.ldq, d.C), dev, True), _buf("scale", scale, torch.float32, rows, dev),
+                                     _buf("q", q, ty.i8, _span(rows, d.ldq, d.C), dev, True), _buf("scale", scale, ty.f32, rows, dev),
                                      _buf("y", y, dt, _span(rows, d.ldy, d.C), dev, True), _stream_handle(stream)), "dsn_rmsnorm_quant")
 
 
@@ -455,10 +477,9 @@ def make_linear_i8_desc(R, C_in, C_out, k_in, k_out, W, w_scale, bias=None, bn_s
                         act=ACT_NONE, in_order=INPUT_ORDER, out_order=INPUT_ORDER, tail=TAIL_UNTOUCHED, ldx=None, ldw=None,
                         ldy=None) -> LinearI8Desc:
     """Linear layer on int8 rows and weights; leading dimensions default to the extents."""
-    import torch
     ldx, ldw, ldy = C_in if ldx is None else ldx, C_in if ldw is None else ldw, C_out if ldy is None else ldy
-    f = torch.float32
-    _buf("W", W, torch.int8, _span(C_out, ldw, C_in), rows=True)
+    f = _types().f32
+    _buf("W", W, _types().i8, _span(C_out, ldw, C_in), rows=True)
     for what, t, n in (("w_scale", w_scale, C_out), ("bias", bias, C_out), ("bn_scale", bn_scale, len(k_out) * C_out),
                        ("bn_shift", bn_shift, len(k_out) * C_out)):
         _buf(what, t, f, n)
@@ -474,15 +495,15 @@ def dsn_linear_i8_workspace_bytes(d: LinearI8Desc, B: int) -> int:
 
 
 def dsn_sliced_linear_i8(ctx: Context, d: LinearI8Desc, routing: Routing, x, x_scale, y, workspace=None, stream=None):
-    import torch
-    dt, rows, dev = _torch_dtype(d.y_dtype), routing.B * d.R, ctx.device
+    ty, rows, dev = _types(), routing.B * d.R, ctx.device
+    dt = ty.of_code.get(d.y_dtype)
     span = _span(rows, d.ldy, d.C_out)
     _buf("residual", d._keep[-1], dt, span, dev, True)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     if workspace is not None and workspace.get_device() != dev:
         raise DsnError(ERR_INVALID_ARG, f"workspace on {workspace.device}, expected cuda:{dev}")
-    _check(ctx.lib.dsn_sliced_linear_i8(ctx.handle, C.byref(d), C.byref(routing), _buf("x", x, torch.int8, _span(rows, d.ldx, d.C_in), dev, True),
-                                        _buf("x_scale", x_scale, torch.float32, rows, dev), _buf("y", y, dt, span, dev, True), _ptr(workspace),
+    _check(ctx.lib.dsn_sliced_linear_i8(ctx.handle, d, routing, _buf("x", x, ty.i8, _span(rows, d.ldx, d.C_in), dev, True),
+                                        _buf("x_scale", x_scale, ty.f32, rows, dev), _buf("y", y, dt, span, dev, True), _ptr(workspace),
                                         ws_bytes, _stream_handle(stream)), "dsn_sliced_linear_i8")
 
 
@@ -500,10 +521,10 @@ def make_rotary_desc(dtype, N, H, D, heads, pairs, vectors=3, rotated=2, base=10
 
 
 def dsn_rotary_axes(ctx: Context, d: RotaryDesc, routing: Routing, positions, x, y, stream=None):
-    import torch
-    dt, rows, dev = _torch_dtype(d.dtype), routing.B * d.N, ctx.device
+    ty, rows, dev = _types(), routing.B * d.N, ctx.device
+    dt = ty.of_code.get(d.dtype)
     row = d.H * d.vectors * d.D
-    _check(ctx.lib.dsn_rotary_axes(ctx.handle, C.byref(d), C.byref(routing),
-                                   _buf("positions", positions, torch.int32, d.n_axes * (d.N if d.shared_positions else rows), dev),
+    _check(ctx.lib.dsn_rotary_axes(ctx.handle, d, routing,
+                                   _buf("positions", positions, ty.i32, d.n_axes * (d.N if d.shared_positions else rows), dev),
                                    _buf("x", x, dt, _span(rows, d.ldx, row), dev, True), _buf("y", y, dt, _span(rows, d.ldy, row), dev, True),
                                    _stream_handle(stream)), "dsn_rotary_axes")

@@ -1274,12 +1274,12 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
   if (r->B == 0) return DSN_OK;
   NormParams p;
   memset(&p, 0, sizeof(p));
-  int max_k = 1;
   for (int t = 0; t < d->T; ++t) {
     p.k[t] = (int16_t)d->k[t];
-    if (d->k[t] > max_k) max_k = d->k[t];
+    if (d->k[t] > p.max_k) p.max_k = d->k[t];
   }
   p.R = d->R; p.B = r->B; p.G = r->G; p.T = d->T;
+  p.by_R = dsn_fast_div((uint32_t)d->R);
   p.in_input_order = d->in_order == DSN_INPUT_ORDER;
   p.out_input_order = d->out_order == DSN_INPUT_ORDER;
   p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
@@ -1287,7 +1287,7 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
   p.ldx = d->ldx; p.ld_res = d->ld_res; p.ld_sum = d->ld_sum; p.ldq = d->ldq; p.ldy = d->ldy;
   p.weight = d->weight; p.eps = d->eps;
   count_launch(ctx, &dsn_stats::launches_norm);
-  return dsn_launch_norm_quant(p, d->dtype == DSN_F32, max_k, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+  return dsn_launch_norm_quant(p, d->dtype == DSN_F32, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }
 
 size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B) {
@@ -1339,19 +1339,25 @@ int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r
   memset(&p, 0, sizeof(p));
   const int n[3] = {d->pairs[0], d->n_axes > 1 ? d->pairs[1] : 0, d->n_axes > 2 ? d->pairs[2] : 0};
   p.pairs = n[0] + n[1] + n[2];
+  // Turns per unit of position in units of 2^-64 (at most 2^64 / 2 pi: fits).  A ladder is a geometric sequence: its ratio once, then
+  // products in 64-bit mantissas (127 of them are off by 2^-55, which 2^31 positions make 2^-26 of a turn).
   int i = 0;
-  for (int a = 0; a < d->n_axes; ++a)
-    for (int j = 0; j < n[a]; ++j, ++i) {
-      // turns per unit of position in units of 2^-64 (at most 2^64 / 2 pi: fits), from 64-bit mantissas
-      const long double ex = d->ladder == DSN_ROTARY_SHARED ? (long double)i / p.pairs : (long double)j / n[a];
-      p.freq[i] = (uint64_t)(powl((long double)d->base, -ex) * 18446744073709551616.0L / 6.283185307179586476925286766559L + 0.5L);
+  long double f = 1.0L, ratio = powl((long double)d->base, -1.0L / p.pairs);
+  for (int a = 0; a < d->n_axes; ++a) {
+    if (d->ladder == DSN_ROTARY_PER_AXIS) {
+      f = 1.0L;
+      ratio = powl((long double)d->base, -1.0L / n[a]);
+    }
+    for (int j = 0; j < n[a]; ++j, ++i, f *= ratio) {
+      p.freq[i] = (uint64_t)(f * (18446744073709551616.0L / 6.283185307179586476925286766559L) + 0.5L);
       p.axis[i] = (uint8_t)a;
     }
-  int max_heads = 1;
+  }
   for (int t = 0; t < d->T; ++t) {
     p.heads[t] = (int16_t)d->heads[t];
-    if (d->heads[t] > max_heads) max_heads = d->heads[t];
+    if (d->heads[t] > p.max_heads) p.max_heads = d->heads[t];
   }
+  p.by_N = dsn_fast_div((uint32_t)d->N);
   p.N = d->N; p.D = d->D; p.vectors = d->vectors; p.rotated = d->rotated;
   p.B = r->B; p.G = r->G; p.T = d->T; p.grouped = d->order == DSN_GROUPED;
   p.shared = d->shared_positions != 0;
@@ -1363,7 +1369,7 @@ int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r
   p.positions = positions; p.x = x; p.y = y; p.ldx = d->ldx; p.ldy = d->ldy;
   const int aligned = aligned16(x) && aligned16(y) && (d->ldx * es) % 16 == 0 && (d->ldy * es) % 16 == 0;
   count_launch(ctx, &dsn_stats::launches_rotary);
-  return dsn_launch_rotary(p, d->dtype == DSN_F32, max_heads, aligned, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+  return dsn_launch_rotary(p, d->dtype == DSN_F32, aligned, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }
 
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L) {

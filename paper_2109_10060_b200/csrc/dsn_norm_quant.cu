@@ -2,37 +2,55 @@
 //   h = x + residual;  n = h / sqrt(mean h^2 + eps) * w;  s = max|n| / 127;  q = round(h w * 127 / max|h w|).
 // The factor 1 / sqrt(...) is common to a row, so it drops out of the code: the sum of squares and the maximum of |h w|
 // come out of ONE reduction, and the codes do not depend on the order of the sum.
-// Bound by memory: a row lives in the registers of 32 .. 1024 threads between its only read and its writes; eight
-// columns (16 bytes of bf16, 32 of fp32) a thread and step.
+// Bound by memory once the instructions per element are few: a row lives in the registers of 32 .. 1024 threads between its only
+// read and its writes, eight columns (16 bytes of bf16, 32 of fp32) a thread and step, two columns an instruction.  A thread keeps its
+// columns' weights in registers and walks rows with the stride of the grid; the place of the next row is looked up a row ahead.
+#include "dsn_gemm_device.cuh"
 #include "dsn_transformer.cuh"
 
 namespace {
 
+using dsn_gemm::fadd2;
+using dsn_gemm::ffma2;
+using dsn_gemm::pack2;
+using dsn_gemm::unpack2;
+
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+__device__ __forceinline__ float max_abs3_nan(float m, uint64_t v2) {
+  float a, b, r;
+  unpack2(v2, a, b);
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+  return r;
+}
 
+// Eight columns as four pairs of fp32.
 template <bool F32>
 struct Elem;
 template <>
 struct Elem<false> {
   typedef __nv_bfloat16 type;
-  static __device__ __forceinline__ void load8(const type* p, float (&v)[8]) {
+  static __device__ __forceinline__ void load(const type* p, uint64_t (&v)[4]) {
     const uint4 a = *reinterpret_cast<const uint4*>(p);
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
   }
-  static __device__ __forceinline__ void store8(type* p, const float (&v)[8]) {
+  static __device__ __forceinline__ void store(type* p, const uint64_t (&v)[4]) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      float a, b;
+      unpack2(v[i], a, b);
+      __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
       w[i] = *reinterpret_cast<uint32_t*>(&h);
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -43,220 +61,301 @@ struct Elem<false> {
 template <>
 struct Elem<true> {
   typedef float type;
-  static __device__ __forceinline__ void load8(const type* p, float (&v)[8]) {
+  static __device__ __forceinline__ void load(const type* p, uint64_t (&v)[4]) {
     const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = pack2(a.x, a.y); v[1] = pack2(a.z, a.w); v[2] = pack2(b.x, b.y); v[3] = pack2(b.z, b.w);
   }
-  static __device__ __forceinline__ void store8(type* p, const float (&v)[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  static __device__ __forceinline__ void store(type* p, const uint64_t (&v)[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
   }
   static __device__ __forceinline__ float load1(const type* p) { return *p; }
   static __device__ __forceinline__ void store1(type* p, float v) { *p = v; }
 };
+// A step of which only the first n columns belong to the row (n < 8, none or fewer than none included).
+template <bool F32>
+__device__ __forceinline__ void load_part(const typename Elem<F32>::type* p, const typename Elem<F32>::type* res, int n, uint64_t (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = 0.f, b = 0.f;
+    if (2 * i < n) a = Elem<F32>::load1(p + 2 * i) + (res ? Elem<F32>::load1(res + 2 * i) : 0.f);
+    if (2 * i + 1 < n) b = Elem<F32>::load1(p + 2 * i + 1) + (res ? Elem<F32>::load1(res + 2 * i + 1) : 0.f);
+    v[i] = pack2(a, b);
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void store_part(typename Elem<F32>::type* p, int n, const uint64_t (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpack2(v[i], a, b);
+    if (2 * i < n) Elem<F32>::store1(p + 2 * i, a);
+    if (2 * i + 1 < n) Elem<F32>::store1(p + 2 * i + 1, b);
+  }
+}
 
-// (sum, maximum) over the TPR threads of a row; every thread of the CTA calls this.
+// (sum, maximum) over the TPR threads of a row; every thread of the CTA calls this.  `buf` alternates between two calls in a row: one
+// barrier is enough then.
 template <int TPR, int THREADS>
-__device__ __forceinline__ void row_reduce(float& ss, float& mx) {
+__device__ __forceinline__ void row_reduce(float& ss, float& mx, int& buf) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     ss += __shfl_xor_sync(0xffffffffu, ss, o);
     mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   }
   if constexpr (TPR > 32) {
-    __shared__ float2 part[THREADS / 32];
+    __shared__ float2 part[2][THREADS / 32];
     const int warp = threadIdx.x >> 5;
-    __syncthreads();   // an earlier reduction's reads are done
-    if ((threadIdx.x & 31) == 0) part[warp] = make_float2(ss, mx);
+    if ((threadIdx.x & 31) == 0) part[buf][warp] = make_float2(ss, mx);
     __syncthreads();
     const int w0 = warp & ~(TPR / 32 - 1);
     ss = 0.f;
     mx = 0.f;
 #pragma unroll
     for (int i = 0; i < TPR / 32; ++i) {
-      const float2 v = part[w0 + i];
+      const float2 v = part[buf][w0 + i];
       ss += v.x;
       mx = max_nan(mx, v.y);
     }
+    buf ^= 1;
   }
 }
 
-// TPR threads a row, VPT steps of eight columns a thread, THREADS a CTA.
-template <bool F32, int TPR, int VPT, int THREADS>
+struct RowAt {
+  int k;             // 0: no such row
+  int64_t in, out;   // row numbers
+};
+__device__ __forceinline__ RowAt locate_row(const NormParams& p, uint32_t row) {
+  const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
+  RowAt a{0, 0, 0};
+  if (pos < p.B) {
+    const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
+    if (at.slice >= 0) {
+      a.k = p.k[at.slice];
+      a.in = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
+      a.out = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
+    }
+  }
+  return a;
+}
+
+// TPR threads a row, VPT steps of eight columns a thread, THREADS a CTA; RES: there is a residual.
+template <bool F32, bool RES, int TPR, int VPT, int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_quant_kernel(const __grid_constant__ NormParams p) {
   typedef Elem<F32> E;
   typedef typename E::type elem;
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
-  const uint32_t row = blockIdx.x * (uint32_t)(THREADS / TPR) + threadIdx.x / TPR;   // B * R < 2^31
+  constexpr int RPC = THREADS / TPR;
+  const uint32_t rows = (uint32_t)p.B * (uint32_t)p.R;   // below 2^31
+  const uint32_t stride = gridDim.x * RPC;
   const int t = threadIdx.x % TPR;
-  const int pos = (int)(row / (uint32_t)p.R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
-  PosInfo at{0, -1};
-  if (pos < p.B) at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
-  const int k = at.slice < 0 ? 0 : p.k[at.slice];   // 0: this row does not exist; its threads only take part in the barriers
-  const int64_t in_row = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
-  const int64_t out_row = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
-  const elem* x = static_cast<const elem*>(p.x) + in_row * p.ldx;
-  const elem* res = p.residual ? static_cast<const elem*>(p.residual) + in_row * p.ld_res : nullptr;
+  uint32_t row = blockIdx.x * RPC + threadIdx.x / TPR;
+  RowAt next = locate_row(p, row);
 
-  float h[VPT][8], w[VPT][8];
+  uint64_t w[VPT][4];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int c = 8 * (t + j * TPR);
-    if (c + 8 <= k) {
-      E::load8(x + c, h[j]);
-      if (res) {
-        float b[8];
-        E::load8(res + c, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[j][i] += b[i];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        h[j][i] = 0.f;
-        if (c + i < k) h[j][i] = E::load1(x + c + i) + (res ? E::load1(res + c + i) : 0.f);
-      }
+    for (int i = 0; i < 4; ++i) w[j][i] = pack2(1.f, 1.f);
+    if (p.weight) {
+      if (c + 8 <= p.max_k) Elem<true>::load(p.weight + c, w[j]);
+      else if (c < p.max_k) load_part<true>(p.weight + c, nullptr, p.max_k - c, w[j]);
     }
   }
-  float ss = 0.f, mx = 0.f;
+  int buf = 0;
+  for (uint32_t base = blockIdx.x * RPC; base < rows; base += stride) {   // the CTA's rows leave the loop together: barriers inside
+    const RowAt cur = next;
+    const int k = cur.k;
+    uint64_t h[VPT][4];
+    {
+      const elem* x = static_cast<const elem*>(p.x) + cur.in * p.ldx;
+      const elem* res = RES ? static_cast<const elem*>(p.residual) + cur.in * p.ld_res : nullptr;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int c = 8 * (t + j * TPR);
-    if (p.weight && c + 8 <= k) {
-      Elem<true>::load8(p.weight + c, w[j]);
-    } else {
+      for (int j = 0; j < VPT; ++j) {
+        const int c = 8 * (t + j * TPR);
+        if (c + 8 <= k) {
+          E::load(x + c, h[j]);
+          if (RES) {
+            uint64_t b[4];
+            E::load(res + c, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[j][i] = (p.weight && c + i < k) ? p.weight[c + i] : 1.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      ss = fmaf(h[j][i], h[j][i], ss);
-      mx = max_nan(mx, fabsf(h[j][i] * w[j][i]));
-    }
-  }
-  if (p.sum) {
-    elem* d = static_cast<elem*>(p.sum) + in_row * p.ld_sum;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int c = 8 * (t + j * TPR);
-      if (c + 8 <= k) {
-        E::store8(d + c, h[j]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (c + i < k) E::store1(d + c + i, h[j][i]);
-      }
-    }
-  }
-  if (!p.q && !p.y) return;
-  row_reduce<TPR, THREADS>(ss, mx);
-  float eps = p.eps;
-  // The squares (or a product with the weight) left the range of fp32, or the row holds something that is no number.  Rare, and the
-  // same for all threads of a row, but not for all rows of the CTA: the second reduction is entered by all when one row asks.
-  const bool redo = !(ss < INFINITY) || !(mx < INFINITY);
-  if (TPR > 32 ? __syncthreads_or(redo) : __any_sync(0xffffffffu, redo)) {
-    float top = 0.f, any = 0.f;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(h[j][i]));
-    row_reduce<TPR, THREADS>(any, top);
-    // h is scaled by a power of two to less than 4 (exact; what underflows is below 2^-120 of the row's largest value)
-    const uint32_t top_exp = __float_as_uint(top) >> 23;
-    const float f = (redo && top < INFINITY && top > 2.f) ? __uint_as_float((top_exp < 253u ? 254u - top_exp : 1u) << 23) : 1.f;
-    float ss2 = 0.f, mx2 = 0.f;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        h[j][i] *= f;
-        ss2 = fmaf(h[j][i], h[j][i], ss2);
-        mx2 = max_nan(mx2, fabsf(h[j][i] * w[j][i]));
-      }
-    row_reduce<TPR, THREADS>(ss2, mx2);
-    ss = ss2;
-    mx = mx2;
-    eps = eps * f * f;
-    if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);   // NaN or infinity in the row: NaN comes out
-  }
-  if (k == 0) return;
-  const float rs = rsqrtf(ss / (float)k + eps);
-  if (p.q) {
-    // a maximum below 2^-120 would overflow 127 / max: such a row is scaled up first (exact)
-    const float up = mx < 7.52316385e-37f ? 1.32922800e36f : 1.f;
-    const float inv = mx > 0.f ? __fdiv_rn(127.f, mx * up) : (mx == 0.f ? 0.f : mx);
-    const float scale = __fdiv_rn(mx * rs, 127.f);
-    int8_t* q = p.q + out_row * p.ldq;
-    elem* y = p.y ? static_cast<elem*>(p.y) + out_row * p.ldy : nullptr;
-    if (t == 0) p.scale[out_row] = scale;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int c = 8 * (t + j * TPR);
-      uint32_t code[2] = {0u, 0u};
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int n = __float2int_rn(__fmul_rn(__fmul_rn(h[j][i], w[j][i]) * up, inv));   // NaN gives 0
-        code[i >> 2] |= (uint32_t)(n & 0xff) << (8 * (i & 3));
-        v[i] = (float)n * scale;
-      }
-      if (c + 8 <= k) {
-        *reinterpret_cast<uint2*>(q + c) = make_uint2(code[0], code[1]);
-        if (y) E::store8(y + c, v);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (c + i < k) {
-            q[c + i] = (int8_t)(code[i >> 2] >> (8 * (i & 3)));
-            if (y) E::store1(y + c + i, v[i]);
+            for (int i = 0; i < 4; ++i) h[j][i] = fadd2(h[j][i], b[i]);
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h[j][i] = 0ull;
+          if (c < k) load_part<F32>(x + c, res ? res + c : nullptr, k - c, h[j]);
+        }
       }
     }
-  } else {
-    elem* y = static_cast<elem*>(p.y) + out_row * p.ldy;
-    const float f = mx >= 0.f ? rs : mx;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
+    row += stride;
+    next = locate_row(p, row < rows ? row : rows);
+    // product with the weights; columns at and beyond k count as zero whatever the weight there
+    auto product = [&](int j, uint64_t (&v)[4]) {
       const int c = 8 * (t + j * TPR);
-      float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = h[j][i] * w[j][i] * f;
-      if (c + 8 <= k) {
-        E::store8(y + c, v);
-      } else {
+      for (int i = 0; i < 4; ++i) v[i] = fmul2(h[j][i], w[j][i]);
+      if (c + 8 > k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (c + i < k) E::store1(y + c + i, v[i]);
+        for (int i = 0; i < 4; ++i) {
+          float a, b;
+          unpack2(v[i], a, b);
+          v[i] = pack2(c + 2 * i < k ? a : 0.f, c + 2 * i + 1 < k ? b : 0.f);
+        }
+      }
+    };
+    float ss, mx;
+    auto measure = [&]() {
+      uint64_t s2 = 0ull;
+      mx = 0.f;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        uint64_t v[4];
+        product(j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s2 = ffma2(h[j][i], h[j][i], s2);
+          mx = max_abs3_nan(mx, v[i]);
+        }
+      }
+      float a, b;
+      unpack2(s2, a, b);
+      ss = a + b;
+      row_reduce<TPR, THREADS>(ss, mx, buf);
+    };
+    if (p.sum) {
+      elem* d = static_cast<elem*>(p.sum) + cur.in * p.ld_sum;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = 8 * (t + j * TPR);
+        if (c + 8 <= k) E::store(d + c, h[j]);
+        else if (c < k) store_part<F32>(d + c, k - c, h[j]);
+      }
+      if (!p.q && !p.y) continue;
+    }
+    measure();
+    // n = h w rs.  Where the squares (or a product with the weight) left the range of fp32, 127 / max would, or the row holds something
+    // that is no number, the row is looked at again: rare, and the same for all threads of a row, but not for all rows of the CTA.
+    float rs = rsqrtf(ss / (float)k + p.eps);
+    const bool redo = !(ss < INFINITY) || !(mx < INFINITY) || (mx < 7.52316385e-37f && mx > 0.f);
+    if (TPR == THREADS || TPR == 32 ? redo : (bool)__syncthreads_or(redo)) {
+      const float ss1 = ss;
+      float top = 0.f, none = 0.f;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max_abs3_nan(top, h[j][i]);
+      row_reduce<TPR, THREADS>(none, top, buf);
+      // h times a power of two (exact; what underflows is below 2^-120 of the row's largest value), so that its largest is 1 .. 4
+      float f = 1.f;
+      if (redo && top < INFINITY && top > 0.f) {
+        const int e = (int)(__float_as_uint(top) >> 23);
+        f = __uint_as_float((uint32_t)(e > 252 ? 1 : (e < 1 ? 253 : 254 - e)) << 23);
+      }
+      const uint64_t f2 = pack2(f, f);
+#pragma unroll
+      for (int j = 0; j < VPT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[j][i] = fmul2(h[j][i], f2);
+      measure();
+      if (f < 1.f) rs = rsqrtf(ss / (float)k + p.eps * f * f);
+      else if (f > 1.f) rs = rsqrtf(ss1 / (float)k + p.eps) / f;         // eps outweighs squares this small
+      if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);          // NaN or infinity in the row: NaN comes out
+    }
+    if (k == 0) continue;
+    elem* y = p.y ? static_cast<elem*>(p.y) + cur.out * p.ldy : nullptr;
+    if (p.q) {
+      const float inv = mx > 0.f ? __fdiv_rn(127.f, mx) : mx;             // a row of zeros: 0; NaN stays
+      const float scale = __fdiv_rn(mx * rs, 127.f);
+      const uint32_t keep = mx < INFINITY ? 0xffffffffu : 0u;             // a row that is no number has the codes 0
+      const uint64_t inv2 = pack2(inv, inv), scale2 = pack2(scale, scale);
+      const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f);
+      int8_t* q = p.q + cur.out * p.ldq;
+      if (t == 0) p.scale[cur.out] = scale;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = 8 * (t + j * TPR);
+        uint64_t v[4];
+        uint32_t b[8];
+        product(j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // the sum with 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves its low byte in the low byte
+          const uint64_t m = fadd2(fmul2(v[i], inv2), magic);
+          b[2 * i] = (uint32_t)m;
+          b[2 * i + 1] = (uint32_t)(m >> 32);
+          v[i] = fmul2(fadd2(m, nmagic), scale2);
+        }
+        const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) & keep;
+        const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410) & keep;
+        if (c + 8 <= k) {
+          *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
+          if (y) E::store(y + c, v);
+        } else if (c < k) {
+#pragma unroll
+          for (int i = 0; i < 7; ++i)
+            if (c + i < k) q[c + i] = (int8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+          if (y) store_part<F32>(y + c, k - c, v);
+        }
+      }
+    } else {
+      const float f = mx >= 0.f ? rs : mx;
+      const uint64_t f2 = pack2(f, f);
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = 8 * (t + j * TPR);
+        uint64_t v[4];
+        product(j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fmul2(v[i], f2);
+        if (c + 8 <= k) E::store(y + c, v);
+        else if (c < k) store_part<F32>(y + c, k - c, v);
       }
     }
   }
 }
 
-template <bool F32, int TPR, int VPT>
-cudaError_t launch(const NormParams& p, cudaStream_t s) {
+template <bool F32, bool RES, int TPR, int VPT>
+cudaError_t launch(const NormParams& p, int sm_count, cudaStream_t s) {
   constexpr int THREADS = TPR > 128 ? TPR : 128;
-  const int64_t rows = (int64_t)p.B * p.R;
-  const int per = THREADS / TPR;
-  return dsn_launch(norm_quant_kernel<F32, TPR, VPT, THREADS>, dim3((unsigned)((rows + per - 1) / per)), dim3(THREADS), 0, s, 1, p);
+  static int resident[DSN_MAX_DEVICES] = {};   // CTAs per SM of this form
+  auto kernel = norm_quant_kernel<F32, RES, TPR, VPT, THREADS>;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= DSN_MAX_DEVICES) return cudaErrorInvalidDevice;
+  if (resident[dev] == 0) {
+    int n = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, THREADS, 0);
+    if (e != cudaSuccess) return e;
+    resident[dev] = n > 0 ? n : 1;
+  }
+  const int64_t rows = (int64_t)p.B * p.R, ctas = (rows + THREADS / TPR - 1) / (THREADS / TPR);
+  const int64_t most = (int64_t)sm_count * resident[dev];
+  return dsn_launch(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), 0, s, 1, p);
 }
 
-template <bool F32>
-cudaError_t pick(const NormParams& p, int max_k, cudaStream_t s) {
-  const int steps = (max_k + 7) / 8;
-  if (steps <= 32) return launch<F32, 32, 1>(p, s);
-  if (steps <= 64) return launch<F32, 32, 2>(p, s);
-  if (steps <= 128) return launch<F32, 64, 2>(p, s);
-  if (steps <= 256) return launch<F32, 128, 2>(p, s);
-  if (steps <= 512) return launch<F32, 256, 2>(p, s);
-  if (steps <= 1024) return launch<F32, 512, 2>(p, s);
-  if (steps <= 2048) return launch<F32, 1024, 2>(p, s);
-  return launch<F32, 1024, 4>(p, s);
+template <bool F32, bool RES>
+cudaError_t pick(const NormParams& p, int sm_count, cudaStream_t s) {
+  const int steps = (p.max_k + 7) / 8;
+  if (steps <= 32) return launch<F32, RES, 32, 1>(p, sm_count, s);
+  if (steps <= 64) return launch<F32, RES, 32, 2>(p, sm_count, s);
+  if (steps <= 128) return launch<F32, RES, 64, 2>(p, sm_count, s);
+  if (steps <= 256) return launch<F32, RES, 128, 2>(p, sm_count, s);
+  if (steps <= 512) return launch<F32, RES, 256, 2>(p, sm_count, s);
+  if (steps <= 1024) return launch<F32, RES, 512, 2>(p, sm_count, s);
+  if (steps <= 2048) return launch<F32, RES, 1024, 2>(p, sm_count, s);
+  return launch<F32, RES, 1024, 4>(p, sm_count, s);
 }
 
 }  // namespace
 
-cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int max_k, cudaStream_t s) {
-  return f32 ? pick<true>(p, max_k, s) : pick<false>(p, max_k, s);
+cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int sm_count, cudaStream_t s) {
+  if (p.residual) return f32 ? pick<true, true>(p, sm_count, s) : pick<false, true>(p, sm_count, s);
+  return f32 ? pick<true, false>(p, sm_count, s) : pick<false, false>(p, sm_count, s);
 }

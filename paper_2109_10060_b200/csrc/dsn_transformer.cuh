@@ -4,6 +4,17 @@
 
 #include "dsn_internal.cuh"
 
+// Quotient of n < 2^31 by a divisor fixed on the host: (umulhi(n, mul) + n) >> shift.
+struct FastDiv {
+  uint32_t mul, shift, d;
+};
+inline FastDiv dsn_fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return FastDiv{(uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1), l, d};
+}
+__device__ __forceinline__ uint32_t dsn_div(uint32_t n, const FastDiv& f) { return (__umulhi(n, f.mul) + n) >> f.shift; }
+
 // Where a grouped position lies: its sample and the slice of its group.  Up to 32 groups take one load per lane, more
 // a binary search.  All lanes of the warp call this with the same arguments; slice < 0: no work at this position.
 struct PosInfo {
@@ -36,7 +47,8 @@ __device__ __forceinline__ PosInfo dsn_locate_warp(int p, int G, int T, const in
 
 struct NormParams {
   int16_t k[DSN_MAX_SLICES];
-  int32_t R, B, G, T;
+  int32_t R, B, G, T, max_k;
+  FastDiv by_R;
   int32_t in_input_order, out_input_order;
   const int32_t* offsets;
   const int32_t* perm;
@@ -51,13 +63,14 @@ struct NormParams {
   const float* weight;
   float eps;
 };
-cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int max_k, cudaStream_t s);
+cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int sm_count, cudaStream_t s);
 
 struct RotaryParams {
   uint64_t freq[128];   // turns per unit of position, in units of 2^-64
   uint8_t axis[128];
   int16_t heads[DSN_MAX_SLICES];
-  int32_t N, D, vectors, rotated, pairs;
+  int32_t N, D, vectors, rotated, pairs, max_heads;
+  FastDiv by_N;
   int32_t B, G, T, grouped;
   int32_t n_pos;        // rows of one axis of `positions`
   int32_t shared, interleaved, inverse, in_place;
@@ -69,7 +82,7 @@ struct RotaryParams {
   void* y;
   int64_t ldx, ldy;
 };
-cudaError_t dsn_launch_rotary(const RotaryParams& p, int f32, int max_heads, int aligned, cudaStream_t s);
+cudaError_t dsn_launch_rotary(const RotaryParams& p, int f32, int aligned, int sm_count, cudaStream_t s);
 
 // 8-bit linear layer on CTA pairs: `g` as in the bf16 pair kernel (maps on bytes, 128 a chunk; y, residual of either type)
 struct GemmI8Params {
