@@ -439,8 +439,8 @@ size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B);
 int dsn_sliced_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const dsn_routing* r, const int8_t* x,
                          const float* x_scale, void* y, void* workspace, size_t ws_bytes, void* stream);
 
-/* positions: device int32, any values.  y may be x itself (same leading dimension): then only the turned elements are written;
- * otherwise the heads of a sample's path are written whole, the vectors and elements that do not turn copied. */
+/* positions: device int32, any values.  y may be x itself (same leading dimension).  The heads of a sample's path are written whole, the
+ * vectors and elements that do not turn as they were. */
 int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r, const int32_t* positions, const void* x,
                     void* y, void* stream);
 

@@ -1285,7 +1285,7 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
   p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
   p.x = x; p.residual = residual; p.sum = sum; p.q = q; p.scale = q_scale; p.y = y;
   p.ldx = d->ldx; p.ld_res = d->ld_res; p.ld_sum = d->ld_sum; p.ldq = d->ldq; p.ldy = d->ldy;
-  p.weight = d->weight; p.eps = d->eps;
+  p.weight = d->weight; p.eps = d->eps; p.status = ctx->d_status;
   count_launch(ctx, &dsn_stats::launches_norm);
   return dsn_launch_norm_quant(p, d->dtype == DSN_F32, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }
@@ -1358,7 +1358,7 @@ int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r
     if (d->heads[t] > p.max_heads) p.max_heads = d->heads[t];
   }
   p.by_N = dsn_fast_div((uint32_t)d->N);
-  p.N = d->N; p.D = d->D; p.vectors = d->vectors; p.rotated = d->rotated;
+  p.N = d->N; p.D = d->D; p.n_axes = d->n_axes; p.vectors = d->vectors; p.rotated = d->rotated;
   p.B = r->B; p.G = r->G; p.T = d->T; p.grouped = d->order == DSN_GROUPED;
   p.shared = d->shared_positions != 0;
   p.n_pos = p.shared ? d->N : r->B * d->N;
@@ -1366,6 +1366,7 @@ int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r
   p.inverse = d->inverse != 0;
   p.in_place = x == y;
   p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
+  p.status = ctx->d_status;
   p.positions = positions; p.x = x; p.y = y; p.ldx = d->ldx; p.ldy = d->ldy;
   const int aligned = aligned16(x) && aligned16(y) && (d->ldx * es) % 16 == 0 && (d->ldy * es) % 16 == 0;
   count_launch(ctx, &dsn_stats::launches_rotary);

@@ -2,9 +2,13 @@
 //   h = x + residual;  n = h / sqrt(mean h^2 + eps) * w;  s = max|n| / 127;  q = round(h w * 127 / max|h w|).
 // The factor 1 / sqrt(...) is common to a row, so it drops out of the code: the sum of squares and the maximum of |h w|
 // come out of ONE reduction, and the codes do not depend on the order of the sum.
-// Bound by memory once the instructions per element are few: a row lives in the registers of 32 .. 1024 threads between its only
-// read and its writes, eight columns (16 bytes of bf16, 32 of fp32) a thread and step, two columns an instruction.  A thread keeps its
-// columns' weights in registers and walks rows with the stride of the grid; the place of the next row is looked up a row ahead.
+// Bound by memory, once the bytes in flight do not depend on the registers of the threads that work and the instructions per element are
+// few.  Ring form: a group of 16 .. 256 threads has a ring of shared-memory slots of its own, which bulk copies fill with the rows to
+// come (rows are looked up 32 at a time, one a lane); it takes a row into registers, eight columns a thread and step, asks for the row
+// that goes into the free slot, and works two columns an instruction.  (One fetching warp for all groups was the bottleneck
+// of short rows: 59 us on 50,432 rows of 384 columns.)  The weights of a thread's columns stay in its registers.  Direct form
+// (few rows, where the ring's start-up is longer than the rows; rows too long for a ring): the same arithmetic on rows read
+// straight into registers.
 #include "dsn_gemm_device.cuh"
 #include "dsn_transformer.cuh"
 
@@ -97,40 +101,14 @@ __device__ __forceinline__ void store_part(typename Elem<F32>::type* p, int n, c
   }
 }
 
-// (sum, maximum) over the TPR threads of a row; every thread of the CTA calls this.  `buf` alternates between two calls in a row: one
-// barrier is enough then.
-template <int TPR, int THREADS>
-__device__ __forceinline__ void row_reduce(float& ss, float& mx, int& buf) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-  }
-  if constexpr (TPR > 32) {
-    __shared__ float2 part[2][THREADS / 32];
-    const int warp = threadIdx.x >> 5;
-    if ((threadIdx.x & 31) == 0) part[buf][warp] = make_float2(ss, mx);
-    __syncthreads();
-    const int w0 = warp & ~(TPR / 32 - 1);
-    ss = 0.f;
-    mx = 0.f;
-#pragma unroll
-    for (int i = 0; i < TPR / 32; ++i) {
-      const float2 v = part[buf][w0 + i];
-      ss += v.x;
-      mx = max_nan(mx, v.y);
-    }
-    buf ^= 1;
-  }
-}
-
 struct RowAt {
   int k;             // 0: no such row
+  int part;          // the bytes behind the last whole 16 are not in shared memory
   int64_t in, out;   // row numbers
 };
 __device__ __forceinline__ RowAt locate_row(const NormParams& p, uint32_t row) {
   const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
-  RowAt a{0, 0, 0};
+  RowAt a{0, 0, 0, 0};
   if (pos < p.B) {
     const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
     if (at.slice >= 0) {
@@ -142,21 +120,34 @@ __device__ __forceinline__ RowAt locate_row(const NormParams& p, uint32_t row) {
   return a;
 }
 
-// TPR threads a row, VPT steps of eight columns a thread, THREADS a CTA; RES: there is a residual.
-template <bool F32, bool RES, int TPR, int VPT, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_quant_kernel(const __grid_constant__ NormParams p) {
-  typedef Elem<F32> E;
-  typedef typename E::type elem;
-  dsn_grid_dependency_wait();
-  dsn_grid_launch_dependents();
-  constexpr int RPC = THREADS / TPR;
-  const uint32_t rows = (uint32_t)p.B * (uint32_t)p.R;   // below 2^31
-  const uint32_t stride = gridDim.x * RPC;
-  const int t = threadIdx.x % TPR;
-  uint32_t row = blockIdx.x * RPC + threadIdx.x / TPR;
-  RowAt next = locate_row(p, row);
+// (sum, maximum) over the TPR threads of a row: a group of its own named barrier `id` where it is more than a warp.  `part`
+// holds two sets of one entry a warp, taken in turn: one barrier a call is enough then.
+template <int TPR>
+__device__ __forceinline__ void row_reduce(float& ss, float& mx, float2* part, int& turn, int id) {
+#pragma unroll
+  for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
+    ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  }
+  if constexpr (TPR > 32) {
+    constexpr int NW = TPR / 32;
+    float2* mine = part + turn * NW;
+    if ((threadIdx.x & 31) == 0) mine[(threadIdx.x >> 5) % NW] = make_float2(ss, mx);
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(TPR) : "memory");
+    ss = 0.f;
+    mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const float2 v = mine[i];
+      ss += v.x;
+      mx = max_nan(mx, v.y);
+    }
+    turn ^= 1;
+  }
+}
 
-  uint64_t w[VPT][4];
+template <int TPR, int VPT>
+__device__ __forceinline__ void load_weights(const NormParams& p, int t, uint64_t (&w)[VPT][4]) {
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int c = 8 * (t + j * TPR);
@@ -167,182 +158,359 @@ __global__ void __launch_bounds__(THREADS) norm_quant_kernel(const __grid_consta
       else if (c < p.max_k) load_part<true>(p.weight + c, nullptr, p.max_k - c, w[j]);
     }
   }
-  int buf = 0;
-  for (uint32_t base = blockIdx.x * RPC; base < rows; base += stride) {   // the CTA's rows leave the loop together: barriers inside
+}
+
+// A row that lies in the registers of its TPR threads (h, zero at and beyond k) -> everything that is written for it.
+template <bool F32, int TPR, int VPT>
+__device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur, int t, uint64_t (&h)[VPT][4], const uint64_t (&w)[VPT][4], float2* part,
+                                           int& turn, int id) {
+  typedef Elem<F32> E;
+  typedef typename E::type elem;
+  const int k = cur.k;
+  // product with the weights; columns at and beyond k count as zero whatever the weight there
+  auto product = [&](int j, uint64_t (&v)[4]) {
+    const int c = 8 * (t + j * TPR);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = fmul2(h[j][i], w[j][i]);
+    if (c + 8 > k) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a, b;
+        unpack2(v[i], a, b);
+        v[i] = pack2(c + 2 * i < k ? a : 0.f, c + 2 * i + 1 < k ? b : 0.f);
+      }
+    }
+  };
+  float ss, mx;
+  auto measure = [&]() {
+    uint64_t s2 = 0ull;
+    mx = 0.f;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      uint64_t v[4];
+      product(j, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s2 = ffma2(h[j][i], h[j][i], s2);
+        mx = max_abs3_nan(mx, v[i]);
+      }
+    }
+    float a, b;
+    unpack2(s2, a, b);
+    ss = a + b;
+    row_reduce<TPR>(ss, mx, part, turn, id);
+  };
+  if (p.sum) {
+    elem* d = static_cast<elem*>(p.sum) + cur.in * p.ld_sum;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = 8 * (t + j * TPR);
+      if (c + 8 <= k) E::store(d + c, h[j]);
+      else if (c < k) store_part<F32>(d + c, k - c, h[j]);
+    }
+    if (!p.q && !p.y) return;
+  }
+  measure();
+  // n = h w rs.  Where the squares (or a product with the weight) left the range of fp32, 127 / max would, or the row holds something
+  // that is no number, the row is looked at again (rare; the same decision in all threads of the row).
+  const float rk = __fdividef(1.f, (float)k);
+  float rs = rsqrtf(ss * rk + p.eps);
+  const bool redo = !(ss < INFINITY) || !(mx < INFINITY) || (mx < 7.52316385e-37f && mx > 0.f);
+  if (TPR < 32 ? __any_sync(0xffffffffu, redo) : redo) {
+    const float ss1 = ss;
+    float top = 0.f, none = 0.f;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max_abs3_nan(top, h[j][i]);
+    row_reduce<TPR>(none, top, part, turn, id);
+    // h times a power of two (exact; what underflows is below 2^-120 of the row's largest value), so that its largest is 1 .. 4
+    float f = 1.f;
+    if (redo && top < INFINITY && top > 0.f) {
+      const int e = (int)(__float_as_uint(top) >> 23);
+      f = __uint_as_float((uint32_t)(e > 252 ? 1 : (e < 1 ? 253 : 254 - e)) << 23);
+    }
+    const uint64_t f2 = pack2(f, f);
+#pragma unroll
+    for (int j = 0; j < VPT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[j][i] = fmul2(h[j][i], f2);
+    measure();
+    if (f < 1.f) rs = rsqrtf(ss * rk + p.eps * f * f);
+    else if (f > 1.f) rs = rsqrtf(ss1 * rk + p.eps) / f;               // eps outweighs squares this small
+    if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);          // NaN or infinity in the row: NaN comes out
+  }
+  if (k == 0) return;
+  elem* y = p.y ? static_cast<elem*>(p.y) + cur.out * p.ldy : nullptr;
+  if (p.q) {
+    const float inv = mx > 0.f ? __fdiv_rn(127.f, mx) : mx;             // a row of zeros: 0; NaN stays
+    const float scale = mx * rs * (1.f / 127.f);
+    const uint32_t keep = mx < INFINITY ? 0xffffffffu : 0u;             // a row that is no number has the codes 0
+    const uint64_t inv2 = pack2(inv, inv), scale2 = pack2(scale, scale);
+    const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f);
+    int8_t* q = p.q + cur.out * p.ldq;
+    if (t == 0) p.scale[cur.out] = scale;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = 8 * (t + j * TPR);
+      if (c >= k) continue;
+      uint64_t v[4];
+      uint32_t b[8];
+      product(j, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // the sum with 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves its low byte in the low byte
+        const uint64_t m = fadd2(fmul2(v[i], inv2), magic);
+        b[2 * i] = (uint32_t)m;
+        b[2 * i + 1] = (uint32_t)(m >> 32);
+        v[i] = fmul2(fadd2(m, nmagic), scale2);
+      }
+      const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) & keep;
+      const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410) & keep;
+      if (c + 8 <= k) {
+        *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
+        if (y) E::store(y + c, v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+          if (c + i < k) q[c + i] = (int8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+        if (y) store_part<F32>(y + c, k - c, v);
+      }
+    }
+  } else {
+    const float f = mx >= 0.f ? rs : mx;
+    const uint64_t f2 = pack2(f, f);
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = 8 * (t + j * TPR);
+      if (c >= k) continue;
+      uint64_t v[4];
+      product(j, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = fmul2(v[i], f2);
+      if (c + 8 <= k) E::store(y + c, v);
+      else store_part<F32>(y + c, k - c, v);
+    }
+  }
+}
+
+// Direct form: rows read straight into registers, TPR threads (at least a warp) a row.
+template <bool F32, bool RES, int TPR, int VPT, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm_quant_kernel(const __grid_constant__ NormParams p) {
+  typedef Elem<F32> E;
+  typedef typename E::type elem;
+  __shared__ float2 part[TPR > 32 ? 2 * TPR / 32 : 1];
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  constexpr int RPC = THREADS / TPR;                     // more than one only where a row is a warp's
+  const uint32_t rows = (uint32_t)p.B * (uint32_t)p.R;   // below 2^31
+  const uint32_t stride = gridDim.x * RPC;
+  const int t = threadIdx.x % TPR;
+  uint32_t row = blockIdx.x * RPC + threadIdx.x / TPR;
+  RowAt next = locate_row(p, row);
+  uint64_t w[VPT][4];
+  load_weights<TPR, VPT>(p, t, w);
+  int turn = 0;
+  for (; row < rows; row += stride) {
     const RowAt cur = next;
     const int k = cur.k;
     uint64_t h[VPT][4];
-    {
-      const elem* x = static_cast<const elem*>(p.x) + cur.in * p.ldx;
-      const elem* res = RES ? static_cast<const elem*>(p.residual) + cur.in * p.ld_res : nullptr;
+    const elem* x = static_cast<const elem*>(p.x) + cur.in * p.ldx;
+    const elem* res = RES ? static_cast<const elem*>(p.residual) + cur.in * p.ld_res : nullptr;
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int c = 8 * (t + j * TPR);
-        if (c + 8 <= k) {
-          E::load(x + c, h[j]);
+    for (int j = 0; j < VPT; ++j) {
+      const int c = 8 * (t + j * TPR);
+      if (c + 8 <= k) {
+        E::load(x + c, h[j]);
+        if (RES) {
+          uint64_t b[4];
+          E::load(res + c, b);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h[j][i] = fadd2(h[j][i], b[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[j][i] = 0ull;
+        if (c < k) load_part<F32>(x + c, res ? res + c : nullptr, k - c, h[j]);
+      }
+    }
+    next = locate_row(p, row + stride < rows ? row + stride : rows);
+    finish_row<F32, TPR, VPT>(p, cur, t, h, w, part, turn, 0);
+  }
+}
+
+// Ring form.
+constexpr int kRingThreads = 256;
+constexpr int kRingDepth = 8;               // most slots of a group
+
+template <bool F32, bool RES, int TPR, int VPT>
+__global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const __grid_constant__ NormParams p, int depth, uint32_t row_bytes) {
+  typedef Elem<F32> E;
+  typedef typename E::type elem;
+  constexpr int RB = TPR < 32 ? 32 / TPR : 1;                       // rows a group (at least a warp) works on at once: a unit
+  constexpr int GT = TPR < 32 ? 32 : TPR, GROUPS = kRingThreads / GT;
+  constexpr int UB = 32 / RB;                                       // units that the lanes of a warp look up at once
+  constexpr int ES = F32 ? 4 : 2;
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t s_full[GROUPS][kRingDepth];
+  __shared__ RowAt s_at[GROUPS][kRingDepth][RB];
+  __shared__ float2 s_part[GROUPS][TPR > 32 ? 2 * TPR / 32 : 1];
+  __shared__ uint32_t s_abort;
+  const int g = threadIdx.x / GT, lane = threadIdx.x & 31;
+  const int sub = TPR < 32 ? lane / TPR : 0, t = threadIdx.x % TPR;
+  const bool fetches = (threadIdx.x % GT) < 32;                     // the group's first warp asks for rows
+  if (threadIdx.x < GROUPS * kRingDepth) dsn_gemm::mbar_init(dsn_gemm::smem_u32(&s_full[0][0] + threadIdx.x), 1);
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const uint32_t rows = (uint32_t)p.B * (uint32_t)p.R, units = (rows + RB - 1) / RB;
+  const uint32_t gid = blockIdx.x * GROUPS + g, ngroups = gridDim.x * GROUPS;
+  const int mine = gid < units ? (int)((units - gid + ngroups - 1) / ngroups) : 0;   // units of this group
+  const uint32_t copies = RES ? 2u : 1u, slot_bytes = RB * copies * row_bytes;
+  uint8_t* slots = ring + (size_t)g * depth * slot_bytes;
+  volatile uint32_t* abort_flag = &s_abort;
+
+  RowAt ahead{0, 0, 0, 0};   // this lane's row of the units being asked for
+  int asked = 0;             // units asked for
+  auto ask = [&](int slot) {
+    if (asked % UB == 0) {   // the next units' rows, one a lane
+      ahead = RowAt{0, 0, 0, 0};
+      const uint64_t wide = ((uint64_t)(asked + lane / RB) * ngroups + gid) * RB + lane % RB;
+      if (wide < rows) {
+        const uint32_t row = (uint32_t)wide;
+        const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
+        const PosInfo at = dsn_locate(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
+        if (at.slice >= 0) {
+          ahead.k = p.k[at.slice];
+          ahead.in = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
+          ahead.out = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
+          ahead.part = ahead.in + 1 == (int64_t)rows;   // behind the last row's columns nothing need be allocated
+        }
+      }
+      __syncwarp();
+    }
+    const uint32_t bytes = ahead.part ? (uint32_t)(ahead.k * ES) & ~15u : (uint32_t)(ahead.k * ES + 15) & ~15u;
+    const bool turn_of = lane / RB == asked % UB;
+    uint32_t all = bytes;
+#pragma unroll
+    for (int o = 1; o < RB; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    const uint32_t bar = dsn_gemm::smem_u32(&s_full[g][slot]);
+    if (turn_of) {
+      s_at[g][slot][lane % RB] = ahead;
+      __threadfence_block();
+    }
+    if (RB > 1) __syncwarp();   // every row's place is written before the barrier can complete
+    if (turn_of && lane % RB == 0) dsn_gemm::mbar_expect_tx(bar, copies * all);
+    if (RB > 1) __syncwarp();
+    if (turn_of && bytes) {
+      const uint32_t dst = dsn_gemm::smem_u32(slots) + (uint32_t)slot * slot_bytes + (uint32_t)(lane % RB) * copies * row_bytes;
+      dsn_bulk_load(dst, static_cast<const elem*>(p.x) + ahead.in * p.ldx, bytes, bar);
+      if (RES) dsn_bulk_load(dst + row_bytes, static_cast<const elem*>(p.residual) + ahead.in * p.ld_res, bytes, bar);
+    }
+    ++asked;
+  };
+  if (fetches)
+    for (int i = 0; i < depth && i < mine; ++i) ask(i);
+
+  uint64_t w[VPT][4];
+  load_weights<TPR, VPT>(p, t, w);
+  int turn = 0, slot = 0;
+  uint32_t phase = 0;
+  for (int n = 0; n < mine; ++n) {
+    const bool ok = dsn_gemm::mbar_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 71);
+    const RowAt cur = s_at[g][slot][sub];
+    const int k = cur.k;
+    const elem* xs = reinterpret_cast<const elem*>(slots + (size_t)slot * slot_bytes + (size_t)sub * copies * row_bytes);
+    const elem* rsd = reinterpret_cast<const elem*>(reinterpret_cast<const uint8_t*>(xs) + row_bytes);
+    uint64_t h[VPT][4];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = 8 * (t + j * TPR);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[j][i] = 0ull;
+      if (c < k) {
+        if (c + 8 <= k || !cur.part) {
+          E::load(xs + c, h[j]);
           if (RES) {
             uint64_t b[4];
-            E::load(res + c, b);
+            E::load(rsd + c, b);
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[j][i] = fadd2(h[j][i], b[i]);
           }
+          if (c + 8 > k) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float a, b;
+              unpack2(h[j][i], a, b);
+              h[j][i] = pack2(c + 2 * i < k ? a : 0.f, c + 2 * i + 1 < k ? b : 0.f);
+            }
+          }
         } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) h[j][i] = 0ull;
-          if (c < k) load_part<F32>(x + c, res ? res + c : nullptr, k - c, h[j]);
+          load_part<F32>(static_cast<const elem*>(p.x) + cur.in * p.ldx + c, RES ? static_cast<const elem*>(p.residual) + cur.in * p.ld_res + c : nullptr,
+                         k - c, h[j]);
         }
       }
     }
-    row += stride;
-    next = locate_row(p, row < rows ? row : rows);
-    // product with the weights; columns at and beyond k count as zero whatever the weight there
-    auto product = [&](int j, uint64_t (&v)[4]) {
-      const int c = 8 * (t + j * TPR);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = fmul2(h[j][i], w[j][i]);
-      if (c + 8 > k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float a, b;
-          unpack2(v[i], a, b);
-          v[i] = pack2(c + 2 * i < k ? a : 0.f, c + 2 * i + 1 < k ? b : 0.f);
-        }
-      }
-    };
-    float ss, mx;
-    auto measure = [&]() {
-      uint64_t s2 = 0ull;
-      mx = 0.f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        uint64_t v[4];
-        product(j, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s2 = ffma2(h[j][i], h[j][i], s2);
-          mx = max_abs3_nan(mx, v[i]);
-        }
-      }
-      float a, b;
-      unpack2(s2, a, b);
-      ss = a + b;
-      row_reduce<TPR, THREADS>(ss, mx, buf);
-    };
-    if (p.sum) {
-      elem* d = static_cast<elem*>(p.sum) + cur.in * p.ld_sum;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int c = 8 * (t + j * TPR);
-        if (c + 8 <= k) E::store(d + c, h[j]);
-        else if (c < k) store_part<F32>(d + c, k - c, h[j]);
-      }
-      if (!p.q && !p.y) continue;
-    }
-    measure();
-    // n = h w rs.  Where the squares (or a product with the weight) left the range of fp32, 127 / max would, or the row holds something
-    // that is no number, the row is looked at again: rare, and the same for all threads of a row, but not for all rows of the CTA.
-    float rs = rsqrtf(ss / (float)k + p.eps);
-    const bool redo = !(ss < INFINITY) || !(mx < INFINITY) || (mx < 7.52316385e-37f && mx > 0.f);
-    if (TPR == THREADS || TPR == 32 ? redo : (bool)__syncthreads_or(redo)) {
-      const float ss1 = ss;
-      float top = 0.f, none = 0.f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = max_abs3_nan(top, h[j][i]);
-      row_reduce<TPR, THREADS>(none, top, buf);
-      // h times a power of two (exact; what underflows is below 2^-120 of the row's largest value), so that its largest is 1 .. 4
-      float f = 1.f;
-      if (redo && top < INFINITY && top > 0.f) {
-        const int e = (int)(__float_as_uint(top) >> 23);
-        f = __uint_as_float((uint32_t)(e > 252 ? 1 : (e < 1 ? 253 : 254 - e)) << 23);
-      }
-      const uint64_t f2 = pack2(f, f);
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[j][i] = fmul2(h[j][i], f2);
-      measure();
-      if (f < 1.f) rs = rsqrtf(ss / (float)k + p.eps * f * f);
-      else if (f > 1.f) rs = rsqrtf(ss1 / (float)k + p.eps) / f;         // eps outweighs squares this small
-      if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);          // NaN or infinity in the row: NaN comes out
-    }
-    if (k == 0) continue;
-    elem* y = p.y ? static_cast<elem*>(p.y) + cur.out * p.ldy : nullptr;
-    if (p.q) {
-      const float inv = mx > 0.f ? __fdiv_rn(127.f, mx) : mx;             // a row of zeros: 0; NaN stays
-      const float scale = __fdiv_rn(mx * rs, 127.f);
-      const uint32_t keep = mx < INFINITY ? 0xffffffffu : 0u;             // a row that is no number has the codes 0
-      const uint64_t inv2 = pack2(inv, inv), scale2 = pack2(scale, scale);
-      const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f);
-      int8_t* q = p.q + cur.out * p.ldq;
-      if (t == 0) p.scale[cur.out] = scale;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int c = 8 * (t + j * TPR);
-        uint64_t v[4];
-        uint32_t b[8];
-        product(j, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // the sum with 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves its low byte in the low byte
-          const uint64_t m = fadd2(fmul2(v[i], inv2), magic);
-          b[2 * i] = (uint32_t)m;
-          b[2 * i + 1] = (uint32_t)(m >> 32);
-          v[i] = fmul2(fadd2(m, nmagic), scale2);
-        }
-        const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) & keep;
-        const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410) & keep;
-        if (c + 8 <= k) {
-          *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
-          if (y) E::store(y + c, v);
-        } else if (c < k) {
-#pragma unroll
-          for (int i = 0; i < 7; ++i)
-            if (c + i < k) q[c + i] = (int8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
-          if (y) store_part<F32>(y + c, k - c, v);
-        }
-      }
-    } else {
-      const float f = mx >= 0.f ? rs : mx;
-      const uint64_t f2 = pack2(f, f);
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int c = 8 * (t + j * TPR);
-        uint64_t v[4];
-        product(j, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fmul2(v[i], f2);
-        if (c + 8 <= k) E::store(y + c, v);
-        else if (c < k) store_part<F32>(y + c, k - c, v);
-      }
-    }
+    // the unit is in registers, and a group leaves together when a wait ran out anywhere in it
+    if (!(GT > 32 ? dsn_group_all(ok, 1 + g, GT) : (bool)__all_sync(0xffffffffu, ok))) break;
+    if (fetches && asked < mine) ask(slot);
+    finish_row<F32, TPR, VPT>(p, cur, t, h, w, s_part[g], turn, 1 + g);
+    if (++slot == depth) { slot = 0; phase ^= 1u; }
   }
 }
 
 template <bool F32, bool RES, int TPR, int VPT>
 cudaError_t launch(const NormParams& p, int sm_count, cudaStream_t s) {
-  constexpr int THREADS = TPR > 128 ? TPR : 128;
-  static int resident[DSN_MAX_DEVICES] = {};   // CTAs per SM of this form
+  constexpr int THREADS = TPR > 32 ? TPR : 128;
+  static int resident[DSN_MAX_DEVICES] = {};
   auto kernel = norm_quant_kernel<F32, RES, TPR, VPT, THREADS>;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  int n = 0;
+  const cudaError_t e = dsn_ctas_per_sm(kernel, THREADS, 0, resident, &n);
   if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= DSN_MAX_DEVICES) return cudaErrorInvalidDevice;
-  if (resident[dev] == 0) {
-    int n = 0;
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, THREADS, 0);
-    if (e != cudaSuccess) return e;
-    resident[dev] = n > 0 ? n : 1;
-  }
-  const int64_t rows = (int64_t)p.B * p.R, ctas = (rows + THREADS / TPR - 1) / (THREADS / TPR);
-  const int64_t most = (int64_t)sm_count * resident[dev];
+  const int64_t rows = (int64_t)p.B * p.R, ctas = (rows + THREADS / TPR - 1) / (THREADS / TPR), most = (int64_t)sm_count * n;
   return dsn_launch(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), 0, s, 1, p);
+}
+
+// Rings of at most 96 KB a CTA where two CTAs share an SM, of up to 200 KB where one takes it alone (two slots of long rows).
+template <bool F32, bool RES, int TPR, int VPT>
+cudaError_t launch_ring(const NormParams& p, int sm_count, cudaStream_t s) {
+  static size_t configured[DSN_MAX_DEVICES] = {};
+  auto kernel = norm_quant_ring_kernel<F32, RES, TPR, VPT>;
+  constexpr int RB = TPR < 32 ? 32 / TPR : 1, GROUPS = kRingThreads / (TPR < 32 ? 32 : TPR);
+  const uint32_t row = (uint32_t)((p.max_k + 7) / 8 * (F32 ? 32 : 16));   // whole steps of eight columns
+  const uint32_t one = GROUPS * RB * (RES ? 2u : 1u) * row;               // a slot of every group
+  int per_sm = 2, depth = (int)(96 * 1024 / one);
+  if (depth < 2) {
+    per_sm = 1;
+    depth = (int)(200 * 1024 / one);
+  }
+  if (depth < 2) return cudaErrorInvalidConfiguration;
+  if (depth > kRingDepth) depth = kRingDepth;
+  const size_t smem = (size_t)depth * one;
+  const cudaError_t e = dsn_ensure_dynamic_smem(kernel, smem, configured);
+  if (e != cudaSuccess) return e;
+  const int64_t units = ((int64_t)p.B * p.R + RB - 1) / RB, ctas = (units + GROUPS - 1) / GROUPS, most = (int64_t)sm_count * per_sm;
+  return dsn_launch(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kRingThreads), smem, s, 1, p, depth, row);
 }
 
 template <bool F32, bool RES>
 cudaError_t pick(const NormParams& p, int sm_count, cudaStream_t s) {
   const int steps = (p.max_k + 7) / 8;
+  const int64_t rows = (int64_t)p.B * p.R;
+  if (rows >= 8 * sm_count && steps <= 1024) {
+    if (steps <= 16) return launch_ring<F32, RES, 16, 1>(p, sm_count, s);
+    if (steps <= 32) return launch_ring<F32, RES, 16, 2>(p, sm_count, s);
+    if (steps <= 48) return launch_ring<F32, RES, 16, 3>(p, sm_count, s);
+    if (steps <= 96) return launch_ring<F32, RES, 32, 3>(p, sm_count, s);
+    if (steps <= 128) return launch_ring<F32, RES, 32, 4>(p, sm_count, s);
+    if (steps <= 256) return launch_ring<F32, RES, 64, 4>(p, sm_count, s);
+    if (steps <= 512) return launch_ring<F32, RES, 128, 4>(p, sm_count, s);
+    return launch_ring<F32, RES, 256, 4>(p, sm_count, s);
+  }
   if (steps <= 32) return launch<F32, RES, 32, 1>(p, sm_count, s);
   if (steps <= 64) return launch<F32, RES, 32, 2>(p, sm_count, s);
   if (steps <= 128) return launch<F32, RES, 64, 2>(p, sm_count, s);

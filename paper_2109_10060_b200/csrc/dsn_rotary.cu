@@ -2,9 +2,12 @@
 //   (u, v) -> (u cos a - v sin a, u sin a + v cos a),  a = position[axis] * frequency of the pair.
 // The frequency of a pair is held as turns per unit of position in 64-bit fixed point; position * frequency modulo 2^64 IS
 // the angle modulo a full turn, exactly, whatever the position, and its top 32 bits go to sincospi in fp32.
-// Bound by memory.  A token's sines and cosines are computed once into shared memory, one pair a lane; a thread then owns
-// one 16-byte place of a vector, keeps its factors in registers and walks the heads with them, two elements an instruction, several
-// heads' loads in flight.  Every element is read and written once.
+// Bound by memory; two elements an instruction, a token's sines and cosines computed once, one pair a lane, into shared memory.
+// Ring form: a group of 32 .. 256 threads has a ring of shared-memory slots of its own, which bulk copies fill with the rows to come
+// (tokens and their positions are looked up 32 at a time, one a lane); it turns a row where it lies and one bulk copy takes it out, so
+// what does not turn (v, the rest of a head) costs no instruction at all, and the bytes in flight do not depend on registers.
+// Direct form (few tokens, rows that are not made of 16-byte pieces or too long for a ring): a thread owns one place of a vector,
+// keeps its factors in registers and walks the heads with them.
 #include <type_traits>
 
 #include "dsn_gemm_device.cuh"
@@ -198,26 +201,180 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
   }
 }
 
+// Ring form.
+constexpr int kRingThreads = 256;
+constexpr int kRingDepth = 8;    // most slots of a group
+struct TokenAt {
+  int heads;       // 0: no such token
+  int pos[3];
+  int64_t row;
+};
+
+template <bool F32, bool INTER, int TPT>
+__global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __grid_constant__ RotaryParams p, int depth, uint32_t slot_bytes) {
+  typedef Vec<F32> E;
+  constexpr int GROUPS = kRingThreads / TPT, ES = F32 ? 4 : 2, W = E::n, NP = W / 2;
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t s_full[GROUPS][kRingDepth];
+  __shared__ TokenAt s_at[GROUPS][kRingDepth];
+  __shared__ __align__(16) float s_cos[GROUPS][128], s_sin[GROUPS][128];
+  __shared__ uint32_t s_abort;
+  const int g = threadIdx.x / TPT, t = threadIdx.x % TPT, lane = threadIdx.x & 31;
+  const bool fetches = t < 32;   // the group's first warp asks for rows and sends them off
+  if (threadIdx.x < GROUPS * kRingDepth) dsn_gemm::mbar_init(dsn_gemm::smem_u32(&s_full[0][0] + threadIdx.x), 1);
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const uint32_t rows = (uint32_t)p.B * (uint32_t)p.N;
+  const uint32_t gid = blockIdx.x * GROUPS + g, ngroups = gridDim.x * GROUPS;
+  const int mine = gid < rows ? (int)((rows - gid + ngroups - 1) / ngroups) : 0;   // tokens of this group
+  uint8_t* slots = ring + (size_t)g * depth * slot_bytes;
+  volatile uint32_t* abort_flag = &s_abort;
+
+  TokenAt ahead{0, {0, 0, 0}, 0};   // this lane's token of those being asked for
+  int asked = 0;
+  auto ask = [&](int slot) {
+    if (asked % 32 == 0) {
+      ahead = TokenAt{0, {0, 0, 0}, 0};
+      const uint64_t wide = (uint64_t)(asked + lane) * ngroups + gid;
+      if (wide < rows) {
+        const uint32_t row = (uint32_t)wide;
+        const int pos = (int)dsn_div(row, p.by_N), r = (int)(row - (uint32_t)pos * (uint32_t)p.N);
+        const PosInfo at = dsn_locate(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
+        if (at.slice >= 0) {
+          ahead.heads = p.heads[at.slice];
+          ahead.row = (int64_t)(p.grouped ? pos : at.sample) * p.N + r;
+          const int32_t* at_pos = p.positions + (p.shared ? (int64_t)r : ahead.row);
+          ahead.pos[0] = at_pos[0];
+          if (p.n_axes > 1) ahead.pos[1] = at_pos[p.n_pos];
+          if (p.n_axes > 2) ahead.pos[2] = at_pos[2 * (int64_t)p.n_pos];
+        }
+      }
+      __syncwarp();
+    }
+    if (lane == asked % 32) {
+      const uint32_t bytes = (uint32_t)(ahead.heads * p.vectors * p.D * ES), bar = dsn_gemm::smem_u32(&s_full[g][slot]);
+      s_at[g][slot] = ahead;
+      dsn_gemm::mbar_expect_tx(bar, bytes);
+      if (bytes) dsn_bulk_load(dsn_gemm::smem_u32(slots) + (uint32_t)slot * slot_bytes, static_cast<const uint8_t*>(p.x) + ahead.row * p.ldx * ES, bytes, bar);
+    }
+    __syncwarp();
+    ++asked;
+  };
+  if (fetches)
+    for (int i = 0; i < depth && i < mine; ++i) ask(i);
+
+  const int P = p.pairs, D = p.D;
+  const int per = INTER ? 2 * P / W : P / W;        // places of a vector that this kernel's threads take
+  const int dv = TPT / per, di = TPT - dv * per;    // from one of a thread's places to its next
+  const int v0 = t / per, i0 = t - v0 * per;
+  int slot = 0;
+  uint32_t phase = 0;
+  for (int n = 0; n < mine; ++n) {
+    bool ok = dsn_gemm::mbar_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 73);
+    ok = TPT > 32 ? dsn_group_all(ok, 1 + g, TPT) : (bool)__all_sync(0xffffffffu, ok);   // a group leaves together
+    if (!ok) break;
+    const TokenAt cur = s_at[g][slot];
+    uint8_t* row = slots + (size_t)slot * slot_bytes;
+    if (cur.heads > 0) {
+      for (int i = t; i < P; i += TPT) {
+        const int ax = p.axis[i];
+        const int at = ax == 0 ? cur.pos[0] : (ax == 1 ? cur.pos[1] : cur.pos[2]);
+        const uint64_t a = (uint64_t)(int64_t)at * p.freq[i];
+        float c, s;
+        sincospif((float)(int32_t)(a >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: -1 .. 1 half turns
+        s_cos[g][i] = c;
+        s_sin[g][i] = p.inverse ? -s : s;
+      }
+      if (TPT > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(TPT) : "memory"); else __syncwarp();
+      const int turned = cur.heads * p.rotated;
+      int v = v0, pc = i0;
+#pragma unroll 2
+      while (v < turned) {
+        const int i = pc * W;
+        uint8_t* at = row + (size_t)(vec_at(p, v) + i) * ES;
+        uint64_t a[NP];
+        E::widen(*reinterpret_cast<const uint4*>(at), a);
+        if constexpr (!INTER) {
+          uint64_t b[NP], na[NP], nb[NP];
+          E::widen(*reinterpret_cast<const uint4*>(at + P * ES), b);
+#pragma unroll
+          for (int e = 0; e < NP; ++e) {
+            const uint64_t c = *reinterpret_cast<const uint64_t*>(&s_cos[g][i + 2 * e]), s = *reinterpret_cast<const uint64_t*>(&s_sin[g][i + 2 * e]);
+            na[e] = ffma2(neg2(b[e]), s, fmul2(a[e], c));
+            nb[e] = ffma2(b[e], c, fmul2(a[e], s));
+          }
+          *reinterpret_cast<uint4*>(at) = E::narrow(na);
+          *reinterpret_cast<uint4*>(at + P * ES) = E::narrow(nb);
+        } else {
+#pragma unroll
+          for (int e = 0; e < NP; ++e) {
+            const float c = s_cos[g][i / 2 + e], s = s_sin[g][i / 2 + e];
+            a[e] = ffma2(swap2(a[e]), pack2(-s, s), fmul2(a[e], pack2(c, c)));
+          }
+          *reinterpret_cast<uint4*>(at) = E::narrow(a);
+        }
+        v += dv;
+        pc += di;
+        if (pc >= per) { pc -= per; ++v; }
+      }
+      dsn_gemm::fence_async_smem();   // the turned elements are visible to the copy that takes them out
+    }
+    if (TPT > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(TPT) : "memory"); else __syncwarp();
+    if (fetches) {
+      if (t == 0) {
+        if (cur.heads > 0) dsn_bulk_store(static_cast<uint8_t*>(p.y) + cur.row * p.ldy * ES, dsn_gemm::smem_u32(row), (uint32_t)(cur.heads * p.vectors * D * ES));
+        dsn_gemm::bulk_commit();
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // the token before has left its slot
+      }
+      __syncwarp();
+      if (n > 0 && asked < mine) ask(slot == 0 ? depth - 1 : slot - 1);  // which takes the next row
+    }
+    if (++slot == depth) { slot = 0; phase ^= 1u; }
+  }
+  if (t == 0) dsn_gemm::bulk_wait0();
+}
+
+template <bool F32, bool INTER, int TPT>
+cudaError_t launch_ring(const RotaryParams& p, uint32_t row_bytes, int per_sm, int sm_count, cudaStream_t s) {
+  static size_t configured[DSN_MAX_DEVICES] = {};
+  auto kernel = rotary_ring_kernel<F32, INTER, TPT>;
+  constexpr int GROUPS = kRingThreads / TPT;
+  int depth = (int)((per_sm == 2 ? 96 : 192) * 1024 / (GROUPS * row_bytes));
+  if (depth < 2) return cudaErrorInvalidConfiguration;
+  if (depth > kRingDepth) depth = kRingDepth;
+  const size_t smem = (size_t)depth * GROUPS * row_bytes;
+  const cudaError_t e = dsn_ensure_dynamic_smem(kernel, smem, configured);
+  if (e != cudaSuccess) return e;
+  const int64_t ctas = ((int64_t)p.B * p.N + GROUPS - 1) / GROUPS, most = (int64_t)sm_count * per_sm;
+  return dsn_launch(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kRingThreads), smem, s, 1, p, depth, row_bytes);
+}
+
 template <bool F32, bool VEC, bool INTER, int TPT>
 cudaError_t launch(const RotaryParams& p, int sm_count, cudaStream_t s) {
   constexpr int THREADS = TPT > 128 ? TPT : 128;
-  static int resident[DSN_MAX_DEVICES] = {};   // CTAs per SM of this form
+  static int resident[DSN_MAX_DEVICES] = {};
   auto kernel = rotary_kernel<F32, VEC, INTER, TPT, THREADS>;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  int n = 0;
+  const cudaError_t e = dsn_ctas_per_sm(kernel, THREADS, 0, resident, &n);
   if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= DSN_MAX_DEVICES) return cudaErrorInvalidDevice;
-  if (resident[dev] == 0) {
-    int n = 0;
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, THREADS, 0);
-    if (e != cudaSuccess) return e;
-    resident[dev] = n > 0 ? n : 1;
-  }
-  const int64_t ctas = ((int64_t)p.B * p.N + THREADS / TPT - 1) / (THREADS / TPT), most = (int64_t)sm_count * resident[dev];
+  const int64_t ctas = ((int64_t)p.B * p.N + THREADS / TPT - 1) / (THREADS / TPT), most = (int64_t)sm_count * n;
   return dsn_launch(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), 0, s, 1, p);
 }
 template <bool F32, bool VEC, bool INTER>
 cudaError_t pick(const RotaryParams& p, int sm_count, cudaStream_t s) {
+  const int64_t bytes = (int64_t)p.max_heads * p.vectors * p.D * (F32 ? 4 : 2);
+  if (VEC && (int64_t)p.B * p.N >= 8 * sm_count && bytes <= 96 * 1024) {
+    // the fewest threads a row with which two slots a group fit
+    if (bytes <= 6 * 1024) return launch_ring<F32, INTER, 32>(p, (uint32_t)bytes, 2, sm_count, s);
+    if (bytes <= 12 * 1024) return launch_ring<F32, INTER, 64>(p, (uint32_t)bytes, 2, sm_count, s);
+    if (bytes <= 24 * 1024) return launch_ring<F32, INTER, 128>(p, (uint32_t)bytes, 2, sm_count, s);
+    return launch_ring<F32, INTER, 256>(p, (uint32_t)bytes, bytes <= 48 * 1024 ? 2 : 1, sm_count, s);
+  }
   // a warp a token where there are tokens enough to fill the GPU, else 256 threads
   return (int64_t)p.B * p.N >= 16 * sm_count ? launch<F32, VEC, INTER, 32>(p, sm_count, s) : launch<F32, VEC, INTER, 256>(p, sm_count, s);
 }

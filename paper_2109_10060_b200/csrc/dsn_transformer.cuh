@@ -45,6 +45,58 @@ __device__ __forceinline__ PosInfo dsn_locate_warp(int p, int G, int T, const in
   return i;
 }
 
+// The same for one thread on its own.
+__device__ __forceinline__ PosInfo dsn_locate(int p, int G, int T, const int32_t* __restrict__ offsets, const int32_t* __restrict__ perm,
+                                              const int32_t* __restrict__ group_slice) {
+  if (p >= offsets[G]) return PosInfo{0, -1};
+  int lo = 0, hi = G;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid] <= p) lo = mid; else hi = mid;
+  }
+  PosInfo i;
+  i.sample = perm[p];
+  i.slice = group_slice ? group_slice[lo] : lo;
+  if (i.sample < 0 || i.slice >= T) i.slice = -1;
+  return i;
+}
+
+// Untiled bulk copies between global and shared memory: both ends on 16 bytes, whole 16 bytes.
+__device__ __forceinline__ void dsn_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void dsn_bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)), "r"(src), "r"(bytes)
+               : "memory");
+}
+// Barrier `id` of `n` threads (whole warps) that also tells all of them whether `ok` holds in every one.
+__device__ __forceinline__ bool dsn_group_all(bool ok, int id, int n) {
+  int all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.and.pred q, %2, %3, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+               : "=r"(all)
+               : "r"((int)ok), "r"(id), "r"(n)
+               : "memory");
+  return all != 0;
+}
+// Resident CTAs per SM of a kernel form on the current device, asked once.
+template <typename K>
+inline cudaError_t dsn_ctas_per_sm(K kernel, int threads, size_t smem, int* per_device /* [DSN_MAX_DEVICES] */, int* out) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= DSN_MAX_DEVICES) return cudaErrorInvalidDevice;
+  if (per_device[dev] == 0) {
+    int n = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem);
+    if (e != cudaSuccess) return e;
+    per_device[dev] = n > 0 ? n : 1;
+  }
+  *out = per_device[dev];
+  return cudaSuccess;
+}
+
 struct NormParams {
   int16_t k[DSN_MAX_SLICES];
   int32_t R, B, G, T, max_k;
@@ -62,6 +114,7 @@ struct NormParams {
   int64_t ldx, ld_res, ld_sum, ldq, ldy;
   const float* weight;
   float eps;
+  int32_t* status;
 };
 cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int sm_count, cudaStream_t s);
 
@@ -69,7 +122,7 @@ struct RotaryParams {
   uint64_t freq[128];   // turns per unit of position, in units of 2^-64
   uint8_t axis[128];
   int16_t heads[DSN_MAX_SLICES];
-  int32_t N, D, vectors, rotated, pairs, max_heads;
+  int32_t N, D, vectors, rotated, pairs, n_axes, max_heads;
   FastDiv by_N;
   int32_t B, G, T, grouped;
   int32_t n_pos;        // rows of one axis of `positions`
@@ -81,6 +134,7 @@ struct RotaryParams {
   const void* x;
   void* y;
   int64_t ldx, ldy;
+  int32_t* status;
 };
 cudaError_t dsn_launch_rotary(const RotaryParams& p, int f32, int aligned, int sm_count, cudaStream_t s);
 

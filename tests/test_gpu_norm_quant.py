@@ -115,6 +115,50 @@ def test_norm_matches_oracle(dsn, ctx, name, B, R, C, k):
     check(run(dsn, ctx, x, idx, k, name, None, None, raw=True), x, idx, k, name, None, None)
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("C,k", [(120, [7, 64, 120]), (250, [130, 250]), (384, [384, 190]), (765, [500, 761, 765]), (1000, [1000, 999]), (2048, [1030, 2047, 2048]),
+                                 (4096, [4095, 2050]), (8192, [4100, 8191])])
+def test_norm_of_many_rows_matches_oracle(dsn, ctx, name, C, k):
+    """Rows enough for the form that streams them through shared memory, one width list for each number of threads a row."""
+    g = np.random.default_rng(C)
+    B, R = 101, 15
+    idx = g.integers(0, len(k), size=B)
+    x, res = data(g, B, R, C, name), data(g, B, R, C, name)
+    w = g.uniform(-2, 2, size=C).astype(np.float32).astype(np.float64)
+    check(run(dsn, ctx, x, idx, k, name, w, res, out_grouped=True), x, idx, k, name, w, res)
+    check(run(dsn, ctx, x, idx, k, name, w, None, in_grouped=True, raw=C == 384), x, idx, k, name, w, None)
+
+
+def test_many_rows_with_tight_last_row_bad_rows_and_large_rows(dsn, ctx):
+    """The last row ends with the tensor; rows that are no numbers and rows whose squares overflow stand among ordinary ones."""
+    g = np.random.default_rng(12)
+    for C in (77, 1501):
+        B, R, ld = 1300, 1, -(-C // 16) * 16
+        x = g.normal(size=(B, R, C)).astype(np.float32).astype(np.float64)
+        x[5, 0, C - 1], x[17, 0, 3], x[1299, 0, 0] = np.nan, np.inf, 3.0
+        x[6] *= 2.0 ** 70
+        x[7] *= 2.0 ** -125
+        x[8] = 0
+        store = torch.empty((B - 1) * ld + C, device=DEV)
+        xd = store.as_strided((B, C), (ld, 1))
+        xd.copy_(torch.from_numpy(x[:, 0].astype(np.float32)))
+        r, _ = groups(dsn, [0] * B, 1)
+        q, sc = torch.zeros(B, ld, dtype=torch.int8, device=DEV), torch.zeros(B, device=DEV)
+        y = torch.zeros(B, ld, device=DEV)
+        d = dsn.make_norm_desc(dsn.F32, R, C, [C], eps=1e-20, ldx=ld, ldq=ld, ldy=ld)
+        dsn.dsn_rmsnorm_quant(ctx, d, r, xd, q=q, scale=sc, y=y)
+        check_status(ctx, dsn)
+        got, s, v = values(q)[:, :C], values(sc), values(y)[:, :C]
+        for i in (5, 17):
+            assert np.isnan(s[i]) and np.all(got[i] == 0) and np.all(np.isnan(v[i]))
+            x[i] = 0
+        h, n, scale, steps = O.rmsnorm_quant(x, [0] * B, [C], None, 1e-20)
+        keep = [i for i in range(B) if i not in (5, 17)]
+        assert np.all(np.abs(got[keep] - steps[keep, 0]) <= 0.5 + 127 * 7 * U)
+        keep.remove(7)                                            # its squares are below fp32's smallest; the code is exact, the scale is eps's
+        np.testing.assert_allclose(s[keep], scale[keep, 0], rtol=48 * U)
+
+
 @pytest.mark.parametrize("in_grouped", [False, True])
 @pytest.mark.parametrize("out_grouped", [False, True])
 @pytest.mark.parametrize("in_place", [None, "x", "residual"])

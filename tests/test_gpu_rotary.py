@@ -83,6 +83,18 @@ def test_rotary_matches_oracle(dsn, ctx, name, per_axis, interleaved, B, N, H, D
     run(dsn, ctx, 3, B, N, H, D, heads, pairs, name, vectors=4, rotated=4, inverse=True, pitch=16, **kw)
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("H,D,vectors,heads,pairs", [(3, 16, 3, [1, 3], [8]), (12, 64, 3, [12, 5], [16, 16]), (9, 80, 3, [9], [8, 16, 8]), (32, 128, 2, [32, 31], [64]),
+                                                     (24, 256, 4, [24], [8, 40]), (2, 32, 1, [2], [4, 4])])
+def test_rotary_of_many_tokens_matches_oracle(dsn, ctx, name, interleaved, H, D, vectors, heads, pairs):
+    """Tokens enough for the form that streams rows through shared memory, rows for each number of threads a token."""
+    rotated = min(vectors, 2)
+    run(dsn, ctx, 11, 41, 31, H, D, heads, pairs, name, vectors=vectors, rotated=rotated, interleaved=interleaved, shared=True)
+    run(dsn, ctx, 12, 41, 31, H, D, heads, pairs, name, vectors=vectors, rotated=rotated, interleaved=interleaved, grouped=True, in_place=True,
+        per_axis=True, pitch=16, inverse=True)
+
+
 def test_rotary_unaligned_rows_take_the_element_form(dsn, ctx):
     for name in ("bf16", "f32"):
         run(dsn, ctx, 4, 3, 4, 2, 64, [1, 2], [16, 16], name, offset=1)
