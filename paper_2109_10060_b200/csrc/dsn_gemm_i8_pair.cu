@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
       if (g.a_input_order) bsel = t.b0 < t.p_end ? p.perm[t.b0] : p.B;  // past the group: out of range, zeros
       const int cx = g.flat ? t.row0 : t.x0, cb = g.flat ? 0 : bsel;
       for (int kc = 0; kc < nkc; ++kc) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status, 61));
+        ok = __all_sync(0xffffffffu, dsn_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status, 61));
         if (!ok) break;
         if (elect_one()) {
           const uint32_t full_lead = leader_addr(bar_full + 8 * stage);  // the even CTA's barrier
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
         const PairTile t = decode_pair_tile(p, s_prefix, tile, 0, cursor);
         const int acc = it & 1;
         const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, abort_flag, p.status, 62));
+        ok = __all_sync(0xffffffffu, dsn_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, abort_flag, p.status, 62));
         if (!ok) break;
         tc_fence_after();
         const uint32_t idesc = make_idesc_i8(2 * BM, (t.ncols + 31) & ~31);
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
         const int tail_ks = ((t.ki & (kBKB - 1)) + 31) >> 5;  // K steps of a partial last chunk (0: none)
         uint32_t accumulate = 0;
         for (int kc = (t.ki + kBKB - 1) / kBKB; kc > 0; --kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, abort_flag, p.status, 63));
+          ok = __all_sync(0xffffffffu, dsn_wait(bar_full + 8 * stage, phase, abort_flag, p.status, 63));
           if (!ok) break;
           tc_fence_after();
           const int nks = (kc == 1 && tail_ks != 0) ? tail_ks : kBKB / 32;
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
       const long long base_row = __shfl_sync(0xffffffffu, (long long)out_row, 0);
       const bool contig = __all_sync(0xffffffffu, valid && out_row == base_row + lane) && t.ko >= 8;
 
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * acc, acc_phase, abort_flag, p.status, 64));
+      ok = __all_sync(0xffffffffu, dsn_wait(bar_tfull + 8 * acc, acc_phase, abort_flag, p.status, 64));
       if (!ok) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * g.BN);

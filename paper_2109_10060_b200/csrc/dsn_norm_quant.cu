@@ -9,7 +9,7 @@
 // of short rows: 59 us on 50,432 rows of 384 columns.)  The weights of a thread's columns stay in its registers.  Direct form
 // (few rows, where the ring's start-up is longer than the rows; rows too long for a ring): the same arithmetic on rows read
 // straight into registers.
-#include "dsn_gemm_device.cuh"
+
 #include "dsn_transformer.cuh"
 
 namespace {
@@ -120,10 +120,10 @@ __device__ __forceinline__ RowAt locate_row(const NormParams& p, uint32_t row) {
   return a;
 }
 
-// (sum, maximum) over the TPR threads of a row: a group of its own named barrier `id` where it is more than a warp.  `part`
-// holds two sets of one entry a warp, taken in turn: one barrier a call is enough then.
+// (sum, maximum) over the TPR threads of a row, and whether `ok` holds in all of them: a group with its own named barrier `id` where
+// it is more than a warp.  `part` holds two sets of one entry a warp, taken in turn: one barrier a call is enough then.
 template <int TPR>
-__device__ __forceinline__ void row_reduce(float& ss, float& mx, float2* part, int& turn, int id) {
+__device__ __forceinline__ bool row_reduce(float& ss, float& mx, float2* part, int& turn, int id, bool ok) {
 #pragma unroll
   for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
     ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -133,7 +133,7 @@ __device__ __forceinline__ void row_reduce(float& ss, float& mx, float2* part, i
     constexpr int NW = TPR / 32;
     float2* mine = part + turn * NW;
     if ((threadIdx.x & 31) == 0) mine[(threadIdx.x >> 5) % NW] = make_float2(ss, mx);
-    asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(TPR) : "memory");
+    ok = dsn_group_all(ok, id, TPR);
     ss = 0.f;
     mx = 0.f;
 #pragma unroll
@@ -143,7 +143,9 @@ __device__ __forceinline__ void row_reduce(float& ss, float& mx, float2* part, i
       mx = max_nan(mx, v.y);
     }
     turn ^= 1;
+    return ok;
   }
+  return (bool)__all_sync(0xffffffffu, ok);
 }
 
 template <int TPR, int VPT>
@@ -160,10 +162,11 @@ __device__ __forceinline__ void load_weights(const NormParams& p, int t, uint64_
   }
 }
 
-// A row that lies in the registers of its TPR threads (h, zero at and beyond k) -> everything that is written for it.
+// A row that lies in the registers of its TPR threads (h, zero at and beyond k) -> everything that is written for it.  False where `ok`
+// does not hold in all threads of the row; then they all leave.  When it returns, all of them have the row in registers.
 template <bool F32, int TPR, int VPT>
-__device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur, int t, uint64_t (&h)[VPT][4], const uint64_t (&w)[VPT][4], float2* part,
-                                           int& turn, int id) {
+__device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur, int t, uint64_t (&h)[VPT][4], const uint64_t (&w)[VPT][4], float2* part,
+                                           int& turn, int id, bool ok) {
   typedef Elem<F32> E;
   typedef typename E::type elem;
   const int k = cur.k;
@@ -198,7 +201,7 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur
     float a, b;
     unpack2(s2, a, b);
     ss = a + b;
-    row_reduce<TPR>(ss, mx, part, turn, id);
+    ok = row_reduce<TPR>(ss, mx, part, turn, id, ok);
   };
   if (p.sum) {
     elem* d = static_cast<elem*>(p.sum) + cur.in * p.ld_sum;
@@ -208,9 +211,10 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur
       if (c + 8 <= k) E::store(d + c, h[j]);
       else if (c < k) store_part<F32>(d + c, k - c, h[j]);
     }
-    if (!p.q && !p.y) return;
+    if (!p.q && !p.y) return TPR > 32 ? dsn_group_all(ok, id, TPR) : (bool)__all_sync(0xffffffffu, ok);
   }
   measure();
+  if (!ok) return false;
   // n = h w rs.  Where the squares (or a product with the weight) left the range of fp32, 127 / max would, or the row holds something
   // that is no number, the row is looked at again (rare; the same decision in all threads of the row).
   const float rk = __fdividef(1.f, (float)k);
@@ -223,7 +227,7 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = max_abs3_nan(top, h[j][i]);
-    row_reduce<TPR>(none, top, part, turn, id);
+    row_reduce<TPR>(none, top, part, turn, id, true);
     // h times a power of two (exact; what underflows is below 2^-120 of the row's largest value), so that its largest is 1 .. 4
     float f = 1.f;
     if (redo && top < INFINITY && top > 0.f) {
@@ -240,7 +244,7 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur
     else if (f > 1.f) rs = rsqrtf(ss1 * rk + p.eps) / f;               // eps outweighs squares this small
     if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);          // NaN or infinity in the row: NaN comes out
   }
-  if (k == 0) return;
+  if (k == 0) return true;
   elem* y = p.y ? static_cast<elem*>(p.y) + cur.out * p.ldy : nullptr;
   if (p.q) {
     const float inv = mx > 0.f ? __fdiv_rn(127.f, mx) : mx;             // a row of zeros: 0; NaN stays
@@ -292,6 +296,7 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const RowAt& cur
       else store_part<F32>(y + c, k - c, v);
     }
   }
+  return true;
 }
 
 // Direct form: rows read straight into registers, TPR threads (at least a warp) a row.
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(THREADS) norm_quant_kernel(const __grid_consta
       }
     }
     next = locate_row(p, row + stride < rows ? row + stride : rows);
-    finish_row<F32, TPR, VPT>(p, cur, t, h, w, part, turn, 0);
+    finish_row<F32, TPR, VPT>(p, cur, t, h, w, part, turn, 0, true);
   }
 }
 
@@ -421,7 +426,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
   int turn = 0, slot = 0;
   uint32_t phase = 0;
   for (int n = 0; n < mine; ++n) {
-    const bool ok = dsn_gemm::mbar_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 71);
+    const bool ok = dsn_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 71);
     const RowAt cur = s_at[g][slot][sub];
     const int k = cur.k;
     const elem* xs = reinterpret_cast<const elem*>(slots + (size_t)slot * slot_bytes + (size_t)sub * copies * row_bytes);
@@ -455,10 +460,9 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
         }
       }
     }
-    // the unit is in registers, and a group leaves together when a wait ran out anywhere in it
-    if (!(GT > 32 ? dsn_group_all(ok, 1 + g, GT) : (bool)__all_sync(0xffffffffu, ok))) break;
+    // a group leaves together when a wait ran out anywhere in it
+    if (!finish_row<F32, TPR, VPT>(p, cur, t, h, w, s_part[g], turn, 1 + g, ok)) break;
     if (fetches && asked < mine) ask(slot);
-    finish_row<F32, TPR, VPT>(p, cur, t, h, w, s_part[g], turn, 1 + g);
     if (++slot == depth) { slot = 0; phase ^= 1u; }
   }
 }
@@ -475,7 +479,8 @@ cudaError_t launch(const NormParams& p, int sm_count, cudaStream_t s) {
   return dsn_launch(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), 0, s, 1, p);
 }
 
-// Rings of at most 96 KB a CTA where two CTAs share an SM, of up to 200 KB where one takes it alone (two slots of long rows).
+// Rings of at most 64 KB a CTA (more bytes in flight only crowd the writes: 100.6 us at 96 KB, 78 against 81 us without y) where two CTAs
+// share an SM, of up to 200 KB where one takes it alone (two slots of long rows).
 template <bool F32, bool RES, int TPR, int VPT>
 cudaError_t launch_ring(const NormParams& p, int sm_count, cudaStream_t s) {
   static size_t configured[DSN_MAX_DEVICES] = {};
@@ -483,7 +488,8 @@ cudaError_t launch_ring(const NormParams& p, int sm_count, cudaStream_t s) {
   constexpr int RB = TPR < 32 ? 32 / TPR : 1, GROUPS = kRingThreads / (TPR < 32 ? 32 : TPR);
   const uint32_t row = (uint32_t)((p.max_k + 7) / 8 * (F32 ? 32 : 16));   // whole steps of eight columns
   const uint32_t one = GROUPS * RB * (RES ? 2u : 1u) * row;               // a slot of every group
-  int per_sm = 2, depth = (int)(96 * 1024 / one);
+  int per_sm = 2, depth = (int)(64 * 1024 / one);
+  if (depth < 2) depth = (int)(96 * 1024 / one);
   if (depth < 2) {
     per_sm = 1;
     depth = (int)(200 * 1024 / one);
@@ -508,6 +514,9 @@ cudaError_t pick(const NormParams& p, int sm_count, cudaStream_t s) {
     if (steps <= 96) return launch_ring<F32, RES, 32, 3>(p, sm_count, s);
     if (steps <= 128) return launch_ring<F32, RES, 32, 4>(p, sm_count, s);
     if (steps <= 256) return launch_ring<F32, RES, 64, 4>(p, sm_count, s);
+    // 2048 .. 4096 columns: with everything asked for, memory bounds the pass, and fewer rows being written at a time suit it better (16,384
+    // rows of 4096 bf16: 97 us against 112); otherwise the time a row takes from its wait to its stores does, and more rows do (54 against 70)
+    if (steps <= 512 && RES && p.q && p.y) return launch_ring<F32, RES, 256, 2>(p, sm_count, s);
     if (steps <= 512) return launch_ring<F32, RES, 128, 4>(p, sm_count, s);
     return launch_ring<F32, RES, 256, 4>(p, sm_count, s);
   }

@@ -10,7 +10,6 @@
 // keeps its factors in registers and walks the heads with them.
 #include <type_traits>
 
-#include "dsn_gemm_device.cuh"
 #include "dsn_transformer.cuh"
 
 namespace {
@@ -275,7 +274,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
   int slot = 0;
   uint32_t phase = 0;
   for (int n = 0; n < mine; ++n) {
-    bool ok = dsn_gemm::mbar_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 73);
+    bool ok = dsn_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 73);
     ok = TPT > 32 ? dsn_group_all(ok, 1 + g, TPT) : (bool)__all_sync(0xffffffffu, ok);   // a group leaves together
     if (!ok) break;
     const TokenAt cur = s_at[g][slot];

@@ -2,7 +2,17 @@
 // linear layers on codes (dsn_gemm_i8_pair.cu, dsn_rows_i8.cu), rotary positions (dsn_rotary.cu).
 #pragma once
 
+#include "dsn_gemm_device.cuh"
 #include "dsn_internal.cuh"
+
+// Bounded wait that polls for a while before it takes the library's slow path: that one starts with a read of the wait limit from
+// global memory and of the global timer, a microsecond that a wait for the next row or tile should not cost.
+__device__ __forceinline__ bool dsn_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, int32_t* status, int where) {
+#pragma unroll 1
+  for (int i = 0; i < 64; ++i)
+    if (dsn_gemm::mbar_try_wait(bar, parity)) return true;
+  return dsn_gemm::mbar_wait_slow(bar, parity, abort_flag, status, where);
+}
 
 // Quotient of n < 2^31 by a divisor fixed on the host: (umulhi(n, mul) + n) >> shift.
 struct FastDiv {
