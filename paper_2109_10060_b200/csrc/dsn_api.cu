@@ -689,12 +689,41 @@ int check_linear_i8(const dsn_linear_i8_desc* d) {
   return DSN_OK;
 }
 
-// Rows that arrive in input order are tiled sample by sample (a sample's place is known only on the device), and the last
-// tile of each sample is filled up with zero rows.  Where that padding costs more products than a pass that gathers
-// the rows costs traffic, the rows are gathered first.
-bool linear_i8_gathers(const dsn_linear_i8_desc* d, int64_t B) {
-  if (d->in_order != DSN_INPUT_ORDER || B * d->R <= DSN_ROWS_I8_MAX || B < 2) return false;
-  return d->R <= 64;
+// How the tensor-core form of an 8-bit linear layer covers its rows.
+struct I8Plan {
+  int BN;          // n-tile
+  bool gather;     // rows in input order are gathered first
+};
+// Rows in input order are tiled sample by sample (a sample's place is known only on the device), the last tile of each filled up with zero
+// rows; where the waves of tiles that this adds take longer than a pass that gathers the rows, they are gathered.  The n-tile is the
+// one with the shortest estimate, in cycles of a pair of SMs: 2 a column and chunk of 128 (at least 300: an instruction's least time, and the
+// time of its loads), about 9 a column for the epilogue (not hidden behind a first tile), 1500 to fill and drain a wave.
+constexpr int kI8PlanPairs = 74;   // a B200's pairs of SMs: the workspace query has no context to ask
+I8Plan plan_linear_i8(const dsn_linear_i8_desc* d, int64_t B, int pairs) {
+  int max_ki = 1, max_ko = 1;
+  for (int t = 0; t < d->T; ++t) {
+    if (d->k_in[t] > max_ki) max_ki = d->k_in[t];
+    if (d->k_out[t] > max_ko) max_ko = d->k_out[t];
+  }
+  const int64_t rows = B * d->R, chunks = (max_ki + 127) / 128, groups = d->T < B ? d->T : B;
+  const int64_t flat = (rows + 255) / 256 + (groups - 1);                     // a group ends in a part of a tile
+  const int64_t alone = (B * ((d->R + 127) / 128) + 1) / 2 + (groups - 1);
+  const bool input = d->in_order == DSN_INPUT_ORDER && B > 1;
+  I8Plan best{64, false};
+  int64_t least = INT64_MAX;
+  for (int BN = 64; BN <= 256; BN *= 2) {
+    if (BN > 64 && max_ko <= BN / 2) break;
+    const int64_t nt = (max_ko + BN - 1) / BN, tile = chunks * (2 * BN > 300 ? 2 * BN : 300) + 9 * BN;
+    for (int gather = 0; gather <= (input ? 1 : 0); ++gather) {
+      const int64_t tiles = (input && !gather ? alone : flat) * nt, waves = (tiles + pairs - 1) / pairs;
+      const int64_t cost = waves * tile + 1500 + (gather ? 5000 + rows * max_ki / 1500 : 0);   // a launch, and 2 bytes a byte at 5 TB/s
+      if (cost < least) {
+        least = cost;
+        best = I8Plan{BN, gather != 0};
+      }
+    }
+  }
+  return best;
 }
 
 // Tensor maps for the next DSN_GEMM_MAX_MAPS distinct slices not yet done (bytes; 128 of them a chunk).
@@ -753,50 +782,48 @@ int run_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const LayerCall& c,
                   const float* x_scale, void* y, void* workspace, size_t ws_bytes, cudaStream_t s) {
   const int64_t rows = (int64_t)r->B * d->R;
   const int f32 = d->y_dtype == DSN_F32;
+  RowsI8Params q;
+  memset(&q, 0, sizeof(q));
+  q.max_ki = q.max_ko = 1;
+  for (int t = 0; t < d->T; ++t) {
+    q.k_in[t] = (int16_t)d->k_in[t];
+    q.k_out[t] = (int16_t)d->k_out[t];
+    if (d->k_in[t] > q.max_ki) q.max_ki = d->k_in[t];
+    if (d->k_out[t] > q.max_ko) q.max_ko = d->k_out[t];
+  }
+  q.B = r->B; q.R = d->R; q.G = r->G; q.T = d->T; q.C_in = d->C_in;
+  q.in_input_order = d->in_order == DSN_INPUT_ORDER;
+  q.out_input_order = d->out_order == DSN_INPUT_ORDER;
+  q.offsets = r->offsets; q.perm = r->perm; q.group_slice = r->group_slice;
+  q.x = x; q.x_scale = x_scale; q.W = d->W; q.w_scale = d->w_scale; q.bias = d->bias;
+  q.bn_scale = d->bn_scale; q.bn_shift = d->bn_shift; q.bn_ld = d->C_out; q.act = d->act;
+  q.residual = d->residual; q.y = y; q.ldx = d->ldx; q.ldw = d->ldw; q.ldy = d->ldy;
   if (rows <= DSN_ROWS_I8_MAX) {
-    RowsI8Params q;
-    memset(&q, 0, sizeof(q));
-    q.max_ki = q.max_ko = 1;
-    for (int t = 0; t < d->T; ++t) {
-      q.k_in[t] = (int16_t)d->k_in[t];
-      q.k_out[t] = (int16_t)d->k_out[t];
-      if (d->k_in[t] > q.max_ki) q.max_ki = d->k_in[t];
-      if (d->k_out[t] > q.max_ko) q.max_ko = d->k_out[t];
-    }
-    q.B = r->B; q.R = d->R; q.G = r->G; q.T = d->T; q.C_in = d->C_in;
-    q.in_input_order = d->in_order == DSN_INPUT_ORDER;
-    q.out_input_order = d->out_order == DSN_INPUT_ORDER;
-    q.offsets = r->offsets; q.perm = r->perm; q.group_slice = r->group_slice;
-    q.x = x; q.x_scale = x_scale; q.W = d->W; q.w_scale = d->w_scale; q.bias = d->bias;
-    q.bn_scale = d->bn_scale; q.bn_shift = d->bn_shift; q.bn_ld = d->C_out; q.act = d->act;
-    q.residual = d->residual; q.y = y; q.ldx = d->ldx; q.ldw = d->ldw; q.ldy = d->ldy;
     count_launch(ctx, &dsn_stats::launches_rows_i8);
     return dsn_launch_rows_i8(q, f32, s) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
   }
+  const int pairs = resident_pairs(ctx, 256);
+  if (pairs <= 0) return DSN_ERR_UNSUPPORTED;   // this layer has no one-CTA form: DSN_GEMM_MODE leaves it alone
+  const I8Plan plan = plan_linear_i8(d, r->B, kI8PlanPairs);
   LayerCall cc = c;
   int64_t ldx = d->ldx;
   const void* src = x;
-  if (linear_i8_gathers(d, r->B)) {
-    SliceTable st;
-    fill_slice_table(st, c);
+  if (plan.gather) {
     ldx = (int64_t)align_up((size_t)d->C_in, 16);
     if (!workspace || ws_bytes < (size_t)(rows * ldx)) return DSN_ERR_WORKSPACE;
     count_launch(ctx, &dsn_stats::launches_copy);
-    if (dsn_launch_permute_rows(st, 1, d->R, x, d->ldx, workspace, ldx, 1, r->B, r->G, r->offsets, r->perm, r->group_slice, s) !=
-        cudaSuccess)
-      return DSN_ERR_CUDA;
+    if (dsn_launch_gather_i8(q, static_cast<int8_t*>(workspace), ldx, s) != cudaSuccess) return DSN_ERR_CUDA;
     src = workspace;
     cc.in_order = DSN_GROUPED;
   }
-  GemmI8Params q;
-  fill_gemm_params(ctx, cc, r, y, false, q.g);
-  q.x_scale = x_scale;
-  q.w_scale = d->w_scale;
-  q.scale_input_order = d->in_order == DSN_INPUT_ORDER;
-  GemmGeom& g = q.g.g;
-  g.pair = 1;   // this layer has no one-CTA form: DSN_GEMM_MODE leaves it alone
-  const int clusters = resident_pairs(ctx, g.BN);
-  if (clusters <= 0) return DSN_ERR_UNSUPPORTED;
+  GemmI8Params p;
+  fill_gemm_params(ctx, cc, r, y, false, p.g);
+  p.x_scale = x_scale;
+  p.w_scale = d->w_scale;
+  p.scale_input_order = d->in_order == DSN_INPUT_ORDER;
+  GemmGeom& g = p.g.g;
+  g.pair = 1;
+  g.BN = plan.BN;
   g.stages = g.BN == 256 ? 6 : 8;
   while (g.stages > 2 && dsn_gemm_i8_smem_bytes(g.BN, g.stages, r->G) > 227 * 1024) --g.stages;
   const size_t smem = dsn_gemm_i8_smem_bytes(g.BN, g.stages, r->G);
@@ -804,10 +831,10 @@ int run_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const LayerCall& c,
   memset(done, 0, sizeof(done));
   int remaining = d->T;
   while (remaining > 0) {
-    const int e = fill_i8_maps(ctx, cc, r, src, ldx, y, q.g, done, remaining);
+    const int e = fill_i8_maps(ctx, cc, r, src, ldx, y, p.g, done, remaining);
     if (e) return e;
     count_launch(ctx, &dsn_stats::launches_gemm_i8);
-    if (dsn_launch_gemm_i8(q, f32, clusters, smem, s) != cudaSuccess) return DSN_ERR_CUDA;
+    if (dsn_launch_gemm_i8(p, f32, pairs, smem, s) != cudaSuccess) return DSN_ERR_CUDA;
   }
   return DSN_OK;
 }
@@ -1291,7 +1318,7 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
 }
 
 size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B) {
-  if (check_linear_i8(d) || B < 0 || !linear_i8_gathers(d, B)) return 0;
+  if (check_linear_i8(d) || B < 0 || (int64_t)B * d->R <= DSN_ROWS_I8_MAX || !plan_linear_i8(d, B, kI8PlanPairs).gather) return 0;
   return (size_t)B * d->R * align_up((size_t)d->C_in, 16);
 }
 

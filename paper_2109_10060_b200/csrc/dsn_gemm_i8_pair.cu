@@ -3,9 +3,9 @@
 // Tiles, barriers and roles are those of the bf16 pair kernel: a cluster of two CTAs owns a 256-row x BN-column tile, each
 // CTA loads its 128 rows and half of the weight tile, the even CTA issues the products of both.  A 128-byte
 // row piece holds 128 columns here, an instruction takes 32 of them, and at twice the products per byte the main loop of a
-// tile is half as long, so the epilogue weighs twice as much: a warp fetches the channels' factors of its 64 columns before it waits
-// for the accumulator (sw and the affine folded into one factor and one addend, through shared memory), which leaves a
-// conversion, a multiplication and a packed multiply-add per element.
+// tile is half as long, so the epilogue weighs twice as much: a warp fetches the channels' factors and its rows' scales a tile ahead and
+// folds sw and the affine into one factor and one addend a column (in shared memory), which leaves a conversion, a multiplication and a
+// packed multiply-add per element.
 // Barriers (every CTA has the same layout):
 //   full[s]    even CTA only: one arrival (expect_tx for the bytes of both CTAs), completed by the loads of both
 //   empty[s]   both CTAs: the multicast commit frees the stage
@@ -20,7 +20,8 @@ namespace {
 using namespace dsn_gemm;
 
 constexpr int kBKB = 128;                          // bytes (= columns) of a chunk
-constexpr uint32_t kColBytes = kEpiWarps * 64 * 8; // per epilogue warp: factor and addend of 64 columns
+constexpr int kPieces = 4;                         // pieces of 32 columns that an epilogue warp takes of a tile, at most
+constexpr uint32_t kColBytes = kEpiWarps * kPieces * 32 * 8; // per epilogue warp: factor and addend of its columns
 
 // D[tmem] (+)= A[smem] * B[smem]^T on both CTAs' tensor cores, signed 8-bit operands, 32-bit integer sums
 __device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -56,28 +57,18 @@ __device__ __forceinline__ void gelu_pair_i8(float a, float b, float& ra, float&
   unpack2(ffma2(h2, pack2(t0, t1), h2), ra, rb);
 }
 
-struct EpiArgs {
-  const float* w_scale;   // at the tile's first column
-  const float* bias;
-  const float* bn_scale;
-  const float* bn_shift;
+// What the epilogue reads for a tile besides the accumulator, fetched a tile ahead: this lane's column of each of the warp's pieces,
+// and this lane's row.
+struct Ahead {
+  float sw[kPieces], bias[kPieces], bn_scale[kPieces], bn_shift[kPieces];
+  float sx;
+  int64_t out_row;
+  bool valid;
 };
-
-// Factor and addend of this lane's columns of the 32-column piece at `cb` into the warp's shared tile.
-__device__ __forceinline__ void stage_columns(const EpiArgs& a, int cb, int ncols, int lane, float* s_mul, float* s_add) {
-  float m = 0.f, d = 0.f;
-  const int c = cb + lane;
-  if (c < ncols) {
-    m = __ldg(a.w_scale + c);
-    if (a.bias) d = __ldg(a.bias + c);
-    if (a.bn_scale) {
-      const float sc = __ldg(a.bn_scale + c);
-      m *= sc;
-      d = fmaf(d, sc, __ldg(a.bn_shift + c));
-    }
-  }
-  s_mul[lane] = m;
-  s_add[lane] = d;
+// first column of piece j of a warp (bf16 rows are stored 64 columns at a time, fp32 rows 32; two warps share a lane quarter)
+template <bool F32>
+__device__ __forceinline__ int piece_col(int first, int j) {
+  return F32 ? 32 * first + 64 * j : 64 * first + 128 * (j >> 1) + 32 * (j & 1);
 }
 
 // 32 accumulator columns of this thread's row -> 32 values behind scales, affine, skip features and activation.
@@ -152,11 +143,12 @@ __device__ __forceinline__ void epilogue_i8_piece(uint32_t taddr, int cb, int nc
 // 32 rows x 128 bytes, swizzled, staged in shared memory, out by one TMA store where the rows are consecutive, else by
 // row pieces.  Columns that a TMA store cannot clip (its granule is 16 bytes) are written by every lane for its own row.
 template <bool F32, int ACT, bool RES>
-__device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int n0, int first, const EpiArgs& cols, float sx, const void* res_row,
-                                                 uint8_t* stage_w, float* s_col, char* yrow, int lane, bool contig, const CUtensorMap* mapY, int base_row) {
+__device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int n0, int first, float sx, const void* res_row,
+                                                 uint8_t* stage_w, const float* s_col, char* yrow, int lane, bool contig, const CUtensorMap* mapY, int base_row) {
   constexpr int W = F32 ? 32 : 64;          // columns of a staged piece
   constexpr int G = F32 ? 4 : 8;            // columns of 16 bytes
   constexpr int ES = F32 ? 4 : 2;
+  int piece = 0;
   for (int c0 = W * first; c0 < ncols; c0 += 2 * W) {
     if (elect_one()) bulk_wait_read0();     // an earlier store of this warp has read the staging tile
     __syncwarp();
@@ -164,10 +156,8 @@ __device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int 
     for (int h = 0; h < W / 32; ++h) {
       const int cb = c0 + 32 * h;
       if (cb < ncols) {
-        stage_columns(cols, cb, ncols, lane, s_col + 64 * h, s_col + 64 * h + 32);
-        __syncwarp();
         float f[32];
-        epilogue_i8_piece<F32, ACT, RES>(taddr + cb, cb, ncols, sx, s_col + 64 * h, s_col + 64 * h + 32, res_row, f);
+        epilogue_i8_piece<F32, ACT, RES>(taddr + cb, cb, ncols, sx, s_col + 64 * (piece + h), s_col + 64 * (piece + h) + 32, res_row, f);
 #pragma unroll
         for (int j = 0; j < 32 / G; ++j) {
           uint4 o;
@@ -187,7 +177,8 @@ __device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int 
         }
       }
     }
-    const int last = ncols - c0 < W ? ncols - c0 : W;   // columns of this piece
+    piece += W / 32;
+    const int last = ncols - c0 < W ? ncols - c0 : W;   // columns of this store
     if (contig) {
       fence_async_smem();
       __syncwarp();
@@ -380,51 +371,80 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
     bool ok = true;
     const int es = F32 ? 4 : 2;
     uint8_t* stage_w = out_stage + (warp - 2) * (32 * 128);
-    float* s_col = col_stage + (warp - 2) * 128;
-    for (int tile = pair; ok && tile < total; tile += npairs, ++it) {
-      const PairTile t = decode_pair_tile(p, s_prefix, tile, rank, cursor);
-      const int acc = it & 1;
-      const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
-      bool valid;
+    float* s_col = col_stage + (warp - 2) * (kPieces * 64);
+    auto fetch = [&](const PairTile& t, Ahead& a) {
       int pp, r;   // position and row inside the sample
       if (g.flat) {
         const int gr = t.row0 + m;
-        valid = gr < t.rows_end;
+        a.valid = gr < t.rows_end;
         pp = gr / g.R;
         r = gr - pp * g.R;
       } else {
         const int bi = m / g.bw;
         r = t.x0 + (m - bi * g.bw);
         pp = t.b0 + bi;
-        valid = bi < g.nb && r < g.R && pp < t.p_end;
+        a.valid = bi < g.nb && r < g.R && pp < t.p_end;
       }
-      int64_t out_row = 0;
-      float sx = 0.f;
-      if (valid) {
+      a.out_row = 0;
+      a.sx = 0.f;
+      if (a.valid) {
         const int smp = (g.y_input_order || P.scale_input_order) ? p.perm[pp] : 0;
-        out_row = (int64_t)(g.y_input_order ? smp : pp) * g.R + r;
-        sx = __ldg(P.x_scale + (int64_t)(P.scale_input_order ? smp : pp) * g.R + r);
+        a.out_row = (int64_t)(g.y_input_order ? smp : pp) * g.R + r;
+        a.sx = __ldg(P.x_scale + (int64_t)(P.scale_input_order ? smp : pp) * g.R + r);
       }
-      char* yrow = valid ? reinterpret_cast<char*>(p.y) + (out_row * p.ldy + t.n0) * es : nullptr;
-      const void* res_row = (RES && valid) ? reinterpret_cast<const char*>(p.residual) + (out_row * p.ldy + t.n0) * es : nullptr;
-      EpiArgs cols;
-      cols.w_scale = P.w_scale + t.n0;
-      cols.bias = p.bias ? p.bias + t.n0 : nullptr;
-      cols.bn_scale = p.bn_scale ? p.bn_scale + (int64_t)t.slice * p.bn_ld + t.n0 : nullptr;
-      cols.bn_shift = p.bn_scale ? p.bn_shift + (int64_t)t.slice * p.bn_ld + t.n0 : nullptr;
-      const int ncols = t.ncols;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        const int c = piece_col<F32>(first, j) + lane;
+        a.sw[j] = a.bias[j] = a.bn_shift[j] = 0.f;
+        a.bn_scale[j] = 1.f;
+        if (c < t.ncols) {
+          a.sw[j] = __ldg(P.w_scale + t.n0 + c);
+          if (p.bias) a.bias[j] = __ldg(p.bias + t.n0 + c);
+          if (p.bn_scale) {
+            a.bn_scale[j] = __ldg(p.bn_scale + (int64_t)t.slice * p.bn_ld + t.n0 + c);
+            a.bn_shift[j] = __ldg(p.bn_shift + (int64_t)t.slice * p.bn_ld + t.n0 + c);
+          }
+        }
+      }
+    };
+    PairTile t;
+    Ahead ahead;
+    if (pair < total) {
+      t = decode_pair_tile(p, s_prefix, pair, rank, cursor);
+      fetch(t, ahead);
+    }
+    for (int tile = pair; ok && tile < total; tile += npairs, ++it) {
+      const int acc = it & 1;
+      const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
+      __syncwarp();   // the tile before has been read out of s_col
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        s_col[64 * j + lane] = ahead.sw[j] * ahead.bn_scale[j];
+        s_col[64 * j + 32 + lane] = fmaf(ahead.bias[j], ahead.bn_scale[j], ahead.bn_shift[j]);
+      }
+      __syncwarp();
+      const float sx = ahead.sx;
+      const int64_t out_row = ahead.out_row;
+      const bool valid = ahead.valid;
+      const int n0 = t.n0, ncols = t.ncols, map = t.map;
+      char* yrow = valid ? reinterpret_cast<char*>(p.y) + (out_row * p.ldy + n0) * es : nullptr;
+      const void* res_row = (RES && valid) ? reinterpret_cast<const char*>(p.residual) + (out_row * p.ldy + n0) * es : nullptr;
       const long long base_row = __shfl_sync(0xffffffffu, (long long)out_row, 0);
       const bool contig = __all_sync(0xffffffffu, valid && out_row == base_row + lane) && t.ko >= 8;
+      if (tile + npairs < total) {
+        t = decode_pair_tile(p, s_prefix, tile + npairs, rank, cursor);
+        fetch(t, ahead);
+      }
 
       ok = __all_sync(0xffffffffu, dsn_wait(bar_tfull + 8 * acc, acc_phase, abort_flag, p.status, 64));
       if (!ok) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * g.BN);
-      const CUtensorMap* mY = &p.mapY[t.map];
+      const CUtensorMap* mY = &p.mapY[map];
       switch (p.act) {
-        case DSN_ACT_NONE: epilogue_i8_tile<F32, DSN_ACT_NONE, RES>(taddr, ncols, t.n0, first, cols, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
-        case DSN_ACT_RELU: epilogue_i8_tile<F32, DSN_ACT_RELU, RES>(taddr, ncols, t.n0, first, cols, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
-        default: epilogue_i8_tile<F32, DSN_ACT_GELU, RES>(taddr, ncols, t.n0, first, cols, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+        case DSN_ACT_NONE: epilogue_i8_tile<F32, DSN_ACT_NONE, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+        case DSN_ACT_RELU: epilogue_i8_tile<F32, DSN_ACT_RELU, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+        default: epilogue_i8_tile<F32, DSN_ACT_GELU, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
       }
       tc_fence_before();
       __syncwarp();

@@ -129,6 +129,24 @@ __global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant
   }
 }
 
+// Rows of short samples from input order to grouped order, 16 bytes a thread; a piece that runs past its row's k_in takes along
+// what lies there (the products' loads stop at k_in), except behind the very last row, where nothing need be allocated.
+__global__ void __launch_bounds__(kThreads) gather_i8_kernel(const __grid_constant__ RowsI8Params p, int8_t* dst, int64_t ld, FastDiv by_pieces, FastDiv by_R) {
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const uint64_t e = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (e >= (uint64_t)p.B * p.R * by_pieces.d) return;
+  const uint32_t row = e < 0x80000000ull ? dsn_div((uint32_t)e, by_pieces) : (uint32_t)(e / by_pieces.d);
+  const int c = 16 * (int)(e - (uint64_t)row * by_pieces.d);
+  const int pos = (int)dsn_div(row, by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
+  const PosInfo at = dsn_locate(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
+  if (at.slice < 0 || c >= p.k_in[at.slice]) return;
+  const int64_t from = (int64_t)at.sample * p.R + r;
+  const int8_t* s = p.x + from * p.ldx;
+  const bool tight = from + 1 == (int64_t)p.B * p.R;
+  *reinterpret_cast<uint4*>(dst + (int64_t)row * ld + c) = load16(s, c, tight ? p.C_in : (int)ld);
+}
+
 template <bool F32>
 cudaError_t pick(const RowsI8Params& p, cudaStream_t s) {
   const dim3 grid((p.max_ko + 15) / 16), block(kThreads);
@@ -142,4 +160,11 @@ cudaError_t pick(const RowsI8Params& p, cudaStream_t s) {
 
 cudaError_t dsn_launch_rows_i8(const RowsI8Params& p, int f32, cudaStream_t s) {
   return f32 ? pick<true>(p, s) : pick<false>(p, s);
+}
+
+cudaError_t dsn_launch_gather_i8(const RowsI8Params& p, int8_t* dst, int64_t ld, cudaStream_t s) {
+  const uint32_t pieces = (uint32_t)((p.max_ki + 15) / 16);
+  const int64_t n = (int64_t)p.B * p.R * pieces;
+  return dsn_launch(gather_i8_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, 1, p, dst, ld, dsn_fast_div(pieces),
+                    dsn_fast_div((uint32_t)p.R));
 }

@@ -181,3 +181,5 @@ struct RowsI8Params {
   int64_t ldx, ldw, ldy;
 };
 cudaError_t dsn_launch_rows_i8(const RowsI8Params& p, int f32, cudaStream_t s);
+// rows of x, in input order, to rows of `ld` bytes in grouped order
+cudaError_t dsn_launch_gather_i8(const RowsI8Params& p, int8_t* dst, int64_t ld, cudaStream_t s);

@@ -86,9 +86,10 @@ def check(got, c, ki, ko, y, act):
     assert np.all(np.abs(got - ref)[live] <= tol[live]), float(np.max((np.abs(got - ref) / tol)[live]))
 
 
-# few rows in all (a kernel of their own up to 32), one sample in input order, short samples gathered, long samples tiled alone
+# few rows in all (a kernel of their own up to 32), one sample in input order, samples tiled alone, many short samples (gathered)
 SIZES = [(1, 1, 16, 16), (1, 1, 1, 1), (3, 1, 130, 40), (8, 1, 4096, 100), (9, 1, 65, 33), (1, 17, 1000, 24), (32, 1, 777, 130), (2, 16, 64, 7),
-         (33, 1, 512, 64), (5, 9, 96, 70), (40, 7, 200, 300), (3, 64, 129, 130), (3, 65, 300, 257), (2, 197, 384, 520), (1, 300, 100, 260), (7, 128, 48, 9)]
+         (33, 1, 512, 64), (5, 9, 96, 70), (40, 7, 200, 300), (3, 64, 129, 130), (3, 65, 300, 257), (2, 197, 384, 520), (1, 300, 100, 260), (7, 128, 48, 9),
+         (2500, 2, 40, 24), (700, 9, 200, 100)]
 
 
 @pytest.mark.parametrize("y", ["bf16", "f32"])
@@ -211,9 +212,9 @@ def test_linear_i8_refusals(dsn, ctx):
     call(bad, w_scale=sw[:40]), call(bad, W=W[:40].clone()), call(bad, bias=sw[:40]), call(bad, bn_scale=torch.zeros(96, device=DEV))
     call(bad, residual=y), call(bad, R=2), call(bad, ldx=16)
     call(align, C_out=47, ko=(47, 8)), call(align, C_in=31, ki=(16, 31)), call(align, xx=torch.zeros(96, dtype=torch.int8, device=DEV)[1:])
-    r2, _ = groups(dsn, [0, 1] * 20, 2)
-    n = 40 * 32
-    big = dict(xx=torch.zeros(40, 32, dtype=torch.int8, device=DEV), ss=torch.zeros(40, device=DEV), yy=torch.zeros(40, 48, dtype=torch.bfloat16, device=DEV), rr=r2)
+    r2, _ = groups(dsn, [0, 1] * 2000, 2)
+    n = 4000 * 32
+    big = dict(xx=torch.zeros(4000, 32, dtype=torch.int8, device=DEV), ss=torch.zeros(4000, device=DEV), yy=torch.zeros(4000, 48, dtype=torch.bfloat16, device=DEV), rr=r2)
     call(dsn.ERR_WORKSPACE, **big), call(dsn.ERR_WORKSPACE, ws=torch.empty(n - 1, dtype=torch.uint8, device=DEV), **big)
     call(align, ws=torch.empty(n + 16, dtype=torch.uint8, device=DEV)[1:], **big)
     torch.cuda.synchronize()

@@ -88,12 +88,12 @@ def test_linear_i8_workspace(lib):
     ki, ko = (ctypes.c_int32 * 1)(40), (ctypes.c_int32 * 1)(64)
     d.R, d.C_in, d.C_out, d.ldx, d.ldw, d.ldy, d.T, d.k_in, d.k_out = 7, 40, 64, 48, 48, 64, 1, ki, ko
     d.W, d.w_scale, d.y_dtype = 16, 16, lib.BF16
-    assert lib.dsn_linear_i8_workspace_bytes(d, 100) == 100 * 7 * 48       # short samples in input order are gathered
-    assert lib.dsn_linear_i8_workspace_bytes(d, 1) == 0 and lib.dsn_linear_i8_workspace_bytes(d, 4) == 0
+    assert lib.dsn_linear_i8_workspace_bytes(d, 4000) == 4000 * 7 * 48     # many short samples in input order are gathered
+    assert lib.dsn_linear_i8_workspace_bytes(d, 1) == 0 and lib.dsn_linear_i8_workspace_bytes(d, 40) == 0
     d.in_order = lib.GROUPED
-    assert lib.dsn_linear_i8_workspace_bytes(d, 100) == 0
+    assert lib.dsn_linear_i8_workspace_bytes(d, 4000) == 0
     d.in_order, d.ldw = lib.INPUT_ORDER, 40                                # an invalid descriptor needs nothing: the call refuses it
-    assert lib.dsn_linear_i8_workspace_bytes(d, 100) == 0
+    assert lib.dsn_linear_i8_workspace_bytes(d, 4000) == 0
 
 
 def test_binding_refuses_tensors_that_are_not_on_a_gpu(lib):
