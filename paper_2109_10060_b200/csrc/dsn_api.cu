@@ -820,6 +820,7 @@ int run_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const LayerCall& c,
   fill_gemm_params(ctx, cc, r, y, false, p.g);
   p.x_scale = x_scale;
   p.w_scale = d->w_scale;
+  p.by_R = dsn_fast_div((uint32_t)d->R);
   p.scale_input_order = d->in_order == DSN_INPUT_ORDER;
   GemmGeom& g = p.g.g;
   g.pair = 1;

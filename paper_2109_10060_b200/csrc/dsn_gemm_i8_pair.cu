@@ -3,14 +3,16 @@
 // Tiles, barriers and roles are those of the bf16 pair kernel: a cluster of two CTAs owns a 256-row x BN-column tile, each
 // CTA loads its 128 rows and half of the weight tile, the even CTA issues the products of both.  A 128-byte
 // row piece holds 128 columns here, an instruction takes 32 of them, and at twice the products per byte the main loop of a
-// tile is half as long, so the epilogue weighs twice as much: a warp fetches the channels' factors and its rows' scales a tile ahead and
-// folds sw and the affine into one factor and one addend a column (in shared memory), which leaves a conversion, a multiplication and a
-// packed multiply-add per element.
+// tile is half as long, so the epilogue weighs twice as much.  A warp of its own prepares tiles ahead: it decodes the tile, folds sw and the
+// affine into one factor and one addend a column, and puts them with the rows' scales and places into shared memory (done by the
+// epilogue warps themselves, decoding and fetching took 1.7 of their 5.8 thousand cycles a tile); what is left to an element is
+// a conversion, a multiplication and a packed multiply-add.
 // Barriers (every CTA has the same layout):
 //   full[s]    even CTA only: one arrival (expect_tx for the bytes of both CTAs), completed by the loads of both
 //   empty[s]   both CTAs: the multicast commit frees the stage
 //   tfull[a]   both CTAs: the accumulator is complete
 //   tempty[a]  even CTA only, 2 x 8 arrivals: the epilogue warps of both CTAs
+//   ready[a], done[a]  each CTA its own: the prepared tile's hand-over to the epilogue warps and back
 // Every wait is bounded; on a timeout the CTA flags DSN_ERR_TIMEOUT and leaves its loops.
 #include "dsn_gemm_pair_device.cuh"
 #include "dsn_transformer.cuh"
@@ -21,7 +23,15 @@ using namespace dsn_gemm;
 
 constexpr int kBKB = 128;                          // bytes (= columns) of a chunk
 constexpr int kPieces = 4;                         // pieces of 32 columns that an epilogue warp takes of a tile, at most
-constexpr uint32_t kColBytes = kEpiWarps * kPieces * 32 * 8; // per epilogue warp: factor and addend of its columns
+constexpr int kI8Threads = kThreads + 32;          // one more warp: the tiles' preparation
+
+// What the epilogue reads for a tile besides the accumulator.
+struct Prepared {
+  float mul[256], add[256];   // per column: sw (and the affine's scale), bias (and the affine's shift)
+  float sx[BM];               // per row
+  int64_t row[BM];            // output row, -1: not part of the result
+  int n0, ncols, map, ko;
+};
 
 // D[tmem] (+)= A[smem] * B[smem]^T on both CTAs' tensor cores, signed 8-bit operands, 32-bit integer sums
 __device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -57,170 +67,187 @@ __device__ __forceinline__ void gelu_pair_i8(float a, float b, float& ra, float&
   unpack2(ffma2(h2, pack2(t0, t1), h2), ra, rb);
 }
 
-// What the epilogue reads for a tile besides the accumulator, fetched a tile ahead: this lane's column of each of the warp's pieces,
-// and this lane's row.
-struct Ahead {
-  float sw[kPieces], bias[kPieces], bn_scale[kPieces], bn_shift[kPieces];
-  float sx;
-  int64_t out_row;
-  bool valid;
-};
 // first column of piece j of a warp (bf16 rows are stored 64 columns at a time, fp32 rows 32; two warps share a lane quarter)
 template <bool F32>
 __device__ __forceinline__ int piece_col(int first, int j) {
   return F32 ? 32 * first + 64 * j : 64 * first + 128 * (j >> 1) + 32 * (j & 1);
 }
 
-// 32 accumulator columns of this thread's row -> 32 values behind scales, affine, skip features and activation.
-template <bool F32, int ACT, bool RES>
-__device__ __forceinline__ void epilogue_i8_piece(uint32_t taddr, int cb, int ncols, float sx, const float* s_mul, const float* s_add,
-                                                  const void* res_row, float (&f)[32]) {
-  uint32_t v[32];
-  tmem_ld_32x32(taddr, v);
-  tmem_ld_wait();
-  const uint64_t sx2 = pack2(sx, sx), zero2 = pack2(0.f, 0.f);
+// The same eight columns of skip features of this thread's row (columns `cb + 8 * j` ...).
+template <bool F32>
+__device__ __forceinline__ void add_residual(const void* res_row, int c, int ncols, float (&f)[8]) {
+  if (F32) {
+    const float* rp = static_cast<const float*>(res_row) + c;
+    if (c + 8 <= ncols) {
+      const float4 r0 = __ldg(reinterpret_cast<const float4*>(rp)), r1 = __ldg(reinterpret_cast<const float4*>(rp) + 1);
+      f[0] += r0.x; f[1] += r0.y; f[2] += r0.z; f[3] += r0.w;
+      f[4] += r1.x; f[5] += r1.y; f[6] += r1.z; f[7] += r1.w;
+    } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float4 m = reinterpret_cast<const float4*>(s_mul)[j], d = reinterpret_cast<const float4*>(s_add)[j];
-    uint64_t a = ffma2(pack2((float)(int)v[4 * j], (float)(int)v[4 * j + 1]), sx2, zero2);
-    uint64_t b = ffma2(pack2((float)(int)v[4 * j + 2], (float)(int)v[4 * j + 3]), sx2, zero2);
-    a = ffma2(a, pack2(m.x, m.y), pack2(d.x, d.y));
-    b = ffma2(b, pack2(m.z, m.w), pack2(d.z, d.w));
-    unpack2(a, f[4 * j], f[4 * j + 1]);
-    unpack2(b, f[4 * j + 2], f[4 * j + 3]);
-  }
-  if (RES && res_row) {
-    if (F32) {
-      const float* rp = static_cast<const float*>(res_row) + cb;
-      if (cb + 32 <= ncols) {
+      for (int e = 0; e < 8; ++e)
+        if (c + e < ncols) f[e] += __ldg(rp + e);
+    }
+  } else {
+    const __nv_bfloat16* rp = static_cast<const __nv_bfloat16*>(res_row) + c;
+    if (c + 8 <= ncols) {
+      const uint4 r = __ldg(reinterpret_cast<const uint4*>(rp));
+      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float4 r = __ldg(reinterpret_cast<const float4*>(rp) + j);
-          f[4 * j] += r.x; f[4 * j + 1] += r.y; f[4 * j + 2] += r.z; f[4 * j + 3] += r.w;
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 32; ++c)
-          if (cb + c < ncols) f[c] += __ldg(rp + c);
+      for (int e = 0; e < 4; ++e) {
+        f[2 * e] += __uint_as_float(w[e] << 16);
+        f[2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
       }
     } else {
-      const __nv_bfloat16* rp = static_cast<const __nv_bfloat16*>(res_row) + cb;
-      if (cb + 32 <= ncols) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint4 r = __ldg(reinterpret_cast<const uint4*>(rp) + j);
-          const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f[8 * j + 2 * e] += __uint_as_float(w[e] << 16);
-            f[8 * j + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 32; ++c)
-          if (cb + c < ncols) f[c] += __bfloat162float(rp[c]);
-      }
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < 32; c += 2) {
-    if (ACT == DSN_ACT_RELU) {
-      f[c] = relu_nan(f[c]);
-      f[c + 1] = relu_nan(f[c + 1]);
-    } else if (ACT == DSN_ACT_GELU) {
-      if (F32) {
-        f[c] = 0.5f * f[c] * (1.f + erff(f[c] * 0.70710678118654752f));
-        f[c + 1] = 0.5f * f[c + 1] * (1.f + erff(f[c + 1] * 0.70710678118654752f));
-      } else {
-        gelu_pair_i8(f[c], f[c + 1], f[c], f[c + 1]);
-      }
+      for (int e = 0; e < 8; ++e)
+        if (c + e < ncols) f[e] += __bfloat162float(rp[e]);
     }
   }
 }
 
-// Epilogue of one tile for one warp; the warp takes the pieces of 128 bytes (64 bf16 or 32 fp32 columns) `first`, `first + 2`, ...:
-// 32 rows x 128 bytes, swizzled, staged in shared memory, out by one TMA store where the rows are consecutive, else by
-// row pieces.  Columns that a TMA store cannot clip (its granule is 16 bytes) are written by every lane for its own row.
+// 32 accumulator columns of this thread's row -> scales, affine, skip features, activation -> the row's 16-byte places from `place` on
+// in the warp's staging tile.
 template <bool F32, int ACT, bool RES>
-__device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int n0, int first, float sx, const void* res_row,
-                                                 uint8_t* stage_w, const float* s_col, char* yrow, int lane, bool contig, const CUtensorMap* mapY, int base_row) {
+__device__ __forceinline__ void epilogue_i8_piece(const uint32_t (&v)[32], int cb, int ncols, float sx, const float* s_mul, const float* s_add,
+                                                  const void* res_row, uint8_t* stage_w, int lane, int place) {
+  const uint64_t sx2 = pack2(sx, sx), zero2 = pack2(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {   // eight columns at a time
+    float f[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 m = reinterpret_cast<const float4*>(s_mul)[2 * j + h], d = reinterpret_cast<const float4*>(s_add)[2 * j + h];
+      const int c = 8 * j + 4 * h;
+      uint64_t a = ffma2(pack2((float)(int)v[c], (float)(int)v[c + 1]), sx2, zero2);
+      uint64_t b = ffma2(pack2((float)(int)v[c + 2], (float)(int)v[c + 3]), sx2, zero2);
+      a = ffma2(a, pack2(m.x, m.y), pack2(d.x, d.y));
+      b = ffma2(b, pack2(m.z, m.w), pack2(d.z, d.w));
+      unpack2(a, f[4 * h], f[4 * h + 1]);
+      unpack2(b, f[4 * h + 2], f[4 * h + 3]);
+    }
+    if (RES && res_row) add_residual<F32>(res_row, cb + 8 * j, ncols, f);
+#pragma unroll
+    for (int c = 0; c < 8; c += 2) {
+      if (ACT == DSN_ACT_RELU) {
+        f[c] = relu_nan(f[c]);
+        f[c + 1] = relu_nan(f[c + 1]);
+      } else if (ACT == DSN_ACT_GELU) {
+        if (F32) {
+          f[c] = 0.5f * f[c] * (1.f + erff(f[c] * 0.70710678118654752f));
+          f[c + 1] = 0.5f * f[c + 1] * (1.f + erff(f[c + 1] * 0.70710678118654752f));
+        } else {
+          gelu_pair_i8(f[c], f[c + 1], f[c], f[c + 1]);
+        }
+      }
+    }
+    if (F32) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<float4*>(stage_w + lane * 128 + (((place + 2 * j + h) ^ (lane & 7)) << 4)) =
+            make_float4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
+    } else {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+        w[e] = *reinterpret_cast<uint32_t*>(&b);
+      }
+      *reinterpret_cast<uint4*>(stage_w + lane * 128 + (((place + j) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+// The staged piece (32 rows x 128 bytes, swizzled; columns c0 .. of the tile) leaves: one TMA store where the rows are consecutive, else
+// eight lanes a row.  Columns that a TMA store cannot clip (its granule is 16 bytes) are written by every lane for its own row.
+template <bool F32>
+__device__ __forceinline__ void store_piece(uint8_t* stage_w, char* yrow, int c0, int ncols, int n0, int lane, bool contig, const CUtensorMap* mapY, int base_row) {
   constexpr int W = F32 ? 32 : 64;          // columns of a staged piece
   constexpr int G = F32 ? 4 : 8;            // columns of 16 bytes
   constexpr int ES = F32 ? 4 : 2;
-  int piece = 0;
-  for (int c0 = W * first; c0 < ncols; c0 += 2 * W) {
-    if (elect_one()) bulk_wait_read0();     // an earlier store of this warp has read the staging tile
+  const int last = ncols - c0 < W ? ncols - c0 : W;
+  if (contig) {
+    fence_async_smem();
     __syncwarp();
-#pragma unroll
-    for (int h = 0; h < W / 32; ++h) {
-      const int cb = c0 + 32 * h;
-      if (cb < ncols) {
-        float f[32];
-        epilogue_i8_piece<F32, ACT, RES>(taddr + cb, cb, ncols, sx, s_col + 64 * (piece + h), s_col + 64 * (piece + h) + 32, res_row, f);
-#pragma unroll
-        for (int j = 0; j < 32 / G; ++j) {
-          uint4 o;
-          if (F32) {
-            o = make_uint4(__float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j + 2]), __float_as_uint(f[4 * j + 3]));
-          } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              __nv_bfloat162 b = __floats2bfloat162_rn(f[(G * j + 2 * e) & 31], f[(G * j + 2 * e + 1) & 31]);
-              w[e] = *reinterpret_cast<uint32_t*>(&b);
-            }
-            o = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          const int jj = (32 / G) * h + j;   // 16-byte piece of the 128-byte row
-          *reinterpret_cast<uint4*>(stage_w + lane * 128 + ((jj ^ (lane & 7)) << 4)) = o;
-        }
+    if (elect_one()) {
+      tma_store_2d(mapY, n0 + c0, base_row, smem_u32(stage_w));
+      bulk_commit();
+    }
+    const int whole = last & ~(G - 1);
+    if (whole != last) {
+      const uint8_t* sp = stage_w + lane * 128 + (((whole / G) ^ (lane & 7)) << 4);
+      for (int e = 0; e < last - whole; ++e) {
+        if (F32) reinterpret_cast<float*>(yrow)[c0 + whole + e] = reinterpret_cast<const float*>(sp)[e];
+        else reinterpret_cast<uint16_t*>(yrow)[c0 + whole + e] = reinterpret_cast<const uint16_t*>(sp)[e];
       }
     }
-    piece += W / 32;
-    const int last = ncols - c0 < W ? ncols - c0 : W;   // columns of this store
-    if (contig) {
-      fence_async_smem();
-      __syncwarp();
-      if (elect_one()) {
-        tma_store_2d(mapY, n0 + c0, base_row, smem_u32(stage_w));
-        bulk_commit();
-      }
-      const int whole = last & ~(G - 1);
-      if (whole != last) {
-        const uint8_t* sp = stage_w + lane * 128 + (((whole / G) ^ (lane & 7)) << 4);
-        for (int e = 0; e < last - whole; ++e) {
-          if (F32) reinterpret_cast<float*>(yrow)[c0 + whole + e] = reinterpret_cast<const float*>(sp)[e];
-          else reinterpret_cast<uint16_t*>(yrow)[c0 + whole + e] = reinterpret_cast<const uint16_t*>(sp)[e];
-        }
-      }
-    } else {
-      __syncwarp();
-      const int j = lane & 7;
+  } else {
+    __syncwarp();
+    const int j = lane & 7;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {          // eight lanes a row, 16 bytes each
-        const int row = 4 * i + (lane >> 3);
-        char* rp = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(yrow), row));
-        if (rp != nullptr && G * j < last) {
-          const uint8_t* sp = stage_w + row * 128 + ((j ^ (row & 7)) << 4);
-          char* dst = rp + (int64_t)(c0 + G * j) * ES;
-          if (G * j + G <= last) {
-            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(sp);
-          } else {
-            for (int e = 0; e < last - G * j; ++e) {
-              if (F32) reinterpret_cast<float*>(dst)[e] = reinterpret_cast<const float*>(sp)[e];
-              else reinterpret_cast<uint16_t*>(dst)[e] = reinterpret_cast<const uint16_t*>(sp)[e];
-            }
+    for (int i = 0; i < 8; ++i) {          // eight lanes a row, 16 bytes each
+      const int row = 4 * i + (lane >> 3);
+      char* rp = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(yrow), row));
+      if (rp != nullptr && G * j < last) {
+        const uint8_t* sp = stage_w + row * 128 + ((j ^ (row & 7)) << 4);
+        char* dst = rp + (int64_t)(c0 + G * j) * ES;
+        if (G * j + G <= last) {
+          *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(sp);
+        } else {
+          for (int e = 0; e < last - G * j; ++e) {
+            if (F32) reinterpret_cast<float*>(dst)[e] = reinterpret_cast<const float*>(sp)[e];
+            else reinterpret_cast<uint16_t*>(dst)[e] = reinterpret_cast<const uint16_t*>(sp)[e];
           }
         }
       }
-      __syncwarp();
     }
+    __syncwarp();
   }
 }
 
+// Epilogue of one tile for one warp.  The next piece's columns are on their way from TMEM while a piece is worked on, and the accumulator
+// goes back to the issuing warp (`tempty`, in the even CTA) as soon as the last of them have arrived.
+template <bool F32, int ACT, bool RES>
+__device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int n0, int first, float sx, const void* res_row,
+                                                 uint8_t* stage_w, const Prepared* prep, char* yrow, int lane, bool contig, const CUtensorMap* mapY, int base_row,
+                                                 uint32_t tempty, int bn) {
+  // Loads run whether a piece exists or not (a missing one reads the tile's last columns again): straight code keeps the two blocks of 32
+  // registers in place.
+  auto load = [&](int j, uint32_t (&v)[32]) {
+    const int cb = piece_col<F32>(first, j);
+    tmem_ld_32x32(taddr + (cb + 32 <= bn ? cb : bn - 32), v);
+  };
+  auto work = [&](const int j, const uint32_t (&v)[32]) {
+    const int cb = piece_col<F32>(first, j);
+    if (cb < ncols) {
+      if (F32 || !(j & 1)) {                  // a new staging tile: an earlier store of this warp has read it
+        if (elect_one()) bulk_wait_read0();
+        __syncwarp();
+      }
+      epilogue_i8_piece<F32, ACT, RES>(v, cb, ncols, sx, prep->mul + cb, prep->add + cb, res_row, stage_w, lane, (F32 || !(j & 1)) ? 0 : 4);
+      if (F32 || (j & 1) || piece_col<F32>(first, j + 1) >= ncols)
+        store_piece<F32>(stage_w, yrow, F32 ? cb : (cb & ~63), ncols, n0, lane, contig, mapY, base_row);
+    }
+  };
+  uint32_t va[32], vb[32];
+  load(0, va);
+  tmem_ld_wait();
+  load(1, vb);
+  work(0, va);
+  tmem_ld_wait();
+  load(2, va);
+  work(1, vb);
+  tmem_ld_wait();
+  load(3, vb);
+  work(2, va);
+  tmem_ld_wait();
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive_cluster(tempty);
+  work(3, vb);
+}
+
 template <bool F32, bool RES>
-__global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_constant__ GemmI8Params P) {
+__global__ void __launch_bounds__(kI8Threads, 1) gemm_i8_pair_kernel(const __grid_constant__ GemmI8Params P) {
   extern __shared__ uint8_t smem_raw[];
   const GemmParams& p = P.g;
   const GemmGeom& g = p.g;
@@ -234,14 +261,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
   const uint32_t bar_tempty = bar_tfull + 16;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 16 * kMaxStages + 32);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 16 * kMaxStages + 36);
+  const uint32_t bar_ready = base + 16 * kMaxStages + 48, bar_done = bar_ready + 16;
 
   const int stages = g.stages;
   const uint32_t bh_bytes = (uint32_t)(g.BN / 2) * kBKB;  // this CTA's half of the weight tile
   const uint32_t stage_bytes = kABytes + bh_bytes;        // kABytes: 128 rows of 128 bytes
   const uint32_t tiles_base = base + kCtrlBytes;
   uint8_t* out_stage = smem + kCtrlBytes + (size_t)stages * stage_bytes;
-  float* col_stage = reinterpret_cast<float*>(out_stage + kStageOutBytes);
-  int32_t* s_prefix = reinterpret_cast<int32_t*>(out_stage + kStageOutBytes + kColBytes);
+  Prepared* prepared = reinterpret_cast<Prepared*>(out_stage + kStageOutBytes);
+  int32_t* s_prefix = reinterpret_cast<int32_t*>(prepared + 2);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
@@ -256,6 +284,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
     for (int a = 0; a < 2; ++a) {
       mbar_init(bar_tfull + 8 * a, 1);
       mbar_init(bar_tempty + 8 * a, 2 * kEpiWarps);
+      mbar_init(bar_ready + 8 * a, 1);
+      mbar_init(bar_done + 8 * a, kEpiWarps);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -362,6 +392,80 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
         if (ok && elect_one()) umma_commit_pair(bar_tfull + 8 * acc);
       }
     }
+  } else if (warp == 2 + kEpiWarps) {
+    // ------------------------------------------------------------------ preparation (both CTAs): four rows and eight columns a lane
+    int it = 0;
+    for (int tile = pair; tile < total; tile += npairs, ++it) {
+      const PairTile t = decode_pair_tile(p, s_prefix, tile, rank, cursor);
+      float mul[8], add[8], sx[4];
+      int64_t row[4];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = 32 * j + lane;
+        mul[j] = add[j] = 0.f;
+        if (c < t.ncols) {
+          mul[j] = __ldg(P.w_scale + t.n0 + c);
+          if (p.bias) add[j] = __ldg(p.bias + t.n0 + c);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int m = 32 * j + lane;
+        int pp, r;   // position and row inside the sample
+        bool valid;
+        if (g.flat) {
+          const int gr = t.row0 + m;
+          valid = gr < t.rows_end;
+          pp = (int)dsn_div((uint32_t)gr, P.by_R);
+          r = gr - pp * g.R;
+        } else {
+          const int bi = g.nb == 1 ? 0 : m / g.bw;
+          r = t.x0 + (m - bi * g.bw);
+          pp = t.b0 + bi;
+          valid = m < g.bw * g.nb && r < g.R && pp < t.p_end;
+        }
+        sx[j] = 0.f;
+        row[j] = -1;
+        if (valid) {
+          const int smp = (g.y_input_order || P.scale_input_order) ? p.perm[pp] : 0;
+          row[j] = (int64_t)(g.y_input_order ? smp : pp) * g.R + r;
+          sx[j] = __ldg(P.x_scale + (int64_t)(P.scale_input_order ? smp : pp) * g.R + r);
+        }
+      }
+      if (p.bn_scale) {
+        const int64_t at = (int64_t)t.slice * p.bn_ld + t.n0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = 32 * j + lane;
+          if (c < t.ncols) {
+            const float sc = __ldg(p.bn_scale + at + c);
+            mul[j] *= sc;
+            add[j] = fmaf(add[j], sc, __ldg(p.bn_shift + at + c));
+          }
+        }
+      }
+      const int b = it & 1;
+      if (!__all_sync(0xffffffffu, dsn_wait(bar_done + 8 * b, ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, p.status, 65))) break;
+      Prepared& o = prepared[b];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        o.mul[32 * j + lane] = mul[j];
+        o.add[32 * j + lane] = add[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o.sx[32 * j + lane] = sx[j];
+        o.row[32 * j + lane] = row[j];
+      }
+      if (lane == 0) {
+        o.n0 = t.n0;
+        o.ncols = t.ncols;
+        o.map = t.map;
+        o.ko = t.ko;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_ready + 8 * b);
+    }
   } else {
     // ------------------------------------------------------------------ epilogue (warps 2..9, both CTAs)
     const int q = warp & 3;
@@ -371,84 +475,34 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
     bool ok = true;
     const int es = F32 ? 4 : 2;
     uint8_t* stage_w = out_stage + (warp - 2) * (32 * 128);
-    float* s_col = col_stage + (warp - 2) * (kPieces * 64);
-    auto fetch = [&](const PairTile& t, Ahead& a) {
-      int pp, r;   // position and row inside the sample
-      if (g.flat) {
-        const int gr = t.row0 + m;
-        a.valid = gr < t.rows_end;
-        pp = gr / g.R;
-        r = gr - pp * g.R;
-      } else {
-        const int bi = m / g.bw;
-        r = t.x0 + (m - bi * g.bw);
-        pp = t.b0 + bi;
-        a.valid = bi < g.nb && r < g.R && pp < t.p_end;
-      }
-      a.out_row = 0;
-      a.sx = 0.f;
-      if (a.valid) {
-        const int smp = (g.y_input_order || P.scale_input_order) ? p.perm[pp] : 0;
-        a.out_row = (int64_t)(g.y_input_order ? smp : pp) * g.R + r;
-        a.sx = __ldg(P.x_scale + (int64_t)(P.scale_input_order ? smp : pp) * g.R + r);
-      }
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) {
-        const int c = piece_col<F32>(first, j) + lane;
-        a.sw[j] = a.bias[j] = a.bn_shift[j] = 0.f;
-        a.bn_scale[j] = 1.f;
-        if (c < t.ncols) {
-          a.sw[j] = __ldg(P.w_scale + t.n0 + c);
-          if (p.bias) a.bias[j] = __ldg(p.bias + t.n0 + c);
-          if (p.bn_scale) {
-            a.bn_scale[j] = __ldg(p.bn_scale + (int64_t)t.slice * p.bn_ld + t.n0 + c);
-            a.bn_shift[j] = __ldg(p.bn_shift + (int64_t)t.slice * p.bn_ld + t.n0 + c);
-          }
-        }
-      }
-    };
-    PairTile t;
-    Ahead ahead;
-    if (pair < total) {
-      t = decode_pair_tile(p, s_prefix, pair, rank, cursor);
-      fetch(t, ahead);
-    }
     for (int tile = pair; ok && tile < total; tile += npairs, ++it) {
       const int acc = it & 1;
       const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
-      __syncwarp();   // the tile before has been read out of s_col
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) {
-        s_col[64 * j + lane] = ahead.sw[j] * ahead.bn_scale[j];
-        s_col[64 * j + 32 + lane] = fmaf(ahead.bias[j], ahead.bn_scale[j], ahead.bn_shift[j]);
-      }
-      __syncwarp();
-      const float sx = ahead.sx;
-      const int64_t out_row = ahead.out_row;
-      const bool valid = ahead.valid;
-      const int n0 = t.n0, ncols = t.ncols, map = t.map;
+      ok = __all_sync(0xffffffffu, dsn_wait(bar_ready + 8 * acc, acc_phase, abort_flag, p.status, 66));
+      if (!ok) break;
+      const Prepared* prep = prepared + acc;
+      const float sx = prep->sx[m];
+      const int64_t out_row = prep->row[m];
+      const bool valid = out_row >= 0;
+      const int n0 = prep->n0, ncols = prep->ncols;
       char* yrow = valid ? reinterpret_cast<char*>(p.y) + (out_row * p.ldy + n0) * es : nullptr;
       const void* res_row = (RES && valid) ? reinterpret_cast<const char*>(p.residual) + (out_row * p.ldy + n0) * es : nullptr;
       const long long base_row = __shfl_sync(0xffffffffu, (long long)out_row, 0);
-      const bool contig = __all_sync(0xffffffffu, valid && out_row == base_row + lane) && t.ko >= 8;
-      if (tile + npairs < total) {
-        t = decode_pair_tile(p, s_prefix, tile + npairs, rank, cursor);
-        fetch(t, ahead);
-      }
+      const bool contig = __all_sync(0xffffffffu, valid && out_row == base_row + lane) && prep->ko >= 8;
 
       ok = __all_sync(0xffffffffu, dsn_wait(bar_tfull + 8 * acc, acc_phase, abort_flag, p.status, 64));
       if (!ok) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * g.BN);
-      const CUtensorMap* mY = &p.mapY[map];
+      const CUtensorMap* mY = &p.mapY[prep->map];
+      const uint32_t tempty = leader_addr(bar_tempty + 8 * acc);   // the even CTA's issuing warp waits on it
       switch (p.act) {
-        case DSN_ACT_NONE: epilogue_i8_tile<F32, DSN_ACT_NONE, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
-        case DSN_ACT_RELU: epilogue_i8_tile<F32, DSN_ACT_RELU, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
-        default: epilogue_i8_tile<F32, DSN_ACT_GELU, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, s_col, yrow, lane, contig, mY, (int)base_row); break;
+        case DSN_ACT_NONE: epilogue_i8_tile<F32, DSN_ACT_NONE, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, prep, yrow, lane, contig, mY, (int)base_row, tempty, g.BN); break;
+        case DSN_ACT_RELU: epilogue_i8_tile<F32, DSN_ACT_RELU, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, prep, yrow, lane, contig, mY, (int)base_row, tempty, g.BN); break;
+        default: epilogue_i8_tile<F32, DSN_ACT_GELU, RES>(taddr, ncols, n0, first, sx, res_row, stage_w, prep, yrow, lane, contig, mY, (int)base_row, tempty, g.BN); break;
       }
-      tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(leader_addr(bar_tempty + 8 * acc));  // the even CTA's issuing warp waits on it
+      if (lane == 0) mbar_arrive(bar_done + 8 * acc);
     }
     if (elect_one()) bulk_wait0();  // the lane that issued this warp's TMA stores
   }
@@ -467,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_pair_kernel(const __grid_
 }  // namespace
 
 size_t dsn_gemm_i8_smem_bytes(int BN, int stages, int G) {
-  return 1024 + kCtrlBytes + (size_t)stages * (kABytes + (size_t)(BN / 2) * kBKB) + kStageOutBytes + kColBytes + sizeof(int32_t) * (3 * (size_t)G + 3);
+  return 1024 + kCtrlBytes + (size_t)stages * (kABytes + (size_t)(BN / 2) * kBKB) + kStageOutBytes + 2 * sizeof(Prepared) + sizeof(int32_t) * (3 * (size_t)G + 3);
 }
 
 cudaError_t dsn_launch_gemm_i8(const GemmI8Params& p, int f32, int clusters, size_t smem_bytes, cudaStream_t s) {
@@ -478,5 +532,5 @@ cudaError_t dsn_launch_gemm_i8(const GemmI8Params& p, int f32, int clusters, siz
                                  : form == 1 ? gemm_i8_pair_kernel<false, true> : gemm_i8_pair_kernel<false, false>;
   const cudaError_t e = dsn_ensure_dynamic_smem(kernel, smem_bytes, configured[form]);
   if (e != cudaSuccess) return e;
-  return dsn_launch(kernel, dim3(2 * clusters), dim3(kThreads), smem_bytes, s, 2, p);
+  return dsn_launch(kernel, dim3(2 * clusters), dim3(kI8Threads), smem_bytes, s, 2, p);
 }

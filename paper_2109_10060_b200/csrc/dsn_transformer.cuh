@@ -154,6 +154,7 @@ struct GemmI8Params {
   const float* x_scale;   // one per row of x
   const float* w_scale;   // one per output channel
   int32_t scale_input_order;  // rows of x_scale by sample (else by grouped position)
+  FastDiv by_R;
 };
 size_t dsn_gemm_i8_smem_bytes(int BN, int stages, int G);
 cudaError_t dsn_launch_gemm_i8(const GemmI8Params& p, int f32, int clusters, size_t smem_bytes, cudaStream_t s);
