@@ -25,6 +25,25 @@ constexpr int kBKB = 128;                          // bytes (= columns) of a chu
 constexpr int kPieces = 4;                         // pieces of 32 columns that an epilogue warp takes of a tile, at most
 constexpr int kI8Threads = kThreads + 32;          // one more warp: the tiles' preparation
 
+__device__ __forceinline__ float relu_nan(float v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(0.f));
+  return r;
+}
+// GELU for fp32 outputs.  The distribution function by Abramowitz and Stegun's formula 7.1.26 (erf within 1.5e-7):
+// erf(z) = 1 - (a1 t + ... + a5 t^5) exp(-z^2), t = 1 / (1 + p z), z >= 0; x Phi(x) = max(x, 0) - |x| q / 2 with q the product.  A fifth of the
+// instructions of erff, whose code for a tile's 32 columns kept the warps waiting for instructions.
+__device__ __forceinline__ float gelu_f32(float x) {
+  const float z = fabsf(x) * 0.70710678118654752f;
+  const float t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
+  float q = fmaf(t, 1.061405429f, -1.453152027f);
+  q = fmaf(t, q, 1.421413741f);
+  q = fmaf(t, q, -0.284496736f);
+  q = fmaf(t, q, 0.254829592f) * t;
+  q *= __expf(-z * z);
+  return relu_nan(x) - 0.5f * fminf(fabsf(x), 1e30f) * q;   // (infinity: 0 times it would be no number)
+}
+
 // What the epilogue reads for a tile besides the accumulator.
 struct Prepared {
   float mul[256], add[256];   // per column: sw (and the affine's scale), bias (and the affine's shift)
@@ -45,11 +64,6 @@ __device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, u
 // Instruction descriptor: D 32-bit integer, A and B signed 8-bit, both K-major, M x N tile.
 __device__ __forceinline__ uint32_t make_idesc_i8(int M, int N) {
   return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-__device__ __forceinline__ float relu_nan(float v) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(0.f));
-  return r;
 }
 
 // The fitted GELU for two values.  Its odd quintic turns round beyond |v| = 8, where the tanh has long been +-1, so v^2 is
@@ -133,8 +147,8 @@ __device__ __forceinline__ void epilogue_i8_piece(const uint32_t (&v)[32], int c
         f[c + 1] = relu_nan(f[c + 1]);
       } else if (ACT == DSN_ACT_GELU) {
         if (F32) {
-          f[c] = 0.5f * f[c] * (1.f + erff(f[c] * 0.70710678118654752f));
-          f[c + 1] = 0.5f * f[c + 1] * (1.f + erff(f[c + 1] * 0.70710678118654752f));
+          f[c] = gelu_f32(f[c]);
+          f[c + 1] = gelu_f32(f[c + 1]);
         } else {
           gelu_pair_i8(f[c], f[c + 1], f[c], f[c + 1]);
         }
@@ -230,20 +244,21 @@ __device__ __forceinline__ void epilogue_i8_tile(uint32_t taddr, int ncols, int 
   };
   uint32_t va[32], vb[32];
   load(0, va);
-  tmem_ld_wait();
-  load(1, vb);
-  work(0, va);
-  tmem_ld_wait();
-  load(2, va);
-  work(1, vb);
-  tmem_ld_wait();
-  load(3, vb);
-  work(2, va);
-  tmem_ld_wait();
-  tc_fence_before();
-  __syncwarp();
-  if (lane == 0) mbar_arrive_cluster(tempty);
-  work(3, vb);
+#pragma unroll 1   // two pieces a round: the code of four side by side waited for instructions
+  for (int j = 0; j < kPieces; j += 2) {
+    tmem_ld_wait();
+    load(j + 1, vb);
+    work(j, va);
+    tmem_ld_wait();
+    if (j + 2 < kPieces) {
+      load(j + 2, va);
+    } else {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(tempty);
+    }
+    work(j + 1, vb);
+  }
 }
 
 template <bool F32, bool RES>

@@ -4,13 +4,17 @@
 // the warp-level 8-bit matrix instruction (16 channels x 8 rows x 32 columns): at most 32 rows cannot fill the 128 rows of a
 // tensor-memory tile, and this form takes its operands straight from registers.  The order of the columns inside a sum
 // is free, so a lane's 16 consecutive bytes serve as its pieces of two instructions, the same way for weights and rows.
+// One row of 4096 x 4096 takes 5.3 us against 2.6 for its bytes (launch, one round trip to memory and the meeting are the rest), 32 rows 9.5 us; from
+// 33 rows on the tensor-memory form is level (15 us with the gather of its rows).
 // Rows of narrower paths are zero beyond their k_in, so all rows share one reduction over the widest path's columns.
 #include "dsn_transformer.cuh"
 
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kAhead = 4;   // steps of 64 columns whose weights are in flight
+// Steps of 64 columns whose weights a warp has in flight.  One row, 4096 x 4096 from L2: 4.7, 5.3, 5.7 us with 1, 2, 4 (more registers, fewer CTAs an
+// SM); 8192 x 8192 from memory: 17.5, 17.3, 26.5 us; 16 rows of 4096 x 8192: 17.0, 16.4, 16.2 us.
+constexpr int kAhead = 2;
 
 struct RowInfo {
   int64_t src, dst;   // rows of x and y; dst < 0: the row does not exist
@@ -23,19 +27,23 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, ui
                : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// 16 bytes of a row from byte `off`, zero at and beyond `end`
-__device__ __forceinline__ uint4 load16(const int8_t* row, int off, int end) {
-  if (off + 16 <= end) return __ldg(reinterpret_cast<const uint4*>(row + off));
+// The bytes off .. off + 15 of a row, zero at and beyond `end`.  (Out of line: inlined at each of the loads, the byte-wise end of a row was most
+// of the kernel's code.)
+__device__ __noinline__ uint4 load_end(const int8_t* row, int off, int end) {
   uint32_t w[4] = {0u, 0u, 0u, 0u};
-  if (off < end) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (off + i < end) w[i >> 2] |= (uint32_t)(uint8_t)row[off + i] << (8 * (i & 3));
-  }
+  for (int i = 0; i < 16; ++i)
+    if (off + i < end) w[i >> 2] |= (uint32_t)(uint8_t)row[off + i] << (8 * (i & 3));
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ uint4 load16(const int8_t* row, int off, int end) {
+  if (off + 16 <= end) return __ldg(reinterpret_cast<const uint4*>(row + off));
+  if (off >= end) return make_uint4(0u, 0u, 0u, 0u);
+  return load_end(row, off, end);
+}
 
-template <bool F32, int NT>   // NT tiles of eight rows
+// NT tiles of eight rows.
+template <bool F32, int NT>
 __global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant__ RowsI8Params p) {
   __shared__ RowInfo info[8 * NT];
   __shared__ int part[kWarps][8 * NT][17];
@@ -44,20 +52,26 @@ __global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant
   const int o0 = blockIdx.x * 16;
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
-  const int steps = (p.max_ki + 63) >> 6;
-  const int8_t* w0 = p.W + (int64_t)(o0 + g) * p.ldw;
-  const int8_t* w1 = w0 + 8 * p.ldw;
-  const int end0 = o0 + g < p.max_ko ? p.max_ki : 0, end1 = o0 + g + 8 < p.max_ko ? p.max_ki : 0;
+  // channels beyond the last read the last one's weights: their sums go nowhere
+  const int top = p.max_ko - 1;
+  const int8_t* w0 = p.W + (int64_t)(o0 + g < top ? o0 + g : top) * p.ldw + 16 * q;
+  const int8_t* w1 = p.W + (int64_t)(o0 + g + 8 < top ? o0 + g + 8 : top) * p.ldw + 16 * q;
+  const int whole = p.max_ki >> 6;       // steps that lie inside the widest path
   uint4 a0[kAhead], a1[kAhead];
+  auto fetch = [&](int j, int st) {
+    if (st < whole) {
+      a0[j] = __ldg(reinterpret_cast<const uint4*>(w0 + 64 * st));
+      a1[j] = __ldg(reinterpret_cast<const uint4*>(w1 + 64 * st));
+    }
+  };
 #pragma unroll
-  for (int j = 0; j < kAhead; ++j) {   // the weights do not wait for the rows' paths
-    const int st = warp + j * kWarps;
-    a0[j] = load16(w0, 64 * st + 16 * q, st < steps ? end0 : 0);
-    a1[j] = load16(w1, 64 * st + 16 * q, st < steps ? end1 : 0);
-  }
+  for (int j = 0; j < kAhead; ++j) fetch(j, warp + j * kWarps);   // the weights do not wait for the rows' paths
+  // this thread's output channel at the end is the same for all of its rows
+  const int o = o0 + (threadIdx.x & 15);
+  const float sw = o < p.max_ko ? __ldg(p.w_scale + o) : 0.f, bias = (p.bias && o < p.max_ko) ? __ldg(p.bias + o) : 0.f;
   const int rows = p.B * p.R;
   for (int i = warp; i < 8 * NT; i += kWarps) {
-    RowInfo ri{0, -1, 0.f, 0, 0, 0};
+    RowInfo ri{0, -1, 0.f, 0x7fffffff, 0, 0};   // a row that does not exist reads the first one's codes: its sums go nowhere
     if (i < rows) {
       const int pos = i / p.R, r = i - pos * p.R;
       const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
@@ -74,33 +88,49 @@ __global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant
   }
   __syncthreads();
   const int8_t* xr[NT];
-  int xe[NT];
+  int xe[NT], least = p.max_ki;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     xr[n] = p.x + info[8 * n + g].src * p.ldx;
-    xe[n] = info[8 * n + g].ki;
+    xe[n] = info[8 * n + g].ki < p.max_ki ? info[8 * n + g].ki : p.max_ki;
+    least = xe[n] < least ? xe[n] : least;
   }
+  least = __reduce_min_sync(0xffffffffu, least);   // columns that every row has
   int c[NT][4];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) c[n][i] = 0;
-  for (int base = warp; base < steps; base += kAhead * kWarps) {
+  for (int base = warp; base < whole; base += kAhead * kWarps) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int st = base + j * kWarps;
-      if (st < steps) {
-        const int off = 64 * st + 16 * q;
+      const int st = base + j * kWarps, off = 64 * st + 16 * q;
+      if (st < whole) {
+        uint4 b[NT];
+        if (64 * st + 64 <= least) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) b[n] = __ldg(reinterpret_cast<const uint4*>(xr[n] + off));
+        } else {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) b[n] = load16(xr[n], off, xe[n]);
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint4 b = load16(xr[n], off, xe[n]);
-          mma_s8(c[n], a0[j].x, a1[j].x, a0[j].y, a1[j].y, b.x, b.y);
-          mma_s8(c[n], a0[j].z, a1[j].z, a0[j].w, a1[j].w, b.z, b.w);
+          mma_s8(c[n], a0[j].x, a1[j].x, a0[j].y, a1[j].y, b[n].x, b[n].y);
+          mma_s8(c[n], a0[j].z, a1[j].z, a0[j].w, a1[j].w, b[n].z, b[n].w);
         }
-        const int nx = st + kAhead * kWarps;   // this slot's next step
-        a0[j] = load16(w0, 64 * nx + 16 * q, nx < steps ? end0 : 0);
-        a1[j] = load16(w1, 64 * nx + 16 * q, nx < steps ? end1 : 0);
+        fetch(j, st + kAhead * kWarps);   // this slot's next step
       }
+    }
+  }
+  if ((p.max_ki & 63) && warp == (whole & (kWarps - 1))) {   // the step that the widest path ends in
+    const int off = 64 * whole + 16 * q;
+    const uint4 a = load16(w0 - 16 * q, off, p.max_ki), a8 = load16(w1 - 16 * q, off, p.max_ki);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint4 b = load16(xr[n], off, xe[n]);
+      mma_s8(c[n], a.x, a8.x, a.y, a8.y, b.x, b.y);
+      mma_s8(c[n], a.z, a8.z, a.w, a8.w, b.z, b.w);
     }
   }
 #pragma unroll
@@ -112,14 +142,13 @@ __global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant
   }
   __syncthreads();
   for (int e = threadIdx.x; e < 16 * 8 * NT; e += kThreads) {
-    const int row = e >> 4, ch = e & 15, o = o0 + ch;
+    const int row = e >> 4, ch = e & 15;
     const RowInfo ri = info[row];
     if (ri.dst < 0 || o >= ri.ko) continue;
     int sum = 0;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) sum += part[i][row][ch];
-    float v = (float)sum * ri.sx * p.w_scale[o];
-    if (p.bias) v += p.bias[o];
+    float v = fmaf((float)sum * ri.sx, sw, bias);
     if (p.bn_scale) v = fmaf(v, p.bn_scale[(int64_t)ri.slice * p.bn_ld + o], p.bn_shift[(int64_t)ri.slice * p.bn_ld + o]);
     const int64_t at = ri.dst * p.ldy + o;
     if (p.residual) v += F32 ? static_cast<const float*>(p.residual)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at]);
