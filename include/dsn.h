@@ -178,7 +178,7 @@ typedef struct dsn_attention_desc {
  *   h = x + residual                                     (fp32; h = x without a residual)
  *   n = h / sqrt(mean_c h^2 + eps) * weight              (fp32)
  *   s = max_c |n| / 127,   q = round(n / s) to the nearest, ties to even, in -127 .. 127   (an all-zero row: s = 0, q = 0)
- * The code is computed as round(h weight * (127 / max|h weight|)) in fp32, each operation rounded once: the factor that
+ * The code is computed as round(h weight * (127 * (1 / max|h weight|))) in fp32, each operation rounded once: the factor that
  * all columns share drops out, so a code does not depend on the order of the sum of squares.
  * A row that holds a NaN or an infinity comes out as s = NaN, q = 0, y = NaN; squares that overflow fp32 do not. */
 typedef struct dsn_norm_desc {

@@ -1313,7 +1313,7 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
   p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
   p.x = x; p.residual = residual; p.sum = sum; p.q = q; p.scale = q_scale; p.y = y;
   p.ldx = d->ldx; p.ld_res = d->ld_res; p.ld_sum = d->ld_sum; p.ldq = d->ldq; p.ldy = d->ldy;
-  p.weight = d->weight; p.eps = d->eps; p.status = ctx->d_status;
+  p.weight = d->weight; p.eps = d->eps; p.minus_zero = -0.0f; p.status = ctx->d_status;
   count_launch(ctx, &dsn_stats::launches_norm);
   return dsn_launch_norm_quant(p, d->dtype == DSN_F32, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }

@@ -1,5 +1,5 @@
 // Residual addition, root-mean-square norm on elastic widths and 8-bit codes with a scale per row, in one pass:
-//   h = x + residual;  n = h / sqrt(mean h^2 + eps) * w;  s = max|n| / 127;  q = round(h w * 127 / max|h w|).
+//   h = x + residual;  n = h / sqrt(mean h^2 + eps) * w;  s = max|n| / 127;  q = round(h w * (127 * (1 / max|h w|))).
 // The factor 1 / sqrt(...) is common to a row, so it drops out of the code: the sum of squares and the maximum of |h w|
 // come out of ONE reduction, and the codes do not depend on the order of the sum.
 // Bound by memory, once the bytes in flight do not depend on the registers of the threads that work and the instructions per element are
@@ -247,10 +247,11 @@ __device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur
   if (k == 0) return true;
   elem* y = p.y ? static_cast<elem*>(p.y) + cur.out * p.ldy : nullptr;
   if (p.q) {
-    const float inv = mx > 0.f ? __fdiv_rn(127.f, mx) : mx;             // a row of zeros: 0; NaN stays
+    const float inv = mx > 0.f ? __fmul_rn(__frcp_rn(mx), 127.f) : mx;   // a row of zeros: 0; NaN stays
     const float scale = mx * rs * (1.f / 127.f);
     const uint32_t keep = mx < INFINITY ? 0xffffffffu : 0u;             // a row that is no number has the codes 0
     const uint64_t inv2 = pack2(inv, inv), scale2 = pack2(scale, scale);
+    const uint64_t none = pack2(p.minus_zero, p.minus_zero);
     const uint64_t magic = pack2(12582912.f, 12582912.f), nmagic = pack2(-12582912.f, -12582912.f);
     int8_t* q = p.q + cur.out * p.ldq;
     if (t == 0) p.scale[cur.out] = scale;
@@ -263,8 +264,10 @@ __device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur
       product(j, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        // the sum with 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves its low byte in the low byte
-        const uint64_t m = fadd2(fmul2(v[i], inv2), magic);
+        // The sum with 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves its low byte in the low byte.  The product in front
+        // of it is rounded too, as the definition says: it is a fused one with a -0 that comes from the host, because the compiler joins a
+        // packed product, or a fused one with a -0 that it can see, with the sum.
+        const uint64_t m = fadd2(ffma2(v[i], inv2, none), magic);
         b[2 * i] = (uint32_t)m;
         b[2 * i + 1] = (uint32_t)(m >> 32);
         v[i] = fmul2(fadd2(m, nmagic), scale2);

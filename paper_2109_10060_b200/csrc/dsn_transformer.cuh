@@ -123,7 +123,7 @@ struct NormParams {
   void* y;
   int64_t ldx, ld_res, ld_sum, ldq, ldy;
   const float* weight;
-  float eps;
+  float eps, minus_zero;
   int32_t* status;
 };
 cudaError_t dsn_launch_norm_quant(const NormParams& p, int f32, int sm_count, cudaStream_t s);
