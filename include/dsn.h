@@ -433,8 +433,8 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
                       void* sum, int8_t* q, float* q_scale, void* y, void* stream);
 
 /* x: device int8, 16-byte aligned, rows as d->in_order says; x_scale: device float [B * R] in the same order of rows.
- * workspace: device, 16-byte aligned, >= dsn_linear_i8_workspace_bytes (0 for most calls: it holds the rows of short samples
- * that arrive in input order, gathered). */
+ * workspace: device, 16-byte aligned, of dsn_linear_i8_workspace_bytes (0 for most calls): room for the rows of many short samples that
+ * arrive in input order, gathered.  With less, or NULL, the rows are tiled where they lie: the same results, more slowly. */
 size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B);
 int dsn_sliced_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const dsn_routing* r, const int8_t* x,
                          const float* x_scale, void* y, void* workspace, size_t ws_bytes, void* stream);

@@ -699,7 +699,7 @@ struct I8Plan {
 // one with the shortest estimate, in cycles of a pair of SMs: 2 a column and chunk of 128 (at least 300: an instruction's least time, and the
 // time of its loads), about 9 a column for the epilogue (not hidden behind a first tile), 1500 to fill and drain a wave.
 constexpr int kI8PlanPairs = 74;   // a B200's pairs of SMs: the workspace query has no context to ask
-I8Plan plan_linear_i8(const dsn_linear_i8_desc* d, int64_t B, int pairs) {
+I8Plan plan_linear_i8(const dsn_linear_i8_desc* d, int64_t B, int pairs, bool may_gather) {
   int max_ki = 1, max_ko = 1;
   for (int t = 0; t < d->T; ++t) {
     if (d->k_in[t] > max_ki) max_ki = d->k_in[t];
@@ -714,7 +714,7 @@ I8Plan plan_linear_i8(const dsn_linear_i8_desc* d, int64_t B, int pairs) {
   for (int BN = 64; BN <= 256; BN *= 2) {
     if (BN > 64 && max_ko <= BN / 2) break;
     const int64_t nt = (max_ko + BN - 1) / BN, tile = chunks * (2 * BN > 300 ? 2 * BN : 300) + 9 * BN;
-    for (int gather = 0; gather <= (input ? 1 : 0); ++gather) {
+    for (int gather = 0; gather <= (input && may_gather ? 1 : 0); ++gather) {
       const int64_t tiles = (input && !gather ? alone : flat) * nt, waves = (tiles + pairs - 1) / pairs;
       const int64_t cost = waves * tile + 1500 + (gather ? 5000 + rows * max_ki / 1500 : 0);   // a launch, and 2 bytes a byte at 5 TB/s
       if (cost < least) {
@@ -768,7 +768,7 @@ int fill_i8_maps(dsn_ctx* ctx, const LayerCall& c, const dsn_routing* r, const v
     e = encode_map(ctx, &p.mapB[m], c.Wt, 3, wd, ws, wb, CU_TENSOR_MAP_DATA_TYPE_UINT8);
     if (e) return e;
     // columns clipped at k_out rounded down to 16 bytes; the epilogue writes what lies beyond (widths below 8 never use the map)
-    const uint64_t yn = (uint64_t)(map_n[m] >= 8 ? map_n[m] / whole * whole : 8);
+    const uint64_t yn = (uint64_t)(map_n[m] >= 8 ? map_n[m] / whole * whole : whole);
     const uint64_t yd[2] = {yn, (uint64_t)r->B * g.R}, ys[1] = {(uint64_t)c.ldy * es};
     const uint32_t yb[2] = {(uint32_t)(128 / es), 32};
     e = encode_map(ctx, &p.mapY[m], y, 2, yd, ys, yb,
@@ -804,13 +804,13 @@ int run_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const LayerCall& c,
   }
   const int pairs = resident_pairs(ctx, 256);
   if (pairs <= 0) return DSN_ERR_UNSUPPORTED;   // this layer has no one-CTA form: DSN_GEMM_MODE leaves it alone
-  const I8Plan plan = plan_linear_i8(d, r->B, kI8PlanPairs);
+  const int64_t ld_gathered = (int64_t)align_up((size_t)d->C_in, 16);
+  const I8Plan plan = plan_linear_i8(d, r->B, kI8PlanPairs, workspace && ws_bytes >= (size_t)(rows * ld_gathered));
   LayerCall cc = c;
   int64_t ldx = d->ldx;
   const void* src = x;
   if (plan.gather) {
-    ldx = (int64_t)align_up((size_t)d->C_in, 16);
-    if (!workspace || ws_bytes < (size_t)(rows * ldx)) return DSN_ERR_WORKSPACE;
+    ldx = ld_gathered;
     count_launch(ctx, &dsn_stats::launches_copy);
     if (dsn_launch_gather_i8(q, static_cast<int8_t*>(workspace), ldx, s) != cudaSuccess) return DSN_ERR_CUDA;
     src = workspace;
@@ -1319,7 +1319,7 @@ int dsn_rmsnorm_quant(dsn_ctx* ctx, const dsn_norm_desc* d, const dsn_routing* r
 }
 
 size_t dsn_linear_i8_workspace_bytes(const dsn_linear_i8_desc* d, int32_t B) {
-  if (check_linear_i8(d) || B < 0 || (int64_t)B * d->R <= DSN_ROWS_I8_MAX || !plan_linear_i8(d, B, kI8PlanPairs).gather) return 0;
+  if (check_linear_i8(d) || B < 0 || (int64_t)B * d->R <= DSN_ROWS_I8_MAX || !plan_linear_i8(d, B, kI8PlanPairs, true).gather) return 0;
   return (size_t)B * d->R * align_up((size_t)d->C_in, 16);
 }
 

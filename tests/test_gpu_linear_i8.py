@@ -161,6 +161,43 @@ def test_linear_i8_many_groups(dsn, ctx):
     check(got[keep], sub, ki, ko, "f32", 0)
 
 
+def test_linear_i8_workspace_changes_nothing_but_the_time(dsn, ctx):
+    c = make(21, 1200, 3, 100, 70, 2)
+    seen = []
+
+    def without(ctx_, d, r, x, sx, y, ws):
+        seen.append(ws.numel())
+        dsn.dsn_sliced_linear_i8(ctx_, d, r, x, sx, y, None)
+        a = y.clone()
+        y.fill_(MARK)
+        dsn.dsn_sliced_linear_i8(ctx_, d, r, x, sx, y, ws[:-16])        # too small: as if there were none
+        assert torch.equal(a, y)
+
+    a = run(dsn, ctx, c, [60, 100], [70, 41])
+    np.testing.assert_array_equal(run(dsn, ctx, c, [60, 100], [70, 41], call=without), a)
+    assert seen == [1200 * 3 * 112]
+
+
+def test_linear_i8_narrow_rows_on_the_tensor_cores(dsn, ctx):
+    """Outputs of a few columns, pitches of 16 bytes, a single input column."""
+    for C, N in ((1, 1), (5, 3), (16, 4), (130, 7), (33, 9)):
+        for y, ld in (("bf16", -(-N // 8) * 8), ("f32", -(-N // 4) * 4)):
+            B = 50
+            c = make(C + N, B, 1, C, N, 1)
+            dt = torch.bfloat16 if y == "bf16" else torch.float32
+            r, _ = groups(dsn, [0] * B, 1)
+            f = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(DEV)
+            ldx = -(-C // 16) * 16
+            d = dsn.make_linear_i8_desc(1, C, N, [C], [N], rows_with_pitch(c["W"][None], ldx, torch.int8, 103)[0], f(c["sw"]), bias=f(c["bias"]),
+                                        y_dtype=dsn.BF16 if y == "bf16" else dsn.F32, ldx=ldx, ldw=ldx, ldy=ld, in_order=1, out_order=1)
+            yd = torch.full((B, 1, ld), MARK, dtype=dt, device=DEV)
+            dsn.dsn_sliced_linear_i8(ctx, d, r, rows_with_pitch(c["x"], ldx, torch.int8, 101), f(c["sx"]), yd)
+            check_status(ctx, dsn)
+            got = values(yd)
+            assert np.all(got[..., N:] == MARK)
+            check(got[..., :N], c, [C], [N], y, 0)
+
+
 def test_linear_i8_nan_scales_stay_visible(dsn, ctx):
     for B in (3, 50):
         c = make(5, B, 2, 64, 48, 1)
@@ -212,11 +249,7 @@ def test_linear_i8_refusals(dsn, ctx):
     call(bad, w_scale=sw[:40]), call(bad, W=W[:40].clone()), call(bad, bias=sw[:40]), call(bad, bn_scale=torch.zeros(96, device=DEV))
     call(bad, residual=y), call(bad, R=2), call(bad, ldx=16)
     call(align, C_out=47, ko=(47, 8)), call(align, C_in=31, ki=(16, 31)), call(align, xx=torch.zeros(96, dtype=torch.int8, device=DEV)[1:])
-    r2, _ = groups(dsn, [0, 1] * 2000, 2)
-    n = 4000 * 32
-    big = dict(xx=torch.zeros(4000, 32, dtype=torch.int8, device=DEV), ss=torch.zeros(4000, device=DEV), yy=torch.zeros(4000, 48, dtype=torch.bfloat16, device=DEV), rr=r2)
-    call(dsn.ERR_WORKSPACE, **big), call(dsn.ERR_WORKSPACE, ws=torch.empty(n - 1, dtype=torch.uint8, device=DEV), **big)
-    call(align, ws=torch.empty(n + 16, dtype=torch.uint8, device=DEV)[1:], **big)
+    call(align, ws=torch.empty(48, dtype=torch.uint8, device=DEV)[1:]), call(bad, ws=torch.empty(48, dtype=torch.uint8))
     torch.cuda.synchronize()
     assert bool((y == MARK).all())
     r0, _ = groups(dsn, [], 2)
