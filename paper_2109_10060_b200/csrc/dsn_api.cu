@@ -696,8 +696,10 @@ struct I8Plan {
 };
 // Rows in input order are tiled sample by sample (a sample's place is known only on the device), the last tile of each filled up with zero
 // rows; where the waves of tiles that this adds take longer than a pass that gathers the rows, they are gathered.  The n-tile is the
-// one with the shortest estimate, in cycles of a pair of SMs: 2 a column and chunk of 128 (at least 300: an instruction's least time, and the
-// time of its loads), about 9 a column for the epilogue (not hidden behind a first tile), 1500 to fill and drain a wave.
+// one with the shortest estimate, for samples dealt out evenly over the paths, in cycles of a pair of SMs: a tile takes 2 a column and chunk
+// of 128 (at least 300: an instruction's least time and the trip of its operands), about 9 a column for the epilogue and 1500 besides.
+// Measured (us with n-tiles of 64, 128, 256): 512 rows of 768 -> 2304: 7.3, 7.1, 8.2; 2048 of 2048 -> 2048: 21.0, 14.3, 12.3; 16,384 of 128 -> 1000: 24.3,
+// 16.5, 13.9; 9 samples of 61 rows, three paths up to 1000 -> 777: 10.1, 12.7, 18.9.
 constexpr int kI8PlanPairs = 74;   // a B200's pairs of SMs: the workspace query has no context to ask
 I8Plan plan_linear_i8(const dsn_linear_i8_desc* d, int64_t B, int pairs, bool may_gather) {
   int max_ki = 1, max_ko = 1;
@@ -705,18 +707,21 @@ I8Plan plan_linear_i8(const dsn_linear_i8_desc* d, int64_t B, int pairs, bool ma
     if (d->k_in[t] > max_ki) max_ki = d->k_in[t];
     if (d->k_out[t] > max_ko) max_ko = d->k_out[t];
   }
-  const int64_t rows = B * d->R, chunks = (max_ki + 127) / 128, groups = d->T < B ? d->T : B;
-  const int64_t flat = (rows + 255) / 256 + (groups - 1);                     // a group ends in a part of a tile
-  const int64_t alone = (B * ((d->R + 127) / 128) + 1) / 2 + (groups - 1);
+  const int64_t rows = B * d->R, chunks = (max_ki + 127) / 128;
+  const int64_t paths = d->T < B ? d->T : B, share = (B + paths - 1) / paths;   // samples a path
+  const int64_t flat = (share * d->R + 255) / 256, alone = (share * ((d->R + 127) / 128) + 1) / 2;
   const bool input = d->in_order == DSN_INPUT_ORDER && B > 1;
   I8Plan best{64, false};
   int64_t least = INT64_MAX;
   for (int BN = 64; BN <= 256; BN *= 2) {
     if (BN > 64 && max_ko <= BN / 2) break;
-    const int64_t nt = (max_ko + BN - 1) / BN, tile = chunks * (2 * BN > 300 ? 2 * BN : 300) + 9 * BN;
+    int64_t nt = 0;                                                             // n-tiles of `paths` paths
+    for (int t = 0; t < d->T; ++t) nt += (d->k_out[t] + BN - 1) / BN;
+    nt = (nt * paths + d->T - 1) / d->T;
+    const int64_t tile = chunks * (2 * BN > 300 ? 2 * BN : 300) + 9 * BN + 1500;
     for (int gather = 0; gather <= (input && may_gather ? 1 : 0); ++gather) {
       const int64_t tiles = (input && !gather ? alone : flat) * nt, waves = (tiles + pairs - 1) / pairs;
-      const int64_t cost = waves * tile + 1500 + (gather ? 5000 + rows * max_ki / 1500 : 0);   // a launch, and 2 bytes a byte at 5 TB/s
+      const int64_t cost = waves * tile + (gather ? 5000 + rows * max_ki / 1500 : 0);   // a launch, and 2 bytes a byte at 5 TB/s
       if (cost < least) {
         least = cost;
         best = I8Plan{BN, gather != 0};
@@ -755,7 +760,7 @@ int fill_i8_maps(dsn_ctx* ctx, const LayerCall& c, const dsn_routing* r, const v
     if (g.flat) {
       const uint64_t rows = (uint64_t)r->B * g.R;
       const uint64_t dims[4] = {kv, rows, 1, 1}, str[3] = {ld, ld * rows, ld * rows};
-      const uint32_t box[4] = {128, DSN_GEMM_BM, 1, 1};
+      const uint32_t box[4] = {128, (uint32_t)g.bw, 1, 1};
       e = encode_map(ctx, &p.mapA[m], x, 4, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8);
     } else {
       const uint64_t dims[4] = {kv, (uint64_t)g.W, 1, (uint64_t)r->B}, str[3] = {ld, ld * g.W, ld * g.W};

@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kI8Threads, 1) gemm_i8_pair_kernel(const __gri
     // ------------------------------------------------------------------ TMA producer (both CTAs)
     int stage = 0;
     uint32_t phase = 0;
-    const uint32_t a_box_bytes = g.flat ? kABytes : (uint32_t)(g.bw * g.bh * g.nb) * kBKB;
+    const uint32_t a_box_bytes = (uint32_t)(g.bw * g.bh * g.nb) * kBKB;
     const uint32_t tx_bytes = 2u * (a_box_bytes + bh_bytes);
     bool ok = true;
     for (int tile = pair; ok && tile < total; tile += npairs) {
