@@ -388,16 +388,14 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
     if (asked % UB == 0) {   // the next units' rows, one a lane
       ahead = RowAt{0, 0, 0, 0};
       const uint64_t wide = ((uint64_t)(asked + lane / RB) * ngroups + gid) * RB + lane % RB;
-      if (wide < rows) {
-        const uint32_t row = (uint32_t)wide;
-        const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
-        const PosInfo at = dsn_locate(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
-        if (at.slice >= 0) {
-          ahead.k = p.k[at.slice];
-          ahead.in = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
-          ahead.out = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
-          ahead.part = ahead.in + 1 == (int64_t)rows;   // behind the last row's columns nothing need be allocated
-        }
+      const uint32_t row = wide < rows ? (uint32_t)wide : rows;   // rows / R = B: no position
+      const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
+      const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
+      if (at.slice >= 0) {
+        ahead.k = p.k[at.slice];
+        ahead.in = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
+        ahead.out = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
+        ahead.part = ahead.in + 1 == (int64_t)rows;   // behind the last row's columns nothing need be allocated
       }
       __syncwarp();
     }

@@ -240,18 +240,16 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
     if (asked % 32 == 0) {
       ahead = TokenAt{0, {0, 0, 0}, 0};
       const uint64_t wide = (uint64_t)(asked + lane) * ngroups + gid;
-      if (wide < rows) {
-        const uint32_t row = (uint32_t)wide;
-        const int pos = (int)dsn_div(row, p.by_N), r = (int)(row - (uint32_t)pos * (uint32_t)p.N);
-        const PosInfo at = dsn_locate(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
-        if (at.slice >= 0) {
-          ahead.heads = p.heads[at.slice];
-          ahead.row = (int64_t)(p.grouped ? pos : at.sample) * p.N + r;
-          const int32_t* at_pos = p.positions + (p.shared ? (int64_t)r : ahead.row);
-          ahead.pos[0] = at_pos[0];
-          if (p.n_axes > 1) ahead.pos[1] = at_pos[p.n_pos];
-          if (p.n_axes > 2) ahead.pos[2] = at_pos[2 * (int64_t)p.n_pos];
-        }
+      const uint32_t row = wide < rows ? (uint32_t)wide : rows;   // rows / N = B: no position
+      const int pos = (int)dsn_div(row, p.by_N), r = (int)(row - (uint32_t)pos * (uint32_t)p.N);
+      const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
+      if (at.slice >= 0) {
+        ahead.heads = p.heads[at.slice];
+        ahead.row = (int64_t)(p.grouped ? pos : at.sample) * p.N + r;
+        const int32_t* at_pos = p.positions + (p.shared ? (int64_t)r : ahead.row);
+        ahead.pos[0] = at_pos[0];
+        if (p.n_axes > 1) ahead.pos[1] = at_pos[p.n_pos];
+        if (p.n_axes > 2) ahead.pos[2] = at_pos[2 * (int64_t)p.n_pos];
       }
       __syncwarp();
     }

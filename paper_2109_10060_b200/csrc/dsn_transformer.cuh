@@ -71,6 +71,23 @@ __device__ __forceinline__ PosInfo dsn_locate(int p, int G, int T, const int32_t
   return i;
 }
 
+// Every lane a position of its own (p < B, or not below 0 and past the end of all groups); all lanes of the warp call this.  One trip to memory for
+// up to 32 groups, whose ends go round the warp, instead of one a step of a search.
+__device__ __forceinline__ PosInfo dsn_locate_lanes(int p, int B, int G, int T, const int32_t* __restrict__ offsets, const int32_t* __restrict__ perm,
+                                                    const int32_t* __restrict__ group_slice) {
+  if (G > 32) return p < B ? dsn_locate(p, G, T, offsets, perm, group_slice) : PosInfo{0, -1};
+  const int lane = threadIdx.x & 31;
+  const int end = lane < G ? offsets[lane + 1] : 0x7fffffff;
+  const int slice = lane < G ? (group_slice ? group_slice[lane] : lane) : -1;
+  PosInfo i;
+  i.sample = p < B ? perm[p] : -1;
+  int g = 0;
+  for (int j = 0; j < G; ++j) g += __shfl_sync(0xffffffffu, end, j) <= p;
+  i.slice = __shfl_sync(0xffffffffu, slice, g & 31);
+  if (g >= G || i.sample < 0 || i.slice >= T) i.slice = -1;
+  return i;
+}
+
 // Untiled bulk copies between global and shared memory: both ends on 16 bytes, whole 16 bytes.
 __device__ __forceinline__ void dsn_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
