@@ -463,14 +463,26 @@ def make_norm_desc(dtype, R, Cn, k, weight=None, eps=1e-6, ldx=None, ld_res=None
     return d
 
 
+# The calls below look at each tensor in place and hand it to _buf only where something is off (or it is a view of rows): a Python call
+# a tensor is a fifth of the host's time for a small one.
+
 def dsn_rmsnorm_quant(ctx: Context, d: NormDesc, routing: Routing, x, q=None, scale=None, y=None, residual=None, sum_out=None, stream=None):
-    ty, rows, dev = _types(), routing.B * d.R, ctx.device
+    ty, rows, dev, Cn = _Types if _Types.of_code else _types(), routing.B * d.R, ctx.device, d.C
     dt = ty.of_code.get(d.dtype)
-    _check(ctx.lib.dsn_rmsnorm_quant(ctx.handle, d, routing, _buf("x", x, dt, _span(rows, d.ldx, d.C), dev, True),
-                                     _buf("residual", residual, dt, _span(rows, d.ld_res, d.C), dev, True),
-                                     _buf("sum_out", sum_out, dt, _span(rows, d.ld_sum, d.C), dev, True),
-                                     _buf("q", q, ty.i8, _span(rows, d.ldq, d.C), dev, True), _buf("scale", scale, ty.f32, rows, dev),
-                                     _buf("y", y, dt, _span(rows, d.ldy, d.C), dev, True), _stream_handle(stream)), "dsn_rmsnorm_quant")
+    n = rows * max(d.ldx, d.ldy, d.ld_res, d.ld_sum, d.ldq)   # a tensor of so many elements holds any of the spans
+    _check(ctx.lib.dsn_rmsnorm_quant(
+        ctx.handle, d, routing,
+        x.data_ptr() if x is not None and x.dtype is dt and x.get_device() == dev and x.numel() >= n else _buf("x", x, dt, _span(rows, d.ldx, Cn), dev, True),
+        None if residual is None else residual.data_ptr() if residual.dtype is dt and residual.get_device() == dev and residual.numel() >= n
+        else _buf("residual", residual, dt, _span(rows, d.ld_res, Cn), dev, True),
+        None if sum_out is None else sum_out.data_ptr() if sum_out.dtype is dt and sum_out.get_device() == dev and sum_out.numel() >= n
+        else _buf("sum_out", sum_out, dt, _span(rows, d.ld_sum, Cn), dev, True),
+        None if q is None else q.data_ptr() if q.dtype is ty.i8 and q.get_device() == dev and q.numel() >= n
+        else _buf("q", q, ty.i8, _span(rows, d.ldq, Cn), dev, True),
+        None if scale is None else _buf("scale", scale, ty.f32, rows, dev),
+        None if y is None else y.data_ptr() if y.dtype is dt and y.get_device() == dev and y.numel() >= n
+        else _buf("y", y, dt, _span(rows, d.ldy, Cn), dev, True),
+        _stream_handle(stream)), "dsn_rmsnorm_quant")
 
 
 def make_linear_i8_desc(R, C_in, C_out, k_in, k_out, W, w_scale, bias=None, bn_scale=None, bn_shift=None, residual=None, y_dtype=BF16,
@@ -495,16 +507,23 @@ def dsn_linear_i8_workspace_bytes(d: LinearI8Desc, B: int) -> int:
 
 
 def dsn_sliced_linear_i8(ctx: Context, d: LinearI8Desc, routing: Routing, x, x_scale, y, workspace=None, stream=None):
-    ty, rows, dev = _types(), routing.B * d.R, ctx.device
-    dt = ty.of_code.get(d.y_dtype)
-    span = _span(rows, d.ldy, d.C_out)
-    _buf("residual", d._keep[-1], dt, span, dev, True)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    if workspace is not None and workspace.get_device() != dev:
-        raise DsnError(ERR_INVALID_ARG, f"workspace on {workspace.device}, expected cuda:{dev}")
-    _check(ctx.lib.dsn_sliced_linear_i8(ctx.handle, d, routing, _buf("x", x, ty.i8, _span(rows, d.ldx, d.C_in), dev, True),
-                                        _buf("x_scale", x_scale, ty.f32, rows, dev), _buf("y", y, dt, span, dev, True), _ptr(workspace),
-                                        ws_bytes, _stream_handle(stream)), "dsn_sliced_linear_i8")
+    ty, rows, dev = _Types if _Types.of_code else _types(), routing.B * d.R, ctx.device
+    dt, residual, ws_bytes = ty.of_code.get(d.y_dtype), d._keep[-1], 0
+    n = rows * d.ldy
+    if residual is not None and not (residual.dtype is dt and residual.get_device() == dev and residual.numel() >= n):
+        _buf("residual", residual, dt, _span(rows, d.ldy, d.C_out), dev, True)
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+        if workspace.get_device() != dev:
+            raise DsnError(ERR_INVALID_ARG, f"workspace on {workspace.device}, expected cuda:{dev}")
+    _check(ctx.lib.dsn_sliced_linear_i8(
+        ctx.handle, d, routing,
+        x.data_ptr() if x is not None and x.dtype is ty.i8 and x.get_device() == dev and x.numel() >= rows * d.ldx
+        else _buf("x", x, ty.i8, _span(rows, d.ldx, d.C_in), dev, True),
+        _buf("x_scale", x_scale, ty.f32, rows, dev),
+        y.data_ptr() if y is not None and y.dtype is dt and y.get_device() == dev and y.numel() >= n
+        else _buf("y", y, dt, _span(rows, d.ldy, d.C_out), dev, True),
+        _ptr(workspace), ws_bytes, _stream_handle(stream)), "dsn_sliced_linear_i8")
 
 
 def make_rotary_desc(dtype, N, H, D, heads, pairs, vectors=3, rotated=2, base=10000.0, ladder=ROTARY_SHARED, pairing=ROTARY_HALVES,
