@@ -216,7 +216,9 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t s_full[GROUPS][kRingDepth];
   __shared__ TokenAt s_at[GROUPS][kRingDepth];
-  __shared__ __align__(16) float s_cos[GROUPS][128], s_sin[GROUPS][128];
+  // the factors of a token as the places take them: halves cos and sin, neighbours (cos, cos) and (-sin, sin) of every pair
+  constexpr int NS = INTER ? 256 : 128;
+  __shared__ __align__(16) float s_cos[GROUPS][NS], s_sin[GROUPS][NS];
   __shared__ uint32_t s_abort;
   const int g = threadIdx.x / TPT, t = threadIdx.x % TPT, lane = threadIdx.x & 31;
   const bool fetches = t < 32;   // the group's first warp asks for rows and sends them off
@@ -269,6 +271,16 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
   const int per = INTER ? 2 * P / W : P / W;        // places of a vector that this kernel's threads take
   const int dv = TPT / per, di = TPT - dv * per;    // from one of a thread's places to its next
   const int v0 = t / per, i0 = t - v0 * per;
+  // the pairs whose angle this thread computes
+  constexpr int NF = TPT < 128 ? 128 / TPT : 1;
+  uint64_t freq[NF];
+  int axis[NF];
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    const int i = t + j * TPT;
+    freq[j] = i < P ? p.freq[i] : 0;
+    axis[j] = i < P ? p.axis[i] : 0;
+  }
   int slot = 0;
   uint32_t phase = 0;
   for (int n = 0; n < mine; ++n) {
@@ -278,22 +290,37 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
     const TokenAt cur = s_at[g][slot];
     uint8_t* row = slots + (size_t)slot * slot_bytes;
     if (cur.heads > 0) {
-      for (int i = t; i < P; i += TPT) {
-        const int ax = p.axis[i];
-        const int at = ax == 0 ? cur.pos[0] : (ax == 1 ? cur.pos[1] : cur.pos[2]);
-        const uint64_t a = (uint64_t)(int64_t)at * p.freq[i];
-        float c, s;
-        sincospif((float)(int32_t)(a >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: -1 .. 1 half turns
-        s_cos[g][i] = c;
-        s_sin[g][i] = p.inverse ? -s : s;
+#pragma unroll
+      for (int j = 0; j < NF; ++j) {
+        const int i = t + j * TPT;
+        if (i < P) {
+          const int at = axis[j] == 0 ? cur.pos[0] : (axis[j] == 1 ? cur.pos[1] : cur.pos[2]);
+          const uint64_t a = (uint64_t)(int64_t)at * freq[j];
+          float c, s;
+          sincospif((float)(int32_t)(a >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: -1 .. 1 half turns
+          s = p.inverse ? -s : s;
+          if constexpr (INTER) {
+            *reinterpret_cast<float2*>(&s_cos[g][2 * i]) = make_float2(c, c);
+            *reinterpret_cast<float2*>(&s_sin[g][2 * i]) = make_float2(-s, s);
+          } else {
+            s_cos[g][i] = c;
+            s_sin[g][i] = s;
+          }
+        }
       }
       if (TPT > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(TPT) : "memory"); else __syncwarp();
       const int turned = cur.heads * p.rotated;
-      int v = v0, pc = i0;
-#pragma unroll 2
-      while (v < turned) {
-        const int i = pc * W;
-        uint8_t* at = row + (size_t)(vec_at(p, v) + i) * ES;
+      auto factors = [&](int i, uint64_t (&c)[NP], uint64_t (&s)[NP]) {   // of the place that begins at element i
+#pragma unroll
+        for (int e = 0; e < NP; e += 2) {
+          const ulonglong2 cc = *reinterpret_cast<const ulonglong2*>(&s_cos[g][i + 2 * e]), ss = *reinterpret_cast<const ulonglong2*>(&s_sin[g][i + 2 * e]);
+          c[e] = cc.x;
+          c[e + 1] = cc.y;
+          s[e] = ss.x;
+          s[e + 1] = ss.y;
+        }
+      };
+      auto turn_place = [&](uint8_t* at, const uint64_t (&c)[NP], const uint64_t (&s)[NP]) {
         uint64_t a[NP];
         E::widen(*reinterpret_cast<const uint4*>(at), a);
         if constexpr (!INTER) {
@@ -301,23 +328,32 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
           E::widen(*reinterpret_cast<const uint4*>(at + P * ES), b);
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
-            const uint64_t c = *reinterpret_cast<const uint64_t*>(&s_cos[g][i + 2 * e]), s = *reinterpret_cast<const uint64_t*>(&s_sin[g][i + 2 * e]);
-            na[e] = ffma2(neg2(b[e]), s, fmul2(a[e], c));
-            nb[e] = ffma2(b[e], c, fmul2(a[e], s));
+            na[e] = ffma2(neg2(b[e]), s[e], fmul2(a[e], c[e]));
+            nb[e] = ffma2(b[e], c[e], fmul2(a[e], s[e]));
           }
           *reinterpret_cast<uint4*>(at) = E::narrow(na);
           *reinterpret_cast<uint4*>(at + P * ES) = E::narrow(nb);
         } else {
 #pragma unroll
-          for (int e = 0; e < NP; ++e) {
-            const float c = s_cos[g][i / 2 + e], s = s_sin[g][i / 2 + e];
-            a[e] = ffma2(swap2(a[e]), pack2(-s, s), fmul2(a[e], pack2(c, c)));
-          }
+          for (int e = 0; e < NP; ++e) a[e] = ffma2(swap2(a[e]), s[e], fmul2(a[e], c[e]));
           *reinterpret_cast<uint4*>(at) = E::narrow(a);
         }
-        v += dv;
-        pc += di;
-        if (pc >= per) { pc -= per; ++v; }
+      };
+      uint64_t c[NP], s[NP];
+      if (di == 0) {   // this thread's place is the same in all of its vectors
+        factors(i0 * W, c, s);
+#pragma unroll 4
+        for (int v = v0; v < turned; v += dv) turn_place(row + (size_t)(vec_at(p, v) + i0 * W) * ES, c, s);
+      } else {
+        int v = v0, pc = i0;
+#pragma unroll 2
+        while (v < turned) {
+          factors(pc * W, c, s);
+          turn_place(row + (size_t)(vec_at(p, v) + pc * W) * ES, c, s);
+          v += dv;
+          pc += di;
+          if (pc >= per) { pc -= per; ++v; }
+        }
       }
       dsn_gemm::fence_async_smem();   // the turned elements are visible to the copy that takes them out
     }
@@ -341,7 +377,7 @@ cudaError_t launch_ring(const RotaryParams& p, uint32_t row_bytes, int per_sm, i
   static size_t configured[DSN_MAX_DEVICES] = {};
   auto kernel = rotary_ring_kernel<F32, INTER, TPT>;
   constexpr int GROUPS = kRingThreads / TPT;
-  int depth = (int)((per_sm == 2 ? 96 : 192) * 1024 / (GROUPS * row_bytes));
+  int depth = (int)((per_sm == 2 ? 92 : 184) * 1024 / (GROUPS * row_bytes));
   if (depth < 2) return cudaErrorInvalidConfiguration;
   if (depth > kRingDepth) depth = kRingDepth;
   const size_t smem = (size_t)depth * GROUPS * row_bytes;
@@ -365,12 +401,12 @@ cudaError_t launch(const RotaryParams& p, int sm_count, cudaStream_t s) {
 template <bool F32, bool VEC, bool INTER>
 cudaError_t pick(const RotaryParams& p, int sm_count, cudaStream_t s) {
   const int64_t bytes = (int64_t)p.max_heads * p.vectors * p.D * (F32 ? 4 : 2);
-  if (VEC && (int64_t)p.B * p.N >= 8 * sm_count && bytes <= 96 * 1024) {
+  if (VEC && (int64_t)p.B * p.N >= 8 * sm_count && bytes <= 92 * 1024) {
     // the fewest threads a row with which two slots a group fit
-    if (bytes <= 6 * 1024) return launch_ring<F32, INTER, 32>(p, (uint32_t)bytes, 2, sm_count, s);
-    if (bytes <= 12 * 1024) return launch_ring<F32, INTER, 64>(p, (uint32_t)bytes, 2, sm_count, s);
-    if (bytes <= 24 * 1024) return launch_ring<F32, INTER, 128>(p, (uint32_t)bytes, 2, sm_count, s);
-    return launch_ring<F32, INTER, 256>(p, (uint32_t)bytes, bytes <= 48 * 1024 ? 2 : 1, sm_count, s);
+    if (bytes <= 5888) return launch_ring<F32, INTER, 32>(p, (uint32_t)bytes, 2, sm_count, s);
+    if (bytes <= 11776) return launch_ring<F32, INTER, 64>(p, (uint32_t)bytes, 2, sm_count, s);
+    if (bytes <= 23552) return launch_ring<F32, INTER, 128>(p, (uint32_t)bytes, 2, sm_count, s);
+    return launch_ring<F32, INTER, 256>(p, (uint32_t)bytes, bytes <= 47104 ? 2 : 1, sm_count, s);
   }
   // a warp a token where there are tokens enough to fill the GPU, else 256 threads
   return (int64_t)p.B * p.N >= 16 * sm_count ? launch<F32, VEC, INTER, 32>(p, sm_count, s) : launch<F32, VEC, INTER, 256>(p, sm_count, s);
