@@ -385,6 +385,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
   RowAt ahead{0, 0, 0, 0};   // this lane's row of the units being asked for
   int asked = 0;             // units asked for
   auto ask = [&](int slot) {
+    __syncwarp();            // the slot's former row has been taken by all lanes
     if (asked % UB == 0) {   // the next units' rows, one a lane
       ahead = RowAt{0, 0, 0, 0};
       const uint64_t wide = ((uint64_t)(asked + lane / RB) * ngroups + gid) * RB + lane % RB;
@@ -426,7 +427,8 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
   load_weights<TPR, VPT>(p, t, w);
   int turn = 0, slot = 0;
   uint32_t phase = 0;
-  for (int n = 0; n < mine; ++n) {
+  int n = 0;
+  for (; n < mine; ++n) {
     const bool ok = dsn_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 71);
     const RowAt cur = s_at[g][slot][sub];
     const int k = cur.k;
@@ -466,6 +468,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
     if (fetches && asked < mine) ask(slot);
     if (++slot == depth) { slot = 0; phase ^= 1u; }
   }
+  if (fetches && n < mine) dsn_drain(dsn_gemm::smem_u32(&s_full[g][0]), depth, n, asked);
 }
 
 template <bool F32, bool RES, int TPR, int VPT>

@@ -14,6 +14,13 @@ __device__ __forceinline__ bool dsn_wait(uint32_t bar, uint32_t parity, volatile
   return dsn_gemm::mbar_wait_slow(bar, parity, abort_flag, status, where);
 }
 
+// After a wait that ran out: the copies that a group asked for, units first .. asked - 1 of its ring of `depth` barriers, get a last bounded
+// chance to land before the group's shared memory goes to another CTA.
+__device__ __forceinline__ void dsn_drain(uint32_t bars, int depth, int first, int asked) {
+  for (int i = first; i < asked; ++i)
+    for (int j = 0; j < (1 << 14) && !dsn_gemm::mbar_try_wait(bars + 8u * (uint32_t)(i % depth), (uint32_t)(i / depth) & 1u); ++j) {}
+}
+
 // Quotient of n < 2^31 by a divisor fixed on the host: (umulhi(n, mul) + n) >> shift.
 struct FastDiv {
   uint32_t mul, shift, d;
