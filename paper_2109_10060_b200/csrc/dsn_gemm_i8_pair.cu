@@ -312,27 +312,27 @@ __global__ void __launch_bounds__(kI8Threads, 1) gemm_i8_pair_kernel(const __gri
     tmem_relinquish_pair();
   }
 
-  auto ntiles_of = [&](int grp) {
-    const int sl = p.group_slice ? p.group_slice[grp] : grp;
-    if (sl < 0 || sl >= p.T || p.map_id[sl] == 0xFF) return 0;
-    const int cnt = p.offsets[grp + 1] - p.offsets[grp];
-    if (cnt <= 0) return 0;
-    const int mt = g.flat ? (cnt * g.R + BM - 1) / BM : ((cnt + g.nb - 1) / g.nb) * g.tiles_x * g.tiles_y;
-    return ((mt + 1) / 2) * ((p.k_out[sl] + g.BN - 1) / g.BN);
-  };
+  // The CTAs of the pair meet in two halves: what they announce (initialised barriers) is taken up only after the tile table, which hides
+  // the 700 cycles of the meeting.
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   // barriers and TMEM are set up; everything below reads what earlier kernels wrote
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
-  // s_prefix[0..G]: tile prefix; [G+1 .. 2G+1]: group offsets; [2G+2 .. 3G+1]: slice of each group
-  for (int j = threadIdx.x; j <= p.G; j += blockDim.x) s_prefix[p.G + 1 + j] = p.offsets[j];
-  for (int j = threadIdx.x; j < p.G; j += blockDim.x) {
-    const int sl = p.group_slice ? p.group_slice[j] : j;
-    s_prefix[2 * p.G + 2 + j] = (sl >= 0 && sl < p.T) ? sl : 0;
-  }
-  dsn_build_tile_prefix(p.G, s_prefix, ntiles_of);
+  // s_prefix[0..G]: tile prefix; [G+1 .. 2G+1]: group offsets; [2G+2 .. 3G+1]: slice of each group (one trip to memory for all three)
+  dsn_build_tile_prefix(p.G, s_prefix, [&](int grp) {
+    const int sl = p.group_slice ? p.group_slice[grp] : grp;
+    const int lo = p.offsets[grp], hi = p.offsets[grp + 1];
+    const bool known = sl >= 0 && sl < p.T;
+    s_prefix[p.G + 1 + grp] = lo;
+    if (grp == p.G - 1) s_prefix[2 * p.G + 1] = hi;
+    s_prefix[2 * p.G + 2 + grp] = known ? sl : 0;
+    if (!known || p.map_id[sl] == 0xFF || hi <= lo) return 0;
+    const int mt = g.flat ? ((hi - lo) * g.R + BM - 1) / BM : ((hi - lo + g.nb - 1) / g.nb) * g.tiles_x * g.tiles_y;
+    return ((mt + 1) / 2) * ((p.k_out[sl] + g.BN - 1) / g.BN);
+  });
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();  // the peer's barriers are initialised before anything can arrive on them
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // the peer's barriers are initialised before anything can arrive on them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int total = s_prefix[p.G];
