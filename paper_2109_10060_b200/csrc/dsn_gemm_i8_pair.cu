@@ -27,6 +27,17 @@ constexpr int kBKB = 128;                          // bytes (= columns) of a chu
 constexpr int kPieces = 4;                         // pieces of 32 columns that an epilogue warp takes of a tile, at most
 constexpr int kI8Threads = kThreads + 32;          // one more warp: the tiles' preparation
 
+__device__ __forceinline__ uint32_t mbar_test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok;
+}
 __device__ __forceinline__ float relu_nan(float v) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(0.f));
@@ -389,22 +400,38 @@ __global__ void __launch_bounds__(kI8Threads, 1) gemm_i8_pair_kernel(const __gri
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * g.BN);
         const int tail_ks = ((t.ki & (kBKB - 1)) + 31) >> 5;  // K steps of a partial last chunk (0: none)
         uint32_t accumulate = 0;
-        for (int kc = (t.ki + kBKB - 1) / kBKB; kc > 0; --kc) {
-          ok = __all_sync(0xffffffffu, dsn_wait(bar_full + 8 * stage, phase, abort_flag, p.status, 63));
-          if (!ok) break;
-          tc_fence_after();
-          const int nks = (kc == 1 && tail_ks != 0) ? tail_ks : kBKB / 32;
-          if (elect_one()) {
-            umma_i8_pair(d_tmem, da, db, idesc, accumulate);  // +32 bytes per K step
-            if (nks > 1) umma_i8_pair(d_tmem, da + 2u, db + 2u, idesc, 1u);
-            if (nks > 2) umma_i8_pair(d_tmem, da + 4u, db + 4u, idesc, 1u);
-            if (nks > 3) umma_i8_pair(d_tmem, da + 6u, db + 6u, idesc, 1u);
-            umma_commit_pair(bar_empty + 8 * stage);
+        const int whole = t.ki >> 7;                          // chunks of 128 columns
+        // The next stage's barrier is looked at before this stage's products are issued (64 rows of 4096 -> 4096, where 32 chunks are issued one
+        // after the other: 12.7 -> 11.7 us).  A look, not a wait: try_wait would hold the warp for microseconds at a barrier of no tile.
+        uint32_t here = mbar_test_wait(bar_full + 8 * stage, phase);
+        for (int kc = 0; kc < whole + (tail_ks ? 1 : 0); ++kc) {
+          if (!__all_sync(0xffffffffu, here)) {
+            ok = __all_sync(0xffffffffu, dsn_wait(bar_full + 8 * stage, phase, abort_flag, p.status, 63));
+            if (!ok) break;
           }
-          accumulate = 1;
+          tc_fence_after();
+          const uint32_t this_empty = bar_empty + 8 * stage;
+          const uint64_t ca = da, cb = db;
           da += dstep;
           db += dstep;
           if (++stage == stages) { stage = 0; phase ^= 1u; da = da0; db = db0; }
+          here = mbar_test_wait(bar_full + 8 * stage, phase);
+          if (kc < whole) {
+            if (elect_one()) {
+              umma_i8_pair(d_tmem, ca, cb, idesc, accumulate);  // +32 bytes per K step
+              umma_i8_pair(d_tmem, ca + 2u, cb + 2u, idesc, 1u);
+              umma_i8_pair(d_tmem, ca + 4u, cb + 4u, idesc, 1u);
+              umma_i8_pair(d_tmem, ca + 6u, cb + 6u, idesc, 1u);
+              umma_commit_pair(this_empty);
+            }
+          } else if (elect_one()) {
+            umma_i8_pair(d_tmem, ca, cb, idesc, accumulate);
+            if (tail_ks > 1) umma_i8_pair(d_tmem, ca + 2u, cb + 2u, idesc, 1u);
+            if (tail_ks > 2) umma_i8_pair(d_tmem, ca + 4u, cb + 4u, idesc, 1u);
+            if (tail_ks > 3) umma_i8_pair(d_tmem, ca + 6u, cb + 6u, idesc, 1u);
+            umma_commit_pair(this_empty);
+          }
+          accumulate = 1;
         }
         if (ok && elect_one()) umma_commit_pair(bar_tfull + 8 * acc);
       }
