@@ -511,7 +511,9 @@ template <bool F32, bool RES>
 cudaError_t pick(const NormParams& p, int sm_count, cudaStream_t s) {
   const int steps = (p.max_k + 7) / 8;
   const int64_t rows = (int64_t)p.B * p.R;
-  if (rows >= 8 * sm_count && steps <= 1024) {
+  // The ring's start-up costs a microsecond (us, ring and direct form, with residual and codes: 1024 rows of 4096 9.5, 8.5; 2400 of 4096 18.6, 20.0; 4800 of
+  // 768 8.6, 8.7; 4800 of 384 6.0, 5.6).
+  if (rows >= 8 * sm_count && rows * p.max_k >= 5 << 20 && steps <= 1024) {
     if (steps <= 16) return launch_ring<F32, RES, 16, 1>(p, sm_count, s);
     if (steps <= 32) return launch_ring<F32, RES, 16, 2>(p, sm_count, s);
     if (steps <= 48) return launch_ring<F32, RES, 16, 3>(p, sm_count, s);

@@ -406,7 +406,8 @@ cudaError_t launch(const RotaryParams& p, int sm_count, cudaStream_t s) {
 template <bool F32, bool VEC, bool INTER>
 cudaError_t pick(const RotaryParams& p, int sm_count, cudaStream_t s) {
   const int64_t bytes = (int64_t)p.max_heads * p.vectors * p.D * (F32 ? 4 : 2);
-  if (VEC && (int64_t)p.B * p.N >= 8 * sm_count && bytes <= 92 * 1024) {
+  // (us, ring and direct form, 4.6 KB rows: 300 rows 4.4, 3.7; 600 rows 4.4, 5.3; 4800 rows 9.3, 12.1)
+  if (VEC && (int64_t)p.B * p.N >= 4 * sm_count && bytes <= 92 * 1024) {
     // the fewest threads a row with which two slots a group fit
     if (bytes <= 5888) return launch_ring<F32, INTER, 32>(p, (uint32_t)bytes, 2, sm_count, s);
     if (bytes <= 11776) return launch_ring<F32, INTER, 64>(p, (uint32_t)bytes, 2, sm_count, s);

@@ -9,7 +9,8 @@ from transformer_util import groups
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("B,R,C", [(7, 3, 500), (2000, 1, 96), (2000, 1, 384), (1300, 2, 768), (1300, 1, 1000), (1500, 1, 3000), (1200, 1, 7000)])
+@pytest.mark.parametrize("B,R,C", [(7, 3, 500), (2000, 1, 96), (2000, 1, 384), (1300, 2, 768), (1300, 1, 1000), (1500, 1, 3000), (1200, 1, 7000),
+                                   (2000, 30, 96), (2000, 12, 250), (2000, 8, 384), (1300, 6, 768), (1300, 5, 1000), (1300, 3, 2000)])
 @pytest.mark.parametrize("name", ["bf16", "f32"])
 @pytest.mark.parametrize("residual", [False, True])
 def test_codes_are_those_of_the_definition(dsn, B, R, C, name, residual):

@@ -121,7 +121,7 @@ def test_norm_matches_oracle(dsn, ctx, name, B, R, C, k):
 def test_norm_of_many_rows_matches_oracle(dsn, ctx, name, C, k):
     """Rows enough for the form that streams them through shared memory, one width list for each number of threads a row."""
     g = np.random.default_rng(C)
-    B, R = 101, 15
+    B, R = 101, max(15, -(-(5 << 20) // (101 * C)) + 1)
     idx = g.integers(0, len(k), size=B)
     x, res = data(g, B, R, C, name), data(g, B, R, C, name)
     w = g.uniform(-2, 2, size=C).astype(np.float32).astype(np.float64)
@@ -132,10 +132,10 @@ def test_norm_of_many_rows_matches_oracle(dsn, ctx, name, C, k):
 def test_many_rows_with_tight_last_row_bad_rows_and_large_rows(dsn, ctx):
     """The last row ends with the tensor; rows that are no numbers and rows whose squares overflow stand among ordinary ones."""
     g = np.random.default_rng(12)
-    for C in (77, 1501):
-        B, R, ld = 1300, 1, -(-C // 16) * 16
+    for C, B in ((77, 1300), (77, 70000), (1501, 1300), (1501, 4000)):   # either form
+        R, ld = 1, -(-C // 16) * 16
         x = g.normal(size=(B, R, C)).astype(np.float32).astype(np.float64)
-        x[5, 0, C - 1], x[17, 0, 3], x[1299, 0, 0] = np.nan, np.inf, 3.0
+        x[5, 0, C - 1], x[17, 0, 3], x[B - 1, 0, 0] = np.nan, np.inf, 3.0
         x[6] *= 2.0 ** 70
         x[7] *= 2.0 ** -125
         x[8] = 0
