@@ -1402,6 +1402,9 @@ int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r
   p.status = ctx->d_status;
   p.positions = positions; p.x = x; p.y = y; p.ldx = d->ldx; p.ldy = d->ldy;
   const int aligned = aligned16(x) && aligned16(y) && (d->ldx * es) % 16 == 0 && (d->ldy * es) % 16 == 0;
+  p.whole_rows = aligned;
+  for (int t = 0; t < d->T; ++t)
+    if (((int64_t)d->heads[t] * d->vectors * d->D * es) % 16) p.whole_rows = 0;
   count_launch(ctx, &dsn_stats::launches_rotary);
   return dsn_launch_rotary(p, d->dtype == DSN_F32, aligned, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }

@@ -6,7 +6,9 @@
 // Ring form: a group of 32 .. 256 threads has a ring of shared-memory slots of its own, which bulk copies fill with the rows to come
 // (tokens and their positions are looked up 32 at a time, one a lane); it turns a row where it lies and one bulk copy takes it out, so
 // what does not turn (v, the rest of a head) costs no instruction at all, and the bytes in flight do not depend on registers.
-// Direct form (few tokens, rows that are not made of 16-byte pieces or too long for a ring): a thread owns one place of a vector,
+// Where rows are whole 16-byte pieces but vectors or the turned part are not, the ring's threads turn a pair at a time in shared memory (5096 rows of up
+// to 31 heads x 256 bf16 with 67 pairs: 32 us; element by element in global memory, the direct form: 100 us).
+// Direct form (few tokens, rows that are not made of 16-byte pieces or too long for a ring): a thread owns one place of a vector (an element pair if need be),
 // keeps its factors in registers and walks the heads with them.
 // Measured: 32,766 rows of 16 heads x 80 fp32, three axes: 57 us (5.9 TB/s of 6.6 for a copy); q and k of 25,216 rows of up to 12 heads x 64 bf16: 32 us
 // (5.4 TB/s).
@@ -211,15 +213,16 @@ struct TokenAt {
   int64_t row;
 };
 
-template <bool F32, bool INTER, int TPT>
+template <bool F32, bool VEC, bool INTER, int TPT>
 __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __grid_constant__ RotaryParams p, int depth, uint32_t slot_bytes) {
   typedef Vec<F32> E;
-  constexpr int GROUPS = kRingThreads / TPT, ES = F32 ? 4 : 2, W = E::n, NP = W / 2;
+  constexpr int GROUPS = kRingThreads / TPT, ES = F32 ? 4 : 2, W = VEC ? E::n : 1, NP = E::n / 2;
+  typedef typename E::type elem;
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t s_full[GROUPS][kRingDepth];
   __shared__ TokenAt s_at[GROUPS][kRingDepth];
   // the factors of a token as the places take them: halves cos and sin, neighbours (cos, cos) and (-sin, sin) of every pair
-  constexpr int NS = INTER ? 256 : 128;
+  constexpr int NS = VEC && INTER ? 256 : 128;
   __shared__ __align__(16) float s_cos[GROUPS][NS], s_sin[GROUPS][NS];
   __shared__ uint32_t s_abort;
   const int g = threadIdx.x / TPT, t = threadIdx.x % TPT, lane = threadIdx.x & 31;
@@ -271,7 +274,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
     for (int i = 0; i < depth && i < mine; ++i) ask(i);
 
   const int P = p.pairs, D = p.D;
-  const int per = INTER ? 2 * P / W : P / W;        // places of a vector that this kernel's threads take
+  const int per = VEC && INTER ? 2 * P / W : P / W;   // places of a vector that this kernel's threads take (one pair each where places are not whole)
   const int dv = TPT / per, di = TPT - dv * per;    // from one of a thread's places to its next
   const int v0 = t / per, i0 = t - v0 * per;
   // the pairs whose angle this thread computes
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
           float c, s;
           sincospif((float)(int32_t)(a >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: -1 .. 1 half turns
           s = p.inverse ? -s : s;
-          if constexpr (INTER) {
+          if constexpr (VEC && INTER) {
             *reinterpret_cast<float2*>(&s_cos[g][2 * i]) = make_float2(c, c);
             *reinterpret_cast<float2*>(&s_sin[g][2 * i]) = make_float2(-s, s);
           } else {
@@ -343,17 +346,32 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
           *reinterpret_cast<uint4*>(at) = E::narrow(a);
         }
       };
-      uint64_t c[NP], s[NP];
-      if (di == 0) {   // this thread's place is the same in all of its vectors
-        factors(i0 * W, c, s);
+      if constexpr (VEC) {
+        uint64_t c[NP], s[NP];
+        if (di == 0) {   // this thread's place is the same in all of its vectors
+          factors(i0 * W, c, s);
 #pragma unroll 4
-        for (int v = v0; v < turned; v += dv) turn_place(row + (size_t)(vec_at(p, v) + i0 * W) * ES, c, s);
+          for (int v = v0; v < turned; v += dv) turn_place(row + (size_t)(vec_at(p, v) + i0 * W) * ES, c, s);
+        } else {
+          int v = v0, pc = i0;
+#pragma unroll 2
+          while (v < turned) {
+            factors(pc * W, c, s);
+            turn_place(row + (size_t)(vec_at(p, v) + pc * W) * ES, c, s);
+            v += dv;
+            pc += di;
+            if (pc >= per) { pc -= per; ++v; }
+          }
+        }
       } else {
         int v = v0, pc = i0;
 #pragma unroll 2
         while (v < turned) {
-          factors(pc * W, c, s);
-          turn_place(row + (size_t)(vec_at(p, v) + pc * W) * ES, c, s);
+          elem* at = reinterpret_cast<elem*>(row) + vec_at(p, v);
+          const int ia = INTER ? 2 * pc : pc, ib = INTER ? 2 * pc + 1 : pc + P;
+          const float a = E::get(at + ia), b = E::get(at + ib), c = s_cos[g][pc], s = s_sin[g][pc];
+          E::put(at + ia, a * c - b * s);
+          E::put(at + ib, a * s + b * c);
           v += dv;
           pc += di;
           if (pc >= per) { pc -= per; ++v; }
@@ -377,10 +395,10 @@ __global__ void __launch_bounds__(kRingThreads, 2) rotary_ring_kernel(const __gr
   if (fetches && n < mine) dsn_drain(dsn_gemm::smem_u32(&s_full[g][0]), depth, n, asked);
 }
 
-template <bool F32, bool INTER, int TPT>
+template <bool F32, bool VEC, bool INTER, int TPT>
 cudaError_t launch_ring(const RotaryParams& p, uint32_t row_bytes, int per_sm, int sm_count, cudaStream_t s) {
   static size_t configured[DSN_MAX_DEVICES] = {};
-  auto kernel = rotary_ring_kernel<F32, INTER, TPT>;
+  auto kernel = rotary_ring_kernel<F32, VEC, INTER, TPT>;
   constexpr int GROUPS = kRingThreads / TPT;
   int depth = (int)((per_sm == 2 ? 92 : 184) * 1024 / (GROUPS * row_bytes));
   if (depth < 2) return cudaErrorInvalidConfiguration;
@@ -406,13 +424,14 @@ cudaError_t launch(const RotaryParams& p, int sm_count, cudaStream_t s) {
 template <bool F32, bool VEC, bool INTER>
 cudaError_t pick(const RotaryParams& p, int sm_count, cudaStream_t s) {
   const int64_t bytes = (int64_t)p.max_heads * p.vectors * p.D * (F32 ? 4 : 2);
+  // whole_rows: every path's rows are whole 16-byte pieces, whatever their vectors are
   // (us, ring and direct form, 4.6 KB rows: 300 rows 4.4, 3.7; 600 rows 4.4, 5.3; 4800 rows 9.3, 12.1)
-  if (VEC && (int64_t)p.B * p.N >= 4 * sm_count && bytes <= 92 * 1024) {
+  if (p.whole_rows && (int64_t)p.B * p.N >= 4 * sm_count && bytes <= 92 * 1024) {
     // the fewest threads a row with which two slots a group fit
-    if (bytes <= 5888) return launch_ring<F32, INTER, 32>(p, (uint32_t)bytes, 2, sm_count, s);
-    if (bytes <= 11776) return launch_ring<F32, INTER, 64>(p, (uint32_t)bytes, 2, sm_count, s);
-    if (bytes <= 23552) return launch_ring<F32, INTER, 128>(p, (uint32_t)bytes, 2, sm_count, s);
-    return launch_ring<F32, INTER, 256>(p, (uint32_t)bytes, bytes <= 47104 ? 2 : 1, sm_count, s);
+    if (bytes <= 5888) return launch_ring<F32, VEC, INTER, 32>(p, (uint32_t)bytes, 2, sm_count, s);
+    if (bytes <= 11776) return launch_ring<F32, VEC, INTER, 64>(p, (uint32_t)bytes, 2, sm_count, s);
+    if (bytes <= 23552) return launch_ring<F32, VEC, INTER, 128>(p, (uint32_t)bytes, 2, sm_count, s);
+    return launch_ring<F32, VEC, INTER, 256>(p, (uint32_t)bytes, bytes <= 47104 ? 2 : 1, sm_count, s);
   }
   // a warp a token where there are tokens enough to fill the GPU, else 256 threads
   return (int64_t)p.B * p.N >= 16 * sm_count ? launch<F32, VEC, INTER, 32>(p, sm_count, s) : launch<F32, VEC, INTER, 256>(p, sm_count, s);

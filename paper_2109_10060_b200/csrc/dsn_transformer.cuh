@@ -160,7 +160,7 @@ struct RotaryParams {
   FastDiv by_N;
   int32_t B, G, T, grouped;
   int32_t n_pos;        // rows of one axis of `positions`
-  int32_t shared, interleaved, inverse, in_place;
+  int32_t shared, interleaved, inverse, in_place, whole_rows;
   const int32_t* offsets;
   const int32_t* perm;
   const int32_t* group_slice;

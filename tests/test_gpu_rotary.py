@@ -95,6 +95,18 @@ def test_rotary_of_many_tokens_matches_oracle(dsn, ctx, name, interleaved, H, D,
         per_axis=True, pitch=16, inverse=True)
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("H,D,vectors,heads,pairs", [(6, 7, 8, [3, 6], [1, 2]), (2, 34, 4, [2, 1], [5, 7, 5]), (12, 72, 3, [12, 5], [13, 5]),
+                                                     (31, 256, 1, [31, 30], [67]), (24, 256, 4, [24], [8, 41]), (3, 18, 2, [3, 1], [9])])
+def test_rotary_of_many_tokens_with_places_that_are_no_16_bytes(dsn, ctx, name, interleaved, H, D, vectors, heads, pairs):
+    """Whole rows of 16-byte pieces whose turned halves or vectors begin inside a piece; the last shape has such rows in fp32 alone."""
+    rotated = min(vectors, 2)
+    run(dsn, ctx, 21, 41, 31, H, D, heads, pairs, name, vectors=vectors, rotated=rotated, interleaved=interleaved, shared=True)
+    run(dsn, ctx, 22, 41, 31, H, D, heads, pairs, name, vectors=vectors, rotated=rotated, interleaved=interleaved, grouped=True, in_place=True,
+        per_axis=True, pitch=16, inverse=True)
+
+
 def test_rotary_unaligned_rows_take_the_element_form(dsn, ctx):
     for name in ("bf16", "f32"):
         run(dsn, ctx, 4, 3, 4, 2, 64, [1, 2], [16, 16], name, offset=1)
