@@ -70,21 +70,19 @@ __global__ void __launch_bounds__(kThreads) rows_i8_kernel(const __grid_constant
   const int o = o0 + (threadIdx.x & 15);
   const float sw = o < p.max_ko ? __ldg(p.w_scale + o) : 0.f, bias = (p.bias && o < p.max_ko) ? __ldg(p.bias + o) : 0.f;
   const int rows = p.B * p.R;
-  for (int i = warp; i < 8 * NT; i += kWarps) {
+  if (warp == 0) {   // one row a lane
     RowInfo ri{0, -1, 0.f, 0x7fffffff, 0, 0};   // a row that does not exist reads the first one's codes: its sums go nowhere
-    if (i < rows) {
-      const int pos = i / p.R, r = i - pos * p.R;
-      const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
-      if (at.slice >= 0) {
-        ri.src = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
-        ri.dst = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
-        ri.sx = p.x_scale[ri.src];
-        ri.ki = p.k_in[at.slice];
-        ri.ko = p.k_out[at.slice];
-        ri.slice = at.slice;
-      }
+    const int pos = lane < rows ? lane / p.R : p.B, r = lane - pos * p.R;
+    const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
+    if (at.slice >= 0) {
+      ri.src = (int64_t)(p.in_input_order ? at.sample : pos) * p.R + r;
+      ri.dst = (int64_t)(p.out_input_order ? at.sample : pos) * p.R + r;
+      ri.sx = p.x_scale[ri.src];
+      ri.ki = p.k_in[at.slice];
+      ri.ko = p.k_out[at.slice];
+      ri.slice = at.slice;
     }
-    if (lane == 0) info[i] = ri;
+    if (lane < 8 * NT) info[lane] = ri;
   }
   __syncthreads();
   const int8_t* xr[NT];
