@@ -64,6 +64,7 @@ struct Prepared {
   int64_t row[BM];            // output row, -1: not part of the result
   int n0, ncols, map, ko;
 };
+static_assert(sizeof(Prepared) % 16 == 0, "two in a row, whose factors are read 16 bytes at a time");
 
 // D[tmem] (+)= A[smem] * B[smem]^T on both CTAs' tensor cores, signed 8-bit operands, 32-bit integer sums
 __device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {

@@ -114,6 +114,24 @@ def test_linear_i8_epilogues(dsn, ctx, y, act, bias, bn, residual, B, R):
     check(run(dsn, ctx, c, ki, ko, y, act, in_grouped=True, out_grouped=True, tail=1), c, ki, ko, y, act)
 
 
+@pytest.mark.parametrize("y", ["bf16", "f32"])
+@pytest.mark.parametrize("act,bias,bn,residual", [(0, True, False, False), (1, False, True, True), (2, True, False, True)])
+@pytest.mark.parametrize("B,R,C,N", [(64, 1, 1600, 64), (2, 49, 1100, 61), (1, 197, 4096, 300), (5, 40, 2001, 130), (64, 16, 1030, 600), (33, 1, 16000, 16), (40, 1, 4096, 1024),
+                                     (1, 260, 900, 1000)])
+def test_linear_i8_long_rows_and_few_tiles(dsn, ctx, y, act, bias, bn, residual, B, R, C, N):
+    """Long reductions of tiles fewer than the GPU has room for, paths of one piece beside paths of many, and all samples on one path (more tiles than the
+    estimate, which deals samples out evenly)."""
+    T = 4
+    ki, ko = [100, C, C // 2, C - 1], [N, N // 3, 8, N - 1]
+    c = make(B + R + C + N, B, R, C, N, T, bias=bias, bn=bn, residual=residual)
+    for grouped in (False, True):
+        check(run(dsn, ctx, c, ki, ko, y, act, grouped, not grouped), c, ki, ko, y, act)
+    c["idx"][:] = 3
+    check(run(dsn, ctx, c, ki, [16, 16, 16, N], y, act, True, True), c, ki, [16, 16, 16, N], y, act)
+    c["idx"][:] = 0
+    check(run(dsn, ctx, c, ki[:1], [N], y, act, False, True), c, ki[:1], [N], y, act)
+
+
 def test_linear_i8_extreme_codes_sum_exactly(dsn, ctx):
     """-128 * -128 over the longest rows stays inside 32 bits and is exact; fp32 represents the power of two."""
     C, N = 32752, 64
