@@ -85,6 +85,7 @@ class NormDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("R", C.c_int32), ("C", C.c_int32), ("ldx", C.c_int64), ("ld_res", C.c_int64),
                 ("ld_sum", C.c_int64), ("ldy", C.c_int64), ("ldq", C.c_int64), ("T", C.c_int32), ("k", C.POINTER(C.c_int32)),
                 ("weight", C.c_void_p), ("eps", C.c_float), ("in_order", C.c_int32), ("out_order", C.c_int32)]
+    _at = None   # device of the tensors
 
 
 class LinearI8Desc(C.Structure):
@@ -93,6 +94,7 @@ class LinearI8Desc(C.Structure):
                 ("W", C.c_void_p), ("w_scale", C.c_void_p), ("bias", C.c_void_p), ("bn_scale", C.c_void_p), ("bn_shift", C.c_void_p),
                 ("residual", C.c_void_p), ("y_dtype", C.c_int32), ("act", C.c_int32), ("in_order", C.c_int32),
                 ("out_order", C.c_int32), ("tail", C.c_int32)]
+    _at = None   # device of the tensors
 
 
 class RotaryDesc(C.Structure):
@@ -415,7 +417,7 @@ def dsn_layer_forward(ctx: Context, L: LayerDesc, x, idx_in, y, workspace, r_out
                                      ws_bytes, _stream_handle(stream)), "dsn_layer_forward")
 
 
-# ---- transformer blocks in 8 bits.  These calls also check what a pointer cannot say: type, device and extent of every tensor.
+# ---- transformer blocks in 8 bits.  These calls also check what a pointer cannot say: type, device, strides and extent of every tensor.
 
 class _Types:
     """torch's types by the library's codes, looked up once."""
@@ -433,19 +435,63 @@ def _types():
     return _Types if _Types.of_code else _Types.load()
 
 
-def _buf(what: str, t, dtype, need: int, device: Optional[int] = None, rows: bool = False) -> Optional[int]:
-    """Pointer of a device tensor of this type with at least `need` elements: dense, or (rows) from its first one to its storage's end,
-    as rows with a leading dimension lie."""
-    if t is None:
-        return None
+def _placed(what: str, t, dtype, device: Optional[int]) -> None:
     at = t.get_device()
     if t.dtype is not dtype or at < 0 or (device is not None and at != device):
         raise DsnError(ERR_INVALID_ARG, f"{what}: {t.dtype} on {t.device}, expected {dtype} on cuda" + ("" if device is None else f":{device}"))
-    if t.numel() < need and not (rows and t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() >= need):
-        raise DsnError(ERR_INVALID_ARG, f"{what}: {t.numel()} elements, at least {need} are read or written")
-    if not rows and not t.is_contiguous():
+
+
+def _buf(what: str, t, dtype, need: int, device: Optional[int] = None) -> Optional[int]:
+    """Pointer of a dense device tensor of this type with at least `need` elements."""
+    if t is None:
+        return None
+    _placed(what, t, dtype, device)
+    if not t.is_contiguous():
         raise DsnError(ERR_INVALID_ARG, f"{what}: not contiguous")
+    if t.numel() < need:
+        raise DsnError(ERR_INVALID_ARG, f"{what}: {t.numel()} elements, at least {need} are read or written")
     return t.data_ptr()
+
+
+def _rows(what: str, t, dtype, rows: int, ld: int, width: int, device: Optional[int] = None) -> Optional[int]:
+    """Pointer of a device tensor whose memory, from its first element on, holds `rows` rows of `width` elements that lie `ld` apart: a dense
+    tensor of any shape, or a view whose inner dimensions are dense and whose outer ones step by `ld` from row to row (a column range of a wider
+    buffer).  Expanded and transposed tensors have no such rows: the kernels would run past the storage, or read another order."""
+    if t is None:
+        return None
+    _placed(what, t, dtype, device)
+    if not t.is_contiguous():
+        step, outer = 1, False   # what the stride of the next dimension outwards has to be
+        for n, stride in zip(reversed(t.shape), reversed(t.stride())):
+            if n == 1:
+                continue
+            if stride != step and not outer:
+                step, outer = ld, True
+            if stride != step:
+                raise DsnError(ERR_INVALID_ARG,
+                               f"{what}: strides {tuple(t.stride())} of shape {tuple(t.shape)} are not those of rows {ld} elements apart")
+            step *= n
+    need = _span(rows, ld, width)
+    if not (t.is_contiguous() and t.numel() >= need) and t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < need:
+        raise DsnError(ERR_INVALID_ARG, f"{what}: {t.numel()} elements, at least {need} are read or written")
+    return t.data_ptr()
+
+
+def _same_device(**tensors) -> Optional[int]:
+    """The one device of a descriptor's tensors (None: it has no tensors); the calls compare it with the context's."""
+    at = None
+    for what, t in tensors.items():
+        if t is None:
+            continue
+        if at is not None and t.get_device() != at:
+            raise DsnError(ERR_INVALID_ARG, f"{what} on cuda:{t.get_device()}, the descriptor's other tensors on cuda:{at}")
+        at = t.get_device()
+    return at
+
+
+def _check_desc(d, ctx) -> None:
+    if d._at is not None and d._at != ctx.device:
+        raise DsnError(ERR_INVALID_ARG, f"{type(d).__name__}: tensors on cuda:{d._at}, the context on cuda:{ctx.device}")
 
 
 def _span(rows: int, ld: int, width: int) -> int:
@@ -459,29 +505,33 @@ def make_norm_desc(dtype, R, Cn, k, weight=None, eps=1e-6, ldx=None, ld_res=None
     ka = _i32_array(k)
     d = NormDesc(dtype, R, Cn, *(Cn if v is None else v for v in (ldx, ld_res, ld_sum, ldy, ldq)), len(k), ka, _ptr(weight), eps,
                  in_order, out_order)
-    d._keep = (ka, weight)
+    d._keep, d._at = (ka, weight), _same_device(weight=weight)
     return d
 
 
-# The calls below look at each tensor in place and hand it to _buf only where something is off (or it is a view of rows): a Python call
+# The calls below look at each tensor in place and hand it to _rows only where it is no dense tensor that holds all rows whole: a Python call
 # a tensor is a fifth of the host's time for a small one.
 
 def dsn_rmsnorm_quant(ctx: Context, d: NormDesc, routing: Routing, x, q=None, scale=None, y=None, residual=None, sum_out=None, stream=None):
     ty, rows, dev, Cn = _Types if _Types.of_code else _types(), routing.B * d.R, ctx.device, d.C
     dt = ty.of_code.get(d.dtype)
-    n = rows * max(d.ldx, d.ldy, d.ld_res, d.ld_sum, d.ldq)   # a tensor of so many elements holds any of the spans
+    n = rows * max(d.ldx, d.ldy, d.ld_res, d.ld_sum, d.ldq)   # a dense tensor of so many elements holds any of the spans
+    _check_desc(d, ctx)
     _check(ctx.lib.dsn_rmsnorm_quant(
         ctx.handle, d, routing,
-        x.data_ptr() if x is not None and x.dtype is dt and x.get_device() == dev and x.numel() >= n else _buf("x", x, dt, _span(rows, d.ldx, Cn), dev, True),
-        None if residual is None else residual.data_ptr() if residual.dtype is dt and residual.get_device() == dev and residual.numel() >= n
-        else _buf("residual", residual, dt, _span(rows, d.ld_res, Cn), dev, True),
-        None if sum_out is None else sum_out.data_ptr() if sum_out.dtype is dt and sum_out.get_device() == dev and sum_out.numel() >= n
-        else _buf("sum_out", sum_out, dt, _span(rows, d.ld_sum, Cn), dev, True),
-        None if q is None else q.data_ptr() if q.dtype is ty.i8 and q.get_device() == dev and q.numel() >= n
-        else _buf("q", q, ty.i8, _span(rows, d.ldq, Cn), dev, True),
+        x.data_ptr() if x is not None and x.dtype is dt and x.get_device() == dev and x.numel() >= n and x.is_contiguous()
+        else _rows("x", x, dt, rows, d.ldx, Cn, dev),
+        None if residual is None else residual.data_ptr()
+        if residual.dtype is dt and residual.get_device() == dev and residual.numel() >= n and residual.is_contiguous()
+        else _rows("residual", residual, dt, rows, d.ld_res, Cn, dev),
+        None if sum_out is None else sum_out.data_ptr()
+        if sum_out.dtype is dt and sum_out.get_device() == dev and sum_out.numel() >= n and sum_out.is_contiguous()
+        else _rows("sum_out", sum_out, dt, rows, d.ld_sum, Cn, dev),
+        None if q is None else q.data_ptr() if q.dtype is ty.i8 and q.get_device() == dev and q.numel() >= n and q.is_contiguous()
+        else _rows("q", q, ty.i8, rows, d.ldq, Cn, dev),
         None if scale is None else _buf("scale", scale, ty.f32, rows, dev),
-        None if y is None else y.data_ptr() if y.dtype is dt and y.get_device() == dev and y.numel() >= n
-        else _buf("y", y, dt, _span(rows, d.ldy, Cn), dev, True),
+        None if y is None else y.data_ptr() if y.dtype is dt and y.get_device() == dev and y.numel() >= n and y.is_contiguous()
+        else _rows("y", y, dt, rows, d.ldy, Cn, dev),
         _stream_handle(stream)), "dsn_rmsnorm_quant")
 
 
@@ -491,7 +541,7 @@ def make_linear_i8_desc(R, C_in, C_out, k_in, k_out, W, w_scale, bias=None, bn_s
     """Linear layer on int8 rows and weights; leading dimensions default to the extents."""
     ldx, ldw, ldy = C_in if ldx is None else ldx, C_in if ldw is None else ldw, C_out if ldy is None else ldy
     f = _types().f32
-    _buf("W", W, _types().i8, _span(C_out, ldw, C_in), rows=True)
+    _rows("W", W, _types().i8, C_out, ldw, C_in)
     for what, t, n in (("w_scale", w_scale, C_out), ("bias", bias, C_out), ("bn_scale", bn_scale, len(k_out) * C_out),
                        ("bn_shift", bn_shift, len(k_out) * C_out)):
         _buf(what, t, f, n)
@@ -499,6 +549,7 @@ def make_linear_i8_desc(R, C_in, C_out, k_in, k_out, W, w_scale, bias=None, bn_s
     d = LinearI8Desc(R, C_in, C_out, ldx, ldw, ldy, len(k_in), ki, ko, _ptr(W), _ptr(w_scale), _ptr(bias), _ptr(bn_scale), _ptr(bn_shift),
                      _ptr(residual), y_dtype, act, in_order, out_order, tail)
     d._keep = (ki, ko, W, w_scale, bias, bn_scale, bn_shift, residual)
+    d._at = _same_device(W=W, w_scale=w_scale, bias=bias, bn_scale=bn_scale, bn_shift=bn_shift)
     return d
 
 
@@ -510,19 +561,22 @@ def dsn_sliced_linear_i8(ctx: Context, d: LinearI8Desc, routing: Routing, x, x_s
     ty, rows, dev = _Types if _Types.of_code else _types(), routing.B * d.R, ctx.device
     dt, residual, ws_bytes = ty.of_code.get(d.y_dtype), d._keep[-1], 0
     n = rows * d.ldy
-    if residual is not None and not (residual.dtype is dt and residual.get_device() == dev and residual.numel() >= n):
-        _buf("residual", residual, dt, _span(rows, d.ldy, d.C_out), dev, True)
+    _check_desc(d, ctx)
+    if residual is not None and not (residual.dtype is dt and residual.get_device() == dev and residual.numel() >= n
+                                     and residual.is_contiguous()):
+        _rows("residual", residual, dt, rows, d.ldy, d.C_out, dev)
     if workspace is not None:
         ws_bytes = workspace.numel() * workspace.element_size()
-        if workspace.get_device() != dev:
-            raise DsnError(ERR_INVALID_ARG, f"workspace on {workspace.device}, expected cuda:{dev}")
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise DsnError(ERR_INVALID_ARG,
+                           f"workspace: strides {tuple(workspace.stride())} on {workspace.device}, expected a dense tensor on cuda:{dev}")
     _check(ctx.lib.dsn_sliced_linear_i8(
         ctx.handle, d, routing,
-        x.data_ptr() if x is not None and x.dtype is ty.i8 and x.get_device() == dev and x.numel() >= rows * d.ldx
-        else _buf("x", x, ty.i8, _span(rows, d.ldx, d.C_in), dev, True),
+        x.data_ptr() if x is not None and x.dtype is ty.i8 and x.get_device() == dev and x.numel() >= rows * d.ldx and x.is_contiguous()
+        else _rows("x", x, ty.i8, rows, d.ldx, d.C_in, dev),
         _buf("x_scale", x_scale, ty.f32, rows, dev),
-        y.data_ptr() if y is not None and y.dtype is dt and y.get_device() == dev and y.numel() >= n
-        else _buf("y", y, dt, _span(rows, d.ldy, d.C_out), dev, True),
+        y.data_ptr() if y is not None and y.dtype is dt and y.get_device() == dev and y.numel() >= n and y.is_contiguous()
+        else _rows("y", y, dt, rows, d.ldy, d.C_out, dev),
         _ptr(workspace), ws_bytes, _stream_handle(stream)), "dsn_sliced_linear_i8")
 
 
@@ -545,5 +599,5 @@ def dsn_rotary_axes(ctx: Context, d: RotaryDesc, routing: Routing, positions, x,
     row = d.H * d.vectors * d.D
     _check(ctx.lib.dsn_rotary_axes(ctx.handle, d, routing,
                                    _buf("positions", positions, ty.i32, d.n_axes * (d.N if d.shared_positions else rows), dev),
-                                   _buf("x", x, dt, _span(rows, d.ldx, row), dev, True), _buf("y", y, dt, _span(rows, d.ldy, row), dev, True),
+                                   _rows("x", x, dt, rows, d.ldx, row, dev), _rows("y", y, dt, rows, d.ldy, row, dev),
                                    _stream_handle(stream)), "dsn_rotary_axes")
