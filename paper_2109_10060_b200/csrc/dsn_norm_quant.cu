@@ -163,7 +163,8 @@ __device__ __forceinline__ void load_weights(const NormParams& p, int t, uint64_
 }
 
 // A row that lies in the registers of its TPR threads (h, zero at and beyond k) -> everything that is written for it.  False where `ok`
-// does not hold in all threads of the row; then they all leave.  When it returns, all of them have the row in registers.
+// does not hold in all threads of the row (those have k = 0: what precedes the agreement, the stream, is stored by threads with ok alone); then
+// they all leave.  When it returns, all of them have the row in registers.
 template <bool F32, int TPR, int VPT>
 __device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur, int t, uint64_t (&h)[VPT][4], const uint64_t (&w)[VPT][4], float2* part,
                                            int& turn, int id, bool ok) {
@@ -430,7 +431,8 @@ __global__ void __launch_bounds__(kRingThreads, 2) norm_quant_ring_kernel(const 
   int n = 0;
   for (; n < mine; ++n) {
     const bool ok = dsn_wait(dsn_gemm::smem_u32(&s_full[g][slot]), phase, abort_flag, p.status, 71);
-    const RowAt cur = s_at[g][slot][sub];
+    // a thread whose wait ran out has no row: its slot holds an earlier one, or nothing yet, and the stream may be written in place
+    const RowAt cur = ok ? s_at[g][slot][sub] : RowAt{0, 0, 0, 0};
     const int k = cur.k;
     const elem* xs = reinterpret_cast<const elem*>(slots + (size_t)slot * slot_bytes + (size_t)sub * copies * row_bytes);
     const elem* rsd = reinterpret_cast<const elem*>(reinterpret_cast<const uint8_t*>(xs) + row_bytes);
