@@ -80,21 +80,6 @@ __device__ __forceinline__ uint32_t make_idesc_i8(int M, int N) {
   return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// The fitted GELU for two values.  Its odd quintic turns round beyond |v| = 8, where the tanh has long been +-1, so v^2 is
-// held at 36 inside it (at |v| = 6 the argument is 10).
-__device__ __forceinline__ void gelu_pair_i8(float a, float b, float& ra, float& rb) {
-  const uint64_t zero2 = pack2(0.f, 0.f), v2 = pack2(a, b);
-  const uint64_t z2 = pack2(fminf(a * a, 36.f), fminf(b * b, 36.f));
-  uint64_t q = ffma2(z2, pack2(-0.00035873294f, -0.00035873294f), pack2(0.037050344f, 0.037050344f));
-  q = ffma2(z2, q, pack2(0.79745847f, 0.79745847f));
-  float u0, u1, t0, t1;
-  unpack2(ffma2(v2, q, zero2), u0, u1);
-  asm("tanh.approx.f32 %0, %1;" : "=f"(t0) : "f"(u0));
-  asm("tanh.approx.f32 %0, %1;" : "=f"(t1) : "f"(u1));
-  const uint64_t h2 = ffma2(v2, pack2(0.5f, 0.5f), zero2);
-  unpack2(ffma2(h2, pack2(t0, t1), h2), ra, rb);
-}
-
 // first column of piece j of a warp (bf16 rows are stored 64 columns at a time, fp32 rows 32; two warps share a lane quarter)
 template <bool F32>
 __device__ __forceinline__ int piece_col(int first, int j) {
@@ -178,7 +163,7 @@ __device__ __forceinline__ void epilogue_i8_piece(const uint32_t (&v)[32], int c
           f[c] = gelu_f32(f[c]);
           f[c + 1] = gelu_f32(f[c + 1]);
         } else {
-          gelu_pair_i8(f[c], f[c + 1], f[c], f[c + 1]);
+          gelu_pair(f[c], f[c + 1], f[c], f[c + 1]);
         }
       }
     }
