@@ -180,7 +180,8 @@ typedef struct dsn_attention_desc {
  *   s = max_c |n| / 127,   q = round(n / s) to the nearest, ties to even, in -127 .. 127   (an all-zero row: s = 0, q = 0)
  * The code is computed as round(h weight * (127 * (1 / max|h weight|))) in fp32, each operation rounded once: the factor that
  * all columns share drops out, so a code does not depend on the order of the sum of squares.
- * A row that holds a NaN or an infinity comes out as s = NaN, q = 0, y = NaN; squares that overflow fp32 do not. */
+ * A row that holds a NaN or an infinity comes out as s = NaN, q = 0, y = NaN.  Rows whose squares, or products with the weight, leave the range
+ * of fp32 do not: they are scaled by powers of two, which changes neither code nor n. */
 typedef struct dsn_norm_desc {
   int32_t dtype;        /* DSN_BF16 or DSN_F32: x, residual, sum, y                      */
   int32_t R;            /* rows per sample                                               */

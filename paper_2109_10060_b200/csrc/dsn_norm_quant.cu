@@ -162,6 +162,8 @@ __device__ __forceinline__ void load_weights(const NormParams& p, int t, uint64_
   }
 }
 
+constexpr float kSmallMax = 7.52316385e-37f;   // 2^-120: 127 / a maximum below it would leave fp32
+
 // A row that lies in the registers of its TPR threads (h, zero at and beyond k) -> everything that is written for it.  False where `ok`
 // does not hold in all threads of the row (those have k = 0: what precedes the agreement, the stream, is stored by threads with ok alone); then
 // they all leave.  When it returns, all of them have the row in registers.
@@ -220,7 +222,7 @@ __device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur
   // that is no number, the row is looked at again (rare; the same decision in all threads of the row).
   const float rk = __fdividef(1.f, (float)k);
   float rs = rsqrtf(ss * rk + p.eps);
-  const bool redo = !(ss < INFINITY) || !(mx < INFINITY) || (mx < 7.52316385e-37f && mx > 0.f);
+  const bool redo = !(ss < INFINITY) || !(mx < INFINITY) || (mx < kSmallMax && mx > 0.f);
   if (TPR < 32 ? __any_sync(0xffffffffu, redo) : redo) {
     const float ss1 = ss;
     float top = 0.f, none = 0.f;
@@ -235,14 +237,21 @@ __device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur
       const int e = (int)(__float_as_uint(top) >> 23);
       f = __uint_as_float((uint32_t)(e > 252 ? 1 : (e < 1 ? 253 : 254 - e)) << 23);
     }
-    const uint64_t f2 = pack2(f, f);
+#pragma unroll 1
+    for (int again = 0; again < 2; ++again) {
+      const uint64_t f2 = pack2(f, f);
 #pragma unroll
-    for (int j = 0; j < VPT; ++j)
+      for (int j = 0; j < VPT; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[j][i] = fmul2(h[j][i], f2);
-    measure();
-    if (f < 1.f) rs = rsqrtf(ss * rk + p.eps * f * f);
-    else if (f > 1.f) rs = rsqrtf(ss1 * rk + p.eps) / f;               // eps outweighs squares this small
+        for (int i = 0; i < 4; ++i) h[j][i] = fmul2(h[j][i], f2);
+      measure();
+      if (again) rs *= 1.f / f;
+      else if (f < 1.f) rs = rsqrtf(ss * rk + p.eps * f * f);
+      else if (f > 1.f) rs = rsqrtf(ss1 * rk + p.eps) / f;             // eps outweighs squares this small
+      // Weights that take a row of this size out of the range: another power of two, of which the sum of squares knows nothing.
+      f = !redo || !(top < INFINITY) ? 1.f : (mx < kSmallMax && mx > 0.f ? 0x1p100f : (mx == INFINITY ? 0x1p-8f : 1.f));
+      if (!(TPR < 32 ? __any_sync(0xffffffffu, f != 1.f) : f != 1.f)) break;
+    }
     if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);          // NaN or infinity in the row: NaN comes out
   }
   if (k == 0) return true;
