@@ -237,20 +237,23 @@ __device__ __forceinline__ bool finish_row(const NormParams& p, const RowAt& cur
       const int e = (int)(__float_as_uint(top) >> 23);
       f = __uint_as_float((uint32_t)(e > 252 ? 1 : (e < 1 ? 253 : 254 - e)) << 23);
     }
-#pragma unroll 1
-    for (int again = 0; again < 2; ++again) {
+    auto scale_row = [&](float f) {
       const uint64_t f2 = pack2(f, f);
 #pragma unroll
       for (int j = 0; j < VPT; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[j][i] = fmul2(h[j][i], f2);
       measure();
-      if (again) rs *= 1.f / f;
-      else if (f < 1.f) rs = rsqrtf(ss * rk + p.eps * f * f);
-      else if (f > 1.f) rs = rsqrtf(ss1 * rk + p.eps) / f;             // eps outweighs squares this small
-      // Weights that take a row of this size out of the range: another power of two, of which the sum of squares knows nothing.
-      f = !redo || !(top < INFINITY) ? 1.f : (mx < kSmallMax && mx > 0.f ? 0x1p100f : (mx == INFINITY ? 0x1p-8f : 1.f));
-      if (!(TPR < 32 ? __any_sync(0xffffffffu, f != 1.f) : f != 1.f)) break;
+    };
+    scale_row(f);
+    if (f < 1.f) rs = rsqrtf(ss * rk + p.eps * f * f);
+    else if (f > 1.f) rs = rsqrtf(ss1 * rk + p.eps) / f;               // eps outweighs squares this small
+    // Weights that take a row of this size out of the range: another power of two, of which the sum of squares knows nothing.  (As a loop of two
+    // rounds this block cost the rows that never come here: 37 x 121 rows of 1000 fp32 columns 9.4 -> 9.9 us.)
+    f = !redo || !(top < INFINITY) ? 1.f : (mx < kSmallMax && mx > 0.f ? 0x1p100f : (mx == INFINITY ? 0x1p-8f : 1.f));
+    if (TPR < 32 ? __any_sync(0xffffffffu, f != 1.f) : f != 1.f) {
+      scale_row(f);
+      rs *= 1.f / f;
     }
     if (!(top < INFINITY)) mx = __uint_as_float(0x7fffffffu);          // NaN or infinity in the row: NaN comes out
   }
