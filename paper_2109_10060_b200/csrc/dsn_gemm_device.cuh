@@ -209,30 +209,30 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
 // tanh (relative error <= 2^-11), i.e. one special-function instruction per element instead of the
 // two (reciprocal, exponential) a rational erf needs, which kept the epilogue behind the main loop.
 // The total deviation from exact GELU stays below 1e-3 absolute at |x| = 4, a quarter of a bfloat16
-// ulp of the output there.  The quintic turns round at |v| = 8.3 and changes sign at |v| = 11, so its factor
-// c1 + c3 z^2 + c5 z^4 is held at c1 from below: it falls under that at |v| = 10.2 only, where the tanh has long been +-1.
+// ulp of the output there.  The quintic turns round at |x| = 8.3 and changes sign at |x| = 11, so the |x| in its factor
+// c1 + c3 z^2 + c5 z^4 is held at 8.25 (|z| at 5.8), where the tanh has long been +-1: no result below that changes.
 __device__ __forceinline__ float erf_fast(float z) {
-  const float z2 = z * z;
-  const float u = z * fmaxf(fmaf(z2, fmaf(z2, -0.0020293f, 0.1047942f), 1.12777659f), 1.12777659f);
+  const float m = fminf(fabsf(z), 5.8f), z2 = m * m;
+  const float u = z * fmaf(z2, fmaf(z2, -0.0020293f, 0.1047942f), 1.12777659f);
   float t;
   asm("tanh.approx.f32 %0, %1;" : "=f"(t) : "f"(u));
   return t;
 }
 
 // The same GELU for two values at once with packed fp32 arithmetic (two lanes per instruction): the epilogue is bound
-// by instruction issue, not by a pipe, and this form needs 6 packed instructions, 2 maxima and 2 tanh for a pair where the
-// scalar form needs 18 and 2 (measured without the maxima: cfg3 fc1 57.4 -> 53.5 us, cfg5 fc1 on the narrowest path 203 ->
-// 188 us; the maxima cost the cfg3 block 232.8 -> 234.4 us).  0.5 v (1 + t) is evaluated as h + h t with h = v / 2.
+// by instruction issue, not by a pipe, and this form needs 6 packed instructions, 2 minima and 2 tanh for a pair where the
+// scalar form needs 18 and 2 (measured without the minima: cfg3 fc1 57.4 -> 53.5 us, cfg5 fc1 on the narrowest path 203 ->
+// 188 us).  The minima stand in front of the square: cfg3 fc1 52.5 -> 53.2 us, the narrowest path unchanged; behind it 54.0,
+// on the factor itself 54.5.  0.5 v (1 + t) is evaluated as h + h t with h = v / 2.
 __device__ __forceinline__ void gelu_pair(float a, float b, float& ra, float& rb) {
-  // erf(v / sqrt 2) ~= tanh(v max(k1, k1 + k3 v^2 + k5 v^4)) with the 1 / sqrt 2 folded into the coefficients of erf_fast
+  // erf(v / sqrt 2) ~= tanh(v (k1 + k3 m^2 + k5 m^4)), m = min(|v|, 8.25), with the 1 / sqrt 2 folded into the coefficients of erf_fast
   const uint64_t zero2 = pack2(0.f, 0.f);
   const uint64_t v2 = pack2(a, b);
-  const uint64_t z2 = ffma2(v2, v2, zero2);
+  const uint64_t m2 = pack2(fminf(fabsf(a), 8.25f), fminf(fabsf(b), 8.25f));
+  const uint64_t z2 = ffma2(m2, m2, zero2);
   uint64_t q = ffma2(z2, pack2(-0.00035873294f, -0.00035873294f), pack2(0.037050344f, 0.037050344f));
   q = ffma2(z2, q, pack2(0.79745847f, 0.79745847f));
   float u0, u1, t0, t1;
-  unpack2(q, u0, u1);
-  q = pack2(fmaxf(u0, 0.79745847f), fmaxf(u1, 0.79745847f));
   unpack2(ffma2(v2, q, zero2), u0, u1);
   asm("tanh.approx.f32 %0, %1;" : "=f"(t0) : "f"(u0));
   asm("tanh.approx.f32 %0, %1;" : "=f"(t1) : "f"(u1));
