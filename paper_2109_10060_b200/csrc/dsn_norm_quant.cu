@@ -525,6 +525,8 @@ template <bool F32, bool RES>
 cudaError_t pick(const NormParams& p, int sm_count, cudaStream_t s) {
   const int steps = (p.max_k + 7) / 8;
   const int64_t rows = (int64_t)p.B * p.R;
+  // Rows beyond 8192 columns have the direct form alone, whose 32 weights and 32 columns a thread do not fit the registers (2000 rows bf16 with residual, codes
+  // and stream: 8192 columns 25 us, 12,000 68, 30,000 131 against 17, 26, 64 for the bytes).
   // The ring's start-up costs a microsecond (us, ring and direct form, with residual and codes: 1024 rows of 4096 9.5, 8.5; 2400 of 4096 18.6, 20.0; 4800 of
   // 768 8.6, 8.7; 4800 of 384 6.0, 5.6).
   if (rows >= 8 * sm_count && rows * p.max_k >= 5 << 20 && steps <= 1024) {
@@ -534,9 +536,12 @@ cudaError_t pick(const NormParams& p, int sm_count, cudaStream_t s) {
     if (steps <= 96) return launch_ring<F32, RES, 32, 3>(p, sm_count, s);
     if (steps <= 128) return launch_ring<F32, RES, 32, 4>(p, sm_count, s);
     if (steps <= 256) return launch_ring<F32, RES, 64, 4>(p, sm_count, s);
-    // 2048 .. 4096 columns: with everything asked for, memory bounds the pass, and fewer rows being written at a time suit it better (16,384
-    // rows of 4096 bf16: 97 us against 112); otherwise the time a row takes from its wait to its stores does, and more rows do (54 against 70)
-    if (steps <= 512 && RES && p.q && p.y) return launch_ring<F32, RES, 256, 2>(p, sm_count, s);
+    // 2056 .. 4096 columns, 128 or 256 threads a row (us with either).  bf16, 16,384 rows: where the stream and y are both written, memory bounds
+    // the pass from some 3400 columns on and fewer rows being written at a time suit it better (3200 columns 78.0, 92.9; 3456 97.1, 94.8; 4096 113.5,
+    // 95.9, without codes 98.9, 85.1); with less to write, the time a row takes from its wait to its stores does, and more rows do (4096 without the
+    // stream 82.8, 89.0, without y 78.1, 91.8).  fp32, 8192 rows with residual, codes and y: with the stream either way within a tenth (2816: 72.9, 64.4;
+    // 3584: 82.4, 90.9; 4096: 102.9, 105.2), without it 256 threads (3200: 71.7, 56.8; 4096: 76.8, 69.9).
+    if (steps <= 512 && RES && p.y && (F32 ? p.q != nullptr : p.sum != nullptr && steps > 424)) return launch_ring<F32, RES, 256, 2>(p, sm_count, s);
     if (steps <= 512) return launch_ring<F32, RES, 128, 4>(p, sm_count, s);
     return launch_ring<F32, RES, 256, 4>(p, sm_count, s);
   }
