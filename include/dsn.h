@@ -45,9 +45,12 @@ enum dsn_status {
 };
 
 enum dsn_dtype { DSN_F32 = 0, DSN_BF16 = 1 };
-/* DSN_ACT_GELU: x/2 (1 + erf(x / sqrt 2)) with erf evaluated as tanh of a fitted odd quintic on the hardware
- * tanh: within 3e-5 (absolute) of the erf form from the fit, below 1e-3 absolute overall at |x| = 4, i.e. a
- * fraction of a bfloat16 rounding step of the output. */
+/* DSN_ACT_GELU: x/2 (1 + erf(x / sqrt 2)).  How a kernel evaluates it, and how far from the erf form that is, before the output is rounded:
+ *   bf16 layers, and 8-bit layers with bf16 outputs of more than 32 rows (B * R): erf as the hardware tanh of a fitted odd quintic,
+ *     within 3e-5 + |x| 2^-12 (1e-3 at |x| = 4: a fraction of a bfloat16 rounding step at x = 4, more than the value itself at x = -4);
+ *   8-bit layers with fp32 outputs of more than 32 rows: formula 7.1.26 of Abramowitz and Stegun, within 0.75e-7 |x| besides roundings;
+ *   fp32 layers, depthwise layers (unless DSN_DWPW=fused joins them with the next layer: the first form) and 8-bit layers of at most 32 rows: erff.
+ * A row of an 8-bit layer can therefore differ by these bounds between a call of 32 rows and one of 33. */
 enum dsn_act { DSN_ACT_NONE = 0, DSN_ACT_RELU = 1, DSN_ACT_GELU = 2 };
 enum dsn_order { DSN_INPUT_ORDER = 0, DSN_GROUPED = 1 };
 enum dsn_tail { DSN_TAIL_UNTOUCHED = 0, DSN_TAIL_ZERO = 1 };
@@ -214,7 +217,7 @@ typedef struct dsn_linear_i8_desc {
   const float* bn_shift;
   const void* residual; /* as in dsn_linear_desc: y's type, order and leading dimension  */
   int32_t y_dtype;      /* DSN_BF16 or DSN_F32: y and residual                           */
-  int32_t act;          /* DSN_ACT_GELU: the fitted form for bf16 outputs, the erf form itself for fp32 outputs */
+  int32_t act;          /* dsn_act; which form of GELU runs depends on y_dtype and on the number of rows (see there) */
   int32_t in_order;     /* dsn_order of x and x_scale                                    */
   int32_t out_order;    /* dsn_order of y and residual                                   */
   int32_t tail;

@@ -7,8 +7,9 @@
 // affine into one factor and one addend a column, and puts them with the rows' scales and places into shared memory (done by the
 // epilogue warps themselves, decoding and fetching took 1.7 of their 5.8 thousand cycles a tile); what is left to an element is
 // a conversion, a multiplication and a packed multiply-add.
-// Bound by the tensor cores where the reduction is long (16,384 rows, 4096 -> 4096: 166 us, 3.3 POP/s, twice the measured bf16 rate), by the epilogue
-// where it is short (50,432 rows, 768 -> 2304: 76.5 us, 2.3 POP/s; the bf16 kernel takes 131 us).
+// Bound by the tensor cores where the reduction is long (16,384 rows, 4096 -> 4096: 166 us and 3.3 POP/s, twice the measured bf16 rate, while the power
+// allows it, 176 to 195 us in longer runs), by the epilogue where it is short (50,432 rows, 768 -> 2304: 76 us, 2.3 POP/s; the bf16 kernel
+// without a bias takes 129 us).  Times are those of calls in a graph.
 // Barriers (every CTA has the same layout):
 //   full[s]    even CTA only: one arrival (expect_tx for the bytes of both CTAs), completed by the loads of both
 //   empty[s]   both CTAs: the multicast commit frees the stage

@@ -10,8 +10,8 @@
 // to 31 heads x 256 bf16 with 67 pairs: 32 us; element by element in global memory, the direct form: 100 us).
 // Direct form (few tokens, rows that are not made of 16-byte pieces or too long for a ring): a thread owns one place of a vector (an element pair if need be),
 // keeps its factors in registers and walks the heads with them.
-// Measured: 32,766 rows of 16 heads x 80 fp32, three axes: 57 us (5.9 TB/s of 6.6 for a copy); q and k of 25,216 rows of up to 12 heads x 64 bf16: 32 us
-// (5.4 TB/s).
+// Measured in a graph: 32,766 rows of 16 heads x 80 fp32, three axes: 58 us (5.8 TB/s of 6.6 for a copy); q and k of 25,216 rows of up to 12 heads x 64
+// bf16: 32 us (5.4 TB/s), and 33 us in place, where v need not move but does: rows pass whole (the q and k alone would take 18).
 #include <type_traits>
 
 #include "dsn_transformer.cuh"

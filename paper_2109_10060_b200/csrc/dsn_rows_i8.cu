@@ -4,8 +4,9 @@
 // the warp-level 8-bit matrix instruction (16 channels x 8 rows x 32 columns): at most 32 rows cannot fill the 128 rows of a
 // tensor-memory tile, and this form takes its operands straight from registers.  The order of the columns inside a sum
 // is free, so a lane's 16 consecutive bytes serve as its pieces of two instructions, the same way for weights and rows.
-// One row of 4096 x 4096 takes 5.3 us against 2.6 for its bytes (launch, one round trip to memory and the meeting are the rest), 32 rows 9.5 us; from
-// 33 rows on the tensor-memory form is the faster one (64 rows: 13.2 us, with eight tiles of rows here 19.4).
+// One row of 4096 x 4096 takes 4.8 us in a graph, weights in L2, against 2.6 for its bytes (launch, one round trip to memory and the meeting are the
+// rest), 32 rows 6.5 us; from 33 rows on the tensor-memory form is the faster one (64 rows: 11.3 us, with eight tiles of rows here 19.4).  Weights that
+// come from memory: one row of 8192 x 8192 16.5 us against 10.2.
 // Rows of narrower paths are zero beyond their k_in, so all rows share one reduction over the widest path's columns.
 #include "dsn_transformer.cuh"
 
