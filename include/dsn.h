@@ -41,7 +41,8 @@ enum dsn_status {
   DSN_ERR_BAD_INDEX = -5,   /* (device) a routing index outside [0, T)                     */
   DSN_ERR_CUDA = -6,        /* a CUDA runtime / driver call failed                         */
   DSN_ERR_TIMEOUT = -7,     /* (device) a bounded wait inside a kernel ran out             */
-  DSN_ERR_NONFINITE = -8    /* (device) a gate score was NaN or infinite                   */
+  DSN_ERR_NONFINITE = -8,   /* (device) a gate score was NaN or infinite                   */
+  DSN_ERR_CACHE_FULL = -9   /* (device) a request's new tokens found no room in the cache  */
 };
 
 enum dsn_dtype { DSN_F32 = 0, DSN_BF16 = 1 };
@@ -250,6 +251,55 @@ typedef struct dsn_rotary_desc {
   int32_t inverse;      /* 1: turn by the negative angle                                 */
 } dsn_rotary_desc;
 
+/* Cache of keys and values in 4 bits, for transformer blocks that run token by token or piece by piece (not in the paper).
+ * A sample of the batch is a request that keeps its cache from call to call; it has to keep its path, or move to one with fewer
+ * heads, for as long as it is cached (a head that an earlier token's path did not have holds nothing for that token).
+ *
+ * Rows of a call lie as everywhere, [B][R][ld]; request i has rows 0 .. placed[i] - 1 of its R, the rest is padding that is neither
+ * read nor written.  A row of qkv holds H heads of group + 2 vectors of D_h elements, [head][q x group | k | v][D_h]: group = 1 is the
+ * layout of the sliced attention core, larger groups share a head's keys and values among their queries.  A row of the output
+ * holds [head][group][D_h].  Heads >= heads[t] of a request of path t are neither read nor written.
+ *
+ * Pages: [n_pages][H][page / 16] blocks of 16 tokens.  A block holds the keys, then the values, each as
+ *   codes [D_h / 64][16][32 bytes]   64 elements a token, element 2 j in the low half of byte j, 2 j + 1 in the high half
+ *   pairs [D_h / 64][16]             scale and middle, bfloat16 each
+ * which makes 18 D_h bytes a block (1152 for D_h = 64).  An element is middle + scale * (code - 8).
+ * A group of 64 elements x with least and greatest value a, b is rounded as follows, every operation once in fp32:
+ *   scale = bf16(b / 15 - a / 15), the quotients as products with the fp32 number nearest 1 / 15;  0 if that is below 2^-126
+ *   middle = bf16(2 (a / 2 + 4 scale));  code = round((x - middle) * (1 / scale)) + 8, ties to even, held in 0 .. 15;  8 where scale = 0
+ * (b - a and a + 8 scale could leave fp32's range.)  A token whose k or v holds a NaN or an infinity in a head is stored as NaN there:
+ * middle NaN, scale 0 in all groups of k and v, and every query of the head that sees it comes out as NaN.
+ *
+ * Token number n of request i (0 is its first) lies in page table[i][n / page], at place n % page of it. */
+typedef struct dsn_cache_desc {
+  int32_t dtype;        /* DSN_BF16: qkv, out, values                                    */
+  int32_t R;            /* rows per request in this call, 1..2^24                        */
+  int32_t H, D_h;       /* full head count 1..4096 (heads of k and v); 64 or 128         */
+  int32_t group;        /* query vectors per head, 1..64                                 */
+  int32_t page;         /* tokens per page: a multiple of 16, 16..1024                   */
+  int32_t n_pages;      /* pages that exist; n_pages * page < 2^31                       */
+  int32_t max_pages;    /* columns of the table: the most pages that a request can hold; max_pages * page < 2^30 */
+  int64_t ld_qkv;       /* elements between rows of qkv, >= H * (group + 2) * D_h, a multiple of 8 */
+  int64_t ld_out;       /* of out, >= H * group * D_h, a multiple of 8                   */
+  int64_t ld_values;    /* of values, >= H * 2 * D_h, a multiple of 8                    */
+  int32_t T;
+  const int32_t* heads; /* host [T]: head count of each path, 1..H                       */
+  int32_t order;        /* dsn_order of the rows of qkv, out and values; what dsn_cache holds is always by request */
+  float scale;          /* of the scores, finite; 0: 1 / sqrt(D_h)                       */
+  int32_t window;       /* a query sees the last `window` tokens up to and with its own; 0: all of them */
+} dsn_cache_desc;
+
+/* Where a cache lies; all of it device memory of the caller. */
+typedef struct dsn_cache {
+  uint8_t* pages;       /* dsn_cache_bytes(), 16-byte aligned                            */
+  int32_t* table;       /* [B][max_pages]; entries behind the pages that a request holds mean nothing */
+  int32_t* lengths;     /* [B] tokens of each request                                    */
+  int32_t* placed;      /* [B] rows of each request in this call                         */
+  int32_t* slots;       /* [B][R] where each row's token goes: page * tokens per page + place, -1: nowhere */
+  int32_t* pool;        /* [n_pages] ring of the pages that no request holds             */
+  int32_t* pool_state;  /* [2] place of the first of them in the ring, how many there are */
+} dsn_cache;
+
 /* One dynamic block: optional gate, routing, then up to DSN_MAX_CHAIN layers that all inherit
  * the block's routing (Sec. 5, "inherit the control signal").  Layer j reads layer j-1's output;
  * layer 0 reads x in input order, the last layer writes y in input order; intermediate
@@ -331,6 +381,9 @@ typedef struct dsn_stats {
   uint64_t launches_gemm_i8;      /* 8-bit linear layers on the tensor cores, CTA pairs                    */
   uint64_t launches_rows_i8;      /* 8-bit linear layers of a few rows                                     */
   uint64_t launches_rotary;
+  uint64_t launches_cache_plan;   /* 4-bit cache: pages and slots                                          */
+  uint64_t launches_cache_write;  /* 4-bit cache: keys and values rounded into their pages                 */
+  uint64_t launches_cache_attention; /* 4-bit cache: attention over the pages, with the joining of its parts */
 } dsn_stats;
 int dsn_get_stats(dsn_ctx* ctx, dsn_stats* out);
 
@@ -447,6 +500,39 @@ int dsn_sliced_linear_i8(dsn_ctx* ctx, const dsn_linear_i8_desc* d, const dsn_ro
  * vectors and elements that do not turn as they were. */
 int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r, const int32_t* positions, const void* x,
                     void* y, void* stream);
+
+/* ---- attention over a 4-bit cache -------------------------------------------------------- */
+/* Bytes of dsn_cache.pages (0: the descriptor is not valid). */
+size_t dsn_cache_bytes(const dsn_cache_desc* d);
+/* An empty cache: lengths 0, every page in the pool.  Uses lengths, pool, pool_state. */
+int dsn_cache_reset(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, int32_t B, void* stream);
+
+/* Finds room for the new tokens of every request: new_tokens device [B], 0 .. R to append, -1 to end the request (its pages go back
+ * to the pool, from which the next call can take them).  Requests are served in order: one that needs pages gets them if its need and that of all
+ * requests before it, served or not, fits into the pool, and if its row of the table has room; else nothing of it is placed and DSN_ERR_CACHE_FULL is
+ * recorded with its number.  A length or new_tokens value out of range counts as a request that changes nothing and records
+ * DSN_ERR_BAD_INDEX.  Pages leave the ring from its front and return at its end, in the order of requests: the same call gives the same pages.
+ * Reads lengths, table, pool, pool_state; writes the new entries of table, placed (rows placed, 0 for a request that ended), slots, the
+ * returned entries of pool, and lengths and pool_state after the call to lengths_out [B] and pool_state_out [2] (NULL, or c's own: in place).
+ * Only pages that were taken here may be given back here: none is held by two requests. */
+int dsn_cache_plan(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, int32_t B, const int32_t* new_tokens, int32_t* lengths_out,
+                   int32_t* pool_state_out, void* stream);
+
+/* Rounds k and v of the rows to 4 bits and writes them to their slots (rows with slot -1 go nowhere; other slots outside the cache record
+ * DSN_ERR_BAD_INDEX and go nowhere either; no two rows may have the same slot).  values (or NULL): the values that the codes stand for, rounded
+ * to bfloat16, rows [head][k | v][D_h].  Uses pages and slots. */
+int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* values,
+                       void* stream);
+
+/* out = softmax(scale * q k^T) v over the cached tokens that a row's query sees: row j of request i is token n = lengths[i] - placed[i] + j of
+ * it (its keys are in the cache already) and sees tokens max(0, n - window + 1) .. n.  Scores, softmax and sums in fp32, probabilities in bfloat16 for the second
+ * product.  A row that sees nothing (n < 0) comes out as zeros.  Uses pages, table, lengths, and placed (NULL: R rows of every request).  A length or
+ * placed value out of range is held at the nearest end of it, tokens of a page outside the cache are left out, and both record DSN_ERR_BAD_INDEX.
+ * workspace: device, 16-byte aligned, of dsn_cache_attention_q4_workspace_bytes; nothing in it has to start at zero.  It must not be
+ * used by two calls at once. */
+size_t dsn_cache_attention_q4_workspace_bytes(const dsn_cache_desc* d, int32_t B);
+int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* out,
+                           void* workspace, size_t ws_bytes, void* stream);
 
 /* ---- whole dynamic block (Eq. (dyn_net)) ------------------------------------------------ */
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L);

@@ -424,3 +424,103 @@ def rotary_axes(x, positions, pairs, base=10000.0, per_axis=False, interleaved=F
             y[..., v] = xu * np.sin(angle) + xv * np.cos(angle)
             i += 1
     return y
+
+
+# --------------------------------------------------------------------------- 4-bit cache
+def cache_round(x):
+    """Groups of 64 elements (last axis) of bf16 values to (code 0..15, scale, middle); scale and middle [..., D / 64].
+
+    The stored pair and the codes are defined by operations in fp32 and bf16, each rounded once; those roundings are mirrored."""
+    f = np.float32
+    v = np.asarray(x, dtype=F64).reshape(*np.shape(x)[:-1], -1, 64)
+    lo, hi = v.min(-1), v.max(-1)
+    def rf(a):
+        with np.errstate(over="ignore"):          # x - middle of the widest groups: an infinity, which the ends hold
+            return np.asarray(a, dtype=F64).astype(f).astype(F64)
+    fifteenth = F64(f(1.0) / f(15.0))
+    s = round_bf16(rf(rf(hi * fifteenth) - rf(lo * fifteenth)))
+    s = np.where(s < 2.0 ** -126, 0.0, s)
+    z = round_bf16(2 * rf(0.5 * lo + 4 * s))
+    with np.errstate(divide="ignore"):
+        inv = np.where(s > 0, rf(1 / np.where(s > 0, s, 1.0)), 0.0)
+    step = np.rint(rf(rf(v - z[..., None]) * inv[..., None]))
+    code = np.where(s[..., None] > 0, np.clip(step + 8, 0, 15), 8)
+    bad = ~np.isfinite(np.asarray(x, dtype=F64))
+    assert not bad.any(), "rows that are not finite are not rounded by this form"
+    return code.astype(np.uint8), s, z
+
+
+def cache_values(code, s, z):
+    """What codes stand for, [..., D]."""
+    v = z[..., None] + s[..., None] * (code.astype(F64) - 8)
+    return v.reshape(*v.shape[:-2], 64 * v.shape[-2])
+
+
+def cache_place(D, page, H, slot, head, half, group, element):
+    """Byte and shift of an element's code, and byte of its group's pair, in the pages of a cache; half 0: k, 1: v."""
+    n = D // 64
+    pg, tok = divmod(slot, page)
+    block = (pg * H + head) * (page // 16) + tok // 16
+    at = block * 18 * D + half * 9 * D
+    return at + (group * 16 + tok % 16) * 32 + element // 2, 4 * (element % 2), at + n * 512 + (group * 16 + tok % 16) * 4
+
+
+def cache_plan(held, new, table, ring, first, free, page, max_pages, R):
+    """One call of the plan, request by request.  `table`: list of lists of the pages that a request holds.  Returns placed, lengths, table,
+    slots, ring, first, free and the requests that found no room and those that were out of range."""
+    from collections import deque
+    N = len(ring)
+    queue = deque(ring[(first + j) % N] for j in range(free))
+    asked, taken = 0, 0
+    placed, lengths, slots, full, bad, returned = [], [], [], [], [], []
+    table = [list(t) for t in table]
+    for i, (h, n) in enumerate(zip(held, new)):
+        row = [-1] * R
+        ok = 0 <= h <= max_pages * page and -1 <= n <= R
+        if not ok:
+            bad.append(i)
+            placed.append(0), lengths.append(h), slots.append(row)
+            continue
+        have = -(-h // page)
+        if n < 0:
+            returned += table[i][:have]
+            placed.append(0), lengths.append(0), slots.append(row)
+            continue
+        need = -(-(h + n) // page) - have
+        if have + need > max_pages:
+            full.append(i)
+            placed.append(0), lengths.append(h), slots.append(row)
+            continue
+        asked += need
+        if need and asked > free:
+            full.append(i)
+            placed.append(0), lengths.append(h), slots.append(row)
+            continue
+        table[i] = table[i][:have] + [queue.popleft() for _ in range(need)]
+        taken += need
+        for r in range(n):
+            row[r] = table[i][(h + r) // page] * page + (h + r) % page
+        placed.append(n), lengths.append(h + n), slots.append(row)
+    ring = list(ring)
+    for j, p in enumerate(returned):
+        ring[(first + free + j) % N] = p
+    return placed, lengths, table, slots, ring, (first + taken) % N, free - taken + len(returned), full, bad
+
+
+def cache_attention(q, k, v, scale, first_token, window=0):
+    """q [n][D] of tokens first_token ..., k, v [L][D] -> out [n][D], weights [n][L]; rows that see nothing are zero."""
+    n, L = len(q), len(k)
+    me = first_token + np.arange(n)[:, None]
+    key = np.arange(L)[None, :]
+    seen = key <= me
+    if window:
+        seen &= key > me - window
+    if L == 0:
+        return np.zeros((n, np.shape(v)[-1])), np.zeros((n, 0))
+    s = np.where(seen, (np.asarray(q, dtype=F64) @ np.asarray(k, dtype=F64).T) * scale, -np.inf)
+    top = s.max(-1, keepdims=True)
+    p = np.exp(s - np.where(np.isfinite(top), top, 0.0))
+    p = np.where(seen, p, 0.0)
+    tot = p.sum(-1, keepdims=True)
+    p = p / np.where(tot > 0, tot, 1.0)
+    return p @ np.asarray(v, dtype=F64), p

@@ -6,5 +6,5 @@ CUDA library raises ImportError.
 """
 from .binding import *  # noqa: F401,F403
 from .binding import (Context, DsnError, EXPORTS, LIB_PATH, Routing, GateDesc, LinearDesc, ConvDesc, LayerDesc, AttentionDesc, DepthwiseDesc, NormDesc,
-                      LinearI8Desc, RotaryDesc, Stats,
+                      LinearI8Desc, RotaryDesc, CacheDesc, Cache, Stats,
                       load_library)

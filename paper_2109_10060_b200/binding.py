@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libdsn.so")
 
 OK = 0
 ERR_INVALID_ARG, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_UNSUPPORTED = -1, -2, -3, -4
-ERR_BAD_INDEX, ERR_CUDA, ERR_TIMEOUT, ERR_NONFINITE = -5, -6, -7, -8
+ERR_BAD_INDEX, ERR_CUDA, ERR_TIMEOUT, ERR_NONFINITE, ERR_CACHE_FULL = -5, -6, -7, -8, -9
 F32, BF16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 INPUT_ORDER, GROUPED = 0, 1
@@ -31,6 +31,8 @@ EXPORTS = [
     "dsn_sliced_attention", "dsn_sliced_depthwise", "dsn_linear_workspace_bytes", "dsn_conv_workspace_bytes", "dsn_sliced_linear", "dsn_sliced_conv",
     "dsn_layer_workspace_bytes", "dsn_layer_forward",
     "dsn_rmsnorm_quant", "dsn_linear_i8_workspace_bytes", "dsn_sliced_linear_i8", "dsn_rotary_axes",
+    "dsn_cache_bytes", "dsn_cache_reset", "dsn_cache_plan", "dsn_cache_write_q4", "dsn_cache_attention_q4_workspace_bytes",
+    "dsn_cache_attention_q4",
 ]
 
 
@@ -104,12 +106,25 @@ class RotaryDesc(C.Structure):
                 ("base", C.c_double), ("shared_positions", C.c_int32), ("inverse", C.c_int32)]
 
 
+class CacheDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("R", C.c_int32), ("H", C.c_int32), ("D_h", C.c_int32), ("group", C.c_int32), ("page", C.c_int32),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("ld_qkv", C.c_int64), ("ld_out", C.c_int64), ("ld_values", C.c_int64),
+                ("T", C.c_int32), ("heads", C.POINTER(C.c_int32)), ("order", C.c_int32), ("scale", C.c_float), ("window", C.c_int32)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("table", C.c_void_p), ("lengths", C.c_void_p), ("placed", C.c_void_p), ("slots", C.c_void_p),
+                ("pool", C.c_void_p), ("pool_state", C.c_void_p)]
+    _at = None   # device of the tensors
+
+
 class Stats(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("calls", "launches", "launches_gemm_pair", "launches_gemm_halo", "launches_gemm_chain",
                                           "launches_gemm_one_cta", "launches_linear_f32", "launches_attention",
                                           "launches_depthwise", "launches_dwpw", "launches_gate", "launches_route",
                                           "launches_copy", "map_hits", "map_misses", "launches_gemm_chain_tmem",
-                                          "launches_norm", "launches_gemm_i8", "launches_rows_i8", "launches_rotary")]
+                                          "launches_norm", "launches_gemm_i8", "launches_rows_i8", "launches_rotary",
+                                          "launches_cache_plan", "launches_cache_write", "launches_cache_attention")]
 
 
 class LayerDesc(C.Structure):
@@ -167,9 +182,17 @@ def load_library():
     lib.dsn_linear_i8_workspace_bytes.restype = sz
     lib.dsn_sliced_linear_i8.argtypes = [vp, C.POINTER(LinearI8Desc), C.POINTER(Routing), vp, vp, vp, vp, sz, vp]
     lib.dsn_rotary_axes.argtypes = [vp, C.POINTER(RotaryDesc), C.POINTER(Routing), vp, vp, vp, vp]
+    lib.dsn_cache_bytes.argtypes = [C.POINTER(CacheDesc)]
+    lib.dsn_cache_bytes.restype = sz
+    lib.dsn_cache_reset.argtypes = [vp, C.POINTER(CacheDesc), C.POINTER(Cache), i32, vp]
+    lib.dsn_cache_plan.argtypes = [vp, C.POINTER(CacheDesc), C.POINTER(Cache), i32, vp, vp, vp, vp]
+    lib.dsn_cache_write_q4.argtypes = [vp, C.POINTER(CacheDesc), C.POINTER(Cache), C.POINTER(Routing), vp, vp, vp]
+    lib.dsn_cache_attention_q4_workspace_bytes.argtypes = [C.POINTER(CacheDesc), i32]
+    lib.dsn_cache_attention_q4_workspace_bytes.restype = sz
+    lib.dsn_cache_attention_q4.argtypes = [vp, C.POINTER(CacheDesc), C.POINTER(Cache), C.POINTER(Routing), vp, vp, vp, sz, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
-        if name not in ("dsn_strerror", "dsn_executed_macs") and not name.endswith("workspace_bytes"):
+        if name not in ("dsn_strerror", "dsn_executed_macs") and not name.endswith(("workspace_bytes", "cache_bytes")):
             fn.restype = C.c_int
     _lib = lib
     return lib
@@ -601,3 +624,89 @@ def dsn_rotary_axes(ctx: Context, d: RotaryDesc, routing: Routing, positions, x,
                                    _buf("positions", positions, ty.i32, d.n_axes * (d.N if d.shared_positions else rows), dev),
                                    _rows("x", x, dt, rows, d.ldx, row, dev), _rows("y", y, dt, rows, d.ldy, row, dev),
                                    _stream_handle(stream)), "dsn_rotary_axes")
+
+
+# ---- attention over a 4-bit cache
+
+def make_cache_desc(R, H, D_h, heads, group=1, page=64, n_pages=1, max_pages=1, order=INPUT_ORDER, scale=0.0, window=0, ld_qkv=None, ld_out=None,
+                    ld_values=None) -> CacheDesc:
+    """Paged cache of keys and values in 4 bits, rows [head][q x group | k | v][D_h]; leading dimensions default to the rows' extents."""
+    hs = _i32_array(heads)
+    d = CacheDesc(BF16, R, H, D_h, group, page, n_pages, max_pages, H * (group + 2) * D_h if ld_qkv is None else ld_qkv,
+                  H * group * D_h if ld_out is None else ld_out, H * 2 * D_h if ld_values is None else ld_values, len(heads), hs, order, scale,
+                  window)
+    d._keep = (hs,)
+    return d
+
+
+def dsn_cache_bytes(d: CacheDesc) -> int:
+    return int(load_library().dsn_cache_bytes(C.byref(d)))
+
+
+def make_cache(pages=None, table=None, lengths=None, placed=None, slots=None, pool=None, pool_state=None) -> Cache:
+    """Where a cache lies: dense tensors, pages of uint8 (or int8), the others of int32.  A call checks the sizes of those it uses; the others
+    may be left out."""
+    import torch
+    for what, t in (("table", table), ("lengths", lengths), ("placed", placed), ("slots", slots), ("pool", pool), ("pool_state", pool_state)):
+        _buf(what, t, torch.int32, 0)
+    if pages is not None:
+        _buf("pages", pages, torch.int8 if pages.dtype is torch.int8 else torch.uint8, 0)
+    c = Cache(*(_ptr(t) for t in (pages, table, lengths, placed, slots, pool, pool_state)))
+    c._at = _same_device(pages=pages, table=table, lengths=lengths, placed=placed, slots=slots, pool=pool, pool_state=pool_state)
+    c._keep = (pages, table, lengths, placed, slots, pool, pool_state)
+    c._n = tuple(-1 if t is None else t.numel() for t in c._keep)
+    return c
+
+
+def _check_cache(what: str, ctx: Context, c: Cache, need) -> None:
+    """`need`: least number of elements of pages, table, lengths, placed, slots, pool, pool_state (0: not used)."""
+    if c._at is not None and c._at != ctx.device:
+        raise DsnError(ERR_INVALID_ARG, f"{what}: cache on cuda:{c._at}, the context on cuda:{ctx.device}")
+    for (name, _), have, n in zip(Cache._fields_, c._n, need):
+        if 0 <= have < n:
+            raise DsnError(ERR_INVALID_ARG, f"{what}: {name} has {have} elements, at least {n} are read or written")
+
+
+def dsn_cache_reset(ctx: Context, d: CacheDesc, cache: Cache, B: int, stream=None):
+    _check_cache("dsn_cache_reset", ctx, cache, (0, 0, B, 0, 0, d.n_pages, 2))
+    _check(ctx.lib.dsn_cache_reset(ctx.handle, d, cache, B, _stream_handle(stream)), "dsn_cache_reset")
+
+
+def dsn_cache_plan(ctx: Context, d: CacheDesc, cache: Cache, B: int, new_tokens, lengths_out=None, pool_state_out=None, stream=None):
+    i32, dev = _types().i32, ctx.device
+    _check_cache("dsn_cache_plan", ctx, cache, (0, B * d.max_pages, B, B, B * d.R, d.n_pages, 2))
+    _check(ctx.lib.dsn_cache_plan(ctx.handle, d, cache, B, _buf("new_tokens", new_tokens, i32, B, dev),
+                                  _buf("lengths_out", lengths_out, i32, B, dev), _buf("pool_state_out", pool_state_out, i32, 2, dev),
+                                  _stream_handle(stream)), "dsn_cache_plan")
+
+
+def dsn_cache_write_q4(ctx: Context, d: CacheDesc, cache: Cache, routing: Routing, qkv, values=None, stream=None):
+    dt, rows, dev = _types().of_code.get(d.dtype), routing.B * d.R, ctx.device
+    _check_cache("dsn_cache_write_q4", ctx, cache, (d.n_pages * d.H * (d.page // 16) * 18 * d.D_h, 0, 0, 0, rows, 0, 0))
+    _check(ctx.lib.dsn_cache_write_q4(
+        ctx.handle, d, cache, routing,
+        qkv.data_ptr() if qkv is not None and qkv.dtype is dt and qkv.get_device() == dev and qkv.numel() >= rows * d.ld_qkv and qkv.is_contiguous()
+        else _rows("qkv", qkv, dt, rows, d.ld_qkv, d.H * (d.group + 2) * d.D_h, dev),
+        _rows("values", values, dt, rows, d.ld_values, d.H * 2 * d.D_h, dev), _stream_handle(stream)), "dsn_cache_write_q4")
+
+
+def dsn_cache_attention_q4_workspace_bytes(d: CacheDesc, B: int) -> int:
+    return int(load_library().dsn_cache_attention_q4_workspace_bytes(C.byref(d), B))
+
+
+def dsn_cache_attention_q4(ctx: Context, d: CacheDesc, cache: Cache, routing: Routing, qkv, out, workspace=None, stream=None):
+    dt, B, dev, ws_bytes = _types().of_code.get(d.dtype), routing.B, ctx.device, 0
+    rows = B * d.R
+    _check_cache("dsn_cache_attention_q4", ctx, cache, (d.n_pages * d.H * (d.page // 16) * 18 * d.D_h, B * d.max_pages, B, B, 0, 0, 0))
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise DsnError(ERR_INVALID_ARG,
+                           f"workspace: strides {tuple(workspace.stride())} on {workspace.device}, expected a dense tensor on cuda:{dev}")
+    _check(ctx.lib.dsn_cache_attention_q4(
+        ctx.handle, d, cache, routing,
+        qkv.data_ptr() if qkv is not None and qkv.dtype is dt and qkv.get_device() == dev and qkv.numel() >= rows * d.ld_qkv and qkv.is_contiguous()
+        else _rows("qkv", qkv, dt, rows, d.ld_qkv, d.H * (d.group + 2) * d.D_h, dev),
+        out.data_ptr() if out is not None and out.dtype is dt and out.get_device() == dev and out.numel() >= rows * d.ld_out and out.is_contiguous()
+        else _rows("out", out, dt, rows, d.ld_out, d.H * d.group * d.D_h, dev),
+        _ptr(workspace), ws_bytes, _stream_handle(stream)), "dsn_cache_attention_q4")

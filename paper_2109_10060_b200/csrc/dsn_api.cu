@@ -6,6 +6,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include "dsn_cache.cuh"
 #include "dsn_internal.cuh"
 #include "dsn_transformer.cuh"
 
@@ -871,6 +872,45 @@ int check_rotary(const dsn_rotary_desc* d, const dsn_routing* r) {
   return DSN_OK;
 }
 
+// ------------------------------------------------------------------ 4-bit cache
+int check_cache_desc(const dsn_cache_desc* d) {
+  if (!d || !d->heads || d->dtype != DSN_BF16) return DSN_ERR_INVALID_ARG;
+  if (d->R < 1 || d->R > (1 << 24) || d->H < 1 || d->H > 4096 || (d->D_h != 64 && d->D_h != 128) || d->group < 1 || d->group > 64) return DSN_ERR_INVALID_ARG;
+  if (d->page < 16 || d->page > 1024 || d->page % DSN_CACHE_BLOCK || d->n_pages < 1 || d->max_pages < 1) return DSN_ERR_INVALID_ARG;
+  if ((int64_t)d->n_pages * d->page > INT32_MAX || (int64_t)d->max_pages * d->page >= (1LL << 30)) return DSN_ERR_INVALID_ARG;
+  if (d->T < 1 || d->T > DSN_MAX_SLICES || !valid_order(d->order)) return DSN_ERR_INVALID_ARG;
+  if (!(d->scale > -INFINITY && d->scale < INFINITY) || d->window < 0) return DSN_ERR_INVALID_ARG;
+  for (int t = 0; t < d->T; ++t)
+    if (d->heads[t] < 1 || d->heads[t] > d->H) return DSN_ERR_INVALID_ARG;
+  return DSN_OK;
+}
+
+int check_cache(const dsn_cache_desc* d, const dsn_cache* c) {
+  if (!c) return DSN_ERR_INVALID_ARG;
+  return check_cache_desc(d);
+}
+
+// d, c and the routing of a call on rows
+int check_cache_call(const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r) {
+  int e = check_cache(d, c);
+  if (!e) e = check_routing(r, d->T);
+  if (e) return e;
+  if (!c->pages || (int64_t)r->B * d->R > kMaxRows) return DSN_ERR_INVALID_ARG;
+  return aligned16(c->pages) ? DSN_OK : DSN_ERR_ALIGNMENT;
+}
+
+template <typename P>
+void fill_cache_routing(P& p, const dsn_cache_desc* d, const dsn_routing* r) {
+  for (int t = 0; t < d->T; ++t) {
+    p.heads[t] = (int16_t)d->heads[t];
+    if (d->heads[t] > p.max_heads) p.max_heads = d->heads[t];
+  }
+  p.B = r->B; p.R = d->R; p.H = d->H; p.group = d->group; p.G = r->G; p.T = d->T; p.page = d->page;
+  p.grouped = d->order == DSN_GROUPED;
+  p.by_page = dsn_fast_div((uint32_t)d->page);
+  p.offsets = r->offsets; p.perm = r->perm; p.group_slice = r->group_slice;
+}
+
 // workspace carving for dsn_layer_forward
 struct LayerPlan {
   size_t off_idx, off_counts, off_offsets, off_perm, off_inv, off_gate, off_buf[2], off_gather, total;
@@ -979,6 +1019,7 @@ const char* dsn_strerror(int code) {
     case DSN_ERR_CUDA: return "CUDA call failed";
     case DSN_ERR_TIMEOUT: return "bounded device wait ran out";
     case DSN_ERR_NONFINITE: return "non-finite gate score";
+    case DSN_ERR_CACHE_FULL: return "no room in the cache for a request's new tokens";
     default: return "unknown dsn status";
   }
 }
@@ -1407,6 +1448,96 @@ int dsn_rotary_axes(dsn_ctx* ctx, const dsn_rotary_desc* d, const dsn_routing* r
     if (((int64_t)d->heads[t] * d->vectors * d->D * es) % 16) p.whole_rows = 0;
   count_launch(ctx, &dsn_stats::launches_rotary);
   return dsn_launch_rotary(p, d->dtype == DSN_F32, aligned, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+}
+
+size_t dsn_cache_bytes(const dsn_cache_desc* d) {
+  if (check_cache_desc(d)) return 0;
+  return (size_t)d->n_pages * d->H * (size_t)(d->page / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(d->D_h);
+}
+
+int dsn_cache_reset(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, int32_t B, void* stream) {
+  int e = check_ctx(ctx);
+  if (!e) e = check_cache(d, c);
+  if (e) return e;
+  if (B < 0 || (B && !c->lengths) || !c->pool || !c->pool_state) return DSN_ERR_INVALID_ARG;
+  count_launch(ctx, &dsn_stats::launches_cache_plan);
+  return dsn_launch_cache_reset(B, d->n_pages, c->lengths, c->pool, c->pool_state, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+}
+
+int dsn_cache_plan(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, int32_t B, const int32_t* new_tokens, int32_t* lengths_out,
+                   int32_t* pool_state_out, void* stream) {
+  int e = check_ctx(ctx);
+  if (!e) e = check_cache(d, c);
+  if (e) return e;
+  if (B < 0 || (int64_t)B * d->R > kMaxRows || (B && !new_tokens) || !c->table || !c->lengths || !c->placed || !c->slots || !c->pool || !c->pool_state)
+    return DSN_ERR_INVALID_ARG;
+  CachePlanParams p;
+  p.B = B; p.R = d->R; p.page = d->page; p.n_pages = d->n_pages; p.max_pages = d->max_pages;
+  p.by_page = dsn_fast_div((uint32_t)d->page);
+  p.new_tokens = new_tokens; p.lengths = c->lengths; p.pool_state = c->pool_state;
+  p.lengths_out = lengths_out ? lengths_out : c->lengths;
+  p.pool_state_out = pool_state_out ? pool_state_out : c->pool_state;
+  p.table = c->table; p.placed = c->placed; p.slots = c->slots; p.pool = c->pool;
+  p.status = ctx->d_status;
+  if (p.lengths_out == new_tokens || p.lengths_out == c->placed || c->placed == new_tokens || c->placed == c->lengths || c->slots == new_tokens ||
+      c->slots == c->lengths || c->slots == c->placed)
+    return DSN_ERR_INVALID_ARG;
+  count_launch(ctx, &dsn_stats::launches_cache_plan);
+  return dsn_launch_cache_plan(p, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+}
+
+int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* values,
+                       void* stream) {
+  if (!qkv || (values && values == qkv)) return DSN_ERR_INVALID_ARG;
+  int e = check_ctx(ctx);
+  if (!e) e = check_cache_call(d, c, r);
+  if (!e && !c->slots) e = DSN_ERR_INVALID_ARG;
+  if (!e) e = check_rows(qkv, d->ld_qkv, (int64_t)d->H * (d->group + 2) * d->D_h, 2);
+  if (!e && values) e = check_rows(values, d->ld_values, (int64_t)d->H * 2 * d->D_h, 2);
+  if (e || r->B == 0) return e;
+  CacheWriteParams p;
+  memset(&p, 0, sizeof(p));
+  fill_cache_routing(p, d, r);
+  p.D = d->D_h;
+  p.n_slots = (int64_t)d->n_pages * d->page;
+  p.by_R = dsn_fast_div((uint32_t)d->R);
+  p.slots = c->slots; p.pages = c->pages;
+  p.qkv = static_cast<const __nv_bfloat16*>(qkv); p.ld_qkv = d->ld_qkv;
+  p.values = static_cast<__nv_bfloat16*>(values); p.ld_values = d->ld_values;
+  p.status = ctx->d_status;
+  count_launch(ctx, &dsn_stats::launches_cache_write);
+  return dsn_launch_cache_write(p, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+}
+
+size_t dsn_cache_attention_q4_workspace_bytes(const dsn_cache_desc* d, int32_t B) {
+  if (check_cache_desc(d) || B < 0) return 0;
+  return 0;
+}
+
+int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* out,
+                           void* workspace, size_t ws_bytes, void* stream) {
+  if (!qkv || !out || out == qkv) return DSN_ERR_INVALID_ARG;
+  int e = check_ctx(ctx);
+  if (!e) e = check_cache_call(d, c, r);
+  if (!e && (!c->table || !c->lengths)) e = DSN_ERR_INVALID_ARG;
+  if (!e) e = check_rows(qkv, d->ld_qkv, (int64_t)d->H * (d->group + 2) * d->D_h, 2);
+  if (!e) e = check_rows(out, d->ld_out, (int64_t)d->H * d->group * d->D_h, 2);
+  if (e) return e;
+  if (workspace && !aligned16(workspace)) return DSN_ERR_ALIGNMENT;
+  if (ws_bytes < dsn_cache_attention_q4_workspace_bytes(d, r->B) || (!workspace && dsn_cache_attention_q4_workspace_bytes(d, r->B)))
+    return DSN_ERR_WORKSPACE;
+  if (r->B == 0) return DSN_OK;
+  CacheAttParams p;
+  memset(&p, 0, sizeof(p));
+  fill_cache_routing(p, d, r);
+  p.n_pages = d->n_pages; p.max_pages = d->max_pages; p.window = d->window;
+  p.scale_log2 = (float)((d->scale != 0.f ? (double)d->scale : 1.0 / sqrt((double)d->D_h)) * 1.4426950408889634);
+  p.table = c->table; p.lengths = c->lengths; p.placed = c->placed; p.pages = c->pages;
+  p.qkv = static_cast<const __nv_bfloat16*>(qkv); p.ld_qkv = d->ld_qkv;
+  p.out = static_cast<__nv_bfloat16*>(out); p.ld_out = d->ld_out;
+  p.status = ctx->d_status;
+  count_launch(ctx, &dsn_stats::launches_cache_attention);
+  return dsn_launch_cache_attention(p, d->D_h, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }
 
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L) {

@@ -1,0 +1,256 @@
+// 4-bit cache of keys and values: which pages and slots the new tokens of a batch take (plan), and the write that rounds k and v into them.
+#include "dsn_cache.cuh"
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ plan
+// One cluster of CTAs; every CTA scans all requests on its own (8 bytes each), 1024 at a time, one a thread, and then the warps of the cluster share
+// the slots, a piece of a request's rows at a time.  A slot needs no other thread's result: a token's page stands in the table already or
+// is the ring's entry at a place that the scan gives.  What a CTA of the cluster still has to read (lengths, ring counters) is overwritten only behind the
+// cluster's barrier.  Pages taken and pages returned are different entries of the ring, so those need no order.
+constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
+constexpr int kPlanRows = 128;   // rows of a request that a warp does at a time
+
+struct PlanRequest {
+  int32_t held, placed;   // placed < 0: the request ends
+  uint32_t start;         // new pages of the requests before it; or returned pages of the requests before it
+};
+
+__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_constant__ CachePlanParams p) {
+  __shared__ PlanRequest s_req[kPlanThreads];
+  __shared__ unsigned long long s_warp[kPlanWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x, ranks = gridDim.x;   // the grid is one cluster
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const uint32_t N = (uint32_t)p.n_pages;
+  const uint32_t first = (uint32_t)p.pool_state[0] % N;
+  const uint32_t avail = min((uint32_t)max(p.pool_state[1], 0), N);
+  const int64_t room = (int64_t)p.max_pages * p.page;
+  uint32_t asked = 0, used = 0, returned = 0;   // pages: asked for, taken, given back by the requests before this chunk
+  const int segs = (p.R + kPlanRows - 1) / kPlanRows;
+  for (int base = 0; base < p.B; base += kPlanThreads) {
+    const int i = base + tid;
+    int held = 0, n = 0, have = 0, need = 0;
+    bool end = false;
+    if (i < p.B) {
+      held = p.lengths[i];
+      n = p.new_tokens[i];
+      if (held < 0 || held > room || n < -1 || n > p.R) {
+        if (rank == 0) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, i);
+        n = 0;
+        held = held < 0 ? 0 : held;   // no page is asked for or returned; no row is placed
+      } else {
+        have = (int)dsn_div((uint32_t)(held + p.page - 1), p.by_page);
+        end = n < 0;
+        if (!end) need = (int)dsn_div((uint32_t)(held + n + p.page - 1), p.by_page) - have;
+      }
+    }
+    bool fits = have + need <= p.max_pages;
+    const bool room_short = !fits;
+    if (room_short) need = 0;
+    // one scan for both sums: pages asked for in the low half, pages returned in the high half
+    unsigned long long v = (unsigned long long)(uint32_t)need | ((unsigned long long)(uint32_t)(end ? have : 0) << 32);
+    unsigned long long incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    __syncthreads();   // the chunk before is done with s_req and s_warp
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    unsigned long long before = 0, total = 0;
+#pragma unroll 8
+    for (int w = 0; w < kPlanWarps; ++w) {
+      const unsigned long long u = s_warp[w];
+      if (w < warp) before += u;
+      total += u;
+    }
+    incl += before;
+    const uint32_t upto = asked + (uint32_t)incl;
+    if (need > 0 && upto > avail) fits = false;
+    if (i < p.B) {
+      const bool ok = fits || end;
+      if (!ok && rank == 0) dsn_set_status(p.status, DSN_ERR_CACHE_FULL, i);
+      const int placed = end ? -1 : (ok ? n : 0);
+      s_req[tid] = PlanRequest{held, placed, end ? returned + (uint32_t)(incl >> 32) - (uint32_t)have : upto - (uint32_t)need};
+      if (rank == 0) p.placed[i] = placed > 0 ? placed : 0;
+    }
+    // served requests are those up to a point (and those that need nothing), so what they take is the largest sum that fits
+    {
+      const uint32_t mine = i < p.B && need > 0 && fits ? upto : 0u;
+      const uint32_t top = __reduce_max_sync(0xffffffffu, mine);
+      __syncthreads();
+      if (lane == 0) s_warp[warp] = top;
+      __syncthreads();
+      for (int w = 0; w < kPlanWarps; ++w) used = max(used, (uint32_t)s_warp[w]);
+    }
+    asked += (uint32_t)total;
+    returned += (uint32_t)(total >> 32);
+    // slots and table entries, a warp a piece
+    const int count = min(kPlanThreads, p.B - base);
+    for (int64_t it = (int64_t)rank * kPlanWarps + warp; it < (int64_t)count * segs; it += (int64_t)ranks * kPlanWarps) {
+      const int k = (int)(it / segs), seg = (int)(it - (int64_t)k * segs);
+      const PlanRequest q = s_req[k];
+      const int64_t row = (int64_t)(base + k) * p.max_pages;
+      const int have_k = (int)dsn_div((uint32_t)(q.held + p.page - 1), p.by_page);
+      int32_t* slots = p.slots + (int64_t)(base + k) * p.R;
+#pragma unroll
+      for (int j = 0; j < kPlanRows / 32; ++j) {
+        const int r = seg * kPlanRows + j * 32 + lane;
+        if (r >= p.R) break;
+        int slot = -1;
+        if (r < q.placed) {
+          const int pos = q.held + r;
+          const int col = (int)dsn_div((uint32_t)pos, p.by_page), at = pos - col * p.page;
+          int pg;
+          if (col < have_k) {
+            pg = p.table[row + col];
+          } else {
+            const uint32_t e = (first + q.start + (uint32_t)(col - have_k)) % N;
+            pg = p.pool[e];
+            if (at == 0) p.table[row + col] = pg;
+          }
+          slot = pg < 0 || pg >= p.n_pages ? -1 : pg * p.page + at;
+        }
+        slots[r] = slot;
+      }
+      if (q.placed < 0 && seg == 0)
+        for (int j = lane; j < have_k; j += 32) p.pool[(first + avail + q.start + (uint32_t)j) % N] = p.table[row + j];
+    }
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (rank == 0) {
+    for (int i = tid; i < p.B; i += kPlanThreads) {
+      const int held = p.lengths[i], n = p.new_tokens[i];
+      const bool end = n == -1 && held >= 0 && held <= room;
+      p.lengths_out[i] = end ? 0 : held + p.placed[i];   // placed[i] is this thread's own write
+    }
+    if (tid == 0) {
+      p.pool_state_out[0] = (int32_t)((first + used) % N);
+      p.pool_state_out[1] = (int32_t)min(avail - used + returned, N);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) cache_reset_kernel(int32_t B, int32_t n_pages, int32_t* lengths, int32_t* pool, int32_t* pool_state) {
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const int64_t n = max(B, n_pages);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    if (i < B) lengths[i] = 0;
+    if (i < n_pages) pool[i] = (int32_t)i;
+    if (i == 0) {
+      pool_state[0] = 0;
+      pool_state[1] = n_pages;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ write
+// A lane takes eight elements: 8 lanes a group of 64, 2 D / 8 lanes the k and v of a head, which lie side by side in the row.
+template <int D>
+__global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
+  constexpr int LPH = D / 4;             // lanes a head
+  constexpr int HPW = 32 / LPH;          // heads a warp does at a time
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int head_chunks = (p.max_heads + HPW - 1) / HPW;
+  const int64_t items = (int64_t)p.B * p.R * head_chunks;
+  const int64_t warps = (int64_t)gridDim.x * 8;
+  for (int64_t it = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); it < items; it += warps) {
+    const uint32_t row = (uint32_t)(it / head_chunks);
+    const int hc = (int)(it - (int64_t)row * head_chunks);
+    const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
+    const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
+    if (at.slice < 0 || at.sample >= p.B) continue;
+    const int slot = p.slots[(int64_t)at.sample * p.R + r];
+    if (slot == -1) continue;
+    if (slot < 0 || slot >= p.n_slots) {
+      if (lane == 0) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, (int)row);
+      continue;
+    }
+    const int head = hc * HPW + lane / LPH, sub = lane % LPH;
+    const bool live = head < p.heads[at.slice];
+    const int64_t xrow = (int64_t)(p.grouped ? pos : at.sample) * p.R + r;
+    float x[8];
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (live) raw = *reinterpret_cast<const uint4*>(p.qkv + xrow * p.ld_qkv + ((int64_t)head * (p.group + 2) + p.group) * D + sub * 8);
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(w[j] << 16);
+      x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+    bool bad = false;
+    float lo = x[0], hi = x[0];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      bad |= (__float_as_uint(x[j]) & 0x7f800000u) == 0x7f800000u;
+      lo = fminf(lo, x[j]);
+      hi = fmaxf(hi, x[j]);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    const uint32_t all = __ballot_sync(0xffffffffu, bad);
+    const bool poison = (LPH == 32 ? all : (all >> (lane & 16)) & 0xffffu) != 0;
+    const float fifteenth = 1.0f / 15.0f;
+    float s = __bfloat162float(__float2bfloat16_rn(__fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))));
+    if (s < 1.17549435e-38f) s = 0.f;
+    float z = __bfloat162float(__float2bfloat16_rn(2.f * __fadd_rn(0.5f * lo, 4.f * s)));
+    const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+    if (poison) {
+      s = 0.f;
+      z = __uint_as_float(0x7fc00000u);
+    }
+    uint32_t code = 0;
+    uint32_t val[4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      int c = __float2int_rn(__fmul_rn(__fsub_rn(x[j], z), inv)) + 8;
+      c = s > 0.f ? min(max(c, 0), 15) : 8;
+      code |= (uint32_t)c << (4 * j);
+      const float v = fmaf(s, (float)(c - 8), z);
+      const uint32_t h = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+      val[j >> 1] = j & 1 ? val[j >> 1] | (h << 16) : h;
+    }
+    if (!live) continue;
+    const int pg = (int)dsn_div((uint32_t)slot, p.by_page), tok = slot - pg * p.page;
+    const int half = sub / (D / 8), grp = (sub % (D / 8)) >> 3, word = sub & 7;
+    uint8_t* blk = p.pages + (((int64_t)pg * p.H + head) * (p.page / DSN_CACHE_BLOCK) + tok / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D) +
+                   half * (dsn_cache_block_bytes(D) / 2);
+    const int t = tok % DSN_CACHE_BLOCK;
+    *reinterpret_cast<uint32_t*>(blk + (grp * DSN_CACHE_BLOCK + t) * 32 + word * 4) = code;
+    if (word == 0)
+      *reinterpret_cast<uint32_t*>(blk + D / 64 * DSN_CACHE_BLOCK * 32 + (grp * DSN_CACHE_BLOCK + t) * 4) =
+          (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xffff0000u);
+    if (p.values)
+      *reinterpret_cast<uint4*>(p.values + xrow * p.ld_values + (int64_t)head * 2 * D + sub * 8) = make_uint4(val[0], val[1], val[2], val[3]);
+  }
+}
+
+}  // namespace
+
+cudaError_t dsn_launch_cache_plan(const CachePlanParams& p, cudaStream_t s) {
+  const int ranks = (int64_t)p.B * p.R > 4096 ? 8 : 1;   // portable cluster size
+  return dsn_launch(cache_plan_kernel, dim3((unsigned)ranks), dim3(kPlanThreads), 0, s, ranks, p);
+}
+
+cudaError_t dsn_launch_cache_reset(int32_t B, int32_t n_pages, int32_t* lengths, int32_t* pool, int32_t* pool_state, cudaStream_t s) {
+  const int64_t n = B > n_pages ? B : n_pages;
+  const int64_t ctas = (n + 255) / 256;
+  return dsn_launch(cache_reset_kernel, dim3((unsigned)(ctas < 592 ? ctas : 592)), dim3(256), 0, s, 1, B, n_pages, lengths, pool, pool_state);
+}
+
+cudaError_t dsn_launch_cache_write(const CacheWriteParams& p, int sm_count, cudaStream_t s) {
+  const int hpw = p.D == 64 ? 2 : 1;
+  const int64_t items = (int64_t)p.B * p.R * ((p.max_heads + hpw - 1) / hpw), ctas = (items + 7) / 8;
+  const int64_t most = (int64_t)sm_count * 8;
+  const dim3 grid((unsigned)(ctas < most ? ctas : most));
+  return p.D == 64 ? dsn_launch(cache_write_kernel<64>, grid, dim3(256), 0, s, 1, p) : dsn_launch(cache_write_kernel<128>, grid, dim3(256), 0, s, 1, p);
+}
