@@ -1511,7 +1511,7 @@ int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c
 
 size_t dsn_cache_attention_q4_workspace_bytes(const dsn_cache_desc* d, int32_t B) {
   if (check_cache_desc(d) || B < 0) return 0;
-  return 0;
+  return (int64_t)d->R * d->group <= DSN_CACHE_FEW ? dsn_cache_attention_ws_bytes(d->D_h, d->R * d->group, B) : 0;
 }
 
 int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* out,
@@ -1524,9 +1524,9 @@ int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cach
   if (!e) e = check_rows(out, d->ld_out, (int64_t)d->H * d->group * d->D_h, 2);
   if (e) return e;
   if (workspace && !aligned16(workspace)) return DSN_ERR_ALIGNMENT;
-  if (ws_bytes < dsn_cache_attention_q4_workspace_bytes(d, r->B) || (!workspace && dsn_cache_attention_q4_workspace_bytes(d, r->B)))
-    return DSN_ERR_WORKSPACE;
   if (r->B == 0) return DSN_OK;
+  const size_t need = dsn_cache_attention_q4_workspace_bytes(d, r->B);
+  if (need && (!workspace || ws_bytes < need)) return DSN_ERR_WORKSPACE;
   CacheAttParams p;
   memset(&p, 0, sizeof(p));
   fill_cache_routing(p, d, r);
@@ -1536,8 +1536,12 @@ int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cach
   p.qkv = static_cast<const __nv_bfloat16*>(qkv); p.ld_qkv = d->ld_qkv;
   p.out = static_cast<__nv_bfloat16*>(out); p.ld_out = d->ld_out;
   p.status = ctx->d_status;
+  if ((int64_t)d->R * d->group <= DSN_CACHE_FEW) {
+    count_launch(ctx, &dsn_stats::launches_cache_attention, 2);
+    return dsn_launch_cache_attention(p, d->D_h, ctx->sm_count, workspace, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+  }
   count_launch(ctx, &dsn_stats::launches_cache_attention);
-  return dsn_launch_cache_attention(p, d->D_h, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+  return dsn_launch_cache_attention_rows(p, d->D_h, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
 }
 
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L) {

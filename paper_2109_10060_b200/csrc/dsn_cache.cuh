@@ -42,6 +42,21 @@ struct CacheWriteParams {
 };
 cudaError_t dsn_launch_cache_write(const CacheWriteParams& p, int sm_count, cudaStream_t s);
 
+// A request of the line of steps.
+struct __align__(16) CacheEntry {
+  int64_t first;       // its first step in the line
+  int32_t sample, pos;
+  int32_t heads, steps, len, rows;
+};
+// What a warp (in shared memory) or a CTA (in the workspace) has to say about the items at the ends of its stretch.
+struct __align__(16) CachePart {
+  int32_t head_state;  // 0: the stretch begins with an item of its own; 1: an earlier one's item ends here; 2: all of it lies inside one item; 3: it is empty
+  int32_t tail;        // 1: its last item began here and goes on
+  int32_t sample, pos, head, rows;   // of that last item
+  int32_t head_far;    // (warp) the first item's part is in the workspace, not in the warp's ring
+  int32_t pad;
+};
+
 struct CacheAttParams {
   int16_t heads[DSN_MAX_SLICES];
   int32_t B, R, H, group, G, T, page, n_pages, max_pages, max_heads, grouped, window;
@@ -59,5 +74,14 @@ struct CacheAttParams {
   int64_t ld_out;
   const uint8_t* pages;
   int32_t* status;
+  // in the workspace
+  CachePart* parts;      // [CTAs]
+  CacheEntry* list;      // [B]
+  float* warp_data;
+  float* cta_data;
 };
-cudaError_t dsn_launch_cache_attention(const CacheAttParams& p, int D, int sm_count, cudaStream_t s);
+#define DSN_CACHE_MAX_CTAS 148   // a B200's SMs: the workspace query has no context to ask
+#define DSN_CACHE_FEW 16         // query vectors of a head (rows * group) up to which the form for a few of them runs
+size_t dsn_cache_attention_ws_bytes(int D, int cols, int64_t B);
+cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s);
+cudaError_t dsn_launch_cache_attention_rows(const CacheAttParams& p, int D, int sm_count, cudaStream_t s);

@@ -1,106 +1,692 @@
-// Attention over the 4-bit cache.
+// Attention over the 4-bit cache, a few query vectors a head (rows * group <= 16: single tokens, shared heads, a few tokens at once).
+//
+// Bound by memory: a cached token is 18 D / 16 bytes a head, read once for all query vectors of the head.  Work is dealt out in steps of 32 tokens:
+// all steps of all (request, head) items stand in one line, and every warp of the GPU gets an equal stretch of it, so neither few long requests nor
+// many short ones leave SMs idle.  A warp keeps the steps to come in flight as bulk copies into a ring of its own (no barrier with other
+// warps), a block of 16 tokens a copy, as pages may end after any block.
+// An item that lies in one warp's stretch is finished there; of an item that is cut, each warp leaves its maximum, sum and products (fp32) in the
+// workspace, and a second small kernel joins them.
+//
+// Products on the tensor cores, with the tokens as rows: S^T = K Q^T (16 tokens x 8 queries x 16 elements an instruction), O^T = V^T P^T.
+//   Codes become bf16 numbers 128 + code with one mask each; for K the 128 + 8 is taken off by starting the accumulator at -136 sum(q), which costs
+//   nothing, and scale and middle of a token's group are applied to the sum in fp32: the scores are as exact as fp32 sums.
+//   For V the 136 is subtracted (a sum over thousands of tokens would lose bits to it), the scale goes into the probability before its
+//   one rounding to bf16, the middle into a sum of its own in fp32.
+// The order of elements in a product is free, so a lane takes whole words: 16 elements of K in 8 bytes, 8 elements of V in 4.  Row i of a block's K is token
+// i ^ (i >> 2 & 1): then neither K's rows nor the pairs of tokens that a lane needs of V meet in a bank.
+// The maximum is a reference that moves only when a score stands more than 2^8 above it (one vote a step instead of a reduction).
 #include "dsn_cache.cuh"
 
 namespace {
 
-// One warp a query vector; 32 keys at a time, a lane a key for the scores, a lane D / 32 elements for the values.
+using dsn_gemm::smem_u32;
+
+constexpr int kStepBlocks = 2, kStepTokens = 32;
+constexpr int kListSmem = 64;      // items' requests that a CTA keeps in shared memory; further ones are read from the workspace
+constexpr uint32_t kCtrl = 2048;  // behind the list: sums of a scan, the abort flag, what the warps say about their ends
+constexpr float kLowest = -1e38f;  // reference before any score: finite, so that differences are
+constexpr float kSlack = 8.f;
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t nibbles(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }   // 128 + code, twice
+__device__ __forceinline__ uint32_t minus136(uint32_t w) {
+  uint32_t r;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x43084308u));
+  return r;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// First token that the item's rows can see, rounded down to a block, and one behind the last.
+__device__ __forceinline__ void item_range(int len, int rows, int window, int& lo, int& hi) {
+  const int first = len - rows;                                // token of the first row
+  hi = len;
+  lo = window ? max(0, first - window + 1) & ~(DSN_CACHE_BLOCK - 1) : 0;
+}
+
+template <int THREADS>
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* s_warp, uint64_t& total) {   // exclusive
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t u = __shfl_up_sync(0xffffffffu, (unsigned long long)incl, o);
+    if (lane >= o) incl += u;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  uint64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const uint64_t u = s_warp[w];
+    if (w < warp) before += u;
+    total += u;
+  }
+  return before + incl - v;
+}
+
+// One request's place in the line: what it needs to know and how many steps its heads make.
+__device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, bool report) {
+  const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
+  CacheEntry e;
+  e.first = 0;
+  e.sample = at.sample; e.pos = pos; e.heads = 0; e.steps = 0; e.len = 0; e.rows = 0;
+  if (pos >= p.B || at.slice < 0 || at.sample >= p.B) return e;
+  const int most = p.max_pages * p.page;
+  const int len = p.lengths[at.sample], rows = p.placed ? p.placed[at.sample] : p.R;
+  e.len = min(max(len, 0), most);
+  e.rows = min(max(rows, 0), p.R);
+  if (report && (len != e.len || rows != e.rows)) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
+  if (e.rows == 0) return e;
+  int lo, hi;
+  item_range(e.len, e.rows, p.window, lo, hi);
+  e.heads = p.heads[at.slice];
+  e.steps = max(1, (hi - lo + kStepTokens - 1) / kStepTokens);   // a request without tokens: a step that sees nothing, for the zeros
+  return e;
+}
+
+// A walk along the line.
+struct Walk {
+  const CacheEntry* smem;
+  const CacheEntry* more;   // the CTA's entries in the workspace
+  int j;                    // entry
+  int head, step;
+  CacheEntry e;
+  __device__ __forceinline__ void load(int i) {
+    j = i;
+    e = i < kListSmem ? smem[i] : more[i];
+  }
+  __device__ __forceinline__ void advance() {
+    if (++step == e.steps) {
+      step = 0;
+      if (++head == e.heads) {
+        head = 0;
+        load(j + 1);
+      }
+    }
+  }
+};
+
 template <int D>
-__global__ void __launch_bounds__(128) cache_attention_simple(const __grid_constant__ CacheAttParams p) {
-  constexpr int E = D / 32;
-  __shared__ float s_q[4][D];
+__host__ __device__ constexpr uint32_t step_bytes() { return kStepBlocks * dsn_cache_block_bytes(D); }
+template <int D, int WARPS, int DEPTH>
+constexpr size_t attention_smem() { return kCtrl + kListSmem * sizeof(CacheEntry) + WARPS * DEPTH * 8 + (size_t)WARPS * DEPTH * step_bytes<D>(); }
+
+template <int D, int NT, int WARPS, int DEPTH>
+__global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __grid_constant__ CacheAttParams p) {
+  constexpr int THREADS = WARPS * 32, GR = D / 64, NC = 8 * NT;
+  constexpr int kPart = NC * (D + 2);   // floats of a part: references, sums, products
+  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kHalf = kBlock / 2, kPairs = GR * 512;
+  extern __shared__ __align__(128) uint8_t smem[];
+  CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem);
+  uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + kListSmem * sizeof(CacheEntry));
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + kListSmem * sizeof(CacheEntry) + 512);
+  const uint32_t base = smem_u32(smem) + (uint32_t)(kListSmem * sizeof(CacheEntry)) + kCtrl;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t ring = base + (uint32_t)(warp * DEPTH) * step_bytes<D>();
+  const uint32_t bars = base + (uint32_t)(WARPS * DEPTH) * step_bytes<D>() + (uint32_t)(warp * DEPTH) * 8u;
+
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t per_row = (int64_t)p.max_heads * p.group, items = (int64_t)p.B * p.R * per_row;
-  const uint32_t block = dsn_cache_block_bytes(D);
-  for (int64_t it = (int64_t)blockIdx.x * 4 + warp; it < items; it += (int64_t)gridDim.x * 4) {
-    const int64_t row = it / per_row;
-    const int vec = (int)(it - row * per_row), head = vec / p.group, e = vec - head * p.group;
-    const int pos = (int)(row / p.R), r = (int)(row - (int64_t)pos * p.R);
-    const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
-    if (at.slice < 0 || at.sample >= p.B || head >= p.heads[at.slice]) continue;
-    const int most = p.max_pages * p.page;
-    const int len_in = p.lengths[at.sample], n_in = p.placed ? p.placed[at.sample] : p.R;
-    const int L = min(max(len_in, 0), most), n = min(max(n_in, 0), p.R);
-    if ((L != len_in || n != n_in) && lane == 0) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
-    if (r >= n) continue;
-    const int64_t xrow = (int64_t)(p.grouped ? pos : at.sample) * p.R + r;
-    const __nv_bfloat16* q = p.qkv + xrow * p.ld_qkv + ((int64_t)head * (p.group + 2) + e) * D;
-    __syncwarp();
-    for (int j = lane; j < D; j += 32) s_q[warp][j] = __bfloat162float(q[j]);
-    __syncwarp();
-    const int me = L - n + r;                                   // this query's token
-    const int lo = p.window ? max(0, me - p.window + 1) : 0;
-    float m = -INFINITY, l = 0.f, o[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) o[j] = 0.f;
-    for (int k0 = lo & ~15; k0 <= me; k0 += 32) {
-      const int key = k0 + lane;
-      const int col = key / p.page;
-      const int pg = key <= me ? p.table[(int64_t)at.sample * p.max_pages + col] : 0;
-      bool seen = key >= lo && key <= me;
-      if (seen && (pg < 0 || pg >= p.n_pages)) {
-        dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
-        seen = false;
+  if (tid == 0) *abort_flag = 0;
+  if (lane == 0) {
+    for (int i = 0; i < DEPTH; ++i) dsn_gemm::mbar_init(bars + 8u * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+
+  // ---- the line: how long it is, this CTA's stretch, the requests in it
+  __shared__ int s_first_order, s_count;
+  if (tid == 0) s_first_order = 0, s_count = 0;
+  const CacheEntry e0 = look_up(p, tid, blockIdx.x == 0);
+  uint64_t sum0, ones0, total;
+  const uint64_t first0 = block_scan<THREADS>((uint64_t)e0.heads * e0.steps, s_scan, sum0);
+  const uint64_t order0 = block_scan<THREADS>(e0.heads > 0, s_scan, ones0);
+  total = sum0;
+  for (int b = THREADS; b < p.B; b += THREADS) {
+    uint64_t sum;
+    const CacheEntry e = look_up(p, b + tid, blockIdx.x == 0);
+    block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
+    total += sum;
+  }
+  const uint64_t A = total * blockIdx.x / gridDim.x, Z = total * (blockIdx.x + 1) / gridDim.x;
+  {
+    uint64_t at_first = 0, at_order = 0;
+    for (int b = 0; b < p.B; b += THREADS) {
+      CacheEntry e = e0;
+      uint64_t first = first0, order = order0, sum = sum0, ones = ones0;
+      if (b > 0) {
+        e = look_up(p, b + tid, false);
+        first = at_first + block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
+        order = at_order + block_scan<THREADS>(e.heads > 0, s_scan, ones);
       }
-      const int tok = key - col * p.page;
-      const uint8_t* blk = p.pages + (((int64_t)(seen ? pg : 0) * p.H + head) * (p.page / 16) + (seen ? tok / 16 : 0)) * block;
-      const int t = tok & 15;
-      float sc = -INFINITY;
-      if (seen) {
-        sc = 0.f;
-        for (int g = 0; g < D / 64; ++g) {
-          const uint32_t pr = *reinterpret_cast<const uint32_t*>(blk + D / 64 * 512 + (g * 16 + t) * 4);
-          float dot = 0.f, sum = 0.f;
-          for (int w = 0; w < 8; ++w) {
-            const uint32_t c = *reinterpret_cast<const uint32_t*>(blk + (g * 16 + t) * 32 + w * 4);
-            for (int j = 0; j < 8; ++j) {
-              const float qv = s_q[warp][g * 64 + w * 8 + j];
-              dot = fmaf(qv, (float)((int)((c >> (4 * j)) & 15) - 8), dot);
-              sum += qv;
-            }
+      at_first += sum;
+      at_order += ones;
+      const bool here = e.heads > 0 && first < Z && first + (uint64_t)e.heads * e.steps > A;
+      if (here && first <= A) s_first_order = (int)order;   // one thread of all: the request that holds step A
+      __syncthreads();
+      if (here) {
+        const int i = (int)order - s_first_order;
+        e.first = (int64_t)first;
+        if (i < kListSmem) s_list[i] = e; else p.list[order] = e;
+        atomicMax(&s_count, i + 1);
+      }
+      __syncthreads();
+    }
+  }
+  const uint64_t u0 = A + (Z - A) * warp / WARPS, u1 = A + (Z - A) * (warp + 1) / WARPS;
+  int head_state = 3, tail = 0, head_far = 0;
+  Walk work;
+  if (u0 < u1) {
+  Walk fetch;
+  fetch.smem = s_list;
+  fetch.more = p.list + s_first_order;
+  {   // the last request that begins at or before u0
+    const int count = s_count;
+    int j = 0;
+    for (int b = 0; b < count; b += 32) {
+      const int i = b + lane;
+      const bool le = i < count && (uint64_t)(i < kListSmem ? s_list[i].first : fetch.more[i].first) <= u0;
+      const uint32_t m = __ballot_sync(0xffffffffu, le);
+      if (m) j = b + 31 - __clz(m);
+      if (m != 0xffffffffu) break;
+    }
+    fetch.load(j);
+    const uint64_t off = u0 - (uint64_t)fetch.e.first;
+    fetch.head = (int)(off / (uint32_t)fetch.e.steps);
+    fetch.step = (int)(off - (uint64_t)fetch.head * fetch.e.steps);
+  }
+  work = fetch;
+  const int n_steps = (int)(u1 - u0);
+  const int bpp = p.page / DSN_CACHE_BLOCK;   // blocks a page
+
+  // copies of one step into a slot; bit b of the result: block b is there
+  auto issue = [&](int slot) -> uint32_t {
+    int lo, hi;
+    item_range(fetch.e.len, fetch.e.rows, p.window, lo, hi);
+    const int tok = lo + fetch.step * kStepTokens + lane * DSN_CACHE_BLOCK;
+    bool ok = lane < kStepBlocks && tok < hi;
+    const uint8_t* src = nullptr;
+    if (ok) {
+      const int blk = tok / DSN_CACHE_BLOCK, col = (int)dsn_div((uint32_t)tok, p.by_page);
+      const int pg = p.table[(int64_t)fetch.e.sample * p.max_pages + col];
+      if (pg < 0 || pg >= p.n_pages) {
+        dsn_set_status(p.status, DSN_ERR_BAD_INDEX, fetch.e.sample);
+        ok = false;
+      }
+      src = p.pages + (((int64_t)pg * p.H + fetch.head) * bpp + (blk - col * bpp)) * kBlock;
+    }
+    const uint32_t there = __ballot_sync(0xffffffffu, ok);
+    if (lane == 0) dsn_gemm::mbar_expect_tx(bars + 8u * slot, (uint32_t)__popc(there) * kBlock);
+    __syncwarp();
+    if (ok) dsn_bulk_load(ring + (uint32_t)slot * step_bytes<D>() + (uint32_t)lane * kBlock, src, kBlock, bars + 8u * slot);
+    return there;
+  };
+
+  int asked = 0;
+  uint32_t there = 0;   // two bits a slot
+  for (; asked < DEPTH && asked < n_steps; ++asked) {
+    there |= issue(asked) << (2 * asked);
+    if (asked + 1 < n_steps) fetch.advance();
+  }
+
+  uint32_t qf[NT][GR][4][2];
+  float qsum[NT][GR][2];
+  float o[NT][GR][4][4], oz[NT][GR][2], l[NT][2], mref[NT][2];
+  bool fresh = true, ok = true;
+  bool head_open = work.step != 0;   // the first item began in an earlier warp's stretch
+  head_state = 0;
+  int row_of[NT][2];   // rows of this lane's columns
+  const int kap = g ^ (g >> 2);      // token of K's row g in a block
+  uint32_t slot = 0, parity = 0;
+
+  for (int i = 0; i < n_steps; ++i) {
+    const CacheEntry& e = work.e;
+    const int cols = e.rows * p.group;
+    const int64_t row0 = (int64_t)(p.grouped ? e.pos : e.sample) * p.R;
+    if (fresh) {
+      fresh = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int v = nt * 8 + g, r = v / p.group, ev = v - r * p.group;
+        const __nv_bfloat16* q = p.qkv + (row0 + r) * p.ld_qkv + ((int64_t)work.head * (p.group + 2) + ev) * D;
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr) {
+          float sum = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (v < cols) w = *reinterpret_cast<const uint4*>(q + gr * 64 + 16 * t + 8 * h);
+            sum += ((lo_bf16(w.x) + hi_bf16(w.x)) + (lo_bf16(w.y) + hi_bf16(w.y))) + ((lo_bf16(w.z) + hi_bf16(w.z)) + (lo_bf16(w.w) + hi_bf16(w.w)));
+            qf[nt][gr][2 * h][0] = __byte_perm(w.x, w.z, 0x5410);
+            qf[nt][gr][2 * h][1] = __byte_perm(w.x, w.z, 0x7632);
+            qf[nt][gr][2 * h + 1][0] = __byte_perm(w.y, w.w, 0x5410);
+            qf[nt][gr][2 * h + 1][1] = __byte_perm(w.y, w.w, 0x7632);
           }
-          sc += dot * __uint_as_float(pr << 16) + sum * __uint_as_float(pr & 0xffff0000u);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          qsum[nt][gr][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+          qsum[nt][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+          oz[nt][gr][0] = oz[nt][gr][1] = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[nt][gr][mt][x] = 0.f;
         }
-        sc *= p.scale_log2;
+        l[nt][0] = l[nt][1] = 0.f;
+        mref[nt][0] = mref[nt][1] = kLowest;
+        row_of[nt][0] = (nt * 8 + 2 * t) / p.group;
+        row_of[nt][1] = (nt * 8 + 2 * t + 1) / p.group;
       }
-      float mx = sc;
-      for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-      const float m2 = fmaxf(m, mx);
-      const float pr = seen ? exp2f(sc - (m2 == -INFINITY ? 0.f : m2)) : 0.f;
-      const float keep = m2 == -INFINITY ? 1.f : exp2f(m - m2);
-      m = m2;
-      l = l * keep + pr;
+    }
+    int lo, hi;
+    item_range(e.len, e.rows, p.window, lo, hi);
+    const int tok0 = lo + work.step * kStepTokens;
+    const uint32_t here = (there >> (2 * slot)) & 3u;
+    // all tokens of the step seen by all rows?
+    const int first_tok = e.len - e.rows;
+    const bool plain = here == 3u && tok0 + kStepTokens <= first_tok + 1 && (p.window == 0 || tok0 > e.len - 1 - p.window);
+    ok = dsn_wait(bars + 8u * slot, parity, abort_flag, p.status, 71);
+    if (!ok) break;
+    const uint32_t st = ring + slot * step_bytes<D>();
+
+    float s[kStepBlocks][NT][4];
+    uint32_t vpair[kStepBlocks][GR][2];
 #pragma unroll
-      for (int j = 0; j < E; ++j) o[j] *= keep;
-      for (int i = 0; i < 32; ++i) {
-        const float pi = __shfl_sync(0xffffffffu, pr, i);
-        const uint64_t bi = __shfl_sync(0xffffffffu, (unsigned long long)reinterpret_cast<uint64_t>(blk), i);
-        const int ti = __shfl_sync(0xffffffffu, t, i);
-        if (!__shfl_sync(0xffffffffu, (int)seen, i)) continue;
-        const uint8_t* v = reinterpret_cast<const uint8_t*>(bi) + block / 2;
-        const int d0 = lane * E, g = d0 / 64;
-        const uint32_t prm = *reinterpret_cast<const uint32_t*>(v + D / 64 * 512 + (g * 16 + ti) * 4);
+    for (int b = 0; b < kStepBlocks; ++b) {
+      const uint32_t blk = st + b * kBlock;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const int d = d0 + j - g * 64;
-          const int c = (v[(g * 16 + ti) * 32 + d / 2] >> (4 * (d & 1))) & 15;
-          const float z = __uint_as_float(prm & 0xffff0000u), s = __uint_as_float(prm << 16);
-          o[j] = fmaf(pi, z == z ? fmaf(s, (float)(c - 8), z) : 0.f, o[j]);   // NaN tokens come through the scores
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[b][nt][x] = 0.f;
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+        const uint2 w0 = lds64(blk + gr * 512 + kap * 32 + t * 8), w1 = lds64(blk + gr * 512 + (kap + 8) * 32 + t * 8);
+        uint32_t k0 = lds32(blk + kPairs + gr * 64 + kap * 4), k1 = lds32(blk + kPairs + gr * 64 + (kap + 8) * 4);
+        vpair[b][gr][0] = lds32(blk + kHalf + kPairs + gr * 64 + kap * 4);
+        vpair[b][gr][1] = lds32(blk + kHalf + kPairs + gr * 64 + (kap + 8) * 4);
+        float acc[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          acc[nt][0] = acc[nt][2] = -136.f * qsum[nt][gr][0];
+          acc[nt][1] = acc[nt][3] = -136.f * qsum[nt][gr][1];
+        }
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          const uint32_t x0 = ks < 2 ? w0.x : w0.y, x1 = ks < 2 ? w1.x : w1.y;
+          const int sh = 8 * (ks & 1);
+          const uint32_t a[4] = {nibbles(x0 >> sh), nibbles(x1 >> sh), nibbles(x0 >> (sh + 4)), nibbles(x1 >> (sh + 4))};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt], a, qf[nt][gr][ks][0], qf[nt][gr][ks][1]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          s[b][nt][0] = fmaf(lo_bf16(k0), acc[nt][0], fmaf(hi_bf16(k0), qsum[nt][gr][0], s[b][nt][0]));
+          s[b][nt][1] = fmaf(lo_bf16(k0), acc[nt][1], fmaf(hi_bf16(k0), qsum[nt][gr][1], s[b][nt][1]));
+          s[b][nt][2] = fmaf(lo_bf16(k1), acc[nt][2], fmaf(hi_bf16(k1), qsum[nt][gr][0], s[b][nt][2]));
+          s[b][nt][3] = fmaf(lo_bf16(k1), acc[nt][3], fmaf(hi_bf16(k1), qsum[nt][gr][1], s[b][nt][3]));
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[b][nt][x] *= p.scale_log2;
+    }
+    if (!plain) {
+#pragma unroll
+      for (int b = 0; b < kStepBlocks; ++b) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const int key = tok0 + b * DSN_CACHE_BLOCK + kap + 8 * hf;
+          const bool exists = (here >> b & 1u) && key < hi;
+#pragma unroll
+          for (int gr = 0; gr < GR; ++gr) {   // nothing of a token that does not exist, no NaN of one that some row does not see
+            const uint32_t w = vpair[b][gr][hf];
+            if (!exists) vpair[b][gr][hf] = 0u;
+            else if (!(fabsf(hi_bf16(w)) <= 3.4e38f) || !(fabsf(lo_bf16(w)) <= 3.4e38f)) vpair[b][gr][hf] = 0u;
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int me = first_tok + row_of[nt][c];
+              const bool seen = exists && key <= me && (p.window == 0 || key > me - p.window);
+              if (!seen) s[b][nt][2 * hf + c] = -INFINITY;
+            }
         }
       }
     }
-    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    // a score far above its reference?
+    bool far = false;
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-      p.out[xrow * p.ld_out + ((int64_t)head * p.group + e) * D + lane * E + j] = __float2bfloat16_rn(l == 0.f ? 0.f : o[j] / l);
+    for (int b = 0; b < kStepBlocks; ++b)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) far |= s[b][nt][x] > mref[nt][x & 1] + kSlack;
+    if (__any_sync(0xffffffffu, far)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float m = mref[nt][c];
+#pragma unroll
+          for (int b = 0; b < kStepBlocks; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+          const float f = ex2(mref[nt][c] - m);
+          mref[nt][c] = m;
+          l[nt][c] *= f;
+#pragma unroll
+          for (int gr = 0; gr < GR; ++gr) {
+            oz[nt][gr][c] *= f;
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+              o[nt][gr][mt][c] *= f;
+              o[nt][gr][mt][2 + c] *= f;
+            }
+          }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < kStepBlocks; ++b)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          s[b][nt][x] = ex2(s[b][nt][x] - mref[nt][x & 1]);
+          l[nt][x & 1] += s[b][nt][x];
+        }
+#pragma unroll
+    for (int b = 0; b < kStepBlocks; ++b) {
+      const uint32_t blk = st + b * kBlock + kHalf;
+      const int ka = 2 * t + (t >> 1), kb = 2 * t + 1 - (t >> 1);   // tokens of columns 2 t and 2 t + 1
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const float sc = lo_bf16(vpair[b][gr][hf]), z = hi_bf16(vpair[b][gr][hf]);
+            const float p0 = s[b][nt][2 * hf], p1 = s[b][nt][2 * hf + 1];
+            oz[nt][gr][0] = fmaf(p0, z, oz[nt][gr][0]);
+            oz[nt][gr][1] = fmaf(p1, z, oz[nt][gr][1]);
+            pb[nt][hf] = transpose8x8(pack_bf16(p0 * sc, p1 * sc));
+          }
+        const uint32_t va = lds32(blk + gr * 512 + ka * 32 + g * 4), vb = lds32(blk + gr * 512 + kb * 32 + g * 4);
+        const uint32_t vc = lds32(blk + gr * 512 + (ka + 8) * 32 + g * 4), vd = lds32(blk + gr * 512 + (kb + 8) * 32 + g * 4);
+        const uint32_t l0 = __byte_perm(va, vb, 0x5410), h0 = __byte_perm(va, vb, 0x7632);
+        const uint32_t l1 = __byte_perm(vc, vd, 0x5410), h1 = __byte_perm(vc, vd, 0x7632);
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+          const uint32_t a[4] = {minus136(nibbles(l0 >> (4 * mt))), minus136(nibbles(h0 >> (4 * mt))), minus136(nibbles(l1 >> (4 * mt))),
+                                 minus136(nibbles(h1 >> (4 * mt)))};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][gr][mt], a, pb[nt][0], pb[nt][1]);
+        }
+      }
+    }
+    __syncwarp();   // every lane has read the slot
+    if (asked < n_steps) {
+      there = (there & ~(3u << (2 * slot))) | (issue(slot) << (2 * slot));
+      ++asked;
+      if (asked < n_steps) fetch.advance();
+    }
+    if (++slot == DEPTH) slot = 0, parity ^= 1u;
+
+    const bool item_ends = work.step + 1 == e.steps, last = i + 1 == n_steps;
+    if (item_ends || last) {
+      const bool whole = item_ends && !head_open;
+      if (!item_ends) {
+        if (head_open) head_state = 2; else tail = 1;
+      } else if (head_open) {
+        head_state = 1;
+      }
+      // the last thing that the warp does may use its ring; the first of more goes to the workspace
+      float* dst = last ? reinterpret_cast<float*>(smem + (ring - smem_u32(smem))) : p.warp_data + ((int64_t)blockIdx.x * WARPS + warp) * kPart;
+      if (!whole && head_open && !last) head_far = 1;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float sum = l[nt][c];
+          sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+          const int v = nt * 8 + 2 * t + c;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          const int r = row_of[nt][c], ev = v - r * p.group;
+#pragma unroll
+          for (int gr = 0; gr < GR; ++gr) {
+            float z = oz[nt][gr][c];
+            z += __shfl_xor_sync(0xffffffffu, z, 4);
+            z += __shfl_xor_sync(0xffffffffu, z, 8);
+            z += __shfl_xor_sync(0xffffffffu, z, 16);
+            float y[8];
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+              y[mt] = o[nt][gr][mt][c] + z;
+              y[mt + 4] = o[nt][gr][mt][2 + c] + z;
+            }
+            if (v < cols) {
+              if (whole) {
+                uint4 w;
+                w.x = pack_bf16(y[0] * inv, y[1] * inv);
+                w.y = pack_bf16(y[2] * inv, y[3] * inv);
+                w.z = pack_bf16(y[4] * inv, y[5] * inv);
+                w.w = pack_bf16(y[6] * inv, y[7] * inv);
+                *reinterpret_cast<uint4*>(p.out + (row0 + r) * p.ld_out + ((int64_t)work.head * p.group + ev) * D + gr * 64 + 8 * g) = w;
+              } else {
+                float4* d4 = reinterpret_cast<float4*>(dst + 2 * NC + v * D + gr * 64 + 8 * g);
+                d4[0] = make_float4(y[0], y[1], y[2], y[3]);
+                d4[1] = make_float4(y[4], y[5], y[6], y[7]);
+              }
+            }
+          }
+          if (!whole && v < cols && g == 0) {
+            dst[v] = mref[nt][c];
+            dst[NC + v] = sum;
+          }
+        }
+      head_open = false;
+      fresh = true;
+    }
+    if (!last) work.advance();
+  }
+  if (!ok) {
+    dsn_drain(bars, DEPTH, 0, asked);
+    head_state = 3;
+    tail = 0;
+  }
+  }
+
+  // ---- what the warps of the CTA cut among themselves
+  CachePart* s_part = reinterpret_cast<CachePart*>(s_scan + 128);
+  if (lane == 0) s_part[warp] = CachePart{head_state, tail, work.e.sample, work.e.pos, work.head, work.e.rows, head_far, 0};
+  __syncthreads();
+  auto part_of = [&](int w, bool of_tail) -> const float* {   // where a warp left a part
+    if (!of_tail && s_part[w].head_far) return p.warp_data + ((int64_t)blockIdx.x * WARPS + w) * kPart;
+    return reinterpret_cast<const float*>(smem + (base - smem_u32(smem)) + (size_t)w * DEPTH * step_bytes<D>());
+  };
+  int chain = 0;
+  int cta_head = 3, cta_tail = 0, tail_warp = 0;
+  for (int a = -1; a < WARPS; ++a) {
+    if (a >= 0) {
+      if (cta_head == 3 && s_part[a].head_state != 3) cta_head = 0;   // the first warp that has work begins with an item of its own
+      if (!s_part[a].tail) continue;
+    }
+    // the chain: the tail of warp a (a = -1: what came before this CTA), then heads up to the one that ends
+    int end = a, closed = 0, any = a >= 0;
+    for (int j = a + 1; j < WARPS; ++j) {
+      const int st = s_part[j].head_state;
+      if (st == 3) continue;
+      if (st == 0) break;
+      end = j;
+      any = 1;
+      if (st == 1) {
+        closed = 1;
+        break;
+      }
+    }
+    if (!any) continue;
+    if (a < 0) cta_head = closed ? 1 : 2;
+    else if (!closed) cta_tail = 1, tail_warp = a;
+    const int cols = a >= 0 ? s_part[a].rows * p.group : NC;
+    for (int v = 0; v < NC; ++v, ++chain) {
+      if (chain % WARPS != warp || v >= cols) continue;
+      float m = kLowest, sum = 0.f, y[D / 32];
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) y[x] = 0.f;
+#pragma unroll 4
+      for (int j = a; j <= end; ++j) {
+        if (j < 0 || (j != a && s_part[j].head_state == 3)) continue;
+        const float* src = part_of(j, j == a);
+        const float mj = src[v], lj = src[NC + v];
+        const float m2 = fmaxf(m, mj), fa = ex2(m - m2), fb = ex2(mj - m2);
+        m = m2;
+        sum = sum * fa + lj * fb;
+        if constexpr (D == 128) {
+          const float4 q = *reinterpret_cast<const float4*>(src + 2 * NC + v * D + 4 * lane);
+          y[0] = y[0] * fa + q.x * fb; y[1] = y[1] * fa + q.y * fb; y[2] = y[2] * fa + q.z * fb; y[3] = y[3] * fa + q.w * fb;
+        } else {
+          const float2 q = *reinterpret_cast<const float2*>(src + 2 * NC + v * D + 2 * lane);
+          y[0] = y[0] * fa + q.x * fb; y[1] = y[1] * fa + q.y * fb;
+        }
+      }
+      if (a >= 0 && closed) {
+        const CachePart& q = s_part[a];
+        const int r = v / p.group, ev = v - r * p.group;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? q.pos : q.sample) * p.R + r) * p.ld_out + ((int64_t)q.head * p.group + ev) * D;
+        if constexpr (D == 128)
+          *reinterpret_cast<uint2*>(dst + 4 * lane) = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
+        else
+          *reinterpret_cast<uint32_t*>(dst + 2 * lane) = pack_bf16(y[0] * inv, y[1] * inv);
+      } else {
+        float* dst = p.cta_data + ((int64_t)blockIdx.x * 2 + (a >= 0)) * kPart;
+        if (lane == 0) {
+          dst[v] = m;
+          dst[NC + v] = sum;
+        }
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) dst[2 * NC + v * D + (D / 32) * lane + x] = y[x];
+      }
+    }
+  }
+  if (tid == 0) {
+    CachePart q = s_part[tail_warp];
+    q.head_state = cta_head;
+    q.tail = cta_tail;
+    p.parts[blockIdx.x] = q;
   }
 }
 
+// Joins the parts of the items that were cut between CTAs: a CTA of D threads for every column of every CTA's last item.
+template <int D>
+__global__ void __launch_bounds__(D) cache_join_kernel(const __grid_constant__ CacheAttParams p, int ctas, int NC) {
+  __shared__ int s_end;
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const int tid = threadIdx.x, w = blockIdx.x, v = blockIdx.y, kPart = NC * (D + 2);
+  const CachePart part = p.parts[w];
+  if (!part.tail || v >= part.rows * p.group) return;
+  if (tid == 0) s_end = ctas - 1;
+  __syncthreads();
+  for (int b = w + 1 + tid; b < ctas; b += D)
+    if (p.parts[b].head_state < 2) atomicMin(&s_end, b);   // the CTA in whose stretch the item ends
+  __syncthreads();
+  const int end = s_end;
+  float m = kLowest, l = 0.f, o = 0.f;
+#pragma unroll 8
+  for (int j = w; j <= end; ++j) {
+    if (j > w && p.parts[j].head_state == 3) continue;
+    const float* src = p.cta_data + ((int64_t)j * 2 + (j == w)) * kPart;
+    const float mj = src[v], lj = src[NC + v], oj = src[2 * NC + v * D + tid];
+    const float m2 = fmaxf(m, mj);
+    const float fa = ex2(m - m2), fb = ex2(mj - m2);
+    l = l * fa + lj * fb;
+    o = o * fa + oj * fb;
+    m = m2;
+  }
+  const int r = v / p.group, ev = v - r * p.group;
+  const int64_t row = (int64_t)(p.grouped ? part.pos : part.sample) * p.R + r;
+  p.out[row * p.ld_out + ((int64_t)part.head * p.group + ev) * D + tid] = __float2bfloat16_rn(l == 0.f ? 0.f : o / l);
+}
+
+template <int D, int NT, int WARPS, int DEPTH>
+cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
+  static size_t configured[DSN_MAX_DEVICES] = {};
+  constexpr size_t smem = attention_smem<D, WARPS, DEPTH>();
+  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+  auto kernel = cache_attention_kernel<D, NT, WARPS, DEPTH>;
+  cudaError_t e = dsn_ensure_dynamic_smem(kernel, smem, configured);
+  if (e != cudaSuccess) return e;
+  e = dsn_launch(kernel, dim3((unsigned)ctas), dim3(WARPS * 32), smem, s, 1, p);
+  if (e != cudaSuccess) return e;
+  return dsn_launch(cache_join_kernel<D>, dim3((unsigned)ctas, 8 * NT), dim3(D), 0, s, 1, p, ctas, 8 * NT);
+}
+
+constexpr int kWarps1 = 16, kWarps2 = 8;   // warps a CTA for up to 8 and up to 16 query vectors a head: registers of the products
+
 }  // namespace
 
-cudaError_t dsn_launch_cache_attention(const CacheAttParams& p, int D, int sm_count, cudaStream_t s) {
-  const int64_t ctas = ((int64_t)p.B * p.R * p.max_heads * p.group + 3) / 4, most = (int64_t)sm_count * 16;
-  const dim3 grid((unsigned)(ctas < most ? ctas : most));
-  return D == 64 ? dsn_launch(cache_attention_simple<64>, grid, dim3(128), 0, s, 1, p) : dsn_launch(cache_attention_simple<128>, grid, dim3(128), 0, s, 1, p);
+// Workspace: the CTAs' words about their ends, requests beyond a CTA's own list, parts of warps and of CTAs.
+struct CacheWorkspace {
+  size_t parts, list, warp_data, cta_data, total;
+};
+static CacheWorkspace carve(int D, int cols, int64_t B, int ctas) {
+  const size_t part = (size_t)(cols <= 8 ? 8 : 16) * (D + 2) * sizeof(float);
+  CacheWorkspace w;
+  w.parts = 0;
+  w.list = w.parts + sizeof(CachePart) * (size_t)ctas;
+  w.warp_data = w.list + sizeof(CacheEntry) * (size_t)B;
+  w.cta_data = w.warp_data + (size_t)ctas * (cols <= 8 ? kWarps1 : kWarps2) * part;
+  w.total = w.cta_data + (size_t)ctas * 2 * part;
+  return w;
+}
+
+size_t dsn_cache_attention_ws_bytes(int D, int cols, int64_t B) { return cols > 16 ? 0 : carve(D, cols, B, DSN_CACHE_MAX_CTAS).total; }
+
+cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s) {
+  const int cols = p.R * p.group, ctas = sm_count < DSN_CACHE_MAX_CTAS ? sm_count : DSN_CACHE_MAX_CTAS;
+  const CacheWorkspace w = carve(D, cols, p.B, ctas);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.parts = reinterpret_cast<CachePart*>(ws + w.parts);
+  p.list = reinterpret_cast<CacheEntry*>(ws + w.list);
+  p.warp_data = reinterpret_cast<float*>(ws + w.warp_data);
+  p.cta_data = reinterpret_cast<float*>(ws + w.cta_data);
+  if (D == 64) return cols <= 8 ? launch<64, 1, kWarps1, 5>(p, ctas, s) : launch<64, 2, kWarps2, 8>(p, ctas, s);
+  return cols <= 8 ? launch<128, 1, kWarps1, 3>(p, ctas, s) : launch<128, 2, kWarps2, 6>(p, ctas, s);
 }
