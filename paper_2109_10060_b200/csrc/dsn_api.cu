@@ -880,6 +880,8 @@ int check_cache_desc(const dsn_cache_desc* d) {
   if ((int64_t)d->n_pages * d->page > INT32_MAX || (int64_t)d->max_pages * d->page >= (1LL << 30)) return DSN_ERR_INVALID_ARG;
   if (d->T < 1 || d->T > DSN_MAX_SLICES || !valid_order(d->order)) return DSN_ERR_INVALID_ARG;
   if (!(d->scale > -INFINITY && d->scale < INFINITY) || d->window < 0) return DSN_ERR_INVALID_ARG;
+  // tiles of a request in one head, counted in 32 bits
+  if (((int64_t)d->max_pages * d->page / 128 + 2) * ((int64_t)d->R * d->group / 256 + 1) > INT32_MAX) return DSN_ERR_UNSUPPORTED;
   for (int t = 0; t < d->T; ++t)
     if (d->heads[t] < 1 || d->heads[t] > d->H) return DSN_ERR_INVALID_ARG;
   return DSN_OK;
@@ -1511,7 +1513,7 @@ int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c
 
 size_t dsn_cache_attention_q4_workspace_bytes(const dsn_cache_desc* d, int32_t B) {
   if (check_cache_desc(d) || B < 0) return 0;
-  return (int64_t)d->R * d->group <= DSN_CACHE_FEW ? dsn_cache_attention_ws_bytes(d->D_h, d->R * d->group, B) : 0;
+  return (int64_t)d->R * d->group <= DSN_CACHE_FEW ? dsn_cache_attention_ws_bytes(d->D_h, d->R * d->group, B) : dsn_cache_rows_ws_bytes(d->D_h, B);
 }
 
 int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* out,
@@ -1536,12 +1538,10 @@ int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cach
   p.qkv = static_cast<const __nv_bfloat16*>(qkv); p.ld_qkv = d->ld_qkv;
   p.out = static_cast<__nv_bfloat16*>(out); p.ld_out = d->ld_out;
   p.status = ctx->d_status;
-  if ((int64_t)d->R * d->group <= DSN_CACHE_FEW) {
-    count_launch(ctx, &dsn_stats::launches_cache_attention, 2);
-    return dsn_launch_cache_attention(p, d->D_h, ctx->sm_count, workspace, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
-  }
-  count_launch(ctx, &dsn_stats::launches_cache_attention);
-  return dsn_launch_cache_attention_rows(p, d->D_h, ctx->sm_count, as_stream(stream)) == cudaSuccess ? DSN_OK : DSN_ERR_CUDA;
+  count_launch(ctx, &dsn_stats::launches_cache_attention, 2);
+  const bool few = (int64_t)d->R * d->group <= DSN_CACHE_FEW;
+  return (few ? dsn_launch_cache_attention : dsn_launch_cache_attention_rows)(p, d->D_h, ctx->sm_count, workspace, as_stream(stream)) == cudaSuccess
+             ? DSN_OK : DSN_ERR_CUDA;
 }
 
 size_t dsn_layer_workspace_bytes(const dsn_layer_desc* L) {

@@ -84,4 +84,5 @@ struct CacheAttParams {
 #define DSN_CACHE_FEW 16         // query vectors of a head (rows * group) up to which the form for a few of them runs
 size_t dsn_cache_attention_ws_bytes(int D, int cols, int64_t B);
 cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s);
-cudaError_t dsn_launch_cache_attention_rows(const CacheAttParams& p, int D, int sm_count, cudaStream_t s);
+size_t dsn_cache_rows_ws_bytes(int D, int64_t B);
+cudaError_t dsn_launch_cache_attention_rows(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s);

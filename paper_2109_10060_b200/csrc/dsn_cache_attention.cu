@@ -15,17 +15,15 @@
 // The order of elements in a product is free, so a lane takes whole words: 16 elements of K in 8 bytes, 8 elements of V in 4.  Row i of a block's K is token
 // i ^ (i >> 2 & 1): then neither K's rows nor the pairs of tokens that a lane needs of V meet in a bank.
 // The maximum is a reference that moves only when a score stands more than 2^8 above it (one vote a step instead of a reduction).
-#include "dsn_cache.cuh"
+#include "dsn_cache_line.cuh"
 
 namespace {
 
+using namespace dsn_q4;
 using dsn_gemm::smem_u32;
 
 constexpr int kStepBlocks = 2, kStepTokens = 32;
-constexpr int kListSmem = 64;      // items' requests that a CTA keeps in shared memory; further ones are read from the workspace
 constexpr uint32_t kCtrl = 2048;  // behind the list: sums of a scan, the abort flag, what the warps say about their ends
-constexpr float kLowest = -1e38f;  // reference before any score: finite, so that differences are
-constexpr float kSlack = 8.f;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -35,22 +33,6 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t nibbles(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }   // 128 + code, twice
-__device__ __forceinline__ uint32_t minus136(uint32_t w) {
-  uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x43084308u));
   return r;
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
@@ -63,57 +45,12 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // First token that the item's rows can see, rounded down to a block, and one behind the last.
 __device__ __forceinline__ void item_range(int len, int rows, int window, int& lo, int& hi) {
   const int first = len - rows;                                // token of the first row
   hi = len;
   lo = window ? max(0, first - window + 1) & ~(DSN_CACHE_BLOCK - 1) : 0;
-}
-
-template <int THREADS>
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* s_warp, uint64_t& total) {   // exclusive
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint64_t incl = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint64_t u = __shfl_up_sync(0xffffffffu, (unsigned long long)incl, o);
-    if (lane >= o) incl += u;
-  }
-  __syncthreads();
-  if (lane == 31) s_warp[warp] = incl;
-  __syncthreads();
-  uint64_t before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    const uint64_t u = s_warp[w];
-    if (w < warp) before += u;
-    total += u;
-  }
-  return before + incl - v;
-}
-
-// One request's place in the line: what it needs to know and how many steps its heads make.
-__device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, bool report) {
-  const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
-  CacheEntry e;
-  e.first = 0;
-  e.sample = at.sample; e.pos = pos; e.heads = 0; e.steps = 0; e.len = 0; e.rows = 0;
-  if (pos >= p.B || at.slice < 0 || at.sample >= p.B) return e;
-  const int most = p.max_pages * p.page;
-  const int len = p.lengths[at.sample], rows = p.placed ? p.placed[at.sample] : p.R;
-  e.len = min(max(len, 0), most);
-  e.rows = min(max(rows, 0), p.R);
-  if (report && (len != e.len || rows != e.rows)) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
-  if (e.rows == 0) return e;
-  int lo, hi;
-  item_range(e.len, e.rows, p.window, lo, hi);
-  e.heads = p.heads[at.slice];
-  e.steps = max(1, (hi - lo + kStepTokens - 1) / kStepTokens);   // a request without tokens: a step that sees nothing, for the zeros
-  return e;
 }
 
 // A walk along the line.
@@ -165,54 +102,21 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
 
-  // ---- the line: how long it is, this CTA's stretch, the requests in it
-  __shared__ int s_first_order, s_count;
-  if (tid == 0) s_first_order = 0, s_count = 0;
-  const CacheEntry e0 = look_up(p, tid, blockIdx.x == 0);
-  uint64_t sum0, ones0, total;
-  const uint64_t first0 = block_scan<THREADS>((uint64_t)e0.heads * e0.steps, s_scan, sum0);
-  const uint64_t order0 = block_scan<THREADS>(e0.heads > 0, s_scan, ones0);
-  total = sum0;
-  for (int b = THREADS; b < p.B; b += THREADS) {
-    uint64_t sum;
-    const CacheEntry e = look_up(p, b + tid, blockIdx.x == 0);
-    block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
-    total += sum;
-  }
-  const uint64_t A = total * blockIdx.x / gridDim.x, Z = total * (blockIdx.x + 1) / gridDim.x;
-  {
-    uint64_t at_first = 0, at_order = 0;
-    for (int b = 0; b < p.B; b += THREADS) {
-      CacheEntry e = e0;
-      uint64_t first = first0, order = order0, sum = sum0, ones = ones0;
-      if (b > 0) {
-        e = look_up(p, b + tid, false);
-        first = at_first + block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
-        order = at_order + block_scan<THREADS>(e.heads > 0, s_scan, ones);
-      }
-      at_first += sum;
-      at_order += ones;
-      const bool here = e.heads > 0 && first < Z && first + (uint64_t)e.heads * e.steps > A;
-      if (here && first <= A) s_first_order = (int)order;   // one thread of all: the request that holds step A
-      __syncthreads();
-      if (here) {
-        const int i = (int)order - s_first_order;
-        e.first = (int64_t)first;
-        if (i < kListSmem) s_list[i] = e; else p.list[order] = e;
-        atomicMax(&s_count, i + 1);
-      }
-      __syncthreads();
-    }
-  }
+  const Stretch stretch = find_stretch<THREADS>(p, s_list, s_scan, [&](int len, int rows) {
+    int lo, hi;
+    item_range(len, rows, p.window, lo, hi);
+    return max(1, (hi - lo + kStepTokens - 1) / kStepTokens);   // a request without tokens: a step that sees nothing, for the zeros
+  });
+  const uint64_t A = stretch.A, Z = stretch.Z;
   const uint64_t u0 = A + (Z - A) * warp / WARPS, u1 = A + (Z - A) * (warp + 1) / WARPS;
   int head_state = 3, tail = 0, head_far = 0;
   Walk work;
   if (u0 < u1) {
   Walk fetch;
   fetch.smem = s_list;
-  fetch.more = p.list + s_first_order;
+  fetch.more = p.list + stretch.first_order;
   {   // the last request that begins at or before u0
-    const int count = s_count;
+    const int count = stretch.count;
     int j = 0;
     for (int b = 0; b < count; b += 32) {
       const int i = b + lane;

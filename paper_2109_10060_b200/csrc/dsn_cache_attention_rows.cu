@@ -1,106 +1,684 @@
-// Attention over the 4-bit cache, many rows.
-#include "dsn_cache.cuh"
+// Attention over the 4-bit cache, many query vectors a head (rows * group > 16: prompts, pieces of prompts), on tcgen05.
+//
+// One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 128; the tiles of all items
+// stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
+// rows (fp32) in the workspace, and a second kernel joins them.
+// Roles (416 threads):
+//   warps 0-3    values: codes of the tile after the next come into registers (a thread a token), are turned into bf16 K and V tiles in shared memory, swizzled
+//                as the products read them (two buffers each).  The products need every element only once for 256 rows, so this costs a quarter of their time.
+//   warp 4       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
+//                of one half runs under the products of the other.
+//   warps 5-8    softmax of half 0, warps 9-12 of half 1: a thread a row (= TMEM lane).  Pass 1: the row's maximum; a reference that moves only
+//                when it stands more than 2^8 below, when O is read, scaled and written back.  Pass 2: exp2, sum, probabilities as bf16 over the columns
+//                of S already read, from where the second product takes them.  They also fetch the rows of Q and write those of O.
+// The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (one mask each pair), so Q's and O's columns are in that order, too.
+// TMEM: 512 columns = two regions of 256: S_h 0..127, P_h over 0..63, O_h from 128.
+// Rounded to bf16 besides Q: elements of K and V (once, scale * (code - 8) + middle) and probabilities.  Every wait is bounded.
+#include "dsn_cache_line.cuh"
 
 namespace {
 
-// One warp a query vector; 32 keys at a time, a lane a key for the scores, a lane D / 32 elements for the values.
-template <int D>
-__global__ void __launch_bounds__(128) cache_attention_simple(const __grid_constant__ CacheAttParams p) {
-  constexpr int E = D / 32;
-  __shared__ float s_q[4][D];
-  dsn_grid_dependency_wait();
-  dsn_grid_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t per_row = (int64_t)p.max_heads * p.group, items = (int64_t)p.B * p.R * per_row;
-  const uint32_t block = dsn_cache_block_bytes(D);
-  for (int64_t it = (int64_t)blockIdx.x * 4 + warp; it < items; it += (int64_t)gridDim.x * 4) {
-    const int64_t row = it / per_row;
-    const int vec = (int)(it - row * per_row), head = vec / p.group, e = vec - head * p.group;
-    const int pos = (int)(row / p.R), r = (int)(row - (int64_t)pos * p.R);
-    const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
-    if (at.slice < 0 || at.sample >= p.B || head >= p.heads[at.slice]) continue;
-    const int most = p.max_pages * p.page;
-    const int len_in = p.lengths[at.sample], n_in = p.placed ? p.placed[at.sample] : p.R;
-    const int L = min(max(len_in, 0), most), n = min(max(n_in, 0), p.R);
-    if ((L != len_in || n != n_in) && lane == 0) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
-    if (r >= n) continue;
-    const int64_t xrow = (int64_t)(p.grouped ? pos : at.sample) * p.R + r;
-    const __nv_bfloat16* q = p.qkv + xrow * p.ld_qkv + ((int64_t)head * (p.group + 2) + e) * D;
-    __syncwarp();
-    for (int j = lane; j < D; j += 32) s_q[warp][j] = __bfloat162float(q[j]);
-    __syncwarp();
-    const int me = L - n + r;                                   // this query's token
-    const int lo = p.window ? max(0, me - p.window + 1) : 0;
-    float m = -INFINITY, l = 0.f, o[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) o[j] = 0.f;
-    for (int k0 = lo & ~15; k0 <= me; k0 += 32) {
-      const int key = k0 + lane;
-      const int col = key / p.page;
-      const int pg = key <= me ? p.table[(int64_t)at.sample * p.max_pages + col] : 0;
-      bool seen = key >= lo && key <= me;
-      if (seen && (pg < 0 || pg >= p.n_pages)) {
-        dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
-        seen = false;
-      }
-      const int tok = key - col * p.page;
-      const uint8_t* blk = p.pages + (((int64_t)(seen ? pg : 0) * p.H + head) * (p.page / 16) + (seen ? tok / 16 : 0)) * block;
-      const int t = tok & 15;
-      float sc = -INFINITY;
-      if (seen) {
-        sc = 0.f;
-        for (int g = 0; g < D / 64; ++g) {
-          const uint32_t pr = *reinterpret_cast<const uint32_t*>(blk + D / 64 * 512 + (g * 16 + t) * 4);
-          float dot = 0.f, sum = 0.f;
-          for (int w = 0; w < 8; ++w) {
-            const uint32_t c = *reinterpret_cast<const uint32_t*>(blk + (g * 16 + t) * 32 + w * 4);
-            for (int j = 0; j < 8; ++j) {
-              const float qv = s_q[warp][g * 64 + w * 8 + j];
-              dot = fmaf(qv, (float)((int)((c >> (4 * j)) & 15) - 8), dot);
-              sum += qv;
-            }
-          }
-          sc += dot * __uint_as_float(pr << 16) + sum * __uint_as_float(pr & 0xffff0000u);
+using namespace dsn_q4;
+using namespace dsn_gemm;
+
+constexpr int kThreadsR = 416, kRows = 256, kTile = 128;
+constexpr int kValueWarps = 4, kIssueWarp = 4, kSoftWarp = 5;
+constexpr uint32_t kTileBytes = 128 * 128;   // 128 rows of 64 bf16
+constexpr uint32_t kCtrlR = 4096;
+constexpr uint32_t kRegion = 256, kOCol = 128;
+
+__device__ __forceinline__ void mma_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_32(uint32_t taddr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+        "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {   // NaN if any of them is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^t of two arguments without the special-function unit, t at most a few tens: t = n + f with n = round(t) taken from the mantissa of t + 1.5 * 2^23, 2^f by a
+// cubic (own fit, relative error 7.5e-5, a fiftieth of a bf16 rounding step), n added to the exponent.  Below -126: 2^-126.
+__device__ __forceinline__ void exp2_pair(uint64_t t2, float& x0, float& x1) {
+  float t0, t1;
+  unpack2(t2, t0, t1);
+  t2 = pack2(fmaxf(t0, -126.f), fmaxf(t1, -126.f));
+  const uint64_t r2 = fadd2(t2, pack2(12582912.f, 12582912.f));
+  const uint64_t n2 = fadd2(r2, pack2(-12582912.f, -12582912.f));
+  const uint64_t f2 = ffma2(n2, pack2(-1.f, -1.f), t2);
+  uint64_t p2 = ffma2(pack2(0.0551716685f, 0.0551716685f), f2, pack2(0.2426111251f, 0.2426111251f));
+  p2 = ffma2(p2, f2, pack2(0.6932609677f, 0.6932609677f));
+  p2 = ffma2(p2, f2, pack2(0.9999280572f, 0.9999280572f));
+  float r0, r1, p0, p1;
+  unpack2(r2, r0, r1);
+  unpack2(p2, p0, p1);
+  x0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23));
+  x1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23));
+}
+// V as it lies: rows are tokens, 64 elements in 128 bytes; 128 elements are two such tiles.
+__device__ __forceinline__ uint64_t make_desc_mn(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(kTileBytes >> 4) << 16;   // from 64 elements to the next 64
+  d |= (uint64_t)(1024 >> 4) << 32;         // from 8 tokens to the next 8
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// 256 (or the last) query vectors of a head of a request: their tokens and the tiles that they need.
+struct Span {
+  int v0, v1;         // vectors
+  int me0, me1;       // tokens of the first and the last
+  int lo, tiles;      // first token of the first tile, tiles
+};
+__device__ __forceinline__ Span span_of(int len, int rows, int ct, int group, int window) {
+  Span s;
+  s.v0 = ct * kRows;
+  s.v1 = min(rows * group, s.v0 + kRows);
+  const int first = len - rows;
+  s.me0 = first + s.v0 / group;
+  s.me1 = first + (s.v1 - 1) / group;
+  s.lo = window ? max(0, s.me0 - window + 1) & ~(DSN_CACHE_BLOCK - 1) : 0;
+  s.tiles = max(1, (s.me1 + 1 - s.lo + kTile - 1) / kTile);
+  return s;
+}
+__device__ __forceinline__ int head_tiles(int len, int rows, int group, int window) {
+  const int cts = (rows * group + kRows - 1) / kRows;
+  int sum = 0;
+  for (int ct = 0; ct < cts; ++ct) sum += span_of(len, rows, ct, group, window).tiles;
+  return sum;
+}
+
+// What a CTA does of one item: tiles c0 .. c1 - 1 of the span.
+struct Item {
+  CacheEntry e;
+  Span s;
+  int head, c0, c1;
+};
+struct RowWalk {
+  const CacheEntry* smem;
+  const CacheEntry* more;
+  int j, head, ct, c0;
+  int64_t left;         // tiles of the stretch still to come
+  CacheEntry e;
+  __device__ __forceinline__ void load(int i) {
+    j = i;
+    e = i < kListSmem ? smem[i] : more[i];
+  }
+  __device__ __forceinline__ bool next(const CacheAttParams& p, Item& it) {
+    if (left <= 0) return false;
+    it.e = e;
+    it.head = head;
+    it.s = span_of(e.len, e.rows, ct, p.group, p.window);
+    it.c0 = c0;
+    it.c1 = (int)min((int64_t)it.s.tiles, c0 + left);
+    left -= it.c1 - it.c0;
+    if (left > 0) {
+      c0 = 0;
+      if (it.s.v1 == e.rows * p.group) {
+        ct = 0;
+        if (++head == e.heads) {
+          head = 0;
+          load(j + 1);
         }
-        sc *= p.scale_log2;
-      }
-      float mx = sc;
-      for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-      const float m2 = fmaxf(m, mx);
-      const float pr = seen ? exp2f(sc - (m2 == -INFINITY ? 0.f : m2)) : 0.f;
-      const float keep = m2 == -INFINITY ? 1.f : exp2f(m - m2);
-      m = m2;
-      l = l * keep + pr;
-#pragma unroll
-      for (int j = 0; j < E; ++j) o[j] *= keep;
-      for (int i = 0; i < 32; ++i) {
-        const float pi = __shfl_sync(0xffffffffu, pr, i);
-        const uint64_t bi = __shfl_sync(0xffffffffu, (unsigned long long)reinterpret_cast<uint64_t>(blk), i);
-        const int ti = __shfl_sync(0xffffffffu, t, i);
-        if (!__shfl_sync(0xffffffffu, (int)seen, i)) continue;
-        const uint8_t* v = reinterpret_cast<const uint8_t*>(bi) + block / 2;
-        const int d0 = lane * E, g = d0 / 64;
-        const uint32_t prm = *reinterpret_cast<const uint32_t*>(v + D / 64 * 512 + (g * 16 + ti) * 4);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const int d = d0 + j - g * 64;
-          const int c = (v[(g * 16 + ti) * 32 + d / 2] >> (4 * (d & 1))) & 15;
-          const float z = __uint_as_float(prm & 0xffff0000u), s = __uint_as_float(prm << 16);
-          o[j] = fmaf(pi, z == z ? fmaf(s, (float)(c - 8), z) : 0.f, o[j]);   // NaN tokens come through the scores
-        }
+      } else {
+        ++ct;
       }
     }
-    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-#pragma unroll
-    for (int j = 0; j < E; ++j)
-      p.out[xrow * p.ld_out + ((int64_t)head * p.group + e) * D + lane * E + j] = __float2bfloat16_rn(l == 0.f ? 0.f : o[j] / l);
+    return true;
   }
+};
+// Tiles of the CTA's part that half h of the item needs: a .. b - 1 (none: a == b).
+__device__ __forceinline__ void half_tiles(const Item& it, int h, int group, int window, int& a, int& b) {
+  const int w0 = it.s.v0 + 128 * h, w1 = min(it.s.v1, w0 + 128);
+  a = b = it.c0;
+  if (w0 >= w1) return;
+  const int first = it.e.len - it.e.rows, m0 = first + w0 / group, m1 = first + (w1 - 1) / group;
+  if (m1 < 0) return;
+  a = max(it.c0, ((window ? max(0, m0 - window + 1) : 0) - it.s.lo) / kTile);
+  b = min(it.c1, (m1 + 1 - it.s.lo + kTile - 1) / kTile);
+  if (b < a) b = a;
+}
+
+// Codes of one token of a head, as they lie.
+template <int D>
+struct Raw {
+  uint4 k[D / 32], v[D / 32];
+  uint32_t kp[D / 64], vp[D / 64];
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_constant__ CacheAttParams p) {
+  constexpr int GR = D / 64;
+  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (base - raw);
+  const uint32_t q_full = base, k_full = base + 16, v_full = base + 32, k_empty = base + 48, v_empty = base + 64, s_full = base + 80,
+                 p_full = base + 96, o_full = base + 112, o_empty = base + 128;   // [2] each
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 144);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 148);
+  uint8_t* s_bad = smem + 160;                                                     // [4 tiles][4 warps]: blocks of a page outside the cache
+  uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 256);
+  CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 512);
+  static_assert(512 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
+  const uint32_t q_at = base + kCtrlR, k_at = q_at + 2 * kOperand, v_at = k_at + 2 * kOperand;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full + 8 * i, 4);
+      mbar_init(k_full + 8 * i, kValueWarps);
+      mbar_init(v_full + 8 * i, kValueWarps);
+      mbar_init(k_empty + 8 * i, 1);
+      mbar_init(v_empty + 8 * i, 1);
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 8 * i, 4);
+      mbar_init(o_full + 8 * i, 1);
+      mbar_init(o_empty + 8 * i, 4);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.window); });
+  if (warp == kIssueWarp) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  RowWalk walk;
+  walk.smem = s_list;
+  walk.more = p.list + stretch.first_order;
+  walk.left = (int64_t)(stretch.Z - stretch.A);
+  if (walk.left > 0) {
+    walk.load(0);   // the request that holds tile A is the list's first
+    uint64_t off = stretch.A - (uint64_t)walk.e.first;
+    walk.head = (int)(off / (uint32_t)walk.e.steps);
+    int in_head = (int)(off - (uint64_t)walk.head * walk.e.steps);
+    walk.ct = 0;
+    while (true) {
+      const int n = span_of(walk.e.len, walk.e.rows, walk.ct, p.group, p.window).tiles;
+      if (in_head < n) break;
+      in_head -= n;
+      ++walk.ct;
+    }
+    walk.c0 = in_head;
+  }
+  Item it;
+
+  if (warp < kValueWarps) {
+    // ------------------------------------------------------------------------------ codes to values
+    const int bpp = p.page / DSN_CACHE_BLOCK;
+    const int tt = tid;   // this thread's token in a tile
+    Raw<D> r;
+    uint32_t bad = 0;
+    bool have = walk.next(p, it);
+    int tile = it.c0;
+    auto fetch = [&]() {   // this thread's token of the walk's current tile
+      const int key = it.s.lo + tile * kTile + tt;
+      const bool exists = key <= it.s.me1;
+      int pg = -1, tok = 0;
+      if (exists) {
+        const int col = (int)dsn_div((uint32_t)key, p.by_page);
+        pg = p.table[(int64_t)it.e.sample * p.max_pages + col];
+        tok = key - col * p.page;
+      }
+      const bool ok = pg >= 0 && pg < p.n_pages;
+      bad = __ballot_sync(0xffffffffu, exists && !ok);
+      if (exists && !ok) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
+      const uint8_t* blk = p.pages + (((int64_t)(ok ? pg : 0) * p.H + it.head) * bpp + tok / DSN_CACHE_BLOCK) * kBlock;
+      const int t16 = tok % DSN_CACHE_BLOCK;
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          r.k[2 * gr + x] = ok ? *reinterpret_cast<const uint4*>(blk + (gr * 16 + t16) * 32 + 16 * x) : make_uint4(0, 0, 0, 0);
+          r.v[2 * gr + x] = ok ? *reinterpret_cast<const uint4*>(blk + kBlock / 2 + (gr * 16 + t16) * 32 + 16 * x) : make_uint4(0, 0, 0, 0);
+        }
+        r.kp[gr] = ok ? *reinterpret_cast<const uint32_t*>(blk + GR * 512 + (gr * 16 + t16) * 4) : 0u;
+        r.vp[gr] = ok ? *reinterpret_cast<const uint32_t*>(blk + kBlock / 2 + GR * 512 + (gr * 16 + t16) * 4) : 0u;
+      }
+    };
+    auto values = [&](const uint4 (&c)[D / 32], const uint32_t (&pair)[D / 64], uint32_t dst) {
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+        __nv_bfloat162 s2, z2;
+        *reinterpret_cast<uint32_t*>(&s2) = __byte_perm(pair[gr], pair[gr], 0x1010);
+        *reinterpret_cast<uint32_t*>(&z2) = __byte_perm(pair[gr], pair[gr], 0x3232);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          const uint4 q = c[2 * gr + (w >> 2)];
+          const uint32_t word = (w & 3) == 0 ? q.x : (w & 3) == 1 ? q.y : (w & 3) == 2 ? q.z : q.w;
+          uint32_t o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t n = minus136(nibbles(word >> (4 * i)));
+            const __nv_bfloat162 y = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&n), s2, z2);
+            o[i] = *reinterpret_cast<const uint32_t*>(&y);
+          }
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + gr * kTileBytes + (uint32_t)tt * 128u + (uint32_t)((w ^ (tt & 7)) << 4)),
+                       "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                       : "memory");
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+    };
+    if (have) fetch();
+    for (uint32_t n = 0; have; ++n) {
+      const uint32_t s = n & 1u;
+      if (n >= 2 && !dsn_wait(k_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
+      if (lane == 0) s_bad[(n & 3u) * 4 + warp] = (uint8_t)((bad & 0xffffu ? 1u : 0u) | (bad >> 16 ? 2u : 0u));
+      values(r.k, r.kp, k_at + s * kOperand);
+      if (lane == 0) mbar_arrive(k_full + 8 * s);
+      if (n >= 2 && !dsn_wait(v_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 82)) break;
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr)   // a token that is not finite shows in its scores; rows that do not see it must not meet it here
+        if (!(fabsf(lo_bf16(r.vp[gr])) <= 3.4e38f) || !(fabsf(hi_bf16(r.vp[gr])) <= 3.4e38f)) r.vp[gr] = 0u;
+      values(r.v, r.vp, v_at + s * kOperand);
+      if (lane == 0) mbar_arrive(v_full + 8 * s);
+      if (++tile == it.c1) {
+        have = walk.next(p, it);
+        tile = it.c0;
+      }
+      if (have) fetch();
+    }
+  } else if (warp == kIssueWarp) {
+    // ------------------------------------------------------------------------------ products
+    const uint32_t idesc_s = make_idesc(128, kTile), idesc_o = make_idesc(128, D) | (1u << 16);   // V: elements first
+    uint32_t n = 0;                       // tiles so far
+    uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, n_o[2] = {0, 0};   // P waited for, Q waited for, items of the half
+    bool pend[2] = {false, false}, first_pv[2] = {true, true};
+    bool ok = true;
+    auto pv = [&](int h, uint32_t tile_n) {   // O_h (+)= P_h V
+      const uint32_t s = tile_n & 1u;
+      ok = ok && dsn_wait(p_full + 8 * h, n_p[h] & 1u, abort_flag, p.status, 83);
+      ok = ok && dsn_wait(v_full + 8 * s, (tile_n >> 1) & 1u, abort_flag, p.status, 84);
+      if (first_pv[h] && n_o[h] > 0) ok = ok && dsn_wait(o_empty + 8 * h, (n_o[h] - 1u) & 1u, abort_flag, p.status, 85);
+      ++n_p[h];
+      if (!ok) return;
+      if (elect_one()) {
+        tc_fence_after();
+        const uint32_t region = tmem + h * kRegion;
+#pragma unroll
+        for (int ks = 0; ks < kTile / 16; ++ks)
+          mma_a_tmem(region + kOCol, region + 8u * ks, make_desc_mn(v_at + s * kOperand + ks * 2048), idesc_o, first_pv[h] && ks == 0 ? 0u : 1u);
+        umma_commit(o_full + 8 * h);
+      }
+      __syncwarp();
+      first_pv[h] = false;
+      pend[h] = false;
+    };
+    auto release = [&](uint32_t bar) {
+      if (elect_one()) umma_commit(bar);
+      __syncwarp();
+    };
+    while (ok && walk.next(p, it)) {
+      int a[2], b[2];
+      half_tiles(it, 0, p.group, p.window, a[0], b[0]);
+      half_tiles(it, 1, p.group, p.window, a[1], b[1]);
+      for (int j = it.c0; j < it.c1 && ok; ++j, ++n) {
+        const uint32_t s = n & 1u;
+        if (j == it.c0) {   // what the item before still needs comes first: this item's Q arrives only behind its softmax
+          for (int h = 0; h < 2; ++h)
+            if (pend[h]) pv(h, n - 1u);
+          if (n > 0 && ok) release(v_empty + 8 * (s ^ 1u));
+          for (int h = 0; h < 2; ++h)
+            if (a[h] < b[h]) {
+              if (!first_pv[h]) ++n_o[h];
+              first_pv[h] = true;
+            }
+        }
+        for (int h = 0; h < 2 && ok; ++h) {
+          if (pend[h]) pv(h, n - 1u);
+          if (j >= a[h] && j < b[h] && ok) {
+            if (j == a[h]) ok = dsn_wait(q_full + 8 * h, n_q[h]++ & 1u, abort_flag, p.status, 86);
+            ok = ok && dsn_wait(k_full + 8 * s, (n >> 1) & 1u, abort_flag, p.status, 87);
+            if (!ok) break;
+            if (elect_one()) {
+              tc_fence_after();
+#pragma unroll
+              for (int ks = 0; ks < D / 16; ++ks) {
+                const uint32_t off = (uint32_t)(ks >> 2) * kTileBytes;
+                umma_bf16(tmem + h * kRegion, make_smem_desc(q_at + h * kOperand + off) + 2u * (ks & 3), make_smem_desc(k_at + s * kOperand + off) + 2u * (ks & 3),
+                          idesc_s, ks > 0 ? 1u : 0u);
+              }
+              umma_commit(s_full + 8 * h);
+            }
+            __syncwarp();
+            pend[h] = true;
+          }
+        }
+        if (!ok) break;
+        if (a[0] == b[0] && a[1] == b[1]) ok = dsn_wait(k_full + 8 * s, (n >> 1) & 1u, abort_flag, p.status, 87);   // a tile that nobody needs
+        release(k_empty + 8 * s);
+        if (j > it.c0) release(v_empty + 8 * (s ^ 1u));
+      }
+    }
+    for (int h = 0; h < 2; ++h)
+      if (pend[h] && ok) pv(h, n - 1u);
+  } else {
+    // ------------------------------------------------------------------------------ softmax, a thread a row
+    const int h = (warp - kSoftWarp) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t region = tmem + h * kRegion + ((uint32_t)(quarter * 32) << 16);
+    const float c2 = fabsf(p.scale_log2);
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale goes into Q's signs
+    const uint32_t q_row = q_at + h * kOperand + (uint32_t)row * 128u;
+    uint32_t n_s = 0, n_pv = 0, n = 0;   // S waited for, products with V asked for, tiles so far
+    bool ok = true;
+    auto load_q = [&](const Item& x) {
+      const int v = x.s.v0 + 128 * h + row;
+      const bool live = v < x.s.v1;
+      const int r = v / p.group, ev = v - r * p.group;
+      const __nv_bfloat16* src = p.qkv + ((int64_t)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((int64_t)x.head * (p.group + 2) + ev) * D;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) w = *reinterpret_cast<const uint4*>(src + 8 * c);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (uint32_t)(c >> 3) * kTileBytes + (uint32_t)(((c & 7) ^ (row & 7)) << 4)),
+                     "r"(__byte_perm(w.x, w.z, 0x5410) ^ flip), "r"(__byte_perm(w.x, w.z, 0x7632) ^ flip), "r"(__byte_perm(w.y, w.w, 0x5410) ^ flip),
+                     "r"(__byte_perm(w.y, w.w, 0x7632) ^ flip)
+                     : "memory");
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full + 8 * h);
+    };
+    CachePart ends{3, 0, 0, 0, 0, 0, 0, 0};   // what the CTA has to say about the ends of its stretch; rows: the tail's first vector, pad: one behind its last
+    bool have = walk.next(p, it);
+    int a = 0, b = 0;
+    if (have) {
+      half_tiles(it, h, p.group, p.window, a, b);
+      if (a < b) load_q(it);
+    }
+    while (have && ok) {
+      const int v = it.s.v0 + 128 * h + row;
+      const bool live = v < it.s.v1;
+      const int me = it.e.len - it.e.rows + v / p.group;
+      float mref = kLowest, l = 0.f;
+      for (int j = a; j < b && ok; ++j) {
+        ok = dsn_wait(s_full + 8 * h, n_s & 1u, abort_flag, p.status, 88);
+        if (!ok) break;
+        ++n_s;
+        tc_fence_after();
+        // columns of this tile that the row sees
+        const int t0 = it.s.lo + j * kTile;
+        const int k1 = me + 1 - t0, k0 = p.window ? me - p.window + 1 - t0 : 0;
+        const uint32_t bad = *reinterpret_cast<const volatile uint32_t*>(s_bad + ((n + (uint32_t)(j - it.c0)) & 3u) * 4);
+        const bool cut = __any_sync(0xffffffffu, live && (k1 < kTile || k0 > 0)) || bad != 0;
+        auto hide = [&](uint32_t (&x)[32], int c) {   // block c of 32 columns
+          const int e1 = min(max(k1 - 32 * c, 0), 32), e0 = min(max(k0 - 32 * c, 0), 32);
+          uint32_t m = (e1 >= 32 ? 0xffffffffu : (1u << e1) - 1u) & (e0 >= 32 ? 0u : 0xffffffffu << e0);
+          const uint32_t bb = bad >> (8 * c);
+          if (bb & 1u) m &= 0xffff0000u;
+          if (bb & 2u) m &= 0x0000ffffu;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (!(m >> i & 1u)) x[i] = 0xff800000u;
+        };
+        float m0 = -INFINITY, m1 = -INFINITY;
+        uint32_t va[32], vb[32];
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+          tmem_ld_32x32(region + 32 * c, va);
+          tmem_ld_32x32(region + 32 * (c + 1), vb);
+          tmem_ld_wait();
+          if (cut) {
+            hide(va, c);
+            hide(vb, c + 1);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            m0 = max3_nan(m0, __uint_as_float(va[i]), __uint_as_float(va[i + 1]));
+            m1 = max3_nan(m1, __uint_as_float(vb[i]), __uint_as_float(vb[i + 1]));
+          }
+        }
+        const float top = max3_nan(m0, m1, m1) * c2;
+        if (top != top) l = top;   // a token that is not finite: so is the row
+        if (__any_sync(0xffffffffu, top > mref + kSlack)) {
+          const float m = fmaxf(mref, top), f = ex2(mref - m);
+          mref = m;
+          l *= f;
+          if (j > a) {
+            ok = dsn_wait(o_full + 8 * h, (n_pv - 1u) & 1u, abort_flag, p.status, 89);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              tmem_ld_32x32(region + kOCol + c, va);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) va[i] = __float_as_uint(__uint_as_float(va[i]) * f);
+              tmem_st_32(region + kOCol + c, va);
+            }
+            tmem_st_done();
+          }
+        }
+        const uint64_t c2_2 = pack2(c2, c2), ref_2 = pack2(-mref, -mref);
+        uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
+        auto block = [&](uint32_t (&x)[32], int c) {
+          if (cut) hide(x, c);
+#pragma unroll
+          for (int half_b = 0; half_b < 2; ++half_b) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float x0, x1;
+              const uint64_t t2 = ffma2(pack2(__uint_as_float(x[16 * half_b + 2 * e]), __uint_as_float(x[16 * half_b + 2 * e + 1])), c2_2, ref_2);
+              if ((e & 1) && !cut) {
+                exp2_pair(t2, x0, x1);   // every other pair on the FMA pipe
+              } else {
+                float t0f, t1f;
+                unpack2(t2, t0f, t1f);
+                x0 = ex2(t0f);
+                x1 = ex2(t1f);
+              }
+              if (e & 2) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
+              w[e] = pack_bf16(x0, x1);
+            }
+            tmem_st_8(region + (uint32_t)(16 * c + 8 * half_b), w);
+          }
+        };
+        tmem_ld_32x32(region, va);
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+          tmem_ld_32x32(region + 32 * (c + 1), vb);
+          block(va, c);
+          tmem_ld_wait();
+          if (c + 2 < 4) tmem_ld_32x32(region + 32 * (c + 2), va);
+          block(vb, c + 1);
+          tmem_ld_wait();
+        }
+        float s0, s1, s2, s3;
+        unpack2(sum_a, s0, s1);
+        unpack2(sum_b, s2, s3);
+        l += (s0 + s1) + (s2 + s3);
+        tmem_st_done();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 8 * h);
+        ++n_pv;
+      }
+      if (!ok) break;
+      // the next item's Q: every product with this item's has run
+      const Item cur = it;
+      const bool ran = a < b;
+      n += (uint32_t)(cur.c1 - cur.c0);
+      have = walk.next(p, it);
+      if (have) {
+        half_tiles(it, h, p.group, p.window, a, b);
+        if (a < b) load_q(it);
+      }
+      if (ran) {
+        ok = dsn_wait(o_full + 8 * h, (n_pv - 1u) & 1u, abort_flag, p.status, 90);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const bool whole = cur.c0 == 0 && cur.c1 == cur.s.tiles;
+      const int r = v / p.group, ev = v - r * p.group;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? cur.e.pos : cur.e.sample) * p.R + r) * p.ld_out + ((int64_t)cur.head * p.group + ev) * D;
+      // a part: references, sums, then four elements of every row after the other
+      float* part = p.cta_data + ((int64_t)blockIdx.x * 2 + (cur.c0 == 0)) * (kRows * (D + 2)) + 128 * h + row;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        if (ran) {
+          tmem_ld_32x32(region + kOCol + c, o);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0u;
+        }
+        if (c + 32 == D && ran) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(o_empty + 8 * h);
+        }
+        if (!live) continue;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float y[8];   // columns 0 4 1 5 2 6 3 7
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(o[8 * x + i]);
+          if (whole) {
+            uint4 w;
+            w.x = pack_bf16(y[0] * inv, y[2] * inv);
+            w.y = pack_bf16(y[4] * inv, y[6] * inv);
+            w.z = pack_bf16(y[1] * inv, y[3] * inv);
+            w.w = pack_bf16(y[5] * inv, y[7] * inv);
+            *reinterpret_cast<uint4*>(dst + c + 8 * x) = w;
+          } else {
+            float* to = part - (128 * h + row) + 2 * kRows + (int64_t)((c + 8 * x) / 4) * (4 * kRows) + 4 * (128 * h + row);
+            *reinterpret_cast<float4*>(to) = make_float4(y[0], y[2], y[4], y[6]);
+            *reinterpret_cast<float4*>(to + 4 * kRows) = make_float4(y[1], y[3], y[5], y[7]);
+          }
+        }
+      }
+      if (!whole && live) {
+        part[0] = mref;
+        part[kRows] = l;
+      }
+      if (cur.c0 > 0) ends.head_state = cur.c1 == cur.s.tiles ? 1 : 2;
+      else if (ends.head_state == 3) ends.head_state = 0;
+      if (cur.c0 == 0 && !whole)
+        ends = CachePart{ends.head_state, 1, cur.e.sample, cur.e.pos, cur.head, cur.s.v0, 0, cur.s.v1};
+    }
+    if (!ok) ends.head_state = 3, ends.tail = 0;
+    if (warp == kSoftWarp && lane == 0) p.parts[blockIdx.x] = ends;
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kIssueWarp) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of the items that were cut: rows of a CTA's last item by threads, D / 8 CTAs for the elements.
+template <int D>
+__global__ void __launch_bounds__(kRows) cache_rows_join_kernel(const __grid_constant__ CacheAttParams p, int ctas) {
+  __shared__ int s_end;
+  dsn_grid_dependency_wait();
+  dsn_grid_launch_dependents();
+  const int w = blockIdx.x, c = 8 * blockIdx.y, i = threadIdx.x;
+  const CachePart part = p.parts[w];
+  if (!part.tail) return;
+  if (i == 0) s_end = ctas - 1;
+  __syncthreads();
+  for (int b = w + 1 + i; b < ctas; b += kRows)
+    if (p.parts[b].head_state < 2) atomicMin(&s_end, b);
+  __syncthreads();
+  const int v = part.rows + i, end = s_end;
+  if (v >= part.pad) return;
+  float m = kLowest, l = 0.f, y[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) y[x] = 0.f;
+#pragma unroll 4
+  for (int j = w; j <= end; ++j) {
+    if (j > w && p.parts[j].head_state == 3) continue;
+    const float* src = p.cta_data + ((int64_t)j * 2 + (j == w)) * (kRows * (D + 2));
+    const float4 q0 = *reinterpret_cast<const float4*>(src + 2 * kRows + (int64_t)(c / 4) * (4 * kRows) + 4 * i);
+    const float4 q1 = *reinterpret_cast<const float4*>(src + 2 * kRows + (int64_t)(c / 4 + 1) * (4 * kRows) + 4 * i);
+    const float mj = src[i], lj = src[kRows + i], m2 = fmaxf(m, mj), fa = ex2(m - m2), fb = ex2(mj - m2);
+    m = m2;
+    l = l * fa + lj * fb;
+    y[0] = y[0] * fa + q0.x * fb; y[1] = y[1] * fa + q0.y * fb; y[2] = y[2] * fa + q0.z * fb; y[3] = y[3] * fa + q0.w * fb;
+    y[4] = y[4] * fa + q1.x * fb; y[5] = y[5] * fa + q1.y * fb; y[6] = y[6] * fa + q1.z * fb; y[7] = y[7] * fa + q1.w * fb;
+  }
+  const int r = v / p.group, ev = v - r * p.group;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint4 o;
+  o.x = pack_bf16(y[0] * inv, y[1] * inv);
+  o.y = pack_bf16(y[2] * inv, y[3] * inv);
+  o.z = pack_bf16(y[4] * inv, y[5] * inv);
+  o.w = pack_bf16(y[6] * inv, y[7] * inv);
+  *reinterpret_cast<uint4*>(p.out + ((int64_t)(p.grouped ? part.pos : part.sample) * p.R + r) * p.ld_out + ((int64_t)part.head * p.group + ev) * D + c) = o;
+}
+
+template <int D>
+cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
+  static size_t configured[DSN_MAX_DEVICES] = {};
+  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes;
+  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+  cudaError_t e = dsn_ensure_dynamic_smem(cache_rows_kernel<D>, smem, configured);
+  if (e != cudaSuccess) return e;
+  e = dsn_launch(cache_rows_kernel<D>, dim3((unsigned)ctas), dim3(kThreadsR), smem, s, 1, p);
+  if (e != cudaSuccess) return e;
+  return dsn_launch(cache_rows_join_kernel<D>, dim3((unsigned)ctas, D / 8), dim3(kRows), 0, s, 1, p, ctas);
+}
+
+struct RowsWorkspace {
+  size_t parts, list, data, total;
+};
+RowsWorkspace carve(int D, int64_t B, int ctas) {
+  RowsWorkspace w;
+  w.parts = 0;
+  w.list = w.parts + sizeof(CachePart) * (size_t)ctas;
+  w.data = w.list + sizeof(CacheEntry) * (size_t)B;
+  w.total = w.data + (size_t)ctas * 2 * kRows * (D + 2) * sizeof(float);
+  return w;
 }
 
 }  // namespace
 
-cudaError_t dsn_launch_cache_attention_rows(const CacheAttParams& p, int D, int sm_count, cudaStream_t s) {
-  const int64_t ctas = ((int64_t)p.B * p.R * p.max_heads * p.group + 3) / 4, most = (int64_t)sm_count * 16;
-  const dim3 grid((unsigned)(ctas < most ? ctas : most));
-  return D == 64 ? dsn_launch(cache_attention_simple<64>, grid, dim3(128), 0, s, 1, p) : dsn_launch(cache_attention_simple<128>, grid, dim3(128), 0, s, 1, p);
+size_t dsn_cache_rows_ws_bytes(int D, int64_t B) { return carve(D, B, DSN_CACHE_MAX_CTAS).total; }
+
+cudaError_t dsn_launch_cache_attention_rows(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s) {
+  const int ctas = sm_count < DSN_CACHE_MAX_CTAS ? sm_count : DSN_CACHE_MAX_CTAS;
+  const RowsWorkspace w = carve(D, p.B, ctas);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.parts = reinterpret_cast<CachePart*>(ws + w.parts);
+  p.list = reinterpret_cast<CacheEntry*>(ws + w.list);
+  p.cta_data = reinterpret_cast<float*>(ws + w.data);
+  return D == 64 ? launch<64>(p, ctas, s) : launch<128>(p, ctas, s);
 }

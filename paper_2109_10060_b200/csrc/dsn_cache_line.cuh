@@ -1,0 +1,125 @@
+// The line of steps that the attention kernels over the 4-bit cache deal out: the steps of all (request, head) items, one request after the other,
+// cut into equal stretches, one a CTA.  Every CTA scans the requests' lengths on its own and keeps the requests of its stretch.
+#pragma once
+
+#include "dsn_cache.cuh"
+
+namespace dsn_q4 {
+
+constexpr int kListSmem = 64;      // requests that a CTA keeps in shared memory; further ones are read from the workspace
+constexpr float kLowest = -1e38f;  // reference before any score: finite, so that differences are
+constexpr float kSlack = 8.f;      // a reference moves when a score stands further above it
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t nibbles(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }   // bf16 128 + code, of the elements 0 and 4
+__device__ __forceinline__ uint32_t minus136(uint32_t w) {
+  uint32_t r;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x43084308u));
+  return r;
+}
+__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+template <int THREADS>
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* s_warp, uint64_t& total) {   // exclusive
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t u = __shfl_up_sync(0xffffffffu, (unsigned long long)incl, o);
+    if (lane >= o) incl += u;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  uint64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const uint64_t u = s_warp[w];
+    if (w < warp) before += u;
+    total += u;
+  }
+  return before + incl - v;
+}
+
+// One request's place in the line: what it needs to know and how many steps each of its heads makes, steps(len, rows).
+template <typename Steps>
+__device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, bool report, Steps steps) {
+  const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
+  CacheEntry e;
+  e.first = 0;
+  e.sample = at.sample; e.pos = pos; e.heads = 0; e.steps = 0; e.len = 0; e.rows = 0;
+  if (pos >= p.B || at.slice < 0 || at.sample >= p.B) return e;
+  const int most = p.max_pages * p.page;
+  const int len = p.lengths[at.sample], rows = p.placed ? p.placed[at.sample] : p.R;
+  e.len = min(max(len, 0), most);
+  e.rows = min(max(rows, 0), p.R);
+  if (report && (len != e.len || rows != e.rows)) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
+  if (e.rows == 0) return e;
+  e.heads = p.heads[at.slice];
+  e.steps = steps(e.len, e.rows);
+  return e;
+}
+
+// The CTA's stretch A .. Z - 1 and the requests in it: number i of them in s_list[i], from kListSmem on in p.list[first_order + i].
+struct Stretch {
+  uint64_t A, Z;
+  int first_order, count;
+};
+template <int THREADS, typename Steps>
+__device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEntry* s_list, uint64_t* s_scan, Steps steps) {
+  __shared__ int s_first_order, s_count;
+  const int tid = threadIdx.x;
+  if (tid == 0) s_first_order = 0, s_count = 0;
+  const CacheEntry e0 = look_up(p, tid, blockIdx.x == 0, steps);
+  uint64_t sum0, ones0, total;
+  const uint64_t first0 = block_scan<THREADS>((uint64_t)e0.heads * e0.steps, s_scan, sum0);
+  const uint64_t order0 = block_scan<THREADS>(e0.heads > 0, s_scan, ones0);
+  total = sum0;
+  for (int b = THREADS; b < p.B; b += THREADS) {
+    uint64_t sum;
+    const CacheEntry e = look_up(p, b + tid, blockIdx.x == 0, steps);
+    block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
+    total += sum;
+  }
+  Stretch st;
+  st.A = total * blockIdx.x / gridDim.x;
+  st.Z = total * (blockIdx.x + 1) / gridDim.x;
+  uint64_t at_first = 0, at_order = 0;
+  for (int b = 0; b < p.B; b += THREADS) {
+    CacheEntry e = e0;
+    uint64_t first = first0, order = order0, sum = sum0, ones = ones0;
+    if (b > 0) {
+      e = look_up(p, b + tid, false, steps);
+      first = at_first + block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
+      order = at_order + block_scan<THREADS>(e.heads > 0, s_scan, ones);
+    }
+    at_first += sum;
+    at_order += ones;
+    const bool here = e.heads > 0 && first < st.Z && first + (uint64_t)e.heads * e.steps > st.A;
+    if (here && first <= st.A) s_first_order = (int)order;   // one thread of all: the request that holds step A
+    __syncthreads();
+    if (here) {
+      const int i = (int)order - s_first_order;
+      e.first = (int64_t)first;
+      if (i < kListSmem) s_list[i] = e; else p.list[order] = e;
+      atomicMax(&s_count, i + 1);
+    }
+    __syncthreads();
+  }
+  st.first_order = s_first_order;
+  st.count = s_count;
+  return st;
+}
+
+}  // namespace dsn_q4
