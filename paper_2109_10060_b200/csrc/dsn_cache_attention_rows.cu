@@ -3,17 +3,21 @@
 // One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 128; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
 // rows (fp32) in the workspace, and a second kernel joins them.
-// Roles (416 threads):
-//   warps 0-3    values: codes of the tile after the next come into registers (a thread a token), are turned into bf16 K and V tiles in shared memory, swizzled
-//                as the products read them (two buffers each).  The products need every element only once for 256 rows, so this costs a quarter of their time.
+// Roles (512 threads):
+//   warps 0-3    values: codes of the tile to come are in registers (a thread a token), are turned into fp16 K and V tiles in shared memory, swizzled
+//                as the products read them (two buffers each).  The products need every element only once for 256 rows.
 //   warp 4       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
 //                of one half runs under the products of the other.
-//   warps 5-8    softmax of half 0, warps 9-12 of half 1: a thread a row (= TMEM lane).  Pass 1: the row's maximum; a reference that moves only
-//                when it stands more than 2^8 below, when O is read, scaled and written back.  Pass 2: exp2, sum, probabilities as bf16 over the columns
-//                of S already read, from where the second product takes them.  They also fetch the rows of Q and write those of O.
-// The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (one mask each pair), so Q's and O's columns are in that order, too.
-// TMEM: 512 columns = two regions of 256: S_h 0..127, P_h over 0..63, O_h from 128.
-// Rounded to bf16 besides Q: elements of K and V (once, scale * (code - 8) + middle) and probabilities.  Every wait is bounded.
+//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), the row of S in registers; maximum, exp2, sum, probabilities over
+//                the columns of S, from where the second product takes them.  They also fetch the rows of Q and write those of O.
+// Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
+// goes into the scale of its scores; 32 tokens of a tile have one for K, which goes there, too, and one for V, which the probabilities of
+// those tokens take up.  Everything of a row is in units of 2^g, g a reference that moves only when a probability with its power of two would
+// pass 2^15: then O is read, scaled and written back.
+// The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (a mask each pair), so Q's and O's columns are in that order, too.
+// TMEM: 512 columns = two regions of 256: S_h 0..127, P_h over 0..63, O_h from 128.  Every wait is bounded.
+#include <cuda_fp16.h>
+
 #include "dsn_cache_line.cuh"
 
 namespace {
@@ -21,8 +25,9 @@ namespace {
 using namespace dsn_q4;
 using namespace dsn_gemm;
 
-constexpr int kThreadsR = 416, kRows = 256, kTile = 128;
-constexpr int kValueWarps = 4, kIssueWarp = 4, kSoftWarp = 5;
+constexpr int kThreadsR = 512, kRows = 256, kTile = 128;
+constexpr int kValueWarps = 4, kIssueWarp = 4, kSoftWarp = 8;
+constexpr float kTop = 15.f, kAim = 7.f;     // a probability with its power of two is at most 2^15, 2^7 where the reference has just moved
 constexpr uint32_t kTileBytes = 128 * 128;   // 128 rows of 64 bf16
 constexpr uint32_t kCtrlR = 4096;
 constexpr uint32_t kRegion = 256, kOCol = 128;
@@ -35,19 +40,37 @@ __device__ __forceinline__ void mma_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uin
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// fp16 code - 8 of the elements (0, 4), (1, 5), (2, 6), (3, 7) of a word: the code in the low bits of 1024, or of 1024 + 16 code
+__device__ __forceinline__ void code_pairs(uint32_t w, __half2 (&c)[4]) {
+  const uint32_t x = w >> 8;
+  const uint32_t n[4] = {(w & 0x000f000fu) | 0x64006400u, (w & 0x00f000f0u) | 0x64006400u, (x & 0x000f000fu) | 0x64006400u, (x & 0x00f000f0u) | 0x64006400u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 h = *reinterpret_cast<const __half2*>(&n[i]);
+    c[i] = i & 1 ? __hfma2(h, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hadd2(h, __float2half2_rn(-1032.f));
+  }
+}
 __device__ __forceinline__ void tmem_st_8(uint32_t taddr, const uint32_t (&v)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-__device__ __forceinline__ void tmem_st_32(uint32_t taddr, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void tmem_ld_8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_16(uint32_t taddr, const uint32_t (&v)[32]) {   // the first 16
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
-        "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -160,13 +183,6 @@ __device__ __forceinline__ void half_tiles(const Item& it, int h, int group, int
   if (b < a) b = a;
 }
 
-// Codes of one token of a head, as they lie.
-template <int D>
-struct Raw {
-  uint4 k[D / 32], v[D / 32];
-  uint32_t kp[D / 64], vp[D / 64];
-};
-
 template <int D>
 __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_constant__ CacheAttParams p) {
   constexpr int GR = D / 64;
@@ -179,9 +195,11 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 144);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 148);
   uint8_t* s_bad = smem + 160;                                                     // [4 tiles][4 warps]: blocks of a page outside the cache
-  uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 256);
-  CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 512);
-  static_assert(512 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
+  uint32_t* s_ke = reinterpret_cast<uint32_t*>(smem + 192);                        // the same: biased exponent that K was divided by
+  uint32_t* s_ve = reinterpret_cast<uint32_t*>(smem + 256);                        // and V
+  uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 512);
+  CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 1024);
+  static_assert(1024 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
   const uint32_t q_at = base + kCtrlR, k_at = q_at + 2 * kOperand, v_at = k_at + 2 * kOperand;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -232,55 +250,76 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   }
   Item it;
 
+
   if (warp < kValueWarps) {
     // ------------------------------------------------------------------------------ codes to values
     const int bpp = p.page / DSN_CACHE_BLOCK;
     const int tt = tid;   // this thread's token in a tile
-    Raw<D> r;
-    uint32_t bad = 0;
-    bool have = walk.next(p, it);
+    uint4 kc[D / 32], vc[D / 32];
+    uint32_t kp[GR], vp[GR], bad = 0;
+    bool have = walk.next(p, it), there = false;
     int tile = it.c0;
-    auto fetch = [&]() {   // this thread's token of the walk's current tile
+    const uint8_t* blk = nullptr;   // this thread's token in its block: codes
+    uint32_t pair_at = 0;
+    int pg = -1, tok = 0;
+    bool exists = false;
+    auto find = [&]() {      // the page of this thread's token in the walk's tile
       const int key = it.s.lo + tile * kTile + tt;
-      const bool exists = key <= it.s.me1;
-      int pg = -1, tok = 0;
+      exists = key <= it.s.me1;
+      pg = -1;
+      tok = 0;
       if (exists) {
         const int col = (int)dsn_div((uint32_t)key, p.by_page);
         pg = p.table[(int64_t)it.e.sample * p.max_pages + col];
         tok = key - col * p.page;
       }
-      const bool ok = pg >= 0 && pg < p.n_pages;
-      bad = __ballot_sync(0xffffffffu, exists && !ok);
-      if (exists && !ok) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
-      const uint8_t* blk = p.pages + (((int64_t)(ok ? pg : 0) * p.H + it.head) * bpp + tok / DSN_CACHE_BLOCK) * kBlock;
-      const int t16 = tok % DSN_CACHE_BLOCK;
+    };
+    auto fetch_k = [&]() {
+      there = pg >= 0 && pg < p.n_pages;
+      bad = __ballot_sync(0xffffffffu, exists && !there);
+      if (exists && !there) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
+      const uint32_t t16 = (uint32_t)(tok % DSN_CACHE_BLOCK);
+      blk = p.pages + (((int64_t)(there ? pg : 0) * p.H + it.head) * bpp + tok / DSN_CACHE_BLOCK) * kBlock + t16 * 32u;
+      pair_at = GR * 512u - t16 * 28u;
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          r.k[2 * gr + x] = ok ? *reinterpret_cast<const uint4*>(blk + (gr * 16 + t16) * 32 + 16 * x) : make_uint4(0, 0, 0, 0);
-          r.v[2 * gr + x] = ok ? *reinterpret_cast<const uint4*>(blk + kBlock / 2 + (gr * 16 + t16) * 32 + 16 * x) : make_uint4(0, 0, 0, 0);
-        }
-        r.kp[gr] = ok ? *reinterpret_cast<const uint32_t*>(blk + GR * 512 + (gr * 16 + t16) * 4) : 0u;
-        r.vp[gr] = ok ? *reinterpret_cast<const uint32_t*>(blk + kBlock / 2 + GR * 512 + (gr * 16 + t16) * 4) : 0u;
+        for (int x = 0; x < 2; ++x) kc[2 * gr + x] = there ? *reinterpret_cast<const uint4*>(blk + gr * 512 + 16 * x) : make_uint4(0, 0, 0, 0);
+        kp[gr] = there ? *reinterpret_cast<const uint32_t*>(blk + pair_at + gr * 64) : 0u;
+        vp[gr] = there ? *reinterpret_cast<const uint32_t*>(blk + kBlock / 2 + pair_at + gr * 64) : 0u;
       }
     };
-    auto values = [&](const uint4 (&c)[D / 32], const uint32_t (&pair)[D / 64], uint32_t dst) {
+    auto fetch_v = [&]() {
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) vc[2 * gr + x] = there ? *reinterpret_cast<const uint4*>(blk + kBlock / 2 + gr * 512 + 16 * x) : make_uint4(0, 0, 0, 0);
+    };
+    // exponent of the largest element of the warp's tokens, held where 2^e and 2^-e are normal numbers
+    auto exponent = [&](const uint32_t (&pair)[GR]) -> uint32_t {
+      uint32_t e = 0;
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
-        __nv_bfloat162 s2, z2;
-        *reinterpret_cast<uint32_t*>(&s2) = __byte_perm(pair[gr], pair[gr], 0x1010);
-        *reinterpret_cast<uint32_t*>(&z2) = __byte_perm(pair[gr], pair[gr], 0x3232);
+        const float top = fabsf(hi_bf16(pair[gr])) + 8.f * fabsf(lo_bf16(pair[gr]));
+        if (top <= 3.4e38f) e = max(e, __float_as_uint(top) >> 23);
+      }
+      return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
+    };
+    auto values = [&](const uint4 (&c)[D / 32], const uint32_t (&pair)[GR], uint32_t e, uint32_t dst) {
+      const float down = __uint_as_float((254u - e) << 23);
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+        const __half2 s2 = __float2half2_rn(lo_bf16(pair[gr]) * down), z2 = __float2half2_rn(hi_bf16(pair[gr]) * down);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
           const uint4 q = c[2 * gr + (w >> 2)];
-          const uint32_t word = (w & 3) == 0 ? q.x : (w & 3) == 1 ? q.y : (w & 3) == 2 ? q.z : q.w;
+          __half2 x[4];
+          code_pairs((w & 3) == 0 ? q.x : (w & 3) == 1 ? q.y : (w & 3) == 2 ? q.z : q.w, x);
           uint32_t o[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint32_t n = minus136(nibbles(word >> (4 * i)));
-            const __nv_bfloat162 y = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&n), s2, z2);
-            o[i] = *reinterpret_cast<const uint32_t*>(&y);
+            x[i] = __hfma2(x[i], s2, z2);
+            o[i] = *reinterpret_cast<const uint32_t*>(&x[i]);
           }
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + gr * kTileBytes + (uint32_t)tt * 128u + (uint32_t)((w ^ (tt & 7)) << 4)),
                        "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
@@ -290,28 +329,53 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       fence_async_smem();
       __syncwarp();
     };
-    if (have) fetch();
-    for (uint32_t n = 0; have; ++n) {
-      const uint32_t s = n & 1u;
-      if (n >= 2 && !dsn_wait(k_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
-      if (lane == 0) s_bad[(n & 3u) * 4 + warp] = (uint8_t)((bad & 0xffffu ? 1u : 0u) | (bad >> 16 ? 2u : 0u));
-      values(r.k, r.kp, k_at + s * kOperand);
-      if (lane == 0) mbar_arrive(k_full + 8 * s);
-      if (n >= 2 && !dsn_wait(v_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 82)) break;
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr)   // a token that is not finite shows in its scores; rows that do not see it must not meet it here
-        if (!(fabsf(lo_bf16(r.vp[gr])) <= 3.4e38f) || !(fabsf(hi_bf16(r.vp[gr])) <= 3.4e38f)) r.vp[gr] = 0u;
-      values(r.v, r.vp, v_at + s * kOperand);
-      if (lane == 0) mbar_arrive(v_full + 8 * s);
+    auto step = [&]() {
       if (++tile == it.c1) {
         have = walk.next(p, it);
         tile = it.c0;
       }
-      if (have) fetch();
+    };
+    bool now = have;   // is there a tile in the registers?
+    if (now) {
+      find();
+      fetch_k();
+      fetch_v();
+      step();
+      if (have) find();
+    }
+    for (uint32_t n = 0; now; ++n) {
+      const uint32_t s = n & 1u;
+      if (n >= 2 && !dsn_wait(k_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr)   // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
+        if (!(fabsf(lo_bf16(vp[gr])) <= 3.4e38f) || !(fabsf(hi_bf16(vp[gr])) <= 3.4e38f)) vp[gr] = 0u;
+      const uint32_t ke = exponent(kp), ve = exponent(vp);
+      if (lane == 0) {
+        s_bad[(n & 3u) * 4 + warp] = (uint8_t)((bad & 0xffffu ? 1u : 0u) | (bad >> 16 ? 2u : 0u));
+        s_ke[(n & 3u) * 4 + warp] = ke;
+        s_ve[(n & 3u) * 4 + warp] = ve;
+      }
+      values(kc, kp, ke, k_at + s * kOperand);
+      if (lane == 0) mbar_arrive(k_full + 8 * s);
+      const bool more = have;
+      uint32_t vq[GR];
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) vq[gr] = vp[gr];
+      if (more) fetch_k();
+      if (n >= 2 && !dsn_wait(v_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 82)) break;
+      values(vc, vq, ve, v_at + s * kOperand);
+      if (lane == 0) mbar_arrive(v_full + 8 * s);
+      if (more) {
+        fetch_v();
+        step();
+        if (have) find();
+      }
+      now = more;
     }
   } else if (warp == kIssueWarp) {
     // ------------------------------------------------------------------------------ products
-    const uint32_t idesc_s = make_idesc(128, kTile), idesc_o = make_idesc(128, D) | (1u << 16);   // V: elements first
+    const uint32_t f16 = ~((1u << 7) | (1u << 10));                                               // both operands fp16
+    const uint32_t idesc_s = make_idesc(128, kTile) & f16, idesc_o = (make_idesc(128, D) & f16) | (1u << 16);   // V: elements first
     uint32_t n = 0;                       // tiles so far
     uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, n_o[2] = {0, 0};   // P waited for, Q waited for, items of the half
     bool pend[2] = {false, false}, first_pv[2] = {true, true};
@@ -383,7 +447,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     }
     for (int h = 0; h < 2; ++h)
       if (pend[h] && ok) pv(h, n - 1u);
-  } else {
+  } else if (warp >= kSoftWarp) {
     // ------------------------------------------------------------------------------ softmax, a thread a row
     const int h = (warp - kSoftWarp) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t region = tmem + h * kRegion + ((uint32_t)(quarter * 32) << 16);
@@ -392,36 +456,51 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     const uint32_t q_row = q_at + h * kOperand + (uint32_t)row * 128u;
     uint32_t n_s = 0, n_pv = 0, n = 0;   // S waited for, products with V asked for, tiles so far
     bool ok = true;
-    auto load_q = [&](const Item& x) {
+    // The row of Q as fp16, its largest element brought to 1 .. 2; returns the power of two that goes into the row's scores.
+    auto load_q = [&](const Item& x) -> float {
       const int v = x.s.v0 + 128 * h + row;
       const bool live = v < x.s.v1;
       const int r = v / p.group, ev = v - r * p.group;
       const __nv_bfloat16* src = p.qkv + ((int64_t)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((int64_t)x.head * (p.group + 2) + ev) * D;
+      uint32_t top = 0;   // largest of the magnitudes' bits, two at a time
 #pragma unroll
       for (int c = 0; c < D / 8; ++c) {
         uint4 w = make_uint4(0, 0, 0, 0);
         if (live) w = *reinterpret_cast<const uint4*>(src + 8 * c);
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
+      }
+      uint32_t e = max(top & 0xffffu, top >> 16) >> 7;
+      e = e == 255u ? 127u : min(max(e, 27u), 253u);    // a row that is not finite stays so
+      const float down = __uint_as_float((254u - e) << 23);
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) w = *reinterpret_cast<const uint4*>(src + 8 * c);
+        const uint32_t y0 = w.x ^ flip, y1 = w.y ^ flip, y2 = w.z ^ flip, y3 = w.w ^ flip;
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (uint32_t)(c >> 3) * kTileBytes + (uint32_t)(((c & 7) ^ (row & 7)) << 4)),
-                     "r"(__byte_perm(w.x, w.z, 0x5410) ^ flip), "r"(__byte_perm(w.x, w.z, 0x7632) ^ flip), "r"(__byte_perm(w.y, w.w, 0x5410) ^ flip),
-                     "r"(__byte_perm(w.y, w.w, 0x7632) ^ flip)
+                     "r"(pack_f16(lo_bf16(y0) * down, lo_bf16(y2) * down)), "r"(pack_f16(hi_bf16(y0) * down, hi_bf16(y2) * down)),
+                     "r"(pack_f16(lo_bf16(y1) * down, lo_bf16(y3) * down)), "r"(pack_f16(hi_bf16(y1) * down, hi_bf16(y3) * down))
                      : "memory");
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full + 8 * h);
+      return __uint_as_float(e << 23);
     };
     CachePart ends{3, 0, 0, 0, 0, 0, 0, 0};   // what the CTA has to say about the ends of its stretch; rows: the tail's first vector, pad: one behind its last
     bool have = walk.next(p, it);
     int a = 0, b = 0;
+    float up = 1.f;
     if (have) {
       half_tiles(it, h, p.group, p.window, a, b);
-      if (a < b) load_q(it);
+      if (a < b) up = load_q(it);
     }
     while (have && ok) {
       const int v = it.s.v0 + 128 * h + row;
       const bool live = v < it.s.v1;
       const int me = it.e.len - it.e.rows + v / p.group;
-      float mref = kLowest, l = 0.f;
+      float ref = kLowest, l = 0.f;
+      const float cs = c2 * up;
       for (int j = a; j < b && ok; ++j) {
         ok = dsn_wait(s_full + 8 * h, n_s & 1u, abort_flag, p.status, 88);
         if (!ok) break;
@@ -430,7 +509,14 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         // columns of this tile that the row sees
         const int t0 = it.s.lo + j * kTile;
         const int k1 = me + 1 - t0, k0 = p.window ? me - p.window + 1 - t0 : 0;
-        const uint32_t bad = *reinterpret_cast<const volatile uint32_t*>(s_bad + ((n + (uint32_t)(j - it.c0)) & 3u) * 4);
+        const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 3u;
+        const uint32_t bad = *reinterpret_cast<const volatile uint32_t*>(s_bad + nt * 4);
+        float to[4], shift[4];        // a score of block c to units of the exponent; the power of two of its V
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          to[c] = fmaxf(cs * __uint_as_float(s_ke[nt * 4 + c] << 23), 1e-37f);   // not 0: what is hidden is -infinity
+          shift[c] = (float)((int)s_ve[nt * 4 + c] - 127);
+        }
         const bool cut = __any_sync(0xffffffffu, live && (k1 < kTile || k0 > 0)) || bad != 0;
         auto hide = [&](uint32_t (&x)[32], int c) {   // block c of 32 columns
           const int e1 = min(max(k1 - 32 * c, 0), 32), e0 = min(max(k0 - 32 * c, 0), 32);
@@ -442,84 +528,80 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
           for (int i = 0; i < 32; ++i)
             if (!(m >> i & 1u)) x[i] = 0xff800000u;
         };
-        float m0 = -INFINITY, m1 = -INFINITY;
-        uint32_t va[32], vb[32];
+        // the maximum over blocks 2, 3, then 0, 1, which stay in registers
+        float need = -INFINITY;
+        uint32_t x[2][32];
 #pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-          tmem_ld_32x32(region + 32 * c, va);
-          tmem_ld_32x32(region + 32 * (c + 1), vb);
+        for (int c = 2; c >= 0; c -= 2) {
+          tmem_ld_32x32(region + 32 * c, x[0]);
+          tmem_ld_32x32(region + 32 * (c + 1), x[1]);
           tmem_ld_wait();
-          if (cut) {
-            hide(va, c);
-            hide(vb, c + 1);
-          }
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            m0 = max3_nan(m0, __uint_as_float(va[i]), __uint_as_float(va[i + 1]));
-            m1 = max3_nan(m1, __uint_as_float(vb[i]), __uint_as_float(vb[i + 1]));
+          for (int k = 0; k < 2; ++k) {
+            if (cut) hide(x[k], c + k);
+            float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              m0 = max3_nan(m0, __uint_as_float(x[k][i]), __uint_as_float(x[k][i + 1]));
+              m1 = max3_nan(m1, __uint_as_float(x[k][i + 2]), __uint_as_float(x[k][i + 3]));
+            }
+            need = max3_nan(need, fmaf(m0, to[c + k], shift[c + k]), fmaf(m1, to[c + k], shift[c + k]));
           }
         }
-        const float top = max3_nan(m0, m1, m1) * c2;
-        if (top != top) l = top;   // a token that is not finite: so is the row
-        if (__any_sync(0xffffffffu, top > mref + kSlack)) {
-          const float m = fmaxf(mref, top), f = ex2(mref - m);
-          mref = m;
+        if (need != need) l = need;   // a token that is not finite: so is the row
+        if (__any_sync(0xffffffffu, need > ref + kTop)) {
+          const float m = fmaxf(ref, need - kAim), f = ex2(ref - m);
+          ref = m;
           l *= f;
           if (j > a) {
             ok = dsn_wait(o_full + 8 * h, (n_pv - 1u) & 1u, abort_flag, p.status, 89);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              tmem_ld_32x32(region + kOCol + c, va);
+            for (int c = 0; c < D; c += 8) {
+              uint32_t y[8];
+              tmem_ld_8(region + kOCol + c, y);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) va[i] = __float_as_uint(__uint_as_float(va[i]) * f);
-              tmem_st_32(region + kOCol + c, va);
+              for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+              tmem_st_8(region + kOCol + c, y);
             }
-            tmem_st_done();
           }
         }
-        const uint64_t c2_2 = pack2(c2, c2), ref_2 = pack2(-mref, -mref);
-        uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
         auto block = [&](uint32_t (&x)[32], int c) {
-          if (cut) hide(x, c);
+          const uint64_t to_2 = pack2(to[c], to[c]), ref_2 = pack2(shift[c] - ref, shift[c] - ref);
+          uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
 #pragma unroll
-          for (int half_b = 0; half_b < 2; ++half_b) {
-            uint32_t w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float x0, x1;
-              const uint64_t t2 = ffma2(pack2(__uint_as_float(x[16 * half_b + 2 * e]), __uint_as_float(x[16 * half_b + 2 * e + 1])), c2_2, ref_2);
-              if ((e & 1) && !cut) {
-                exp2_pair(t2, x0, x1);   // every other pair on the FMA pipe
-              } else {
-                float t0f, t1f;
-                unpack2(t2, t0f, t1f);
-                x0 = ex2(t0f);
-                x1 = ex2(t1f);
-              }
-              if (e & 2) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
-              w[e] = pack_bf16(x0, x1);
+          for (int e = 0; e < 16; ++e) {
+            float x0, x1;
+            const uint64_t t2 = ffma2(pack2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), to_2, ref_2);
+            if ((e & 3) == 3 && !cut) {
+              exp2_pair(t2, x0, x1);   // some on the FMA pipe
+            } else {
+              float t0f, t1f;
+              unpack2(t2, t0f, t1f);
+              x0 = ex2(t0f);
+              x1 = ex2(t1f);
             }
-            tmem_st_8(region + (uint32_t)(16 * c + 8 * half_b), w);
+            if (e & 1) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
+            x[e] = pack_f16(x0, x1);
           }
+          tmem_st_16(region + (uint32_t)(16 * c), x);
+          float s0, s1;
+          unpack2(fadd2(sum_a, sum_b), s0, s1);
+          l = fmaf(s0 + s1, __uint_as_float((254u - s_ve[nt * 4 + c]) << 23), l);   // in units of 2^ref, without V's power
         };
-        tmem_ld_32x32(region, va);
+        block(x[0], 0);
+        block(x[1], 1);
+        tmem_ld_32x32(region + 64, x[0]);
+        tmem_ld_32x32(region + 96, x[1]);
         tmem_ld_wait();
-#pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-          tmem_ld_32x32(region + 32 * (c + 1), vb);
-          block(va, c);
-          tmem_ld_wait();
-          if (c + 2 < 4) tmem_ld_32x32(region + 32 * (c + 2), va);
-          block(vb, c + 1);
-          tmem_ld_wait();
+        if (cut) {
+          hide(x[0], 2);
+          hide(x[1], 3);
         }
-        float s0, s1, s2, s3;
-        unpack2(sum_a, s0, s1);
-        unpack2(sum_b, s2, s3);
-        l += (s0 + s1) + (s2 + s3);
+        block(x[0], 2);
+        block(x[1], 3);
         tmem_st_done();
         tc_fence_before();
         __syncwarp();
@@ -534,7 +616,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       have = walk.next(p, it);
       if (have) {
         half_tiles(it, h, p.group, p.window, a, b);
-        if (a < b) load_q(it);
+        if (a < b) up = load_q(it);
       }
       if (ran) {
         ok = dsn_wait(o_full + 8 * h, (n_pv - 1u) & 1u, abort_flag, p.status, 90);
@@ -583,7 +665,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         }
       }
       if (!whole && live) {
-        part[0] = mref;
+        part[0] = ref;
         part[kRows] = l;
       }
       if (cur.c0 > 0) ends.head_state = cur.c1 == cur.s.tiles ? 1 : 2;
