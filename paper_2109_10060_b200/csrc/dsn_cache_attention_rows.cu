@@ -390,9 +390,10 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (elect_one()) {
         tc_fence_after();
         const uint32_t region = tmem + h * kRegion;
+        const uint64_t dv = make_desc_mn(v_at + s * kOperand);
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks)
-          mma_a_tmem(region + kOCol, region + 8u * ks, make_desc_mn(v_at + s * kOperand + ks * 2048), idesc_o, first_pv[h] && ks == 0 ? 0u : 1u);
+          mma_a_tmem(region + kOCol, region + 8u * ks, dv + 128u * ks, idesc_o, ks > 0 ? 1u : (first_pv[h] ? 0u : 1u));
         umma_commit(o_full + 8 * h);
       }
       __syncwarp();
@@ -427,11 +428,11 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
             if (!ok) break;
             if (elect_one()) {
               tc_fence_after();
+              const uint64_t dq = make_smem_desc(q_at + h * kOperand), dk = make_smem_desc(k_at + s * kOperand);
 #pragma unroll
               for (int ks = 0; ks < D / 16; ++ks) {
-                const uint32_t off = (uint32_t)(ks >> 2) * kTileBytes;
-                umma_bf16(tmem + h * kRegion, make_smem_desc(q_at + h * kOperand + off) + 2u * (ks & 3), make_smem_desc(k_at + s * kOperand + off) + 2u * (ks & 3),
-                          idesc_s, ks > 0 ? 1u : 0u);
+                const uint32_t off = (uint32_t)(ks >> 2) * (kTileBytes >> 4) + 2u * (ks & 3);
+                umma_bf16(tmem + h * kRegion, dq + off, dk + off, idesc_s, ks > 0 ? 1u : 0u);
               }
               umma_commit(s_full + 8 * h);
             }
@@ -531,21 +532,28 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         // the maximum over blocks 2, 3, then 0, 1, which stay in registers
         float need = -INFINITY;
         uint32_t x[2][32];
-#pragma unroll
+#pragma unroll 1
         for (int c = 2; c >= 0; c -= 2) {
           tmem_ld_32x32(region + 32 * c, x[0]);
           tmem_ld_32x32(region + 32 * (c + 1), x[1]);
           tmem_ld_wait();
+          if (cut) {
+            hide(x[0], c);
+            hide(x[1], c + 1);
+          }
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            if (cut) hide(x[k], c + k);
-            float m0 = -INFINITY, m1 = -INFINITY;
+            const float t = c ? to[2 + k] : to[k], sh = c ? shift[2 + k] : shift[k];
+            float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
+            for (int i = 0; i < 32; i += 8) {
               m0 = max3_nan(m0, __uint_as_float(x[k][i]), __uint_as_float(x[k][i + 1]));
               m1 = max3_nan(m1, __uint_as_float(x[k][i + 2]), __uint_as_float(x[k][i + 3]));
+              m2 = max3_nan(m2, __uint_as_float(x[k][i + 4]), __uint_as_float(x[k][i + 5]));
+              m3 = max3_nan(m3, __uint_as_float(x[k][i + 6]), __uint_as_float(x[k][i + 7]));
             }
-            need = max3_nan(need, fmaf(m0, to[c + k], shift[c + k]), fmaf(m1, to[c + k], shift[c + k]));
+            m0 = max3_nan(m0, m1, m2);
+            need = max3_nan(need, fmaf(m0, t, sh), fmaf(m3, t, sh));
           }
         }
         if (need != need) l = need;   // a token that is not finite: so is the row
@@ -568,15 +576,15 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
             }
           }
         }
-        auto block = [&](uint32_t (&x)[32], int c) {
-          const uint64_t to_2 = pack2(to[c], to[c]), ref_2 = pack2(shift[c] - ref, shift[c] - ref);
+        auto block = [&](uint32_t (&x)[32], int c, float t, float sh) {
+          const uint64_t to_2 = pack2(t, t), ref_2 = pack2(sh - ref, sh - ref);
           uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float x0, x1;
             const uint64_t t2 = ffma2(pack2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), to_2, ref_2);
-            if ((e & 3) == 3 && !cut) {
-              exp2_pair(t2, x0, x1);   // some on the FMA pipe
+            if ((e & 3) == 3) {
+              exp2_pair(t2, x0, x1);   // some on the FMA pipe; what is hidden comes out as 2^-126, a zero in fp16
             } else {
               float t0f, t1f;
               unpack2(t2, t0f, t1f);
@@ -589,19 +597,22 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
           tmem_st_16(region + (uint32_t)(16 * c), x);
           float s0, s1;
           unpack2(fadd2(sum_a, sum_b), s0, s1);
-          l = fmaf(s0 + s1, __uint_as_float((254u - s_ve[nt * 4 + c]) << 23), l);   // in units of 2^ref, without V's power
+          l = fmaf(s0 + s1, __uint_as_float((127u - (uint32_t)(int)sh) << 23), l);   // in units of 2^ref, without V's power
         };
-        block(x[0], 0);
-        block(x[1], 1);
-        tmem_ld_32x32(region + 64, x[0]);
-        tmem_ld_32x32(region + 96, x[1]);
-        tmem_ld_wait();
-        if (cut) {
-          hide(x[0], 2);
-          hide(x[1], 3);
+#pragma unroll 1
+        for (int c = 0; c < 4; c += 2) {
+          if (c) {
+            tmem_ld_32x32(region + 64, x[0]);
+            tmem_ld_32x32(region + 96, x[1]);
+            tmem_ld_wait();
+            if (cut) {
+              hide(x[0], 2);
+              hide(x[1], 3);
+            }
+          }
+          block(x[0], c, c ? to[2] : to[0], c ? shift[2] : shift[0]);
+          block(x[1], c + 1, c ? to[3] : to[1], c ? shift[3] : shift[1]);
         }
-        block(x[0], 2);
-        block(x[1], 3);
         tmem_st_done();
         tc_fence_before();
         __syncwarp();
