@@ -61,7 +61,7 @@ struct CacheAttParams {
   int16_t heads[DSN_MAX_SLICES];
   int32_t B, R, H, group, G, T, page, n_pages, max_pages, max_heads, grouped, window;
   float scale_log2;     // scale of the scores times log2(e)
-  FastDiv by_page;
+  FastDiv by_page, by_group;
   const int32_t* offsets;
   const int32_t* perm;
   const int32_t* group_slice;

@@ -3,12 +3,12 @@
 // One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 128; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
 // rows (fp32) in the workspace, and a second kernel joins them.
-// Roles (512 threads):
-//   warps 0-3    values: codes of the tile to come are in registers (a thread a token), are turned into fp16 K and V tiles in shared memory, swizzled
-//                as the products read them (two buffers each).  The products need every element only once for 256 rows.
-//   warp 4       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
+// Roles (384 threads, 168 registers each):
+//   warps 0-2    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, two buffers each; a unit is K or V of 32 tokens, a token a
+//                lane; its codes come as bulk copies, three units ahead.  Every element is made once for 256 rows.
+//   warp 3       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
 //                of one half runs under the products of the other.
-//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), the row of S in registers; maximum, exp2, sum, probabilities over
+//   warps 4-7    softmax of half 0, warps 8-11 of half 1: a thread a row (= TMEM lane), half a row of S in registers; maximum, exp2, sum, probabilities over
 //                the columns of S, from where the second product takes them.  They also fetch the rows of Q and write those of O.
 // Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
 // goes into the scale of its scores; 32 tokens of a tile have one for K, which goes there, too, and one for V, which the probabilities of
@@ -25,11 +25,14 @@ namespace {
 using namespace dsn_q4;
 using namespace dsn_gemm;
 
-constexpr int kThreadsR = 512, kRows = 256, kTile = 128;
-constexpr int kValueWarps = 4, kIssueWarp = 4, kSoftWarp = 8;
+constexpr int kThreadsR = 384, kRows = 256, kTile = 128;
+constexpr int kValueWarps = 3, kIssueWarp = 3, kSoftWarp = 4;
 constexpr float kTop = 15.f, kAim = 7.f;     // a probability with its power of two is at most 2^15, 2^7 where the reference has just moved
 constexpr uint32_t kTileBytes = 128 * 128;   // 128 rows of 64 bf16
 constexpr uint32_t kCtrlR = 4096;
+constexpr uint32_t kRawDepth = 3;            // units in a warp's ring of codes
+template <int D>
+__host__ __device__ constexpr uint32_t unit_bytes() { return 2u * (9u * D + D); }   // two blocks: codes and pairs of a half, pairs of V
 constexpr uint32_t kRegion = 256, kOCol = 128;
 
 __device__ __forceinline__ void mma_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -114,21 +117,21 @@ struct Span {
   int me0, me1;       // tokens of the first and the last
   int lo, tiles;      // first token of the first tile, tiles
 };
-__device__ __forceinline__ Span span_of(int len, int rows, int ct, int group, int window) {
+__device__ __forceinline__ Span span_of(int len, int rows, int ct, int group, const FastDiv& by_group, int window) {
   Span s;
   s.v0 = ct * kRows;
   s.v1 = min(rows * group, s.v0 + kRows);
   const int first = len - rows;
-  s.me0 = first + s.v0 / group;
-  s.me1 = first + (s.v1 - 1) / group;
+  s.me0 = first + (int)dsn_div((uint32_t)s.v0, by_group);
+  s.me1 = first + (int)dsn_div((uint32_t)(s.v1 - 1), by_group);
   s.lo = window ? max(0, s.me0 - window + 1) & ~(DSN_CACHE_BLOCK - 1) : 0;
   s.tiles = max(1, (s.me1 + 1 - s.lo + kTile - 1) / kTile);
   return s;
 }
-__device__ __forceinline__ int head_tiles(int len, int rows, int group, int window) {
+__device__ __forceinline__ int head_tiles(int len, int rows, int group, const FastDiv& by_group, int window) {
   const int cts = (rows * group + kRows - 1) / kRows;
   int sum = 0;
-  for (int ct = 0; ct < cts; ++ct) sum += span_of(len, rows, ct, group, window).tiles;
+  for (int ct = 0; ct < cts; ++ct) sum += span_of(len, rows, ct, group, by_group, window).tiles;
   return sum;
 }
 
@@ -152,7 +155,7 @@ struct RowWalk {
     if (left <= 0) return false;
     it.e = e;
     it.head = head;
-    it.s = span_of(e.len, e.rows, ct, p.group, p.window);
+    it.s = span_of(e.len, e.rows, ct, p.group, p.by_group, p.window);
     it.c0 = c0;
     it.c1 = (int)min((int64_t)it.s.tiles, c0 + left);
     left -= it.c1 - it.c0;
@@ -172,11 +175,11 @@ struct RowWalk {
   }
 };
 // Tiles of the CTA's part that half h of the item needs: a .. b - 1 (none: a == b).
-__device__ __forceinline__ void half_tiles(const Item& it, int h, int group, int window, int& a, int& b) {
+__device__ __forceinline__ void half_tiles(const Item& it, int h, const FastDiv& by_group, int window, int& a, int& b) {
   const int w0 = it.s.v0 + 128 * h, w1 = min(it.s.v1, w0 + 128);
   a = b = it.c0;
   if (w0 >= w1) return;
-  const int first = it.e.len - it.e.rows, m0 = first + w0 / group, m1 = first + (w1 - 1) / group;
+  const int first = it.e.len - it.e.rows, m0 = first + (int)dsn_div((uint32_t)w0, by_group), m1 = first + (int)dsn_div((uint32_t)(w1 - 1), by_group);
   if (m1 < 0) return;
   a = max(it.c0, ((window ? max(0, m0 - window + 1) : 0) - it.s.lo) / kTile);
   b = min(it.c1, (m1 + 1 - it.s.lo + kTile - 1) / kTile);
@@ -186,12 +189,13 @@ __device__ __forceinline__ void half_tiles(const Item& it, int h, int group, int
 template <int D>
 __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_constant__ CacheAttParams p) {
   constexpr int GR = D / 64;
-  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes;
+  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes, kUnit = unit_bytes<D>();
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (base - raw);
   const uint32_t q_full = base, k_full = base + 16, v_full = base + 32, k_empty = base + 48, v_empty = base + 64, s_full = base + 80,
                  p_full = base + 96, o_full = base + 112, o_empty = base + 128;   // [2] each
+  const uint32_t raw_full = base + 320;   // [3 warps][kRawDepth]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 144);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 148);
   uint8_t* s_bad = smem + 160;                                                     // [4 tiles][4 warps]: blocks of a page outside the cache
@@ -200,7 +204,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 512);
   CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 1024);
   static_assert(1024 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
-  const uint32_t q_at = base + kCtrlR, k_at = q_at + 2 * kOperand, v_at = k_at + 2 * kOperand;
+  const uint32_t q_at = base + kCtrlR, k_at = q_at + 2 * kOperand, v_at = k_at + 2 * kOperand, raw_at = v_at + 2 * kOperand;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   dsn_grid_dependency_wait();
@@ -208,8 +212,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full + 8 * i, 4);
-      mbar_init(k_full + 8 * i, kValueWarps);
-      mbar_init(v_full + 8 * i, kValueWarps);
+      mbar_init(k_full + 8 * i, 4);   // units of 32 tokens
+      mbar_init(v_full + 8 * i, 4);
       mbar_init(k_empty + 8 * i, 1);
       mbar_init(v_empty + 8 * i, 1);
       mbar_init(s_full + 8 * i, 1);
@@ -217,10 +221,11 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       mbar_init(o_full + 8 * i, 1);
       mbar_init(o_empty + 8 * i, 4);
     }
+    for (int i = 0; i < kValueWarps * (int)kRawDepth; ++i) mbar_init(raw_full + 8 * i, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.window); });
+  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.by_group, p.window); });
   if (warp == kIssueWarp) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
@@ -241,7 +246,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     int in_head = (int)(off - (uint64_t)walk.head * walk.e.steps);
     walk.ct = 0;
     while (true) {
-      const int n = span_of(walk.e.len, walk.e.rows, walk.ct, p.group, p.window).tiles;
+      const int n = span_of(walk.e.len, walk.e.rows, walk.ct, p.group, p.by_group, p.window).tiles;
       if (in_head < n) break;
       in_head -= n;
       ++walk.ct;
@@ -253,49 +258,50 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
 
   if (warp < kValueWarps) {
     // ------------------------------------------------------------------------------ codes to values
+    // This warp's units are numbers warp, warp + 3, ... of all.  A unit's codes and pairs come as bulk copies into a slot of the warp's own ring, three units ahead
+    // (K's with V's pairs beside them); the page's number was read a unit before that.  Lanes 0 and 1 fetch a block of 16 tokens each.
     const int bpp = p.page / DSN_CACHE_BLOCK;
-    const int tt = tid;   // this thread's token in a tile
-    uint4 kc[D / 32], vc[D / 32];
-    uint32_t kp[GR], vp[GR], bad = 0;
-    bool have = walk.next(p, it), there = false;
+    const uint32_t ring = raw_at + (uint32_t)warp * (kRawDepth * kUnit), full = raw_full + (uint32_t)warp * (8 * kRawDepth);
+    uint32_t number = (uint32_t)warp, walk_n = 0;     // the unit that the walk stands at, and its tile
+    bool more = walk.next(p, it);
     int tile = it.c0;
-    const uint8_t* blk = nullptr;   // this thread's token in its block: codes
-    uint32_t pair_at = 0;
-    int pg = -1, tok = 0;
+    int pg = -1, place = 0;                           // page of this lane's block and the block in it
     bool exists = false;
-    auto find = [&]() {      // the page of this thread's token in the walk's tile
-      const int key = it.s.lo + tile * kTile + tt;
-      exists = key <= it.s.me1;
+    auto find = [&]() {
+      while (more && walk_n < (number >> 3)) {
+        ++walk_n;
+        if (++tile == it.c1) {
+          more = walk.next(p, it);
+          tile = it.c0;
+        }
+      }
+      const int key = it.s.lo + tile * kTile + 32 * (int)(number & 3u) + DSN_CACHE_BLOCK * lane;
+      exists = more && lane < 2 && key <= it.s.me1;
       pg = -1;
-      tok = 0;
       if (exists) {
         const int col = (int)dsn_div((uint32_t)key, p.by_page);
         pg = p.table[(int64_t)it.e.sample * p.max_pages + col];
-        tok = key - col * p.page;
+        place = key / DSN_CACHE_BLOCK - col * bpp;
       }
     };
-    auto fetch_k = [&]() {
-      there = pg >= 0 && pg < p.n_pages;
-      bad = __ballot_sync(0xffffffffu, exists && !there);
-      if (exists && !there) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
-      const uint32_t t16 = (uint32_t)(tok % DSN_CACHE_BLOCK);
-      blk = p.pages + (((int64_t)(there ? pg : 0) * p.H + it.head) * bpp + tok / DSN_CACHE_BLOCK) * kBlock + t16 * 32u;
-      pair_at = GR * 512u - t16 * 28u;
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) kc[2 * gr + x] = there ? *reinterpret_cast<const uint4*>(blk + gr * 512 + 16 * x) : make_uint4(0, 0, 0, 0);
-        kp[gr] = there ? *reinterpret_cast<const uint32_t*>(blk + pair_at + gr * 64) : 0u;
-        vp[gr] = there ? *reinterpret_cast<const uint32_t*>(blk + kBlock / 2 + pair_at + gr * 64) : 0u;
+    auto fetch = [&](uint32_t slot) -> uint32_t {     // copies of the unit that was found; bit b: block b is missing, bit 2 + b: it is on its way
+      const bool ok = pg >= 0 && pg < p.n_pages, lost = exists && !ok;
+      if (lost) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
+      const uint32_t go = __ballot_sync(0xffffffffu, ok), bad = __ballot_sync(0xffffffffu, lost);
+      const bool is_v = (number & 4u) != 0;
+      const uint32_t bytes = 9u * D + (is_v ? 0u : 64u * GR);
+      if (lane == 0) mbar_expect_tx(full + 8 * slot, (uint32_t)__popc(go) * bytes);
+      __syncwarp();
+      if (ok) {
+        const uint8_t* blk = p.pages + (((int64_t)pg * p.H + it.head) * bpp + place) * kBlock;
+        const uint32_t dst = ring + slot * kUnit + (uint32_t)lane * (kUnit / 2);
+        dsn_bulk_load(dst, blk + (is_v ? kBlock / 2 : 0u), 9u * D, full + 8 * slot);
+        if (!is_v) dsn_bulk_load(dst + 9u * D, blk + kBlock / 2 + GR * 512, 64u * GR, full + 8 * slot);
       }
+      number += kValueWarps;
+      return bad | (go << 2);
     };
-    auto fetch_v = [&]() {
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) vc[2 * gr + x] = there ? *reinterpret_cast<const uint4*>(blk + kBlock / 2 + gr * 512 + 16 * x) : make_uint4(0, 0, 0, 0);
-    };
-    // exponent of the largest element of the warp's tokens, held where 2^e and 2^-e are normal numbers
+    // exponent of the largest element of the unit, held where 2^e and 2^-e are normal numbers
     auto exponent = [&](const uint32_t (&pair)[GR]) -> uint32_t {
       uint32_t e = 0;
 #pragma unroll
@@ -305,73 +311,84 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       }
       return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
     };
-    auto values = [&](const uint4 (&c)[D / 32], const uint32_t (&pair)[GR], uint32_t e, uint32_t dst) {
-      const float down = __uint_as_float((254u - e) << 23);
+    uint32_t asked = 0, state = 0, live = 0;          // units asked for; four bits a slot; a bit a slot
+    int ends[kRawDepth];                              // tokens of the unit that exist
+    find();
+#pragma unroll
+    for (uint32_t i = 0; i < kRawDepth; ++i) {
+      ends[i] = 0;
+      if (more) {
+        live |= 1u << i;
+        ends[i] = it.s.me1 + 1 - (it.s.lo + tile * kTile + 32 * (int)(number & 3u));
+        state |= fetch(i) << (4 * i);
+        ++asked;
+        find();
+      }
+    }
+    uint32_t slot = 0, turn = 0;
+    for (uint32_t which = (uint32_t)warp; live >> slot & 1u; which += kValueWarps) {
+      const uint32_t n = which >> 3, s = n & 1u, blk32 = which & 3u, flags = state >> (4 * slot);
+      const bool is_v = (which & 4u) != 0;
+      const int end = slot == 0 ? ends[0] : slot == 1 ? ends[1] : ends[2];
+      if (!dsn_wait(full + 8 * slot, turn, abort_flag, p.status, 82)) break;
+      const uint32_t src = ring + slot * kUnit + (uint32_t)(lane >> 4) * (kUnit / 2), t16 = (uint32_t)lane & 15u;
+      const bool there = (flags >> (2 + (lane >> 4)) & 1u) && lane < end;
+      uint32_t pair[GR], v_pair[GR];
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
-        const __half2 s2 = __float2half2_rn(lo_bf16(pair[gr]) * down), z2 = __float2half2_rn(hi_bf16(pair[gr]) * down);
+        pair[gr] = there ? lds32(src + GR * 512 + gr * 64 + t16 * 4) : 0u;
+        v_pair[gr] = there ? (is_v ? pair[gr] : lds32(src + 9 * D + gr * 64 + t16 * 4)) : 0u;
+        // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
+        if (!(fabsf(lo_bf16(v_pair[gr])) <= 3.4e38f) || !(fabsf(hi_bf16(v_pair[gr])) <= 3.4e38f)) v_pair[gr] = 0u;
+      }
+      const uint32_t ve = exponent(v_pair), e = is_v ? ve : exponent(pair);
+      if (n >= 2 && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
+      if (!is_v && lane == 0) {
+        const uint32_t k = (n & 3u) * 4 + blk32;
+        s_bad[k] = (uint8_t)(flags & 3u);
+        s_ke[k] = e;
+        s_ve[k] = ve;
+      }
+      const float down = __uint_as_float((254u - e) << 23);
+      const uint32_t dst = (is_v ? v_at : k_at) + s * kOperand + (blk32 * 32u + (uint32_t)lane) * 128u;
+#pragma unroll 1
+      for (int i = 0; i < 2 * GR; ++i) {              // 32 elements at a time
+        const int gr = i >> 1;
+        const uint32_t pr = GR == 1 || gr == 0 ? (is_v ? v_pair[0] : pair[0]) : (is_v ? v_pair[GR - 1] : pair[GR - 1]);
+        const __half2 s2 = __float2half2_rn(lo_bf16(pr) * down), z2 = __float2half2_rn(hi_bf16(pr) * down);
+        uint32_t q[4];
+        lds128(src + gr * 512 + t16 * 32 + 16 * (i & 1), q);
+        const uint32_t to = dst + gr * kTileBytes;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          const uint4 q = c[2 * gr + (w >> 2)];
+        for (int w = 0; w < 4; ++w) {
           __half2 x[4];
-          code_pairs((w & 3) == 0 ? q.x : (w & 3) == 1 ? q.y : (w & 3) == 2 ? q.z : q.w, x);
+          code_pairs(q[w], x);
           uint32_t o[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[i] = __hfma2(x[i], s2, z2);
-            o[i] = *reinterpret_cast<const uint32_t*>(&x[i]);
+          for (int j = 0; j < 4; ++j) {
+            x[j] = __hfma2(x[j], s2, z2);
+            o[j] = *reinterpret_cast<const uint32_t*>(&x[j]);
           }
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + gr * kTileBytes + (uint32_t)tt * 128u + (uint32_t)((w ^ (tt & 7)) << 4)),
-                       "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(((4 * (i & 1) + w) ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]),
+                       "r"(o[3])
                        : "memory");
         }
       }
       fence_async_smem();
-      __syncwarp();
-    };
-    auto step = [&]() {
-      if (++tile == it.c1) {
-        have = walk.next(p, it);
-        tile = it.c0;
-      }
-    };
-    bool now = have;   // is there a tile in the registers?
-    if (now) {
-      find();
-      fetch_k();
-      fetch_v();
-      step();
-      if (have) find();
-    }
-    for (uint32_t n = 0; now; ++n) {
-      const uint32_t s = n & 1u;
-      if (n >= 2 && !dsn_wait(k_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr)   // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
-        if (!(fabsf(lo_bf16(vp[gr])) <= 3.4e38f) || !(fabsf(hi_bf16(vp[gr])) <= 3.4e38f)) vp[gr] = 0u;
-      const uint32_t ke = exponent(kp), ve = exponent(vp);
-      if (lane == 0) {
-        s_bad[(n & 3u) * 4 + warp] = (uint8_t)((bad & 0xffffu ? 1u : 0u) | (bad >> 16 ? 2u : 0u));
-        s_ke[(n & 3u) * 4 + warp] = ke;
-        s_ve[(n & 3u) * 4 + warp] = ve;
-      }
-      values(kc, kp, ke, k_at + s * kOperand);
-      if (lane == 0) mbar_arrive(k_full + 8 * s);
-      const bool more = have;
-      uint32_t vq[GR];
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr) vq[gr] = vp[gr];
-      if (more) fetch_k();
-      if (n >= 2 && !dsn_wait(v_empty + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 82)) break;
-      values(vc, vq, ve, v_at + s * kOperand);
-      if (lane == 0) mbar_arrive(v_full + 8 * s);
+      __syncwarp();   // every lane has read the slot and written its rows
+      if (lane == 0) mbar_arrive((is_v ? v_full : k_full) + 8 * s);
+      live &= ~(1u << slot);
       if (more) {
-        fetch_v();
-        step();
-        if (have) find();
+        live |= 1u << slot;
+        const int left = it.s.me1 + 1 - (it.s.lo + tile * kTile + 32 * (int)(number & 3u));
+        if (slot == 0) ends[0] = left; else if (slot == 1) ends[1] = left; else ends[2] = left;
+        state = (state & ~(15u << (4 * slot))) | (fetch(slot) << (4 * slot));
+        ++asked;
+        find();
       }
-      now = more;
+      if (++slot == kRawDepth) slot = 0, turn ^= 1u;
     }
+    if (*abort_flag) dsn_drain(full, kRawDepth, 0, (int)asked);
   } else if (warp == kIssueWarp) {
     // ------------------------------------------------------------------------------ products
     const uint32_t f16 = ~((1u << 7) | (1u << 10));                                               // both operands fp16
@@ -406,8 +423,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     };
     while (ok && walk.next(p, it)) {
       int a[2], b[2];
-      half_tiles(it, 0, p.group, p.window, a[0], b[0]);
-      half_tiles(it, 1, p.group, p.window, a[1], b[1]);
+      half_tiles(it, 0, p.by_group, p.window, a[0], b[0]);
+      half_tiles(it, 1, p.by_group, p.window, a[1], b[1]);
       for (int j = it.c0; j < it.c1 && ok; ++j, ++n) {
         const uint32_t s = n & 1u;
         if (j == it.c0) {   // what the item before still needs comes first: this item's Q arrives only behind its softmax
@@ -454,52 +471,63 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     const uint32_t region = tmem + h * kRegion + ((uint32_t)(quarter * 32) << 16);
     const float c2 = fabsf(p.scale_log2);
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale goes into Q's signs
-    const uint32_t q_row = q_at + h * kOperand + (uint32_t)row * 128u;
     uint32_t n_s = 0, n_pv = 0, n = 0;   // S waited for, products with V asked for, tiles so far
     bool ok = true;
-    // The row of Q as fp16, its largest element brought to 1 .. 2; returns the power of two that goes into the row's scores.
+    // The warp's rows of Q as fp16, the largest element of each brought to 1 .. 2; returns the power of two that goes into the scores of this lane's row.
+    // D / 8 lanes read a row.
     auto load_q = [&](const Item& x) -> float {
+      constexpr int L = D / 8, PER = 32 / L, NB = L;   // lanes a row, rows a load, loads at once
       const int v = x.s.v0 + 128 * h + row;
-      const bool live = v < x.s.v1;
-      const int r = v / p.group, ev = v - r * p.group;
-      const __nv_bfloat16* src = p.qkv + ((int64_t)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((int64_t)x.head * (p.group + 2) + ev) * D;
-      uint32_t top = 0;   // largest of the magnitudes' bits, two at a time
+      const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
+      const long long mine = v < x.s.v1 ? ((long long)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((long long)x.head * (p.group + 2) + ev) * D
+                                        : -1;
+      const int sub = lane % L, of = lane / L;
+      uint32_t my_e = 127u;
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (live) w = *reinterpret_cast<const uint4*>(src + 8 * c);
-        top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
-      }
-      uint32_t e = max(top & 0xffffu, top >> 16) >> 7;
-      e = e == 255u ? 127u : min(max(e, 27u), 253u);    // a row that is not finite stays so
-      const float down = __uint_as_float((254u - e) << 23);
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (live) w = *reinterpret_cast<const uint4*>(src + 8 * c);
-        const uint32_t y0 = w.x ^ flip, y1 = w.y ^ flip, y2 = w.z ^ flip, y3 = w.w ^ flip;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (uint32_t)(c >> 3) * kTileBytes + (uint32_t)(((c & 7) ^ (row & 7)) << 4)),
-                     "r"(pack_f16(lo_bf16(y0) * down, lo_bf16(y2) * down)), "r"(pack_f16(hi_bf16(y0) * down, hi_bf16(y2) * down)),
-                     "r"(pack_f16(lo_bf16(y1) * down, lo_bf16(y3) * down)), "r"(pack_f16(hi_bf16(y1) * down, hi_bf16(y3) * down))
-                     : "memory");
+      for (int b = 0; b < 32; b += NB * PER) {
+        uint4 w[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const long long at = __shfl_sync(0xffffffffu, mine, b + i * PER + of);
+          w[i] = at >= 0 ? *reinterpret_cast<const uint4*>(p.qkv + at + 8 * sub) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const int rr = b + i * PER + of, row_at = quarter * 32 + rr;
+          const uint32_t m2 = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
+          uint32_t e = max(m2 & 0xffffu, m2 >> 16);
+#pragma unroll
+          for (int o = 1; o < L; o <<= 1) e = max(e, __shfl_xor_sync(0xffffffffu, e, o));
+          e >>= 7;
+          e = e == 255u ? 127u : min(max(e, 27u), 253u);    // a row that is not finite stays so
+          const uint32_t given = __shfl_sync(0xffffffffu, e, (lane % PER) * L);
+          if (lane / PER == b / PER + i) my_e = given;
+          const float down = __uint_as_float((254u - e) << 23);
+          const uint32_t y0 = w[i].x ^ flip, y1 = w[i].y ^ flip, y2 = w[i].z ^ flip, y3 = w[i].w ^ flip;
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_at + h * kOperand + (uint32_t)row_at * 128u + (uint32_t)(sub >> 3) * kTileBytes +
+                                                                        (uint32_t)(((sub & 7) ^ (row_at & 7)) << 4)),
+                       "r"(pack_f16(lo_bf16(y0) * down, lo_bf16(y2) * down)), "r"(pack_f16(hi_bf16(y0) * down, hi_bf16(y2) * down)),
+                       "r"(pack_f16(lo_bf16(y1) * down, lo_bf16(y3) * down)), "r"(pack_f16(hi_bf16(y1) * down, hi_bf16(y3) * down))
+                       : "memory");
+        }
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full + 8 * h);
-      return __uint_as_float(e << 23);
+      return __uint_as_float(my_e << 23);
     };
     CachePart ends{3, 0, 0, 0, 0, 0, 0, 0};   // what the CTA has to say about the ends of its stretch; rows: the tail's first vector, pad: one behind its last
     bool have = walk.next(p, it);
     int a = 0, b = 0;
     float up = 1.f;
     if (have) {
-      half_tiles(it, h, p.group, p.window, a, b);
+      half_tiles(it, h, p.by_group, p.window, a, b);
       if (a < b) up = load_q(it);
     }
     while (have && ok) {
       const int v = it.s.v0 + 128 * h + row;
       const bool live = v < it.s.v1;
-      const int me = it.e.len - it.e.rows + v / p.group;
+      const int me = it.e.len - it.e.rows + (int)dsn_div((uint32_t)v, p.by_group);
       float ref = kLowest, l = 0.f;
       const float cs = c2 * up;
       for (int j = a; j < b && ok; ++j) {
@@ -626,7 +654,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       n += (uint32_t)(cur.c1 - cur.c0);
       have = walk.next(p, it);
       if (have) {
-        half_tiles(it, h, p.group, p.window, a, b);
+        half_tiles(it, h, p.by_group, p.window, a, b);
         if (a < b) up = load_q(it);
       }
       if (ran) {
@@ -635,7 +663,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         tc_fence_after();
       }
       const bool whole = cur.c0 == 0 && cur.c1 == cur.s.tiles;
-      const int r = v / p.group, ev = v - r * p.group;
+      const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? cur.e.pos : cur.e.sample) * p.R + r) * p.ld_out + ((int64_t)cur.head * p.group + ev) * D;
       // a part: references, sums, then four elements of every row after the other
@@ -741,7 +769,7 @@ __global__ void __launch_bounds__(kRows) cache_rows_join_kernel(const __grid_con
 template <int D>
 cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
   static size_t configured[DSN_MAX_DEVICES] = {};
-  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes;
+  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes + kValueWarps * kRawDepth * unit_bytes<D>();
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
   cudaError_t e = dsn_ensure_dynamic_smem(cache_rows_kernel<D>, smem, configured);
   if (e != cudaSuccess) return e;
