@@ -3,15 +3,16 @@
 // One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 128; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
 // rows (fp32) in the workspace, and a second kernel joins them.
-// Roles (384 threads, 168 registers each):
-//   warps 0-2    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, two buffers each; a unit is K or V of 32 tokens, a token a
-//                lane; its codes come as bulk copies, three units ahead.  Every element is made once for 256 rows.
-//   warp 3       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
+// Roles (512 threads):
+//   warps 0-5    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, two buffers each.  A unit is K or V of a block of 16
+//                tokens, two lanes a token.  Every element is made once for 256 rows.
+//   warp 6       loader: pages' numbers, and the blocks as bulk copies into two slots of 64 tokens.
+//   warp 7       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
 //                of one half runs under the products of the other.
-//   warps 4-7    softmax of half 0, warps 8-11 of half 1: a thread a row (= TMEM lane), half a row of S in registers; maximum, exp2, sum, probabilities over
+//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), half a row of S in registers; maximum, exp2, sum, probabilities over
 //                the columns of S, from where the second product takes them.  They also fetch the rows of Q and write those of O.
 // Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
-// goes into the scale of its scores; 32 tokens of a tile have one for K, which goes there, too, and one for V, which the probabilities of
+// goes into the scale of its scores; a block of 16 tokens has one for K, which goes there, too, and one for V, which the probabilities of
 // those tokens take up.  Everything of a row is in units of 2^g, g a reference that moves only when a probability with its power of two would
 // pass 2^15: then O is read, scaled and written back.
 // The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (a mask each pair), so Q's and O's columns are in that order, too.
@@ -25,14 +26,13 @@ namespace {
 using namespace dsn_q4;
 using namespace dsn_gemm;
 
-constexpr int kThreadsR = 384, kRows = 256, kTile = 128;
-constexpr int kValueWarps = 3, kIssueWarp = 3, kSoftWarp = 4;
+constexpr int kThreadsR = 512, kRows = 256, kTile = 128;
+constexpr int kValueWarps = 6, kLoadWarp = 6, kIssueWarp = 7, kSoftWarp = 8;
 constexpr float kTop = 15.f, kAim = 7.f;     // a probability with its power of two is at most 2^15, 2^7 where the reference has just moved
 constexpr uint32_t kTileBytes = 128 * 128;   // 128 rows of 64 bf16
 constexpr uint32_t kCtrlR = 4096;
-constexpr uint32_t kRawDepth = 3;            // units in a warp's ring of codes
-template <int D>
-__host__ __device__ constexpr uint32_t unit_bytes() { return 2u * (9u * D + D); }   // two blocks: codes and pairs of a half, pairs of V
+constexpr int kEvery = 4;                     // of so many exponentials one is computed on the FMA pipe
+constexpr int kHalf = 64;                     // tokens of a slot of codes
 constexpr uint32_t kRegion = 256, kOCol = 128;
 
 __device__ __forceinline__ void mma_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -189,18 +189,18 @@ __device__ __forceinline__ void half_tiles(const Item& it, int h, const FastDiv&
 template <int D>
 __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_constant__ CacheAttParams p) {
   constexpr int GR = D / 64;
-  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes, kUnit = unit_bytes<D>();
+  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes, kSlot = kHalf / DSN_CACHE_BLOCK * kBlock;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (base - raw);
   const uint32_t q_full = base, k_full = base + 16, v_full = base + 32, k_empty = base + 48, v_empty = base + 64, s_full = base + 80,
                  p_full = base + 96, o_full = base + 112, o_empty = base + 128;   // [2] each
-  const uint32_t raw_full = base + 320;   // [3 warps][kRawDepth]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 144);
-  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 148);
-  uint8_t* s_bad = smem + 160;                                                     // [4 tiles][4 warps]: blocks of a page outside the cache
-  uint32_t* s_ke = reinterpret_cast<uint32_t*>(smem + 192);                        // the same: biased exponent that K was divided by
-  uint32_t* s_ve = reinterpret_cast<uint32_t*>(smem + 256);                        // and V
+  const uint32_t raw_full = base + 144, raw_empty = base + 160;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 176);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 180);
+  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 184);                       // [2 slots]: bit b: block b is there, bit 4 + b: its page is outside the cache; tokens << 8
+  uint8_t* s_bad = smem + 192;                                                     // [4 tiles][8 blocks]: 1: of a page outside the cache
+  float2* s_fac = reinterpret_cast<float2*>(smem + 256);                           // [4 tiles][8 blocks]: K's power of two; V's, as its exponent
   uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 512);
   CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 1024);
   static_assert(1024 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
@@ -212,8 +212,10 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full + 8 * i, 4);
-      mbar_init(k_full + 8 * i, 4);   // units of 32 tokens
-      mbar_init(v_full + 8 * i, 4);
+      mbar_init(k_full + 8 * i, 8);   // units of 16 tokens
+      mbar_init(v_full + 8 * i, 8);
+      mbar_init(raw_full + 8 * i, 1);
+      mbar_init(raw_empty + 8 * i, 8);
       mbar_init(k_empty + 8 * i, 1);
       mbar_init(v_empty + 8 * i, 1);
       mbar_init(s_full + 8 * i, 1);
@@ -221,7 +223,6 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       mbar_init(o_full + 8 * i, 1);
       mbar_init(o_empty + 8 * i, 4);
     }
-    for (int i = 0; i < kValueWarps * (int)kRawDepth; ++i) mbar_init(raw_full + 8 * i, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -258,25 +259,74 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
 
   if (warp < kValueWarps) {
     // ------------------------------------------------------------------------------ codes to values
-    // This warp's units are numbers warp, warp + 3, ... of all.  A unit's codes and pairs come as bulk copies into a slot of the warp's own ring, three units ahead
-    // (K's with V's pairs beside them); the page's number was read a unit before that.  Lanes 0 and 1 fetch a block of 16 tokens each.
-    const int bpp = p.page / DSN_CACHE_BLOCK;
-    const uint32_t ring = raw_at + (uint32_t)warp * (kRawDepth * kUnit), full = raw_full + (uint32_t)warp * (8 * kRawDepth);
-    uint32_t number = (uint32_t)warp, walk_n = 0;     // the unit that the walk stands at, and its tile
-    bool more = walk.next(p, it);
-    int tile = it.c0;
-    int pg = -1, place = 0;                           // page of this lane's block and the block in it
-    bool exists = false;
-    auto find = [&]() {
-      while (more && walk_n < (number >> 3)) {
-        ++walk_n;
-        if (++tile == it.c1) {
-          more = walk.next(p, it);
-          tile = it.c0;
+    // Unit u of slot number i: K (0-3) or V (4-7) of block u & 3; warp w takes units w, w + 6, ... of all.
+    const uint32_t units = 16u * (uint32_t)(stretch.Z - stretch.A);
+    const int tok = lane & 15, part = lane >> 4;      // D = 128: a lane takes a group; D = 64: half of it
+    auto top_of = [](uint32_t pair) -> uint32_t {     // exponent of the largest element that the pair can stand for
+      const float top = fabsf(hi_bf16(pair)) + 8.f * fabsf(lo_bf16(pair));
+      return top <= 3.4e38f ? __float_as_uint(top) >> 23 : 0u;
+    };
+    auto held = [](uint32_t e) -> uint32_t { return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u); };   // 2^e and 2^-e are normal numbers
+#pragma unroll 1
+    for (uint32_t unit = (uint32_t)warp; unit < units; unit += kValueWarps) {
+      const uint32_t i = unit >> 3, n = i >> 1, s = n & 1u, b = unit & 3u;
+      const bool is_v = (unit & 4u) != 0;
+      if (!dsn_wait(raw_full + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
+      const uint32_t info = *reinterpret_cast<const volatile uint32_t*>(s_raw + (i & 1u));
+      const bool there = (info >> b & 1u) && (int)(b * 16u) + tok < (int)(info >> 8);
+      const uint32_t blk = raw_at + (i & 1u) * kSlot + b * kBlock, src = blk + (is_v ? kBlock / 2 : 0u);
+      const uint32_t pair_at = GR * 512u + (GR == 2 ? (uint32_t)part * 64u : 0u) + (uint32_t)tok * 4u;
+      uint32_t v_pair = there ? lds32(blk + kBlock / 2 + pair_at) : 0u, pair = there ? lds32(src + pair_at) : 0u;
+      // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
+      if (!(fabsf(lo_bf16(v_pair)) <= 3.4e38f) || !(fabsf(hi_bf16(v_pair)) <= 3.4e38f)) v_pair = 0u;
+      if (is_v) pair = v_pair;
+      const uint32_t e = held(top_of(pair));
+      uint32_t q[GR][4];
+#pragma unroll
+      for (int x = 0; x < GR; ++x) lds128(src + (GR == 2 ? (uint32_t)(part * 512 + tok * 32 + 16 * x) : (uint32_t)(tok * 32 + 16 * part)), q[x]);
+      if (n >= 2 && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
+      if (!is_v) {
+        const uint32_t ve = held(top_of(v_pair)), k = (n & 3u) * 8 + (i & 1u) * 4 + b;
+        if (lane == 0) {
+          s_bad[k] = (uint8_t)(info >> (4 + b) & 1u);
+          s_fac[k] = make_float2(__uint_as_float(e << 23), (float)((int)ve - 127));
         }
       }
-      const int key = it.s.lo + tile * kTile + 32 * (int)(number & 3u) + DSN_CACHE_BLOCK * lane;
-      exists = more && lane < 2 && key <= it.s.me1;
+      const float down = __uint_as_float((254u - e) << 23);
+      const __half2 s2 = __float2half2_rn(lo_bf16(pair) * down), z2 = __float2half2_rn(hi_bf16(pair) * down);
+      const uint32_t dst = (is_v ? v_at : k_at) + s * kOperand + ((i & 1u) * 64u + b * 16u + (uint32_t)tok) * 128u + (GR == 2 ? (uint32_t)part * kTileBytes : 0u);
+#pragma unroll
+      for (int x = 0; x < GR; ++x)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          __half2 c[4];
+          code_pairs(q[x][w], c);
+          uint32_t o[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            c[j] = __hfma2(c[j], s2, z2);
+            o[j] = *reinterpret_cast<const uint32_t*>(&c[j]);
+          }
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((((GR == 2 ? 4 * x : 4 * part) + w) ^ (tok & 7)) << 4)), "r"(o[0]), "r"(o[1]),
+                       "r"(o[2]), "r"(o[3])
+                       : "memory");
+        }
+      fence_async_smem();
+      __syncwarp();   // every lane has read its codes and written its elements
+      if (lane == 0) {
+        mbar_arrive((is_v ? v_full : k_full) + 8 * s);
+        mbar_arrive(raw_empty + 8 * (i & 1u));
+      }
+    }
+  } else if (warp == kLoadWarp) {
+    // ------------------------------------------------------------------------------ codes from the pages
+    const int bpp = p.page / DSN_CACHE_BLOCK;
+    bool more = walk.next(p, it);
+    int tile = it.c0, half = 0, pg = -1, place = 0;   // the slot's tokens; page of this lane's block, the block in it
+    bool exists = false;
+    auto find = [&]() {
+      const int key = it.s.lo + tile * kTile + half * kHalf + DSN_CACHE_BLOCK * lane;
+      exists = more && lane < kHalf / DSN_CACHE_BLOCK && key <= it.s.me1;
       pg = -1;
       if (exists) {
         const int col = (int)dsn_div((uint32_t)key, p.by_page);
@@ -284,111 +334,31 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         place = key / DSN_CACHE_BLOCK - col * bpp;
       }
     };
-    auto fetch = [&](uint32_t slot) -> uint32_t {     // copies of the unit that was found; bit b: block b is missing, bit 2 + b: it is on its way
+    uint32_t i = 0;
+    find();
+    for (; more; ++i) {
+      const uint32_t slot = i & 1u;
+      if (i >= 2 && !dsn_wait(raw_empty + 8 * slot, ((i >> 1) - 1u) & 1u, abort_flag, p.status, 91)) break;
       const bool ok = pg >= 0 && pg < p.n_pages, lost = exists && !ok;
       if (lost) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
       const uint32_t go = __ballot_sync(0xffffffffu, ok), bad = __ballot_sync(0xffffffffu, lost);
-      const bool is_v = (number & 4u) != 0;
-      const uint32_t bytes = 9u * D + (is_v ? 0u : 64u * GR);
-      if (lane == 0) mbar_expect_tx(full + 8 * slot, (uint32_t)__popc(go) * bytes);
+      if (lane == 0) {
+        const int left = min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile + half * kHalf), 0), kHalf);
+        *reinterpret_cast<volatile uint32_t*>(s_raw + slot) = go | (bad << 4) | ((uint32_t)left << 8);
+        mbar_expect_tx(raw_full + 8 * slot, (uint32_t)__popc(go) * kBlock);
+      }
       __syncwarp();
-      if (ok) {
-        const uint8_t* blk = p.pages + (((int64_t)pg * p.H + it.head) * bpp + place) * kBlock;
-        const uint32_t dst = ring + slot * kUnit + (uint32_t)lane * (kUnit / 2);
-        dsn_bulk_load(dst, blk + (is_v ? kBlock / 2 : 0u), 9u * D, full + 8 * slot);
-        if (!is_v) dsn_bulk_load(dst + 9u * D, blk + kBlock / 2 + GR * 512, 64u * GR, full + 8 * slot);
-      }
-      number += kValueWarps;
-      return bad | (go << 2);
-    };
-    // exponent of the largest element of the unit, held where 2^e and 2^-e are normal numbers
-    auto exponent = [&](const uint32_t (&pair)[GR]) -> uint32_t {
-      uint32_t e = 0;
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr) {
-        const float top = fabsf(hi_bf16(pair[gr])) + 8.f * fabsf(lo_bf16(pair[gr]));
-        if (top <= 3.4e38f) e = max(e, __float_as_uint(top) >> 23);
-      }
-      return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
-    };
-    uint32_t asked = 0, state = 0, live = 0;          // units asked for; four bits a slot; a bit a slot
-    int ends[kRawDepth];                              // tokens of the unit that exist
-    find();
-#pragma unroll
-    for (uint32_t i = 0; i < kRawDepth; ++i) {
-      ends[i] = 0;
-      if (more) {
-        live |= 1u << i;
-        ends[i] = it.s.me1 + 1 - (it.s.lo + tile * kTile + 32 * (int)(number & 3u));
-        state |= fetch(i) << (4 * i);
-        ++asked;
-        find();
-      }
-    }
-    uint32_t slot = 0, turn = 0;
-    for (uint32_t which = (uint32_t)warp; live >> slot & 1u; which += kValueWarps) {
-      const uint32_t n = which >> 3, s = n & 1u, blk32 = which & 3u, flags = state >> (4 * slot);
-      const bool is_v = (which & 4u) != 0;
-      const int end = slot == 0 ? ends[0] : slot == 1 ? ends[1] : ends[2];
-      if (!dsn_wait(full + 8 * slot, turn, abort_flag, p.status, 82)) break;
-      const uint32_t src = ring + slot * kUnit + (uint32_t)(lane >> 4) * (kUnit / 2), t16 = (uint32_t)lane & 15u;
-      const bool there = (flags >> (2 + (lane >> 4)) & 1u) && lane < end;
-      uint32_t pair[GR], v_pair[GR];
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr) {
-        pair[gr] = there ? lds32(src + GR * 512 + gr * 64 + t16 * 4) : 0u;
-        v_pair[gr] = there ? (is_v ? pair[gr] : lds32(src + 9 * D + gr * 64 + t16 * 4)) : 0u;
-        // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
-        if (!(fabsf(lo_bf16(v_pair[gr])) <= 3.4e38f) || !(fabsf(hi_bf16(v_pair[gr])) <= 3.4e38f)) v_pair[gr] = 0u;
-      }
-      const uint32_t ve = exponent(v_pair), e = is_v ? ve : exponent(pair);
-      if (n >= 2 && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
-      if (!is_v && lane == 0) {
-        const uint32_t k = (n & 3u) * 4 + blk32;
-        s_bad[k] = (uint8_t)(flags & 3u);
-        s_ke[k] = e;
-        s_ve[k] = ve;
-      }
-      const float down = __uint_as_float((254u - e) << 23);
-      const uint32_t dst = (is_v ? v_at : k_at) + s * kOperand + (blk32 * 32u + (uint32_t)lane) * 128u;
-#pragma unroll 1
-      for (int i = 0; i < 2 * GR; ++i) {              // 32 elements at a time
-        const int gr = i >> 1;
-        const uint32_t pr = GR == 1 || gr == 0 ? (is_v ? v_pair[0] : pair[0]) : (is_v ? v_pair[GR - 1] : pair[GR - 1]);
-        const __half2 s2 = __float2half2_rn(lo_bf16(pr) * down), z2 = __float2half2_rn(hi_bf16(pr) * down);
-        uint32_t q[4];
-        lds128(src + gr * 512 + t16 * 32 + 16 * (i & 1), q);
-        const uint32_t to = dst + gr * kTileBytes;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          __half2 x[4];
-          code_pairs(q[w], x);
-          uint32_t o[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[j] = __hfma2(x[j], s2, z2);
-            o[j] = *reinterpret_cast<const uint32_t*>(&x[j]);
-          }
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(((4 * (i & 1) + w) ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]),
-                       "r"(o[3])
-                       : "memory");
+      if (ok)
+        dsn_bulk_load(raw_at + slot * kSlot + (uint32_t)lane * kBlock, p.pages + (((int64_t)pg * p.H + it.head) * bpp + place) * kBlock, kBlock,
+                      raw_full + 8 * slot);
+      if (half ^= 1, half == 0)
+        if (++tile == it.c1) {
+          more = walk.next(p, it);
+          tile = it.c0;
         }
-      }
-      fence_async_smem();
-      __syncwarp();   // every lane has read the slot and written its rows
-      if (lane == 0) mbar_arrive((is_v ? v_full : k_full) + 8 * s);
-      live &= ~(1u << slot);
-      if (more) {
-        live |= 1u << slot;
-        const int left = it.s.me1 + 1 - (it.s.lo + tile * kTile + 32 * (int)(number & 3u));
-        if (slot == 0) ends[0] = left; else if (slot == 1) ends[1] = left; else ends[2] = left;
-        state = (state & ~(15u << (4 * slot))) | (fetch(slot) << (4 * slot));
-        ++asked;
-        find();
-      }
-      if (++slot == kRawDepth) slot = 0, turn ^= 1u;
+      find();
     }
-    if (*abort_flag) dsn_drain(full, kRawDepth, 0, (int)asked);
+    if (*abort_flag) dsn_drain(raw_full, 2, i > 2 ? (int)i - 2 : 0, (int)i);
   } else if (warp == kIssueWarp) {
     // ------------------------------------------------------------------------------ products
     const uint32_t f16 = ~((1u << 7) | (1u << 10));                                               // both operands fp16
@@ -476,7 +446,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     // The warp's rows of Q as fp16, the largest element of each brought to 1 .. 2; returns the power of two that goes into the scores of this lane's row.
     // D / 8 lanes read a row.
     auto load_q = [&](const Item& x) -> float {
-      constexpr int L = D / 8, PER = 32 / L, NB = L;   // lanes a row, rows a load, loads at once
+      constexpr int L = D / 8, PER = 32 / L, NB = 8;   // lanes a row, rows a load, loads at once
       const int v = x.s.v0 + 128 * h + row;
       const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
       const long long mine = v < x.s.v1 ? ((long long)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((long long)x.head * (p.group + 2) + ev) * D
@@ -539,25 +509,26 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         const int t0 = it.s.lo + j * kTile;
         const int k1 = me + 1 - t0, k0 = p.window ? me - p.window + 1 - t0 : 0;
         const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 3u;
-        const uint32_t bad = *reinterpret_cast<const volatile uint32_t*>(s_bad + nt * 4);
-        float to[4], shift[4];        // a score of block c to units of the exponent; the power of two of its V
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          to[c] = fmaxf(cs * __uint_as_float(s_ke[nt * 4 + c] << 23), 1e-37f);   // not 0: what is hidden is -infinity
-          shift[c] = (float)((int)s_ve[nt * 4 + c] - 127);
-        }
+        const uint64_t bad = *reinterpret_cast<const volatile uint64_t*>(s_bad + nt * 8);
+        const float2* fac = s_fac + nt * 8;
+        // of a block of 16: scores to units of the exponent (not 0: what is hidden is -infinity), the power of two of its V
+        auto factors = [&](int c, float& t, float& sh) {
+          const float2 f = fac[c];
+          t = fmaxf(cs * f.x, 1e-37f);
+          sh = f.y;
+        };
         const bool cut = __any_sync(0xffffffffu, live && (k1 < kTile || k0 > 0)) || bad != 0;
-        auto hide = [&](uint32_t (&x)[32], int c) {   // block c of 32 columns
+        auto hide = [&](uint32_t (&x)[32], int c) {   // columns 32 c ...
           const int e1 = min(max(k1 - 32 * c, 0), 32), e0 = min(max(k0 - 32 * c, 0), 32);
           uint32_t m = (e1 >= 32 ? 0xffffffffu : (1u << e1) - 1u) & (e0 >= 32 ? 0u : 0xffffffffu << e0);
-          const uint32_t bb = bad >> (8 * c);
-          if (bb & 1u) m &= 0xffff0000u;
-          if (bb & 2u) m &= 0x0000ffffu;
+          const uint32_t bb = (uint32_t)(bad >> (16 * c));
+          if (bb & 0xffu) m &= 0xffff0000u;
+          if (bb & 0xff00u) m &= 0x0000ffffu;
 #pragma unroll
           for (int i = 0; i < 32; ++i)
             if (!(m >> i & 1u)) x[i] = 0xff800000u;
         };
-        // the maximum over blocks 2, 3, then 0, 1, which stay in registers
+        // the maximum over columns 64 .. 127, then 0 .. 63, which stay in registers
         float need = -INFINITY;
         uint32_t x[2][32];
 #pragma unroll 1
@@ -570,18 +541,16 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
             hide(x[1], c + 1);
           }
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float t = c ? to[2 + k] : to[k], sh = c ? shift[2 + k] : shift[k];
-            float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+          for (int k = 0; k < 4; ++k) {
+            float t, sh, m0 = -INFINITY, m1 = -INFINITY;
+            factors(2 * c + k, t, sh);
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              m0 = max3_nan(m0, __uint_as_float(x[k][i]), __uint_as_float(x[k][i + 1]));
-              m1 = max3_nan(m1, __uint_as_float(x[k][i + 2]), __uint_as_float(x[k][i + 3]));
-              m2 = max3_nan(m2, __uint_as_float(x[k][i + 4]), __uint_as_float(x[k][i + 5]));
-              m3 = max3_nan(m3, __uint_as_float(x[k][i + 6]), __uint_as_float(x[k][i + 7]));
+            for (int i = 0; i < 16; i += 4) {
+              const uint32_t* y = x[k >> 1] + 16 * (k & 1) + i;
+              m0 = max3_nan(m0, __uint_as_float(y[0]), __uint_as_float(y[1]));
+              m1 = max3_nan(m1, __uint_as_float(y[2]), __uint_as_float(y[3]));
             }
-            m0 = max3_nan(m0, m1, m2);
-            need = max3_nan(need, fmaf(m0, t, sh), fmaf(m3, t, sh));
+            need = max3_nan(need, fmaf(m0, t, sh), fmaf(m1, t, sh));
           }
         }
         if (need != need) l = need;   // a token that is not finite: so is the row
@@ -604,28 +573,33 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
             }
           }
         }
-        auto block = [&](uint32_t (&x)[32], int c, float t, float sh) {
-          const uint64_t to_2 = pack2(t, t), ref_2 = pack2(sh - ref, sh - ref);
-          uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
+        auto block = [&](uint32_t (&x)[32], int c) {   // columns 32 c ...
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float x0, x1;
-            const uint64_t t2 = ffma2(pack2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), to_2, ref_2);
-            if ((e & 3) == 3) {
-              exp2_pair(t2, x0, x1);   // some on the FMA pipe; what is hidden comes out as 2^-126, a zero in fp16
-            } else {
-              float t0f, t1f;
-              unpack2(t2, t0f, t1f);
-              x0 = ex2(t0f);
-              x1 = ex2(t1f);
+          for (int k = 0; k < 2; ++k) {
+            float t, sh;
+            factors(2 * c + k, t, sh);
+            const uint64_t to_2 = pack2(t, t), ref_2 = pack2(sh - ref, sh - ref);
+            uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float x0, x1;
+              const uint64_t t2 = ffma2(pack2(__uint_as_float(x[16 * k + 2 * e]), __uint_as_float(x[16 * k + 2 * e + 1])), to_2, ref_2);
+              if (e % kEvery == kEvery - 1) {
+                exp2_pair(t2, x0, x1);   // some on the FMA pipe; what is hidden comes out as 2^-126, a zero in fp16
+              } else {
+                float t0f, t1f;
+                unpack2(t2, t0f, t1f);
+                x0 = ex2(t0f);
+                x1 = ex2(t1f);
+              }
+              if (e & 1) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
+              x[8 * k + e] = pack_f16(x0, x1);
             }
-            if (e & 1) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
-            x[e] = pack_f16(x0, x1);
+            float s0, s1;
+            unpack2(fadd2(sum_a, sum_b), s0, s1);
+            l = fmaf(s0 + s1, __uint_as_float((127u - (uint32_t)(int)sh) << 23), l);   // in units of 2^ref, without V's power
           }
           tmem_st_16(region + (uint32_t)(16 * c), x);
-          float s0, s1;
-          unpack2(fadd2(sum_a, sum_b), s0, s1);
-          l = fmaf(s0 + s1, __uint_as_float((127u - (uint32_t)(int)sh) << 23), l);   // in units of 2^ref, without V's power
         };
 #pragma unroll 1
         for (int c = 0; c < 4; c += 2) {
@@ -638,8 +612,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
               hide(x[1], 3);
             }
           }
-          block(x[0], c, c ? to[2] : to[0], c ? shift[2] : shift[0]);
-          block(x[1], c + 1, c ? to[3] : to[1], c ? shift[3] : shift[1]);
+          block(x[0], c);
+          block(x[1], c + 1);
         }
         tmem_st_done();
         tc_fence_before();
@@ -769,7 +743,7 @@ __global__ void __launch_bounds__(kRows) cache_rows_join_kernel(const __grid_con
 template <int D>
 cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
   static size_t configured[DSN_MAX_DEVICES] = {};
-  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes + kValueWarps * kRawDepth * unit_bytes<D>();
+  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes + 2 * (kHalf / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
   cudaError_t e = dsn_ensure_dynamic_smem(cache_rows_kernel<D>, smem, configured);
   if (e != cudaSuccess) return e;
