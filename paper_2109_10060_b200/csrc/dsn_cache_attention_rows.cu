@@ -9,7 +9,7 @@
 //   warp 6       loader: pages' numbers, and the blocks as bulk copies into two slots of 64 tokens.
 //   warp 7       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
 //                of one half runs under the products of the other.
-//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), half a row of S in registers; maximum, exp2, sum, probabilities over
+//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), 32 columns of S in registers at a time (few registers let more instructions overlap); maximum, exp2, sum, probabilities over
 //                the columns of S, from where the second product takes them.  They also fetch the rows of Q and write those of O.
 // Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
 // goes into the scale of its scores; a block of 16 tokens has one for K, which goes there, too, and one for V, which the probabilities of
@@ -528,30 +528,24 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
           for (int i = 0; i < 32; ++i)
             if (!(m >> i & 1u)) x[i] = 0xff800000u;
         };
-        // the maximum over columns 64 .. 127, then 0 .. 63, which stay in registers
         float need = -INFINITY;
-        uint32_t x[2][32];
 #pragma unroll 1
-        for (int c = 2; c >= 0; c -= 2) {
-          tmem_ld_32x32(region + 32 * c, x[0]);
-          tmem_ld_32x32(region + 32 * (c + 1), x[1]);
+        for (int c = 0; c < 4; ++c) {
+          uint32_t x[32];
+          tmem_ld_32x32(region + 32 * c, x);
+          float t0c, sh0, t1c, sh1;
+          factors(2 * c, t0c, sh0);
+          factors(2 * c + 1, t1c, sh1);
           tmem_ld_wait();
-          if (cut) {
-            hide(x[0], c);
-            hide(x[1], c + 1);
-          }
+          if (cut) hide(x, c);
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float t, sh, m0 = -INFINITY, m1 = -INFINITY;
-            factors(2 * c + k, t, sh);
+          for (int i = 0; i < 16; i += 4)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              const uint32_t* y = x[k >> 1] + 16 * (k & 1) + i;
-              m0 = max3_nan(m0, __uint_as_float(y[0]), __uint_as_float(y[1]));
-              m1 = max3_nan(m1, __uint_as_float(y[2]), __uint_as_float(y[3]));
-            }
-            need = max3_nan(need, fmaf(m0, t, sh), fmaf(m1, t, sh));
-          }
+            for (int k = 0; k < 4; ++k)
+              m[k] = max3_nan(m[k], __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1)]), __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1) + 1]));
+          need = max3_nan(need, fmaf(m[0], t0c, sh0), fmaf(m[1], t0c, sh0));
+          need = max3_nan(need, fmaf(m[2], t1c, sh1), fmaf(m[3], t1c, sh1));
         }
         if (need != need) l = need;   // a token that is not finite: so is the row
         if (__any_sync(0xffffffffu, need > ref + kTop)) {
@@ -602,18 +596,12 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
           tmem_st_16(region + (uint32_t)(16 * c), x);
         };
 #pragma unroll 1
-        for (int c = 0; c < 4; c += 2) {
-          if (c) {
-            tmem_ld_32x32(region + 64, x[0]);
-            tmem_ld_32x32(region + 96, x[1]);
-            tmem_ld_wait();
-            if (cut) {
-              hide(x[0], 2);
-              hide(x[1], 3);
-            }
-          }
-          block(x[0], c);
-          block(x[1], c + 1);
+        for (int c = 0; c < 4; ++c) {
+          uint32_t x[32];
+          tmem_ld_32x32(region + 32 * c, x);
+          tmem_ld_wait();
+          if (cut) hide(x, c);
+          block(x, c);
         }
         tmem_st_done();
         tc_fence_before();
