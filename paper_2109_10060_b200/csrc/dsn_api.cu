@@ -881,7 +881,7 @@ int check_cache_desc(const dsn_cache_desc* d) {
   if (d->T < 1 || d->T > DSN_MAX_SLICES || !valid_order(d->order)) return DSN_ERR_INVALID_ARG;
   if (!(d->scale > -INFINITY && d->scale < INFINITY) || d->window < 0) return DSN_ERR_INVALID_ARG;
   // tiles of a request in one head, counted in 32 bits
-  if (((int64_t)d->max_pages * d->page / 128 + 2) * ((int64_t)d->R * d->group / 256 + 1) > INT32_MAX) return DSN_ERR_UNSUPPORTED;
+  if (((int64_t)d->max_pages * d->page / 64 + 2) * ((int64_t)d->R * d->group / 256 + 1) > INT32_MAX) return DSN_ERR_UNSUPPORTED;
   for (int t = 0; t < d->T; ++t)
     if (d->heads[t] < 1 || d->heads[t] > d->H) return DSN_ERR_INVALID_ARG;
   return DSN_OK;

@@ -1,22 +1,23 @@
 // Attention over the 4-bit cache, many query vectors a head (rows * group > 16: prompts, pieces of prompts), on tcgen05.
 //
-// One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 128; the tiles of all items
+// One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 64; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
 // rows (fp32) in the workspace, and a second kernel joins them.
 // Roles (512 threads):
-//   warps 0-5    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, two buffers each.  A unit is K or V of a block of 16
+//   warps 0-4    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, four buffers each.  A unit is K or V of a block of 16
 //                tokens, two lanes a token.  Every element is made once for 256 rows.
-//   warp 6       loader: pages' numbers, and the blocks as bulk copies into two slots of 64 tokens.
-//   warp 7       issue: S_h = Q_h K^T and O_h += P_h V of the two halves h in the order PV_0(i), QK_0(i + 1), PV_1(i), QK_1(i + 1): the softmax
-//                of one half runs under the products of the other.
-//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), 32 columns of S in registers at a time (few registers let more instructions overlap); maximum, exp2, sum, probabilities over
-//                the columns of S, from where the second product takes them.  They also fetch the rows of Q and write those of O.
+//   warp 5       loader: pages' numbers, and the blocks as bulk copies into two slots of a tile.
+//   warps 6-7    issue, one a half: S_h = Q_h K^T and O_h += P_h V.  S has two buffers a half: a half's product of scores runs a tile ahead, so its softmax
+//                never waits for it.  (One warp for both spends more time on barriers than the products take.)
+//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), 32 columns of S in registers at a time (few registers let more
+//                instructions overlap); maximum, exp2, sum, probabilities over the columns of S, from where the second product takes them.  They also fetch the
+//                rows of Q and write those of O.
 // Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
 // goes into the scale of its scores; a block of 16 tokens has one for K, which goes there, too, and one for V, which the probabilities of
 // those tokens take up.  Everything of a row is in units of 2^g, g a reference that moves only when a probability with its power of two would
 // pass 2^15: then O is read, scaled and written back.
 // The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (a mask each pair), so Q's and O's columns are in that order, too.
-// TMEM: 512 columns = two regions of 256: S_h 0..127, P_h over 0..63, O_h from 128.  Every wait is bounded.
+// TMEM: 512 columns = two regions of 256: two buffers of S_h at 0 and 64, P_h over the first half of each, O_h from 128.  Every wait is bounded.
 #include <cuda_fp16.h>
 
 #include "dsn_cache_line.cuh"
@@ -26,13 +27,12 @@ namespace {
 using namespace dsn_q4;
 using namespace dsn_gemm;
 
-constexpr int kThreadsR = 512, kRows = 256, kTile = 128;
-constexpr int kValueWarps = 6, kLoadWarp = 6, kIssueWarp = 7, kSoftWarp = 8;
+constexpr int kThreadsR = 512, kRows = 256, kTile = 64, kStages = 4;
+constexpr int kValueWarps = 5, kLoadWarp = 5, kIssueWarp = 6, kSoftWarp = 8;
 constexpr float kTop = 15.f, kAim = 7.f;     // a probability with its power of two is at most 2^15, 2^7 where the reference has just moved
 constexpr uint32_t kTileBytes = 128 * 128;   // 128 rows of 64 bf16
 constexpr uint32_t kCtrlR = 4096;
 constexpr int kEvery = 4;                     // of so many exponentials one is computed on the FMA pipe
-constexpr int kHalf = 64;                     // tokens of a slot of codes
 constexpr uint32_t kRegion = 256, kOCol = 128;
 
 __device__ __forceinline__ void mma_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -100,11 +100,11 @@ __device__ __forceinline__ void exp2_pair(uint64_t t2, float& x0, float& x1) {
   x0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23));
   x1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23));
 }
-// V as it lies: rows are tokens, 64 elements in 128 bytes; 128 elements are two such tiles.
+// V as it lies: rows are tokens, 64 elements in 128 bytes; 128 elements are two such pieces of a stage.
 __device__ __forceinline__ uint64_t make_desc_mn(uint32_t addr) {
   uint64_t d = 0;
   d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(kTileBytes >> 4) << 16;   // from 64 elements to the next 64
+  d |= (uint64_t)(kTileBytes / 2 >> 4) << 16;   // from 64 elements to the next 64
   d |= (uint64_t)(1024 >> 4) << 32;         // from 8 tokens to the next 8
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
@@ -189,22 +189,22 @@ __device__ __forceinline__ void half_tiles(const Item& it, int h, const FastDiv&
 template <int D>
 __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_constant__ CacheAttParams p) {
   constexpr int GR = D / 64;
-  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes, kSlot = kHalf / DSN_CACHE_BLOCK * kBlock;
+  constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kOperand = GR * kTileBytes, kStage = kOperand / 2, kSlot = kTile / DSN_CACHE_BLOCK * kBlock;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (base - raw);
-  const uint32_t q_full = base, k_full = base + 16, v_full = base + 32, k_empty = base + 48, v_empty = base + 64, s_full = base + 80,
-                 p_full = base + 96, o_full = base + 112, o_empty = base + 128;   // [2] each
-  const uint32_t raw_full = base + 144, raw_empty = base + 160;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 176);
-  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 180);
-  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 184);                       // [2 slots]: bit b: block b is there, bit 4 + b: its page is outside the cache; tokens << 8
-  uint8_t* s_bad = smem + 192;                                                     // [4 tiles][8 blocks]: 1: of a page outside the cache
-  float2* s_fac = reinterpret_cast<float2*>(smem + 256);                           // [4 tiles][8 blocks]: K's power of two; V's, as its exponent
-  uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 512);
+  // barriers: [2 halves] of q and o_empty, [4 stages] of k and v, [2 slots] of raw, [2 halves][2 buffers] of s, p, o
+  const uint32_t q_full = base, o_empty = base + 16, k_full = base + 32, k_empty = base + 64, v_full = base + 96, v_empty = base + 128,
+                 raw_full = base + 160, raw_empty = base + 176, s_full = base + 192, p_full = base + 224, o_full = base + 256;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 288);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 292);
+  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there, bit 4 + b: its page is outside the cache; tokens << 8
+  uint8_t* s_bad = smem + 320;                                                     // [8 tiles][4 blocks]: 1: of a page outside the cache
+  float2* s_fac = reinterpret_cast<float2*>(smem + 384);                           // [8 tiles][4 blocks]: K's power of two; V's, as its exponent
+  uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 640);
   CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 1024);
   static_assert(1024 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
-  const uint32_t q_at = base + kCtrlR, k_at = q_at + 2 * kOperand, v_at = k_at + 2 * kOperand, raw_at = v_at + 2 * kOperand;
+  const uint32_t q_at = base + kCtrlR, k_at = q_at + 2 * kOperand, v_at = k_at + kStages * kStage, raw_at = v_at + kStages * kStage;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   dsn_grid_dependency_wait();
@@ -212,16 +212,18 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full + 8 * i, 4);
-      mbar_init(k_full + 8 * i, 8);   // units of 16 tokens
-      mbar_init(v_full + 8 * i, 8);
+      mbar_init(o_empty + 8 * i, 4);
       mbar_init(raw_full + 8 * i, 1);
       mbar_init(raw_empty + 8 * i, 8);
-      mbar_init(k_empty + 8 * i, 1);
-      mbar_init(v_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(k_full + 8 * i, 4);   // units of 16 tokens
+      mbar_init(v_full + 8 * i, 4);
+      mbar_init(k_empty + 8 * i, 2);   // the halves
+      mbar_init(v_empty + 8 * i, 2);
       mbar_init(s_full + 8 * i, 1);
       mbar_init(p_full + 8 * i, 4);
       mbar_init(o_full + 8 * i, 1);
-      mbar_init(o_empty + 8 * i, 4);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -259,8 +261,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
 
   if (warp < kValueWarps) {
     // ------------------------------------------------------------------------------ codes to values
-    // Unit u of slot number i: K (0-3) or V (4-7) of block u & 3; warp w takes units w, w + 6, ... of all.
-    const uint32_t units = 16u * (uint32_t)(stretch.Z - stretch.A);
+    // Unit u of tile number i: K (0-3) or V (4-7) of block u & 3; warp w takes units w, w + 5, ... of all.
+    const uint32_t units = 8u * (uint32_t)(stretch.Z - stretch.A);
     const int tok = lane & 15, part = lane >> 4;      // D = 128: a lane takes a group; D = 64: half of it
     auto top_of = [](uint32_t pair) -> uint32_t {     // exponent of the largest element that the pair can stand for
       const float top = fabsf(hi_bf16(pair)) + 8.f * fabsf(lo_bf16(pair));
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     auto held = [](uint32_t e) -> uint32_t { return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u); };   // 2^e and 2^-e are normal numbers
 #pragma unroll 1
     for (uint32_t unit = (uint32_t)warp; unit < units; unit += kValueWarps) {
-      const uint32_t i = unit >> 3, n = i >> 1, s = n & 1u, b = unit & 3u;
+      const uint32_t i = unit >> 3, s = i % kStages, b = unit & 3u;
       const bool is_v = (unit & 4u) != 0;
       if (!dsn_wait(raw_full + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
       const uint32_t info = *reinterpret_cast<const volatile uint32_t*>(s_raw + (i & 1u));
@@ -284,9 +286,9 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       uint32_t q[GR][4];
 #pragma unroll
       for (int x = 0; x < GR; ++x) lds128(src + (GR == 2 ? (uint32_t)(part * 512 + tok * 32 + 16 * x) : (uint32_t)(tok * 32 + 16 * part)), q[x]);
-      if (n >= 2 && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, ((n >> 1) - 1u) & 1u, abort_flag, p.status, 81)) break;
+      if (i >= kStages && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, (i / kStages - 1u) & 1u, abort_flag, p.status, 81)) break;
       if (!is_v) {
-        const uint32_t ve = held(top_of(v_pair)), k = (n & 3u) * 8 + (i & 1u) * 4 + b;
+        const uint32_t ve = held(top_of(v_pair)), k = (i & 7u) * 4 + b;
         if (lane == 0) {
           s_bad[k] = (uint8_t)(info >> (4 + b) & 1u);
           s_fac[k] = make_float2(__uint_as_float(e << 23), (float)((int)ve - 127));
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       }
       const float down = __uint_as_float((254u - e) << 23);
       const __half2 s2 = __float2half2_rn(lo_bf16(pair) * down), z2 = __float2half2_rn(hi_bf16(pair) * down);
-      const uint32_t dst = (is_v ? v_at : k_at) + s * kOperand + ((i & 1u) * 64u + b * 16u + (uint32_t)tok) * 128u + (GR == 2 ? (uint32_t)part * kTileBytes : 0u);
+      const uint32_t dst = (is_v ? v_at : k_at) + s * kStage + (b * 16u + (uint32_t)tok) * 128u + (GR == 2 ? (uint32_t)part * (kTileBytes / 2) : 0u);
 #pragma unroll
       for (int x = 0; x < GR; ++x)
 #pragma unroll
@@ -322,11 +324,11 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     // ------------------------------------------------------------------------------ codes from the pages
     const int bpp = p.page / DSN_CACHE_BLOCK;
     bool more = walk.next(p, it);
-    int tile = it.c0, half = 0, pg = -1, place = 0;   // the slot's tokens; page of this lane's block, the block in it
+    int tile = it.c0, pg = -1, place = 0;   // page of this lane's block, the block in it
     bool exists = false;
     auto find = [&]() {
-      const int key = it.s.lo + tile * kTile + half * kHalf + DSN_CACHE_BLOCK * lane;
-      exists = more && lane < kHalf / DSN_CACHE_BLOCK && key <= it.s.me1;
+      const int key = it.s.lo + tile * kTile + DSN_CACHE_BLOCK * lane;
+      exists = more && lane < kTile / DSN_CACHE_BLOCK && key <= it.s.me1;
       pg = -1;
       if (exists) {
         const int col = (int)dsn_div((uint32_t)key, p.by_page);
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (lost) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
       const uint32_t go = __ballot_sync(0xffffffffu, ok), bad = __ballot_sync(0xffffffffu, lost);
       if (lane == 0) {
-        const int left = min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile + half * kHalf), 0), kHalf);
+        const int left = min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile), 0), kTile);
         *reinterpret_cast<volatile uint32_t*>(s_raw + slot) = go | (bad << 4) | ((uint32_t)left << 8);
         mbar_expect_tx(raw_full + 8 * slot, (uint32_t)__popc(go) * kBlock);
       }
@@ -351,97 +353,95 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (ok)
         dsn_bulk_load(raw_at + slot * kSlot + (uint32_t)lane * kBlock, p.pages + (((int64_t)pg * p.H + it.head) * bpp + place) * kBlock, kBlock,
                       raw_full + 8 * slot);
-      if (half ^= 1, half == 0)
-        if (++tile == it.c1) {
-          more = walk.next(p, it);
-          tile = it.c0;
-        }
+      if (++tile == it.c1) {
+        more = walk.next(p, it);
+        tile = it.c0;
+      }
       find();
     }
     if (*abort_flag) dsn_drain(raw_full, 2, i > 2 ? (int)i - 2 : 0, (int)i);
-  } else if (warp == kIssueWarp) {
+  } else if (warp < kSoftWarp) {
     // ------------------------------------------------------------------------------ products
+    // A warp issues what one half needs.  The scores of tile number m (of those that the half needs) go to buffer m & 1, which the product with the
+    // probabilities of number m - 2 has read by then: that one is issued first, so up to two of them wait for their softmax.
+    const int h = warp - kIssueWarp;
     const uint32_t f16 = ~((1u << 7) | (1u << 10));                                               // both operands fp16
     const uint32_t idesc_s = make_idesc(128, kTile) & f16, idesc_o = (make_idesc(128, D) & f16) | (1u << 16);   // V: elements first
-    uint32_t n = 0;                       // tiles so far
-    uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, n_o[2] = {0, 0};   // P waited for, Q waited for, items of the half
-    bool pend[2] = {false, false}, first_pv[2] = {true, true};
+    const uint32_t region = tmem + h * kRegion;
+    const uint64_t dq = make_smem_desc(q_at + h * kOperand);
+    uint32_t n = 0, freed = 0;                     // tiles so far; stages of V given back
+    uint32_t n_s = 0, n_p = 0, n_q = 0, n_o = 0;   // scores and products issued, Q waited for, items begun
+    uint32_t at0 = 0, at1 = 0;                     // tiles of the products that are due, the older first
+    bool first0 = false, first1 = false;           // of those: the first of an item
     bool ok = true;
-    auto pv = [&](int h, uint32_t tile_n) {   // O_h (+)= P_h V
-      const uint32_t s = tile_n & 1u;
-      ok = ok && dsn_wait(p_full + 8 * h, n_p[h] & 1u, abort_flag, p.status, 83);
-      ok = ok && dsn_wait(v_full + 8 * s, (tile_n >> 1) & 1u, abort_flag, p.status, 84);
-      if (first_pv[h] && n_o[h] > 0) ok = ok && dsn_wait(o_empty + 8 * h, (n_o[h] - 1u) & 1u, abort_flag, p.status, 85);
-      ++n_p[h];
+    auto pv = [&]() {   // O_h (+)= P_h V, the oldest that is due
+      const uint32_t s = at0 % kStages, buf = n_p & 1u;
+      ok = ok && dsn_wait(p_full + 16 * h + 8 * buf, (n_p >> 1) & 1u, abort_flag, p.status, 83);
+      ok = ok && dsn_wait(v_full + 8 * s, (at0 / kStages) & 1u, abort_flag, p.status, 84);
+      if (first0 && n_o++ > 0) ok = ok && dsn_wait(o_empty + 8 * h, (n_o - 2u) & 1u, abort_flag, p.status, 85);
       if (!ok) return;
       if (elect_one()) {
         tc_fence_after();
-        const uint32_t region = tmem + h * kRegion;
-        const uint64_t dv = make_desc_mn(v_at + s * kOperand);
+        const uint64_t dv = make_desc_mn(v_at + s * kStage);
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks)
-          mma_a_tmem(region + kOCol, region + 8u * ks, dv + 128u * ks, idesc_o, ks > 0 ? 1u : (first_pv[h] ? 0u : 1u));
-        umma_commit(o_full + 8 * h);
+          mma_a_tmem(region + kOCol, region + kTile * buf + 8u * ks, dv + 128u * ks, idesc_o, ks > 0 ? 1u : (first0 ? 0u : 1u));
+        umma_commit(o_full + 16 * h + 8 * buf);
       }
       __syncwarp();
-      first_pv[h] = false;
-      pend[h] = false;
+      ++n_p;
+      at0 = at1;
+      first0 = first1;
     };
     auto release = [&](uint32_t bar) {
       if (elect_one()) umma_commit(bar);
       __syncwarp();
     };
     while (ok && walk.next(p, it)) {
-      int a[2], b[2];
-      half_tiles(it, 0, p.by_group, p.window, a[0], b[0]);
-      half_tiles(it, 1, p.by_group, p.window, a[1], b[1]);
+      int a, b;
+      half_tiles(it, h, p.by_group, p.window, a, b);
       for (int j = it.c0; j < it.c1 && ok; ++j, ++n) {
-        const uint32_t s = n & 1u;
-        if (j == it.c0) {   // what the item before still needs comes first: this item's Q arrives only behind its softmax
-          for (int h = 0; h < 2; ++h)
-            if (pend[h]) pv(h, n - 1u);
-          if (n > 0 && ok) release(v_empty + 8 * (s ^ 1u));
-          for (int h = 0; h < 2; ++h)
-            if (a[h] < b[h]) {
-              if (!first_pv[h]) ++n_o[h];
-              first_pv[h] = true;
-            }
-        }
-        for (int h = 0; h < 2 && ok; ++h) {
-          if (pend[h]) pv(h, n - 1u);
-          if (j >= a[h] && j < b[h] && ok) {
-            if (j == a[h]) ok = dsn_wait(q_full + 8 * h, n_q[h]++ & 1u, abort_flag, p.status, 86);
-            ok = ok && dsn_wait(k_full + 8 * s, (n >> 1) & 1u, abort_flag, p.status, 87);
-            if (!ok) break;
-            if (elect_one()) {
-              tc_fence_after();
-              const uint64_t dq = make_smem_desc(q_at + h * kOperand), dk = make_smem_desc(k_at + s * kOperand);
-#pragma unroll
-              for (int ks = 0; ks < D / 16; ++ks) {
-                const uint32_t off = (uint32_t)(ks >> 2) * (kTileBytes >> 4) + 2u * (ks & 3);
-                umma_bf16(tmem + h * kRegion, dq + off, dk + off, idesc_s, ks > 0 ? 1u : 0u);
-              }
-              umma_commit(s_full + 8 * h);
-            }
-            __syncwarp();
-            pend[h] = true;
-          }
-        }
+        const uint32_t s = n % kStages;
+        const bool needed = j >= a && j < b;
+        // a half that rests owes nothing: its softmax must come to the end of its item to fetch the next one's Q, and V's stages must come back
+        while (n_s - n_p > (needed ? 1u : 0u) && ok) pv();
+        if (needed && j == a) ok = ok && dsn_wait(q_full + 8 * h, n_q++ & 1u, abort_flag, p.status, 86);
+        ok = ok && dsn_wait(k_full + 8 * s, (n / kStages) & 1u, abort_flag, p.status, 87);
         if (!ok) break;
-        if (a[0] == b[0] && a[1] == b[1]) ok = dsn_wait(k_full + 8 * s, (n >> 1) & 1u, abort_flag, p.status, 87);   // a tile that nobody needs
-        release(k_empty + 8 * s);
-        if (j > it.c0) release(v_empty + 8 * (s ^ 1u));
+        if (elect_one()) {
+          if (needed) {
+            tc_fence_after();
+            const uint64_t dk = make_smem_desc(k_at + s * kStage);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+              umma_bf16(region + kTile * (n_s & 1u), dq + (uint32_t)(ks >> 2) * (kTileBytes >> 4) + 2u * (ks & 3),
+                        dk + (uint32_t)(ks >> 2) * (kTileBytes >> 5) + 2u * (ks & 3), idesc_s, ks > 0 ? 1u : 0u);
+            umma_commit(s_full + 16 * h + 8 * (n_s & 1u));
+          }
+          umma_commit(k_empty + 8 * s);
+        }
+        __syncwarp();
+        if (needed) {
+          if (n_s == n_p) at0 = n, first0 = j == a;
+          else at1 = n, first1 = j == a;
+          ++n_s;
+        }
+        // V's stages that no product is due with
+        const uint32_t due = n_s != n_p ? at0 : n + 1u;
+        for (; freed < due && ok; ++freed) {
+          ok = dsn_wait(v_full + 8 * (freed % kStages), (freed / kStages) & 1u, abort_flag, p.status, 92);
+          if (ok) release(v_empty + 8 * (freed % kStages));
+        }
       }
     }
-    for (int h = 0; h < 2; ++h)
-      if (pend[h] && ok) pv(h, n - 1u);
+    while (n_s != n_p && ok) pv();
   } else if (warp >= kSoftWarp) {
     // ------------------------------------------------------------------------------ softmax, a thread a row
     const int h = (warp - kSoftWarp) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t region = tmem + h * kRegion + ((uint32_t)(quarter * 32) << 16);
     const float c2 = fabsf(p.scale_log2);
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale goes into Q's signs
-    uint32_t n_s = 0, n_pv = 0, n = 0;   // S waited for, products with V asked for, tiles so far
+    uint32_t m = 0, n = 0;   // tiles of the half, of both
     bool ok = true;
     // The warp's rows of Q as fp16, the largest element of each brought to 1 .. 2; returns the power of two that goes into the scores of this lane's row.
     // D / 8 lanes read a row.
@@ -486,31 +486,48 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (lane == 0) mbar_arrive(q_full + 8 * h);
       return __uint_as_float(my_e << 23);
     };
+    // the lines of this lane's row of Q on their way to the second level of cache
+    auto warm_q = [&](const Item& x) {
+      const int v = x.s.v0 + 128 * h + row;
+      if (v >= x.s.v1) return;
+      const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
+      const __nv_bfloat16* q = p.qkv + ((int64_t)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((int64_t)x.head * (p.group + 2) + ev) * D;
+#pragma unroll
+      for (int i = 0; i < D; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
+    };
     CachePart ends{3, 0, 0, 0, 0, 0, 0, 0};   // what the CTA has to say about the ends of its stretch; rows: the tail's first vector, pad: one behind its last
     bool have = walk.next(p, it);
     int a = 0, b = 0;
-    float up = 1.f;
+    float up = 1.f, up_next = 1.f;
     if (have) {
       half_tiles(it, h, p.by_group, p.window, a, b);
       if (a < b) up = load_q(it);
     }
     while (have && ok) {
+      Item nx;
+      int na = 0, nb = 0;
+      have = walk.next(p, nx);
+      if (have) half_tiles(nx, h, p.by_group, p.window, na, nb);
       const int v = it.s.v0 + 128 * h + row;
       const bool live = v < it.s.v1;
       const int me = it.e.len - it.e.rows + (int)dsn_div((uint32_t)v, p.by_group);
       float ref = kLowest, l = 0.f;
       const float cs = c2 * up;
+      if (na < nb) warm_q(nx);
+      if (a == b && na < nb) up_next = load_q(nx);
       for (int j = a; j < b && ok; ++j) {
-        ok = dsn_wait(s_full + 8 * h, n_s & 1u, abort_flag, p.status, 88);
+        const uint32_t buf = m & 1u;
+        ok = dsn_wait(s_full + 16 * h + 8 * buf, (m >> 1) & 1u, abort_flag, p.status, 88);
         if (!ok) break;
-        ++n_s;
         tc_fence_after();
+        if (j + 1 == b && na < nb) up_next = load_q(nx);   // every product with this item's Q has run
+        const uint32_t at = region + kTile * buf;
         // columns of this tile that the row sees
         const int t0 = it.s.lo + j * kTile;
         const int k1 = me + 1 - t0, k0 = p.window ? me - p.window + 1 - t0 : 0;
-        const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 3u;
-        const uint64_t bad = *reinterpret_cast<const volatile uint64_t*>(s_bad + nt * 8);
-        const float2* fac = s_fac + nt * 8;
+        const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 7u;
+        const uint32_t bad = *reinterpret_cast<const volatile uint32_t*>(s_bad + nt * 4);
+        const float2* fac = s_fac + nt * 4;
         // of a block of 16: scores to units of the exponent (not 0: what is hidden is -infinity), the power of two of its V
         auto factors = [&](int c, float& t, float& sh) {
           const float2 f = fac[c];
@@ -521,7 +538,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         auto hide = [&](uint32_t (&x)[32], int c) {   // columns 32 c ...
           const int e1 = min(max(k1 - 32 * c, 0), 32), e0 = min(max(k0 - 32 * c, 0), 32);
           uint32_t m = (e1 >= 32 ? 0xffffffffu : (1u << e1) - 1u) & (e0 >= 32 ? 0u : 0xffffffffu << e0);
-          const uint32_t bb = (uint32_t)(bad >> (16 * c));
+          const uint32_t bb = bad >> (16 * c);
           if (bb & 0xffu) m &= 0xffff0000u;
           if (bb & 0xff00u) m &= 0x0000ffffu;
 #pragma unroll
@@ -530,30 +547,30 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         };
         float need = -INFINITY;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kTile / 32; ++c) {
           uint32_t x[32];
-          tmem_ld_32x32(region + 32 * c, x);
+          tmem_ld_32x32(at + 32 * c, x);
           float t0c, sh0, t1c, sh1;
           factors(2 * c, t0c, sh0);
           factors(2 * c + 1, t1c, sh1);
           tmem_ld_wait();
           if (cut) hide(x, c);
-          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              m[k] = max3_nan(m[k], __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1)]), __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1) + 1]));
-          need = max3_nan(need, fmaf(m[0], t0c, sh0), fmaf(m[1], t0c, sh0));
-          need = max3_nan(need, fmaf(m[2], t1c, sh1), fmaf(m[3], t1c, sh1));
+              top[k] = max3_nan(top[k], __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1)]), __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1) + 1]));
+          need = max3_nan(need, fmaf(top[0], t0c, sh0), fmaf(top[1], t0c, sh0));
+          need = max3_nan(need, fmaf(top[2], t1c, sh1), fmaf(top[3], t1c, sh1));
         }
         if (need != need) l = need;   // a token that is not finite: so is the row
         if (__any_sync(0xffffffffu, need > ref + kTop)) {
-          const float m = fmaxf(ref, need - kAim), f = ex2(ref - m);
-          ref = m;
+          const float to = fmaxf(ref, need - kAim), f = ex2(ref - to);
+          ref = to;
           l *= f;
           if (j > a) {
-            ok = dsn_wait(o_full + 8 * h, (n_pv - 1u) & 1u, abort_flag, p.status, 89);
+            ok = dsn_wait(o_full + 16 * h + 8 * (buf ^ 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 89);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -593,12 +610,12 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
             unpack2(fadd2(sum_a, sum_b), s0, s1);
             l = fmaf(s0 + s1, __uint_as_float((127u - (uint32_t)(int)sh) << 23), l);   // in units of 2^ref, without V's power
           }
-          tmem_st_16(region + (uint32_t)(16 * c), x);
+          tmem_st_16(at + (uint32_t)(16 * c), x);
         };
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kTile / 32; ++c) {
           uint32_t x[32];
-          tmem_ld_32x32(region + 32 * c, x);
+          tmem_ld_32x32(at + 32 * c, x);
           tmem_ld_wait();
           if (cut) hide(x, c);
           block(x, c);
@@ -606,30 +623,22 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         tmem_st_done();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 8 * h);
-        ++n_pv;
+        if (lane == 0) mbar_arrive(p_full + 16 * h + 8 * buf);
+        ++m;
       }
       if (!ok) break;
-      // the next item's Q: every product with this item's has run
-      const Item cur = it;
       const bool ran = a < b;
-      n += (uint32_t)(cur.c1 - cur.c0);
-      have = walk.next(p, it);
-      if (have) {
-        half_tiles(it, h, p.by_group, p.window, a, b);
-        if (a < b) up = load_q(it);
-      }
       if (ran) {
-        ok = dsn_wait(o_full + 8 * h, (n_pv - 1u) & 1u, abort_flag, p.status, 90);
+        ok = dsn_wait(o_full + 16 * h + 8 * ((m - 1u) & 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 90);
         if (!ok) break;
         tc_fence_after();
       }
-      const bool whole = cur.c0 == 0 && cur.c1 == cur.s.tiles;
+      const bool whole = it.c0 == 0 && it.c1 == it.s.tiles;
       const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? cur.e.pos : cur.e.sample) * p.R + r) * p.ld_out + ((int64_t)cur.head * p.group + ev) * D;
+      __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? it.e.pos : it.e.sample) * p.R + r) * p.ld_out + ((int64_t)it.head * p.group + ev) * D;
       // a part: references, sums, then four elements of every row after the other
-      float* part = p.cta_data + ((int64_t)blockIdx.x * 2 + (cur.c0 == 0)) * (kRows * (D + 2)) + 128 * h + row;
+      float* part = p.cta_data + ((int64_t)blockIdx.x * 2 + (it.c0 == 0)) * (kRows * (D + 2)) + 128 * h + row;
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
@@ -669,10 +678,15 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         part[0] = ref;
         part[kRows] = l;
       }
-      if (cur.c0 > 0) ends.head_state = cur.c1 == cur.s.tiles ? 1 : 2;
+      if (it.c0 > 0) ends.head_state = it.c1 == it.s.tiles ? 1 : 2;
       else if (ends.head_state == 3) ends.head_state = 0;
-      if (cur.c0 == 0 && !whole)
-        ends = CachePart{ends.head_state, 1, cur.e.sample, cur.e.pos, cur.head, cur.s.v0, 0, cur.s.v1};
+      if (it.c0 == 0 && !whole)
+        ends = CachePart{ends.head_state, 1, it.e.sample, it.e.pos, it.head, it.s.v0, 0, it.s.v1};
+      n += (uint32_t)(it.c1 - it.c0);
+      it = nx;
+      a = na;
+      b = nb;
+      up = up_next;
     }
     if (!ok) ends.head_state = 3, ends.tail = 0;
     if (warp == kSoftWarp && lane == 0) p.parts[blockIdx.x] = ends;
@@ -731,7 +745,7 @@ __global__ void __launch_bounds__(kRows) cache_rows_join_kernel(const __grid_con
 template <int D>
 cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
   static size_t configured[DSN_MAX_DEVICES] = {};
-  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes + 2 * (kHalf / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D);
+  constexpr size_t smem = 1024 + kCtrlR + 6 * (size_t)(D / 64) * kTileBytes + 2 * (kTile / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
   cudaError_t e = dsn_ensure_dynamic_smem(cache_rows_kernel<D>, smem, configured);
   if (e != cudaSuccess) return e;

@@ -250,6 +250,22 @@ def test_long_request(dsn, R, group):
     compare(pages, [1], group, [0, 0], R, None, x, got)
 
 
+@pytest.mark.parametrize("D,group", [(64, 3), (128, 4), (128, 1)])
+def test_many_items_one_after_the_other(dsn, D, group):
+    """Stretches of many tiles and many items: whole, half filled and cut ones, tiles that only one half of the rows needs."""
+    g = np.random.default_rng(13)
+    lengths = [int(n) for n in g.integers(1, 400, size=260)] + [4000, 300, 2000, 129]
+    R = 90
+    placed = [int(min(n, g.integers(0, R + 1))) for n in lengths]
+    placed[-4:] = [R, R, 17, R]
+    pages = Pages(g, lengths, 2, D, 48)
+    idx = [i % 2 for i in range(len(lengths))]
+    for window in (0, 70):
+        x, got, status = attend(dsn, g, pages, [1, 2], group, idx, R, placed, "grouped", window=window)
+        assert status[0] == 0
+        compare(pages, [1, 2], group, idx, R, placed, x, got, window=window, every=3)
+
+
 def test_samples_outside_every_group_are_left_alone(dsn):
     g = np.random.default_rng(12)
     pages = Pages(g, [50, 60, 70], 1, 64, 16)
