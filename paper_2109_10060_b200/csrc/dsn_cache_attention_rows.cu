@@ -9,12 +9,11 @@
 //   warp 5       loader: pages' numbers, and the blocks as bulk copies into two slots of a tile.
 //   warps 6-7    issue, one a half: S_h = Q_h K^T and O_h += P_h V.  S has two buffers a half: a half's product of scores runs a tile ahead, so its softmax
 //                never waits for it.  (One warp for both spends more time on barriers than the products take.)
-//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), 32 columns of S in registers at a time (few registers let more
-//                instructions overlap); maximum, exp2, sum, probabilities over the columns of S, from where the second product takes them.  They also fetch the
+//   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), the tile's row of S in registers; maximum, exp2, sum, probabilities over the columns of S, from where the second product takes them.  They also fetch the
 //                rows of Q and write those of O.
 // Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
-// goes into the scale of its scores; a block of 16 tokens has one for K, which goes there, too, and one for V, which the probabilities of
-// those tokens take up.  Everything of a row is in units of 2^g, g a reference that moves only when a probability with its power of two would
+// goes into the scale of its scores; a tile has one for K, which goes there, too, and one for V, which the probabilities of its tokens
+// take up.  Everything of a row is in units of 2^g, g a reference that moves only when a probability with its power of two would
 // pass 2^15: then O is read, scaled and written back.
 // The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (a mask each pair), so Q's and O's columns are in that order, too.
 // TMEM: 512 columns = two regions of 256: two buffers of S_h at 0 and 64, P_h over the first half of each, O_h from 128.  Every wait is bounded.
@@ -32,7 +31,6 @@ constexpr int kValueWarps = 5, kLoadWarp = 5, kIssueWarp = 6, kSoftWarp = 8;
 constexpr float kTop = 15.f, kAim = 7.f;     // a probability with its power of two is at most 2^15, 2^7 where the reference has just moved
 constexpr uint32_t kTileBytes = 128 * 128;   // 128 rows of 64 bf16
 constexpr uint32_t kCtrlR = 4096;
-constexpr int kEvery = 4;                     // of so many exponentials one is computed on the FMA pipe
 constexpr uint32_t kRegion = 256, kOCol = 128;
 
 __device__ __forceinline__ void mma_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -81,24 +79,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {   // NaN 
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-// 2^t of two arguments without the special-function unit, t at most a few tens: t = n + f with n = round(t) taken from the mantissa of t + 1.5 * 2^23, 2^f by a
-// cubic (own fit, relative error 7.5e-5, a fiftieth of a bf16 rounding step), n added to the exponent.  Below -126: 2^-126.
-__device__ __forceinline__ void exp2_pair(uint64_t t2, float& x0, float& x1) {
-  float t0, t1;
-  unpack2(t2, t0, t1);
-  t2 = pack2(fmaxf(t0, -126.f), fmaxf(t1, -126.f));
-  const uint64_t r2 = fadd2(t2, pack2(12582912.f, 12582912.f));
-  const uint64_t n2 = fadd2(r2, pack2(-12582912.f, -12582912.f));
-  const uint64_t f2 = ffma2(n2, pack2(-1.f, -1.f), t2);
-  uint64_t p2 = ffma2(pack2(0.0551716685f, 0.0551716685f), f2, pack2(0.2426111251f, 0.2426111251f));
-  p2 = ffma2(p2, f2, pack2(0.6932609677f, 0.6932609677f));
-  p2 = ffma2(p2, f2, pack2(0.9999280572f, 0.9999280572f));
-  float r0, r1, p0, p1;
-  unpack2(r2, r0, r1);
-  unpack2(p2, p0, p1);
-  x0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23));
-  x1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23));
 }
 // V as it lies: rows are tokens, 64 elements in 128 bytes; 128 elements are two such pieces of a stage.
 __device__ __forceinline__ uint64_t make_desc_mn(uint32_t addr) {
@@ -199,8 +179,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 288);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 292);
   uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there, bit 4 + b: its page is outside the cache; tokens << 8
-  uint8_t* s_bad = smem + 320;                                                     // [8 tiles][4 blocks]: 1: of a page outside the cache
-  float2* s_fac = reinterpret_cast<float2*>(smem + 384);                           // [8 tiles][4 blocks]: K's power of two; V's, as its exponent
+  uint8_t* s_bad = smem + 320;                                                     // [8 tiles]: bit b: block b is of a page outside the cache
+  float2* s_fac = reinterpret_cast<float2*>(smem + 384);                           // [8 tiles]: K's power of two; V's, as its exponent
   uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 640);
   CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 1024);
   static_assert(1024 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
@@ -264,11 +244,22 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     // Unit u of tile number i: K (0-3) or V (4-7) of block u & 3; warp w takes units w, w + 5, ... of all.
     const uint32_t units = 8u * (uint32_t)(stretch.Z - stretch.A);
     const int tok = lane & 15, part = lane >> 4;      // D = 128: a lane takes a group; D = 64: half of it
-    auto top_of = [](uint32_t pair) -> uint32_t {     // exponent of the largest element that the pair can stand for
-      const float top = fabsf(hi_bf16(pair)) + 8.f * fabsf(lo_bf16(pair));
-      return top <= 3.4e38f ? __float_as_uint(top) >> 23 : 0u;
+    // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers; every unit finds it anew from the tile's pairs
+    auto exponent = [&](uint32_t slot, uint32_t info, bool of_v) -> uint32_t {
+      uint32_t e = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int t = lane + 32 * i;
+        const bool there = (info >> (t >> 4) & 1u) && t < (int)(info >> 8);
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr) {
+          const uint32_t pr = lds32(slot + (uint32_t)(t >> 4) * kBlock + (of_v ? kBlock / 2 : 0u) + GR * 512 + gr * 64 + (t & 15) * 4);
+          const float top = fabsf(hi_bf16(pr)) + 8.f * fabsf(lo_bf16(pr));
+          if (there && top <= 3.4e38f) e = max(e, __float_as_uint(top) >> 23);
+        }
+      }
+      return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
     };
-    auto held = [](uint32_t e) -> uint32_t { return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u); };   // 2^e and 2^-e are normal numbers
 #pragma unroll 1
     for (uint32_t unit = (uint32_t)warp; unit < units; unit += kValueWarps) {
       const uint32_t i = unit >> 3, s = i % kStages, b = unit & 3u;
@@ -276,22 +267,20 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (!dsn_wait(raw_full + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
       const uint32_t info = *reinterpret_cast<const volatile uint32_t*>(s_raw + (i & 1u));
       const bool there = (info >> b & 1u) && (int)(b * 16u) + tok < (int)(info >> 8);
-      const uint32_t blk = raw_at + (i & 1u) * kSlot + b * kBlock, src = blk + (is_v ? kBlock / 2 : 0u);
-      const uint32_t pair_at = GR * 512u + (GR == 2 ? (uint32_t)part * 64u : 0u) + (uint32_t)tok * 4u;
-      uint32_t v_pair = there ? lds32(blk + kBlock / 2 + pair_at) : 0u, pair = there ? lds32(src + pair_at) : 0u;
+      const uint32_t slot = raw_at + (i & 1u) * kSlot, src = slot + b * kBlock + (is_v ? kBlock / 2 : 0u);
+      uint32_t pair = there ? lds32(src + GR * 512u + (GR == 2 ? (uint32_t)part * 64u : 0u) + (uint32_t)tok * 4u) : 0u;
       // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
-      if (!(fabsf(lo_bf16(v_pair)) <= 3.4e38f) || !(fabsf(hi_bf16(v_pair)) <= 3.4e38f)) v_pair = 0u;
-      if (is_v) pair = v_pair;
-      const uint32_t e = held(top_of(pair));
+      if (is_v && (!(fabsf(lo_bf16(pair)) <= 3.4e38f) || !(fabsf(hi_bf16(pair)) <= 3.4e38f))) pair = 0u;
+      const uint32_t e = exponent(slot, info, is_v);
       uint32_t q[GR][4];
 #pragma unroll
       for (int x = 0; x < GR; ++x) lds128(src + (GR == 2 ? (uint32_t)(part * 512 + tok * 32 + 16 * x) : (uint32_t)(tok * 32 + 16 * part)), q[x]);
       if (i >= kStages && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, (i / kStages - 1u) & 1u, abort_flag, p.status, 81)) break;
-      if (!is_v) {
-        const uint32_t ve = held(top_of(v_pair)), k = (i & 7u) * 4 + b;
+      if ((unit & 7u) == 0) {
+        const uint32_t ve = exponent(slot, info, true);
         if (lane == 0) {
-          s_bad[k] = (uint8_t)(info >> (4 + b) & 1u);
-          s_fac[k] = make_float2(__uint_as_float(e << 23), (float)((int)ve - 127));
+          s_bad[i & 7u] = (uint8_t)(info >> 4 & 15u);
+          s_fac[i & 7u] = make_float2(__uint_as_float(e << 23), (float)((int)ve - 127));
         }
       }
       const float down = __uint_as_float((254u - e) << 23);
@@ -513,6 +502,10 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       const int me = it.e.len - it.e.rows + (int)dsn_div((uint32_t)v, p.by_group);
       float ref = kLowest, l = 0.f;
       const float cs = c2 * up;
+      // tiles that all rows of the warp see whole: plain0 .. plain1 - 1 (rows in a row: the first sees least, the last begins last)
+      const int first_me = __reduce_min_sync(0xffffffffu, live ? me : INT32_MAX), last_me = __reduce_max_sync(0xffffffffu, live ? me : INT32_MIN);
+      const int plain1 = first_me == INT32_MAX ? INT32_MAX : max(0, first_me + 1 - it.s.lo) / kTile;
+      const int plain0 = p.window && last_me != INT32_MIN ? (max(0, last_me - p.window + 1 - it.s.lo) + kTile - 1) / kTile : 0;
       if (na < nb) warm_q(nx);
       if (a == b && na < nb) up_next = load_q(nx);
       for (int j = a; j < b && ok; ++j) {
@@ -522,48 +515,35 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         tc_fence_after();
         if (j + 1 == b && na < nb) up_next = load_q(nx);   // every product with this item's Q has run
         const uint32_t at = region + kTile * buf;
-        // columns of this tile that the row sees
-        const int t0 = it.s.lo + j * kTile;
-        const int k1 = me + 1 - t0, k0 = p.window ? me - p.window + 1 - t0 : 0;
         const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 7u;
-        const uint32_t bad = *reinterpret_cast<const volatile uint32_t*>(s_bad + nt * 4);
-        const float2* fac = s_fac + nt * 4;
-        // of a block of 16: scores to units of the exponent (not 0: what is hidden is -infinity), the power of two of its V
-        auto factors = [&](int c, float& t, float& sh) {
-          const float2 f = fac[c];
-          t = fmaxf(cs * f.x, 1e-37f);
-          sh = f.y;
-        };
-        const bool cut = __any_sync(0xffffffffu, live && (k1 < kTile || k0 > 0)) || bad != 0;
-        auto hide = [&](uint32_t (&x)[32], int c) {   // columns 32 c ...
-          const int e1 = min(max(k1 - 32 * c, 0), 32), e0 = min(max(k0 - 32 * c, 0), 32);
-          uint32_t m = (e1 >= 32 ? 0xffffffffu : (1u << e1) - 1u) & (e0 >= 32 ? 0u : 0xffffffffu << e0);
-          const uint32_t bb = bad >> (16 * c);
-          if (bb & 0xffu) m &= 0xffff0000u;
-          if (bb & 0xff00u) m &= 0x0000ffffu;
+        const uint32_t bad = *reinterpret_cast<const volatile uint8_t*>(s_bad + nt);
+        // scores to units of the exponent (not 0: what is hidden is -infinity), V's power of two
+        const float2 fac = s_fac[nt];
+        const float t = fmaxf(cs * fac.x, 1e-37f), sh = fac.y;
+        uint32_t x[2][32];
+        tmem_ld_32x32(at, x[0]);
+        tmem_ld_32x32(at + 32, x[1]);
+        tmem_ld_wait();
+        if (j < plain0 || j >= plain1 || bad != 0) {   // columns that the row does not see
+          const int t0 = it.s.lo + j * kTile, k1 = me + 1 - t0, k0 = p.window ? me - p.window + 1 - t0 : 0;
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (!(m >> i & 1u)) x[i] = 0xff800000u;
-        };
-        float need = -INFINITY;
-#pragma unroll 1
-        for (int c = 0; c < kTile / 32; ++c) {
-          uint32_t x[32];
-          tmem_ld_32x32(at + 32 * c, x);
-          float t0c, sh0, t1c, sh1;
-          factors(2 * c, t0c, sh0);
-          factors(2 * c + 1, t1c, sh1);
-          tmem_ld_wait();
-          if (cut) hide(x, c);
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int c = 0; c < 2; ++c) {
+            const int e1 = min(max(k1 - 32 * c, 0), 32), e0 = min(max(k0 - 32 * c, 0), 32);
+            uint32_t m = (e1 >= 32 ? 0xffffffffu : (1u << e1) - 1u) & (e0 >= 32 ? 0u : 0xffffffffu << e0);
+            if (bad >> (2 * c) & 1u) m &= 0xffff0000u;
+            if (bad >> (2 * c) & 2u) m &= 0x0000ffffu;
 #pragma unroll
-          for (int i = 0; i < 16; i += 4)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              top[k] = max3_nan(top[k], __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1)]), __uint_as_float(x[16 * (k >> 1) + i + 2 * (k & 1) + 1]));
-          need = max3_nan(need, fmaf(top[0], t0c, sh0), fmaf(top[1], t0c, sh0));
-          need = max3_nan(need, fmaf(top[2], t1c, sh1), fmaf(top[3], t1c, sh1));
+            for (int i = 0; i < 32; ++i)
+              if (!(m >> i & 1u)) x[c][i] = 0xff800000u;
+          }
         }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            top[k] = max3_nan(top[k], __uint_as_float(x[k >> 1][i + 2 * (k & 1)]), __uint_as_float(x[k >> 1][i + 2 * (k & 1) + 1]));
+        const float need = fmaf(max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]), t, sh);
         if (need != need) l = need;   // a token that is not finite: so is the row
         if (__any_sync(0xffffffffu, need > ref + kTop)) {
           const float to = fmaxf(ref, need - kAim), f = ex2(ref - to);
@@ -584,42 +564,23 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
             }
           }
         }
-        auto block = [&](uint32_t (&x)[32], int c) {   // columns 32 c ...
+        const uint64_t t_2 = pack2(t, t), ref_2 = pack2(sh - ref, sh - ref);
+        uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float t, sh;
-            factors(2 * c + k, t, sh);
-            const uint64_t to_2 = pack2(t, t), ref_2 = pack2(sh - ref, sh - ref);
-            uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
+        for (int c = 0; c < 2; ++c) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float x0, x1;
-              const uint64_t t2 = ffma2(pack2(__uint_as_float(x[16 * k + 2 * e]), __uint_as_float(x[16 * k + 2 * e + 1])), to_2, ref_2);
-              if (e % kEvery == kEvery - 1) {
-                exp2_pair(t2, x0, x1);   // some on the FMA pipe; what is hidden comes out as 2^-126, a zero in fp16
-              } else {
-                float t0f, t1f;
-                unpack2(t2, t0f, t1f);
-                x0 = ex2(t0f);
-                x1 = ex2(t1f);
-              }
-              if (e & 1) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
-              x[8 * k + e] = pack_f16(x0, x1);
-            }
-            float s0, s1;
-            unpack2(fadd2(sum_a, sum_b), s0, s1);
-            l = fmaf(s0 + s1, __uint_as_float((127u - (uint32_t)(int)sh) << 23), l);   // in units of 2^ref, without V's power
+          for (int e = 0; e < 16; ++e) {
+            float t0, t1;
+            unpack2(ffma2(pack2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), t_2, ref_2), t0, t1);
+            const float x0 = ex2(t0), x1 = ex2(t1);
+            if (e & 1) sum_b = fadd2(sum_b, pack2(x0, x1)); else sum_a = fadd2(sum_a, pack2(x0, x1));
+            x[c][e] = pack_f16(x0, x1);
           }
-          tmem_st_16(at + (uint32_t)(16 * c), x);
-        };
-#pragma unroll 1
-        for (int c = 0; c < kTile / 32; ++c) {
-          uint32_t x[32];
-          tmem_ld_32x32(at + 32 * c, x);
-          tmem_ld_wait();
-          if (cut) hide(x, c);
-          block(x, c);
+          tmem_st_16(at + (uint32_t)(16 * c), x[c]);
         }
+        float s0, s1;
+        unpack2(fadd2(sum_a, sum_b), s0, s1);
+        l = fmaf(s0 + s1, __uint_as_float((127u - (uint32_t)(int)sh) << 23), l);   // in units of 2^ref, without V's power
         tmem_st_done();
         tc_fence_before();
         __syncwarp();
