@@ -1,20 +1,25 @@
 // Attention over the 4-bit cache, a few query vectors a head (rows * group <= 16: single tokens, shared heads, a few tokens at once).
 //
-// Bound by memory: a cached token is 18 D / 16 bytes a head, read once for all query vectors of the head.  Work is dealt out in steps of 32 tokens:
-// all steps of all (request, head) items stand in one line, and every warp of the GPU gets an equal stretch of it, so neither few long requests nor
-// many short ones leave SMs idle.  A warp keeps the steps to come in flight as bulk copies into a ring of its own (no barrier with other
-// warps), a block of 16 tokens a copy, as pages may end after any block.
-// An item that lies in one warp's stretch is finished there; of an item that is cut, each warp leaves its maximum, sum and products (fp32) in the
-// workspace, and a second small kernel joins them.
+// Bound by memory: a cached token is 18 D / 16 bytes a head, read once for all query vectors of the head.  Work is dealt out in steps (32 tokens of 128
+// elements, 64 of 64): all steps of all (request, head) items stand in one line, and every warp of the GPU gets an equal stretch of it, so neither few
+// long requests nor many short ones leave SMs idle.  A warp keeps the steps to come in flight as bulk copies into a ring of its own (no barrier with
+// other warps), a block of 16 tokens a copy, as pages may end after any block.
+// An item that lies in one warp's stretch is finished there.  What the warps of a CTA cut among themselves they join in shared memory; of an item that is
+// cut between CTAs, each leaves its reference, sum and products (fp32) in the workspace, and a second small kernel joins them.
 //
-// Products on the tensor cores, with the tokens as rows: S^T = K Q^T (16 tokens x 8 queries x 16 elements an instruction), O^T = V^T P^T.
-//   Codes become bf16 numbers 128 + code with one mask each; for K the 128 + 8 is taken off by starting the accumulator at -136 sum(q), which costs
-//   nothing, and scale and middle of a token's group are applied to the sum in fp32: the scores are as exact as fp32 sums.
-//   For V the 136 is subtracted (a sum over thousands of tokens would lose bits to it), the scale goes into the probability before its
-//   one rounding to bf16, the middle into a sum of its own in fp32.
+// Products on the tensor cores, with the tokens as rows: S^T = K Q^T (16 tokens x 8 queries x 16 elements an instruction), O^T = V^T P^T, fp16 operands.
+//   Codes become fp16 numbers with one mask each: 1024 + code, or 1024 + 16 code from the high half of a byte.  For K the offsets are taken off by
+//   starting the accumulator at minus their product with the query (and the 16 by a sixteenth in the query), which costs nothing; scale and
+//   middle of a token's group are applied to the sum in fp32, so the scores are nearly as exact as fp32 sums (the offset costs 2^-24 of 1024 |q|).
+//   For V the offset is subtracted (a sum over thousands of tokens would lose bits to it), the scale goes into the probability before its
+//   one rounding to fp16, the middle into a sum of its own in fp32.
 // The order of elements in a product is free, so a lane takes whole words: 16 elements of K in 8 bytes, 8 elements of V in 4.  Row i of a block's K is token
 // i ^ (i >> 2 & 1): then neither K's rows nor the pairs of tokens that a lane needs of V meet in a bank.
-// The maximum is a reference that moves only when a score stands more than 2^8 above it (one vote a step instead of a reduction).
+// Queries are brought to 1 .. 2 by a power of two, which goes into the scale.  Everything of a query is in units of 2^ref, a reference that moves only when a
+// probability times the largest power of two in the step's scales would pass 2^15 (one vote a step instead of a reduction): fp16 then holds every product of
+// a probability and a scale, whatever their range.
+#include <cuda_fp16.h>
+
 #include "dsn_cache_line.cuh"
 
 namespace {
@@ -22,11 +27,11 @@ namespace {
 using namespace dsn_q4;
 using dsn_gemm::smem_u32;
 
-constexpr int kStepBlocks = 2, kStepTokens = 32;
+constexpr float kTop = 15.f, kAim = 7.f;   // see the reference above; 2^7 is what the largest has when it has just moved
 constexpr uint32_t kCtrl = 2048;  // behind the list: sums of a scan, the abort flag, what the warps say about their ends
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -65,13 +70,28 @@ struct Walk {
 };
 
 template <int D>
-__host__ __device__ constexpr uint32_t step_bytes() { return kStepBlocks * dsn_cache_block_bytes(D); }
+__host__ __device__ constexpr int step_blocks() { return 256 / D; }
+template <int D>
+__host__ __device__ constexpr uint32_t step_bytes() { return step_blocks<D>() * dsn_cache_block_bytes(D); }
 template <int D, int WARPS, int DEPTH>
 constexpr size_t attention_smem() { return kCtrl + kListSmem * sizeof(CacheEntry) + WARPS * DEPTH * 8 + (size_t)WARPS * DEPTH * step_bytes<D>(); }
+
+// 1024 + code of elements 0 and 4 (1 and 5 of the word shifted by 8: 2 and 6), 1024 + 16 code of elements 1 and 5 (3 and 7)
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return (w & 0x000f000fu) | 0x64006400u; }
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return (w & 0x00f000f0u) | 0x64006400u; }
+__device__ __forceinline__ uint32_t code_of_low(uint32_t h) {   // code - 8
+  const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(-1032.f));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t code_of_high(uint32_t h) {
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(0.0625f), __float2half2_rn(-72.f));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
 
 template <int D, int NT, int WARPS, int DEPTH>
 __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __grid_constant__ CacheAttParams p) {
   constexpr int THREADS = WARPS * 32, GR = D / 64, NC = 8 * NT;
+  constexpr int SB = step_blocks<D>(), kStepTokens = SB * DSN_CACHE_BLOCK;
   constexpr int kPart = NC * (D + 2);   // floats of a part: references, sums, products
   constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kHalf = kBlock / 2, kPairs = GR * 512;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -94,7 +114,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   const Stretch stretch = find_stretch<THREADS>(p, s_list, s_scan, [&](int len, int rows) {
     int lo, hi;
     item_range(len, rows, p.window, lo, hi);
-    return max(1, (hi - lo + kStepTokens - 1) / kStepTokens);   // a request without tokens: a step that sees nothing, for the zeros
+    return max(1, (hi - lo + 256 / D * DSN_CACHE_BLOCK - 1) / (256 / D * DSN_CACHE_BLOCK));   // a request without tokens: a step that sees nothing, for the zeros
   });
   const uint64_t A = stretch.A, Z = stretch.Z;
   const uint64_t u0 = A + (Z - A) * warp / WARPS, u1 = A + (Z - A) * (warp + 1) / WARPS;
@@ -123,43 +143,62 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   const int n_steps = (int)(u1 - u0);
   const int bpp = p.page / DSN_CACHE_BLOCK;   // blocks a page
 
-  // copies of one step into a slot; bit b of the result: block b is there
-  auto issue = [&](int slot) -> uint32_t {
-    int lo, hi;
-    item_range(fetch.e.len, fetch.e.rows, p.window, lo, hi);
-    const int tok = lo + fetch.step * kStepTokens + lane * DSN_CACHE_BLOCK;
-    bool ok = lane < kStepBlocks && tok < hi;
-    const uint8_t* src = nullptr;
-    if (ok) {
-      const int blk = tok / DSN_CACHE_BLOCK, col = (int)dsn_div((uint32_t)tok, p.by_page);
-      const int pg = p.table[(int64_t)fetch.e.sample * p.max_pages + col];
-      if (pg < 0 || pg >= p.n_pages) {
-        dsn_set_status(p.status, DSN_ERR_BAD_INDEX, fetch.e.sample);
-        ok = false;
-      }
-      src = p.pages + (((int64_t)pg * p.H + fetch.head) * bpp + (blk - col * bpp)) * kBlock;
+  // The fetching side: lane b < SB fetches block b of a step; the page's number is read a step before the copy that needs it.
+  int f_tok = 0, f_hi = 0, pg = -1, place = 0;   // this lane's token, the item's end; the page and the block in it
+  const int32_t* f_row = nullptr;
+  int64_t f_head = 0;
+  bool wanted = false;
+  auto enter = [&]() {   // the item that `fetch` stands in
+    int lo;
+    item_range(fetch.e.len, fetch.e.rows, p.window, lo, f_hi);
+    f_tok = lo + fetch.step * kStepTokens + lane * DSN_CACHE_BLOCK;
+    f_row = p.table + (int64_t)fetch.e.sample * p.max_pages;
+    f_head = (int64_t)fetch.head * bpp;
+  };
+  auto find = [&]() {
+    wanted = lane < SB && f_tok < f_hi;
+    pg = -1;
+    if (wanted) {
+      const int col = (int)dsn_div((uint32_t)f_tok, p.by_page);
+      pg = f_row[col];
+      place = f_tok / DSN_CACHE_BLOCK - col * bpp;
     }
+  };
+  const int64_t page_blocks = (int64_t)p.H * bpp;
+  auto issue = [&](int slot) -> uint32_t {   // bit b of the result: block b is on its way
+    const bool ok = pg >= 0 && pg < p.n_pages;
+    if (wanted && !ok) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, fetch.e.sample);
     const uint32_t there = __ballot_sync(0xffffffffu, ok);
     if (lane == 0) dsn_gemm::mbar_expect_tx(bars + 8u * slot, (uint32_t)__popc(there) * kBlock);
     __syncwarp();
-    if (ok) dsn_bulk_load(ring + (uint32_t)slot * step_bytes<D>() + (uint32_t)lane * kBlock, src, kBlock, bars + 8u * slot);
+    if (ok)
+      dsn_bulk_load(ring + (uint32_t)slot * step_bytes<D>() + (uint32_t)lane * kBlock, p.pages + (pg * page_blocks + f_head + place) * kBlock, kBlock,
+                    bars + 8u * slot);
     return there;
+  };
+  auto step_on = [&]() {   // to the next step of the stretch
+    const int j = fetch.j, hd = fetch.head;
+    fetch.advance();
+    if (fetch.j != j || fetch.head != hd) enter(); else f_tok += kStepTokens;
+    find();
   };
 
   int asked = 0;
-  uint32_t there = 0;   // two bits a slot
+  uint32_t there = 0;   // SB bits a slot
+  enter();
+  find();
   for (; asked < DEPTH && asked < n_steps; ++asked) {
-    there |= issue(asked) << (2 * asked);
-    if (asked + 1 < n_steps) fetch.advance();
+    there |= issue(asked) << (SB * asked);
+    if (asked + 1 < n_steps) step_on();
   }
 
   uint32_t qf[NT][GR][4][2];
-  float qsum[NT][GR][2];
-  float o[NT][GR][4][4], oz[NT][GR][2], l[NT][2], mref[NT][2];
+  float qsum[NT][GR][2], qoff[NT][GR][2], cs[NT][2];   // of this lane's columns: sum of the query, minus the offsets' product with it, factor of the scores
+  float o[NT][GR][4][4], oz[NT][GR][2], l[NT][2], ref[NT][2];
+  int row_of[NT][2];                 // rows of this lane's columns
   bool fresh = true, ok = true;
   bool head_open = work.step != 0;   // the first item began in an earlier warp's stretch
   head_state = 0;
-  int row_of[NT][2];   // rows of this lane's columns
   const int kap = g ^ (g >> 2);      // token of K's row g in a block
   uint32_t slot = 0, parity = 0;
 
@@ -171,25 +210,55 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
       fresh = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int v = nt * 8 + g, r = v / p.group, ev = v - r * p.group;
+        const int v = nt * 8 + g, r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
         const __nv_bfloat16* q = p.qkv + (row0 + r) * p.ld_qkv + ((int64_t)work.head * (p.group + 2) + ev) * D;
+        uint4 w[GR][2];
+        uint32_t top = 0;
 #pragma unroll
-        for (int gr = 0; gr < GR; ++gr) {
-          float sum = 0.f;
+        for (int gr = 0; gr < GR; ++gr)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (v < cols) w = *reinterpret_cast<const uint4*>(q + gr * 64 + 16 * t + 8 * h);
-            sum += ((lo_bf16(w.x) + hi_bf16(w.x)) + (lo_bf16(w.y) + hi_bf16(w.y))) + ((lo_bf16(w.z) + hi_bf16(w.z)) + (lo_bf16(w.w) + hi_bf16(w.w)));
-            qf[nt][gr][2 * h][0] = __byte_perm(w.x, w.z, 0x5410);
-            qf[nt][gr][2 * h][1] = __byte_perm(w.x, w.z, 0x7632);
-            qf[nt][gr][2 * h + 1][0] = __byte_perm(w.y, w.w, 0x5410);
-            qf[nt][gr][2 * h + 1][1] = __byte_perm(w.y, w.w, 0x7632);
+            w[gr][h] = make_uint4(0, 0, 0, 0);
+            if (v < cols) w[gr][h] = *reinterpret_cast<const uint4*>(q + gr * 64 + 16 * t + 8 * h);
           }
-          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(w[gr][h].x & 0x7fff7fffu, w[gr][h].y & 0x7fff7fffu), __vmaxu2(w[gr][h].z & 0x7fff7fffu, w[gr][h].w & 0x7fff7fffu)));
+        uint32_t ex = max(top & 0xffffu, top >> 16);
+        ex = max(ex, __shfl_xor_sync(0xffffffffu, ex, 1));
+        ex = max(ex, __shfl_xor_sync(0xffffffffu, ex, 2)) >> 7;
+        ex = ex == 255u ? 127u : min(max(ex, 27u), 253u);   // a query that is not finite stays so
+        const float down = __uint_as_float((254u - ex) << 23), up = p.scale_log2 * __uint_as_float(ex << 23);
+        cs[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t);
+        cs[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr) {
+          float even = 0.f, odd = 0.f;   // sums of the numbers as they stand in the product
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 x = w[gr][h];
+            const __half2 y[4] = {__floats2half2_rn(lo_bf16(x.x) * down, lo_bf16(x.z) * down),                         // elements 0, 4
+                                  __floats2half2_rn(hi_bf16(x.x) * down * 0.0625f, hi_bf16(x.z) * down * 0.0625f),     // 1, 5
+                                  __floats2half2_rn(lo_bf16(x.y) * down, lo_bf16(x.w) * down),                         // 2, 6
+                                  __floats2half2_rn(hi_bf16(x.y) * down * 0.0625f, hi_bf16(x.w) * down * 0.0625f)};    // 3, 7
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float2 f = __half22float2(y[k]);
+              if (k & 1) odd += f.x + f.y; else even += f.x + f.y;
+              qf[nt][gr][2 * h + (k >> 1)][k & 1] = *reinterpret_cast<const uint32_t*>(&y[k]);
+            }
+          }
+          even += __shfl_xor_sync(0xffffffffu, even, 1);
+          even += __shfl_xor_sync(0xffffffffu, even, 2);
+          odd += __shfl_xor_sync(0xffffffffu, odd, 1);
+          odd += __shfl_xor_sync(0xffffffffu, odd, 2);
+          const float sum = fmaf(16.f, odd, even), off = -fmaf(1032.f, even, 1152.f * odd);   // code - 8 is the number less 1032, a sixteenth of it less 72
           qsum[nt][gr][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
           qsum[nt][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+          qoff[nt][gr][0] = __shfl_sync(0xffffffffu, off, 8 * t);
+          qoff[nt][gr][1] = __shfl_sync(0xffffffffu, off, 8 * t + 4);
           oz[nt][gr][0] = oz[nt][gr][1] = 0.f;
 #pragma unroll
           for (int mt = 0; mt < 4; ++mt)
@@ -197,67 +266,63 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
             for (int x = 0; x < 4; ++x) o[nt][gr][mt][x] = 0.f;
         }
         l[nt][0] = l[nt][1] = 0.f;
-        mref[nt][0] = mref[nt][1] = kLowest;
-        row_of[nt][0] = (nt * 8 + 2 * t) / p.group;
-        row_of[nt][1] = (nt * 8 + 2 * t + 1) / p.group;
+        ref[nt][0] = ref[nt][1] = kLowest;
+        row_of[nt][0] = (int)dsn_div((uint32_t)(nt * 8 + 2 * t), p.by_group);
+        row_of[nt][1] = (int)dsn_div((uint32_t)(nt * 8 + 2 * t + 1), p.by_group);
       }
     }
     int lo, hi;
     item_range(e.len, e.rows, p.window, lo, hi);
     const int tok0 = lo + work.step * kStepTokens;
-    const uint32_t here = (there >> (2 * slot)) & 3u;
+    const uint32_t here = (there >> (SB * slot)) & ((1u << SB) - 1u);
     // all tokens of the step seen by all rows?
     const int first_tok = e.len - e.rows;
-    const bool plain = here == 3u && tok0 + kStepTokens <= first_tok + 1 && (p.window == 0 || tok0 > e.len - 1 - p.window);
+    const bool plain = here == (1u << SB) - 1u && tok0 + kStepTokens <= first_tok + 1 && (p.window == 0 || tok0 > e.len - 1 - p.window);
     ok = dsn_wait(bars + 8u * slot, parity, abort_flag, p.status, 71);
     if (!ok) break;
     const uint32_t st = ring + slot * step_bytes<D>();
 
-    float s[kStepBlocks][NT][4];
-    uint32_t vpair[kStepBlocks][GR][2];
+    float s[SB][NT][4];
+    uint32_t vpair[SB][GR][2];
+    uint32_t big = 0;   // largest of the scales' bits
 #pragma unroll
-    for (int b = 0; b < kStepBlocks; ++b) {
+    for (int b = 0; b < SB; ++b) {
       const uint32_t blk = st + b * kBlock;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[b][nt][x] = 0.f;
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
         const uint2 w0 = lds64(blk + gr * 512 + kap * 32 + t * 8), w1 = lds64(blk + gr * 512 + (kap + 8) * 32 + t * 8);
-        uint32_t k0 = lds32(blk + kPairs + gr * 64 + kap * 4), k1 = lds32(blk + kPairs + gr * 64 + (kap + 8) * 4);
+        const uint32_t k0 = lds32(blk + kPairs + gr * 64 + kap * 4), k1 = lds32(blk + kPairs + gr * 64 + (kap + 8) * 4);
         vpair[b][gr][0] = lds32(blk + kHalf + kPairs + gr * 64 + kap * 4);
         vpair[b][gr][1] = lds32(blk + kHalf + kPairs + gr * 64 + (kap + 8) * 4);
         float acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          acc[nt][0] = acc[nt][2] = -136.f * qsum[nt][gr][0];
-          acc[nt][1] = acc[nt][3] = -136.f * qsum[nt][gr][1];
+          acc[nt][0] = acc[nt][2] = qoff[nt][gr][0];
+          acc[nt][1] = acc[nt][3] = qoff[nt][gr][1];
         }
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-          const uint32_t x0 = ks < 2 ? w0.x : w0.y, x1 = ks < 2 ? w1.x : w1.y;
-          const int sh = 8 * (ks & 1);
-          const uint32_t a[4] = {nibbles(x0 >> sh), nibbles(x1 >> sh), nibbles(x0 >> (sh + 4)), nibbles(x1 >> (sh + 4))};
+          const uint32_t x0 = (ks < 2 ? w0.x : w0.y) >> (8 * (ks & 1)), x1 = (ks < 2 ? w1.x : w1.y) >> (8 * (ks & 1));
+          const uint32_t a[4] = {low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1)};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt], a, qf[nt][gr][ks][0], qf[nt][gr][ks][1]);
+          for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt], a, qf[nt][gr][ks][0], qf[nt][gr][ks][1]);
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          s[b][nt][0] = fmaf(lo_bf16(k0), acc[nt][0], fmaf(hi_bf16(k0), qsum[nt][gr][0], s[b][nt][0]));
-          s[b][nt][1] = fmaf(lo_bf16(k0), acc[nt][1], fmaf(hi_bf16(k0), qsum[nt][gr][1], s[b][nt][1]));
-          s[b][nt][2] = fmaf(lo_bf16(k1), acc[nt][2], fmaf(hi_bf16(k1), qsum[nt][gr][0], s[b][nt][2]));
-          s[b][nt][3] = fmaf(lo_bf16(k1), acc[nt][3], fmaf(hi_bf16(k1), qsum[nt][gr][1], s[b][nt][3]));
-        }
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float sc = lo_bf16(x < 2 ? k0 : k1), z = hi_bf16(x < 2 ? k0 : k1) * qsum[nt][gr][x & 1];
+            s[b][nt][x] = gr == 0 ? fmaf(sc, acc[nt][x], z) : s[b][nt][x] + fmaf(sc, acc[nt][x], z);
+          }
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) s[b][nt][x] *= p.scale_log2;
+        for (int x = 0; x < 4; ++x) s[b][nt][x] *= cs[nt][x & 1];
     }
     if (!plain) {
 #pragma unroll
-      for (int b = 0; b < kStepBlocks; ++b) {
+      for (int b = 0; b < SB; ++b) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           const int key = tok0 + b * DSN_CACHE_BLOCK + kap + 8 * hf;
@@ -279,27 +344,37 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         }
       }
     }
-    // a score far above its reference?
-    bool far = false;
 #pragma unroll
-    for (int b = 0; b < kStepBlocks; ++b)
+    for (int b = 0; b < SB; ++b)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int gr = 0; gr < GR; ++gr) big = max(big, max(vpair[b][gr][0] & 0x7fffu, vpair[b][gr][1] & 0x7fffu));
+    big = min(__reduce_max_sync(0xffffffffu, big), 0x7f7fu);
+    const float power = fmaxf((float)(int)(big >> 7) - 127.f, -20.f);   // of the largest scale; smaller ones need no more room
+    // a probability that would pass the top?
+    float most = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) far |= s[b][nt][x] > mref[nt][x & 1] + kSlack;
-    if (__any_sync(0xffffffffu, far)) {
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < SB; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
+        most = fmaxf(most, m - ref[nt][c]);
+      }
+    if (__any_sync(0xffffffffu, most + power > kTop)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float m = mref[nt][c];
+          float m = -INFINITY;
 #pragma unroll
-          for (int b = 0; b < kStepBlocks; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
+          for (int b = 0; b < SB; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-          const float f = ex2(mref[nt][c] - m);
-          mref[nt][c] = m;
+          m = fmaxf(ref[nt][c], m + power - kAim);
+          const float f = ex2(ref[nt][c] - m);
+          ref[nt][c] = m;
           l[nt][c] *= f;
 #pragma unroll
           for (int gr = 0; gr < GR; ++gr) {
@@ -313,16 +388,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         }
     }
 #pragma unroll
-    for (int b = 0; b < kStepBlocks; ++b)
+    for (int b = 0; b < SB; ++b)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          s[b][nt][x] = ex2(s[b][nt][x] - mref[nt][x & 1]);
+          s[b][nt][x] = ex2(s[b][nt][x] - ref[nt][x & 1]);
           l[nt][x & 1] += s[b][nt][x];
         }
 #pragma unroll
-    for (int b = 0; b < kStepBlocks; ++b) {
+    for (int b = 0; b < SB; ++b) {
       const uint32_t blk = st + b * kBlock + kHalf;
       const int ka = 2 * t + (t >> 1), kb = 2 * t + 1 - (t >> 1);   // tokens of columns 2 t and 2 t + 1
 #pragma unroll
@@ -336,26 +411,31 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
             const float p0 = s[b][nt][2 * hf], p1 = s[b][nt][2 * hf + 1];
             oz[nt][gr][0] = fmaf(p0, z, oz[nt][gr][0]);
             oz[nt][gr][1] = fmaf(p1, z, oz[nt][gr][1]);
-            pb[nt][hf] = transpose8x8(pack_bf16(p0 * sc, p1 * sc));
+            const __half2 ps = __floats2half2_rn(p0 * sc, p1 * sc);
+            pb[nt][hf] = transpose8x8(*reinterpret_cast<const uint32_t*>(&ps));
           }
         const uint32_t va = lds32(blk + gr * 512 + ka * 32 + g * 4), vb = lds32(blk + gr * 512 + kb * 32 + g * 4);
         const uint32_t vc = lds32(blk + gr * 512 + (ka + 8) * 32 + g * 4), vd = lds32(blk + gr * 512 + (kb + 8) * 32 + g * 4);
-        const uint32_t l0 = __byte_perm(va, vb, 0x5410), h0 = __byte_perm(va, vb, 0x7632);
-        const uint32_t l1 = __byte_perm(vc, vd, 0x5410), h1 = __byte_perm(vc, vd, 0x7632);
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
-          const uint32_t a[4] = {minus136(nibbles(l0 >> (4 * mt))), minus136(nibbles(h0 >> (4 * mt))), minus136(nibbles(l1 >> (4 * mt))),
-                                 minus136(nibbles(h1 >> (4 * mt)))};
+        for (int by = 0; by < 2; ++by) {
+          // byte `by` and byte `by` + 2 of the words of two tokens side by side: elements 2 by, 2 by + 1 and 2 by + 4, 2 by + 5
+          const uint32_t x0 = __byte_perm(va, vb, by ? 0x5511 : 0x4400), x1 = __byte_perm(va, vb, by ? 0x7733 : 0x6622);
+          const uint32_t y0 = __byte_perm(vc, vd, by ? 0x5511 : 0x4400), y1 = __byte_perm(vc, vd, by ? 0x7733 : 0x6622);
+          const uint32_t lo4[4] = {code_of_low(low_codes(x0)), code_of_low(low_codes(x1)), code_of_low(low_codes(y0)), code_of_low(low_codes(y1))};
+          const uint32_t hi4[4] = {code_of_high(high_codes(x0)), code_of_high(high_codes(x1)), code_of_high(high_codes(y0)), code_of_high(high_codes(y1))};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][gr][mt], a, pb[nt][0], pb[nt][1]);
+          for (int nt = 0; nt < NT; ++nt) {
+            mma_f16(o[nt][gr][2 * by], lo4, pb[nt][0], pb[nt][1]);
+            mma_f16(o[nt][gr][2 * by + 1], hi4, pb[nt][0], pb[nt][1]);
+          }
         }
       }
     }
     __syncwarp();   // every lane has read the slot
     if (asked < n_steps) {
-      there = (there & ~(3u << (2 * slot))) | (issue(slot) << (2 * slot));
+      there = (there & ~(((1u << SB) - 1u) << (SB * slot))) | (issue(slot) << (SB * slot));
       ++asked;
-      if (asked < n_steps) fetch.advance();
+      if (asked < n_steps) step_on();
     }
     if (++slot == DEPTH) slot = 0, parity ^= 1u;
 
@@ -409,7 +489,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
             }
           }
           if (!whole && v < cols && g == 0) {
-            dst[v] = mref[nt][c];
+            dst[v] = ref[nt][c];
             dst[NC + v] = sum;
           }
         }
@@ -580,6 +660,6 @@ cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, v
   p.list = reinterpret_cast<CacheEntry*>(ws + w.list);
   p.warp_data = reinterpret_cast<float*>(ws + w.warp_data);
   p.cta_data = reinterpret_cast<float*>(ws + w.cta_data);
-  if (D == 64) return cols <= 8 ? launch<64, 1, kWarps1, 5>(p, ctas, s) : launch<64, 2, kWarps2, 8>(p, ctas, s);
+  if (D == 64) return cols <= 8 ? launch<64, 1, kWarps1, 3>(p, ctas, s) : launch<64, 2, kWarps2, 6>(p, ctas, s);
   return cols <= 8 ? launch<128, 1, kWarps1, 3>(p, ctas, s) : launch<128, 2, kWarps2, 6>(p, ctas, s);
 }

@@ -8,7 +8,6 @@ namespace dsn_q4 {
 
 constexpr int kListSmem = 64;      // requests that a CTA keeps in shared memory; further ones are read from the workspace
 constexpr float kLowest = -1e38f;  // reference before any score: finite, so that differences are
-constexpr float kSlack = 8.f;      // a reference moves when a score stands further above it
 
 __device__ __forceinline__ float ex2(float x) {
   float r;
@@ -18,12 +17,6 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t nibbles(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }   // bf16 128 + code, of the elements 0 and 4
-__device__ __forceinline__ uint32_t minus136(uint32_t w) {
-  uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x43084308u));
   return r;
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
