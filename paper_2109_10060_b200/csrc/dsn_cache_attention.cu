@@ -18,8 +18,6 @@
 // Queries are brought to 1 .. 2 by a power of two, which goes into the scale.  Everything of a query is in units of 2^ref, a reference that moves only when a
 // probability times the largest power of two in the step's scales would pass 2^15 (one vote a step instead of a reduction): fp16 then holds every product of
 // a probability and a scale, whatever their range.
-#include <cuda_fp16.h>
-
 #include "dsn_cache_line.cuh"
 
 namespace {
@@ -75,18 +73,6 @@ template <int D>
 __host__ __device__ constexpr uint32_t step_bytes() { return step_blocks<D>() * dsn_cache_block_bytes(D); }
 template <int D, int WARPS, int DEPTH>
 constexpr size_t attention_smem() { return kCtrl + kListSmem * sizeof(CacheEntry) + WARPS * DEPTH * 8 + (size_t)WARPS * DEPTH * step_bytes<D>(); }
-
-// 1024 + code of elements 0 and 4 (1 and 5 of the word shifted by 8: 2 and 6), 1024 + 16 code of elements 1 and 5 (3 and 7)
-__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return (w & 0x000f000fu) | 0x64006400u; }
-__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return (w & 0x00f000f0u) | 0x64006400u; }
-__device__ __forceinline__ uint32_t code_of_low(uint32_t h) {   // code - 8
-  const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(-1032.f));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ __forceinline__ uint32_t code_of_high(uint32_t h) {
-  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(0.0625f), __float2half2_rn(-72.f));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
 
 template <int D, int NT, int WARPS, int DEPTH>
 __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __grid_constant__ CacheAttParams p) {
@@ -199,6 +185,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   bool fresh = true, ok = true;
   bool head_open = work.step != 0;   // the first item began in an earlier warp's stretch
   head_state = 0;
+  const uint32_t k1024 = opaque_1024();
   const int kap = g ^ (g >> 2);      // token of K's row g in a block
   uint32_t slot = 0, parity = 0;
 
@@ -303,7 +290,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           const uint32_t x0 = (ks < 2 ? w0.x : w0.y) >> (8 * (ks & 1)), x1 = (ks < 2 ? w1.x : w1.y) >> (8 * (ks & 1));
-          const uint32_t a[4] = {low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1)};
+          const uint32_t a[4] = {low_codes(x0, k1024), low_codes(x1, k1024), high_codes(x0, k1024), high_codes(x1, k1024)};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt], a, qf[nt][gr][ks][0], qf[nt][gr][ks][1]);
         }
@@ -421,8 +408,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
           // byte `by` and byte `by` + 2 of the words of two tokens side by side: elements 2 by, 2 by + 1 and 2 by + 4, 2 by + 5
           const uint32_t x0 = __byte_perm(va, vb, by ? 0x5511 : 0x4400), x1 = __byte_perm(va, vb, by ? 0x7733 : 0x6622);
           const uint32_t y0 = __byte_perm(vc, vd, by ? 0x5511 : 0x4400), y1 = __byte_perm(vc, vd, by ? 0x7733 : 0x6622);
-          const uint32_t lo4[4] = {code_of_low(low_codes(x0)), code_of_low(low_codes(x1)), code_of_low(low_codes(y0)), code_of_low(low_codes(y1))};
-          const uint32_t hi4[4] = {code_of_high(high_codes(x0)), code_of_high(high_codes(x1)), code_of_high(high_codes(y0)), code_of_high(high_codes(y1))};
+          const uint32_t lo4[4] = {code_of_low(low_codes(x0, k1024)), code_of_low(low_codes(x1, k1024)), code_of_low(low_codes(y0, k1024)), code_of_low(low_codes(y1, k1024))};
+          const uint32_t hi4[4] = {code_of_high(high_codes(x0, k1024)), code_of_high(high_codes(x1, k1024)), code_of_high(high_codes(y0, k1024)), code_of_high(high_codes(y1, k1024))};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             mma_f16(o[nt][gr][2 * by], lo4, pb[nt][0], pb[nt][1]);

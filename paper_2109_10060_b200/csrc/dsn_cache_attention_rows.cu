@@ -17,8 +17,6 @@
 // pass 2^15: then O is read, scaled and written back.
 // The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (a mask each pair), so Q's and O's columns are in that order, too.
 // TMEM: 512 columns = two regions of 256: two buffers of S_h at 0 and 64, P_h over the first half of each, O_h from 128.  Every wait is bounded.
-#include <cuda_fp16.h>
-
 #include "dsn_cache_line.cuh"
 
 namespace {
@@ -45,16 +43,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
-}
-// fp16 code - 8 of the elements (0, 4), (1, 5), (2, 6), (3, 7) of a word: the code in the low bits of 1024, or of 1024 + 16 code
-__device__ __forceinline__ void code_pairs(uint32_t w, __half2 (&c)[4]) {
-  const uint32_t x = w >> 8;
-  const uint32_t n[4] = {(w & 0x000f000fu) | 0x64006400u, (w & 0x00f000f0u) | 0x64006400u, (x & 0x000f000fu) | 0x64006400u, (x & 0x00f000f0u) | 0x64006400u};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2 h = *reinterpret_cast<const __half2*>(&n[i]);
-    c[i] = i & 1 ? __hfma2(h, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hadd2(h, __float2half2_rn(-1032.f));
-  }
 }
 __device__ __forceinline__ void tmem_st_8(uint32_t taddr, const uint32_t (&v)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -243,6 +231,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     // ------------------------------------------------------------------------------ codes to values
     // Unit u of tile number i: K (0-3) or V (4-7) of block u & 3; warp w takes units w, w + 5, ... of all.
     const uint32_t units = 8u * (uint32_t)(stretch.Z - stretch.A);
+    const uint32_t k1024 = opaque_1024();
     const int tok = lane & 15, part = lane >> 4;      // D = 128: a lane takes a group; D = 64: half of it
     // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers; every unit finds it anew from the tile's pairs
     auto exponent = [&](uint32_t slot, uint32_t info, bool of_v) -> uint32_t {
@@ -290,13 +279,13 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       for (int x = 0; x < GR; ++x)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          __half2 c[4];
-          code_pairs(q[x][w], c);
-          uint32_t o[4];
+          const uint32_t lo = q[x][w], hi = lo >> 8;   // elements (0, 4), (1, 5), (2, 6), (3, 7)
+          uint32_t o[4] = {code_of_low(low_codes(lo, k1024)), code_of_high(high_codes(lo, k1024)), code_of_low(low_codes(hi, k1024)),
+                           code_of_high(high_codes(hi, k1024))};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            c[j] = __hfma2(c[j], s2, z2);
-            o[j] = *reinterpret_cast<const uint32_t*>(&c[j]);
+            const __half2 y = __hfma2(*reinterpret_cast<const __half2*>(&o[j]), s2, z2);
+            o[j] = *reinterpret_cast<const uint32_t*>(&y);
           }
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((((GR == 2 ? 4 * x : 4 * part) + w) ^ (tok & 7)) << 4)), "r"(o[0]), "r"(o[1]),
                        "r"(o[2]), "r"(o[3])

@@ -2,6 +2,8 @@
 // cut into equal stretches, one a CTA.  Every CTA scans the requests' lengths on its own and keeps the requests of its stretch.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "dsn_cache.cuh"
 
 namespace dsn_q4 {
@@ -18,6 +20,28 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+// Codes as fp16 numbers, two at a time: 1024 + code from the low half of a byte in each 16 bits, 1024 + 16 code from its high half.  One instruction each as
+// long as the 1024 is in a register: the compiler, which knows the constant, would rather spend a second instruction (304 -> 180 logic instructions for
+// 32 tokens of 128 elements); hence a value that it cannot know.
+__device__ __forceinline__ uint32_t opaque_1024() { return 0x64006400u | (threadIdx.x >> 16); }
+__device__ __forceinline__ uint32_t low_codes(uint32_t w, uint32_t k1024) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xEA;" : "=r"(r) : "r"(w), "r"(k1024));
+  return r;
+}
+__device__ __forceinline__ uint32_t high_codes(uint32_t w, uint32_t k1024) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xEA;" : "=r"(r) : "r"(w), "r"(k1024));
+  return r;
+}
+__device__ __forceinline__ uint32_t code_of_low(uint32_t h) {   // code - 8
+  const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(-1032.f));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t code_of_high(uint32_t h) {
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(0.0625f), __float2half2_rn(-72.f));
+  return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
