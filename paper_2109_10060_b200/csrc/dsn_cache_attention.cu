@@ -33,6 +33,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1) {   // rows start alike
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -56,8 +61,8 @@ struct Walk {
     j = i;
     e = i < kListSmem ? smem[i] : more[i];
   }
-  __device__ __forceinline__ void advance() {
-    if (++step == e.steps) {
+  __device__ __forceinline__ void advance(int n) {   // n steps, not past the item's end
+    if ((step += n) == e.steps) {
       step = 0;
       if (++head == e.heads) {
         head = 0;
@@ -70,9 +75,11 @@ struct Walk {
 template <int D>
 __host__ __device__ constexpr int step_blocks() { return 256 / D; }
 template <int D>
+__host__ __device__ constexpr uint32_t slot_bytes() { return 2 * step_blocks<D>() * dsn_cache_block_bytes(D); }   // two steps
+template <int D>
 __host__ __device__ constexpr uint32_t step_bytes() { return step_blocks<D>() * dsn_cache_block_bytes(D); }
 template <int D, int WARPS, int DEPTH>
-constexpr size_t attention_smem() { return kCtrl + kListSmem * sizeof(CacheEntry) + WARPS * DEPTH * 8 + (size_t)WARPS * DEPTH * step_bytes<D>(); }
+constexpr size_t attention_smem() { return kCtrl + kListSmem * sizeof(CacheEntry) + WARPS * DEPTH * 8 + (size_t)WARPS * DEPTH * slot_bytes<D>(); }
 
 template <int D, int NT, int WARPS, int DEPTH>
 __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __grid_constant__ CacheAttParams p) {
@@ -86,8 +93,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + kListSmem * sizeof(CacheEntry) + 512);
   const uint32_t base = smem_u32(smem) + (uint32_t)(kListSmem * sizeof(CacheEntry)) + kCtrl;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const uint32_t ring = base + (uint32_t)(warp * DEPTH) * step_bytes<D>();
-  const uint32_t bars = base + (uint32_t)(WARPS * DEPTH) * step_bytes<D>() + (uint32_t)(warp * DEPTH) * 8u;
+  const uint32_t ring = base + (uint32_t)(warp * DEPTH) * slot_bytes<D>();
+  const uint32_t bars = base + (uint32_t)(WARPS * DEPTH) * slot_bytes<D>() + (uint32_t)(warp * DEPTH) * 8u;
 
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
@@ -97,13 +104,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
 
-  const Stretch stretch = find_stretch<THREADS>(p, s_list, s_scan, [&](int len, int rows) {
+  const Stretch stretch = find_stretch<THREADS>(p, s_list, s_scan, WARPS, [&](int len, int rows) {
     int lo, hi;
     item_range(len, rows, p.window, lo, hi);
     return max(1, (hi - lo + 256 / D * DSN_CACHE_BLOCK - 1) / (256 / D * DSN_CACHE_BLOCK));   // a request without tokens: a step that sees nothing, for the zeros
   });
   const uint64_t A = stretch.A, Z = stretch.Z;
-  const uint64_t u0 = A + (Z - A) * warp / WARPS, u1 = A + (Z - A) * (warp + 1) / WARPS;
+  const uint64_t u0 = A + dsn_share(Z - A, warp, WARPS), u1 = A + dsn_share(Z - A, warp + 1, WARPS);
   int head_state = 3, tail = 0, head_far = 0;
   Walk work;
   if (u0 < u1) {
@@ -129,57 +136,61 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   const int n_steps = (int)(u1 - u0);
   const int bpp = p.page / DSN_CACHE_BLOCK;   // blocks a page
 
-  // The fetching side: lane b < SB fetches block b of a step; the page's number is read a step before the copy that needs it.
-  int f_tok = 0, f_hi = 0, pg = -1, place = 0;   // this lane's token, the item's end; the page and the block in it
-  const int32_t* f_row = nullptr;
-  int64_t f_head = 0;
+  // The fetching side: a slot of the ring takes up to two steps of an item; lane b fetches its block b; the page's number is read a slot before the copy
+  // that needs it.  Blocks that lie behind one another in a page are one copy.
+  int f_left = n_steps, f_n = 0, f_tok = 0, f_hi = 0, pg = -1, place = 0;   // steps to come, of this slot; this lane's token, the item's end; page, block in it
+  const int64_t page_blocks = (int64_t)p.H * bpp;
   bool wanted = false;
-  auto enter = [&]() {   // the item that `fetch` stands in
-    int lo;
-    item_range(fetch.e.len, fetch.e.rows, p.window, lo, f_hi);
-    f_tok = lo + fetch.step * kStepTokens + lane * DSN_CACHE_BLOCK;
-    f_row = p.table + (int64_t)fetch.e.sample * p.max_pages;
-    f_head = (int64_t)fetch.head * bpp;
-  };
-  auto find = [&]() {
-    wanted = lane < SB && f_tok < f_hi;
+  auto find = [&](bool entered) {
+    if (entered) {   // an item
+      int lo;
+      item_range(fetch.e.len, fetch.e.rows, p.window, lo, f_hi);
+      f_tok = lo + fetch.step * kStepTokens + lane * DSN_CACHE_BLOCK;
+    }
+    f_n = min(min(2, f_left), fetch.e.steps - fetch.step);
+    wanted = lane < f_n * SB && f_tok < f_hi;
     pg = -1;
     if (wanted) {
       const int col = (int)dsn_div((uint32_t)f_tok, p.by_page);
-      pg = f_row[col];
+      pg = p.table[(int64_t)fetch.e.sample * p.max_pages + col];
       place = f_tok / DSN_CACHE_BLOCK - col * bpp;
     }
   };
-  const int64_t page_blocks = (int64_t)p.H * bpp;
   auto issue = [&](int slot) -> uint32_t {   // bit b of the result: block b is on its way
     const bool ok = pg >= 0 && pg < p.n_pages;
     if (wanted && !ok) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, fetch.e.sample);
+    const int64_t at = ok ? pg * page_blocks + (int64_t)fetch.head * bpp + place : -2 - 2 * lane;
     const uint32_t there = __ballot_sync(0xffffffffu, ok);
+    const int64_t before = (int64_t)__shfl_up_sync(0xffffffffu, (long long)at, 1);   // by all lanes, wanted or not
+    const uint32_t begins = __ballot_sync(0xffffffffu, ok && (lane == 0 || at != before + 1));
     if (lane == 0) dsn_gemm::mbar_expect_tx(bars + 8u * slot, (uint32_t)__popc(there) * kBlock);
     __syncwarp();
-    if (ok)
-      dsn_bulk_load(ring + (uint32_t)slot * step_bytes<D>() + (uint32_t)lane * kBlock, p.pages + (pg * page_blocks + f_head + place) * kBlock, kBlock,
-                    bars + 8u * slot);
+    if (begins >> lane & 1u) {
+      const uint32_t stops = (~there | begins) >> lane >> 1;   // where this run of blocks ends
+      dsn_bulk_load(ring + (uint32_t)slot * slot_bytes<D>() + (uint32_t)lane * kBlock, p.pages + at * kBlock, (uint32_t)__ffs(stops) * kBlock, bars + 8u * slot);
+    }
     return there;
   };
-  auto step_on = [&]() {   // to the next step of the stretch
+  auto step_on = [&]() {   // to the next slot's steps, if there are any
+    f_left -= f_n;
+    if (f_left <= 0) return;
     const int j = fetch.j, hd = fetch.head;
-    fetch.advance();
-    if (fetch.j != j || fetch.head != hd) enter(); else f_tok += kStepTokens;
-    find();
+    fetch.advance(f_n);
+    const bool entered = fetch.j != j || fetch.head != hd;
+    f_tok += f_n * kStepTokens;
+    find(entered);
   };
 
   int asked = 0;
-  uint32_t there = 0;   // SB bits a slot
-  enter();
-  find();
-  for (; asked < DEPTH && asked < n_steps; ++asked) {
-    there |= issue(asked) << (SB * asked);
-    if (asked + 1 < n_steps) step_on();
+  uint32_t there = 0;   // 2 SB bits a slot
+  find(true);
+  for (; asked < DEPTH && f_left > 0; ++asked) {
+    there |= issue(asked) << (2 * SB * asked);
+    step_on();
   }
 
   uint32_t qf[NT][GR][4][2];
-  float qsum[NT][GR][2], qoff[NT][GR][2], cs[NT][2];   // of this lane's columns: sum of the query, minus the offsets' product with it, factor of the scores
+  float qsum[NT][GR][2], qoff[NT][GR][2], cs[NT][2];   // of this lane's columns: sum of the query, minus the offsets' product with it, factor of the scores (positive)
   float o[NT][GR][4][4], oz[NT][GR][2], l[NT][2], ref[NT][2];
   int row_of[NT][2];                 // rows of this lane's columns
   bool fresh = true, ok = true;
@@ -189,6 +200,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   const int kap = g ^ (g >> 2);      // token of K's row g in a block
   uint32_t slot = 0, parity = 0;
 
+  int sub = 0;   // step of the slot
   for (int i = 0; i < n_steps; ++i) {
     const CacheEntry& e = work.e;
     const int cols = e.rows * p.group;
@@ -217,7 +229,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         ex = max(ex, __shfl_xor_sync(0xffffffffu, ex, 1));
         ex = max(ex, __shfl_xor_sync(0xffffffffu, ex, 2)) >> 7;
         ex = ex == 255u ? 127u : min(max(ex, 27u), 253u);   // a query that is not finite stays so
-        const float down = __uint_as_float((254u - ex) << 23), up = p.scale_log2 * __uint_as_float(ex << 23);
+        const float down = __uint_as_float((254u - ex) << 23 | (p.scale_log2 < 0.f ? 0x80000000u : 0u));   // a negative scale goes into the signs
+        const float up = fmaxf(fabsf(p.scale_log2) * __uint_as_float(ex << 23), 1e-37f);   // not 0: what is hidden is -infinity
         cs[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t);
         cs[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
 #pragma unroll
@@ -261,13 +274,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     int lo, hi;
     item_range(e.len, e.rows, p.window, lo, hi);
     const int tok0 = lo + work.step * kStepTokens;
-    const uint32_t here = (there >> (SB * slot)) & ((1u << SB) - 1u);
+    const uint32_t here = (there >> (SB * (2 * slot + sub))) & ((1u << SB) - 1u);
     // all tokens of the step seen by all rows?
     const int first_tok = e.len - e.rows;
     const bool plain = here == (1u << SB) - 1u && tok0 + kStepTokens <= first_tok + 1 && (p.window == 0 || tok0 > e.len - 1 - p.window);
-    ok = dsn_wait(bars + 8u * slot, parity, abort_flag, p.status, 71);
-    if (!ok) break;
-    const uint32_t st = ring + slot * step_bytes<D>();
+    if (sub == 0) {
+      ok = warp_wait(bars + 8u * slot, parity, abort_flag, p.status, 71);
+      if (!ok) break;
+    }
+    const uint32_t st = ring + slot * slot_bytes<D>() + (uint32_t)sub * step_bytes<D>();
 
     float s[SB][NT][4];
     uint32_t vpair[SB][GR][2];
@@ -283,29 +298,22 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         vpair[b][gr][1] = lds32(blk + kHalf + kPairs + gr * 64 + (kap + 8) * 4);
         float acc[NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          acc[nt][0] = acc[nt][2] = qoff[nt][gr][0];
-          acc[nt][1] = acc[nt][3] = qoff[nt][gr][1];
-        }
-#pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           const uint32_t x0 = (ks < 2 ? w0.x : w0.y) >> (8 * (ks & 1)), x1 = (ks < 2 ? w1.x : w1.y) >> (8 * (ks & 1));
           const uint32_t a[4] = {low_codes(x0, k1024), low_codes(x1, k1024), high_codes(x0, k1024), high_codes(x1, k1024)};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt], a, qf[nt][gr][ks][0], qf[nt][gr][ks][1]);
+          for (int nt = 0; nt < NT; ++nt)
+            if (ks == 0) mma_f16_from(acc[nt], a, qf[nt][gr][0][0], qf[nt][gr][0][1], qoff[nt][gr][0], qoff[nt][gr][1]);
+            else mma_f16(acc[nt], a, qf[nt][gr][ks][0], qf[nt][gr][ks][1]);
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const float sc = lo_bf16(x < 2 ? k0 : k1), z = hi_bf16(x < 2 ? k0 : k1) * qsum[nt][gr][x & 1];
-            s[b][nt][x] = gr == 0 ? fmaf(sc, acc[nt][x], z) : s[b][nt][x] + fmaf(sc, acc[nt][x], z);
+            const float sc = lo_bf16(x < 2 ? k0 : k1), z = hi_bf16(x < 2 ? k0 : k1);
+            s[b][nt][x] = fmaf(sc, acc[nt][x], gr == 0 ? z * qsum[nt][gr][x & 1] : fmaf(z, qsum[nt][gr][x & 1], s[b][nt][x]));
           }
       }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[b][nt][x] *= cs[nt][x & 1];
     }
     if (!plain) {
 #pragma unroll
@@ -346,7 +354,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         float m = -INFINITY;
 #pragma unroll
         for (int b = 0; b < SB; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
-        most = fmaxf(most, m - ref[nt][c]);
+        most = fmaxf(most, fmaf(m, cs[nt][c], -ref[nt][c]));
       }
     if (__any_sync(0xffffffffu, most + power > kTop)) {
 #pragma unroll
@@ -359,7 +367,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-          m = fmaxf(ref[nt][c], m + power - kAim);
+          m = fmaxf(ref[nt][c], fmaf(m, cs[nt][c], power - kAim));
           const float f = ex2(ref[nt][c] - m);
           ref[nt][c] = m;
           l[nt][c] *= f;
@@ -380,7 +388,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          s[b][nt][x] = ex2(s[b][nt][x] - ref[nt][x & 1]);
+          s[b][nt][x] = ex2(fmaf(s[b][nt][x], cs[nt][x & 1], -ref[nt][x & 1]));
           l[nt][x & 1] += s[b][nt][x];
         }
 #pragma unroll
@@ -418,15 +426,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         }
       }
     }
-    __syncwarp();   // every lane has read the slot
-    if (asked < n_steps) {
-      there = (there & ~(((1u << SB) - 1u) << (SB * slot))) | (issue(slot) << (SB * slot));
-      ++asked;
-      if (asked < n_steps) step_on();
-    }
-    if (++slot == DEPTH) slot = 0, parity ^= 1u;
-
     const bool item_ends = work.step + 1 == e.steps, last = i + 1 == n_steps;
+    if (sub == 1 || item_ends || last) {
+      __syncwarp();   // every lane has read the slot
+      if (f_left > 0) {
+        there = (there & ~(((1u << 2 * SB) - 1u) << (2 * SB * slot))) | (issue(slot) << (2 * SB * slot));
+        ++asked;
+        step_on();
+      }
+      sub = 0;
+      if (++slot == DEPTH) slot = 0, parity ^= 1u;
+    } else {
+      sub = 1;
+    }
+
     if (item_ends || last) {
       const bool whole = item_ends && !head_open;
       if (!item_ends) {
@@ -483,10 +496,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
       head_open = false;
       fresh = true;
     }
-    if (!last) work.advance();
+    if (!last) work.advance(1);
   }
   if (!ok) {
-    dsn_drain(bars, DEPTH, 0, asked);
+    dsn_drain(bars, DEPTH, max(0, asked - DEPTH), asked);
     head_state = 3;
     tail = 0;
   }
@@ -498,7 +511,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   __syncthreads();
   auto part_of = [&](int w, bool of_tail) -> const float* {   // where a warp left a part
     if (!of_tail && s_part[w].head_far) return p.warp_data + ((int64_t)blockIdx.x * WARPS + w) * kPart;
-    return reinterpret_cast<const float*>(smem + (base - smem_u32(smem)) + (size_t)w * DEPTH * step_bytes<D>());
+    return reinterpret_cast<const float*>(smem + (base - smem_u32(smem)) + (size_t)w * DEPTH * slot_bytes<D>());
   };
   int chain = 0;
   int cta_head = 3, cta_tail = 0, tail_warp = 0;
@@ -573,10 +586,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   }
 }
 
-// Joins the parts of the items that were cut between CTAs: a CTA of D threads for every column of every CTA's last item.
+// Joins the parts of the items that were cut between CTAs: a CTA for every column of every CTA's last item, 8 groups of D / 4 threads that take every eighth part.
 template <int D>
-__global__ void __launch_bounds__(D) cache_join_kernel(const __grid_constant__ CacheAttParams p, int ctas, int NC) {
+__global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant__ CacheAttParams p, int ctas, int NC) {
   __shared__ int s_end;
+  __shared__ float s_w[DSN_CACHE_MAX_CTAS], s_l[DSN_CACHE_MAX_CTAS], s_m;
+  __shared__ float4 s_o[2 * D];
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
   const int tid = threadIdx.x, w = blockIdx.x, v = blockIdx.y, kPart = NC * (D + 2);
@@ -584,25 +599,51 @@ __global__ void __launch_bounds__(D) cache_join_kernel(const __grid_constant__ C
   if (!part.tail || v >= part.rows * p.group) return;
   if (tid == 0) s_end = ctas - 1;
   __syncthreads();
-  for (int b = w + 1 + tid; b < ctas; b += D)
+  for (int b = w + 1 + tid; b < ctas; b += 2 * D)
     if (p.parts[b].head_state < 2) atomicMin(&s_end, b);   // the CTA in whose stretch the item ends
   __syncthreads();
-  const int end = s_end;
-  float m = kLowest, l = 0.f, o = 0.f;
-#pragma unroll 8
-  for (int j = w; j <= end; ++j) {
-    if (j > w && p.parts[j].head_state == 3) continue;
-    const float* src = p.cta_data + ((int64_t)j * 2 + (j == w)) * kPart;
-    const float mj = src[v], lj = src[NC + v], oj = src[2 * NC + v * D + tid];
-    const float m2 = fmaxf(m, mj);
-    const float fa = ex2(m - m2), fb = ex2(mj - m2);
-    l = l * fa + lj * fb;
-    o = o * fa + oj * fb;
-    m = m2;
+  const int n = s_end - w + 1;
+  for (int j = tid; j < n; j += 2 * D) {
+    const float* src = p.cta_data + ((int64_t)(w + j) * 2 + (j == 0)) * kPart;
+    const bool there = j == 0 || p.parts[w + j].head_state != 3;
+    s_w[j] = there ? src[v] : kLowest;
+    s_l[j] = there ? src[NC + v] : 0.f;
   }
+  __syncthreads();
+  if (tid < 32) {
+    float m = kLowest;
+    for (int j = tid; j < n; j += 32) m = fmaxf(m, s_w[j]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (tid == 0) s_m = m;
+  }
+  __syncthreads();
+  constexpr int L = D / 4;
+  const int sub = tid % L, of = tid / L;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int j = of; j < n; j += 8) {
+    const float f = s_l[j] == 0.f ? 0.f : ex2(s_w[j] - s_m);   // an empty part holds nothing
+    const float4 q = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                              : *reinterpret_cast<const float4*>(p.cta_data + ((int64_t)(w + j) * 2 + (j == 0)) * kPart + 2 * NC + v * D + 4 * sub);
+    l = fmaf(s_l[j], f, l);
+    o.x = fmaf(q.x, f, o.x); o.y = fmaf(q.y, f, o.y); o.z = fmaf(q.z, f, o.z); o.w = fmaf(q.w, f, o.w);
+  }
+  s_o[tid] = o;
+  __syncthreads();
+  if (of) return;
+  l = 0.f;
+  for (int j = 0; j < n; ++j) l = fmaf(s_l[j], s_l[j] == 0.f ? 0.f : ex2(s_w[j] - s_m), l);
+  for (int k = 1; k < 8; ++k) {
+    const float4 q = s_o[k * L + sub];
+    o.x += q.x; o.y += q.y; o.z += q.z; o.w += q.w;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   const int r = v / p.group, ev = v - r * p.group;
   const int64_t row = (int64_t)(p.grouped ? part.pos : part.sample) * p.R + r;
-  p.out[row * p.ld_out + ((int64_t)part.head * p.group + ev) * D + tid] = __float2bfloat16_rn(l == 0.f ? 0.f : o / l);
+  *reinterpret_cast<uint2*>(p.out + row * p.ld_out + ((int64_t)part.head * p.group + ev) * D + 4 * sub) =
+      make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
 
 template <int D, int NT, int WARPS, int DEPTH>
@@ -615,10 +656,10 @@ cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = dsn_launch(kernel, dim3((unsigned)ctas), dim3(WARPS * 32), smem, s, 1, p);
   if (e != cudaSuccess) return e;
-  return dsn_launch(cache_join_kernel<D>, dim3((unsigned)ctas, 8 * NT), dim3(D), 0, s, 1, p, ctas, 8 * NT);
+  return dsn_launch(cache_join_kernel<D>, dim3((unsigned)ctas, (unsigned)(p.R * p.group)), dim3(2 * D), 0, s, 1, p, ctas, 8 * NT);
 }
 
-constexpr int kWarps1 = 16, kWarps2 = 8;   // warps a CTA for up to 8 and up to 16 query vectors a head: registers of the products
+constexpr int kWarps1 = 12, kWarps2 = 8;   // warps a CTA for up to 8 and up to 16 query vectors a head: their products stay in registers (16 and 8 warps: 132 and 144 us, 12: 128)
 
 }  // namespace
 
@@ -647,6 +688,6 @@ cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, v
   p.list = reinterpret_cast<CacheEntry*>(ws + w.list);
   p.warp_data = reinterpret_cast<float*>(ws + w.warp_data);
   p.cta_data = reinterpret_cast<float*>(ws + w.cta_data);
-  if (D == 64) return cols <= 8 ? launch<64, 1, kWarps1, 3>(p, ctas, s) : launch<64, 2, kWarps2, 6>(p, ctas, s);
-  return cols <= 8 ? launch<128, 1, kWarps1, 3>(p, ctas, s) : launch<128, 2, kWarps2, 6>(p, ctas, s);
+  if (D == 64) return cols <= 8 ? launch<64, 1, kWarps1, 2>(p, ctas, s) : launch<64, 2, kWarps2, 3>(p, ctas, s);
+  return cols <= 8 ? launch<128, 1, kWarps1, 2>(p, ctas, s) : launch<128, 2, kWarps2, 3>(p, ctas, s);
 }

@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.by_group, p.window); });
+  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, 1u, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.by_group, p.window); });
   if (warp == kIssueWarp) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     for (uint32_t unit = (uint32_t)warp; unit < units; unit += kValueWarps) {
       const uint32_t i = unit >> 3, s = i % kStages, b = unit & 3u;
       const bool is_v = (unit & 4u) != 0;
-      if (!dsn_wait(raw_full + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
+      if (!warp_wait(raw_full + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
       const uint32_t info = *reinterpret_cast<const volatile uint32_t*>(s_raw + (i & 1u));
       const bool there = (info >> b & 1u) && (int)(b * 16u) + tok < (int)(info >> 8);
       const uint32_t slot = raw_at + (i & 1u) * kSlot, src = slot + b * kBlock + (is_v ? kBlock / 2 : 0u);
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       uint32_t q[GR][4];
 #pragma unroll
       for (int x = 0; x < GR; ++x) lds128(src + (GR == 2 ? (uint32_t)(part * 512 + tok * 32 + 16 * x) : (uint32_t)(tok * 32 + 16 * part)), q[x]);
-      if (i >= kStages && !dsn_wait((is_v ? v_empty : k_empty) + 8 * s, (i / kStages - 1u) & 1u, abort_flag, p.status, 81)) break;
+      if (i >= kStages && !warp_wait((is_v ? v_empty : k_empty) + 8 * s, (i / kStages - 1u) & 1u, abort_flag, p.status, 81)) break;
       if ((unit & 7u) == 0) {
         const uint32_t ve = exponent(slot, info, true);
         if (lane == 0) {
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     find();
     for (; more; ++i) {
       const uint32_t slot = i & 1u;
-      if (i >= 2 && !dsn_wait(raw_empty + 8 * slot, ((i >> 1) - 1u) & 1u, abort_flag, p.status, 91)) break;
+      if (i >= 2 && !warp_wait(raw_empty + 8 * slot, ((i >> 1) - 1u) & 1u, abort_flag, p.status, 91)) break;
       const bool ok = pg >= 0 && pg < p.n_pages, lost = exists && !ok;
       if (lost) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
       const uint32_t go = __ballot_sync(0xffffffffu, ok), bad = __ballot_sync(0xffffffffu, lost);
@@ -354,9 +354,9 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     bool ok = true;
     auto pv = [&]() {   // O_h (+)= P_h V, the oldest that is due
       const uint32_t s = at0 % kStages, buf = n_p & 1u;
-      ok = ok && dsn_wait(p_full + 16 * h + 8 * buf, (n_p >> 1) & 1u, abort_flag, p.status, 83);
-      ok = ok && dsn_wait(v_full + 8 * s, (at0 / kStages) & 1u, abort_flag, p.status, 84);
-      if (first0 && n_o++ > 0) ok = ok && dsn_wait(o_empty + 8 * h, (n_o - 2u) & 1u, abort_flag, p.status, 85);
+      ok = ok && warp_wait(p_full + 16 * h + 8 * buf, (n_p >> 1) & 1u, abort_flag, p.status, 83);
+      ok = ok && warp_wait(v_full + 8 * s, (at0 / kStages) & 1u, abort_flag, p.status, 84);
+      if (first0 && n_o++ > 0) ok = ok && warp_wait(o_empty + 8 * h, (n_o - 2u) & 1u, abort_flag, p.status, 85);
       if (!ok) return;
       if (elect_one()) {
         tc_fence_after();
@@ -383,8 +383,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         const bool needed = j >= a && j < b;
         // a half that rests owes nothing: its softmax must come to the end of its item to fetch the next one's Q, and V's stages must come back
         while (n_s - n_p > (needed ? 1u : 0u) && ok) pv();
-        if (needed && j == a) ok = ok && dsn_wait(q_full + 8 * h, n_q++ & 1u, abort_flag, p.status, 86);
-        ok = ok && dsn_wait(k_full + 8 * s, (n / kStages) & 1u, abort_flag, p.status, 87);
+        if (needed && j == a) ok = ok && warp_wait(q_full + 8 * h, n_q++ & 1u, abort_flag, p.status, 86);
+        ok = ok && warp_wait(k_full + 8 * s, (n / kStages) & 1u, abort_flag, p.status, 87);
         if (!ok) break;
         if (elect_one()) {
           if (needed) {
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         // V's stages that no product is due with
         const uint32_t due = n_s != n_p ? at0 : n + 1u;
         for (; freed < due && ok; ++freed) {
-          ok = dsn_wait(v_full + 8 * (freed % kStages), (freed / kStages) & 1u, abort_flag, p.status, 92);
+          ok = warp_wait(v_full + 8 * (freed % kStages), (freed / kStages) & 1u, abort_flag, p.status, 92);
           if (ok) release(v_empty + 8 * (freed % kStages));
         }
       }
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (a == b && na < nb) up_next = load_q(nx);
       for (int j = a; j < b && ok; ++j) {
         const uint32_t buf = m & 1u;
-        ok = dsn_wait(s_full + 16 * h + 8 * buf, (m >> 1) & 1u, abort_flag, p.status, 88);
+        ok = warp_wait(s_full + 16 * h + 8 * buf, (m >> 1) & 1u, abort_flag, p.status, 88);
         if (!ok) break;
         tc_fence_after();
         if (j + 1 == b && na < nb) up_next = load_q(nx);   // every product with this item's Q has run
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
           ref = to;
           l *= f;
           if (j > a) {
-            ok = dsn_wait(o_full + 16 * h + 8 * (buf ^ 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 89);
+            ok = warp_wait(o_full + 16 * h + 8 * (buf ^ 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 89);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (!ok) break;
       const bool ran = a < b;
       if (ran) {
-        ok = dsn_wait(o_full + 16 * h + 8 * ((m - 1u) & 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 90);
+        ok = warp_wait(o_full + 16 * h + 8 * ((m - 1u) & 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 90);
         if (!ok) break;
         tc_fence_after();
       }

@@ -11,6 +11,14 @@ namespace dsn_q4 {
 constexpr int kListSmem = 64;      // requests that a CTA keeps in shared memory; further ones are read from the workspace
 constexpr float kLowest = -1e38f;  // reference before any score: finite, so that differences are
 
+// Bounded wait of a whole warp, whose lanes all get the same answer: a wait that runs out while the barrier completes must not part them.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, int32_t* status, int where) {
+#pragma unroll 1
+  for (int i = 0; i < 64; ++i)
+    if (__all_sync(0xffffffffu, dsn_gemm::mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, dsn_gemm::mbar_wait_slow(bar, parity, abort_flag, status, where));
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -83,6 +91,13 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* s_warp, uin
   return before + incl - v;
 }
 
+// Where share i of n of a line of `total` begins: shares differ by one at most.
+__device__ __forceinline__ uint64_t dsn_share(uint64_t total, uint32_t i, uint32_t n) {
+  if (total >> 32) return total / n * i + min((uint64_t)i, total % n);
+  const uint32_t t = (uint32_t)total, q = t / n, r = t - q * n;
+  return (uint64_t)q * i + min(i, r);
+}
+
 // One request's place in the line: what it needs to know and how many steps each of its heads makes, steps(len, rows).
 template <typename Steps>
 __device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, bool report, Steps steps) {
@@ -108,7 +123,7 @@ struct Stretch {
   int first_order, count;
 };
 template <int THREADS, typename Steps>
-__device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEntry* s_list, uint64_t* s_scan, Steps steps) {
+__device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEntry* s_list, uint64_t* s_scan, uint32_t workers, Steps steps) {
   __shared__ int s_first_order, s_count;
   const int tid = threadIdx.x;
   if (tid == 0) s_first_order = 0, s_count = 0;
@@ -124,8 +139,10 @@ __device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEn
     total += sum;
   }
   Stretch st;
-  st.A = total * blockIdx.x / gridDim.x;
-  st.Z = total * (blockIdx.x + 1) / gridDim.x;
+  // a short line goes to as few CTAs as give each of their `workers` a step: what one CTA cuts it joins by itself
+  const uint32_t in_use = total >= (uint64_t)gridDim.x * workers ? gridDim.x : max(1u, ((uint32_t)total + workers - 1) / workers);
+  st.A = dsn_share(total, min(blockIdx.x, in_use), in_use);
+  st.Z = dsn_share(total, min(blockIdx.x + 1, in_use), in_use);
   uint64_t at_first = 0, at_order = 0;
   for (int b = 0; b < p.B; b += THREADS) {
     CacheEntry e = e0;

@@ -60,15 +60,25 @@ class Pages:
         return [O.cache_values(self.code[pg, head, at, half], self.s[pg, head, at, half], self.z[pg, head, at, half]) for half in range(2)]
 
 
-def attention_bound(q, k, v, p, out, scale):
+    def v_size(self, i, head):
+        """|middle| + |scale (code - 8)| of the values of request i in a head, [L][D]."""
+        t = np.arange(self.lengths[i])
+        pg, at = self.table[i, t // self.page], t % self.page
+        code, s, z = self.code[pg, head, at, 1], self.s[pg, head, at, 1], self.z[pg, head, at, 1]
+        return O.cache_values(np.abs(code.astype(np.float64) - 8) + 8, s, np.abs(z))
+
+
+def attention_bound(q, k, v_size, p, out, scale):
     """How far an output may be off, element by element.
 
     Rounding the output moves it by U |out|.  Rounding a probability (times a scale) and a value to bf16 before the second product moves a term by 2 U of
-    its size.  A kernel that rounds the key elements to bf16 moves a score by at most U sum |q_d k_d| |scale|; sums in fp32 add a share of 2^-12 of
+    its size.  A value is middle + scale (code - 8), and a kernel may sum the two parts apart: p middle, and round(p scale) (code - 8) with
+    |round(p scale) - p scale| <= U p scale.  The parts can cancel (a value can be exactly 0), the roundings do not, so a term's size is
+    p (|middle| + |scale (code - 8)|), which is what v_size holds; fp32 sums of the parts add 2^-12 of the same.  A kernel that rounds the key elements to bf16 moves a score by at most U sum |q_d k_d| |scale|; sums in fp32 add a share of 2^-12 of
     that.  A score off by e moves every weight by a factor within exp(2 e), numerator and denominator together."""
     size = abs(scale) * (np.abs(q) @ np.abs(k).T)                               # [n][L]; a movement has no sign
     e = (U + 2.0 ** -12) * np.where(p > 0, size, 0.0).max(-1, keepdims=True) if p.shape[1] else np.zeros((len(q), 1))
-    terms = p @ np.abs(v) if p.shape[1] else 0.0
+    terms = p @ v_size if p.shape[1] else 0.0
     return U * np.abs(out) + (2 * U + 2.0 ** -12 + np.expm1(2 * e)) * terms + 1e-30
 
 

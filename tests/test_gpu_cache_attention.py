@@ -55,11 +55,11 @@ def compare(pages, heads, group, idx, R, placed, x, got, scale=0.0, window=0, ev
         if i % every:
             continue
         for h in range(heads[idx[i]]):
-            k, v = pages.kv(i, h)
+            (k, v), size = pages.kv(i, h), pages.v_size(i, h)
             for e in range(group):
                 q = x[i, :n, h, e]
                 ref, p = O.cache_attention(q, k, v, sc, L - n, window)
-                bound = attention_bound(q, k, v, p, ref, sc)
+                bound = attention_bound(q, k, size, p, ref, sc)
                 err = np.abs(got[i, :n, h, e] - ref)
                 assert np.all(err <= bound), (i, h, e, float((err / bound).max()))
                 if n:
@@ -176,7 +176,7 @@ def test_tokens_that_are_not_finite_reach_only_the_queries_that_see_them(dsn, D,
             if t > L - R + r:
                 for e in range(group):
                     ref, p = O.cache_attention(x[i, r:r + 1, 1, e], k, v, D ** -0.5, L - R + r)
-                    assert np.all(np.abs(got[i, r, 1, e] - ref[0]) <= attention_bound(x[i, r:r + 1, 1, e], k, v, p, ref, D ** -0.5)[0])
+                    assert np.all(np.abs(got[i, r, 1, e] - ref[0]) <= attention_bound(x[i, r:r + 1, 1, e], k, pages.v_size(i, 1), p, ref, D ** -0.5)[0])
 
 
 @pytest.mark.parametrize("R", [1, 140])
@@ -211,7 +211,7 @@ def test_pages_and_lengths_outside_the_cache(dsn, R):
         p = np.exp(s - s.max(-1, keepdims=True))
         p /= p.sum(-1, keepdims=True)
         ref = p @ v
-        assert np.all(np.abs(got[1, :, 0, 0] - ref) <= attention_bound(x[1, :, 0, 0], k, v, p, ref, 1 / 8))
+        assert np.all(np.abs(got[1, :, 0, 0] - ref) <= attention_bound(x[1, :, 0, 0], k, pages.v_size(1, 0), p, ref, 1 / 8))
     lengths = pages.lengths
     for wrong, used in ((10 ** 9, pages.max_pages * 16), (-5, 0)):
         pages.lengths = [L, wrong, L]
@@ -282,4 +282,4 @@ def test_samples_outside_every_group_are_left_alone(dsn):
     for i in (0, 2):
         k, v = pages.kv(i, 0)
         ref, p = O.cache_attention(q[i, :, :64], k, v, 1 / 8, pages.lengths[i] - 1)
-        assert np.all(np.abs(got[i] - ref) <= attention_bound(q[i, :, :64], k, v, p, ref, 1 / 8))
+        assert np.all(np.abs(got[i] - ref) <= attention_bound(q[i, :, :64], k, pages.v_size(i, 0), p, ref, 1 / 8))
