@@ -513,54 +513,61 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     if (!of_tail && s_part[w].head_far) return p.warp_data + ((int64_t)blockIdx.x * WARPS + w) * kPart;
     return reinterpret_cast<const float*>(smem + (base - smem_u32(smem)) + (size_t)w * DEPTH * slot_bytes<D>());
   };
-  int chain = 0;
-  int cta_head = 3, cta_tail = 0, tail_warp = 0;
-  for (int a = -1; a < WARPS; ++a) {
-    if (a >= 0) {
-      if (cta_head == 3 && s_part[a].head_state != 3) cta_head = 0;   // the first warp that has work begins with an item of its own
-      if (!s_part[a].tail) continue;
-    }
-    // the chain: the tail of warp a (a = -1: what came before this CTA), then heads up to the one that ends
-    int end = a, closed = 0, any = a >= 0;
-    for (int j = a + 1; j < WARPS; ++j) {
-      const int st = s_part[j].head_state;
-      if (st == 3) continue;
-      if (st == 0) break;
-      end = j;
-      any = 1;
-      if (st == 1) {
-        closed = 1;
-        break;
-      }
-    }
-    if (!any) continue;
-    if (a < 0) cta_head = closed ? 1 : 2;
-    else if (!closed) cta_tail = 1, tail_warp = a;
+  // A chain is the tail of a warp (or what came before this CTA) and the heads behind it up to the one that ends its item.
+  const CachePart mine = s_part[lane < WARPS ? lane : 0];
+  constexpr uint32_t kAll = (1u << WARPS) - 1u;
+  const uint32_t closes = __ballot_sync(0xffffffffu, mine.head_state == 1) & kAll, passes = __ballot_sync(0xffffffffu, mine.head_state == 2) & kAll,
+                 begins = __ballot_sync(0xffffffffu, mine.head_state == 0) & kAll, tails = __ballot_sync(0xffffffffu, mine.tail != 0) & kAll;
+  const uint32_t first_heads = (closes | passes) & ~(begins ? ~((begins & (0u - begins)) - 1u) : 0u);   // heads in front of the first item that begins here
+  // parts of the chain behind warp a (-1: in front of all): up to the first that closes
+  auto heads_of = [&](int a) -> uint32_t {
+    const uint32_t behind = a < 0 ? kAll : kAll & ~((2u << a) - 1u);
+    const uint32_t stop = (closes | begins) & behind;
+    const uint32_t upto = stop ? (stop & (0u - stop)) * 2u - 1u : ~0u;
+    return (closes | passes) & behind & upto;
+  };
+  const uint32_t none = closes | passes | begins;
+  const int cta_head = !none ? 3 : (first_heads ? ((heads_of(-1) & closes) ? 1 : 2) : 0);
+  int cta_tail = 0, tail_warp = 0, task = 0;
+  for (uint32_t left = (tails << 1) | (first_heads ? 1u : 0u); left; left &= left - 1u) {
+    const int a = __ffs(left) - 2;
+    const uint32_t heads = heads_of(a);
+    const bool closed = (heads & closes) != 0;
+    if (a >= 0 && !closed) cta_tail = 1, tail_warp = a;
     const int cols = a >= 0 ? s_part[a].rows * p.group : NC;
-    for (int v = 0; v < NC; ++v, ++chain) {
-      if (chain % WARPS != warp || v >= cols) continue;
-      float m = kLowest, sum = 0.f, y[D / 32];
+    const bool in = (heads >> lane & 1u) || lane == a;   // lane j: the part of warp j
+    const float* src = in ? part_of(lane, lane == a) : nullptr;
+    const int begin = (warp + WARPS - task % WARPS) % WARPS;
+    task += cols;
+    for (int v = begin; v < cols; v += WARPS) {
+      const float m = in ? src[v] : kLowest, l = in ? src[NC + v] : 0.f;
+      float top = m;
+#pragma unroll
+      for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));   // at most 15 parts
+      top = __shfl_sync(0xffffffffu, top, 0);
+      const float f = l == 0.f ? 0.f : ex2(m - top);   // an empty part holds nothing
+      float sum = l * f;
+#pragma unroll
+      for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      sum = __shfl_sync(0xffffffffu, sum, 0);
+      float y[D / 32];
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) y[x] = 0.f;
-#pragma unroll 4
-      for (int j = a; j <= end; ++j) {
-        if (j < 0 || (j != a && s_part[j].head_state == 3)) continue;
-        const float* src = part_of(j, j == a);
-        const float mj = src[v], lj = src[NC + v];
-        const float m2 = fmaxf(m, mj), fa = ex2(m - m2), fb = ex2(mj - m2);
-        m = m2;
-        sum = sum * fa + lj * fb;
+#pragma unroll
+      for (int j = 0; j < WARPS; ++j) {
+        const float fj = __shfl_sync(0xffffffffu, f, j);
+        const float* at = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)reinterpret_cast<uint64_t>(src), j)) + 2 * NC + v * D;
         if constexpr (D == 128) {
-          const float4 q = *reinterpret_cast<const float4*>(src + 2 * NC + v * D + 4 * lane);
-          y[0] = y[0] * fa + q.x * fb; y[1] = y[1] * fa + q.y * fb; y[2] = y[2] * fa + q.z * fb; y[3] = y[3] * fa + q.w * fb;
+          const float4 q = fj == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(at + 4 * lane);
+          y[0] = fmaf(q.x, fj, y[0]); y[1] = fmaf(q.y, fj, y[1]); y[2] = fmaf(q.z, fj, y[2]); y[3] = fmaf(q.w, fj, y[3]);
         } else {
-          const float2 q = *reinterpret_cast<const float2*>(src + 2 * NC + v * D + 2 * lane);
-          y[0] = y[0] * fa + q.x * fb; y[1] = y[1] * fa + q.y * fb;
+          const float2 q = fj == 0.f ? make_float2(0.f, 0.f) : *reinterpret_cast<const float2*>(at + 2 * lane);
+          y[0] = fmaf(q.x, fj, y[0]); y[1] = fmaf(q.y, fj, y[1]);
         }
       }
       if (a >= 0 && closed) {
         const CachePart& q = s_part[a];
-        const int r = v / p.group, ev = v - r * p.group;
+        const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? q.pos : q.sample) * p.R + r) * p.ld_out + ((int64_t)q.head * p.group + ev) * D;
         if constexpr (D == 128)
@@ -570,14 +577,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
       } else {
         float* dst = p.cta_data + ((int64_t)blockIdx.x * 2 + (a >= 0)) * kPart;
         if (lane == 0) {
-          dst[v] = m;
+          dst[v] = top;
           dst[NC + v] = sum;
         }
-#pragma unroll
-        for (int x = 0; x < D / 32; ++x) dst[2 * NC + v * D + (D / 32) * lane + x] = y[x];
+        if constexpr (D == 128) *reinterpret_cast<float4*>(dst + 2 * NC + v * D + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<float2*>(dst + 2 * NC + v * D + 2 * lane) = make_float2(y[0], y[1]);
       }
     }
   }
+  static_assert(WARPS <= 15, "a chain's parts are joined by 16 lanes");
   if (tid == 0) {
     CachePart q = s_part[tail_warp];
     q.head_state = cta_head;

@@ -68,27 +68,35 @@ __device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// Exclusive sums over the CTA of two numbers at once (s_warp: two numbers a warp).
 template <int THREADS>
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* s_warp, uint64_t& total) {   // exclusive
+__device__ __forceinline__ void block_scan(uint64_t& v, uint32_t& w, uint64_t* s_warp, uint64_t& v_total, uint32_t& w_total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint64_t incl = v;
+  uint32_t count = w;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const uint64_t u = __shfl_up_sync(0xffffffffu, (unsigned long long)incl, o);
-    if (lane >= o) incl += u;
+    const uint32_t c = __shfl_up_sync(0xffffffffu, count, o);
+    if (lane >= o) incl += u, count += c;
   }
   __syncthreads();
-  if (lane == 31) s_warp[warp] = incl;
+  if (lane == 31) s_warp[2 * warp] = incl, s_warp[2 * warp + 1] = count;
   __syncthreads();
   uint64_t before = 0;
-  total = 0;
+  uint32_t before_w = 0;
+  v_total = 0;
+  w_total = 0;
 #pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    const uint64_t u = s_warp[w];
-    if (w < warp) before += u;
-    total += u;
+  for (int k = 0; k < THREADS / 32; ++k) {
+    const uint64_t u = s_warp[2 * k];
+    const uint32_t c = (uint32_t)s_warp[2 * k + 1];
+    if (k < warp) before += u, before_w += c;
+    v_total += u;
+    w_total += c;
   }
-  return before + incl - v;
+  v = before + incl - v;
+  w = before_w + count - w;
 }
 
 // Where share i of n of a line of `total` begins: shares differ by one at most.
@@ -128,14 +136,15 @@ __device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEn
   const int tid = threadIdx.x;
   if (tid == 0) s_first_order = 0, s_count = 0;
   const CacheEntry e0 = look_up(p, tid, blockIdx.x == 0, steps);
-  uint64_t sum0, ones0, total;
-  const uint64_t first0 = block_scan<THREADS>((uint64_t)e0.heads * e0.steps, s_scan, sum0);
-  const uint64_t order0 = block_scan<THREADS>(e0.heads > 0, s_scan, ones0);
-  total = sum0;
+  uint64_t sum0, first0 = (uint64_t)e0.heads * e0.steps;
+  uint32_t ones0, order0 = e0.heads > 0;
+  block_scan<THREADS>(first0, order0, s_scan, sum0, ones0);
+  uint64_t total = sum0;
   for (int b = THREADS; b < p.B; b += THREADS) {
-    uint64_t sum;
     const CacheEntry e = look_up(p, b + tid, blockIdx.x == 0, steps);
-    block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
+    uint64_t sum, first = (uint64_t)e.heads * e.steps;
+    uint32_t ones, order = e.heads > 0;
+    block_scan<THREADS>(first, order, s_scan, sum, ones);
     total += sum;
   }
   Stretch st;
@@ -143,14 +152,19 @@ __device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEn
   const uint32_t in_use = total >= (uint64_t)gridDim.x * workers ? gridDim.x : max(1u, ((uint32_t)total + workers - 1) / workers);
   st.A = dsn_share(total, min(blockIdx.x, in_use), in_use);
   st.Z = dsn_share(total, min(blockIdx.x + 1, in_use), in_use);
-  uint64_t at_first = 0, at_order = 0;
+  uint64_t at_first = 0;
+  uint32_t at_order = 0;
   for (int b = 0; b < p.B; b += THREADS) {
     CacheEntry e = e0;
-    uint64_t first = first0, order = order0, sum = sum0, ones = ones0;
+    uint64_t first = first0, sum = sum0;
+    uint32_t order = order0, ones = ones0;
     if (b > 0) {
       e = look_up(p, b + tid, false, steps);
-      first = at_first + block_scan<THREADS>((uint64_t)e.heads * e.steps, s_scan, sum);
-      order = at_order + block_scan<THREADS>(e.heads > 0, s_scan, ones);
+      first = (uint64_t)e.heads * e.steps;
+      order = e.heads > 0;
+      block_scan<THREADS>(first, order, s_scan, sum, ones);
+      first += at_first;
+      order += at_order;
     }
     at_first += sum;
     at_order += ones;
