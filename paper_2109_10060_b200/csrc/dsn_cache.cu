@@ -149,20 +149,24 @@ __global__ void __launch_bounds__(256) cache_reset_kernel(int32_t B, int32_t n_p
 }
 
 // ------------------------------------------------------------------------------------------------ write
-// A lane takes eight elements: 8 lanes a group of 64, 2 D / 8 lanes the k and v of a head, which lie side by side in the row.
-template <int D>
+// A lane takes eight elements: 8 lanes a group of 64, 2 D / 8 lanes the k and v of a head, which lie side by side in the row.  A warp takes a row, or every
+// `split`th piece of it where there are few rows, four pieces on their way at a time.
+// Bound by instructions once memory is busy: least and greatest value go through the shuffles as one pair of bf16 numbers (the least, minus the greatest);
+// a code comes out of an addition that rounds (1.5 * 2^23 + 8: its low four bits are the code), eight of them are put together by multiply-adds.
+template <int D, bool VALUES>
 __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
   constexpr int LPH = D / 4;             // lanes a head
   constexpr int HPW = 32 / LPH;          // heads a warp does at a time
+  constexpr int U = 4;
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int head_chunks = (p.max_heads + HPW - 1) / HPW;
-  const int64_t items = (int64_t)p.B * p.R * head_chunks;
-  const int64_t warps = (int64_t)gridDim.x * 8;
+  const int lane = threadIdx.x & 31, sub = lane % LPH;
+  const int chunks = (p.max_heads + HPW - 1) / HPW;
+  const int half = sub / (D / 8), grp = (sub % (D / 8)) >> 3, word = sub & 7;
+  const int64_t items = (int64_t)p.B * p.R * p.split, warps = (int64_t)gridDim.x * 8;
   for (int64_t it = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); it < items; it += warps) {
-    const uint32_t row = (uint32_t)(it / head_chunks);
-    const int hc = (int)(it - (int64_t)row * head_chunks);
+    const uint32_t row = (uint32_t)(it / p.split);
+    const int part = (int)(it - (int64_t)row * p.split);
     const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
     const PosInfo at = dsn_locate_warp(pos, p.G, p.T, p.offsets, p.perm, p.group_slice);
     if (at.slice < 0 || at.sample >= p.B) continue;
@@ -172,65 +176,75 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
       if (lane == 0) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, (int)row);
       continue;
     }
-    const int head = hc * HPW + lane / LPH, sub = lane % LPH;
-    const bool live = head < p.heads[at.slice];
+    const int heads = p.heads[at.slice];
     const int64_t xrow = (int64_t)(p.grouped ? pos : at.sample) * p.R + r;
-    float x[8];
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (live) raw = *reinterpret_cast<const uint4*>(p.qkv + xrow * p.ld_qkv + ((int64_t)head * (p.group + 2) + p.group) * D + sub * 8);
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    const __nv_bfloat16* x = p.qkv + xrow * p.ld_qkv + (int64_t)p.group * D + sub * 8;
+    const int pg = (int)dsn_div((uint32_t)slot, p.by_page), tok = slot - pg * p.page, t = tok % DSN_CACHE_BLOCK;
+    const int64_t head_bytes = (int64_t)(p.page / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D);
+    uint8_t* blk = p.pages + pg * (p.H * head_bytes) + (tok / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D) + half * (dsn_cache_block_bytes(D) / 2);
+    for (int c0 = part; c0 < chunks; c0 += U * p.split) {
+      uint4 raw[U];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __uint_as_float(w[j] << 16);
-      x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    }
-    bool bad = false;
-    float lo = x[0], hi = x[0];
+      for (int u = 0; u < U; ++u) {
+        const int head = (c0 + u * p.split) * HPW + lane / LPH;
+        raw[u] = make_uint4(0, 0, 0, 0);
+        if (head < heads) raw[u] = *reinterpret_cast<const uint4*>(x + (int64_t)head * (p.group + 2) * D);
+      }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      bad |= (__float_as_uint(x[j]) & 0x7f800000u) == 0x7f800000u;
-      lo = fminf(lo, x[j]);
-      hi = fmaxf(hi, x[j]);
-    }
+      for (int u = 0; u < U; ++u) {
+        if (c0 + u * p.split >= chunks) break;
+        const int head = (c0 + u * p.split) * HPW + lane / LPH;
+        const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+        const uint32_t mag = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+        const uint32_t all = __ballot_sync(0xffffffffu, max(mag & 0xffffu, mag >> 16) >= 0x7f80u);   // NaN or infinity
+        const bool poison = (LPH == 32 ? all : (all >> (lane & 16)) & 0xffffu) != 0;
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
+        const __nv_bfloat162 mn = __hmin2(__hmin2(h[0], h[1]), __hmin2(h[2], h[3])), mx = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        __nv_bfloat162 ends = __halves2bfloat162(__hmin(mn.x, mn.y), __hneg(__hmax(mx.x, mx.y)));
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
-    const uint32_t all = __ballot_sync(0xffffffffu, bad);
-    const bool poison = (LPH == 32 ? all : (all >> (lane & 16)) & 0xffffu) != 0;
-    const float fifteenth = 1.0f / 15.0f;
-    float s = __bfloat162float(__float2bfloat16_rn(__fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))));
-    if (s < 1.17549435e-38f) s = 0.f;
-    float z = __bfloat162float(__float2bfloat16_rn(2.f * __fadd_rn(0.5f * lo, 4.f * s)));
-    const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
-    if (poison) {
-      s = 0.f;
-      z = __uint_as_float(0x7fc00000u);
-    }
-    uint32_t code = 0;
-    uint32_t val[4];
+        for (int o = 1; o < 8; o <<= 1) {
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&ends), o);
+          ends = __hmin2(ends, *reinterpret_cast<const __nv_bfloat162*>(&other));
+        }
+        const float lo = __bfloat162float(ends.x), hi = -__bfloat162float(ends.y);
+        const float fifteenth = 1.0f / 15.0f;
+        float s = __bfloat162float(__float2bfloat16_rn(__fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))));
+        if (s < 1.17549435e-38f) s = 0.f;
+        float z = __bfloat162float(__float2bfloat16_rn(2.f * __fadd_rn(0.5f * lo, 4.f * s)));
+        const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+        if (poison) {
+          s = 0.f;
+          z = __uint_as_float(0x7fc00000u);
+        }
+        constexpr float magic = 12582920.f;   // 1.5 * 2^23 + 8
+        float step[8];
+        uint32_t code = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      int c = __float2int_rn(__fmul_rn(__fsub_rn(x[j], z), inv)) + 8;
-      c = s > 0.f ? min(max(c, 0), 15) : 8;
-      code |= (uint32_t)c << (4 * j);
-      const float v = fmaf(s, (float)(c - 8), z);
-      const uint32_t h = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-      val[j >> 1] = j & 1 ? val[j >> 1] | (h << 16) : h;
+        for (int j = 7; j >= 0; --j) {
+          const float v = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+          const float q = __fmul_rn(__fsub_rn(v, z), inv);                     // what the ends cut off may be an infinity; s = 0: NaN, 0
+          step[j] = __fadd_rn(fminf(fmaxf(s > 0.f ? q : 0.f, -8.f), 7.f), magic);
+          code = code * 16u + __float_as_uint(step[j]);
+        }
+        code -= 0x4b400000u * 0x11111111u;                                     // the eight exponents' share
+        if (head < heads) {
+          uint8_t* to = blk + head * head_bytes;
+          *reinterpret_cast<uint32_t*>(to + (grp * DSN_CACHE_BLOCK + t) * 32 + word * 4) = code;
+          if (word == 0)
+            *reinterpret_cast<uint32_t*>(to + D / 64 * DSN_CACHE_BLOCK * 32 + (grp * DSN_CACHE_BLOCK + t) * 4) =
+                (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xffff0000u);
+          if (VALUES) {
+            uint32_t val[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const __nv_bfloat162 y = __floats2bfloat162_rn(fmaf(s, step[2 * j] - magic, z), fmaf(s, step[2 * j + 1] - magic, z));
+              val[j] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            *reinterpret_cast<uint4*>(p.values + xrow * p.ld_values + (int64_t)head * 2 * D + sub * 8) = make_uint4(val[0], val[1], val[2], val[3]);
+          }
+        }
+      }
     }
-    if (!live) continue;
-    const int pg = (int)dsn_div((uint32_t)slot, p.by_page), tok = slot - pg * p.page;
-    const int half = sub / (D / 8), grp = (sub % (D / 8)) >> 3, word = sub & 7;
-    uint8_t* blk = p.pages + (((int64_t)pg * p.H + head) * (p.page / DSN_CACHE_BLOCK) + tok / DSN_CACHE_BLOCK) * dsn_cache_block_bytes(D) +
-                   half * (dsn_cache_block_bytes(D) / 2);
-    const int t = tok % DSN_CACHE_BLOCK;
-    *reinterpret_cast<uint32_t*>(blk + (grp * DSN_CACHE_BLOCK + t) * 32 + word * 4) = code;
-    if (word == 0)
-      *reinterpret_cast<uint32_t*>(blk + D / 64 * DSN_CACHE_BLOCK * 32 + (grp * DSN_CACHE_BLOCK + t) * 4) =
-          (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xffff0000u);
-    if (p.values)
-      *reinterpret_cast<uint4*>(p.values + xrow * p.ld_values + (int64_t)head * 2 * D + sub * 8) = make_uint4(val[0], val[1], val[2], val[3]);
   }
 }
 
@@ -247,10 +261,14 @@ cudaError_t dsn_launch_cache_reset(int32_t B, int32_t n_pages, int32_t* lengths,
   return dsn_launch(cache_reset_kernel, dim3((unsigned)(ctas < 592 ? ctas : 592)), dim3(256), 0, s, 1, B, n_pages, lengths, pool, pool_state);
 }
 
-cudaError_t dsn_launch_cache_write(const CacheWriteParams& p, int sm_count, cudaStream_t s) {
-  const int hpw = p.D == 64 ? 2 : 1;
-  const int64_t items = (int64_t)p.B * p.R * ((p.max_heads + hpw - 1) / hpw), ctas = (items + 7) / 8;
-  const int64_t most = (int64_t)sm_count * 8;
+cudaError_t dsn_launch_cache_write(CacheWriteParams& p, int sm_count, cudaStream_t s) {
+  const int hpw = p.D == 64 ? 2 : 1, chunks = (p.max_heads + hpw - 1) / hpw;
+  const int64_t rows = (int64_t)p.B * p.R, most = (int64_t)sm_count * 8;
+  // few rows: as many warps a row as fill the GPU, up to one a piece
+  int64_t split = most * 8 / rows;
+  p.split = (int32_t)(split < 1 ? 1 : (split > chunks ? chunks : split));
+  const int64_t ctas = (rows * p.split + 7) / 8;
   const dim3 grid((unsigned)(ctas < most ? ctas : most));
-  return p.D == 64 ? dsn_launch(cache_write_kernel<64>, grid, dim3(256), 0, s, 1, p) : dsn_launch(cache_write_kernel<128>, grid, dim3(256), 0, s, 1, p);
+  if (p.D == 64) return p.values ? dsn_launch(cache_write_kernel<64, true>, grid, dim3(256), 0, s, 1, p) : dsn_launch(cache_write_kernel<64, false>, grid, dim3(256), 0, s, 1, p);
+  return p.values ? dsn_launch(cache_write_kernel<128, true>, grid, dim3(256), 0, s, 1, p) : dsn_launch(cache_write_kernel<128, false>, grid, dim3(256), 0, s, 1, p);
 }

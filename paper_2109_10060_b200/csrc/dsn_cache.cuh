@@ -26,7 +26,7 @@ cudaError_t dsn_launch_cache_reset(int32_t B, int32_t n_pages, int32_t* lengths,
 
 struct CacheWriteParams {
   int16_t heads[DSN_MAX_SLICES];
-  int32_t B, R, H, D, group, G, T, page, max_heads, grouped;
+  int32_t B, R, H, D, group, G, T, page, max_heads, grouped, split;   // split: warps a row
   int64_t n_slots;      // tokens that the pages hold
   FastDiv by_R, by_page;
   const int32_t* offsets;
@@ -40,7 +40,7 @@ struct CacheWriteParams {
   uint8_t* pages;
   int32_t* status;
 };
-cudaError_t dsn_launch_cache_write(const CacheWriteParams& p, int sm_count, cudaStream_t s);
+cudaError_t dsn_launch_cache_write(CacheWriteParams& p, int sm_count, cudaStream_t s);
 
 // A request of the line of steps.
 struct __align__(16) CacheEntry {

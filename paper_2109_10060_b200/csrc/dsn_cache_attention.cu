@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   // The fetching side: a slot of the ring takes up to two steps of an item; lane b fetches its block b; the page's number is read a slot before the copy
   // that needs it.  Blocks that lie behind one another in a page are one copy.
   int f_left = n_steps, f_n = 0, f_tok = 0, f_hi = 0, pg = -1, place = 0;   // steps to come, of this slot; this lane's token, the item's end; page, block in it
-  const int64_t page_blocks = (int64_t)p.H * bpp;
+  const uint32_t page_bytes = (uint32_t)p.H * (uint32_t)bpp * kBlock;   // below 2^30
   bool wanted = false;
   auto find = [&](bool entered) {
     if (entered) {   // an item
@@ -159,15 +159,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   auto issue = [&](int slot) -> uint32_t {   // bit b of the result: block b is on its way
     const bool ok = pg >= 0 && pg < p.n_pages;
     if (wanted && !ok) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, fetch.e.sample);
-    const int64_t at = ok ? pg * page_blocks + (int64_t)fetch.head * bpp + place : -2 - 2 * lane;
     const uint32_t there = __ballot_sync(0xffffffffu, ok);
-    const int64_t before = (int64_t)__shfl_up_sync(0xffffffffu, (long long)at, 1);   // by all lanes, wanted or not
-    const uint32_t begins = __ballot_sync(0xffffffffu, ok && (lane == 0 || at != before + 1));
+    const int before = __shfl_up_sync(0xffffffffu, pg, 1);   // by all lanes, wanted or not
+    const uint32_t begins = __ballot_sync(0xffffffffu, ok && (lane == 0 || pg != before || place == 0));
     if (lane == 0) dsn_gemm::mbar_expect_tx(bars + 8u * slot, (uint32_t)__popc(there) * kBlock);
     __syncwarp();
     if (begins >> lane & 1u) {
       const uint32_t stops = (~there | begins) >> lane >> 1;   // where this run of blocks ends
-      dsn_bulk_load(ring + (uint32_t)slot * slot_bytes<D>() + (uint32_t)lane * kBlock, p.pages + at * kBlock, (uint32_t)__ffs(stops) * kBlock, bars + 8u * slot);
+      dsn_bulk_load(ring + (uint32_t)slot * slot_bytes<D>() + (uint32_t)lane * kBlock, p.pages + (uint64_t)(uint32_t)pg * page_bytes + (uint32_t)(fetch.head * bpp + place) * kBlock,
+                    (uint32_t)__ffs(stops) * kBlock, bars + 8u * slot);
     }
     return there;
   };
