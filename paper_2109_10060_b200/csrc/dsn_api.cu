@@ -1476,6 +1476,7 @@ int dsn_cache_plan(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, in
   CachePlanParams p;
   p.B = B; p.R = d->R; p.page = d->page; p.n_pages = d->n_pages; p.max_pages = d->max_pages;
   p.by_page = dsn_fast_div((uint32_t)d->page);
+  p.by_R = dsn_fast_div((uint32_t)d->R);
   p.new_tokens = new_tokens; p.lengths = c->lengths; p.pool_state = c->pool_state;
   p.lengths_out = lengths_out ? lengths_out : c->lengths;
   p.pool_state_out = pool_state_out ? pool_state_out : c->pool_state;

@@ -4,21 +4,24 @@
 namespace {
 
 // ------------------------------------------------------------------------------------------------ plan
-// One cluster of CTAs; every CTA scans all requests on its own (8 bytes each), 1024 at a time, one a thread, and then the warps of the cluster share
-// the slots, a piece of a request's rows at a time.  A slot needs no other thread's result: a token's page stands in the table already or
+// One cluster of CTAs (one CTA for few rows); every CTA scans all requests on its own (8 bytes each), one a thread and THREADS at a time, and then the threads of
+// the cluster share the slots.  A slot needs no other thread's result: a token's page stands in the table already or
 // is the ring's entry at a place that the scan gives.  What a CTA of the cluster still has to read (lengths, ring counters) is overwritten only behind the
 // cluster's barrier.  Pages taken and pages returned are different entries of the ring, so those need no order.
-constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
-constexpr int kPlanRows = 128;   // rows of a request that a warp does at a time
-
+// Bound by trips to memory: lengths, then pages, then the stores; eight rows a thread are looked up at once (one after the other: 18 us for 128 x 2048 rows).
 struct PlanRequest {
   int32_t held, placed;   // placed < 0: the request ends
   uint32_t start;         // new pages of the requests before it; or returned pages of the requests before it
 };
 
-__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_constant__ CachePlanParams p) {
-  __shared__ PlanRequest s_req[kPlanThreads];
-  __shared__ unsigned long long s_warp[kPlanWarps];
+// Place i of the ring: what is taken or given back together does not pass the whole ring.
+__device__ __forceinline__ uint32_t ring(uint32_t i, uint32_t N) { return i >= N ? (i - N < N ? i - N : (i - N) % N) : i; }
+
+template <int THREADS, bool LONG>   // LONG: many rows a request
+__global__ void __launch_bounds__(THREADS) cache_plan_kernel(const __grid_constant__ CachePlanParams p) {
+  constexpr int WARPS = THREADS / 32;
+  __shared__ PlanRequest s_req[THREADS];
+  __shared__ unsigned long long s_warp[WARPS];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x, ranks = gridDim.x;   // the grid is one cluster
   dsn_grid_dependency_wait();
@@ -28,8 +31,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
   const uint32_t avail = min((uint32_t)max(p.pool_state[1], 0), N);
   const int64_t room = (int64_t)p.max_pages * p.page;
   uint32_t asked = 0, used = 0, returned = 0;   // pages: asked for, taken, given back by the requests before this chunk
-  const int segs = (p.R + kPlanRows - 1) / kPlanRows;
-  for (int base = 0; base < p.B; base += kPlanThreads) {
+  for (int base = 0; base < p.B; base += THREADS) {
     const int i = base + tid;
     int held = 0, n = 0, have = 0, need = 0;
     bool end = false;
@@ -47,10 +49,9 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
       }
     }
     bool fits = have + need <= p.max_pages;
-    const bool room_short = !fits;
-    if (room_short) need = 0;
+    if (!fits) need = 0;
     // one scan for both sums: pages asked for in the low half, pages returned in the high half
-    unsigned long long v = (unsigned long long)(uint32_t)need | ((unsigned long long)(uint32_t)(end ? have : 0) << 32);
+    const unsigned long long v = (unsigned long long)(uint32_t)need | ((unsigned long long)(uint32_t)(end ? have : 0) << 32);
     unsigned long long incl = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
     __syncthreads();
     unsigned long long before = 0, total = 0;
 #pragma unroll 8
-    for (int w = 0; w < kPlanWarps; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
       const unsigned long long u = s_warp[w];
       if (w < warp) before += u;
       total += u;
@@ -77,52 +78,116 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
       s_req[tid] = PlanRequest{held, placed, end ? returned + (uint32_t)(incl >> 32) - (uint32_t)have : upto - (uint32_t)need};
       if (rank == 0) p.placed[i] = placed > 0 ? placed : 0;
     }
-    // served requests are those up to a point (and those that need nothing), so what they take is the largest sum that fits
-    {
-      const uint32_t mine = i < p.B && need > 0 && fits ? upto : 0u;
-      const uint32_t top = __reduce_max_sync(0xffffffffu, mine);
+    asked += (uint32_t)total;
+    returned += (uint32_t)(total >> 32);
+    if (asked <= avail) {   // all of them
+      used = asked;
+      __syncthreads();
+    } else {                // served requests are those up to a point (and those that need nothing): what they take is the largest sum that fits
+      const uint32_t top = __reduce_max_sync(0xffffffffu, i < p.B && need > 0 && fits ? upto : 0u);
       __syncthreads();
       if (lane == 0) s_warp[warp] = top;
       __syncthreads();
-      for (int w = 0; w < kPlanWarps; ++w) used = max(used, (uint32_t)s_warp[w]);
+      for (int w = 0; w < WARPS; ++w) used = max(used, (uint32_t)s_warp[w]);
     }
-    asked += (uint32_t)total;
-    returned += (uint32_t)(total >> 32);
-    // slots and table entries, a warp a piece
-    const int count = min(kPlanThreads, p.B - base);
-    for (int64_t it = (int64_t)rank * kPlanWarps + warp; it < (int64_t)count * segs; it += (int64_t)ranks * kPlanWarps) {
-      const int k = (int)(it / segs), seg = (int)(it - (int64_t)k * segs);
-      const PlanRequest q = s_req[k];
-      const int64_t row = (int64_t)(base + k) * p.max_pages;
-      const int have_k = (int)dsn_div((uint32_t)(q.held + p.page - 1), p.by_page);
-      int32_t* slots = p.slots + (int64_t)(base + k) * p.R;
+    const int count = min(THREADS, p.B - base);
+    if (LONG) {
+      // 512 rows of a request a warp, four in a row a lane: they lie in one page or two
+      const int segs = (p.R + 511) / 512;
+      const bool wide = p.R % 4 == 0 && (reinterpret_cast<uintptr_t>(p.slots) & 15) == 0;
+      for (int64_t it = (int64_t)rank * WARPS + warp; it < (int64_t)count * segs; it += (int64_t)ranks * WARPS) {
+        const int k = (int)(it / segs), r0 = (int)(it - (int64_t)k * segs) * 512 + lane * 4;
+        const PlanRequest q = s_req[k];
+        const int have_k = (int)dsn_div((uint32_t)(q.held + p.page - 1), p.by_page);
+        int32_t* table = p.table + (int64_t)(base + k) * p.max_pages;
+        int32_t* slots = p.slots + (int64_t)(base + k) * p.R;
+        int pa[4], pb[4], col[4];
 #pragma unroll
-      for (int j = 0; j < kPlanRows / 32; ++j) {
-        const int r = seg * kPlanRows + j * 32 + lane;
-        if (r >= p.R) break;
-        int slot = -1;
-        if (r < q.placed) {
-          const int pos = q.held + r;
-          const int col = (int)dsn_div((uint32_t)pos, p.by_page), at = pos - col * p.page;
-          int pg;
-          if (col < have_k) {
-            pg = p.table[row + col];
-          } else {
-            const uint32_t e = (first + q.start + (uint32_t)(col - have_k)) % N;
-            pg = p.pool[e];
-            if (at == 0) p.table[row + col] = pg;
+        for (int j = 0; j < 4; ++j) {   // all pages first, as no load may pass a store
+          const int r = r0 + 128 * j;
+          col[j] = (int)dsn_div((uint32_t)(q.held + r), p.by_page);
+          pa[j] = pb[j] = -1;
+          const int last = min(r + 3, q.placed - 1);   // of these rows, the last that is placed
+          if (r <= last) {
+            pa[j] = *(col[j] < have_k ? table + col[j] : p.pool + ring(first + q.start + (uint32_t)(col[j] - have_k), N));
+            if (q.held + last >= (col[j] + 1) * p.page)
+              pb[j] = *(col[j] + 1 < have_k ? table + col[j] + 1 : p.pool + ring(first + q.start + (uint32_t)(col[j] + 1 - have_k), N));
           }
-          slot = pg < 0 || pg >= p.n_pages ? -1 : pg * p.page + at;
         }
-        slots[r] = slot;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = r0 + 128 * j, at = q.held + r - col[j] * p.page;
+          int slot[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool second = at + i >= p.page;
+            const int pg = second ? pb[j] : pa[j], in = second ? at + i - p.page : at + i;
+            slot[i] = r + i >= q.placed || pg < 0 || pg >= p.n_pages ? -1 : pg * p.page + in;
+            if (r + i < q.placed && in == 0 && col[j] + second >= have_k) table[col[j] + second] = pg;
+          }
+          if (r >= p.R) continue;
+          if (wide) *reinterpret_cast<int4*>(slots + r) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+          else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (r + i < p.R) slots[r + i] = slot[i];
+        }
       }
-      if (q.placed < 0 && seg == 0)
-        for (int j = lane; j < have_k; j += 32) p.pool[(first + avail + q.start + (uint32_t)j) % N] = p.table[row + j];
+    } else {
+    // rows of all requests of the chunk in a line, eight a thread at a time; all pages first, as no load may pass a store
+    const uint32_t stride = (uint32_t)(ranks * THREADS), stop = (uint32_t)(base + count) * (uint32_t)p.R;   // rows: below 2^31
+    for (uint32_t row0 = (uint32_t)base * (uint32_t)p.R + (uint32_t)(rank * THREADS + tid); row0 < stop; row0 += 8u * stride) {
+      int pg[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t row = row0 + (uint32_t)j * stride;
+        pg[j] = -1;
+        if (row < stop) {
+          const uint32_t k = dsn_div(row, p.by_R), r = row - k * (uint32_t)p.R;
+          const PlanRequest q = s_req[k - base];
+          if ((int)r < q.placed) {
+            const int have_k = (int)dsn_div((uint32_t)(q.held + p.page - 1), p.by_page), col = (int)dsn_div((uint32_t)q.held + r, p.by_page);
+            pg[j] = *(col < have_k ? p.table + (int64_t)k * p.max_pages + col : p.pool + ring(first + q.start + (uint32_t)(col - have_k), N));
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t row = row0 + (uint32_t)j * stride;
+        if (row >= stop) break;
+        const uint32_t k = dsn_div(row, p.by_R), r = row - k * (uint32_t)p.R;
+        const PlanRequest q = s_req[k - base];
+        int slot = -1;
+        if ((int)r < q.placed) {
+          const int pos = q.held + (int)r, have_k = (int)dsn_div((uint32_t)(q.held + p.page - 1), p.by_page);
+          const int col = (int)dsn_div((uint32_t)pos, p.by_page), at = pos - col * p.page;
+          if (col >= have_k && at == 0) p.table[(int64_t)k * p.max_pages + col] = pg[j];
+          slot = pg[j] < 0 || pg[j] >= p.n_pages ? -1 : pg[j] * p.page + at;
+        }
+        p.slots[row] = slot;
+      }
     }
+    }
+    // pages of requests that ended, a warp a request
+    if ((uint32_t)(total >> 32))
+      for (int k = rank * WARPS + warp; k < count; k += ranks * WARPS) {
+        const PlanRequest q = s_req[k];
+        if (q.placed >= 0) continue;
+        const int have_k = (int)dsn_div((uint32_t)(q.held + p.page - 1), p.by_page);
+        const int32_t* from = p.table + (int64_t)(base + k) * p.max_pages;
+        for (int j0 = lane; j0 < have_k; j0 += 256) {
+          int pg[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) pg[j] = j0 + 32 * j < have_k ? from[j0 + 32 * j] : 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j0 + 32 * j < have_k) p.pool[ring(first + avail + q.start + (uint32_t)(j0 + 32 * j), N)] = pg[j];
+        }
+      }
   }
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (rank == 0) {
-    for (int i = tid; i < p.B; i += kPlanThreads) {
+    for (int i = tid; i < p.B; i += THREADS) {
       const int held = p.lengths[i], n = p.new_tokens[i];
       const bool end = n == -1 && held >= 0 && held <= room;
       p.lengths_out[i] = end ? 0 : held + p.placed[i];   // placed[i] is this thread's own write
@@ -251,8 +316,10 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
 }  // namespace
 
 cudaError_t dsn_launch_cache_plan(const CachePlanParams& p, cudaStream_t s) {
-  const int ranks = (int64_t)p.B * p.R > 4096 ? 8 : 1;   // portable cluster size
-  return dsn_launch(cache_plan_kernel, dim3((unsigned)ranks), dim3(kPlanThreads), 0, s, ranks, p);
+  const int64_t rows = (int64_t)p.B * p.R;
+  if (p.B <= 128 && rows <= 1024) return dsn_launch(cache_plan_kernel<128, false>, dim3(1), dim3(128), 0, s, 1, p);   // fewer warps meet sooner
+  const int ranks = rows > 4096 ? 8 : 1;   // portable cluster size
+  return dsn_launch(p.R >= 64 ? cache_plan_kernel<1024, true> : cache_plan_kernel<1024, false>, dim3((unsigned)ranks), dim3(1024), 0, s, ranks, p);
 }
 
 cudaError_t dsn_launch_cache_reset(int32_t B, int32_t n_pages, int32_t* lengths, int32_t* pool, int32_t* pool_state, cudaStream_t s) {

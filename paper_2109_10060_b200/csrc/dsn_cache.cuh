@@ -9,7 +9,7 @@ __host__ __device__ constexpr uint32_t dsn_cache_block_bytes(int D) { return 18u
 
 struct CachePlanParams {
   int32_t B, R, page, n_pages, max_pages;
-  FastDiv by_page;
+  FastDiv by_page, by_R;
   const int32_t* new_tokens;
   const int32_t* lengths;
   const int32_t* pool_state;
