@@ -432,7 +432,7 @@ def cache_round(x):
 
     The stored pair and the codes are defined by operations in fp32 and bf16, each rounded once; those roundings are mirrored."""
     f = np.float32
-    v = np.asarray(x, dtype=F64).reshape(*np.shape(x)[:-1], -1, 64)
+    v = np.asarray(x, dtype=F64).reshape(*np.shape(x)[:-1], np.shape(x)[-1] // 64, 64)
     lo, hi = v.min(-1), v.max(-1)
     def rf(a):
         with np.errstate(over="ignore"):          # x - middle of the widest groups: an infinity, which the ends hold
