@@ -6,7 +6,7 @@
 // Roles (512 threads):
 //   warps 0-4    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, four buffers each.  A unit is K or V of a block of 16
 //                tokens, two lanes a token.  Every element is made once for 256 rows.
-//   warp 5       loader: pages' numbers, and the blocks as bulk copies into two slots of a tile.
+//   warp 5       loader: pages' numbers, the blocks as bulk copies into two slots of a tile, and the tile's powers of two (see below).
 //   warps 6-7    issue, one a half: S_h = Q_h K^T and O_h += P_h V.  S has two buffers a half: a half's product of scores runs a tile ahead, so its softmax
 //                never waits for it.  (One warp for both spends more time on barriers than the products take.)
 //   warps 8-11   softmax of half 0, warps 12-15 of half 1: a thread a row (= TMEM lane), the tile's row of S in registers; maximum, exp2, sum, probabilities over the columns of S, from where the second product takes them.  They also fetch the
@@ -163,12 +163,12 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   uint8_t* smem = smem_raw + (base - raw);
   // barriers: [2 halves] of q and o_empty, [4 stages] of k and v, [2 slots] of raw, [2 halves][2 buffers] of s, p, o
   const uint32_t q_full = base, o_empty = base + 16, k_full = base + 32, k_empty = base + 64, v_full = base + 96, v_empty = base + 128,
-                 raw_full = base + 160, raw_empty = base + 176, s_full = base + 192, p_full = base + 224, o_full = base + 256;
+                 raw_full = base + 160, raw_empty = base + 176, raw_ready = base + 304, s_full = base + 192, p_full = base + 224, o_full = base + 256;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 288);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 292);
-  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there, bit 4 + b: its page is outside the cache; tokens << 8
-  uint8_t* s_bad = smem + 320;                                                     // [8 tiles]: bit b: block b is of a page outside the cache
-  float2* s_fac = reinterpret_cast<float2*>(smem + 384);                           // [8 tiles]: K's power of two; V's, as its exponent
+  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there; tokens << 8; exponents that K and V are divided by << 16, << 24
+  uint8_t* s_bad = smem + 320;                                                     // [16 tiles]: bit b: block b is of a page outside the cache
+  float2* s_fac = reinterpret_cast<float2*>(smem + 384);                           // [16 tiles]: K's power of two; V's, as its exponent
   uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 640);
   CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem + 1024);
   static_assert(1024 + kListSmem * sizeof(CacheEntry) <= kCtrlR, "control block");
@@ -183,6 +183,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       mbar_init(o_empty + 8 * i, 4);
       mbar_init(raw_full + 8 * i, 1);
       mbar_init(raw_empty + 8 * i, 8);
+      mbar_init(raw_ready + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(k_full + 8 * i, 4);   // units of 16 tokens
@@ -233,45 +234,22 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     const uint32_t units = 8u * (uint32_t)(stretch.Z - stretch.A);
     const uint32_t k1024 = opaque_1024();
     const int tok = lane & 15, part = lane >> 4;      // D = 128: a lane takes a group; D = 64: half of it
-    // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers; every unit finds it anew from the tile's pairs
-    auto exponent = [&](uint32_t slot, uint32_t info, bool of_v) -> uint32_t {
-      uint32_t e = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int t = lane + 32 * i;
-        const bool there = (info >> (t >> 4) & 1u) && t < (int)(info >> 8);
-#pragma unroll
-        for (int gr = 0; gr < GR; ++gr) {
-          const uint32_t pr = lds32(slot + (uint32_t)(t >> 4) * kBlock + (of_v ? kBlock / 2 : 0u) + GR * 512 + gr * 64 + (t & 15) * 4);
-          const float top = fabsf(hi_bf16(pr)) + 8.f * fabsf(lo_bf16(pr));
-          if (there && top <= 3.4e38f) e = max(e, __float_as_uint(top) >> 23);
-        }
-      }
-      return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
-    };
 #pragma unroll 1
     for (uint32_t unit = (uint32_t)warp; unit < units; unit += kValueWarps) {
       const uint32_t i = unit >> 3, s = i % kStages, b = unit & 3u;
       const bool is_v = (unit & 4u) != 0;
-      if (!warp_wait(raw_full + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
+      if (!warp_wait(raw_ready + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
       const uint32_t info = *reinterpret_cast<const volatile uint32_t*>(s_raw + (i & 1u));
-      const bool there = (info >> b & 1u) && (int)(b * 16u) + tok < (int)(info >> 8);
+      const bool there = (info >> b & 1u) && b * 16u + (uint32_t)tok < (info >> 8 & 0xffu);
       const uint32_t slot = raw_at + (i & 1u) * kSlot, src = slot + b * kBlock + (is_v ? kBlock / 2 : 0u);
       uint32_t pair = there ? lds32(src + GR * 512u + (GR == 2 ? (uint32_t)part * 64u : 0u) + (uint32_t)tok * 4u) : 0u;
       // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
       if (is_v && (!(fabsf(lo_bf16(pair)) <= 3.4e38f) || !(fabsf(hi_bf16(pair)) <= 3.4e38f))) pair = 0u;
-      const uint32_t e = exponent(slot, info, is_v);
+      const uint32_t e = is_v ? info >> 24 : info >> 16 & 0xffu;
       uint32_t q[GR][4];
 #pragma unroll
       for (int x = 0; x < GR; ++x) lds128(src + (GR == 2 ? (uint32_t)(part * 512 + tok * 32 + 16 * x) : (uint32_t)(tok * 32 + 16 * part)), q[x]);
       if (i >= kStages && !warp_wait((is_v ? v_empty : k_empty) + 8 * s, (i / kStages - 1u) & 1u, abort_flag, p.status, 81)) break;
-      if ((unit & 7u) == 0) {
-        const uint32_t ve = exponent(slot, info, true);
-        if (lane == 0) {
-          s_bad[i & 7u] = (uint8_t)(info >> 4 & 15u);
-          s_fac[i & 7u] = make_float2(__uint_as_float(e << 23), (float)((int)ve - 127));
-        }
-      }
       const float down = __uint_as_float((254u - e) << 23);
       const __half2 s2 = __float2half2_rn(lo_bf16(pair) * down), z2 = __float2half2_rn(hi_bf16(pair) * down);
       const uint32_t dst = (is_v ? v_at : k_at) + s * kStage + (b * 16u + (uint32_t)tok) * 128u + (GR == 2 ? (uint32_t)part * (kTileBytes / 2) : 0u);
@@ -314,6 +292,22 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         place = key / DSN_CACHE_BLOCK - col * bpp;
       }
     };
+    // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers
+    auto exponent = [&](uint32_t slot, uint32_t go, uint32_t left, bool of_v) -> uint32_t {
+      uint32_t e = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int t = lane + 32 * i;
+        const bool there = (go >> (t >> 4) & 1u) && t < (int)left;
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr) {
+          const uint32_t pr = lds32(slot + (uint32_t)(t >> 4) * kBlock + (of_v ? kBlock / 2 : 0u) + GR * 512 + gr * 64 + (t & 15) * 4);
+          const float top = fabsf(hi_bf16(pr)) + 8.f * fabsf(lo_bf16(pr));
+          if (there && top <= 3.4e38f) e = max(e, __float_as_uint(top) >> 23);
+        }
+      }
+      return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
+    };
     uint32_t i = 0;
     find();
     for (; more; ++i) {
@@ -323,19 +317,28 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (lost) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, it.e.sample);
       const uint32_t go = __ballot_sync(0xffffffffu, ok), bad = __ballot_sync(0xffffffffu, lost);
       if (lane == 0) {
-        const int left = min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile), 0), kTile);
-        *reinterpret_cast<volatile uint32_t*>(s_raw + slot) = go | (bad << 4) | ((uint32_t)left << 8);
         mbar_expect_tx(raw_full + 8 * slot, (uint32_t)__popc(go) * kBlock);
       }
       __syncwarp();
       if (ok)
         dsn_bulk_load(raw_at + slot * kSlot + (uint32_t)lane * kBlock, p.pages + (((int64_t)pg * p.H + it.head) * bpp + place) * kBlock, kBlock,
                       raw_full + 8 * slot);
+      const uint32_t left = (uint32_t)min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile), 0), kTile);
       if (++tile == it.c1) {
         more = walk.next(p, it);
         tile = it.c0;
       }
       find();
+      // what the tile's K and V are divided by, from their pairs
+      if (!warp_wait(raw_full + 8 * slot, (i >> 1) & 1u, abort_flag, p.status, 93)) break;
+      const uint32_t ke = exponent(raw_at + slot * kSlot, go, left, false), ve = exponent(raw_at + slot * kSlot, go, left, true);
+      if (lane == 0) {
+        s_bad[i & 15u] = (uint8_t)bad;
+        s_fac[i & 15u] = make_float2(__uint_as_float(ke << 23), (float)((int)ve - 127));
+        *reinterpret_cast<volatile uint32_t*>(s_raw + slot) = go | left << 8 | ke << 16 | ve << 24;
+        mbar_arrive(raw_ready + 8 * slot);
+      }
+      __syncwarp();
     }
     if (*abort_flag) dsn_drain(raw_full, 2, i > 2 ? (int)i - 2 : 0, (int)i);
   } else if (warp < kSoftWarp) {
@@ -504,7 +507,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         tc_fence_after();
         if (j + 1 == b && na < nb) up_next = load_q(nx);   // every product with this item's Q has run
         const uint32_t at = region + kTile * buf;
-        const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 7u;
+        const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 15u;
         const uint32_t bad = *reinterpret_cast<const volatile uint8_t*>(s_bad + nt);
         // scores to units of the exponent (not 0: what is hidden is -infinity), V's power of two
         const float2 fac = s_fac[nt];

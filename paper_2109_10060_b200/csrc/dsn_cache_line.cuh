@@ -11,11 +11,24 @@ namespace dsn_q4 {
 constexpr int kListSmem = 64;      // requests that a CTA keeps in shared memory; further ones are read from the workspace
 constexpr float kLowest = -1e38f;  // reference before any score: finite, so that differences are
 
+// One look at a barrier that may put the thread to sleep for up to 20 us until the phase ends: a warp that only looks again and again takes issue slots from
+// those that work (a third of all instructions of the many-rows kernel).
+__device__ __forceinline__ bool patient_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(20000u)
+      : "memory");
+  return ok != 0;
+}
 // Bounded wait of a whole warp, whose lanes all get the same answer: a wait that runs out while the barrier completes must not part them.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, int32_t* status, int where) {
 #pragma unroll 1
   for (int i = 0; i < 64; ++i)
-    if (__all_sync(0xffffffffu, dsn_gemm::mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, patient_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, dsn_gemm::mbar_wait_slow(bar, parity, abort_flag, status, where));
 }
 
