@@ -506,6 +506,13 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         if (!ok) break;
         tc_fence_after();
         if (j + 1 == b && na < nb) up_next = load_q(nx);   // every product with this item's Q has run
+        if (first_me == INT32_MAX) {   // rows that do not exist: whatever stands in their lanes stays there
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + 16 * h + 8 * buf);
+          ++m;
+          continue;
+        }
         const uint32_t at = region + kTile * buf;
         const uint32_t nt = (n + (uint32_t)(j - it.c0)) & 15u;
         const uint32_t bad = *reinterpret_cast<const volatile uint8_t*>(s_bad + nt);
