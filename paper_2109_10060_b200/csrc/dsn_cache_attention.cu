@@ -1,4 +1,4 @@
-// Attention over the 4-bit cache, a few query vectors a head (rows * group <= 16: single tokens, shared heads, a few tokens at once).
+// Attention over the 4-bit cache, a few query vectors a head (rows * group <= 32: single tokens, shared heads, a few tokens at once).
 //
 // Bound by memory: a cached token is 18 D / 16 bytes a head, read once for all query vectors of the head.  Work is dealt out in steps (32 tokens of 128
 // elements, 64 of 64): all steps of all (request, head) items stand in one line, and every warp of the GPU gets an equal stretch of it, so neither few
@@ -104,11 +104,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
 
+  // 17 to 32 query vectors of a head are two items of up to 16, next to each other in the line
+  auto halves = [&](int rows) -> int { return NT == 2 && rows * p.group > NC; };
   const Stretch stretch = find_stretch<THREADS>(p, s_list, s_scan, WARPS, [&](int len, int rows) {
     int lo, hi;
     item_range(len, rows, p.window, lo, hi);
     return max(1, (hi - lo + 256 / D * DSN_CACHE_BLOCK - 1) / (256 / D * DSN_CACHE_BLOCK));   // a request without tokens: a step that sees nothing, for the zeros
-  });
+  }, [&](int rows) { return 1 << halves(rows); });
   const uint64_t A = stretch.A, Z = stretch.Z;
   const uint64_t u0 = A + dsn_share(Z - A, warp, WARPS), u1 = A + dsn_share(Z - A, warp + 1, WARPS);
   int head_state = 3, tail = 0, head_far = 0;
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     __syncwarp();
     if (begins >> lane & 1u) {
       const uint32_t stops = (~there | begins) >> lane >> 1;   // where this run of blocks ends
-      dsn_bulk_load(ring + (uint32_t)slot * slot_bytes<D>() + (uint32_t)lane * kBlock, p.pages + (uint64_t)(uint32_t)pg * page_bytes + (uint32_t)(fetch.head * bpp + place) * kBlock,
+      dsn_bulk_load(ring + (uint32_t)slot * slot_bytes<D>() + (uint32_t)lane * kBlock, p.pages + (uint64_t)(uint32_t)pg * page_bytes + (uint32_t)((fetch.head >> halves(fetch.e.rows)) * bpp + place) * kBlock,
                     (uint32_t)__ffs(stops) * kBlock, bars + 8u * slot);
     }
     return there;
@@ -203,14 +205,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   int sub = 0;   // step of the slot
   for (int i = 0; i < n_steps; ++i) {
     const CacheEntry& e = work.e;
-    const int cols = e.rows * p.group;
+    const int two = halves(e.rows), kv = work.head >> two, v0 = two ? NC * (work.head & 1) : 0;   // head of k and v, first query vector of the item
+    const int cols = min(e.rows * p.group - v0, NC);
     const int64_t row0 = (int64_t)(p.grouped ? e.pos : e.sample) * p.R;
     if (fresh) {
       fresh = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int v = nt * 8 + g, r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
-        const __nv_bfloat16* q = p.qkv + (row0 + r) * p.ld_qkv + ((int64_t)work.head * (p.group + 2) + ev) * D;
+        const int v = nt * 8 + g, r = (int)dsn_div((uint32_t)(v0 + v), p.by_group), ev = v0 + v - r * p.group;
+        const __nv_bfloat16* q = p.qkv + (row0 + r) * p.ld_qkv + ((int64_t)kv * (p.group + 2) + ev) * D;
         uint4 w[GR][2];
         uint32_t top = 0;
 #pragma unroll
@@ -267,8 +270,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         }
         l[nt][0] = l[nt][1] = 0.f;
         ref[nt][0] = ref[nt][1] = kLowest;
-        row_of[nt][0] = (int)dsn_div((uint32_t)(nt * 8 + 2 * t), p.by_group);
-        row_of[nt][1] = (int)dsn_div((uint32_t)(nt * 8 + 2 * t + 1), p.by_group);
+        row_of[nt][0] = (int)dsn_div((uint32_t)(v0 + nt * 8 + 2 * t), p.by_group);
+        row_of[nt][1] = (int)dsn_div((uint32_t)(v0 + nt * 8 + 2 * t + 1), p.by_group);
       }
     }
     int lo, hi;
@@ -460,7 +463,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
           sum += __shfl_xor_sync(0xffffffffu, sum, 16);
           const int v = nt * 8 + 2 * t + c;
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          const int r = row_of[nt][c], ev = v - r * p.group;
+          const int r = row_of[nt][c], ev = v0 + v - r * p.group;
 #pragma unroll
           for (int gr = 0; gr < GR; ++gr) {
             float z = oz[nt][gr][c];
@@ -480,7 +483,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
                 w.y = pack_bf16(y[2] * inv, y[3] * inv);
                 w.z = pack_bf16(y[4] * inv, y[5] * inv);
                 w.w = pack_bf16(y[6] * inv, y[7] * inv);
-                *reinterpret_cast<uint4*>(p.out + (row0 + r) * p.ld_out + ((int64_t)work.head * p.group + ev) * D + gr * 64 + 8 * g) = w;
+                *reinterpret_cast<uint4*>(p.out + (row0 + r) * p.ld_out + ((int64_t)kv * p.group + ev) * D + gr * 64 + 8 * g) = w;
               } else {
                 float4* d4 = reinterpret_cast<float4*>(dst + 2 * NC + v * D + gr * 64 + 8 * g);
                 d4[0] = make_float4(y[0], y[1], y[2], y[3]);
@@ -534,7 +537,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     const uint32_t heads = heads_of(a);
     const bool closed = (heads & closes) != 0;
     if (a >= 0 && !closed) cta_tail = 1, tail_warp = a;
-    const int cols = a >= 0 ? s_part[a].rows * p.group : NC;
+    const int two = a >= 0 ? halves(s_part[a].rows) : 0, v0 = two ? NC * (s_part[a].head & 1) : 0;
+    const int cols = a >= 0 ? min(s_part[a].rows * p.group - v0, NC) : NC;
     const bool in = (heads >> lane & 1u) || lane == a;   // lane j: the part of warp j
     const float* src = in ? part_of(lane, lane == a) : nullptr;
     const int begin = (warp + WARPS - task % WARPS) % WARPS;
@@ -567,9 +571,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
       }
       if (a >= 0 && closed) {
         const CachePart& q = s_part[a];
-        const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
+        const int r = (int)dsn_div((uint32_t)(v0 + v), p.by_group), ev = v0 + v - r * p.group;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? q.pos : q.sample) * p.R + r) * p.ld_out + ((int64_t)q.head * p.group + ev) * D;
+        __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? q.pos : q.sample) * p.R + r) * p.ld_out + ((int64_t)(q.head >> two) * p.group + ev) * D;
         if constexpr (D == 128)
           *reinterpret_cast<uint2*>(dst + 4 * lane) = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
         else
@@ -604,7 +608,8 @@ __global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant
   dsn_grid_launch_dependents();
   const int tid = threadIdx.x, w = blockIdx.x, v = blockIdx.y, kPart = NC * (D + 2);
   const CachePart part = p.parts[w];
-  if (!part.tail || v >= part.rows * p.group) return;
+  const int two = NC == 16 && part.rows * p.group > NC, v0 = two ? NC * (part.head & 1) : 0;
+  if (!part.tail || v >= min(part.rows * p.group - v0, NC)) return;
   if (tid == 0) s_end = ctas - 1;
   __syncthreads();
   for (int b = w + 1 + tid; b < ctas; b += 2 * D)
@@ -648,9 +653,9 @@ __global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant
     o.x += q.x; o.y += q.y; o.z += q.z; o.w += q.w;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int r = v / p.group, ev = v - r * p.group;
+  const int r = (v0 + v) / p.group, ev = v0 + v - r * p.group;
   const int64_t row = (int64_t)(p.grouped ? part.pos : part.sample) * p.R + r;
-  *reinterpret_cast<uint2*>(p.out + row * p.ld_out + ((int64_t)part.head * p.group + ev) * D + 4 * sub) =
+  *reinterpret_cast<uint2*>(p.out + row * p.ld_out + ((int64_t)(part.head >> two) * p.group + ev) * D + 4 * sub) =
       make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
 
@@ -664,7 +669,7 @@ cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = dsn_launch(kernel, dim3((unsigned)ctas), dim3(WARPS * 32), smem, s, 1, p);
   if (e != cudaSuccess) return e;
-  return dsn_launch(cache_join_kernel<D>, dim3((unsigned)ctas, (unsigned)(p.R * p.group)), dim3(2 * D), 0, s, 1, p, ctas, 8 * NT);
+  return dsn_launch(cache_join_kernel<D>, dim3((unsigned)ctas, (unsigned)(p.R * p.group < 8 * NT ? p.R * p.group : 8 * NT)), dim3(2 * D), 0, s, 1, p, ctas, 8 * NT);
 }
 
 constexpr int kWarps1 = 12, kWarps2 = 8;   // warps a CTA for up to 8 and up to 16 query vectors a head: their products stay in registers (16 and 8 warps: 132 and 144 us, 12: 128)
@@ -686,7 +691,7 @@ static CacheWorkspace carve(int D, int cols, int64_t B, int ctas) {
   return w;
 }
 
-size_t dsn_cache_attention_ws_bytes(int D, int cols, int64_t B) { return cols > 16 ? 0 : carve(D, cols, B, DSN_CACHE_MAX_CTAS).total; }
+size_t dsn_cache_attention_ws_bytes(int D, int cols, int64_t B) { return carve(D, cols, B, DSN_CACHE_MAX_CTAS).total; }
 
 cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s) {
   const int cols = p.R * p.group, ctas = sm_count < DSN_CACHE_MAX_CTAS ? sm_count : DSN_CACHE_MAX_CTAS;

@@ -1,4 +1,4 @@
-// Attention over the 4-bit cache, many query vectors a head (rows * group > 16: prompts, pieces of prompts), on tcgen05.
+// Attention over the 4-bit cache, many query vectors a head (rows * group > 32: prompts, pieces of prompts), on tcgen05.
 //
 // One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 64; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
@@ -197,7 +197,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, 1u, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.by_group, p.window); });
+  const Stretch stretch = find_stretch<kThreadsR>(p, s_list, s_scan, 1u, [&](int len, int rows) { return head_tiles(len, rows, p.group, p.by_group, p.window); },
+                                                     [](int) { return 1; });
   if (warp == kIssueWarp) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();

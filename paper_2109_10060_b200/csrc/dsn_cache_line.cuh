@@ -119,9 +119,10 @@ __device__ __forceinline__ uint64_t dsn_share(uint64_t total, uint32_t i, uint32
   return (uint64_t)q * i + min(i, r);
 }
 
-// One request's place in the line: what it needs to know and how many steps each of its heads makes, steps(len, rows).
-template <typename Steps>
-__device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, bool report, Steps steps) {
+// One request's place in the line: what it needs to know, the items it has (its heads, pieces(rows) times each) and how many steps each of them makes,
+// steps(len, rows).
+template <typename Steps, typename Pieces>
+__device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, bool report, Steps steps, Pieces pieces) {
   const PosInfo at = dsn_locate_lanes(pos, p.B, p.G, p.T, p.offsets, p.perm, p.group_slice);
   CacheEntry e;
   e.first = 0;
@@ -133,7 +134,7 @@ __device__ __forceinline__ CacheEntry look_up(const CacheAttParams& p, int pos, 
   e.rows = min(max(rows, 0), p.R);
   if (report && (len != e.len || rows != e.rows)) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, at.sample);
   if (e.rows == 0) return e;
-  e.heads = p.heads[at.slice];
+  e.heads = p.heads[at.slice] * pieces(e.rows);
   e.steps = steps(e.len, e.rows);
   return e;
 }
@@ -143,18 +144,18 @@ struct Stretch {
   uint64_t A, Z;
   int first_order, count;
 };
-template <int THREADS, typename Steps>
-__device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEntry* s_list, uint64_t* s_scan, uint32_t workers, Steps steps) {
+template <int THREADS, typename Steps, typename Pieces>
+__device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEntry* s_list, uint64_t* s_scan, uint32_t workers, Steps steps, Pieces pieces) {
   __shared__ int s_first_order, s_count;
   const int tid = threadIdx.x;
   if (tid == 0) s_first_order = 0, s_count = 0;
-  const CacheEntry e0 = look_up(p, tid, blockIdx.x == 0, steps);
+  const CacheEntry e0 = look_up(p, tid, blockIdx.x == 0, steps, pieces);
   uint64_t sum0, first0 = (uint64_t)e0.heads * e0.steps;
   uint32_t ones0, order0 = e0.heads > 0;
   block_scan<THREADS>(first0, order0, s_scan, sum0, ones0);
   uint64_t total = sum0;
   for (int b = THREADS; b < p.B; b += THREADS) {
-    const CacheEntry e = look_up(p, b + tid, blockIdx.x == 0, steps);
+    const CacheEntry e = look_up(p, b + tid, blockIdx.x == 0, steps, pieces);
     uint64_t sum, first = (uint64_t)e.heads * e.steps;
     uint32_t ones, order = e.heads > 0;
     block_scan<THREADS>(first, order, s_scan, sum, ones);
@@ -172,7 +173,7 @@ __device__ __forceinline__ Stretch find_stretch(const CacheAttParams& p, CacheEn
     uint64_t first = first0, sum = sum0;
     uint32_t order = order0, ones = ones0;
     if (b > 0) {
-      e = look_up(p, b + tid, false, steps);
+      e = look_up(p, b + tid, false, steps, pieces);
       first = (uint64_t)e.heads * e.steps;
       order = e.heads > 0;
       block_scan<THREADS>(first, order, s_scan, sum, ones);

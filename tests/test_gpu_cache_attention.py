@@ -77,6 +77,10 @@ CASES = [
     (128, 1, 7, 32, [1], 1, "input", [3, 64, 1025], None),
     (128, 1, 16, 256, [1], 1, "grouped", [300, 31, 2000], None),
     (64, 1, 64, 16, [1], 2, "input", [300, 2, 90], None),
+    (128, 2, 16, 16, [1, 2], 2, "grouped", [300, 2, 2000, 31, 65], [2, 2, 1, 2, 0]),   # 32 query vectors a head, or 16, or none
+    (64, 3, 17, 32, [3], 1, "input", [1, 64, 129, 5000], None),
+    (128, 1, 1, 16, [1], 32, "grouped", [32, 1000, 40], [32, 17, 16]),
+    (64, 2, 11, 16, [2], 3, "input", [700, 3], None),                                  # 33
     (64, 4, 2, 32, [2, 4], 5, "grouped", [5, 40, 700, 64, 12], [5, 3, 5, 0, 1]),
     (128, 2, 3, 16, [2], 9, "input", [9, 100, 1000], [9, 9, 2]),
     (128, 1, 1, 1024, [1], 33, "input", [33, 3000, 100], [33, 33, 7]),
