@@ -3,6 +3,11 @@
 // One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 64; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
 // rows (fp32) in the workspace, and a second kernel joins them.
+// Measured (in a graph): 2 requests of 4096 rows behind nothing, 8 heads of 128, 4 queries a head: 482 us, 570 TFLOP/s of the visible pairs, where products at a
+// plain matrix product's rate would take 170.  What bounds it is the softmax: some 3,000 cycles a tile of 64 tokens and warp, half of them the exponentials (16
+// cycles an instruction of a warp), the rest the trip through TMEM; eight warps of 128 registers are all that fit, and the tensor pipe is busy a quarter of the time.
+// Tried: 128 tokens a tile with one S buffer 491 us, two threads a row 709, more registers for the softmax warps 507 to 550, a part of the exponentials as
+// polynomials within 3 %.
 // Roles (512 threads):
 //   warps 0-4    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, four buffers each.  A unit is K or V of a block of 16
 //                tokens, two lanes a token.  Every element is made once for 256 rows.
@@ -293,7 +298,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         place = key / DSN_CACHE_BLOCK - col * bpp;
       }
     };
-    // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers
+    // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers; V's from 2^-50 up: fp32 holds the probabilities and
+    // their sums without the power, too
     auto exponent = [&](uint32_t slot, uint32_t go, uint32_t left, bool of_v) -> uint32_t {
       uint32_t e = 0;
 #pragma unroll
@@ -307,7 +313,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
           if (there && top <= 3.4e38f) e = max(e, __float_as_uint(top) >> 23);
         }
       }
-      return min(max(__reduce_max_sync(0xffffffffu, e), 27u), 253u);
+      return min(max(__reduce_max_sync(0xffffffffu, e), of_v ? 77u : 27u), 253u);
     };
     uint32_t i = 0;
     find();
@@ -546,9 +552,9 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         const float need = fmaf(max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]), t, sh);
         if (need != need) l = need;   // a token that is not finite: so is the row
         if (__any_sync(0xffffffffu, need > ref + kTop)) {
-          const float to = fmaxf(ref, need - kAim), f = ex2(ref - to);
+          const float to = fmaxf(ref, need - kAim), f = ex2(0.5f * (ref - to));   // twice: references can lie further apart than fp32 reaches
           ref = to;
-          l *= f;
+          l = l * f * f;
           if (j > a) {
             ok = warp_wait(o_full + 16 * h + 8 * (buf ^ 1u), ((m - 1u) >> 1) & 1u, abort_flag, p.status, 89);
             if (!ok) break;
@@ -559,7 +565,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
               tmem_ld_8(region + kOCol + c, y);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+              for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f * f);
               tmem_st_8(region + kOCol + c, y);
             }
           }
@@ -687,11 +693,11 @@ __global__ void __launch_bounds__(kRows) cache_rows_join_kernel(const __grid_con
     const float* src = p.cta_data + ((int64_t)j * 2 + (j == w)) * (kRows * (D + 2));
     const float4 q0 = *reinterpret_cast<const float4*>(src + 2 * kRows + (int64_t)(c / 4) * (4 * kRows) + 4 * i);
     const float4 q1 = *reinterpret_cast<const float4*>(src + 2 * kRows + (int64_t)(c / 4 + 1) * (4 * kRows) + 4 * i);
-    const float mj = src[i], lj = src[kRows + i], m2 = fmaxf(m, mj), fa = ex2(m - m2), fb = ex2(mj - m2);
+    const float mj = src[i], lj = src[kRows + i], m2 = fmaxf(m, mj), fa = ex2(0.5f * (m - m2)), fb = ex2(0.5f * (mj - m2));   // twice, as above
     m = m2;
-    l = l * fa + lj * fb;
-    y[0] = y[0] * fa + q0.x * fb; y[1] = y[1] * fa + q0.y * fb; y[2] = y[2] * fa + q0.z * fb; y[3] = y[3] * fa + q0.w * fb;
-    y[4] = y[4] * fa + q1.x * fb; y[5] = y[5] * fa + q1.y * fb; y[6] = y[6] * fa + q1.z * fb; y[7] = y[7] * fa + q1.w * fb;
+    l = l * fa * fa + lj * fb * fb;
+    y[0] = y[0] * fa * fa + q0.x * fb * fb; y[1] = y[1] * fa * fa + q0.y * fb * fb; y[2] = y[2] * fa * fa + q0.z * fb * fb; y[3] = y[3] * fa * fa + q0.w * fb * fb;
+    y[4] = y[4] * fa * fa + q1.x * fb * fb; y[5] = y[5] * fa * fa + q1.y * fb * fb; y[6] = y[6] * fa * fa + q1.z * fb * fb; y[7] = y[7] * fa * fa + q1.w * fb * fb;
   }
   const int r = v / p.group, ev = v - r * p.group;
   const float inv = l == 0.f ? 0.f : 1.f / l;

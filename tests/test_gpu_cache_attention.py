@@ -146,6 +146,29 @@ def test_scores_of_every_size(dsn, gain, D, R, group):
         compare(pages, [2], group, [0, 0, 0], R, None, x, got)
 
 
+@pytest.mark.parametrize("size", ["small", "large", "both", "constant"])
+@pytest.mark.parametrize("D,R,group", [(64, 1, 1), (128, 1, 4), (128, 5, 4), (128, 150, 1)])
+def test_values_of_every_size(dsn, size, D, R, group):
+    """Magnitudes of v from 1e-14 to 1e33.  In "both" the small ones come first, and the large ones show whether their share of the sum is kept."""
+    g = np.random.default_rng(15)
+    lengths = [3000, 1000, 160]
+    pages = Pages(g, lengths, 2, D, 16)
+    s, z = pages.s[:, :, :, 1], pages.z[:, :, :, 1]
+    gain = np.full(s.shape, {"small": 2.0 ** -44, "large": 2.0 ** 108, "both": 2.0 ** 108, "constant": 1.0}[size])
+    for i, L in enumerate(lengths):
+        for t in range(L):
+            pg, at = pages.table[i, t // 16], t % 16
+            if size == "both" and t < L // 128 * 64:              # tokens that share a power are alike
+                gain[pg, :, at] = 2.0 ** -44
+            if size == "constant" and t % 3 == 0:                # a group of one value has scale 0
+                s[pg, :, at], z[pg, :, at] = 0.0, 2.0 ** 100
+    s *= gain
+    z *= gain
+    x, got, status = attend(dsn, g, pages, [2], group, [0, 0, 0], R, None)
+    assert status[0] == 0 and np.all(np.isfinite(got))
+    compare(pages, [2], group, [0, 0, 0], R, None, x, got)
+
+
 @pytest.mark.parametrize("scale", [-0.5, 1e-6])
 def test_other_scales(dsn, scale):
     g = np.random.default_rng(6)
