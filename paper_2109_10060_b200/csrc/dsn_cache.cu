@@ -3,6 +3,11 @@
 
 namespace {
 
+using dsn_gemm::fadd2;
+using dsn_gemm::ffma2;
+using dsn_gemm::pack2;
+using dsn_gemm::unpack2;
+
 // ------------------------------------------------------------------------------------------------ plan
 // One cluster of CTAs (one CTA for few rows); every CTA scans all requests on its own (8 bytes each), one a thread and THREADS at a time, and then the threads of
 // the cluster share the slots.  A slot needs no other thread's result: a token's page stands in the table already or
@@ -219,6 +224,11 @@ __global__ void __launch_bounds__(256) cache_reset_kernel(int32_t B, int32_t n_p
 // Bound by instructions once memory is busy: least and greatest value go through the shuffles as one pair of bf16 numbers (the least, minus the greatest);
 // a code comes out of an addition that rounds (1.5 * 2^23 + 8: its low four bits are the code), eight of them are put together by multiply-adds.
 // Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 28.5 us, 4 x 4096 rows of 8 heads of 128 with values 34.9 (floors 10.6 and 23.3 at a copy's rate); one row 2.2.
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 template <int D, bool VALUES>
 __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
   constexpr int LPH = D / 4;             // lanes a head
@@ -277,20 +287,23 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
         float s = __bfloat162float(__float2bfloat16_rn(__fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))));
         if (s < 1.17549435e-38f) s = 0.f;
         float z = __bfloat162float(__float2bfloat16_rn(2.f * __fadd_rn(0.5f * lo, 4.f * s)));
-        const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+        float inv = s > 0.f ? __frcp_rn(s) : 0.f, from = -z;                   // s = 0: all differences are finite, all codes 8
         if (poison) {
-          s = 0.f;
+          s = inv = from = 0.f;
           z = __uint_as_float(0x7fc00000u);
         }
         constexpr float magic = 12582920.f;   // 1.5 * 2^23 + 8
-        float step[8];
+        const uint64_t from_2 = pack2(from, from), inv_2 = pack2(inv, inv), magic_2 = pack2(magic, magic);
+        uint64_t step[4];
         uint32_t code = 0;
 #pragma unroll
-        for (int j = 7; j >= 0; --j) {
-          const float v = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-          const float q = __fmul_rn(__fsub_rn(v, z), inv);                     // what the ends cut off may be an infinity; s = 0: NaN, 0
-          step[j] = __fadd_rn(fminf(fmaxf(s > 0.f ? q : 0.f, -8.f), 7.f), magic);
-          code = code * 16u + __float_as_uint(step[j]);
+        for (int j = 3; j >= 0; --j) {
+          const uint32_t v = poison ? 0u : w[j];
+          float q0, q1;
+          unpack2(fmul2(fadd2(pack2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)), from_2), inv_2), q0, q1);   // what the ends cut off may be an infinity
+          step[j] = fadd2(pack2(fminf(fmaxf(q0, -8.f), 7.f), fminf(fmaxf(q1, -8.f), 7.f)), magic_2);
+          unpack2(step[j], q0, q1);
+          code = (code * 16u + __float_as_uint(q1)) * 16u + __float_as_uint(q0);
         }
         code -= 0x4b400000u * 0x11111111u;                                     // the eight exponents' share
         if (head < heads) {
@@ -303,7 +316,9 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
             uint32_t val[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const __nv_bfloat162 y = __floats2bfloat162_rn(fmaf(s, step[2 * j] - magic, z), fmaf(s, step[2 * j + 1] - magic, z));
+              float y0, y1;
+              unpack2(ffma2(pack2(s, s), fadd2(step[j], pack2(-magic, -magic)), pack2(z, z)), y0, y1);
+              const __nv_bfloat162 y = __floats2bfloat162_rn(y0, y1);
               val[j] = *reinterpret_cast<const uint32_t*>(&y);
             }
             *reinterpret_cast<uint4*>(p.values + xrow * p.ld_values + (int64_t)head * 2 * D + sub * 8) = make_uint4(val[0], val[1], val[2], val[3]);
