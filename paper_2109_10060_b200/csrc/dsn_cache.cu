@@ -237,7 +237,6 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % LPH;
-  const int chunks = (p.max_heads + HPW - 1) / HPW;
   const int half = sub / (D / 8), grp = (sub % (D / 8)) >> 3, word = sub & 7;
   const int64_t items = (int64_t)p.B * p.R * p.split, warps = (int64_t)gridDim.x * 8;
   for (int64_t it = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); it < items; it += warps) {
@@ -252,7 +251,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
       if (lane == 0) dsn_set_status(p.status, DSN_ERR_BAD_INDEX, (int)row);
       continue;
     }
-    const int heads = p.heads[at.slice];
+    const int heads = p.heads[at.slice], chunks = (heads + HPW - 1) / HPW;
     const int64_t xrow = (int64_t)(p.grouped ? pos : at.sample) * p.R + r;
     const __nv_bfloat16* x = p.qkv + xrow * p.ld_qkv + (int64_t)p.group * D + sub * 8;
     const int pg = (int)dsn_div((uint32_t)slot, p.by_page), tok = slot - pg * p.page, t = tok % DSN_CACHE_BLOCK;
