@@ -219,18 +219,22 @@ __global__ void __launch_bounds__(256) cache_reset_kernel(int32_t B, int32_t n_p
 }
 
 // ------------------------------------------------------------------------------------------------ write
-// A lane takes eight elements: 8 lanes a group of 64, 2 D / 8 lanes the k and v of a head, which lie side by side in the row.  A warp takes a row, or every
-// `split`th piece of it where there are few rows, four pieces on their way at a time.
-// Bound by instructions once memory is busy: least and greatest value go through the shuffles as one pair of bf16 numbers (the least, minus the greatest);
-// a code comes out of an addition that rounds (1.5 * 2^23 + 8: its low four bits are the code), eight of them are put together by multiply-adds.
-// Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 28.5 us, 4 x 4096 rows of 8 heads of 128 with values 34.9 (floors 10.6 and 23.3 at a copy's rate); one row 2.2.
 __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+
+constexpr int kWriteWarps = 4, kWriteCtas = 28;   // warps a CTA; CTAs an SM at most (8 are resident): rows differ, and small CTAs in three waves even that out
+                                                  // (by path 22.6 us, 4 x 4096 rows 31.9; 8 warps, 8 CTAs an SM: 26.2, 31.8)
+
+// A lane takes eight elements: 8 lanes a group of 64, 2 D / 8 lanes the k and v of a head, which lie side by side in the row.  A warp takes a row, or every
+// `split`th piece of it where there are few rows, four pieces on their way at a time.
+// Bound by instructions once memory is busy: least and greatest value go through the shuffles as one pair of bf16 numbers (the least, minus the greatest);
+// a code comes out of an addition that rounds (1.5 * 2^23 + 8: its low four bits are the code), eight of them are put together by multiply-adds.
+// Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 22.6 us, 4 x 4096 rows of 8 heads of 128 with values 31.9 (floors 10.6 and 23.3 at a copy's rate); one row 2.2.
 template <int D, bool VALUES>
-__global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
+__global__ void __launch_bounds__(kWriteWarps * 32) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
   constexpr int LPH = D / 4;             // lanes a head
   constexpr int HPW = 32 / LPH;          // heads a warp does at a time
   constexpr int U = 4;
@@ -238,8 +242,8 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
   dsn_grid_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % LPH;
   const int half = sub / (D / 8), grp = (sub % (D / 8)) >> 3, word = sub & 7;
-  const int64_t items = (int64_t)p.B * p.R * p.split, warps = (int64_t)gridDim.x * 8;
-  for (int64_t it = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); it < items; it += warps) {
+  const int64_t items = (int64_t)p.B * p.R * p.split, warps = (int64_t)gridDim.x * kWriteWarps;
+  for (int64_t it = (int64_t)blockIdx.x * kWriteWarps + (threadIdx.x >> 5); it < items; it += warps) {
     const uint32_t row = (uint32_t)(it / p.split);
     const int part = (int)(it - (int64_t)row * p.split);
     const int pos = (int)dsn_div(row, p.by_R), r = (int)(row - (uint32_t)pos * (uint32_t)p.R);
@@ -345,12 +349,12 @@ cudaError_t dsn_launch_cache_reset(int32_t B, int32_t n_pages, int32_t* lengths,
 
 cudaError_t dsn_launch_cache_write(CacheWriteParams& p, int sm_count, cudaStream_t s) {
   const int hpw = p.D == 64 ? 2 : 1, chunks = (p.max_heads + hpw - 1) / hpw;
-  const int64_t rows = (int64_t)p.B * p.R, most = (int64_t)sm_count * 8;
+  const int64_t rows = (int64_t)p.B * p.R, most = (int64_t)sm_count * kWriteCtas;
   // few rows: as many warps a row as fill the GPU, up to one a piece
-  int64_t split = most * 8 / rows;
+  int64_t split = (int64_t)sm_count * 64 / rows;
   p.split = (int32_t)(split < 1 ? 1 : (split > chunks ? chunks : split));
-  const int64_t ctas = (rows * p.split + 7) / 8;
+  const int64_t ctas = (rows * p.split + kWriteWarps - 1) / kWriteWarps;
   const dim3 grid((unsigned)(ctas < most ? ctas : most));
-  if (p.D == 64) return p.values ? dsn_launch(cache_write_kernel<64, true>, grid, dim3(256), 0, s, 1, p) : dsn_launch(cache_write_kernel<64, false>, grid, dim3(256), 0, s, 1, p);
-  return p.values ? dsn_launch(cache_write_kernel<128, true>, grid, dim3(256), 0, s, 1, p) : dsn_launch(cache_write_kernel<128, false>, grid, dim3(256), 0, s, 1, p);
+  if (p.D == 64) return p.values ? dsn_launch(cache_write_kernel<64, true>, grid, dim3(kWriteWarps * 32), 0, s, 1, p) : dsn_launch(cache_write_kernel<64, false>, grid, dim3(kWriteWarps * 32), 0, s, 1, p);
+  return p.values ? dsn_launch(cache_write_kernel<128, true>, grid, dim3(kWriteWarps * 32), 0, s, 1, p) : dsn_launch(cache_write_kernel<128, false>, grid, dim3(kWriteWarps * 32), 0, s, 1, p);
 }
