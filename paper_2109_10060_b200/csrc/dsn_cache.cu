@@ -274,17 +274,18 @@ __global__ void __launch_bounds__(kWriteWarps * 32) cache_write_kernel(const __g
         if (c0 + u * p.split >= chunks) break;
         const int head = (c0 + u * p.split) * HPW + lane / LPH;
         const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-        const uint32_t mag = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
-        const uint32_t all = __ballot_sync(0xffffffffu, max(mag & 0xffffu, mag >> 16) >= 0x7f80u);   // NaN or infinity
-        const bool poison = (LPH == 32 ? all : (all >> (lane & 16)) & 0xffffu) != 0;
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
-        const __nv_bfloat162 mn = __hmin2(__hmin2(h[0], h[1]), __hmin2(h[2], h[3])), mx = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        __nv_bfloat162 ends = __halves2bfloat162(__hmin(mn.x, mn.y), __hneg(__hmax(mx.x, mx.y)));
+        const __nv_bfloat162 mn = __hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3])),
+                             mx = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        __nv_bfloat162 ends = __halves2bfloat162(__hmin_nan(mn.x, mn.y), __hneg(__hmax_nan(mx.x, mx.y)));
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) {
           const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&ends), o);
-          ends = __hmin2(ends, *reinterpret_cast<const __nv_bfloat162*>(&other));
+          ends = __hmin2_nan(ends, *reinterpret_cast<const __nv_bfloat162*>(&other));
         }
+        const uint32_t size = *reinterpret_cast<const uint32_t*>(&ends) & 0x7fff7fffu;
+        const uint32_t all = __ballot_sync(0xffffffffu, max(size & 0xffffu, size >> 16) >= 0x7f80u);   // NaN or infinity
+        const bool poison = (LPH == 32 ? all : (all >> (lane & 16)) & 0xffffu) != 0;
         const float lo = __bfloat162float(ends.x), hi = -__bfloat162float(ends.y);
         const float fifteenth = 1.0f / 15.0f;
         float s = __bfloat162float(__float2bfloat16_rn(__fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))));
