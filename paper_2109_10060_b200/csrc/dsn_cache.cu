@@ -121,15 +121,14 @@ __global__ void __launch_bounds__(THREADS) cache_plan_kernel(const __grid_consta
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int r = r0 + 128 * j, at = q.held + r - col[j] * p.page;
+          const int r = r0 + 128 * j, at = q.held + r - col[j] * p.page, turn = p.page - at;   // row r + turn is the first in the second page
+          const int n = min(q.placed - r, 4), na = (uint32_t)pa[j] < N ? min(n, turn) : 0, nb = (uint32_t)pb[j] < N ? n : 0;
+          const int sa = pa[j] * p.page + at, sb = pb[j] * p.page - turn;
           int slot[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool second = at + i >= p.page;
-            const int pg = second ? pb[j] : pa[j], in = second ? at + i - p.page : at + i;
-            slot[i] = r + i >= q.placed || pg < 0 || pg >= p.n_pages ? -1 : pg * p.page + in;
-            if (r + i < q.placed && in == 0 && col[j] + second >= have_k) table[col[j] + second] = pg;
-          }
+          for (int i = 0; i < 4; ++i) slot[i] = i < na ? sa + i : (i >= turn && i < nb ? sb + i : -1);
+          const bool opens = at == 0;   // one page at most begins in four rows
+          if (n > (opens ? 0 : turn) && col[j] + !opens >= have_k) table[col[j] + !opens] = opens ? pa[j] : pb[j];
           if (r >= p.R) continue;
           if (wide) *reinterpret_cast<int4*>(slots + r) = make_int4(slot[0], slot[1], slot[2], slot[3]);
           else
