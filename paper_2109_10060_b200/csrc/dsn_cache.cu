@@ -13,7 +13,7 @@ using dsn_gemm::unpack2;
 // the cluster share the slots.  A slot needs no other thread's result: a token's page stands in the table already or
 // is the ring's entry at a place that the scan gives.  What a CTA of the cluster still has to read (lengths, ring counters) is overwritten only behind the
 // cluster's barrier.  Pages taken and pages returned are different entries of the ring, so those need no order.
-// Bound by trips to memory: lengths, then pages, then the stores; eight rows a thread are looked up at once (128 x 2048 rows: 11.0 us, one after the other 18; 64 x 1 row 2.3).
+// Bound by trips to memory: lengths, then pages, then the stores; rows are looked up eight a thread, or four neighbours a lane, at once (128 x 2048 rows: 8.0 us, one after the other 18; 64 x 1 row 2.4).
 struct PlanRequest {
   int32_t held, placed;   // placed < 0: the request ends
   uint32_t start;         // new pages of the requests before it; or returned pages of the requests before it
@@ -231,7 +231,7 @@ constexpr int kWriteWarps = 4, kWriteCtas = 28;   // warps a CTA; CTAs an SM at 
 // `split`th piece of it where there are few rows, four pieces on their way at a time.
 // Bound by instructions once memory is busy: least and greatest value go through the shuffles as one pair of bf16 numbers (the least, minus the greatest);
 // a code comes out of an addition that rounds (1.5 * 2^23 + 8: its low four bits are the code), eight of them are put together by multiply-adds.
-// Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 22.6 us, 4 x 4096 rows of 8 heads of 128 with values 31.9 (floors 10.6 and 23.3 at a copy's rate); one row 2.2.
+// Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 22.3 us, 4 x 4096 rows of 8 heads of 128 with values 31.6 (floors 10.6 and 23.3 at a copy's rate); one row 2.2.
 template <int D, bool VALUES>
 __global__ void __launch_bounds__(kWriteWarps * 32) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
   constexpr int LPH = D / 4;             // lanes a head
@@ -334,10 +334,40 @@ __global__ void __launch_bounds__(kWriteWarps * 32) cache_write_kernel(const __g
 
 }  // namespace
 
+namespace {
+
+// CTAs of a cluster for many rows: 16 where the device can hold such a cluster, else 8, which it always can (128 prompts: 8.0 and 10.4 us; 4: 15.5).
+template <bool LONG>
+int plan_ranks() {
+  static int known[DSN_MAX_DEVICES] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DSN_MAX_DEVICES) return 8;
+  if (known[dev]) return known[dev];
+  auto kernel = cache_plan_kernel<1024, LONG>;
+  int ranks = 8, n = 0;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 16;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(1024);
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0)
+    ranks = 16;
+  else
+    cudaGetLastError();   // 8, then; not an error of the call
+  return known[dev] = ranks;
+}
+
+}  // namespace
+
 cudaError_t dsn_launch_cache_plan(const CachePlanParams& p, cudaStream_t s) {
   const int64_t rows = (int64_t)p.B * p.R;
   if (p.B <= 128 && rows <= 1024) return dsn_launch(cache_plan_kernel<128, false>, dim3(1), dim3(128), 0, s, 1, p);   // fewer warps meet sooner
-  const int ranks = rows > 4096 ? 8 : 1;   // portable cluster size
+  const int ranks = rows > 4096 ? (p.R >= 64 ? plan_ranks<true>() : plan_ranks<false>()) : 1;
   return dsn_launch(p.R >= 64 ? cache_plan_kernel<1024, true> : cache_plan_kernel<1024, false>, dim3((unsigned)ranks), dim3(1024), 0, s, ranks, p);
 }
 

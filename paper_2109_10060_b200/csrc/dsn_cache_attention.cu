@@ -5,7 +5,7 @@
 // long requests nor many short ones leave SMs idle.  A warp keeps the steps to come in flight as bulk copies into a ring of its own (no barrier with
 // other warps), a block of 16 tokens a copy, as pages may end after any block.
 // Measured (in a graph): 64 requests of up to 8192 tokens, 8 heads of 128, 4 queries a head: 119 us, 3.9 TB/s; a copy's rate would allow 70 us.  What bounds it is the
-// arithmetic on the codes, some 680 instructions a step and warp at 12 warps of 168 registers an SM (56 % of the issue slots, the rest is their latency); no other
+// arithmetic on the codes, some 700 instructions a step and warp at 12 warps of 168 registers an SM (58 % of the issue slots, the rest is their latency); no other
 // split was faster: 16 and 14 warps spill (132, 148 us), 8 hide less (144).  One token of one request takes 9.0 us: the look-ups in a row of request, page and
 // blocks, the join in shared memory and the joining kernel, not the bytes.
 // An item that lies in one warp's stretch is finished there.  What the warps of a CTA cut among themselves they join in shared memory; of an item that is
