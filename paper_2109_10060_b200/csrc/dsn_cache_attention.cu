@@ -510,6 +510,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     dsn_drain(bars, DEPTH, max(0, asked - DEPTH), asked);
     head_state = 3;
     tail = 0;
+  } else if (head_far) {   // back into the ring, behind the last part: one trip to memory for all warps, where the join below would make one for each of its parts
+    static_assert(2 * kPart * sizeof(float) <= DEPTH * slot_bytes<D>() && kPart % 4 == 0, "two parts in a ring");
+    const float4* from = reinterpret_cast<const float4*>(p.warp_data + ((int64_t)blockIdx.x * WARPS + warp) * kPart);
+    float4* to = reinterpret_cast<float4*>(smem + (ring - smem_u32(smem))) + kPart / 4;
+    constexpr int N = (kPart / 4 + 31) / 32;
+    float4 x[N];
+    __syncwarp();   // other lanes' stores
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (32 * k + lane < kPart / 4) x[k] = from[32 * k + lane];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (32 * k + lane < kPart / 4) to[32 * k + lane] = x[k];
   }
   }
 
@@ -517,15 +530,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
   CachePart* s_part = reinterpret_cast<CachePart*>(s_scan + 128);
   if (lane == 0) s_part[warp] = CachePart{head_state, tail, work.e.sample, work.e.pos, work.head, work.e.rows, head_far, 0};
   __syncthreads();
-  auto part_of = [&](int w, bool of_tail) -> const float* {   // where a warp left a part
-    if (!of_tail && s_part[w].head_far) return p.warp_data + ((int64_t)blockIdx.x * WARPS + w) * kPart;
-    return reinterpret_cast<const float*>(smem + (base - smem_u32(smem)) + (size_t)w * DEPTH * slot_bytes<D>());
-  };
   // A chain is the tail of a warp (or what came before this CTA) and the heads behind it up to the one that ends its item.
   const CachePart mine = s_part[lane < WARPS ? lane : 0];
   constexpr uint32_t kAll = (1u << WARPS) - 1u;
   const uint32_t closes = __ballot_sync(0xffffffffu, mine.head_state == 1) & kAll, passes = __ballot_sync(0xffffffffu, mine.head_state == 2) & kAll,
-                 begins = __ballot_sync(0xffffffffu, mine.head_state == 0) & kAll, tails = __ballot_sync(0xffffffffu, mine.tail != 0) & kAll;
+                 begins = __ballot_sync(0xffffffffu, mine.head_state == 0) & kAll, tails = __ballot_sync(0xffffffffu, mine.tail != 0) & kAll,
+                 far = __ballot_sync(0xffffffffu, mine.head_far != 0) & kAll;
+  auto part_of = [&](int w, bool of_tail) -> const float* {   // where a warp left a part
+    return reinterpret_cast<const float*>(smem + (base - smem_u32(smem)) + (size_t)w * DEPTH * slot_bytes<D>()) + (!of_tail && (far >> w & 1u) ? kPart : 0);
+  };
   const uint32_t first_heads = (closes | passes) & ~(begins ? ~((begins & (0u - begins)) - 1u) : 0u);   // heads in front of the first item that begins here
   // parts of the chain behind warp a (-1: in front of all): up to the first that closes
   auto heads_of = [&](int a) -> uint32_t {
@@ -562,10 +575,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
       float y[D / 32];
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) y[x] = 0.f;
-#pragma unroll
-      for (int j = 0; j < WARPS; ++j) {
+#pragma unroll 2
+      for (uint32_t set = heads | (a >= 0 ? 1u << a : 0u); set; set &= set - 1u) {
+        const int j = __ffs(set) - 1;
         const float fj = __shfl_sync(0xffffffffu, f, j);
-        const float* at = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)reinterpret_cast<uint64_t>(src), j)) + 2 * NC + v * D;
+        const float* at = part_of(j, j == a) + 2 * NC + v * D;
         if constexpr (D == 128) {
           const float4 q = fj == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(at + 4 * lane);
           y[0] = fmaf(q.x * fj, fj, y[0]); y[1] = fmaf(q.y * fj, fj, y[1]); y[2] = fmaf(q.z * fj, fj, y[2]); y[3] = fmaf(q.w * fj, fj, y[3]);
