@@ -257,8 +257,8 @@ typedef struct dsn_rotary_desc {
  *
  * Rows of a call lie as everywhere, [B][R][ld]; request i has rows 0 .. placed[i] - 1 of its R, the rest is padding that is neither
  * read nor written.  A row of qkv holds H heads of group + 2 vectors of D_h elements, [head][q x group | k | v][D_h]: group = 1 is the
- * layout of the sliced attention core, larger groups share a head's keys and values among their queries.  A row of the output
- * holds [head][group][D_h].  Heads >= heads[t] of a request of path t are neither read nor written.
+ * layout of the sliced attention core, larger groups share a head's keys and values among their queries (dsn_rotary_axes turns rows of
+ * group <= 6).  A row of the output holds [head][group][D_h].  Heads >= heads[t] of a request of path t are neither read nor written.
  *
  * Pages: [n_pages][H][page / 16] blocks of 16 tokens.  A block holds the keys, then the values, each as
  *   codes [D_h / 64][16][32 bytes]   64 elements a token, element 2 j in the low half of byte j, 2 j + 1 in the high half
@@ -520,7 +520,7 @@ int dsn_cache_plan(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, in
 
 /* Rounds k and v of the rows to 4 bits and writes them to their slots (rows with slot -1 go nowhere; other slots outside the cache record
  * DSN_ERR_BAD_INDEX and go nowhere either; no two rows may have the same slot).  values (or NULL): the values that the codes stand for, rounded
- * to bfloat16, rows [head][k | v][D_h].  Uses pages and slots. */
+ * to bfloat16, rows [head][k | v][D_h]; they overlap nothing else.  Uses pages and slots. */
 int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* values,
                        void* stream);
 
@@ -530,8 +530,8 @@ int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c
  * tokens in a row share a power of k and one of v: a token whose values are below 2^-17 of the greatest of them has fewer than 8 bits.
  * A row that sees nothing (n < 0) comes out as zeros.  Uses pages, table, lengths, and placed (NULL: R rows of every request).  A length or
  * placed value out of range is held at the nearest end of it, tokens of a page outside the cache are left out, and both record DSN_ERR_BAD_INDEX.
- * workspace: device, 16-byte aligned, of dsn_cache_attention_q4_workspace_bytes; nothing in it has to start at zero.  It must not be
- * used by two calls at once. */
+ * out overlaps nothing else.  workspace: device, 16-byte aligned, of dsn_cache_attention_q4_workspace_bytes; nothing in it has to start at
+ * zero.  It must not be used by two calls at once. */
 size_t dsn_cache_attention_q4_workspace_bytes(const dsn_cache_desc* d, int32_t B);
 int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, const dsn_routing* r, const void* qkv, void* out,
                            void* workspace, size_t ws_bytes, void* stream);
