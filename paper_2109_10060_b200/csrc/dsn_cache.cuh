@@ -53,7 +53,7 @@ struct __align__(16) CachePart {
   int32_t head_state;  // 0: the stretch begins with an item of its own; 1: an earlier one's item ends here; 2: all of it lies inside one item; 3: it is empty
   int32_t tail;        // 1: its last item began here and goes on
   int32_t sample, pos, head, rows;   // of that last item
-  int32_t head_far;    // (warp) the first item's part is in the workspace, not in the warp's ring
+  int32_t head_far;    // (warp) the first item's part went through the workspace and lies behind the last one's in the ring
   int32_t pad;
 };
 
