@@ -1533,7 +1533,8 @@ int dsn_cache_attention_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cach
   CacheAttParams p;
   memset(&p, 0, sizeof(p));
   fill_cache_routing(p, d, r);
-  p.n_pages = d->n_pages; p.max_pages = d->max_pages; p.window = d->window;
+  p.n_pages = d->n_pages; p.max_pages = d->max_pages;
+  p.window = dsn_cache_window(d->window, d->max_pages, d->page);
   p.by_group = dsn_fast_div((uint32_t)d->group);
   p.scale_log2 = (float)((d->scale != 0.f ? (double)d->scale : 1.0 / sqrt((double)d->D_h)) * 1.4426950408889634);
   p.table = c->table; p.lengths = c->lengths; p.placed = c->placed; p.pages = c->pages;

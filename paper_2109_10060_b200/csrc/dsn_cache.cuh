@@ -7,6 +7,14 @@
 #define DSN_CACHE_BLOCK 16
 __host__ __device__ constexpr uint32_t dsn_cache_block_bytes(int D) { return 18u * (uint32_t)D; }
 
+// The window as the kernels get it.  One that reaches over all tokens a request can hold hides nothing: 0, so that windows are below 2^30 there and their
+// difference to a token's number, which is above -2^24 (rows in front of a request's first token), stays in 32 bits.
+__host__ __device__ constexpr int32_t dsn_cache_window(int32_t window, int32_t max_pages, int32_t page) {
+  return window >= (int64_t)max_pages * page ? 0 : window;
+}
+// First token that token `me` sees.
+__host__ __device__ constexpr int32_t dsn_cache_first_seen(int32_t me, int32_t window) { return window && me - window + 1 > 0 ? me - window + 1 : 0; }
+
 struct CachePlanParams {
   int32_t B, R, page, n_pages, max_pages;
   FastDiv by_page, by_R;

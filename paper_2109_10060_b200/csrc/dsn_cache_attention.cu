@@ -51,7 +51,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
 __device__ __forceinline__ void item_range(int len, int rows, int window, int& lo, int& hi) {
   const int first = len - rows;                                // token of the first row
   hi = len;
-  lo = window ? max(0, first - window + 1) & ~(DSN_CACHE_BLOCK - 1) : 0;
+  lo = dsn_cache_first_seen(first, window) & ~(DSN_CACHE_BLOCK - 1);
 }
 
 // A walk along the line.

@@ -97,7 +97,7 @@ __device__ __forceinline__ Span span_of(int len, int rows, int ct, int group, co
   const int first = len - rows;
   s.me0 = first + (int)dsn_div((uint32_t)s.v0, by_group);
   s.me1 = first + (int)dsn_div((uint32_t)(s.v1 - 1), by_group);
-  s.lo = window ? max(0, s.me0 - window + 1) & ~(DSN_CACHE_BLOCK - 1) : 0;
+  s.lo = dsn_cache_first_seen(s.me0, window) & ~(DSN_CACHE_BLOCK - 1);
   s.tiles = max(1, (s.me1 + 1 - s.lo + kTile - 1) / kTile);
   return s;
 }
@@ -154,7 +154,7 @@ __device__ __forceinline__ void half_tiles(const Item& it, int h, const FastDiv&
   if (w0 >= w1) return;
   const int first = it.e.len - it.e.rows, m0 = first + (int)dsn_div((uint32_t)w0, by_group), m1 = first + (int)dsn_div((uint32_t)(w1 - 1), by_group);
   if (m1 < 0) return;
-  a = max(it.c0, ((window ? max(0, m0 - window + 1) : 0) - it.s.lo) / kTile);
+  a = max(it.c0, (dsn_cache_first_seen(m0, window) - it.s.lo) / kTile);
   b = min(it.c1, (m1 + 1 - it.s.lo + kTile - 1) / kTile);
   if (b < a) b = a;
 }
