@@ -315,9 +315,9 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       }
       return min(max(__reduce_max_sync(0xffffffffu, e), of_v ? 77u : 27u), 253u);
     };
-    uint32_t i = 0;
+    int asked = 0;   // tiles whose copies were issued
     find();
-    for (; more; ++i) {
+    for (uint32_t i = 0; more; ++i) {
       const uint32_t slot = i & 1u;
       if (i >= 2 && !warp_wait(raw_empty + 8 * slot, ((i >> 1) - 1u) & 1u, abort_flag, p.status, 91)) break;
       const bool ok = pg >= 0 && pg < p.n_pages, lost = exists && !ok;
@@ -330,6 +330,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       if (ok)
         dsn_bulk_load(raw_at + slot * kSlot + (uint32_t)lane * kBlock, p.pages + (((int64_t)pg * p.H + it.head) * bpp + place) * kBlock, kBlock,
                       raw_full + 8 * slot);
+      ++asked;
       const uint32_t left = (uint32_t)min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile), 0), kTile);
       if (++tile == it.c1) {
         more = walk.next(p, it);
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       }
       __syncwarp();
     }
-    if (*abort_flag) dsn_drain(raw_full, 2, i > 2 ? (int)i - 2 : 0, (int)i);
+    if (*abort_flag) dsn_drain(raw_full, 2, max(0, asked - 2), asked);   // the tile whose wait ran out among them
   } else if (warp < kSoftWarp) {
     // ------------------------------------------------------------------------------ products
     // A warp issues what one half needs.  The scores of tile number m (of those that the half needs) go to buffer m & 1, which the product with the
