@@ -166,9 +166,9 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (base - raw);
-  // barriers: [2 halves] of q and o_empty, [4 stages] of k and v, [2 slots] of raw, [2 halves][2 buffers] of s, p, o
+  // barriers: [2 halves] of q, o_empty and idle, [4 stages] of k and v, [2 slots] of raw, [2 halves][2 buffers] of s, p, o
   const uint32_t q_full = base, o_empty = base + 16, k_full = base + 32, k_empty = base + 64, v_full = base + 96, v_empty = base + 128,
-                 raw_full = base + 160, raw_empty = base + 176, raw_ready = base + 304, s_full = base + 192, p_full = base + 224, o_full = base + 256;
+                 raw_full = base + 160, raw_empty = base + 176, raw_ready = base + 304, idle = base + 336, s_full = base + 192, p_full = base + 224, o_full = base + 256;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 288);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 292);
   uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there; tokens << 8; exponents that K and V are divided by << 16, << 24
@@ -189,6 +189,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       mbar_init(raw_full + 8 * i, 1);
       mbar_init(raw_empty + 8 * i, 8);
       mbar_init(raw_ready + 8 * i, 1);
+      mbar_init(idle + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(k_full + 8 * i, 4);   // units of 16 tokens
@@ -424,6 +425,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       }
     }
     while (n_s != n_p && ok) pv();
+    if (!ok) products_end(idle + 8 * h);
   } else if (warp >= kSoftWarp) {
     // ------------------------------------------------------------------------------ softmax, a thread a row
     const int h = (warp - kSoftWarp) >> 2, quarter = warp & 3, row = quarter * 32 + lane;

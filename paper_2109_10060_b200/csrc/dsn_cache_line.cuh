@@ -32,6 +32,15 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, dsn_gemm::mbar_wait_slow(bar, parity, abort_flag, status, where));
 }
 
+// After a wait that ran out: the products that this warp issued get a last bounded chance to end before the CTA gives TMEM and shared memory back.
+__device__ __forceinline__ bool products_end(uint32_t bar) {
+  if (dsn_gemm::elect_one()) dsn_gemm::umma_commit(bar);
+  __syncwarp();
+  for (int j = 0; j < (1 << 14); ++j)
+    if (__all_sync(0xffffffffu, dsn_gemm::mbar_try_wait(bar, 0))) return true;
+  return false;
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));

@@ -17,18 +17,27 @@ __device__ __forceinline__ void drain_noted(uint32_t bars, int depth, int first,
   if ((threadIdx.x & 31) == 0) g_drain[blockIdx.x][0] = first, g_drain[blockIdx.x][1] = asked;
   dsn_drain(bars, depth, first, asked);
 }
+__device__ int g_ended[DSN_CACHE_MAX_CTAS];
+__device__ __forceinline__ void products_noted(uint32_t bar) {
+  const bool ok = dsn_q4::products_end(bar);
+  if ((threadIdx.x & 31) == 0) atomicAdd(&g_ended[blockIdx.x], ok ? 1 : 100);
+}
 }  // namespace
+#define products_end products_noted
 #define dsn_bulk_load load_unless_withheld
 #define dsn_drain drain_noted
 #include "dsn_cache_attention_rows.cu"
 
-// One request of one path and one head of 64, pages of 64 tokens in a row; drain: host [148][2], -1 where a CTA waited for nothing.  Returns a cudaError_t.
+// One request of one path and one head of 64, pages of 64 tokens in a row; drain: host [148][2], -1 where a CTA waited for nothing.
+// ended: host [148], warps of a CTA whose products had ended when they left early (100: had not).  Returns a cudaError_t.
 extern "C" int cache_rows_withheld(const void* qkv, void* out, const uint8_t* pages, const int32_t* table, const int32_t* lengths, const int32_t* offsets, const int32_t* perm,
-                                   int rows, int n_pages, const void* from, const void* to, int32_t* status, int sm_count, void* workspace, int32_t* drain) {
+                                   int rows, int n_pages, const void* from, const void* to, int32_t* status, int sm_count, void* workspace, int32_t* drain, int32_t* ended) {
   const uint64_t range[2] = {reinterpret_cast<uint64_t>(from), reinterpret_cast<uint64_t>(to)};
   cudaError_t e = cudaMemcpyToSymbol(g_range, range, sizeof(range));
   memset(drain, 0xff, sizeof(g_drain));
   if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_drain, drain, sizeof(g_drain));
+  memset(ended, 0, sizeof(g_ended));
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_ended, ended, sizeof(g_ended));
   if (e != cudaSuccess) return e;
   CacheAttParams p;
   memset(&p, 0, sizeof(p));
@@ -42,6 +51,7 @@ extern "C" int cache_rows_withheld(const void* qkv, void* out, const uint8_t* pa
   e = dsn_launch_cache_attention_rows(p, 64, sm_count, workspace, nullptr);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpyFromSymbol(drain, g_drain, sizeof(g_drain));
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(ended, g_ended, sizeof(g_ended));
   return e;
 }
 extern "C" long cache_rows_ws_bytes() { return (long)dsn_cache_rows_ws_bytes(64, 1); }

@@ -1,5 +1,5 @@
 """The many-rows attention over the 4-bit cache when a tile never arrives: the waits give up, the status says so, and before its CTA ends the loader
-waits for every copy that it issued, those of the missing tile among them.  Nothing faults: one page's copies are left out, every wait is bounded."""
+waits for every copy that it issued, those of the missing tile among them, and both issuing warps for their products.  Nothing faults: one page's copies are left out, every wait is bounded."""
 import ctypes
 import os
 import subprocess
@@ -27,7 +27,7 @@ def withheld(tmp_path_factory):
                     os.path.join(HERE, "cache_rows_withheld.cu"), "-o", out], check=True)
     lib = ctypes.CDLL(out)
     vp, i32 = ctypes.c_void_p, ctypes.c_int
-    lib.cache_rows_withheld.argtypes = [vp] * 7 + [i32] * 2 + [vp] * 3 + [i32] + [vp] * 2
+    lib.cache_rows_withheld.argtypes = [vp] * 7 + [i32] * 2 + [vp] * 3 + [i32] + [vp] * 3
     lib.cache_rows_ws_bytes.restype = ctypes.c_long
     return lib
 
@@ -49,22 +49,24 @@ def test_a_tile_that_never_arrives(withheld, tile):
     status[WAIT_US] = 1000
     per = raw.numel() // pages.n_pages
     at = raw.data_ptr() + int(pages.table[0, 5 * 9 + tile]) * per
-    drain = np.zeros((148, 2), np.int32)
+    drain, ended = np.zeros((148, 2), np.int32), np.zeros(148, np.int32)
 
     def go(first, last):
         torch.cuda.synchronize()
         err = withheld.cache_rows_withheld(x.data_ptr(), out.data_ptr(), raw.data_ptr(), table.data_ptr(), lengths.data_ptr(), offsets.data_ptr(), perm.data_ptr(), rows,
-                                           pages.n_pages, first, last, status.data_ptr(), sms, ws.data_ptr(), drain.ctypes.data)
+                                           pages.n_pages, first, last, status.data_ptr(), sms, ws.data_ptr(), drain.ctypes.data,
+                                           ended.ctypes.data)
         assert err == 0
 
     go(0, 0)
-    assert status[0].item() == 0 and np.all(drain == -1)
+    assert status[0].item() == 0 and np.all(drain == -1) and not ended.any()
     whole = out.clone()
     go(at, at + per)
     assert status[0].item() == TIMEOUT
     assert np.all(np.delete(drain, 9, 0) == -1)
     first, asked = drain[9]
     assert asked == tile + 1 and first == max(0, asked - 2)
+    assert ended[9] in (1, 2) and not np.delete(ended, 9).any()      # the half without rows may have had nothing left to wait for
     status[0] = 0
     go(0, 0)
     assert status[0].item() == 0 and torch.equal(out, whole) and bool(out.isfinite().all())
