@@ -526,7 +526,8 @@ int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c
 
 /* out = softmax(scale * q k^T) v over the cached tokens that a row's query sees: row j of request i is token n = lengths[i] - placed[i] + j of
  * it (its keys are in the cache already) and sees tokens max(0, n - window + 1) .. n.  Softmax and sums in fp32; the operands of both products are rounded to
- * 11 bits (fp16 behind powers of two: q and k, a probability or its product with v's scale, v), magnitudes of v from 1e-15 to 1e34 in a cache keep them.  With R * group > 32, 64
+ * 11 bits (fp16 behind powers of two: q and k, a probability or its product with v's scale, v).  With R * group <= 32 magnitudes of v from 1e-15 to 1e34 in a
+ * cache keep them, whatever other groups of 64 elements, other tokens or tokens that a row does not see hold.  With R * group > 32, 64
  * tokens in a row share a power of k and one of v: a token whose values are below 2^-17 of the greatest of them has fewer than 8 bits.
  * A row that sees nothing (n < 0) comes out as zeros.  Uses pages, table, lengths, and placed (NULL: R rows of every request).  A length or
  * placed value out of range is held at the nearest end of it, tokens of a page outside the cache are left out, and both record DSN_ERR_BAD_INDEX.

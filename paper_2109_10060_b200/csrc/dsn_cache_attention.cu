@@ -4,7 +4,8 @@
 // elements, 64 of 64): all steps of all (request, head) items stand in one line, and every warp of the GPU gets an equal stretch of it, so neither few
 // long requests nor many short ones leave SMs idle.  A warp keeps the steps to come in flight as bulk copies into a ring of its own (no barrier with
 // other warps), a block of 16 tokens a copy, as pages may end after any block.
-// Measured (in a graph): 64 requests of up to 8192 tokens, 8 heads of 128, 4 queries a head: 119 us, 3.9 TB/s; a copy's rate would allow 70 us.  What bounds it is the
+// Measured (in a graph): 64 requests of up to 8192 tokens, 8 heads of 128, 4 queries a head: 122 us, 3.8 TB/s (118 with one
+// reference a query, which lost what lay 2^20 below the largest scale of a step); a copy's rate would allow 70 us.  What bounds it is the
 // arithmetic on the codes, some 700 instructions a step and warp at 12 warps of 168 registers an SM (58 % of the issue slots, the rest is their latency); no other
 // split was faster: 16 and 14 warps spill (132, 148 us), 8 hide less (144).  One token of one request takes 9.0 us: the look-ups in a row of request, page and
 // blocks, the join in shared memory and the joining kernel, not the bytes.
@@ -19,9 +20,10 @@
 //   one rounding to fp16, the middle into a sum of its own in fp32.
 // The order of elements in a product is free, so a lane takes whole words: 16 elements of K in 8 bytes, 8 elements of V in 4.  Row i of a block's K is token
 // i ^ (i >> 2 & 1): then neither K's rows nor the pairs of tokens that a lane needs of V meet in a bank.
-// Queries are brought to 1 .. 2 by a power of two, which goes into the scale.  Everything of a query is in units of 2^ref, a reference that moves only when a
-// probability times the largest power of two in the step's scales would pass 2^15 (one vote a step instead of a reduction): fp16 then holds every product of
-// a probability and a scale, whatever their range.
+// Queries are brought to 1 .. 2 by a power of two, which goes into the scale.  What a query gathers of a group of 64 elements is in units of 2^ref, a reference of
+// the query and the group: the largest product of a probability and a scale among the tokens that the query sees stands at 2^7 .. 2^15, so that fp16 holds
+// every product that counts, however far the scales of other groups, of other tokens or of tokens that are hidden lie from it.  A step first looks at a
+// bound (a lane's largest score and its largest power of two); only where that passes 2^15 are the products themselves looked at and the reference moved.
 #include "dsn_cache_line.cuh"
 
 namespace {
@@ -85,11 +87,31 @@ __host__ __device__ constexpr uint32_t step_bytes() { return step_blocks<D>() * 
 template <int D, int WARPS, int DEPTH>
 constexpr size_t attention_smem() { return kCtrl + kListSmem * sizeof(CacheEntry) + WARPS * DEPTH * 8 + (size_t)WARPS * DEPTH * slot_bytes<D>(); }
 
+// Power of two of a pair's scale, or of its middle less 2^40: a probability with a middle is at most 2^55 then, a probability 2^65, which fp32 sums hold.  `pair`:
+// magnitudes, or the largest of several.
+__device__ __forceinline__ float pair_power(uint32_t pair) {
+  const uint32_t top = min(max(pair & 0xffffu, max(pair >> 16, 40u << 7) - (40u << 7)), 0x7f7fu);
+  return fmaxf((float)(int)(top >> 7) - 127.f, -50.f);
+}
+// From a group's unit and the sum's to the output, for references that can lie further apart than fp32 reaches: a result that fp32 holds is met by no factor
+// that it does not.
+struct Unit {
+  float once, again;
+  __device__ __forceinline__ float operator()(float y) const { return y * once * again; }
+};
+__device__ __forceinline__ Unit out_unit(float ref, float ref_of_sum, float inv) {
+  const float half = ex2(0.5f * (ref - ref_of_sum));
+  return Unit{inv * half, half};
+}
+// Floats of a part: references of the groups, sums (in units of the first group's reference), products.
+template <int D>
+__host__ __device__ constexpr int part_floats(int NC) { return NC * (D + D / 64 + 1); }
+
 template <int D, int NT, int WARPS, int DEPTH>
 __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __grid_constant__ CacheAttParams p) {
   constexpr int THREADS = WARPS * 32, GR = D / 64, NC = 8 * NT;
   constexpr int SB = step_blocks<D>(), kStepTokens = SB * DSN_CACHE_BLOCK;
-  constexpr int kPart = NC * (D + 2);   // floats of a part: references, sums, products
+  constexpr int kPart = part_floats<D>(NC), kSums = GR * NC, kProducts = (GR + 1) * NC;
   constexpr uint32_t kBlock = dsn_cache_block_bytes(D), kHalf = kBlock / 2, kPairs = GR * 512;
   extern __shared__ __align__(128) uint8_t smem[];
   CacheEntry* s_list = reinterpret_cast<CacheEntry*>(smem);
@@ -197,7 +219,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
 
   uint32_t qf[NT][GR][4][2];
   float qsum[NT][GR][2], qoff[NT][GR][2], cs[NT][2];   // of this lane's columns: sum of the query, minus the offsets' product with it, factor of the scores (positive)
-  float o[NT][GR][4][4], oz[NT][GR][2], l[NT][2], ref[NT][2];
+  float o[NT][GR][4][4], oz[NT][GR][2], l[NT][2], ref[NT][GR][2];
   int row_of[NT][2];                 // rows of this lane's columns
   bool fresh = true, ok = true;
   bool head_open = work.step != 0;   // the first item began in an earlier warp's stretch
@@ -267,13 +289,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
           qoff[nt][gr][0] = __shfl_sync(0xffffffffu, off, 8 * t);
           qoff[nt][gr][1] = __shfl_sync(0xffffffffu, off, 8 * t + 4);
           oz[nt][gr][0] = oz[nt][gr][1] = 0.f;
+          ref[nt][gr][0] = ref[nt][gr][1] = kLowest;
 #pragma unroll
           for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int x = 0; x < 4; ++x) o[nt][gr][mt][x] = 0.f;
         }
         l[nt][0] = l[nt][1] = 0.f;
-        ref[nt][0] = ref[nt][1] = kLowest;
         row_of[nt][0] = (int)dsn_div((uint32_t)(v0 + nt * 8 + 2 * t), p.by_group);
         row_of[nt][1] = (int)dsn_div((uint32_t)(v0 + nt * 8 + 2 * t + 1), p.by_group);
       }
@@ -293,7 +315,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
 
     float s[SB][NT][4];
     uint32_t vpair[SB][GR][2];
-    uint32_t big = 0;   // largest of the scales' bits, largest of the middles'
 #pragma unroll
     for (int b = 0; b < SB; ++b) {
       const uint32_t blk = st + b * kBlock;
@@ -346,41 +367,55 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         }
       }
     }
+    // a product of a probability and a scale that would pass the top?
+    float power[GR];
 #pragma unroll
-    for (int b = 0; b < SB; ++b)
+    for (int gr = 0; gr < GR; ++gr) {
+      uint32_t big = 0;   // largest of the scales' bits, largest of the middles'
 #pragma unroll
-      for (int gr = 0; gr < GR; ++gr) big = __vmaxu2(big, __vmaxu2(vpair[b][gr][0] & 0x7fff7fffu, vpair[b][gr][1] & 0x7fff7fffu));
-    // the power of the largest scale, or of a middle 2^40 times as large (a probability with a middle is at most 2^55 then, a probability 2^65: fp32 sums hold them)
-    big = min(__reduce_max_sync(0xffffffffu, max(big & 0xffffu, max(big >> 16, 40u << 7) - (40u << 7))), 0x7f7fu);
-    const float power = fmaxf((float)(int)(big >> 7) - 127.f, -50.f);
-    // a probability that would pass the top?
+      for (int b = 0; b < SB; ++b) big = __vmaxu2(big, __vmaxu2(vpair[b][gr][0] & 0x7fff7fffu, vpair[b][gr][1] & 0x7fff7fffu));
+      power[gr] = pair_power(big);
+    }
     float most = -INFINITY;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float m = -INFINITY;
+        float m = -INFINITY, up = -INFINITY;
 #pragma unroll
         for (int b = 0; b < SB; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
-        most = fmaxf(most, fmaf(m, cs[nt][c], -ref[nt][c]));
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr) up = fmaxf(up, power[gr] - ref[nt][gr][c]);
+        most = fmaxf(most, fmaf(m, cs[nt][c], up));
       }
-    if (__any_sync(0xffffffffu, most + power > kTop)) {
+    if (__any_sync(0xffffffffu, most > kTop)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int gr = 0; gr < GR; ++gr) {
+        float top[NT][2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float m = -INFINITY;
+        for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = -INFINITY;
 #pragma unroll
-          for (int b = 0; b < SB; ++b) m = fmaxf(m, fmaxf(s[b][nt][c], s[b][nt][2 + c]));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-          m = fmaxf(ref[nt][c], fmaf(m, cs[nt][c], power - kAim));
-          const float f = ex2(0.5f * (ref[nt][c] - m));   // twice: references can lie further apart than fp32 reaches
-          ref[nt][c] = m;
-          l[nt][c] = l[nt][c] * f * f;
+        for (int b = 0; b < SB; ++b)
 #pragma unroll
-          for (int gr = 0; gr < GR; ++gr) {
+          for (int hf = 0; hf < 2; ++hf) {
+            const float e = pair_power(vpair[b][gr][hf] & 0x7fff7fffu);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) top[nt][c] = fmaxf(top[nt][c], fmaf(s[b][nt][2 * hf + c], cs[nt][c], e));
+          }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float m = top[nt][c];
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            m = fmaxf(ref[nt][gr][c], m - kAim);
+            const float f = ex2(0.5f * (ref[nt][gr][c] - m));   // twice: references can lie further apart than fp32 reaches
+            ref[nt][gr][c] = m;
+            if (gr == 0) l[nt][c] = l[nt][c] * f * f;
             oz[nt][gr][c] = oz[nt][gr][c] * f * f;
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
@@ -388,17 +423,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
               o[nt][gr][mt][2 + c] = o[nt][gr][mt][2 + c] * f * f;
             }
           }
-        }
+      }
     }
-#pragma unroll
-    for (int b = 0; b < SB; ++b)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          s[b][nt][x] = ex2(fmaf(s[b][nt][x], cs[nt][x & 1], -ref[nt][x & 1]));
-          l[nt][x & 1] += s[b][nt][x];
-        }
 #pragma unroll
     for (int b = 0; b < SB; ++b) {
       const uint32_t blk = st + b * kBlock + kHalf;
@@ -411,7 +437,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
             const float sc = lo_bf16(vpair[b][gr][hf]), z = hi_bf16(vpair[b][gr][hf]);
-            const float p0 = s[b][nt][2 * hf], p1 = s[b][nt][2 * hf + 1];
+            const float p0 = ex2(fmaf(s[b][nt][2 * hf], cs[nt][0], -ref[nt][gr][0])), p1 = ex2(fmaf(s[b][nt][2 * hf + 1], cs[nt][1], -ref[nt][gr][1]));
+            if (gr == 0) l[nt][0] += p0, l[nt][1] += p1;
             oz[nt][gr][0] = fmaf(p0, z, oz[nt][gr][0]);
             oz[nt][gr][1] = fmaf(p1, z, oz[nt][gr][1]);
             const __half2 ps = __floats2half2_rn(p0 * sc, p1 * sc);
@@ -481,24 +508,26 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
               y[mt] = o[nt][gr][mt][c] + z;
               y[mt + 4] = o[nt][gr][mt][2 + c] + z;
             }
+            const Unit to = out_unit(ref[nt][gr][c], ref[nt][0][c], inv);
             if (v < cols) {
               if (whole) {
                 uint4 w;
-                w.x = pack_bf16(y[0] * inv, y[1] * inv);
-                w.y = pack_bf16(y[2] * inv, y[3] * inv);
-                w.z = pack_bf16(y[4] * inv, y[5] * inv);
-                w.w = pack_bf16(y[6] * inv, y[7] * inv);
+                w.x = pack_bf16(to(y[0]), to(y[1]));
+                w.y = pack_bf16(to(y[2]), to(y[3]));
+                w.z = pack_bf16(to(y[4]), to(y[5]));
+                w.w = pack_bf16(to(y[6]), to(y[7]));
                 *reinterpret_cast<uint4*>(p.out + (row0 + r) * p.ld_out + ((int64_t)kv * p.group + ev) * D + gr * 64 + 8 * g) = w;
               } else {
-                float4* d4 = reinterpret_cast<float4*>(dst + 2 * NC + v * D + gr * 64 + 8 * g);
+                float4* d4 = reinterpret_cast<float4*>(dst + kProducts + v * D + gr * 64 + 8 * g);
                 d4[0] = make_float4(y[0], y[1], y[2], y[3]);
                 d4[1] = make_float4(y[4], y[5], y[6], y[7]);
               }
             }
           }
           if (!whole && v < cols && g == 0) {
-            dst[v] = ref[nt][c];
-            dst[NC + v] = sum;
+#pragma unroll
+            for (int gr = 0; gr < GR; ++gr) dst[gr * NC + v] = ref[nt][gr][c];
+            dst[kSums + v] = sum;
           }
         }
       head_open = false;
@@ -562,13 +591,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
     const int begin = (warp + WARPS - task % WARPS) % WARPS;
     task += cols;
     for (int v = begin; v < cols; v += WARPS) {
-      const float m = in ? src[v] : kLowest, l = in ? src[NC + v] : 0.f;
-      float top = m;
+      const float l = in ? src[kSums + v] : 0.f;
+      float top[GR], f[GR];
 #pragma unroll
-      for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));   // at most 15 parts
-      top = __shfl_sync(0xffffffffu, top, 0);
-      const float f = l == 0.f ? 0.f : ex2(0.5f * (m - top));   // an empty part holds nothing; applied twice, as above
-      float sum = l * f * f;
+      for (int gr = 0; gr < GR; ++gr) {
+        const float m = in ? src[gr * NC + v] : kLowest;
+        top[gr] = m;
+#pragma unroll
+        for (int o = 8; o; o >>= 1) top[gr] = fmaxf(top[gr], __shfl_xor_sync(0xffffffffu, top[gr], o));   // at most 15 parts
+        top[gr] = __shfl_sync(0xffffffffu, top[gr], 0);
+        f[gr] = l == 0.f ? 0.f : ex2(0.5f * (m - top[gr]));   // an empty part holds nothing; applied twice, as above
+      }
+      float sum = l * f[0] * f[0];
 #pragma unroll
       for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       sum = __shfl_sync(0xffffffffu, sum, 0);
@@ -578,8 +612,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
 #pragma unroll 2
       for (uint32_t set = heads | (a >= 0 ? 1u << a : 0u); set; set &= set - 1u) {
         const int j = __ffs(set) - 1;
-        const float fj = __shfl_sync(0xffffffffu, f, j);
-        const float* at = part_of(j, j == a) + 2 * NC + v * D;
+        float fj = __shfl_sync(0xffffffffu, f[0], j);
+        if constexpr (GR == 2) {   // lanes 16 to 31 have the second group's elements
+          const float second = __shfl_sync(0xffffffffu, f[1], j);
+          if (lane >= 16) fj = second;
+        }
+        const float* at = part_of(j, j == a) + kProducts + v * D;
         if constexpr (D == 128) {
           const float4 q = fj == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(at + 4 * lane);
           y[0] = fmaf(q.x * fj, fj, y[0]); y[1] = fmaf(q.y * fj, fj, y[1]); y[2] = fmaf(q.z * fj, fj, y[2]); y[3] = fmaf(q.w * fj, fj, y[3]);
@@ -593,18 +631,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
         const int r = (int)dsn_div((uint32_t)(v0 + v), p.by_group), ev = v0 + v - r * p.group;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         __nv_bfloat16* dst = p.out + ((int64_t)(p.grouped ? q.pos : q.sample) * p.R + r) * p.ld_out + ((int64_t)(q.head >> two) * p.group + ev) * D;
+        const Unit to = out_unit(GR == 2 && lane >= 16 ? top[GR - 1] : top[0], top[0], inv);
         if constexpr (D == 128)
-          *reinterpret_cast<uint2*>(dst + 4 * lane) = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
+          *reinterpret_cast<uint2*>(dst + 4 * lane) = make_uint2(pack_bf16(to(y[0]), to(y[1])), pack_bf16(to(y[2]), to(y[3])));
         else
-          *reinterpret_cast<uint32_t*>(dst + 2 * lane) = pack_bf16(y[0] * inv, y[1] * inv);
+          *reinterpret_cast<uint32_t*>(dst + 2 * lane) = pack_bf16(to(y[0]), to(y[1]));
       } else {
         float* dst = p.cta_data + ((int64_t)blockIdx.x * 2 + (a >= 0)) * kPart;
         if (lane == 0) {
-          dst[v] = top;
-          dst[NC + v] = sum;
+#pragma unroll
+          for (int gr = 0; gr < GR; ++gr) dst[gr * NC + v] = top[gr];
+          dst[kSums + v] = sum;
         }
-        if constexpr (D == 128) *reinterpret_cast<float4*>(dst + 2 * NC + v * D + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
-        else *reinterpret_cast<float2*>(dst + 2 * NC + v * D + 2 * lane) = make_float2(y[0], y[1]);
+        if constexpr (D == 128) *reinterpret_cast<float4*>(dst + kProducts + v * D + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<float2*>(dst + kProducts + v * D + 2 * lane) = make_float2(y[0], y[1]);
       }
     }
   }
@@ -621,11 +661,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) cache_attention_kernel(const __
 template <int D>
 __global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant__ CacheAttParams p, int ctas, int NC) {
   __shared__ int s_end;
-  __shared__ float s_w[DSN_CACHE_MAX_CTAS], s_l[DSN_CACHE_MAX_CTAS], s_m;
+  constexpr int GR = D / 64;
+  __shared__ float s_w[GR][DSN_CACHE_MAX_CTAS], s_l[DSN_CACHE_MAX_CTAS], s_m[GR];
   __shared__ float4 s_o[2 * D];
   dsn_grid_dependency_wait();
   dsn_grid_launch_dependents();
-  const int tid = threadIdx.x, w = blockIdx.x, v = blockIdx.y, kPart = NC * (D + 2);
+  const int tid = threadIdx.x, w = blockIdx.x, v = blockIdx.y, kPart = part_floats<D>(NC), kSums = GR * NC, kProducts = (GR + 1) * NC;
   const CachePart part = p.parts[w];
   const int two = NC == 16 && part.rows * p.group > NC, v0 = two ? NC * (part.head & 1) : 0;
   if (!part.tail || v >= min(part.rows * p.group - v0, NC)) return;
@@ -638,26 +679,29 @@ __global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant
   for (int j = tid; j < n; j += 2 * D) {
     const float* src = p.cta_data + ((int64_t)(w + j) * 2 + (j == 0)) * kPart;
     const bool there = j == 0 || p.parts[w + j].head_state != 3;
-    s_w[j] = there ? src[v] : kLowest;
-    s_l[j] = there ? src[NC + v] : 0.f;
+#pragma unroll
+    for (int gr = 0; gr < GR; ++gr) s_w[gr][j] = there ? src[gr * NC + v] : kLowest;
+    s_l[j] = there ? src[kSums + v] : 0.f;
   }
   __syncthreads();
-  if (tid < 32) {
+  if (tid < 32 * GR) {   // a warp a group
+    const int gr = tid >> 5, lane = tid & 31;
     float m = kLowest;
-    for (int j = tid; j < n; j += 32) m = fmaxf(m, s_w[j]);
+    for (int j = lane; j < n; j += 32) m = fmaxf(m, s_w[gr][j]);
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (tid == 0) s_m = m;
+    if (lane == 0) s_m[gr] = m;
   }
   __syncthreads();
   constexpr int L = D / 4;
-  const int sub = tid % L, of = tid / L;
+  const int sub = tid % L, of = tid / L, gr = sub / 16;   // 16 threads a group of 64
+  const float m = s_m[gr];
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (int j = of; j < n; j += 8) {
-    const float f = s_l[j] == 0.f ? 0.f : ex2(0.5f * (s_w[j] - s_m));   // an empty part holds nothing; applied twice, as above
+    const float f = s_l[j] == 0.f ? 0.f : ex2(0.5f * (s_w[gr][j] - m));   // an empty part holds nothing; applied twice, as above
     const float4 q = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                              : *reinterpret_cast<const float4*>(p.cta_data + ((int64_t)(w + j) * 2 + (j == 0)) * kPart + 2 * NC + v * D + 4 * sub);
+                              : *reinterpret_cast<const float4*>(p.cta_data + ((int64_t)(w + j) * 2 + (j == 0)) * kPart + kProducts + v * D + 4 * sub);
     o.x = fmaf(q.x * f, f, o.x); o.y = fmaf(q.y * f, f, o.y); o.z = fmaf(q.z * f, f, o.z); o.w = fmaf(q.w * f, f, o.w);
   }
   s_o[tid] = o;
@@ -665,7 +709,7 @@ __global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant
   if (of) return;
   float l = 0.f;
   for (int j = 0; j < n; ++j) {
-    const float f = s_l[j] == 0.f ? 0.f : ex2(0.5f * (s_w[j] - s_m));
+    const float f = s_l[j] == 0.f ? 0.f : ex2(0.5f * (s_w[0][j] - s_m[0]));
     l = fmaf(s_l[j] * f, f, l);
   }
   for (int k = 1; k < 8; ++k) {
@@ -673,10 +717,11 @@ __global__ void __launch_bounds__(2 * D) cache_join_kernel(const __grid_constant
     o.x += q.x; o.y += q.y; o.z += q.z; o.w += q.w;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
+  const Unit to = out_unit(m, s_m[0], inv);
   const int r = (v0 + v) / p.group, ev = v0 + v - r * p.group;
   const int64_t row = (int64_t)(p.grouped ? part.pos : part.sample) * p.R + r;
   *reinterpret_cast<uint2*>(p.out + row * p.ld_out + ((int64_t)(part.head >> two) * p.group + ev) * D + 4 * sub) =
-      make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+      make_uint2(pack_bf16(to(o.x), to(o.y)), pack_bf16(to(o.z), to(o.w)));
 }
 
 template <int D, int NT, int WARPS, int DEPTH>
@@ -701,7 +746,7 @@ struct CacheWorkspace {
   size_t parts, list, warp_data, cta_data, total;
 };
 static CacheWorkspace carve(int D, int cols, int64_t B, int ctas) {
-  const size_t part = (size_t)(cols <= 8 ? 8 : 16) * (D + 2) * sizeof(float);
+  const size_t part = (size_t)(cols <= 8 ? 8 : 16) * (D + D / 64 + 1) * sizeof(float);
   CacheWorkspace w;
   w.parts = 0;
   w.list = w.parts + sizeof(CachePart) * (size_t)ctas;
