@@ -19,7 +19,8 @@
 // Operands are fp16 (11 bits, where bf16's 8 would double the output's error) and keep bf16's range by powers of two: a row of Q has one, which
 // goes into the scale of its scores; a tile has one for K, which goes there, too, and one for V, which the probabilities of its tokens
 // take up.  Everything of a row is in units of 2^g, g a reference that moves only when a probability with its power of two would
-// pass 2^15: then O is read, scaled and written back.
+// pass 2^15: then O is read, scaled and written back.  A tile's powers count what some row of the item sees or could see: tokens behind its last row and in front
+// of its first row's window are no part of it, those that single rows do not see are.
 // The eight elements of a code word come out in the order 0 4 1 5 2 6 3 7 (a mask each pair), so Q's and O's columns are in that order, too.
 // TMEM: 512 columns = two regions of 256: two buffers of S_h at 0 and 64, P_h over the first half of each, O_h from 128.  Every wait is bounded.
 #include "dsn_cache_line.cuh"
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
                  raw_full = base + 160, raw_empty = base + 176, raw_ready = base + 304, idle = base + 336, s_full = base + 192, p_full = base + 224, o_full = base + 256;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 288);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 292);
-  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there; tokens << 8; exponents that K and V are divided by << 16, << 24
+  uint32_t* s_raw = reinterpret_cast<uint32_t*>(smem + 296);                       // [2 slots]: bit b: block b is there; tokens in front of every row's window << 4; tokens << 8; exponents that K and V are divided by << 16, << 24
   uint8_t* s_bad = smem + 320;                                                     // [16 tiles]: bit b: block b is of a page outside the cache
   float2* s_fac = reinterpret_cast<float2*>(smem + 384);                           // [16 tiles]: K's power of two; V's, as its exponent
   uint64_t* s_scan = reinterpret_cast<uint64_t*>(smem + 640);
@@ -247,7 +248,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       const bool is_v = (unit & 4u) != 0;
       if (!warp_wait(raw_ready + 8 * (i & 1u), (i >> 1) & 1u, abort_flag, p.status, 82)) break;
       const uint32_t info = *reinterpret_cast<const volatile uint32_t*>(s_raw + (i & 1u));
-      const bool there = (info >> b & 1u) && b * 16u + (uint32_t)tok < (info >> 8 & 0xffu);
+      const uint32_t number = b * 16u + (uint32_t)tok;
+      const bool there = (info >> b & 1u) && number < (info >> 8 & 0xffu) && number >= (info >> 4 & 15u);
       const uint32_t slot = raw_at + (i & 1u) * kSlot, src = slot + b * kBlock + (is_v ? kBlock / 2 : 0u);
       uint32_t pair = there ? lds32(src + GR * 512u + (GR == 2 ? (uint32_t)part * 64u : 0u) + (uint32_t)tok * 4u) : 0u;
       // a token that is not finite shows in its scores; rows that do not see it must not meet it in V
@@ -301,12 +303,12 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     };
     // exponent of the largest element of the tile's K or V, held where 2^e and 2^-e are normal numbers; V's from 2^-50 up: fp32 holds the probabilities and
     // their sums without the power, too
-    auto exponent = [&](uint32_t slot, uint32_t go, uint32_t left, bool of_v) -> uint32_t {
+    auto exponent = [&](uint32_t slot, uint32_t go, uint32_t skip, uint32_t left, bool of_v) -> uint32_t {
       uint32_t e = 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int t = lane + 32 * i;
-        const bool there = (go >> (t >> 4) & 1u) && t < (int)left;
+        const bool there = (go >> (t >> 4) & 1u) && t >= (int)skip && t < (int)left;
 #pragma unroll
         for (int gr = 0; gr < GR; ++gr) {
           const uint32_t pr = lds32(slot + (uint32_t)(t >> 4) * kBlock + (of_v ? kBlock / 2 : 0u) + GR * 512 + gr * 64 + (t & 15) * 4);
@@ -333,6 +335,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
                       raw_full + 8 * slot);
       ++asked;
       const uint32_t left = (uint32_t)min(max(it.s.me1 + 1 - (it.s.lo + tile * kTile), 0), kTile);
+      // in front of the window of the item's first row: below 16, as tiles begin at its block
+      const uint32_t skip = (uint32_t)max(dsn_cache_first_seen(it.s.me0, p.window) - (it.s.lo + tile * kTile), 0);
       if (++tile == it.c1) {
         more = walk.next(p, it);
         tile = it.c0;
@@ -340,11 +344,11 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       find();
       // what the tile's K and V are divided by, from their pairs
       if (!warp_wait(raw_full + 8 * slot, (i >> 1) & 1u, abort_flag, p.status, 93)) break;
-      const uint32_t ke = exponent(raw_at + slot * kSlot, go, left, false), ve = exponent(raw_at + slot * kSlot, go, left, true);
+      const uint32_t ke = exponent(raw_at + slot * kSlot, go, skip, left, false), ve = exponent(raw_at + slot * kSlot, go, skip, left, true);
       if (lane == 0) {
         s_bad[i & 15u] = (uint8_t)bad;
         s_fac[i & 15u] = make_float2(__uint_as_float(ke << 23), (float)((int)ve - 127));
-        *reinterpret_cast<volatile uint32_t*>(s_raw + slot) = go | left << 8 | ke << 16 | ve << 24;
+        *reinterpret_cast<volatile uint32_t*>(s_raw + slot) = go | skip << 4 | left << 8 | ke << 16 | ve << 24;
         mbar_arrive(raw_ready + 8 * slot);
       }
       __syncwarp();

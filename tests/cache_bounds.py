@@ -41,7 +41,7 @@ def few_rows(pages, i, head, q, p, out, scale):
     top = np.abs(q).max(-1, keepdims=True)
     aq = np.abs(q).reshape(len(q), -1, 64).sum(-1)                                          # [n][groups]
     e = abs(scale) * (8 * 2.0 ** -23 * 1040 * aq @ ks[:, ::64].T + 2.0 ** -21 * top * np.abs(k).sum(-1))
-    move = _movement(scale * (q @ k.T), np.where(p > 0, e, 0.0))
+    move = _movement(np.where(p > 0, scale * (q @ k.T), 0.0), np.where(p > 0, e, 0.0))
     size = np.abs(vc) + np.abs(vz)
     unit = np.maximum(np.maximum(vs, np.abs(vz) * 2.0 ** -40), 2.0 ** -50)[:, ::64]         # [L][groups]
     unit = np.repeat((p[:, :, None] * unit[None]).max(1), 64, axis=-1) * 2.0 ** -6
@@ -54,8 +54,9 @@ def _greatest_nearby(x):
     return np.lib.stride_tricks.sliding_window_view(np.concatenate([pad, x, pad]), 127).max(-1)
 
 
-def many_rows(pages, i, head, q, p, out, scale):
-    """rows * group > 32: 64 tokens share a power of k and one of v, over all elements and whether a row sees them or not.
+def many_rows(pages, i, head, q, p, out, scale, first=0):
+    """rows * group > 32: 64 tokens share a power of k and one of v, over all elements and whether a row sees them or not, but for tokens before
+    `first`, which stand in front of the windows of all rows.
 
     Scores: queries as above, S16 of the largest element; a key's element is made in fp16 from its scale and middle, which are exact but for S16 of the tile's greatest,
     and rounded once.  Outputs: the same for values; probabilities are rounded to fp16, S16 of a unit that is up to 2^-7 of the greatest product of a weight
@@ -65,12 +66,13 @@ def many_rows(pages, i, head, q, p, out, scale):
     if L == 0:
         return np.full(out.shape, 1e-30)
     k = kc + kz
-    near = lambda z, s: 2 * np.maximum(_greatest_nearby((np.abs(z) + 8 * s).max(-1)), 2.0 ** -50)
+    counts = np.arange(L) >= first
+    near = lambda z, s: 2 * np.maximum(_greatest_nearby(np.where(counts, (np.abs(z) + 8 * s).max(-1), 0.0)), 2.0 ** -50)
     k_near, v_near = near(kz, ks), near(vz, vs)
     top = np.abs(q).max(-1, keepdims=True)
     a = np.abs(q)
     e = abs(scale) * (a @ (U16 * np.abs(k) + 10 * S16 * k_near[:, None]).T + 2 * S16 * top * np.abs(k).sum(-1) + 2.0 ** -18 * a @ np.abs(k).T)
-    move = _movement(scale * (q @ k.T), np.where(p > 0, e, 0.0))
+    move = _movement(np.where(p > 0, scale * (q @ k.T), 0.0), np.where(p > 0, e, 0.0))
     size = np.abs(vc) + np.abs(vz)
     p_near = np.stack([_greatest_nearby(row) for row in p])
     unit = (p_near * v_near).max(-1, keepdims=True) * 2.0 ** -7

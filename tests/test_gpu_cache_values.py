@@ -121,3 +121,37 @@ def test_many_rows_hold_what_64_tokens_share(dsn, D, R, group, apart):
     x, got, status = attend(dsn, g, pages, [2], group, [0] * 3, R, None)
     assert status[0] == 0
     check(pages, D, R, group, x, got, many_rows)
+
+
+@pytest.mark.parametrize("gain", [2.0 ** 12, 2.0 ** 22, 2.0 ** 60, 2.0 ** 100])
+@pytest.mark.parametrize("D,R,group", [(64, 150, 1), (128, 45, 3), (128, 64, 4), (64, 33, 1)])
+def test_many_rows_large_values_in_front_of_every_window(dsn, D, R, group, gain):
+    """Up to 256 query vectors: tokens that none of them sees, in the block in which the first row's window begins and in front of it."""
+    g = np.random.default_rng(D + R)
+    lengths, window = [2000, 700, 161, R + 12], 37
+    pages = Pages(g, lengths, 2, D, 16)
+    for i, L in enumerate(lengths):
+        first = L - R - window + 1
+        for t in range(max(0, first - 40), max(0, first)):
+            put(pages, i, t, slice(None), gain)
+            pg, at = pages.table[i, t // 16], t % 16
+            pages.s[pg, :, at, 0] *= gain                             # and their keys
+            pages.z[pg, :, at, 0] *= gain
+    x, got, status = attend(dsn, g, pages, [2], group, [0] * 4, R, None, window=window)
+    assert status[0] == 0
+    check(pages, D, R, group, x, got, lambda pg, i, *a: many_rows(pg, i, *a, first=max(0, lengths[i] - R - window + 1)), window=window)
+
+
+@pytest.mark.parametrize("gain", [2.0 ** 6, 2.0 ** 12])
+@pytest.mark.parametrize("D,R,group", MANY)
+def test_many_rows_larger_values_that_not_every_row_sees(dsn, D, R, group, gain):
+    """The last token of all, tokens in the middle of the rows, and tokens where a window begins."""
+    g = np.random.default_rng(D + R)
+    pages = Pages(g, [2000, 700, 160], 2, D, 16)
+    window = 90
+    for i, L in enumerate(pages.lengths):
+        for t in {L - 1, L - R // 2, L - R - 1, max(0, L - R - window + 10)}:
+            put(pages, i, t, slice(None), gain)
+    x, got, status = attend(dsn, g, pages, [2], group, [0] * 3, R, None, window=window)
+    assert status[0] == 0
+    check(pages, D, R, group, x, got, many_rows, window=window)
