@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
 #pragma unroll
           for (int o = 1; o < L; o <<= 1) e = max(e, __shfl_xor_sync(0xffffffffu, e, o));
           e >>= 7;
-          e = e == 255u ? 127u : min(max(e, 27u), 253u);    // a row that is not finite stays so
+          e = e == 255u ? e : min(max(e, 27u), 253u);
           const uint32_t given = __shfl_sync(0xffffffffu, e, (lane % PER) * L);
           if (lane / PER == b / PER + i) my_e = given;
           const float down = __uint_as_float((254u - e) << 23);
@@ -479,7 +479,8 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full + 8 * h);
-      return __uint_as_float(my_e << 23);
+      // NaN for a row that is not finite: an infinity alone could give all tokens scores of minus infinity, as if the row saw none
+      return my_e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(my_e << 23);
     };
     // the lines of this lane's row of Q on their way to the second level of cache
     auto warm_q = [&](const Item& x) {
@@ -532,7 +533,7 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
         const uint32_t bad = *reinterpret_cast<const volatile uint8_t*>(s_bad + nt);
         // scores to units of the exponent (not 0: what is hidden is -infinity), V's power of two
         const float2 fac = s_fac[nt];
-        const float t = fmaxf(cs * fac.x, 1e-37f), sh = fac.y;
+        const float t = max3_nan(cs * fac.x, 1e-37f, 1e-37f), sh = fac.y;
         uint32_t x[2][32];
         tmem_ld_32x32(at, x[0]);
         tmem_ld_32x32(at + 32, x[1]);
