@@ -508,9 +508,9 @@ size_t dsn_cache_bytes(const dsn_cache_desc* d);
 int dsn_cache_reset(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c, int32_t B, void* stream);
 
 /* Finds room for the new tokens of every request: new_tokens device [B], 0 .. R to append, -1 to end the request (its pages go back
- * to the pool, from which the next call can take them).  Requests are served in order: one that needs pages gets them if its need and that of all
- * requests before it, served or not, fits into the pool, and if its row of the table has room; else nothing of it is placed and DSN_ERR_CACHE_FULL is
- * recorded with its number.  A length or new_tokens value out of range counts as a request that changes nothing and records
+ * to the pool, from which the next call can take them).  Requests are served in order.  One whose row of the table has no room for its tokens is not
+ * served and asks the pool for nothing.  Any other that needs pages gets them if its need and that of all such requests before it, served or not, fits into the
+ * pool.  Of a request that is not served nothing is placed, and DSN_ERR_CACHE_FULL is recorded with its number.  A length or new_tokens value out of range counts as a request that changes nothing and records
  * DSN_ERR_BAD_INDEX.  Pages leave the ring from its front and return at its end, in the order of requests: the same call gives the same pages.
  * Reads lengths, table, pool, pool_state; writes the new entries of table, placed (rows placed, 0 for a request that ended), slots, the
  * returned entries of pool, and lengths and pool_state after the call to lengths_out [B] and pool_state_out [2] (NULL, or c's own: in place).
