@@ -13,7 +13,7 @@ def parts(pages, i, head, half):
     t = np.arange(pages.lengths[i])
     pg, at = pages.table[i, t // pages.page], t % pages.page
     s, z = (np.repeat(a[pg, head, at, half], 64, axis=-1) for a in (pages.s, pages.z))
-    code = pages.code[pg, head, at, half].reshape(len(t), -1).astype(np.float64)
+    code = pages.code[pg, head, at, half].reshape(len(t), pages.D).astype(np.float64)
     return s * (code - 8), z, s
 
 
@@ -35,7 +35,7 @@ def few_rows(pages, i, head, q, p, out, scale):
     All sums in fp32: 2^-12 of the terms' sizes."""
     (kc, kz, ks), (vc, vz, vs) = (parts(pages, i, head, half) for half in range(2))
     L, D = kc.shape
-    if L == 0:
+    if L == 0 or len(q) == 0:
         return np.full(out.shape, 1e-30)
     k = kc + kz
     top = np.abs(q).max(-1, keepdims=True)
@@ -63,7 +63,7 @@ def many_rows(pages, i, head, q, p, out, scale, first=0):
     and a value within a tile."""
     (kc, kz, ks), (vc, vz, vs) = (parts(pages, i, head, half) for half in range(2))
     L, D = kc.shape
-    if L == 0:
+    if L == 0 or len(q) == 0:
         return np.full(out.shape, 1e-30)
     k = kc + kz
     counts = np.arange(L) >= first
@@ -77,3 +77,23 @@ def many_rows(pages, i, head, q, p, out, scale, first=0):
     p_near = np.stack([_greatest_nearby(row) for row in p])
     unit = (p_near * v_near).max(-1, keepdims=True) * 2.0 ** -7
     return U * np.abs(out) + (2 * U16 + 2.0 ** -12 + move) * (p @ size) + 10 * S16 * (p @ v_near)[:, None] + L * 2 * S16 * unit + 1e-30
+
+
+# Bounds of every element have to take each rounding at its worst.  What operands are really held in shows in the share of outputs that are not the formula's own
+# rounding to bf16: an error e before that rounding changes it with probability e / step.  With operands of 11 bits and weights over tens to thousands of
+# tokens that share is 3 to 7 % (few rows: probabilities are rounded) and 5 to 12 % (many rows: keys and values, too); with 8 bits it is eight times the error, 15 to 35 and 35 to
+# 59 %.  test_cache_bounds_host.py has both, made from the definition of those roundings.
+FEW_SHARE, MANY_SHARE = 0.12, 0.25
+
+
+def share_off(got, ref):
+    from oracle import dsn_oracle as O
+    return float(np.mean(got != O.round_bf16(ref)))
+
+
+def relative(got, ref):
+    """Norm of the difference over the norm: 2^-8 / sqrt(3 E[m^2]) for roundings of mantissas m in 1 .. 2 alone, about 2^-9.3."""
+    return float(np.sqrt(((got - ref) ** 2).sum() / (ref ** 2).sum()))
+
+
+RELATIVE = 2.0 ** -9
