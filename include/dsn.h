@@ -527,7 +527,7 @@ int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c
 /* out = softmax(scale * q k^T) v over the cached tokens that a row's query sees: row j of request i is token n = lengths[i] - placed[i] + j of
  * it (its keys are in the cache already) and sees tokens max(0, n - window + 1) .. n.  Softmax and sums in fp32; the operands of both products are rounded to
  * 11 bits (fp16 behind powers of two: q and k, a probability or its product with v's scale, v).  With R * group <= 32 magnitudes of v from 1e-15 to 1e34 in a
- * cache keep them, whatever other groups of 64 elements, other tokens or tokens that a row does not see hold.  With R * group > 32, 64
+ * cache keep them, whatever other groups of 64 elements, other tokens or tokens that a row does not see hold (above 1e30 weights below 2^-20 of a row's greatest can be lost).  With R * group > 32, 64
  * tokens in a row share a power of k and one of v over all their elements, seen by a row or not (up to 256 query vectors of a head go together: what lies in front
  * of the window of them all does not count).  With w and a the greatest weight of a row and the greatest magnitude of v among 64 tokens in a row, an
  * output is off by up to 2^-20 of the mean of a under the weights and 2^-30 of the largest w a for each token that the row can see, beside those 11 bits; a score by

@@ -231,7 +231,8 @@ constexpr int kWriteWarps = 4, kWriteCtas = 28;   // warps a CTA; CTAs an SM at 
 // `split`th piece of it where there are few rows, four pieces on their way at a time.
 // Bound by instructions once memory is busy: least and greatest value go through the shuffles as one pair of bf16 numbers (the least, minus the greatest);
 // a code comes out of an addition that rounds (1.5 * 2^23 + 8: its low four bits are the code), eight of them are put together by multiply-adds.
-// Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 22.3 us, 4 x 4096 rows of 8 heads of 128 with values 31.6 (floors 10.6 and 23.3 at a copy's rate); one row 2.2.
+// Measured (in a graph): 128 x 197 rows of 12 heads of 64 by path 22.3 us, 4 x 4096 rows of 8 heads of 128 with values 31.6 (floors 10.6 and 23.3 at a copy's rate); without values 19.9 and
+// 26.9 (6.0 and 13.1: look-ups and arithmetic stay the same); one row 2.2.
 template <int D, bool VALUES>
 __global__ void __launch_bounds__(kWriteWarps * 32) cache_write_kernel(const __grid_constant__ CacheWriteParams p) {
   constexpr int LPH = D / 4;             // lanes a head

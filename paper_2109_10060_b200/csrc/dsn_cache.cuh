@@ -90,7 +90,7 @@ struct CacheAttParams {
 };
 #define DSN_CACHE_MAX_CTAS 148   // a B200's SMs: the workspace query has no context to ask
 // Query vectors of a head (rows * group) up to which the form for a few of them runs.  It reads the cache once for every 16, the many-rows form turns it into
-// fp16 tiles once for 256: 64 requests of up to 8192 tokens, 8 heads of 128: 119 us for 8, 179 for 16, 442 in the many-rows form for 20 and 460 for 64.
+// fp16 tiles once for 256: 64 requests of up to 8192 tokens, 8 heads of 128: 121 us for 8, 185 for 16, 340 for 20 (442 in the many-rows form), 463 in that form for 64.
 #define DSN_CACHE_FEW 32
 size_t dsn_cache_attention_ws_bytes(int D, int cols, int64_t B);
 cudaError_t dsn_launch_cache_attention(CacheAttParams& p, int D, int sm_count, void* workspace, cudaStream_t s);

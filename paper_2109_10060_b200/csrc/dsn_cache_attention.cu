@@ -5,17 +5,19 @@
 // long requests nor many short ones leave SMs idle.  A warp keeps the steps to come in flight as bulk copies into a ring of its own (no barrier with
 // other warps), a block of 16 tokens a copy, as pages may end after any block.
 // Measured (in a graph): 64 requests of up to 8192 tokens, 8 heads of 128, 4 queries a head: 122 us, 3.8 TB/s (118 with one
-// reference a query, which lost what lay 2^20 below the largest scale of a step); a copy's rate would allow 70 us.  What bounds it is the
-// arithmetic on the codes, some 700 instructions a step and warp at 12 warps of 168 registers an SM (58 % of the issue slots, the rest is their latency); no other
-// split was faster: 16 and 14 warps spill (132, 148 us), 8 hide less (144).  One token of one request takes 9.0 us: the look-ups in a row of request, page and
-// blocks, the join in shared memory and the joining kernel, not the bytes.
+// reference a query, behind which fp16 loses what lies 2^20 below the largest scale of a step); a copy's rate would allow 70 us.  What bounds it is the
+// arithmetic on the codes, some 720 instructions a step and warp at 12 warps of 168 registers an SM (58 % of the issue slots, the rest is their latency); no other
+// split was faster: 16 and 14 warps spill (132, 148 us where 12 took 128), 8 hide less (144).  One token of one request takes 9.1 us: the look-ups in a row of
+// request, page and blocks, the join in shared memory and the joining kernel, not the bytes.
 // An item that lies in one warp's stretch is finished there.  What the warps of a CTA cut among themselves they join in shared memory; of an item that is
 // cut between CTAs, each leaves its reference, sum and products (fp32) in the workspace, and a second small kernel joins them.
 //
 // Products on the tensor cores, with the tokens as rows: S^T = K Q^T (16 tokens x 8 queries x 16 elements an instruction), O^T = V^T P^T, fp16 operands.
 //   Codes become fp16 numbers with one mask each: 1024 + code, or 1024 + 16 code from the high half of a byte.  For K the offsets are taken off by
 //   starting the accumulator at minus their product with the query (and the 16 by a sixteenth in the query), which costs nothing; scale and
-//   middle of a token's group are applied to the sum in fp32, so the scores are nearly as exact as fp32 sums (the offset costs 2^-24 of 1024 |q|).
+//   middle of a token's group are applied to the sum in fp32.  (An fp16 number from 1024 on counts in ones: the usual way to turn small integers into
+//   floating point by placing their bits in its fraction.)  Queries keep their 8 bits; but a sum that starts at 1032 times the query's elements is rounded
+//   at that size, 2^-23 of it a product, which comes to some 1e-4 of a score: about what operands of 11 bits cost.
 //   For V the offset is subtracted (a sum over thousands of tokens would lose bits to it), the scale goes into the probability before its
 //   one rounding to fp16, the middle into a sum of its own in fp32.
 // The order of elements in a product is free, so a lane takes whole words: 16 elements of K in 8 bytes, 8 elements of V in 4.  Row i of a block's K is token
@@ -737,7 +739,7 @@ cudaError_t launch(const CacheAttParams& p, int ctas, cudaStream_t s) {
   return dsn_launch(cache_join_kernel<D>, dim3((unsigned)ctas, (unsigned)(p.R * p.group < 8 * NT ? p.R * p.group : 8 * NT)), dim3(2 * D), 0, s, 1, p, ctas, 8 * NT);
 }
 
-constexpr int kWarps1 = 12, kWarps2 = 8;   // warps a CTA for up to 8 and up to 16 query vectors a head: their products stay in registers (16 and 8 warps: 132 and 144 us, 12: 128)
+constexpr int kWarps1 = 12, kWarps2 = 8;   // warps a CTA for up to 8 and up to 16 query vectors a head: their products stay in registers (16 and 8 warps: 132 and 144 us where 12 took 128)
 
 }  // namespace
 

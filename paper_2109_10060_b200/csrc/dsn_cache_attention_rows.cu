@@ -3,10 +3,11 @@
 // One item = (request, head, 256 query vectors in a row: two halves of 128 TMEM lanes), walked along its tokens in tiles of 64; the tiles of all items
 // stand in one line, of which every CTA (one an SM) gets an equal stretch.  An item that is cut leaves references, sums and products of its
 // rows (fp32) in the workspace, and a second kernel joins them.
-// Measured (in a graph): 2 requests of 4096 rows behind nothing, 8 heads of 128, 4 queries a head: 482 us, 570 TFLOP/s of the visible pairs, where products at a
-// plain matrix product's rate would take 170.  What bounds it is the softmax: some 3,000 cycles a tile of 64 tokens and warp, half of them the exponentials (16
-// cycles an instruction of a warp), the rest the trip through TMEM; eight warps of 128 registers are all that fit, and the tensor pipe is busy a quarter of the time.
-// Tried: 128 tokens a tile with one S buffer 491 us, two threads a row 709, more registers for the softmax warps 507 to 550, a part of the exponentials as
+// Measured (in a graph): 2 requests of 4096 rows behind nothing, 8 heads of 128, 4 queries a head: 484 us, 570 TFLOP/s of the visible pairs, where products at a
+// plain matrix product's rate would take 170.  What bounds it is the chain of a tile in the softmax: some 2,900 cycles for 64 tokens, while the exponentials of its 256
+// rows need 1,024 (16 a cycle) and its products as many.  Load from TMEM, maximum, exponentials and store follow one another in a warp, eight warps of 128
+// registers are all that fit, and the tensor pipe is busy 35 % of the time (26 % for 2 x 512 rows behind up to 9999 tokens, 70 us).
+// Tried: 128 tokens a tile with one S buffer 491 us, two threads a row 709, more registers for the softmax warps 507 to 550 (where this form took 476 to 485), a part of the exponentials as
 // polynomials within 3 %.
 // Roles (512 threads):
 //   warps 0-4    values: K and V tiles of fp16 in shared memory, swizzled as the products read them, four buffers each.  A unit is K or V of a block of 16
