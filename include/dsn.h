@@ -258,7 +258,7 @@ typedef struct dsn_rotary_desc {
  * Rows of a call lie as everywhere, [B][R][ld]; request i has rows 0 .. placed[i] - 1 of its R, the rest is padding that is neither
  * read nor written.  A row of qkv holds H heads of group + 2 vectors of D_h elements, [head][q x group | k | v][D_h]: group = 1 is the
  * layout of the sliced attention core, larger groups share a head's keys and values among their queries (dsn_rotary_axes turns rows of
- * group <= 6).  A row of the output holds [head][group][D_h].  Heads >= heads[t] of a request of path t are neither read nor written.
+ * group <= 6 in a call, wider ones head by head, up to eight vectors a call).  A row of the output holds [head][group][D_h].  Heads >= heads[t] of a request of path t are neither read nor written.
  *
  * Pages: [n_pages][H][page / 16] blocks of 16 tokens.  A block holds the keys, then the values, each as
  *   codes [D_h / 64][16][32 bytes]   64 elements a token, element 2 j in the low half of byte j, 2 j + 1 in the high half
