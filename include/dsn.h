@@ -532,7 +532,8 @@ int dsn_cache_write_q4(dsn_ctx* ctx, const dsn_cache_desc* d, const dsn_cache* c
  * of the window of them all does not count).  With w and a the greatest weight of a row and the greatest magnitude of v among 64 tokens in a row, an
  * output is off by up to 2^-20 of the mean of a under the weights and 2^-30 of the largest w a for each token that the row can see, beside those 11 bits; a score by
  * 2^-20 of the one that the greatest magnitude of k among the 64 would give.
- * A row that sees nothing (n < 0) comes out as zeros, one whose query holds a NaN or an infinity as NaN; a score, times log2(e), has to lie within fp32's range.  Uses pages, table, lengths, and placed (NULL: R rows of every request).  A length or
+ * A row that sees nothing (n < 0) comes out as zeros, any other whose query holds a NaN or an infinity as NaN; a score, times log2(e), has to lie
+ * within fp32's range.  Uses pages, table, lengths, and placed (NULL: R rows of every request).  A length or
  * placed value out of range is held at the nearest end of it, tokens of a page outside the cache are left out, and both record DSN_ERR_BAD_INDEX.
  * out overlaps nothing else.  workspace: device, 16-byte aligned, of dsn_cache_attention_q4_workspace_bytes; nothing in it has to start at
  * zero.  It must not be used by two calls at once. */

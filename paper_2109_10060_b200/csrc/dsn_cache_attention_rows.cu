@@ -440,12 +440,12 @@ __global__ void __launch_bounds__(kThreadsR, 1) cache_rows_kernel(const __grid_c
     uint32_t m = 0, n = 0;   // tiles of the half, of both
     bool ok = true;
     // The warp's rows of Q as fp16, the largest element of each brought to 1 .. 2; returns the power of two that goes into the scores of this lane's row.
-    // D / 8 lanes read a row.
+    // D / 8 lanes read a row; one in front of the first token sees nothing, whatever it holds.
     auto load_q = [&](const Item& x) -> float {
       constexpr int L = D / 8, PER = 32 / L, NB = 8;   // lanes a row, rows a load, loads at once
       const int v = x.s.v0 + 128 * h + row;
       const int r = (int)dsn_div((uint32_t)v, p.by_group), ev = v - r * p.group;
-      const long long mine = v < x.s.v1 ? ((long long)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((long long)x.head * (p.group + 2) + ev) * D
+      const long long mine = v < x.s.v1 && x.e.len - x.e.rows + r >= 0 ? ((long long)(p.grouped ? x.e.pos : x.e.sample) * p.R + r) * p.ld_qkv + ((long long)x.head * (p.group + 2) + ev) * D
                                         : -1;
       const int sub = lane % L, of = lane / L;
       uint32_t my_e = 127u;

@@ -37,3 +37,21 @@ def test_rows_that_are_not_finite(dsn, bad, scale, D, R, group):
     assert np.all(np.isfinite(got[~touched]))
     if R * group > 32:
         assert np.array_equal(got[~touched], whole[~touched])
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("D,R,group", [(64, 8, 1), (128, 7, 4), (64, 60, 1), (128, 150, 2)])
+def test_rows_that_see_nothing_are_zero_whatever_they_hold(dsn, bad, D, R, group):
+    """Rows in front of a request's first token, some beside rows that see tokens."""
+    g = np.random.default_rng(D + R)
+    lengths = [0, 1, R - 2, 3]
+    pages = Pages(g, lengths, 2, D, 16)
+    q = O.round_bf16(g.normal(size=(4, R, 2, group, D)))
+    for i, L in enumerate(lengths):
+        q[i, :R - L, :, :, ::3] = bad
+    x, got, status = attend(dsn, g, pages, [2], group, [0] * 4, R, None, q=q)
+    assert status[0] == 0
+    for i, L in enumerate(lengths):
+        assert np.all(got[i, :R - L] == 0)
+        q[i, :R - L] = 0.0
+    compare(pages, [2], group, [0] * 4, R, None, q, got)
